@@ -1,5 +1,6 @@
 /*
- * pcomoe.h - C ABI of the path-composed MoE FFN layer for NVIDIA B200 (sm_100a).
+ * pcomoe.h - C ABI of the path-composed MoE FFN layer for NVIDIA B200 (sm_100a), and of what serves a model around it:
+ * attention over prompts and over a paged cache, the cache's page operations, token scores.
  *
  * The layer (PCoMoE, Sec. 4): every SwiGLU expert e is split into an expansion-side
  * operator U_e(h) = SiLU(W_gate h) (.) (W_up h) and a projection-side operator
@@ -39,7 +40,8 @@ typedef enum {
   PCOMOE_ERR_UNSUPPORTED = 4, /* a size or dtype combination no kernel covers                     */
   PCOMOE_ERR_CUDA = 5,        /* a CUDA runtime / driver call failed                              */
   PCOMOE_ERR_TIMEOUT = 6,     /* device: a bounded wait inside a kernel ran out                   */
-  PCOMOE_ERR_INDEX = 7        /* device: an expert / row index was out of range                   */
+  PCOMOE_ERR_INDEX = 7,       /* device: an expert / row / sequence / page index was out of range */
+  PCOMOE_ERR_CACHE_FULL = 8   /* device: a cache had too few free pages; nothing was changed      */
 } pcomoe_status;
 
 typedef enum { PCOMOE_BF16 = 0, PCOMOE_FP32 = 1 } pcomoe_dtype;
@@ -332,9 +334,147 @@ pcomoe_status pcomoe_router_logits(const pcomoe_layer *layer, int32_t T, const v
 pcomoe_status pcomoe_residual_cast(const pcomoe_layer *layer, int32_t T, const void *d_h_in, const float *d_y,
                                    void *d_h_out, void *stream);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * What stands around the layer when a model is served: attention over packed prompts, a paged cache of keys and values
+ * with its page operations, attention of new or drafted tokens over that cache, and scores of tokens from logits.
+ * (The paper evaluates whole models and writes out none of these.)  Types are the layer's: bf16 or fp32.
+ * --------------------------------------------------------------------------------------------------------------- */
+
+/* Plain data; set struct_size = sizeof(pcomoe_attn_config).  Query head h reads kv head h / (q_heads / kv_heads). */
+typedef struct {
+  int32_t struct_size;
+  int32_t q_heads;      /* Hq, a multiple of kv_heads                                         */
+  int32_t kv_heads;     /* Hkv                                                                */
+  int32_t head_dim;     /* D: 64 or 128                                                       */
+  int32_t dtype;        /* pcomoe_dtype of q, k, v and the output                             */
+  float scale;          /* scores are scale * q.k; finite                                     */
+} pcomoe_attn_config;
+
+/* Bytes of device workspace of the two attention calls.  256-byte aligned; its first PCOMOE_ATTN_ZERO_BYTES must be zero
+ * before its first use (status words and counters; the calls leave the counters at zero), the rest may hold anything,
+ * and one call at a time may use it.  The size depends on the GPU, not on the batch.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED (head_dim), CUDA. */
+#define PCOMOE_ATTN_ZERO_BYTES (256u + 4u * 4096u)
+pcomoe_status pcomoe_attn_workspace_bytes(const pcomoe_attn_config *cfg, size_t *bytes);
+
+/*
+ * Attention over whole prompts: causal, grouped heads, sequences of any lengths (zero among them) packed one after
+ * another.  Sequence s owns the rows [cu_len[s], cu_len[s+1]) of the packed arrays, and its row t sees rows 0..t:
+ *     o_t = sum_{p <= t} a_p v_p / sum_p a_p,   a_p = exp(scale * q_t.k_p);      lse_t = log sum_p a_p.
+ *   d_cu_len [n_seqs+1] int32, device, ascending, d_cu_len[0] = 0, d_cu_len[n_seqs] <= T (rows past it are not written)
+ *   d_q [T,Hq,D], d_k, d_v [T,Hkv,D], d_out [T,Hq,D] in cfg->dtype: a row's heads are contiguous, rows are *_stride
+ *   ELEMENTS apart (column ranges of one fused projection output are fine)
+ *   d_lse [T,Hq] fp32 or NULL.
+ * A value that no row sees (another sequence's, a later row's) never reaches a result, NaN and infinities included.
+ * bf16: tensor cores, scores, maxima, sums and outputs accumulated in fp32, the weights a_p rounded to bf16 before they
+ * meet v, the result rounded once.  fp32: plain FMA kernels.
+ * Bits do not change from call to call.  Asynchronous on `stream`, allocates nothing.
+ * Errors: INVALID_ARG (NULL, n_seqs <= 0 with T > 0, stride below a row, bad config), SHAPE (T < 0), UNSUPPORTED
+ * (head_dim; base or stride not a multiple of 16 bytes), WORKSPACE, CUDA.  Device: INDEX (d_cu_len not ascending or past
+ * T: the offending sequences are skipped), TIMEOUT.
+ */
+pcomoe_status pcomoe_attn_prompt(const pcomoe_attn_config *cfg, int32_t T, int32_t n_seqs, const int32_t *d_cu_len,
+                                 const void *d_q, int64_t q_stride, const void *d_k, int64_t k_stride, const void *d_v,
+                                 int64_t v_stride, void *d_out, int64_t out_stride, float *d_lse, void *d_workspace,
+                                 size_t ws_bytes, void *stream);
+
+/*
+ * A paged cache of keys and values, all arrays owned by the caller.  Set struct_size = sizeof(pcomoe_cache).
+ * Position p of sequence s lies in row p % page_size of page page_table[s][p / page_size], the same page in every layer.
+ * A page belongs to page_ref sequences and is free iff that is 0.  To start: seq_len and page_ref zero, page_table -1.
+ */
+typedef struct {
+  int32_t struct_size;
+  int32_t layers, pages;  /* pages <= 2^18                                                        */
+  int32_t page_size;      /* tokens: 16, 32, 64 or 128                                            */
+  int32_t kv_heads, head_dim, dtype;
+  int32_t max_seqs;       /* <= 4096                                                              */
+  int32_t max_pages;      /* page table entries of a sequence                                     */
+  void *d_k, *d_v;        /* [layers, pages, kv_heads, page_size, head_dim], 16-byte aligned      */
+  int32_t *d_seq_len;     /* [max_seqs]                                                           */
+  int32_t *d_page_ref;    /* [pages]                                                              */
+  int32_t *d_page_table;  /* [max_seqs, max_pages], -1 = no page                                  */
+} pcomoe_cache;
+
+/* Bytes of device workspace of the cache calls (256-byte aligned, first 256 bytes zero before the first use, one call at
+ * a time).  Errors of every cache call: INVALID_ARG (NULL, bad sizes or enum, n < 0), UNSUPPORTED (page_size; a row of a
+ * head not a multiple of 16 bytes; misaligned pools), SHAPE (max_seqs, pages, or more sequences in a call than max_seqs),
+ * WORKSPACE, CUDA.  All work on the device and are asynchronous; sequence lists are device arrays [n] without repeats. */
+pcomoe_status pcomoe_cache_workspace_bytes(const pcomoe_cache *cache, size_t *bytes);
+
+/* Room for d_add[i] >= 0 more tokens in sequence d_seqs[i]: seq_len grows, pages are added, and a partly filled last page
+ * that is shared is copied first (in every layer), so that the new rows belong to this sequence alone; of several
+ * sharers in one call the earlier ones copy and the last may keep the page.  Pages are the lowest free ids in call order
+ * (a sequence's copy before its new pages), so the result is unique.
+ * Device errors, each leaving everything unchanged: INDEX (sequence out of range or repeated, d_add < 0, more than
+ * max_pages pages), CACHE_FULL. */
+pcomoe_status pcomoe_cache_reserve(const pcomoe_cache *cache, int32_t n, const int32_t *d_seqs, const int32_t *d_add,
+                                   void *d_workspace, size_t ws_bytes, void *stream);
+
+/* Rows into the cache: the last d_cu_len[i+1] - d_cu_len[i] positions of sequence d_seqs[i] receive the packed rows
+ * [d_cu_len[i], d_cu_len[i+1]) of d_k and d_v [n_layers, T, kv_heads, head_dim] (rows `row_stride` and layers
+ * `layer_stride` elements apart, for both), into the layers first_layer .. first_layer + n_layers - 1.
+ * Device: INDEX (no such position, or its page is shared: that row is not written). */
+pcomoe_status pcomoe_cache_write(const pcomoe_cache *cache, int32_t first_layer, int32_t n_layers, int32_t T, int32_t n,
+                                 const int32_t *d_seqs, const int32_t *d_cu_len, const void *d_k, const void *d_v,
+                                 int64_t row_stride, int64_t layer_stride, void *d_workspace, size_t ws_bytes,
+                                 void *stream);
+
+/* Sequence d_child[i] (empty) becomes a copy of d_parent[i] that shares its pages.  No data moves.
+ * Device: INDEX (out of range, child not empty, a child named twice or also a parent: those pairs are skipped). */
+pcomoe_status pcomoe_cache_fork(const pcomoe_cache *cache, int32_t n, const int32_t *d_parent, const int32_t *d_child,
+                                void *d_workspace, size_t ws_bytes, void *stream);
+
+/* After drafted tokens were checked: of the last d_cu_len[i+1] - d_cu_len[i] positions of sequence d_seqs[i] those with the
+ * numbers d_keep[i][0 .. d_n_keep[i]) (strictly ascending, counted from the first of them) are moved up behind the
+ * context, in every layer; the others are dropped and their pages freed.  d_keep [n, keep_stride] int32.
+ * Device: INDEX (numbers out of range or not ascending, a row to be written in a shared page, a repeated sequence: that
+ * sequence stays as it is). */
+pcomoe_status pcomoe_cache_keep(const pcomoe_cache *cache, int32_t n, const int32_t *d_seqs, const int32_t *d_cu_len,
+                                const int32_t *d_keep, int32_t keep_stride, const int32_t *d_n_keep, void *d_workspace,
+                                size_t ws_bytes, void *stream);
+
+/* Shortens sequence d_seqs[i] to d_len[i] tokens (0 frees it); pages that nobody holds any more are free.
+ * Device: INDEX (out of range, d_len above the length or below 0, a repeated sequence: those are skipped). */
+pcomoe_status pcomoe_cache_trim(const pcomoe_cache *cache, int32_t n, const int32_t *d_seqs, const int32_t *d_len,
+                                void *d_workspace, size_t ws_bytes, void *stream);
+
+/* Moves the pages in use to the lowest ids: with U pages in use, those at U and above go, in order, to the free ones
+ * below U (in every layer), and every page table and reference count follows. */
+pcomoe_status pcomoe_cache_compact(const pcomoe_cache *cache, void *d_workspace, size_t ws_bytes, void *stream);
+
+/*
+ * Attention of new tokens over the cache.  The last n_i = d_cu_len[i+1] - d_cu_len[i] cached positions of sequence
+ * d_seqs[i] are the packed query rows' own (reserve and write them first).  Row j of them sees every position before
+ * those, and of those the ones its mask names: bit m % 32 of word m / 32 of d_tree_mask [T, mask_words] for the m-th
+ * (bits from n_i on are ignored).  d_tree_mask = NULL: the rows are a chain and row j sees m <= j; one row per sequence
+ * is a decode step.  A row that sees nothing gets o = 0 and lse = -inf.
+ * d_seqs may name a sequence more than once.  Formula, arrays, types, bits and errors as in pcomoe_attn_prompt; also
+ * INVALID_ARG (cache and config disagree, layer out of range), SHAPE (mask_words < 0 or > 8).  Device: INDEX (sequence
+ * or page out of range, more query rows than cached positions or than 32 * mask_words: o = 0, lse = -inf there).
+ */
+pcomoe_status pcomoe_attn_cached(const pcomoe_attn_config *cfg, const pcomoe_cache *cache, int32_t layer, int32_t T,
+                                 int32_t n_seqs, const int32_t *d_seqs, const int32_t *d_cu_len, const void *d_q,
+                                 int64_t q_stride, const uint32_t *d_tree_mask, int32_t mask_words, void *d_out,
+                                 int64_t out_stride, float *d_lse, void *d_workspace, size_t ws_bytes, void *stream);
+
+/*
+ * Scores of tokens from logits, one read of them.  For row t with logits x: logZ = log sum exp(x),
+ *     d_logprob[t] = x[d_tokens[t]] - logZ,     d_entropy[t] = logZ - sum p x,  p = exp(x - logZ),
+ * and the top_n best words by (logit descending, id ascending) with their log probabilities.
+ * A logit that is NaN or infinite is not eligible (the rule for routing scores): probability 0, log probability -inf.
+ * Ranks that cannot be filled get id -1 and -inf; a row with nothing eligible has entropy 0.
+ *   d_logits [T,V] in `dtype`, rows row_stride elements apart (any alignment);
+ *   d_tokens [T] int32 or NULL (then d_logprob may be NULL): an id < 0 stands for no token and scores 0, one >= V gives NaN;
+ *   d_entropy [T] fp32 or NULL; d_top_ids [T,top_n] int32, d_top_logprob [T,top_n] fp32, 0 <= top_n <= 32.
+ * Errors: INVALID_ARG, SHAPE (T < 0, V <= 0, top_n out of range), UNSUPPORTED (V > 2^20), CUDA. */
+pcomoe_status pcomoe_token_logprobs(int32_t dtype, int32_t T, int32_t V, const void *d_logits, int64_t row_stride,
+                                    const int32_t *d_tokens, int32_t top_n, float *d_logprob, float *d_entropy,
+                                    int32_t *d_top_ids, float *d_top_logprob, void *stream);
+
 /* Synchronises `stream`, reads the workspace's status words and returns the first error a kernel
  * recorded (PCOMOE_OK if none): the layer's word is cleared by the next pcomoe_build_path_groups, the
- * router's by this call once it has been read. */
+ * router's by this call once it has been read.  A workspace of the attention or cache calls has one word, kept like the
+ * router's. */
 pcomoe_status pcomoe_device_status(const void *d_workspace, void *stream);
 
 /* Failure detection on the device.  Every wait of the tensor-core kernels (on an mbarrier that a TMA copy, an MMA

@@ -16,8 +16,10 @@ LIB_PATH = os.path.join(_PKG, "libpcomoe.so")
 
 PCOMOE_OK = 0
 STATUS_NAMES = {0: "OK", 1: "ERR_INVALID_ARG", 2: "ERR_SHAPE", 3: "ERR_WORKSPACE", 4: "ERR_UNSUPPORTED",
-                5: "ERR_CUDA", 6: "ERR_TIMEOUT", 7: "ERR_INDEX"}
+                5: "ERR_CUDA", 6: "ERR_TIMEOUT", 7: "ERR_INDEX",
+                8: "ERR_CACHE_FULL"}
 PCOMOE_BF16, PCOMOE_FP32 = 0, 1
+PCOMOE_ATTN_ZERO_BYTES = 256 + 4 * 4096
 PCOMOE_FFN_AUTO, PCOMOE_FFN_SIMT, PCOMOE_FFN_TCGEN05, PCOMOE_FFN_TCGEN05_PAIR = 0, 1, 2, 3
 
 EXPORTS = ["pcomoe_mask_from_bias", "pcomoe_mask_tighten", "pcomoe_layer_create", "pcomoe_layer_destroy", "pcomoe_layer_active_set", "pcomoe_workspace_bytes",
@@ -25,6 +27,9 @@ EXPORTS = ["pcomoe_mask_from_bias", "pcomoe_mask_tighten", "pcomoe_layer_create"
            "pcomoe_ffn_forward_stages", "pcomoe_layer_forward", "pcomoe_router_logits", "pcomoe_residual_cast",
            "pcomoe_host_pipe_create", "pcomoe_host_pipe_submit", "pcomoe_host_pipe_wait", "pcomoe_host_pipe_arrays",
            "pcomoe_host_pipe_destroy",
+           "pcomoe_attn_workspace_bytes", "pcomoe_attn_prompt", "pcomoe_attn_cached", "pcomoe_cache_workspace_bytes",
+           "pcomoe_cache_reserve", "pcomoe_cache_write", "pcomoe_cache_fork", "pcomoe_cache_keep", "pcomoe_cache_trim",
+           "pcomoe_cache_compact", "pcomoe_token_logprobs",
            "pcomoe_device_status", "pcomoe_set_wait_limit_us", "pcomoe_selftest_wait_timeout",
            "pcomoe_launch_count", "pcomoe_status_string"]
 
@@ -46,6 +51,17 @@ class pcomoe_config(ctypes.Structure):
 class pcomoe_groups(ctypes.Structure):
     _fields_ = [(k, ctypes.c_void_p) for k in ("s1_offsets", "s1_token", "path_s1row", "s2_offsets", "s2_path",
                                                 "s2_s1row", "s2_token", "s2_w", "stats")]
+
+
+class pcomoe_attn_config(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class pcomoe_cache(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("struct_size", "layers", "pages", "page_size", "kv_heads", "head_dim", "dtype",
+                                               "max_seqs", "max_pages")] + \
+               [(k, ctypes.c_void_p) for k in ("d_k", "d_v", "d_seq_len", "d_page_ref", "d_page_table")]
 
 
 _lib = None
@@ -84,6 +100,18 @@ def load_library(path: str | None = None):
     lib.pcomoe_host_pipe_destroy.argtypes = [vp]
     lib.pcomoe_set_wait_limit_us.argtypes = [ctypes.c_uint32]
     lib.pcomoe_selftest_wait_timeout.argtypes = [vp, vp]
+    i64, pc, pa = ctypes.c_int64, ctypes.POINTER(pcomoe_cache), ctypes.POINTER(pcomoe_attn_config)
+    lib.pcomoe_attn_workspace_bytes.argtypes = [pa, ctypes.POINTER(sz)]
+    lib.pcomoe_attn_prompt.argtypes = [pa, i32, i32, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, sz, vp]
+    lib.pcomoe_attn_cached.argtypes = [pa, pc, i32, i32, i32, vp, vp, vp, i64, vp, i32, vp, i64, vp, vp, sz, vp]
+    lib.pcomoe_cache_workspace_bytes.argtypes = [pc, ctypes.POINTER(sz)]
+    lib.pcomoe_cache_reserve.argtypes = [pc, i32, vp, vp, vp, sz, vp]
+    lib.pcomoe_cache_write.argtypes = [pc, i32, i32, i32, i32, vp, vp, vp, vp, i64, i64, vp, sz, vp]
+    lib.pcomoe_cache_fork.argtypes = [pc, i32, vp, vp, vp, sz, vp]
+    lib.pcomoe_cache_keep.argtypes = [pc, i32, vp, vp, vp, i32, vp, vp, sz, vp]
+    lib.pcomoe_cache_trim.argtypes = [pc, i32, vp, vp, vp, sz, vp]
+    lib.pcomoe_cache_compact.argtypes = [pc, vp, sz, vp]
+    lib.pcomoe_token_logprobs.argtypes = [i32, i32, i32, vp, i64, vp, i32, vp, vp, vp, vp, vp]
     lib.pcomoe_launch_count.restype = ctypes.c_int64
     lib.pcomoe_status_string.restype = ctypes.c_char_p
     lib.pcomoe_status_string.argtypes = [i32]
@@ -517,6 +545,203 @@ class PathMoEStack:
             if st:
                 return st
         return 0
+
+
+# ---- what serves a model around the layer: attention, the paged cache, token scores.  Marshalling only. ----
+
+_TORCH = {PCOMOE_BF16: torch.bfloat16, PCOMOE_FP32: torch.float32}
+
+
+def _ints(t, device, *shape):
+    """A device list of int32 that a call reads: contiguous, of the given shape."""
+    assert t.dtype == torch.int32 and t.is_contiguous() and t.device == device and tuple(t.shape) == shape, (t.dtype, t.shape, shape)
+    return t
+
+
+class PagedCache:
+    """Keys and values of `layers` blocks in pages (pcomoe_cache_*): position p of a sequence lies in row p % page_size of
+    its page number p // page_size, the same page in every layer.
+
+    ``k``, ``v`` [layers, pages, kv_heads, page_size, head_dim]; ``seq_len`` [max_seqs], ``page_ref`` [pages] and
+    ``page_table`` [max_seqs, max_pages] are views, in this order, of the one int32 buffer ``book``.  Memory that the
+    caller has already (``k``, ``v``, ``book``) is used in place.  Sequence lists are int32 device tensors."""
+
+    def __init__(self, *, layers, pages, page_size, kv_heads, head_dim, max_seqs, max_pages, dtype=PCOMOE_BF16, k=None, v=None,
+                 book=None, device="cuda:0"):
+        self.device = k.device if k is not None else torch.device(device)
+        torch.cuda.set_device(self.device)
+        shape = (layers, pages, kv_heads, page_size, head_dim)
+        n = max_seqs + pages + max_seqs * max_pages
+        self.k = torch.zeros(shape, dtype=_TORCH[dtype], device=self.device) if k is None else k
+        self.v = torch.zeros(shape, dtype=_TORCH[dtype], device=self.device) if v is None else v
+        fresh = book is None
+        self.book = torch.zeros(n, dtype=torch.int32, device=self.device) if fresh else book
+        for t in (self.k, self.v):
+            assert tuple(t.shape) == shape and t.dtype == _TORCH[dtype] and t.is_contiguous() and t.device == self.device
+        _ints(self.book, self.device, n)
+        self.seq_len = self.book[:max_seqs]
+        self.page_ref = self.book[max_seqs:max_seqs + pages]
+        self.page_table = self.book[max_seqs + pages:].view(max_seqs, max_pages)
+        if fresh:
+            self.page_table.fill_(-1)
+        self.kv_heads, self.head_dim, self.page_size, self.dtype = kv_heads, head_dim, page_size, dtype
+        self.c = pcomoe_cache(ctypes.sizeof(pcomoe_cache), layers, pages, page_size, kv_heads, head_dim, dtype, max_seqs, max_pages,
+                              self.k.data_ptr(), self.v.data_ptr(), self.seq_len.data_ptr(), self.page_ref.data_ptr(),
+                              self.page_table.data_ptr())
+        self._ref = ctypes.byref(self.c)
+        size = ctypes.c_size_t(0)
+        _check(load_library().pcomoe_cache_workspace_bytes(self._ref, ctypes.byref(size)), "pcomoe_cache_workspace_bytes")
+        self.workspace = torch.empty(size.value, dtype=torch.uint8, device=self.device)
+        self.workspace[:256].zero_()          # the status words start from zero
+        self._ws = (self.workspace.data_ptr(), size.value)
+
+    def reserve(self, seqs, add):
+        """Room for add[i] more tokens in sequence seqs[i]."""
+        n = seqs.numel()
+        _ints(seqs, self.device, n), _ints(add, self.device, n)
+        _check(load_library().pcomoe_cache_reserve(self._ref, n, seqs.data_ptr(), add.data_ptr(), *self._ws, _stream()),
+               "pcomoe_cache_reserve")
+
+    def write(self, k, v, seqs, cu_len, layer: int = 0):
+        """Packed rows k, v [T, kv_heads, head_dim] into the last positions of the sequences in one layer, or
+        [n_layers, T, kv_heads, head_dim] into that many layers from `layer` on."""
+        n = seqs.numel()
+        _ints(seqs, self.device, n), _ints(cu_len, self.device, n + 1)
+        assert k.dim() in (3, 4) and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype == _TORCH[self.dtype]
+        assert tuple(k.shape[-2:]) == (self.kv_heads, self.head_dim) and k.stride(-1) == 1 and k.stride(-2) == self.head_dim
+        many = k.dim() == 4
+        _check(load_library().pcomoe_cache_write(self._ref, layer, k.shape[0] if many else 1, k.shape[-3], n, seqs.data_ptr(),
+                                                 cu_len.data_ptr(), k.data_ptr(), v.data_ptr(), _row_stride(k),
+                                                 k.stride(0) if many else 0, *self._ws, _stream()), "pcomoe_cache_write")
+
+    def fork(self, parents, children):
+        """Sequence children[i] becomes a copy of parents[i] that shares its pages."""
+        n = parents.numel()
+        _ints(parents, self.device, n), _ints(children, self.device, n)
+        _check(load_library().pcomoe_cache_fork(self._ref, n, parents.data_ptr(), children.data_ptr(), *self._ws, _stream()),
+               "pcomoe_cache_fork")
+
+    def keep(self, seqs, cu_len, keep, n_keep):
+        """Of the last cu_len[i+1] - cu_len[i] (drafted) positions of seqs[i] those numbered keep[i, :n_keep[i]] stay."""
+        n = seqs.numel()
+        _ints(seqs, self.device, n), _ints(cu_len, self.device, n + 1), _ints(n_keep, self.device, n)
+        _ints(keep, self.device, n, keep.shape[1])
+        _check(load_library().pcomoe_cache_keep(self._ref, n, seqs.data_ptr(), cu_len.data_ptr(), keep.data_ptr(), keep.shape[1],
+                                                n_keep.data_ptr(), *self._ws, _stream()), "pcomoe_cache_keep")
+
+    def trim(self, seqs, lens):
+        """Shortens sequence seqs[i] to lens[i] tokens; 0 frees it."""
+        n = seqs.numel()
+        _ints(seqs, self.device, n), _ints(lens, self.device, n)
+        _check(load_library().pcomoe_cache_trim(self._ref, n, seqs.data_ptr(), lens.data_ptr(), *self._ws, _stream()),
+               "pcomoe_cache_trim")
+
+    def compact(self):
+        """Moves the pages in use to the lowest ids."""
+        _check(load_library().pcomoe_cache_compact(self._ref, *self._ws, _stream()), "pcomoe_cache_compact")
+
+    def device_status(self) -> int:
+        return pcomoe_device_status(self.workspace)
+
+
+def _row_stride(x):
+    """Elements from one packed row [heads, head_dim] to the next (a tensor of one row may carry any stride)."""
+    return x.stride(-3) if x.shape[-3] > 1 else x.shape[-2] * x.shape[-1]
+
+
+class Attention:
+    """pcomoe_attn_prompt and pcomoe_attn_cached for one head layout.  Owns the workspace and, for up to `max_tokens` packed
+    rows, the default outputs ``out`` [max_tokens, q_heads, head_dim] and ``lse`` [max_tokens, q_heads] fp32."""
+
+    def __init__(self, *, q_heads, kv_heads, head_dim, max_tokens, max_seqs, dtype=PCOMOE_BF16, scale=None, device="cuda:0"):
+        self.device = torch.device(device)
+        torch.cuda.set_device(self.device)
+        self.q_heads, self.kv_heads, self.head_dim, self.dtype = q_heads, kv_heads, head_dim, dtype
+        self.max_tokens, self.max_seqs = max_tokens, max_seqs
+        self.cfg = pcomoe_attn_config(ctypes.sizeof(pcomoe_attn_config), q_heads, kv_heads, head_dim, dtype,
+                                      head_dim ** -0.5 if scale is None else scale)
+        self._cfg = ctypes.byref(self.cfg)
+        size = ctypes.c_size_t(0)
+        _check(load_library().pcomoe_attn_workspace_bytes(self._cfg, ctypes.byref(size)), "pcomoe_attn_workspace_bytes")
+        self.workspace = torch.empty(size.value, dtype=torch.uint8, device=self.device)
+        self.workspace[:PCOMOE_ATTN_ZERO_BYTES].zero_()          # status words and counters start from zero
+        self._ws = (self.workspace.data_ptr(), size.value)
+        T = max(max_tokens, 1)
+        self.out = torch.empty(T, q_heads, head_dim, dtype=_TORCH[dtype], device=self.device)
+        self.lse = torch.empty(T, q_heads, dtype=torch.float32, device=self.device)
+
+    def _rows(self, x, heads):
+        assert x.dim() == 3 and tuple(x.shape[1:]) == (heads, self.head_dim) and x.dtype == _TORCH[self.dtype] and \
+            x.device.type == "cuda" and x.stride(2) == 1 and (heads == 1 or x.stride(1) == self.head_dim), (x.shape, x.stride(), x.dtype)
+        return x.data_ptr(), _row_stride(x)
+
+    def _outputs(self, T, out, lse):
+        assert (out is not None and lse is not None) or T <= self.max_tokens
+        out = self.out[:T] if out is None else out
+        lse = self.lse[:T] if lse is None else lse
+        assert out.shape[0] == T and tuple(lse.shape) == (T, self.q_heads) and lse.is_contiguous() and lse.dtype == torch.float32
+        return out, lse
+
+    def prompt(self, q, k, v, cu_len, out=None, lse=None):
+        """Causal attention over packed prompts: q [T, q_heads, D], k and v [T, kv_heads, D] (column ranges of a fused
+        projection are fine), cu_len [n+1] int32 on the device.  Returns (out, lse)."""
+        T, n = q.shape[0], cu_len.numel() - 1
+        assert n <= self.max_seqs and k.shape[0] == T and v.shape[0] == T
+        _ints(cu_len, self.device, n + 1)
+        out, lse = self._outputs(T, out, lse)
+        _check(load_library().pcomoe_attn_prompt(self._cfg, T, n, cu_len.data_ptr(), *self._rows(q, self.q_heads),
+                                                 *self._rows(k, self.kv_heads), *self._rows(v, self.kv_heads),
+                                                 *self._rows(out, self.q_heads), lse.data_ptr(), *self._ws, _stream()),
+               "pcomoe_attn_prompt")
+        return out, lse
+
+    def cached(self, q, cache: PagedCache, layer: int, seqs, cu_len, tree_mask=None, out=None, lse=None):
+        """Attention of new tokens over the cache: the last cu_len[i+1] - cu_len[i] cached positions of seqs[i] are the packed
+        rows' own.  tree_mask [T, words] int32 (bit m: the row sees the m-th of them) or None: a chain; one row per sequence
+        is a decode step.  Returns (out, lse)."""
+        T, n = q.shape[0], seqs.numel()
+        assert n <= self.max_seqs
+        _ints(seqs, self.device, n), _ints(cu_len, self.device, n + 1)
+        words = 0
+        if tree_mask is not None:
+            words = tree_mask.shape[1]
+            _ints(tree_mask, self.device, T, words)
+        out, lse = self._outputs(T, out, lse)
+        _check(load_library().pcomoe_attn_cached(self._cfg, cache._ref, layer, T, n, seqs.data_ptr(), cu_len.data_ptr(),
+                                                 *self._rows(q, self.q_heads), None if tree_mask is None else tree_mask.data_ptr(),
+                                                 words, *self._rows(out, self.q_heads), lse.data_ptr(), *self._ws, _stream()),
+               "pcomoe_attn_cached")
+        return out, lse
+
+    def device_status(self) -> int:
+        return pcomoe_device_status(self.workspace)
+
+
+class TokenScores:
+    """pcomoe_token_logprobs for up to `max_tokens` rows.  Owns the outputs."""
+
+    def __init__(self, *, max_tokens, top_n=0, device="cuda:0"):
+        self.device = torch.device(device)
+        torch.cuda.set_device(self.device)
+        self.max_tokens, self.top_n = max_tokens, top_n
+        T = max(max_tokens, 1)
+        f32 = dict(dtype=torch.float32, device=self.device)
+        self.logprob, self.entropy, self.top_logprob = torch.empty(T, **f32), torch.empty(T, **f32), torch.empty(T, top_n, **f32)
+        self.top_ids = torch.empty(T, top_n, dtype=torch.int32, device=self.device)
+
+    def score(self, logits, tokens):
+        """logits [T, V] bf16 or fp32, tokens [T] int32.  Returns (logprob [T], entropy [T], top_ids [T, top_n],
+        top_logprob [T, top_n])."""
+        T, V = logits.shape
+        assert T <= self.max_tokens and logits.stride(1) == 1 and logits.device.type == "cuda"
+        _ints(tokens, self.device, T)
+        dtype = PCOMOE_BF16 if logits.dtype == torch.bfloat16 else PCOMOE_FP32
+        assert logits.dtype == _TORCH[dtype], logits.dtype
+        _check(load_library().pcomoe_token_logprobs(dtype, T, V, logits.data_ptr(), logits.stride(0) if T > 1 else V, tokens.data_ptr(),
+                                                    self.top_n, self.logprob.data_ptr(), self.entropy.data_ptr(),
+                                                    self.top_ids.data_ptr(), self.top_logprob.data_ptr(), _stream()),
+               "pcomoe_token_logprobs")
+        return self.logprob[:T], self.entropy[:T], self.top_ids[:T], self.top_logprob[:T]
 
 
 def to_device(arr: np.ndarray | None, device="cuda:0"):

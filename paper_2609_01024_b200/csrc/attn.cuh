@@ -1,0 +1,273 @@
+// What the attention kernels share: the arguments, the way work is cut, masks, the joining of partial results.
+//
+// Rows.  The query heads that share a kv head are packed into the rows of a tile: row r of (sequence, kv head) is token
+// r / g, head r % g of the group, so a tile reads every key and value once for all of them, whatever g is.
+//
+// Work over a cache.  A tile's blocks of keys are numbered through: (sequence, kv head, tile, block), blocks fastest.  Every
+// block (CTA) of the grid takes an equal, contiguous share of that line, found on the device from the lengths alone (no
+// host copy of them, no plan step), so ragged batches are balanced to one block of keys.  A tile cut by a share's
+// border leaves partial sums; the CTA that finishes last joins them in order of the shares, which fixes the bits.
+#pragma once
+#include "tc_ptx.cuh"
+
+namespace pcomoe {
+
+struct AttnArgs {
+  int32_t T, n_seqs, hq, hkv, g;
+  float scale_log2;                     // scale * log2(e)
+  const int32_t *cu, *seqs;
+  const void *q, *k, *v;                // k, v: packed rows, or the layer's page pools
+  int64_t q_stride, k_stride, v_stride, out_stride;      // elements
+  void *out;
+  float *lse;
+  const uint32_t *mask;
+  int32_t words;
+  const int32_t *len, *table;           // the cache's lengths and page tables; NULL: packed prompts
+  int32_t pages, page, page_shift, max_seqs, max_pages;
+  int32_t *status, *counters;
+  float *part, *part_ml;                // [2 * grid][rows][D] and [2 * grid][rows][2]
+  uint64_t limit_ns;
+};
+
+constexpr int kAttnCounters = 4096;     // one per CTA of a grid
+constexpr int kAttnMaxSeqs = 65535;
+constexpr int kAttnMaxWords = 8;
+constexpr float kLn2f = 0.6931471805599453f;
+
+pcomoe_status launch_attn_simt(const AttnArgs &a, int head_dim, int dtype, int sms, cudaStream_t st);
+size_t attn_simt_part_floats(int head_dim, int sms);
+
+#ifdef __CUDACC__
+namespace {
+
+__device__ __forceinline__ float ex2f(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
+struct Seq {
+  int q0, n;            // first packed row and their number
+  int len, base;        // keys; those before `base` are seen by every row, the others by mask or order
+  int id;               // sequence in the cache
+};
+
+template <bool kCached>
+__device__ __forceinline__ Seq load_seq(const AttnArgs &a, int s) {
+  Seq r;
+  r.q0 = a.cu[s];
+  const int e = a.cu[s + 1];
+  r.n = e - r.q0;
+  r.id = 0;
+  if (r.q0 < 0 || r.n < 0 || e > a.T) {
+    atomicCAS(a.status, 0, (int)PCOMOE_ERR_INDEX);
+    r.q0 = r.n = r.len = r.base = 0;
+    return r;
+  }
+  if (!kCached) {
+    r.len = r.n;
+    r.base = 0;
+    return r;
+  }
+  r.id = a.seqs[s];
+  const bool known = r.id >= 0 && r.id < a.max_seqs;
+  const int len = known ? a.len[r.id] : 0;
+  if (r.n > 0 && (!known || len < r.n || ((len - 1) >> a.page_shift) >= a.max_pages || (a.mask && r.n > 32 * a.words))) {
+    atomicCAS(a.status, 0, (int)PCOMOE_ERR_INDEX);
+    r.len = r.base = r.id = 0;           // its rows see nothing
+    return r;
+  }
+  r.len = len;
+  r.base = len - r.n;
+  return r;
+}
+
+// Blocks of BN keys that tile `tile` (BM rows) of a sequence looks at; at least one, so that rows that see nothing are
+// still written.
+template <bool kCached, int BM, int BN>
+__device__ __forceinline__ int tile_blocks(const AttnArgs &a, const Seq &s, int tile) {
+  int keys = s.len;
+  if (!kCached) keys = min(keys, (min((tile + 1) * BM, s.n * a.g) - 1) / a.g + 1);
+  return max(1, (keys + BN - 1) / BN);
+}
+
+// Which of the 32 positions from p0 on row `tok` of a sequence sees, as bits.
+template <bool kCached>
+__device__ __forceinline__ uint32_t seen_bits(const AttnArgs &a, const Seq &s, int tok, int p0) {
+  const int m0 = p0 - s.base;
+  if (m0 + 32 <= 0) return ~0u;                          // all before the queries' own
+  uint32_t bits;
+  if (kCached && a.mask) {
+    const uint32_t *row = a.mask + (int64_t)(s.q0 + tok) * a.words;
+    const int w = m0 >> 5, sh = m0 & 31;                 // floor
+    const uint32_t lo = w >= 0 && w < a.words ? row[w] : 0u, hi = w + 1 < a.words ? row[w + 1] : 0u;
+    bits = sh ? (lo >> sh) | (hi << (32 - sh)) : lo;
+    const int rest = s.n - m0;                           // drafts from here on
+    if (rest < 32) bits &= rest > 0 ? (1u << rest) - 1u : 0u;
+  } else {
+    const int rest = tok + 1 - m0;
+    bits = rest >= 32 ? ~0u : rest > 0 ? (1u << rest) - 1u : 0u;
+  }
+  if (m0 < 0) bits |= (1u << -m0) - 1u;                  // -m0 < 32
+  const int left = s.len - p0;
+  if (left < 32) bits &= left > 0 ? (1u << left) - 1u : 0u;
+  return bits;
+}
+
+// A CTA's share of the line of blocks, and its walk along it.  All of it is the same in every thread of a warp.
+template <int BM, int BN>
+struct CacheWalk {
+  int64_t at, end;      // blocks of this share still to do
+  int64_t share;
+  int64_t seq_at;       // number of the current sequence's first block
+  int s;                // sequence
+  Seq seq;
+  int tiles, blocks;    // of the current sequence: row tiles, blocks of a tile
+
+  __device__ void measure(const AttnArgs &a) {
+    seq = load_seq<true>(a, s);
+    tiles = (seq.n * a.g + BM - 1) / BM;
+    blocks = max(1, (seq.len + BN - 1) / BN);
+  }
+
+  // One warp, all lanes.  Returns false when the share is empty.
+  __device__ bool start(const AttnArgs &a, int cta, int ctas, int least) {
+    const int lane = threadIdx.x & 31;
+    int64_t total = 0;
+    for (int s0 = 0; s0 < a.n_seqs; s0 += 32) {
+      s = s0 + lane;
+      int64_t w = 0;
+      if (s < a.n_seqs) { measure(a); w = (int64_t)tiles * blocks * a.hkv; }
+#pragma unroll
+      for (int o = 16; o; o >>= 1) w += __shfl_xor_sync(~0u, w, o);
+      total += w;
+    }
+    share = max((total + ctas - 1) / ctas, (int64_t)least);
+    at = cta * share;
+    end = min(at + share, total);
+    if (at >= end) return false;
+    int64_t before = 0;
+    for (int s0 = 0; s0 < a.n_seqs; s0 += 32) {
+      s = s0 + lane;
+      int64_t w = 0;
+      if (s < a.n_seqs) { measure(a); w = (int64_t)tiles * blocks * a.hkv; }
+      int64_t upto = w;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(~0u, upto, o);
+        if (lane >= o) upto += y;
+      }
+      const uint32_t hit = __ballot_sync(~0u, before + upto > at);
+      if (hit) {
+        const int l = __ffs(hit) - 1;
+        s = s0 + l;
+        seq_at = before + __shfl_sync(~0u, upto - w, l);
+        break;
+      }
+      before += __shfl_sync(~0u, upto, 31);
+    }
+    measure(a);
+    return true;
+  }
+
+  struct Piece {
+    int kvh, tile, b0, b1;     // blocks [b0, b1) of a tile of `blocks`
+    int first_cta, n_parts;    // shares that the tile is cut into
+    bool whole;
+  };
+
+  __device__ Piece next(const AttnArgs &a) {
+    while (at >= seq_at + (int64_t)tiles * blocks * a.hkv) {
+      seq_at += (int64_t)tiles * blocks * a.hkv;
+      ++s;
+      measure(a);
+    }
+    Piece p;
+    const int64_t off = at - seq_at;
+    const int t = (int)(off / blocks);
+    p.b0 = (int)(off - (int64_t)t * blocks);
+    p.kvh = t / tiles;
+    p.tile = t - p.kvh * tiles;
+    p.b1 = (int)min((int64_t)blocks, p.b0 + (end - at));
+    const int64_t w0 = at - p.b0, w1 = w0 + blocks - 1;
+    p.first_cta = (int)(w0 / share);
+    p.n_parts = (int)(w1 / share) - p.first_cta + 1;
+    p.whole = p.n_parts == 1;
+    at += p.b1 - p.b0;
+    return p;
+  }
+};
+
+// Place of a partial result: a CTA leaves at most two, of the tile that its share begins inside and of the one that it
+// begins itself and does not finish.
+__device__ __forceinline__ int part_slot(int cta, bool begins_tile) { return 2 * cta + (begins_tile ? 1 : 0); }
+
+// After this CTA's partial result of a tile has been written (all threads call): whether it was the last one.  The counter
+// belongs to the tile's first CTA, which begins only one tile that it does not finish, and is left at zero.
+__device__ __forceinline__ bool last_part(const AttnArgs &a, int first_cta, int n_parts, int *s_flag) {
+  __threadfence();
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    const int old = atomicAdd(&a.counters[first_cta], 1);
+    *s_flag = old == n_parts - 1;
+    if (*s_flag) a.counters[first_cta] = 0;
+  }
+  __syncthreads();
+  const bool last = *s_flag;
+  if (last) __threadfence();
+  __syncthreads();
+  return last;
+}
+
+template <typename T> __device__ __forceinline__ void store4(T *p, float4 v);
+template <> __device__ __forceinline__ void store4<float>(float *p, float4 v) { *(float4 *)p = v; }
+template <> __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16 *p, float4 v) {
+  uint2 u;
+  *(__nv_bfloat162 *)&u.x = __floats2bfloat162_rn(v.x, v.y);
+  *(__nv_bfloat162 *)&u.y = __floats2bfloat162_rn(v.z, v.w);
+  *(uint2 *)p = u;
+}
+
+// Joins the partial results of a tile and writes its rows.  Whole block.  BM: rows of a partial result's place.
+template <typename T, int D, int BM>
+__device__ void join_parts(const AttnArgs &a, const Seq &s, int kvh, int tile, int first_cta, int n_parts) {
+  const int rows = min(BM, s.n * a.g - tile * BM);
+  for (int u = threadIdx.x; u < rows * (D / 4); u += blockDim.x) {
+    const int r = u / (D / 4), c = u - r * (D / 4);
+    float m = -INFINITY;
+    for (int i = 0; i < n_parts; ++i) m = fmaxf(m, __ldcg(a.part_ml + ((int64_t)part_slot(first_cta + i, i == 0) * BM + r) * 2));
+    const float ms = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    float4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = 0; i < n_parts; ++i) {
+      const int64_t at = (int64_t)part_slot(first_cta + i, i == 0) * BM + r;
+      const float2 ml = __ldcg((const float2 *)a.part_ml + at);
+      const float4 x = __ldcg((const float4 *)(a.part + at * D) + c);
+      const float w = ex2f(ml.x - ms);
+      if (w == 0.f) continue;                            // a part in which the row saw nothing
+      l += w * ml.y;
+      o.x += w * x.x; o.y += w * x.y; o.z += w * x.z; o.w += w * x.w;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    const int row = tile * BM + r, tok = row / a.g, head = kvh * a.g + row - tok * a.g;
+    const int64_t t = s.q0 + tok;
+    store4<T>((T *)a.out + t * a.out_stride + head * D + 4 * c, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    if (c == 0 && a.lse) a.lse[t * a.hq + head] = l == 0.f ? -INFINITY : ms * kLn2f + logf(l);
+  }
+}
+
+// Row of a page pool ([page][head][place in the page]) that holds position p.
+__device__ __forceinline__ int64_t page_row(const AttnArgs &a, const int32_t *table, int kvh, int p) {
+  int page = table[p >> a.page_shift];
+  if ((unsigned)page >= (unsigned)a.pages) {
+    atomicCAS(a.status, 0, (int)PCOMOE_ERR_INDEX);
+    page = 0;
+  }
+  return ((int64_t)page * a.hkv + kvh) * a.page + (p & (a.page - 1));
+}
+
+}  // namespace
+#endif
+
+}  // namespace pcomoe

@@ -1,0 +1,266 @@
+// Attention with plain FMA, fp32: prompts and cached.  The fp32 layers' counterpart of the tensor-core kernels.
+//
+// One pass over the keys with the running maximum m and sum l of each row's softmax (in the base-2 domain):
+//   m' = max(m, max s),  o <- 2^(m-m') o + sum 2^(s-m') v,  l <- 2^(m-m') l + sum 2^(s-m').
+// A block of 256 threads owns BM rows and walks blocks of 64 keys through shared memory; a thread holds BM/16 rows x 4
+// columns of the scores and BM/16 rows x D/16 columns of the output, both in registers.  What bounds it: the FMA pipe for
+// prompts; for a few rows over a cache shared-memory reads and HBM, hence the narrow form (BM 16, a quarter of the score
+// work of BM 64) where a sequence has at most 16 rows on average.
+#include <algorithm>
+
+#include "attn.cuh"
+
+namespace pcomoe {
+namespace {
+
+constexpr int BN = 64, kThreads = 256;
+
+template <typename T> __device__ __forceinline__ float4 load4(const T *p);
+template <> __device__ __forceinline__ float4 load4<float>(const float *p) { return *(const float4 *)p; }
+template <> __device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bfloat16 *p) {
+  const uint2 u = *(const uint2 *)p;
+  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
+                     __uint_as_float(u.y & 0xffff0000u));
+}
+
+template <int D, int BM> constexpr int smem_floats() { return (BM + 2 * BN) * (D + 4) + BM * (BN + 4); }
+
+template <typename T, int D, int BM, bool kCached>
+__device__ void run_piece(const AttnArgs &a, const Seq &s, int kvh, int tile, int b0, int b1, bool whole, int slot, float *sm) {
+  constexpr int RM = BM / 16, DP = D + 4, PP = BN + 4, NC = D / 64;
+  float *Q = sm, *K = Q + BM * DP, *V = K + BN * DP, *P = V + BN * DP;
+  const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
+  const int rows = min(BM, s.n * a.g - tile * BM);
+  __syncthreads();                                        // the last piece's readers are done
+  for (int u = tid; u < BM * (D / 4); u += kThreads) {
+    const int r = u / (D / 4), c = u - r * (D / 4);
+    float4 x = {0.f, 0.f, 0.f, 0.f};
+    if (r < rows) {
+      const int row = tile * BM + r, tok = row / a.g, head = kvh * a.g + row - tok * a.g;
+      x = load4<T>((const T *)a.q + (int64_t)(s.q0 + tok) * a.q_stride + head * D + 4 * c);
+    }
+    *(float4 *)(Q + r * DP + 4 * c) = x;
+  }
+  float m[RM], l[RM];
+  float4 o[RM][NC];
+  int tok[RM];
+#pragma unroll
+  for (int i = 0; i < RM; ++i) {
+    m[i] = -INFINITY;
+    l[i] = 0.f;
+    tok[i] = (tile * BM + min(ty * RM + i, rows - 1)) / a.g;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) o[i][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+  }
+  const int32_t *table = kCached ? a.table + (int64_t)s.id * a.max_pages : nullptr;
+  for (int b = b0; b < b1; ++b) {
+    const int p0 = b * BN;
+    __syncthreads();
+    for (int u = tid; u < BN * (D / 4); u += kThreads) {
+      const int r = u / (D / 4), c = u - r * (D / 4), p = p0 + r;
+      float4 x = {0.f, 0.f, 0.f, 0.f}, y = x;               // past the end: zero, so that no stale value can matter
+      if (p < s.len) {
+        if (kCached) {
+          const int64_t at = page_row(a, table, kvh, p) * D + 4 * c;
+          x = load4<T>((const T *)a.k + at);
+          y = load4<T>((const T *)a.v + at);
+        } else {
+          x = load4<T>((const T *)a.k + (int64_t)(s.q0 + p) * a.k_stride + kvh * D + 4 * c);
+          y = load4<T>((const T *)a.v + (int64_t)(s.q0 + p) * a.v_stride + kvh * D + 4 * c);
+        }
+      }
+      *(float4 *)(K + r * DP + 4 * c) = x;
+      *(float4 *)(V + r * DP + 4 * c) = y;
+    }
+    __syncthreads();
+    float acc[RM][4];
+#pragma unroll
+    for (int i = 0; i < RM; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[i][j] = 0.f;
+#pragma unroll 4
+    for (int d = 0; d < D; d += 4) {
+      float4 kk[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) kk[j] = *(const float4 *)(K + (tx + 16 * j) * DP + d);
+#pragma unroll
+      for (int i = 0; i < RM; ++i) {
+        const float4 qq = *(const float4 *)(Q + (ty * RM + i) * DP + d);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc[i][j] = fmaf(qq.x, kk[j].x, fmaf(qq.y, kk[j].y, fmaf(qq.z, kk[j].z, fmaf(qq.w, kk[j].w, acc[i][j]))));
+      }
+    }
+    // some row of the tile may not see all of the block
+    const bool masked = p0 + BN > s.base || p0 + BN > s.len;
+#pragma unroll
+    for (int i = 0; i < RM; ++i) {
+      float x[4], mx = -INFINITY;
+      uint32_t lo = ~0u, hi = ~0u;
+      if (masked) {
+        lo = seen_bits<kCached>(a, s, tok[i], p0);
+        hi = seen_bits<kCached>(a, s, tok[i], p0 + 32);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t w = j < 2 ? lo : hi;
+        x[j] = (w >> (tx + 16 * (j & 1))) & 1u ? acc[i][j] * a.scale_log2 : -INFINITY;
+        mx = fmaxf(mx, x[j]);
+      }
+#pragma unroll
+      for (int q = 8; q; q >>= 1) mx = fmaxf(mx, __shfl_xor_sync(~0u, mx, q));
+      const float mn = fmaxf(m[i], mx), ms = mn == -INFINITY ? 0.f : mn;
+      const float r = ex2f(m[i] - ms);
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float p = ex2f(x[j] - ms);
+        sum += p;
+        P[(ty * RM + i) * PP + tx + 16 * j] = p;
+      }
+#pragma unroll
+      for (int q = 8; q; q >>= 1) sum += __shfl_xor_sync(~0u, sum, q);
+      l[i] = l[i] * r + sum;
+      m[i] = mn;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) { o[i][c].x *= r; o[i][c].y *= r; o[i][c].z *= r; o[i][c].w *= r; }
+    }
+    __syncwarp();                                            // a row's weights are written and read by one warp
+    if (!masked) {
+#pragma unroll 4
+      for (int n = 0; n < BN; ++n)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const float4 vv = *(const float4 *)(V + n * DP + 4 * tx + 64 * c);
+#pragma unroll
+          for (int i = 0; i < RM; ++i) {
+            const float p = P[(ty * RM + i) * PP + n];
+            o[i][c].x = fmaf(p, vv.x, o[i][c].x); o[i][c].y = fmaf(p, vv.y, o[i][c].y);
+            o[i][c].z = fmaf(p, vv.z, o[i][c].z); o[i][c].w = fmaf(p, vv.w, o[i][c].w);
+          }
+        }
+    } else {
+      // a value that a row does not see (weight 0) does not touch it, NaN and infinities included
+      for (int n = 0; n < BN; ++n)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const float4 vv = *(const float4 *)(V + n * DP + 4 * tx + 64 * c);
+#pragma unroll
+          for (int i = 0; i < RM; ++i) {
+            const float p = P[(ty * RM + i) * PP + n];
+            if (p != 0.f) {
+              o[i][c].x = fmaf(p, vv.x, o[i][c].x); o[i][c].y = fmaf(p, vv.y, o[i][c].y);
+              o[i][c].z = fmaf(p, vv.z, o[i][c].z); o[i][c].w = fmaf(p, vv.w, o[i][c].w);
+            }
+          }
+        }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < RM; ++i) {
+    const int r = ty * RM + i;
+    if (r >= rows) continue;
+    if (whole) {
+      const int row = tile * BM + r, head = kvh * a.g + row - tok[i] * a.g;
+      const int64_t t = s.q0 + tok[i];
+      const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        store4<T>((T *)a.out + t * a.out_stride + head * D + 4 * tx + 64 * c,
+                  make_float4(o[i][c].x * inv, o[i][c].y * inv, o[i][c].z * inv, o[i][c].w * inv));
+      if (tx == 0 && a.lse) a.lse[t * a.hq + head] = l[i] == 0.f ? -INFINITY : m[i] * kLn2f + logf(l[i]);
+    } else {
+      const int64_t at = (int64_t)slot * BM + r;
+#pragma unroll
+      for (int c = 0; c < NC; ++c) *(float4 *)(a.part + at * D + 4 * tx + 64 * c) = o[i][c];
+      if (tx == 0) *((float2 *)a.part_ml + at) = make_float2(m[i], l[i]);
+    }
+  }
+}
+
+template <typename T, int D, int BM>
+__global__ void __launch_bounds__(kThreads) simt_cached_kernel(AttnArgs a) {
+  pdl_grid_wait();
+  extern __shared__ float4 sm4[];
+  __shared__ int s_flag;
+  CacheWalk<BM, BN> w;
+  if (!w.start(a, blockIdx.x, gridDim.x, 4)) return;
+  while (w.at < w.end) {
+    const auto p = w.next(a);
+    run_piece<T, D, BM, true>(a, w.seq, p.kvh, p.tile, p.b0, p.b1, p.whole, part_slot(blockIdx.x, p.b0 == 0), (float *)sm4);
+    if (!p.whole && last_part(a, p.first_cta, p.n_parts, &s_flag))
+      join_parts<T, D, BM>(a, w.seq, p.kvh, p.tile, p.first_cta, p.n_parts);
+  }
+}
+
+// One tile per block; the tiles are counted from the last one back, so that those with the most keys start first.
+template <typename T, int D, int BM>
+__global__ void __launch_bounds__(kThreads) simt_prompt_kernel(AttnArgs a) {
+  pdl_grid_wait();
+  extern __shared__ float4 sm4[];
+  const int lane = threadIdx.x & 31;
+  int want = gridDim.x - 1 - blockIdx.x, tile = -1, s = 0;
+  for (int s0 = 0; s0 < a.n_seqs && tile < 0; s0 += 32) {
+    const int n = s0 + lane < a.n_seqs ? (load_seq<false>(a, s0 + lane).n * a.g + BM - 1) / BM : 0;
+    int upto = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(~0u, upto, o);
+      if (lane >= o) upto += y;
+    }
+    const uint32_t hit = __ballot_sync(~0u, upto > want);
+    if (hit) {
+      const int l = __ffs(hit) - 1;
+      s = s0 + l;
+      tile = want - __shfl_sync(~0u, upto - n, l);
+    } else {
+      want -= __shfl_sync(~0u, upto, 31);
+    }
+  }
+  if (tile < 0) return;
+  const Seq seq = load_seq<false>(a, s);
+  run_piece<T, D, BM, false>(a, seq, blockIdx.y, tile, 0, tile_blocks<false, BM, BN>(a, seq, tile), true, 0, (float *)sm4);
+}
+
+template <typename F>
+pcomoe_status launch(F *kernel, PerDeviceOnce &once, dim3 grid, size_t smem, const AttnArgs &a, cudaStream_t st) {
+  int dev = -1;
+  PCOMOE_CUDA_TRY(cudaGetDevice(&dev));
+  if (once.first_use(dev)) {
+    PCOMOE_CUDA_TRY(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    once.done(dev);
+  }
+  PCOMOE_CUDA_TRY(launch_pdl(kernel, grid, dim3(kThreads), smem, st, a));
+  count_launch();
+  return PCOMOE_OK;
+}
+
+template <typename T, int D, int BM>
+pcomoe_status run(const AttnArgs &a, int sms, cudaStream_t st) {
+  const size_t smem = smem_floats<D, BM>() * sizeof(float);
+  if (a.table) {
+    static PerDeviceOnce once;
+    return launch(simt_cached_kernel<T, D, BM>, once, dim3(2 * sms), smem, a, st);
+  }
+  static PerDeviceOnce once;
+  const int64_t tiles = (int64_t)a.T * a.g / BM + std::min(a.n_seqs, a.T);
+  if (tiles > INT32_MAX) return PCOMOE_ERR_SHAPE;
+  return launch(simt_prompt_kernel<T, D, BM>, once, dim3((unsigned)tiles, a.hkv), smem, a, st);
+}
+
+template <typename T>
+pcomoe_status by_size(const AttnArgs &a, int D, int sms, cudaStream_t st) {
+  const bool narrow = (int64_t)a.T * a.g <= (int64_t)16 * a.n_seqs;
+  if (D == 64) return narrow ? run<T, 64, 16>(a, sms, st) : run<T, 64, 64>(a, sms, st);
+  return narrow ? run<T, 128, 16>(a, sms, st) : run<T, 128, 64>(a, sms, st);
+}
+
+}  // namespace
+
+size_t attn_simt_part_floats(int D, int sms) { return (size_t)4 * sms * 64 * (D + 2); }
+
+pcomoe_status launch_attn_simt(const AttnArgs &a, int D, int dtype, int sms, cudaStream_t st) {
+  return dtype == PCOMOE_BF16 ? by_size<__nv_bfloat16>(a, D, sms, st) : by_size<float>(a, D, sms, st);
+}
+
+}  // namespace pcomoe

@@ -79,6 +79,9 @@ WsLayout ws_layout(const pcomoe_layer *L, int32_t max_tokens);
 void count_launch(int n = 1);
 uint64_t wait_limit_ns();            // limit of every bounded device-side wait (pcomoe_set_wait_limit_us)
 
+pcomoe_status current_sms(int *sms); // SM count of the current device
+pcomoe_status check_cache(const pcomoe_cache *c);
+
 inline size_t dtype_size(int dt) { return dt == PCOMOE_BF16 ? 2 : 4; }
 
 // Tokens per block of the grouping kernels for a batch of T tokens: the largest chunk the layer allows

@@ -20,6 +20,16 @@ void count_launch(int n) { g_launches.fetch_add(n, std::memory_order_relaxed); }
 static std::atomic<uint64_t> g_wait_limit_ns{2000000000ull};   // 2 s
 uint64_t wait_limit_ns() { return g_wait_limit_ns.load(std::memory_order_relaxed); }
 
+pcomoe_status current_sms(int *sms) {
+  static std::atomic<int> known[64];
+  int dev;
+  PCOMOE_CUDA_TRY(cudaGetDevice(&dev));
+  if (dev >= 0 && dev < 64 && (*sms = known[dev].load(std::memory_order_relaxed)) > 0) return PCOMOE_OK;
+  PCOMOE_CUDA_TRY(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
+  if (dev >= 0 && dev < 64) known[dev].store(*sms, std::memory_order_relaxed);
+  return PCOMOE_OK;
+}
+
 static size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 WsLayout ws_layout(const pcomoe_layer *L, int32_t max_tokens) {
@@ -395,7 +405,7 @@ pcomoe_status pcomoe_device_status(const void *d_workspace, void *stream) {
         cudaSuccess)
       return PCOMOE_ERR_CUDA;
   }
-  if (st < 0 || st > PCOMOE_ERR_INDEX) return PCOMOE_ERR_CUDA;
+  if (st < 0 || st > PCOMOE_ERR_CACHE_FULL) return PCOMOE_ERR_CUDA;
   return (pcomoe_status)st;
 }
 
@@ -425,6 +435,7 @@ const char *pcomoe_status_string(pcomoe_status s) {
     case PCOMOE_ERR_CUDA: return "CUDA call failed";
     case PCOMOE_ERR_TIMEOUT: return "device wait timed out";
     case PCOMOE_ERR_INDEX: return "device index out of range";
+    case PCOMOE_ERR_CACHE_FULL: return "too few free pages in the cache";
   }
   return "unknown status";
 }
