@@ -347,7 +347,7 @@ typedef struct {
   int32_t kv_heads;     /* Hkv                                                                */
   int32_t head_dim;     /* D: 64 or 128                                                       */
   int32_t dtype;        /* pcomoe_dtype of q, k, v and the output                             */
-  float scale;          /* scores are scale * q.k; finite                                     */
+  float scale;          /* scores are scale * q.k; finite, > 0                                */
 } pcomoe_attn_config;
 
 /* Bytes of device workspace of the two attention calls.  256-byte aligned; its first PCOMOE_ATTN_ZERO_BYTES must be zero

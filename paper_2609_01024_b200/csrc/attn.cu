@@ -9,7 +9,7 @@ namespace {
 
 pcomoe_status check_config(const pcomoe_attn_config *c) {
   if (!c || c->struct_size != (int32_t)sizeof(pcomoe_attn_config)) return PCOMOE_ERR_INVALID_ARG;
-  if (c->q_heads <= 0 || c->kv_heads <= 0 || c->q_heads % c->kv_heads || c->head_dim <= 0 || !std::isfinite(c->scale))
+  if (c->q_heads <= 0 || c->kv_heads <= 0 || c->q_heads % c->kv_heads || c->head_dim <= 0 || !(c->scale > 0.f) || !std::isfinite(c->scale))
     return PCOMOE_ERR_INVALID_ARG;
   if (c->dtype != PCOMOE_BF16 && c->dtype != PCOMOE_FP32) return PCOMOE_ERR_INVALID_ARG;
   if (c->head_dim != 64 && c->head_dim != 128) return PCOMOE_ERR_UNSUPPORTED;
@@ -21,8 +21,9 @@ pcomoe_status check_config(const pcomoe_attn_config *c) {
 constexpr size_t kCountersAt = 256, kPartAt = kCountersAt + sizeof(int32_t) * kAttnCounters;
 static_assert(kPartAt == PCOMOE_ATTN_ZERO_BYTES, "what the caller clears");
 
-size_t part_floats(const pcomoe_attn_config *c, int sms) {
-  return attn_simt_part_floats(c->head_dim, sms);
+// rows of partial results: each D sums, a maximum and a sum
+size_t part_rows(const pcomoe_attn_config *c, int sms) {
+  return c->dtype == PCOMOE_BF16 ? attn_tc_part_rows(sms) : attn_simt_part_rows(sms);
 }
 
 bool aligned16(const void *p, int64_t stride, int64_t e) { return ((uintptr_t)p & 15) == 0 && (stride * e) % 16 == 0; }
@@ -36,8 +37,8 @@ pcomoe_status fill(AttnArgs &a, const pcomoe_attn_config *c, int32_t T, int32_t 
   if (n_seqs > kAttnMaxSeqs || (int64_t)T * (c->q_heads / c->kv_heads) > INT32_MAX) return PCOMOE_ERR_SHAPE;
   const int64_t e = (int64_t)dtype_size(c->dtype);
   if (!aligned16(q, q_stride, e) || !aligned16(out, out_stride, e)) return PCOMOE_ERR_UNSUPPORTED;
-  const size_t floats = part_floats(c, sms);
-  if (!ws || ((uintptr_t)ws & 255) || ws_bytes < kPartAt + floats * sizeof(float)) return PCOMOE_ERR_WORKSPACE;
+  const size_t rows = part_rows(c, sms);
+  if (!ws || ((uintptr_t)ws & 255) || ws_bytes < kPartAt + rows * (c->head_dim + 2) * sizeof(float)) return PCOMOE_ERR_WORKSPACE;
   a = AttnArgs{};
   a.T = T; a.n_seqs = n_seqs; a.hq = c->q_heads; a.hkv = c->kv_heads; a.g = c->q_heads / c->kv_heads;
   a.scale_log2 = c->scale * 1.4426950408889634f;
@@ -45,7 +46,7 @@ pcomoe_status fill(AttnArgs &a, const pcomoe_attn_config *c, int32_t T, int32_t 
   a.status = (int32_t *)((char *)ws + offsetof(DevPlan, status_router));
   a.counters = (int32_t *)((char *)ws + kCountersAt);
   a.part = (float *)((char *)ws + kPartAt);
-  a.part_ml = a.part + floats / (c->head_dim + 2) * c->head_dim;
+  a.part_ml = a.part + rows * c->head_dim;
   a.limit_ns = wait_limit_ns();
   return PCOMOE_OK;
 }
@@ -63,7 +64,7 @@ pcomoe_status pcomoe_attn_workspace_bytes(const pcomoe_attn_config *cfg, size_t 
   if (st != PCOMOE_OK) return st;
   int sms;
   if ((st = current_sms(&sms)) != PCOMOE_OK) return st;
-  *bytes = kPartAt + part_floats(cfg, sms) * sizeof(float);
+  *bytes = kPartAt + part_rows(cfg, sms) * (cfg->head_dim + 2) * sizeof(float);
   return PCOMOE_OK;
 }
 
@@ -85,7 +86,8 @@ pcomoe_status pcomoe_attn_prompt(const pcomoe_attn_config *cfg, int32_t T, int32
   st = fill(a, cfg, T, n_seqs, d_cu_len, d_q, q_stride, d_out, out_stride, d_lse, d_workspace, ws_bytes, sms);
   if (st != PCOMOE_OK) return st;
   a.k = d_k; a.v = d_v; a.k_stride = k_stride; a.v_stride = v_stride;
-  return launch_attn_simt(a, cfg->head_dim, cfg->dtype, sms, (cudaStream_t)stream);
+  return cfg->dtype == PCOMOE_BF16 ? launch_attn_tc(a, cfg->head_dim, sms, (cudaStream_t)stream)
+                                   : launch_attn_simt(a, cfg->head_dim, sms, (cudaStream_t)stream);
 }
 
 pcomoe_status pcomoe_attn_cached(const pcomoe_attn_config *cfg, const pcomoe_cache *cache, int32_t layer, int32_t T,
@@ -113,7 +115,8 @@ pcomoe_status pcomoe_attn_cached(const pcomoe_attn_config *cfg, const pcomoe_cac
   a.len = cache->d_seq_len; a.table = cache->d_page_table;
   a.pages = cache->pages; a.page = cache->page_size; a.max_seqs = cache->max_seqs; a.max_pages = cache->max_pages;
   for (a.page_shift = 0; (1 << a.page_shift) < cache->page_size;) ++a.page_shift;
-  return launch_attn_simt(a, cfg->head_dim, cfg->dtype, sms, (cudaStream_t)stream);
+  return cfg->dtype == PCOMOE_BF16 ? launch_attn_tc(a, cfg->head_dim, sms, (cudaStream_t)stream)
+                                   : launch_attn_simt(a, cfg->head_dim, sms, (cudaStream_t)stream);
 }
 
 }  // extern "C"

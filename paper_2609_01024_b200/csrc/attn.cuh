@@ -34,8 +34,10 @@ constexpr int kAttnMaxSeqs = 65535;
 constexpr int kAttnMaxWords = 8;
 constexpr float kLn2f = 0.6931471805599453f;
 
-pcomoe_status launch_attn_simt(const AttnArgs &a, int head_dim, int dtype, int sms, cudaStream_t st);
-size_t attn_simt_part_floats(int head_dim, int sms);
+pcomoe_status launch_attn_tc(const AttnArgs &a, int head_dim, int sms, cudaStream_t st);
+size_t attn_tc_part_rows(int sms);
+pcomoe_status launch_attn_simt(const AttnArgs &a, int head_dim, int sms, cudaStream_t st);
+size_t attn_simt_part_rows(int sms);
 
 #ifdef __CUDACC__
 namespace {
@@ -202,20 +204,37 @@ struct CacheWalk {
 // begins itself and does not finish.
 __device__ __forceinline__ int part_slot(int cta, bool begins_tile) { return 2 * cta + (begins_tile ? 1 : 0); }
 
-// After this CTA's partial result of a tile has been written (all threads call): whether it was the last one.  The counter
-// belongs to the tile's first CTA, which begins only one tile that it does not finish, and is left at zero.
+// Barrier of the first N threads of the block.
+template <int N> __device__ __forceinline__ void sync_first() {
+  __syncwarp();
+  asm volatile("bar.sync 1, %0;" ::"n"(N) : "memory");
+}
+
+// The same, and whether `ok` holds in all of them.
+template <int N> __device__ __forceinline__ bool all_first(bool ok) {
+  int r;
+  __syncwarp();
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.aligned.pred q, 1, %2, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+               : "=r"(r) : "r"((int)ok), "n"(N) : "memory");
+  return r;
+}
+
+// After this CTA's partial result of a tile has been written (the block's first N threads call): whether it was the last
+// one.  The counter belongs to the tile's first CTA, which begins only one tile that it does not finish, and is left at
+// zero.
+template <int N>
 __device__ __forceinline__ bool last_part(const AttnArgs &a, int first_cta, int n_parts, int *s_flag) {
   __threadfence();
-  __syncthreads();
+  sync_first<N>();
   if (threadIdx.x == 0) {
     const int old = atomicAdd(&a.counters[first_cta], 1);
     *s_flag = old == n_parts - 1;
     if (*s_flag) a.counters[first_cta] = 0;
   }
-  __syncthreads();
+  sync_first<N>();
   const bool last = *s_flag;
   if (last) __threadfence();
-  __syncthreads();
+  sync_first<N>();
   return last;
 }
 
@@ -228,11 +247,12 @@ template <> __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16 
   *(uint2 *)p = u;
 }
 
-// Joins the partial results of a tile and writes its rows.  Whole block.  BM: rows of a partial result's place.
-template <typename T, int D, int BM>
+// Joins the partial results of a tile and writes its rows.  The block's first N threads.  BM: rows of a partial result's
+// place.
+template <typename T, int D, int BM, int N>
 __device__ void join_parts(const AttnArgs &a, const Seq &s, int kvh, int tile, int first_cta, int n_parts) {
   const int rows = min(BM, s.n * a.g - tile * BM);
-  for (int u = threadIdx.x; u < rows * (D / 4); u += blockDim.x) {
+  for (int u = threadIdx.x; u < rows * (D / 4); u += N) {
     const int r = u / (D / 4), c = u - r * (D / 4);
     float m = -INFINITY;
     for (int i = 0; i < n_parts; ++i) m = fmaxf(m, __ldcg(a.part_ml + ((int64_t)part_slot(first_cta + i, i == 0) * BM + r) * 2));

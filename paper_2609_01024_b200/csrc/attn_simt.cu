@@ -15,17 +15,9 @@ namespace {
 
 constexpr int BN = 64, kThreads = 256;
 
-template <typename T> __device__ __forceinline__ float4 load4(const T *p);
-template <> __device__ __forceinline__ float4 load4<float>(const float *p) { return *(const float4 *)p; }
-template <> __device__ __forceinline__ float4 load4<__nv_bfloat16>(const __nv_bfloat16 *p) {
-  const uint2 u = *(const uint2 *)p;
-  return make_float4(__uint_as_float(u.x << 16), __uint_as_float(u.x & 0xffff0000u), __uint_as_float(u.y << 16),
-                     __uint_as_float(u.y & 0xffff0000u));
-}
-
 template <int D, int BM> constexpr int smem_floats() { return (BM + 2 * BN) * (D + 4) + BM * (BN + 4); }
 
-template <typename T, int D, int BM, bool kCached>
+template <int D, int BM, bool kCached>
 __device__ void run_piece(const AttnArgs &a, const Seq &s, int kvh, int tile, int b0, int b1, bool whole, int slot, float *sm) {
   constexpr int RM = BM / 16, DP = D + 4, PP = BN + 4, NC = D / 64;
   float *Q = sm, *K = Q + BM * DP, *V = K + BN * DP, *P = V + BN * DP;
@@ -37,7 +29,7 @@ __device__ void run_piece(const AttnArgs &a, const Seq &s, int kvh, int tile, in
     float4 x = {0.f, 0.f, 0.f, 0.f};
     if (r < rows) {
       const int row = tile * BM + r, tok = row / a.g, head = kvh * a.g + row - tok * a.g;
-      x = load4<T>((const T *)a.q + (int64_t)(s.q0 + tok) * a.q_stride + head * D + 4 * c);
+      x = *(const float4 *)((const float *)a.q + (int64_t)(s.q0 + tok) * a.q_stride + head * D + 4 * c);
     }
     *(float4 *)(Q + r * DP + 4 * c) = x;
   }
@@ -62,11 +54,11 @@ __device__ void run_piece(const AttnArgs &a, const Seq &s, int kvh, int tile, in
       if (p < s.len) {
         if (kCached) {
           const int64_t at = page_row(a, table, kvh, p) * D + 4 * c;
-          x = load4<T>((const T *)a.k + at);
-          y = load4<T>((const T *)a.v + at);
+          x = *(const float4 *)((const float *)a.k + at);
+          y = *(const float4 *)((const float *)a.v + at);
         } else {
-          x = load4<T>((const T *)a.k + (int64_t)(s.q0 + p) * a.k_stride + kvh * D + 4 * c);
-          y = load4<T>((const T *)a.v + (int64_t)(s.q0 + p) * a.v_stride + kvh * D + 4 * c);
+          x = *(const float4 *)((const float *)a.k + (int64_t)(s.q0 + p) * a.k_stride + kvh * D + 4 * c);
+          y = *(const float4 *)((const float *)a.v + (int64_t)(s.q0 + p) * a.v_stride + kvh * D + 4 * c);
         }
       }
       *(float4 *)(K + r * DP + 4 * c) = x;
@@ -166,7 +158,7 @@ __device__ void run_piece(const AttnArgs &a, const Seq &s, int kvh, int tile, in
       const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
 #pragma unroll
       for (int c = 0; c < NC; ++c)
-        store4<T>((T *)a.out + t * a.out_stride + head * D + 4 * tx + 64 * c,
+        store4<float>((float *)a.out + t * a.out_stride + head * D + 4 * tx + 64 * c,
                   make_float4(o[i][c].x * inv, o[i][c].y * inv, o[i][c].z * inv, o[i][c].w * inv));
       if (tx == 0 && a.lse) a.lse[t * a.hq + head] = l[i] == 0.f ? -INFINITY : m[i] * kLn2f + logf(l[i]);
     } else {
@@ -178,7 +170,7 @@ __device__ void run_piece(const AttnArgs &a, const Seq &s, int kvh, int tile, in
   }
 }
 
-template <typename T, int D, int BM>
+template <int D, int BM>
 __global__ void __launch_bounds__(kThreads) simt_cached_kernel(AttnArgs a) {
   pdl_grid_wait();
   extern __shared__ float4 sm4[];
@@ -187,14 +179,14 @@ __global__ void __launch_bounds__(kThreads) simt_cached_kernel(AttnArgs a) {
   if (!w.start(a, blockIdx.x, gridDim.x, 4)) return;
   while (w.at < w.end) {
     const auto p = w.next(a);
-    run_piece<T, D, BM, true>(a, w.seq, p.kvh, p.tile, p.b0, p.b1, p.whole, part_slot(blockIdx.x, p.b0 == 0), (float *)sm4);
-    if (!p.whole && last_part(a, p.first_cta, p.n_parts, &s_flag))
-      join_parts<T, D, BM>(a, w.seq, p.kvh, p.tile, p.first_cta, p.n_parts);
+    run_piece<D, BM, true>(a, w.seq, p.kvh, p.tile, p.b0, p.b1, p.whole, part_slot(blockIdx.x, p.b0 == 0), (float *)sm4);
+    if (!p.whole && last_part<kThreads>(a, p.first_cta, p.n_parts, &s_flag))
+      join_parts<float, D, BM, kThreads>(a, w.seq, p.kvh, p.tile, p.first_cta, p.n_parts);
   }
 }
 
 // One tile per block; the tiles are counted from the last one back, so that those with the most keys start first.
-template <typename T, int D, int BM>
+template <int D, int BM>
 __global__ void __launch_bounds__(kThreads) simt_prompt_kernel(AttnArgs a) {
   pdl_grid_wait();
   extern __shared__ float4 sm4[];
@@ -219,7 +211,7 @@ __global__ void __launch_bounds__(kThreads) simt_prompt_kernel(AttnArgs a) {
   }
   if (tile < 0) return;
   const Seq seq = load_seq<false>(a, s);
-  run_piece<T, D, BM, false>(a, seq, blockIdx.y, tile, 0, tile_blocks<false, BM, BN>(a, seq, tile), true, 0, (float *)sm4);
+  run_piece<D, BM, false>(a, seq, blockIdx.y, tile, 0, tile_blocks<false, BM, BN>(a, seq, tile), true, 0, (float *)sm4);
 }
 
 template <typename F>
@@ -235,32 +227,27 @@ pcomoe_status launch(F *kernel, PerDeviceOnce &once, dim3 grid, size_t smem, con
   return PCOMOE_OK;
 }
 
-template <typename T, int D, int BM>
+template <int D, int BM>
 pcomoe_status run(const AttnArgs &a, int sms, cudaStream_t st) {
   const size_t smem = smem_floats<D, BM>() * sizeof(float);
   if (a.table) {
     static PerDeviceOnce once;
-    return launch(simt_cached_kernel<T, D, BM>, once, dim3(2 * sms), smem, a, st);
+    return launch(simt_cached_kernel<D, BM>, once, dim3(2 * sms), smem, a, st);
   }
   static PerDeviceOnce once;
   const int64_t tiles = (int64_t)a.T * a.g / BM + std::min(a.n_seqs, a.T);
   if (tiles > INT32_MAX) return PCOMOE_ERR_SHAPE;
-  return launch(simt_prompt_kernel<T, D, BM>, once, dim3((unsigned)tiles, a.hkv), smem, a, st);
-}
-
-template <typename T>
-pcomoe_status by_size(const AttnArgs &a, int D, int sms, cudaStream_t st) {
-  const bool narrow = (int64_t)a.T * a.g <= (int64_t)16 * a.n_seqs;
-  if (D == 64) return narrow ? run<T, 64, 16>(a, sms, st) : run<T, 64, 64>(a, sms, st);
-  return narrow ? run<T, 128, 16>(a, sms, st) : run<T, 128, 64>(a, sms, st);
+  return launch(simt_prompt_kernel<D, BM>, once, dim3((unsigned)tiles, a.hkv), smem, a, st);
 }
 
 }  // namespace
 
-size_t attn_simt_part_floats(int D, int sms) { return (size_t)4 * sms * 64 * (D + 2); }
+size_t attn_simt_part_rows(int sms) { return (size_t)4 * sms * 64; }
 
-pcomoe_status launch_attn_simt(const AttnArgs &a, int D, int dtype, int sms, cudaStream_t st) {
-  return dtype == PCOMOE_BF16 ? by_size<__nv_bfloat16>(a, D, sms, st) : by_size<float>(a, D, sms, st);
+pcomoe_status launch_attn_simt(const AttnArgs &a, int D, int sms, cudaStream_t st) {
+  const bool narrow = (int64_t)a.T * a.g <= (int64_t)16 * a.n_seqs;
+  if (D == 64) return narrow ? run<64, 16>(a, sms, st) : run<64, 64>(a, sms, st);
+  return narrow ? run<128, 16>(a, sms, st) : run<128, 64>(a, sms, st);
 }
 
 }  // namespace pcomoe

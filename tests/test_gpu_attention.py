@@ -1,7 +1,8 @@
 """Attention over packed prompts and over the paged cache against the 64-bit definition.
 
 Bounds, derived from the arithmetic and element by element.  With A = sum a_p |v_p| / sum a_p (the reference returns it):
-bf16: every weight is rounded to bf16 (relative 2^-9) and the result once more: |do| <= 2^-9 A + 2^-9 |o|, and the fp32 scores
+bf16 (8 significant bits: rounding to nearest is off by up to u = eps / 2 = 2^-8 of the value): every weight is rounded and the
+result once more: |do| <= u A + u |o|, and the fp32 scores
 (products exact, at most 128 of them summed, relative 2^-24 each, sizes of some tens) and exponentials move a weight by less
 than 3e-4 of itself.  fp32: the scores' error d * 2^-24 * sum |q k| * scale stays under 1e-4 for these inputs, and so does
 everything after it.  lse is an fp32 number of size ~10 with the scores' error: 1e-4."""
@@ -21,7 +22,8 @@ def check(out, lse, ref, dtype):
     o, want_lse, size = ref
     out, lse = out.double().cpu(), lse.double().cpu()
     assert torch.equal(torch.isnan(out), torch.isnan(o))
-    bound = (2.0 ** -9 + 3e-4) * size + 2.0 ** -9 * o.abs() if dtype == "bf16" else 1e-4 * size
+    u = torch.finfo(torch.bfloat16).eps / 2
+    bound = (u + 3e-4) * size + u * o.abs() if dtype == "bf16" else 1e-4 * size
     bad = ((out - o).abs() > bound + 1e-30) & ~torch.isnan(o)
     assert not bad.any(), (int(bad.sum()), float((out - o).abs()[bad].max()))
     fine = torch.isfinite(want_lse)
