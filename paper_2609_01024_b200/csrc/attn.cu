@@ -23,7 +23,7 @@ static_assert(kPartAt == PCOMOE_ATTN_ZERO_BYTES, "what the caller clears");
 
 // rows of partial results: each D sums, a maximum and a sum
 size_t part_rows(const pcomoe_attn_config *c, int sms) {
-  return c->dtype == PCOMOE_BF16 ? attn_tc_part_rows(sms) : attn_simt_part_rows(sms);
+  return c->dtype == PCOMOE_BF16 ? std::max(attn_tc_part_rows(sms), attn_few_part_rows(sms)) : attn_simt_part_rows(sms);
 }
 
 bool aligned16(const void *p, int64_t stride, int64_t e) { return ((uintptr_t)p & 15) == 0 && (stride * e) % 16 == 0; }
@@ -115,6 +115,8 @@ pcomoe_status pcomoe_attn_cached(const pcomoe_attn_config *cfg, const pcomoe_cac
   a.len = cache->d_seq_len; a.table = cache->d_page_table;
   a.pages = cache->pages; a.page = cache->page_size; a.max_seqs = cache->max_seqs; a.max_pages = cache->max_pages;
   for (a.page_shift = 0; (1 << a.page_shift) < cache->page_size;) ++a.page_shift;
+  // at most 16 rows (tokens x heads of a group) per sequence on average: the kernel whose tile has 16 rows
+  if (cfg->dtype == PCOMOE_BF16 && (int64_t)T * a.g <= (int64_t)16 * n_seqs) return launch_attn_few(a, cfg->head_dim, sms, (cudaStream_t)stream);
   return cfg->dtype == PCOMOE_BF16 ? launch_attn_tc(a, cfg->head_dim, sms, (cudaStream_t)stream)
                                    : launch_attn_simt(a, cfg->head_dim, sms, (cudaStream_t)stream);
 }

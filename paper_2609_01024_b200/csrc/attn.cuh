@@ -36,6 +36,8 @@ constexpr float kLn2f = 0.6931471805599453f;
 
 pcomoe_status launch_attn_tc(const AttnArgs &a, int head_dim, int sms, cudaStream_t st);
 size_t attn_tc_part_rows(int sms);
+pcomoe_status launch_attn_few(const AttnArgs &a, int head_dim, int sms, cudaStream_t st);
+size_t attn_few_part_rows(int sms);
 pcomoe_status launch_attn_simt(const AttnArgs &a, int head_dim, int sms, cudaStream_t st);
 size_t attn_simt_part_rows(int sms);
 
@@ -248,33 +250,65 @@ template <> __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16 
 }
 
 // Joins the partial results of a tile and writes its rows.  The block's first N threads.  BM: rows of a partial result's
-// place.
+// place.  scratch: shared memory for BM (maximum, 1 / sum) pairs and then as many weights [part][row] as fit in `room`
+// floats.  The sums are read with every part's load in flight: it is the one CTA that finished last, and all it waits for
+// is L2.
 template <typename T, int D, int BM, int N>
-__device__ void join_parts(const AttnArgs &a, const Seq &s, int kvh, int tile, int first_cta, int n_parts) {
+__device__ void join_parts(const AttnArgs &a, const Seq &s, int kvh, int tile, int first_cta, int n_parts, float *scratch, int room) {
   const int rows = min(BM, s.n * a.g - tile * BM);
-  for (int u = threadIdx.x; u < rows * (D / 4); u += N) {
-    const int r = u / (D / 4), c = u - r * (D / 4);
-    float m = -INFINITY;
+  const int kept = min(n_parts, room / BM - 2);          // parts whose weights are kept
+  float2 *stat = (float2 *)scratch;
+  float *wt = scratch + 2 * BM;
+  for (int r = threadIdx.x; r < rows; r += N) {
+    float m = -INFINITY, l = 0.f;
+#pragma unroll 8
     for (int i = 0; i < n_parts; ++i) m = fmaxf(m, __ldcg(a.part_ml + ((int64_t)part_slot(first_cta + i, i == 0) * BM + r) * 2));
     const float ms = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    float4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
+#pragma unroll 8
     for (int i = 0; i < n_parts; ++i) {
-      const int64_t at = (int64_t)part_slot(first_cta + i, i == 0) * BM + r;
-      const float2 ml = __ldcg((const float2 *)a.part_ml + at);
-      const float4 x = __ldcg((const float4 *)(a.part + at * D) + c);
+      const float2 ml = __ldcg((const float2 *)a.part_ml + (int64_t)part_slot(first_cta + i, i == 0) * BM + r);
       const float w = ex2f(ml.x - ms);
-      if (w == 0.f) continue;                            // a part in which the row saw nothing
-      l += w * ml.y;
-      o.x += w * x.x; o.y += w * x.y; o.z += w * x.z; o.w += w * x.w;
+      if (w != 0.f) l += w * ml.y;                       // 0: a part in which the row saw nothing
+      if (i < kept) wt[i * BM + r] = w;
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int row = tile * BM + r, tok = row / a.g, head = kvh * a.g + row - tok * a.g;
-    const int64_t t = s.q0 + tok;
-    store4<T>((T *)a.out + t * a.out_stride + head * D + 4 * c, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-    if (c == 0 && a.lse) a.lse[t * a.hq + head] = l == 0.f ? -INFINITY : ms * kLn2f + logf(l);
+    stat[r] = make_float2(ms, l == 0.f ? 0.f : 1.f / l);
+    if (a.lse) {
+      const int row = tile * BM + r, tok = row / a.g;
+      a.lse[(int64_t)(s.q0 + tok) * a.hq + kvh * a.g + row - tok * a.g] = l == 0.f ? -INFINITY : ms * kLn2f + logf(l);
+    }
   }
+  sync_first<N>();
+  constexpr int U = 4;                                   // columns of four that a thread has in hand
+  for (int u0 = threadIdx.x; u0 < rows * (D / 4); u0 += N * U) {
+    float4 o[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+    for (int i = 0; i < n_parts; ++i) {
+      const int64_t at = (int64_t)part_slot(first_cta + i, i == 0) * BM;
+      float4 x[U];
+#pragma unroll
+      for (int j = 0; j < U; ++j)
+        if (u0 + j * N < rows * (D / 4)) x[j] = __ldcg((const float4 *)(a.part + at * D) + u0 + j * N);
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        const int r = (u0 + j * N) / (D / 4);
+        if (r >= rows) continue;
+        const float w = i < kept ? wt[i * BM + r] : ex2f(__ldcg(a.part_ml + (at + r) * 2) - stat[r].x);
+        if (w == 0.f) continue;
+        o[j].x += w * x[j].x; o[j].y += w * x[j].y; o[j].z += w * x[j].z; o[j].w += w * x[j].w;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int u = u0 + j * N, r = u / (D / 4), c = u - r * (D / 4);
+      if (r >= rows) continue;
+      const float inv = stat[r].y;
+      const int row = tile * BM + r, tok = row / a.g, head = kvh * a.g + row - tok * a.g;
+      store4<T>((T *)a.out + (int64_t)(s.q0 + tok) * a.out_stride + head * D + 4 * c, make_float4(o[j].x * inv, o[j].y * inv, o[j].z * inv, o[j].w * inv));
+    }
+  }
+  sync_first<N>();                                       // the scratch is free again
 }
 
 // Row of a page pool ([page][head][place in the page]) that holds position p.
@@ -285,6 +319,61 @@ __device__ __forceinline__ int64_t page_row(const AttnArgs &a, const int32_t *ta
     page = 0;
   }
   return ((int64_t)page * a.hkv + kvh) * a.page + (p & (a.page - 1));
+}
+
+// One bf16 row without the tensor cores, by a warp, each lane its columns of the head: positions [p0, p1) that the row
+// sees.  For rows that met a NaN or infinity they do not see (weight 0 times it); rare, so plain.
+template <int D, int BM, bool kCached>
+__device__ __forceinline__ void plain_row(const AttnArgs &a, const Seq &s, int kvh, int tile, int r, int p0, int p1, bool whole, int slot) {
+  constexpr int N = D / 32;
+  const int lane = threadIdx.x & 31;
+  const int row = tile * BM + r, tok = row / a.g, head = kvh * a.g + row - tok * a.g;
+  const int64_t t = s.q0 + tok;
+  float q[N], o[N], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    q[i] = __bfloat162float(((const __nv_bfloat16 *)a.q)[t * a.q_stride + head * D + lane * N + i]);
+    o[i] = 0.f;
+  }
+  p1 = min(p1, s.len);
+  const int32_t *table = kCached ? a.table + (int64_t)s.id * a.max_pages : nullptr;
+  uint32_t bits = 0;
+  for (int p = p0; p < p1; ++p) {
+    if (p == p0 || (p & 31) == 0) bits = seen_bits<kCached>(a, s, tok, p & ~31);
+    if (!((bits >> (p & 31)) & 1)) continue;
+    const __nv_bfloat16 *k, *v;
+    if (kCached) {
+      const int64_t at = page_row(a, table, kvh, p) * D;
+      k = (const __nv_bfloat16 *)a.k + at;
+      v = (const __nv_bfloat16 *)a.v + at;
+    } else {
+      k = (const __nv_bfloat16 *)a.k + (s.q0 + p) * a.k_stride + kvh * D;
+      v = (const __nv_bfloat16 *)a.v + (s.q0 + p) * a.v_stride + kvh * D;
+    }
+    float x = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) x = fmaf(q[i], __bfloat162float(k[lane * N + i]), x);
+#pragma unroll
+    for (int h = 16; h; h >>= 1) x += __shfl_xor_sync(~0u, x, h);
+    x *= a.scale_log2;
+    const float mn = fmaxf(m, x), ms = mn == -INFINITY ? 0.f : mn;
+    const float c = ex2f(m - ms), w = ex2f(x - ms);
+    l = l * c + w;
+    m = mn;
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = fmaf(w, __bfloat162float(v[lane * N + i]), o[i] * c);
+  }
+  if (whole) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int i = 0; i < N; ++i) ((__nv_bfloat16 *)a.out)[t * a.out_stride + head * D + lane * N + i] = __float2bfloat16_rn(o[i] * inv);
+    if (lane == 0 && a.lse) a.lse[t * a.hq + head] = l == 0.f ? -INFINITY : m * kLn2f + logf(l);
+  } else {
+    const int64_t at = (int64_t)slot * BM + r;
+#pragma unroll
+    for (int i = 0; i < N; ++i) a.part[at * D + lane * N + i] = o[i];
+    if (lane == 0) *((float2 *)a.part_ml + at) = make_float2(m, l);
+  }
 }
 
 }  // namespace

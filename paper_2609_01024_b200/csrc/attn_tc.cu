@@ -179,61 +179,6 @@ __device__ __forceinline__ int tile_steps(const AttnArgs &a, const Item &it, int
   return min(n, tile_blocks<false, 128, BN>(a, it.seq, 2 * it.tile) - it.b0);
 }
 
-// One row without the tensor cores, by a warp: positions [p0, p1) that the row sees, lane by lane of the head.  Rare (see
-// above), so plain.
-template <int D, bool kCached>
-__device__ __forceinline__ void plain_row(const AttnArgs &a, const Item &it, int r) {
-  constexpr int N = D / 32;
-  const int lane = threadIdx.x & 31;
-  const int row = it.tile * BM + r, tok = row / a.g, head = it.kvh * a.g + row - tok * a.g;
-  const int64_t t = it.seq.q0 + tok;
-  float q[N], o[N], m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    q[i] = __bfloat162float(((const __nv_bfloat16 *)a.q)[t * a.q_stride + head * D + lane * N + i]);
-    o[i] = 0.f;
-  }
-  const int p1 = min(it.b1 * BN, it.seq.len);
-  const int32_t *table = kCached ? a.table + (int64_t)it.seq.id * a.max_pages : nullptr;
-  uint32_t bits = 0;
-  for (int p = it.b0 * BN; p < p1; ++p) {
-    if ((p & 31) == 0) bits = seen_bits<kCached>(a, it.seq, tok, p);
-    if (!((bits >> (p & 31)) & 1)) continue;
-    const __nv_bfloat16 *k, *v;
-    if (kCached) {
-      const int64_t at = page_row(a, table, it.kvh, p) * D;
-      k = (const __nv_bfloat16 *)a.k + at;
-      v = (const __nv_bfloat16 *)a.v + at;
-    } else {
-      k = (const __nv_bfloat16 *)a.k + (it.seq.q0 + p) * a.k_stride + it.kvh * D;
-      v = (const __nv_bfloat16 *)a.v + (it.seq.q0 + p) * a.v_stride + it.kvh * D;
-    }
-    float x = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) x = fmaf(q[i], __bfloat162float(k[lane * N + i]), x);
-#pragma unroll
-    for (int s = 16; s; s >>= 1) x += __shfl_xor_sync(~0u, x, s);
-    x *= a.scale_log2;
-    const float mn = fmaxf(m, x), ms = mn == -INFINITY ? 0.f : mn;
-    const float c = ex2f(m - ms), w = ex2f(x - ms);
-    l = l * c + w;
-    m = mn;
-#pragma unroll
-    for (int i = 0; i < N; ++i) o[i] = fmaf(w, __bfloat162float(v[lane * N + i]), o[i] * c);
-  }
-  if (it.whole) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-#pragma unroll
-    for (int i = 0; i < N; ++i) ((__nv_bfloat16 *)a.out)[t * a.out_stride + head * D + lane * N + i] = __float2bfloat16_rn(o[i] * inv);
-    if (lane == 0 && a.lse) a.lse[t * a.hq + head] = l == 0.f ? -INFINITY : m * kLn2f + logf(l);
-  } else {
-    const int64_t at = (int64_t)it.slot * BM + r;
-#pragma unroll
-    for (int i = 0; i < N; ++i) a.part[at * D + lane * N + i] = o[i];
-    if (lane == 0) *((float2 *)a.part_ml + at) = make_float2(m, l);
-  }
-}
-
 template <int D, bool kCached>
 __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_constant__ TcMaps maps, const __grid_constant__ AttnArgs a) {
   using S = Shape<D>;
@@ -488,13 +433,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
       sync_first<kSoftmaxThreads>();
       if (s_again) {
         for (int x = warp; x < it.rows; x += 8)
-          if (s_bad[x]) plain_row<D, kCached>(a, it, x);
+          if (s_bad[x]) plain_row<D, BM, kCached>(a, it.seq, it.kvh, it.tile, x, it.b0 * BN, it.b1 * BN, it.whole, it.slot);
         sync_first<kSoftmaxThreads>();
         if (tid == 0) s_again = 0;
         sync_first<kSoftmaxThreads>();
       }
       if (!it.whole && last_part<kSoftmaxThreads>(a, it.first_cta, it.n_parts, &s_flag))
-        join_parts<__nv_bfloat16, D, BM, kSoftmaxThreads>(a, it.seq, it.kvh, it.tile, it.first_cta, it.n_parts);
+        join_parts<__nv_bfloat16, D, BM, kSoftmaxThreads>(a, it.seq, it.kvh, it.tile, it.first_cta, it.n_parts,
+                                                           (float *)(smem_raw + (q_at - smem_u32(smem_raw))), 2 * S::kTileBytes / 4);
       item_done();
     }
   } else {
