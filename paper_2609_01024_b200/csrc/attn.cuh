@@ -29,7 +29,7 @@ struct AttnArgs {
   uint64_t limit_ns;
 };
 
-constexpr int kAttnCounters = 4096;     // one per CTA of a grid
+constexpr int kAttnCounters = 4096;     // one per CTA of a grid; the last two are the prompts' (next piece, CTAs done)
 constexpr int kAttnMaxSeqs = 65535;
 constexpr int kAttnMaxWords = 8;
 constexpr float kLn2f = 0.6931471805599453f;
@@ -137,11 +137,12 @@ struct CacheWalk {
   // One warp, all lanes.  Returns false when the share is empty.
   __device__ bool start(const AttnArgs &a, int cta, int ctas, int least) {
     const int lane = threadIdx.x & 31;
-    int64_t total = 0;
+    int64_t total = 0, w0 = 0;                             // w0: of this lane's sequence among the first 32
     for (int s0 = 0; s0 < a.n_seqs; s0 += 32) {
       s = s0 + lane;
       int64_t w = 0;
       if (s < a.n_seqs) { measure(a); w = (int64_t)tiles * blocks * a.hkv; }
+      if (s0 == 0) w0 = w;
 #pragma unroll
       for (int o = 16; o; o >>= 1) w += __shfl_xor_sync(~0u, w, o);
       total += w;
@@ -153,8 +154,8 @@ struct CacheWalk {
     int64_t before = 0;
     for (int s0 = 0; s0 < a.n_seqs; s0 += 32) {
       s = s0 + lane;
-      int64_t w = 0;
-      if (s < a.n_seqs) { measure(a); w = (int64_t)tiles * blocks * a.hkv; }
+      int64_t w = s0 == 0 ? w0 : 0;
+      if (s0 && s < a.n_seqs) { measure(a); w = (int64_t)tiles * blocks * a.hkv; }
       int64_t upto = w;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -166,6 +167,16 @@ struct CacheWalk {
         const int l = __ffs(hit) - 1;
         s = s0 + l;
         seq_at = before + __shfl_sync(~0u, upto - w, l);
+        if (a.n_seqs <= 32) {                              // what lane l has read already
+          seq.q0 = __shfl_sync(~0u, seq.q0, l);
+          seq.n = __shfl_sync(~0u, seq.n, l);
+          seq.len = __shfl_sync(~0u, seq.len, l);
+          seq.base = __shfl_sync(~0u, seq.base, l);
+          seq.id = __shfl_sync(~0u, seq.id, l);
+          tiles = __shfl_sync(~0u, tiles, l);
+          blocks = __shfl_sync(~0u, blocks, l);
+          return true;
+        }
         break;
       }
       before += __shfl_sync(~0u, upto, 31);
@@ -206,14 +217,14 @@ struct CacheWalk {
 // begins itself and does not finish.
 __device__ __forceinline__ int part_slot(int cta, bool begins_tile) { return 2 * cta + (begins_tile ? 1 : 0); }
 
-// Barrier of the first N threads of the block.
-template <int N> __device__ __forceinline__ void sync_first() {
+// Barrier of N threads of the block (all that use barrier 1).
+template <int N> __device__ __forceinline__ void sync_part() {
   __syncwarp();
   asm volatile("bar.sync 1, %0;" ::"n"(N) : "memory");
 }
 
 // The same, and whether `ok` holds in all of them.
-template <int N> __device__ __forceinline__ bool all_first(bool ok) {
+template <int N> __device__ __forceinline__ bool all_part(bool ok) {
   int r;
   __syncwarp();
   asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.aligned.pred q, 1, %2, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
@@ -221,22 +232,22 @@ template <int N> __device__ __forceinline__ bool all_first(bool ok) {
   return r;
 }
 
-// After this CTA's partial result of a tile has been written (the block's first N threads call): whether it was the last
+// After this CTA's partial result of a tile has been written (N threads from thread F on call): whether it was the last
 // one.  The counter belongs to the tile's first CTA, which begins only one tile that it does not finish, and is left at
 // zero.
-template <int N>
+template <int N, int F = 0>
 __device__ __forceinline__ bool last_part(const AttnArgs &a, int first_cta, int n_parts, int *s_flag) {
   __threadfence();
-  sync_first<N>();
-  if (threadIdx.x == 0) {
+  sync_part<N>();
+  if (threadIdx.x == F) {
     const int old = atomicAdd(&a.counters[first_cta], 1);
     *s_flag = old == n_parts - 1;
     if (*s_flag) a.counters[first_cta] = 0;
   }
-  sync_first<N>();
+  sync_part<N>();
   const bool last = *s_flag;
   if (last) __threadfence();
-  sync_first<N>();
+  sync_part<N>();
   return last;
 }
 
@@ -249,66 +260,88 @@ template <> __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16 
   *(uint2 *)p = u;
 }
 
-// Joins the partial results of a tile and writes its rows.  The block's first N threads.  BM: rows of a partial result's
-// place.  scratch: shared memory for BM (maximum, 1 / sum) pairs and then as many weights [part][row] as fit in `room`
-// floats.  The sums are read with every part's load in flight: it is the one CTA that finished last, and all it waits for
-// is L2.
-template <typename T, int D, int BM, int N>
-__device__ void join_parts(const AttnArgs &a, const Seq &s, int kvh, int tile, int first_cta, int n_parts, float *scratch, int room) {
-  const int rows = min(BM, s.n * a.g - tile * BM);
-  const int kept = min(n_parts, room / BM - 2);          // parts whose weights are kept
-  float2 *stat = (float2 *)scratch;
-  float *wt = scratch + 2 * BM;
-  for (int r = threadIdx.x; r < rows; r += N) {
-    float m = -INFINITY, l = 0.f;
-#pragma unroll 8
-    for (int i = 0; i < n_parts; ++i) m = fmaxf(m, __ldcg(a.part_ml + ((int64_t)part_slot(first_cta + i, i == 0) * BM + r) * 2));
-    const float ms = m == -INFINITY ? 0.f : m;
-#pragma unroll 8
-    for (int i = 0; i < n_parts; ++i) {
-      const float2 ml = __ldcg((const float2 *)a.part_ml + (int64_t)part_slot(first_cta + i, i == 0) * BM + r);
-      const float w = ex2f(ml.x - ms);
-      if (w != 0.f) l += w * ml.y;                       // 0: a part in which the row saw nothing
-      if (i < kept) wt[i * BM + r] = w;
-    }
-    stat[r] = make_float2(ms, l == 0.f ? 0.f : 1.f / l);
-    if (a.lse) {
-      const int row = tile * BM + r, tok = row / a.g;
-      a.lse[(int64_t)(s.q0 + tok) * a.hq + kvh * a.g + row - tok * a.g] = l == 0.f ? -INFINITY : ms * kLn2f + logf(l);
+template <typename T, int V> __device__ __forceinline__ void store_row(T *p, const float (&x)[V], float by) {
+#pragma unroll
+  for (int k = 0; k < V; k += 2) {
+    if (sizeof(T) == 4) {
+      *(float2 *)(p + k) = make_float2(x[k] * by, x[k + 1] * by);
+    } else {
+      const __nv_bfloat162 v = __floats2bfloat162_rn(x[k] * by, x[k + 1] * by);
+      *(uint32_t *)(p + k) = *(const uint32_t *)&v;
     }
   }
-  sync_first<N>();
-  constexpr int U = 4;                                   // columns of four that a thread has in hand
-  for (int u0 = threadIdx.x; u0 < rows * (D / 4); u0 += N * U) {
-    float4 o[U];
+}
+
+// Joins the partial results of a tile and writes its rows.  N threads from thread F on, four rows per warp at a time.  The
+// CTA that finished last does this alone, and all it waits for is L2: eight lanes per row hold the parts' maxima and sums,
+// and the sums of four parts are on their way before the weights are known.  BM: rows of a partial result's place.
+template <typename T, int D, int BM, int N, int F = 0>
+__device__ void join_parts(const AttnArgs &a, const Seq &s, int kvh, int tile, int first_cta, int n_parts) {
+  constexpr int R = 4, U = 4, V = D / 32;                  // rows and parts at a time, columns of a lane
+  const int rows = min(BM, s.n * a.g - tile * BM), lane = threadIdx.x & 31, mine = lane & 7;
+  for (int r0 = ((threadIdx.x - F) >> 5) * R; r0 < rows; r0 += (N / 32) * R) {
+    float x[U][R][V], o[R][V];
+    auto fetch = [&](int i0) {
 #pragma unroll
-    for (int j = 0; j < U; ++j) o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-    for (int i = 0; i < n_parts; ++i) {
-      const int64_t at = (int64_t)part_slot(first_cta + i, i == 0) * BM;
-      float4 x[U];
+      for (int u = 0; u < U; ++u) {
+        const int i = min(i0 + u, n_parts - 1);
 #pragma unroll
-      for (int j = 0; j < U; ++j)
-        if (u0 + j * N < rows * (D / 4)) x[j] = __ldcg((const float4 *)(a.part + at * D) + u0 + j * N);
-#pragma unroll
-      for (int j = 0; j < U; ++j) {
-        const int r = (u0 + j * N) / (D / 4);
-        if (r >= rows) continue;
-        const float w = i < kept ? wt[i * BM + r] : ex2f(__ldcg(a.part_ml + (at + r) * 2) - stat[r].x);
-        if (w == 0.f) continue;
-        o[j].x += w * x[j].x; o[j].y += w * x[j].y; o[j].z += w * x[j].z; o[j].w += w * x[j].w;
+        for (int j = 0; j < R; ++j) {
+          const float *src = a.part + ((int64_t)part_slot(first_cta + i, i == 0) * BM + min(r0 + j, rows - 1)) * D + lane * V;
+          if (V == 4) {
+            const float4 y = __ldcg((const float4 *)src);
+            x[u][j][0] = y.x; x[u][j][1] = y.y; x[u][j][V - 2] = y.z; x[u][j][V - 1] = y.w;
+          } else {
+            const float2 y = __ldcg((const float2 *)src);
+            x[u][j][0] = y.x; x[u][j][1] = y.y;
+          }
+        }
       }
+    };
+    fetch(0);
+    const int row8 = min(r0 + (lane >> 3), rows - 1);      // the row of this lane's parts (mine, mine + 8, ...)
+    auto stat = [&](int i) { return __ldcg((const float2 *)a.part_ml + (int64_t)part_slot(first_cta + i, i == 0) * BM + row8); };
+    const float2 ml0 = mine < n_parts ? stat(mine) : make_float2(-INFINITY, 0.f);
+    float m = ml0.x;
+    for (int i = mine + 8; i < n_parts; i += 8) m = fmaxf(m, stat(i).x);
+#pragma unroll
+    for (int h = 4; h; h >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, h));
+    const float ms = m == -INFINITY ? 0.f : m;
+    float l = 0.f, w = 0.f;
+#pragma unroll
+    for (int j = 0; j < R; ++j)
+#pragma unroll
+      for (int k = 0; k < V; ++k) o[j][k] = 0.f;
+    for (int i0 = 0; i0 < n_parts; i0 += U) {
+      if ((i0 & 7) == 0) {                                 // the weights of eight parts, one per lane
+        const float2 ml = i0 == 0 ? ml0 : i0 + mine < n_parts ? stat(i0 + mine) : make_float2(-INFINITY, 0.f);
+        w = ex2f(ml.x - ms);
+        if (w != 0.f) l += w * ml.y;                       // 0: a part in which the row saw nothing
+      }
+      if (i0) fetch(i0);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+          const float wi = __shfl_sync(~0u, w, 8 * j + ((i0 + u) & 7));
+          if (wi != 0.f && i0 + u < n_parts)
+#pragma unroll
+            for (int k = 0; k < V; ++k) o[j][k] = fmaf(wi, x[u][j][k], o[j][k]);
+        }
     }
 #pragma unroll
-    for (int j = 0; j < U; ++j) {
-      const int u = u0 + j * N, r = u / (D / 4), c = u - r * (D / 4);
-      if (r >= rows) continue;
-      const float inv = stat[r].y;
-      const int row = tile * BM + r, tok = row / a.g, head = kvh * a.g + row - tok * a.g;
-      store4<T>((T *)a.out + (int64_t)(s.q0 + tok) * a.out_stride + head * D + 4 * c, make_float4(o[j].x * inv, o[j].y * inv, o[j].z * inv, o[j].w * inv));
+    for (int h = 4; h; h >>= 1) l += __shfl_xor_sync(~0u, l, h);
+#pragma unroll
+    for (int j = 0; j < R; ++j) {
+      const float lj = __shfl_sync(~0u, l, 8 * j), mj = __shfl_sync(~0u, ms, 8 * j);
+      if (r0 + j >= rows) continue;
+      const int row = tile * BM + r0 + j, tok = row / a.g, head = kvh * a.g + row - tok * a.g;
+      const int64_t t = s.q0 + tok;
+      const float inv = lj == 0.f ? 0.f : 1.f / lj;
+      store_row<T, V>((T *)a.out + t * a.out_stride + head * D + lane * V, o[j], inv);
+      if (lane == 0 && a.lse) a.lse[t * a.hq + head] = lj == 0.f ? -INFINITY : mj * kLn2f + logf(lj);
     }
   }
-  sync_first<N>();                                       // the scratch is free again
 }
 
 // Row of a page pool ([page][head][place in the page]) that holds position p.

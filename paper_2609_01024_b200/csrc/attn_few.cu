@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, 2) few_kernel(AttnArgs a) {
       __syncthreads();
     }
     if (!p.whole && last_part<kThreads>(a, p.first_cta, p.n_parts, &s_flag))
-      join_parts<__nv_bfloat16, D, BM, kThreads>(a, seq, p.kvh, p.tile, p.first_cta, p.n_parts, (float *)smem, smem_bytes<D>() / 4);
+      join_parts<__nv_bfloat16, D, BM, kThreads>(a, seq, p.kvh, p.tile, p.first_cta, p.n_parts);
   }
 }
 

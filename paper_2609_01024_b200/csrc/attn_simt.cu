@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(kThreads) simt_cached_kernel(AttnArgs a) {
     const auto p = w.next(a);
     run_piece<D, BM, true>(a, w.seq, p.kvh, p.tile, p.b0, p.b1, p.whole, part_slot(blockIdx.x, p.b0 == 0), (float *)sm4);
     if (!p.whole && last_part<kThreads>(a, p.first_cta, p.n_parts, &s_flag))
-      join_parts<float, D, BM, kThreads>(a, w.seq, p.kvh, p.tile, p.first_cta, p.n_parts, (float *)sm4, smem_floats<D, BM>());
+      join_parts<float, D, BM, kThreads>(a, w.seq, p.kvh, p.tile, p.first_cta, p.n_parts);
   }
 }
 

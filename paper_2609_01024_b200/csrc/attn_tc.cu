@@ -11,9 +11,18 @@
 // weights are formed, the tensor cores work for the other.  With at most 128 rows both tiles hold the same rows and
 // take alternate blocks of keys, so a few drafted tokens over a long cache still keep both busy; the halves are joined
 // at the end.
-//   warps 0-3, 4-7: softmax of tile 0 and 1, and its epilogue     warp 8: issues the MMAs and owns TMEM
-//   warp 9: TMA loads of K and V into a ring (128-byte swizzle)   warp 10: nothing (register shares go by four warps)
-//   warp 11: finds the CTA's pieces of work and hands them to the others through shared memory
+//   warp 0: issues the MMAs and owns TMEM                         warp 1: TMA loads of K and V into a ring (128-byte swizzle)
+//   warp 2: copies the queries                                    warp 3: finds the CTA's pieces of work and hands them out
+//   warps 4-11, 12-19: softmax of tile 0 and 1, and its epilogue; a row has two threads, with half of the keys each
+// The CTAs are persistent and every role runs ahead of the next as far as its buffers allow: the next piece's queries,
+// keys and first scores come in while the last one's output is written.  Prompts: pieces are whole tiles, drawn from a
+// counter in order of falling length, so that the last ones to finish are short.  Cache: every CTA has an equal share.
+//
+// What the softmax threads do bounds the kernel once the products are fed: an exponential per score, and the special
+// function unit does 16 per clock and SM where the MMAs want 16 scores per clock.  So a quarter is formed on the FMA
+// pipe instead: 2^x = 2^n 2^f with n the nearest integer (the add of 1.5 * 2^23 leaves it in the low bits) and 2^f on
+// [-1/2, 1/2] by a degree-4 polynomial (minimax in the relative error by Remez exchange, 2.7e-6, against the 2^-9 that a
+// bf16 weight keeps).  The weights go to the MMA in two halves, so that it starts on the first while the second is formed.
 // K is the K-major B operand of the first product; V ([key][d] as it lies in memory) the MN-major B operand of the second.
 // The softmax threads clear the V rows past the end of a sequence before they hand over the weights of that block, which
 // keeps stale memory out of the sums; a NaN or infinity in a row of V that only some rows of a tile see meets
@@ -27,36 +36,60 @@ namespace pcomoe {
 namespace {
 
 constexpr int BM = 256, BN = 128;              // rows of a CTA, keys of a block
-constexpr int kSoftmaxThreads = 256, kThreads = 384;
-constexpr int kSoftmaxRegs = 208, kOtherRegs = 88, kLaunchRegs = 168;
-static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs, "register split");
+constexpr int kFirst = 128, kTileThreads = 256, kSoftmaxThreads = 512, kThreads = 640;      // softmax threads from thread kFirst on
 constexpr float kSlack = 8.f;                  // how far a maximum may run ahead of the one in use, in powers of two
+
+template <bool B> struct Bool { static constexpr bool value = B; };
 
 template <int D> struct Shape {
   static constexpr int kHalves = D / 64;                    // 64-column halves, one 128-byte swizzle row each
   static constexpr int kHalfBytes = 128 * 128;
   static constexpr int kTileBytes = kHalves * kHalfBytes;   // 128 rows of Q, K or V
   static constexpr int kStages = D == 128 ? 5 : 8;
-  static constexpr int kSmem = 1024 + (2 + kStages) * kTileBytes;
+  static constexpr int kSmem = (2 + kStages) * kTileBytes;
   static constexpr uint32_t kS = 0, kO = 256;               // TMEM columns: scores of the tiles (128 each), outputs (D each)
 };
 
 struct TcMaps {
-  CUtensorMap k, v;
+  CUtensorMap q, k, v;
 };
 
-// mbar_wait without its call: the register split of the kernel leaves no room for the calling convention.
+// mbar_wait without its call (the register split of the kernel leaves no room for the calling convention), and without the
+// long suspend hint, whose wake-up the short waits of this kernel would feel.
+__device__ __forceinline__ bool probe_bar(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok;
+}
+__device__ __forceinline__ bool pause_bar(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok;
+}
 __device__ __forceinline__ bool wait_bar(uint64_t *bar_ptr, uint32_t parity, volatile int *abort_flag, uint64_t limit_ns) {
   const uint32_t bar = smem_u32(bar_ptr);
-  if (mbar_try_wait(bar, parity)) return true;
+  if (probe_bar(bar, parity)) return true;
+  if (pause_bar(bar, parity)) return true;
   const uint64_t t0 = global_ns();
-  for (uint32_t it = 1; it < (1u << 24); ++it) {
-    if (mbar_try_wait(bar, parity)) return true;
+  for (uint32_t it = 1; it < (1u << 28); ++it) {
+    if (pause_bar(bar, parity)) return true;
     if (*abort_flag) return false;
     if (global_ns() - t0 > limit_ns) break;
   }
   *abort_flag = 1;
   return false;
+}
+
+__device__ __forceinline__ bool elect_lane() {
+  uint32_t e;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+  return e;
+}
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map),
+               "r"(x), "r"(y), "r"(z), "r"(bar)
+               : "memory");
 }
 
 // D (+)= A B, fp32 accumulators, bf16 operands; A from shared memory or from TMEM
@@ -100,6 +133,62 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return *(const uint32_t *)&v;
 }
 
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(*(uint64_t *)&a), "l"(*(uint64_t *)&b), "l"(*(uint64_t *)&c));
+  return *(float2 *)&d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*(uint64_t *)&a), "l"(*(uint64_t *)&b));
+  return *(float2 *)&d;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*(uint64_t *)&a), "l"(*(uint64_t *)&b));
+  return *(float2 *)&d;
+}
+// Two powers of two on the FMA pipe (see the head of the file).  -127 and below, -inf among them, give 0; NaN stays NaN.
+__device__ __forceinline__ float2 ex2_poly(float2 x) {
+  constexpr float kRound = 12582912.f + 127.f;             // the low bits of x + kRound are n + 127, 2^n's exponent field
+  x = make_float2(max_nan(x.x, -127.f), max_nan(x.y, -127.f));
+  const float2 t = add2(x, make_float2(kRound, kRound));
+  const float2 f = add2(x, fma2(t, make_float2(-1.f, -1.f), make_float2(kRound, kRound)));
+  float2 p = fma2(f, make_float2(0.009570102207362652f, 0.009570102207362652f), make_float2(0.05591785907745361f, 0.05591785907745361f));
+  p = fma2(p, f, make_float2(0.240247443318367f, 0.240247443318367f));
+  p = fma2(p, f, make_float2(0.6931217908859253f, 0.6931217908859253f));
+  p = fma2(p, f, make_float2(0.9999992847442627f, 0.9999992847442627f));
+  return mul2(p, make_float2(__int_as_float(__float_as_int(t.x) << 23), __int_as_float(__float_as_int(t.y) << 23)));
+}
+// Four rows of 64 bytes, one per lane of a quad, turned so that every store of the quad is 64 contiguous bytes: lane i ends up
+// with piece i of the four rows.  row[k]: where the quad's k-th row goes (this lane's piece), or NULL.
+__device__ __forceinline__ void store_quad(uint32_t (&x)[16], uint8_t *const (&row)[4]) {
+  const int lane = threadIdx.x & 31;
+#pragma unroll
+  for (int h = 1; h <= 2; h <<= 1) {
+    const bool up = lane & h;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      if (c & h) continue;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        // the pieces that belong on the other side of this bit change places
+        uint32_t &lo = x[4 * c + k], &hi = x[4 * (c | h) + k];
+        const uint32_t got = __shfl_xor_sync(~0u, up ? lo : hi, h);
+        if (up) lo = got; else hi = got;
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (row[k]) *(uint4 *)row[k] = make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+}
+
 // A piece of work: blocks [b0, b1) of keys for the rows of one tile of 256.
 struct Item {
   Seq seq;
@@ -128,45 +217,86 @@ template <> struct Walk<true> {
     it.both = it.rows > 128;
     return true;
   }
+  __device__ void finish(const AttnArgs &) {}
 };
 
-// Prompts: one tile per CTA, counted from the last one back, so that those with the most keys start first.
+// Prompts: whole tiles from a counter, longest first.  The order needs every sequence's number of tiles at hand: four per
+// lane.  Beyond 128 sequences they are taken from the last packed row back instead (a tile is then a small part of the
+// whole, and its place matters little).
 template <> struct Walk<false> {
-  int s, tile;
-  bool some;
+  int mine[4];
+  int total;
+  bool first;
+  __device__ static int tiles_of(const AttnArgs &a, int s) { return s < a.n_seqs ? (load_seq<false>(a, s).n * a.g + BM - 1) / BM : 0; }
+  __device__ static int sum(int x) { return (int)__reduce_add_sync(~0u, (unsigned)x); }
   __device__ void start(const AttnArgs &a) {
     const int lane = threadIdx.x & 31;
-    int want = (int)(gridDim.x - 1 - blockIdx.x) / a.hkv;
-    some = false;
-    for (int s0 = 0; s0 < a.n_seqs; s0 += 32) {
-      const int n = s0 + lane < a.n_seqs ? (load_seq<false>(a, s0 + lane).n * a.g + BM - 1) / BM : 0;
-      int upto = n;
+    total = 0;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(~0u, upto, o);
-        if (lane >= o) upto += y;
-      }
-      const uint32_t hit = __ballot_sync(~0u, upto > want);
-      if (hit) {
-        const int l = __ffs(hit) - 1;
-        s = s0 + l;
-        tile = want - __shfl_sync(~0u, upto - n, l);
-        some = true;
-        return;
-      }
-      want -= __shfl_sync(~0u, upto, 31);
-    }
+    for (int k = 0; k < 4; ++k) total += mine[k] = tiles_of(a, 32 * k + lane);
+    for (int s = 128 + lane; s < a.n_seqs; s += 32) total += tiles_of(a, s);
+    total = sum(total);
+    first = true;
   }
+  // tiles whose number inside their sequence is at least x
+  __device__ int from(int x) const { return sum(max(0, mine[0] - x) + max(0, mine[1] - x) + max(0, mine[2] - x) + max(0, mine[3] - x)); }
   __device__ bool next(const AttnArgs &a, Item &it) {
-    if (!some) return false;
-    some = false;
+    const int lane = threadIdx.x & 31;
+    int w = blockIdx.x;                                    // the first piece needs no counter
+    if (!first) {
+      if (lane == 0) w = gridDim.x + atomicAdd(&a.counters[kAttnCounters - 2], 1);
+      w = __shfl_sync(~0u, w, 0);
+    }
+    first = false;
+    if (w >= total * a.hkv) return false;
+    it.kvh = w % a.hkv;
+    int want = w / a.hkv, s = 0;
+    if (a.n_seqs <= 128) {
+      int lo = 0, hi = (int)__reduce_max_sync(~0u, (unsigned)max(max(mine[0], mine[1]), max(mine[2], mine[3])));
+      while (hi - lo > 1) {                                // the largest number with more than `want` tiles from it on
+        const int mid = (lo + hi) >> 1;
+        if (from(mid) > want) lo = mid; else hi = mid;
+      }
+      want -= from(lo + 1);                                // the want-th of the sequences that have tile lo
+      it.tile = lo;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t b = __ballot_sync(~0u, mine[k] > lo);
+        const uint32_t hit = __ballot_sync(~0u, mine[k] > lo && __popc(b & ((1u << lane) - 1)) == want);
+        if (hit) s = 32 * k + __ffs(hit) - 1;
+        want -= __popc(b);
+      }
+    } else {
+      want = total - 1 - want;
+      for (int s0 = 0; s0 < a.n_seqs; s0 += 32) {
+        const int n = tiles_of(a, s0 + lane);
+        int upto = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(~0u, upto, o);
+          if (lane >= o) upto += y;
+        }
+        const uint32_t hit = __ballot_sync(~0u, upto > want);
+        if (hit) {
+          const int l = __ffs(hit) - 1;
+          s = s0 + l;
+          it.tile = want - __shfl_sync(~0u, upto - n, l);
+          break;
+        }
+        want -= __shfl_sync(~0u, upto, 31);
+      }
+    }
     it.seq = load_seq<false>(a, s);
-    it.kvh = (int)(gridDim.x - 1 - blockIdx.x) % a.hkv;
-    it.tile = tile; it.b0 = 0; it.b1 = tile_blocks<false, BM, BN>(a, it.seq, tile);
+    it.b0 = 0; it.b1 = tile_blocks<false, BM, BN>(a, it.seq, it.tile);
     it.whole = true; it.slot = it.first_cta = 0; it.n_parts = 1;
-    it.rows = min(BM, it.seq.n * a.g - tile * BM);
+    it.rows = min(BM, it.seq.n * a.g - it.tile * BM);
     it.both = it.rows > 128;
     return true;
+  }
+  // the last CTA to leave sets the counter back
+  __device__ void finish(const AttnArgs &a) {
+    if ((threadIdx.x & 31) == 0 && atomicAdd(&a.counters[kAttnCounters - 1], 1) == (int)gridDim.x - 1)
+      a.counters[kAttnCounters - 2] = a.counters[kAttnCounters - 1] = 0;
   }
 };
 
@@ -184,30 +314,36 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
   using S = Shape<D>;
   constexpr uint32_t kIdescS = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
   constexpr uint32_t kIdescO = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);
-  extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t s_full[S::kStages], s_empty[S::kStages], s_sfull[2], s_pfull[2], s_ofull[2], s_qfull;
-  __shared__ uint32_t s_tmem;
-  __shared__ int s_abort, s_flag, s_again;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  __shared__ __align__(8) uint64_t s_full[S::kStages], s_empty[S::kStages], s_sfull[2], s_pfull[2][2], s_ofull[2], s_qfull[2], s_qempty[2], s_join;
   __shared__ __align__(8) uint64_t s_ifull[2], s_iempty[2];
   __shared__ Item s_item[2];
+  __shared__ float s_x[2][2][128];                        // between the threads of a row: [tile][half of the keys][row]
   __shared__ uint8_t s_bad[BM];
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_abort, s_flag;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-  const uint32_t q_at = base, ring = base + 2 * S::kTileBytes;
-  // maxima and sums of the two tiles, for items with one tile of rows: in the place of the second tile's queries
-  float2 *s_ml = (float2 *)(smem_raw + (q_at + S::kTileBytes - smem_u32(smem_raw)));
+  const uint32_t q_at = smem_u32(smem), ring = q_at + 2 * S::kTileBytes;
   volatile int *abort_flag = &s_abort;
 
   if (tid == 0) {
-    s_abort = 0;
-    s_again = 0;
+    s_abort = q_at & 1023 ? 1 : 0;                        // the swizzle needs it; nothing would be right otherwise
     for (int i = 0; i < S::kStages; ++i) { mbar_init(smem_u32(&s_full[i]), 1); mbar_init(smem_u32(&s_empty[i]), 1); }
-    for (int t = 0; t < 2; ++t) { mbar_init(smem_u32(&s_sfull[t]), 1); mbar_init(smem_u32(&s_pfull[t]), 4); mbar_init(smem_u32(&s_ofull[t]), 1); }
-    mbar_init(smem_u32(&s_qfull), 8);
-    for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&s_ifull[i]), 1); mbar_init(smem_u32(&s_iempty[i]), 10); }
+    for (int t = 0; t < 2; ++t) {
+      mbar_init(smem_u32(&s_sfull[t]), 1);
+      mbar_init(smem_u32(&s_pfull[t][0]), 4);
+      mbar_init(smem_u32(&s_pfull[t][1]), 4);
+      mbar_init(smem_u32(&s_ofull[t]), 1);
+      mbar_init(smem_u32(&s_qfull[t]), 1);
+      mbar_init(smem_u32(&s_qempty[t]), 1);
+      mbar_init(smem_u32(&s_ifull[t]), 1);
+      mbar_init(smem_u32(&s_iempty[t]), 19);              // every warp but the one that fills them
+    }
+    mbar_init(smem_u32(&s_join), kSoftmaxThreads / 32);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 8) {
+  if (tid < BM) s_bad[tid] = 0;
+  if (warp == 0) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(512) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
@@ -227,117 +363,102 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
     if (lane == 0) mbar_arrive(smem_u32(&s_iempty[n_item & 1]));
     ++n_item;
   };
-  if (warp < 8) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-    const int t = warp >> 2;                              // tile
+  if (warp >= kFirst / 32) {
+    const int t = (warp - kFirst / 32) >> 3, hw = (warp >> 2) & 1 ? 0 : 1;      // tile; half of the keys (warps 4-7: the first)
     const int r = (warp & 3) * 32 + lane;                 // row of the tile = TMEM lane
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t s_col = tmem + S::kS + t * 128 + lanes, o_col = tmem + S::kO + t * D + lanes;
+    auto all_tile = [&](bool yes) {
+      int out;
+      __syncwarp();
+      asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.aligned.pred q, %2, %3, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+                   : "=r"(out) : "r"((int)yes), "r"(2 + t), "n"(kTileThreads) : "memory");
+      return out != 0;
+    };
+    auto sync_tile = [&]() {
+      __syncwarp();
+      asm volatile("bar.sync %0, %1;" ::"r"(2 + t), "n"(kTileThreads) : "memory");
+    };
     uint32_t n_s = 0, n_o0 = 0, n_o1 = 0;                 // steps so far of this tile, finished outputs of both
+    const float scale_log2 = a.scale_log2;
     bool ok = true;
-    // a warp that gives up a wait goes on without waiting to the end of its piece (the barriers below need every warp);
-    // the next piece is begun by all eight or by none
-    while (all_first<kSoftmaxThreads>(item_ready(ok))) {
+    uint32_t n_join = 0;
+    // all softmax warps: bounded like every wait, so that a tile's warps that have given up hold nobody
+    auto sync_both = [&]() {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&s_join));
+      if (ok) ok = wait_bar(&s_join, n_join & 1, abort_flag, a.limit_ns);
+      ++n_join;
+      __syncwarp();
+    };
+    // a warp that gives up a wait goes on without waiting to the end of its piece (the tile's barriers need every warp);
+    // the next piece is begun by all eight warps of a tile or by none
+    while (all_tile(item_ready(ok))) {
       const Item &it = s_item[n_item & 1];
       if (it.rows == 0) break;
-      // queries into shared memory, rows past the end as zero
-      const int q_rows = it.both ? 256 : 128;
-      for (int u0 = tid; u0 < q_rows * (D / 8); u0 += kSoftmaxThreads * 4) {
-        uint4 x[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int u = u0 + i * kSoftmaxThreads, qr = u / (D / 8), c = u % (D / 8);
-          x[i] = make_uint4(0, 0, 0, 0);
-          if (u < q_rows * (D / 8) && qr < it.rows) {
-            const int row = it.tile * BM + qr, tok = row / a.g, head = it.kvh * a.g + row - tok * a.g;
-            x[i] = *(const uint4 *)((const __nv_bfloat16 *)a.q + (int64_t)(it.seq.q0 + tok) * a.q_stride + head * D + c * 8);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int u = u0 + i * kSoftmaxThreads, qr = u / (D / 8), c = u % (D / 8);
-          if (u >= q_rows * (D / 8)) continue;
-          const uint32_t at = q_at + (qr >> 7) * S::kTileBytes + (c >> 3) * S::kHalfBytes + (qr & 127) * 128 + (((c & 7) ^ (qr & 7)) << 4);
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(x[i].x), "r"(x[i].y), "r"(x[i].z), "r"(x[i].w) : "memory");
-        }
-      }
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(smem_u32(&s_qfull));
-
       const int my_row = it.both ? t * 128 + r : r;       // of the item's rows
       const int tok = (it.tile * BM + min(my_row, it.rows - 1)) / a.g;
       const int first_tok = __shfl_sync(~0u, tok, 0);
-      const int steps = tile_steps<kCached>(a, it, t);
+      const int steps = tile_steps<kCached>(a, it, t), len = it.seq.len, base = it.seq.base, b0 = it.b0, b_last = it.b1 - 1;
+      const bool both = it.both;                           // (in registers: shared memory is busy feeding the MMAs)
       float m = -INFINITY, l = 0.f;
       for (int i = 0; i < steps; ++i, ++n_s) {
-        const int b = it.b0 + (it.both ? i : 2 * i + t), p0 = b * BN;
+        const int b = b0 + (both ? i : 2 * i + t), p0 = b * BN;
         if (ok) ok = wait_bar(&s_sfull[t], n_s & 1, abort_flag, a.limit_ns);
         __syncwarp();
         tc_fence_after();
-        uint32_t s[4][32];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32_issue(s_col + 32 * c, s[c]);
+        const bool masked = p0 + BN > (kCached ? base : first_tok + 1) || p0 + BN > len;
+        uint32_t x[2][32];
+        tmem_ld32_issue(s_col + 64 * hw, x[0]);
+        tmem_ld32_issue(s_col + 64 * hw + 32, x[1]);
         tmem_wait_ld();
+        reg_fence32(x[0]);
+        reg_fence32(x[1]);
+        if (masked) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) reg_fence32(s[c]);
-        if (p0 + BN > (kCached ? it.seq.base : first_tok + 1) || p0 + BN > it.seq.len) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            const uint32_t bits = seen_bits<kCached>(a, it.seq, tok, p0 + 32 * c);
+          for (int c = 0; c < 2; ++c) {
+            const uint32_t bits = seen_bits<kCached>(a, it.seq, tok, p0 + 64 * hw + 32 * c);
 #pragma unroll
             for (int k = 0; k < 32; ++k)
-              if (!((bits >> k) & 1)) s[c][k] = 0xff800000u;
+              if (!((bits >> k) & 1)) x[c][k] = 0xff800000u;
           }
           __syncwarp();
         }
-        float mx[4];
+        float mx[8];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          mx[c] = __uint_as_float(s[c][0]);
+        for (int k = 0; k < 8; ++k) mx[k] = fmaxf(__uint_as_float(x[0][2 * k]), __uint_as_float(x[0][2 * k + 1]));
 #pragma unroll
-          for (int k = 1; k < 32; ++k) mx[c] = fmaxf(mx[c], __uint_as_float(s[c][k]));
-        }
-        const float mb = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.scale_log2;
-        const bool raise = mb > m + kSlack || (m == -INFINITY && mb > m);
+        for (int k = 8; k < 32; ++k) mx[k & 7] = fmaxf(mx[k & 7], fmaxf(__uint_as_float(x[k >> 4][(2 * k) & 31]), __uint_as_float(x[k >> 4][((2 * k) & 31) + 1])));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], mx[k + 4]);
+        const float mine = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+        // the row's other half; its thread cannot come back here before this one has handed over its weights
+        s_x[t][hw][r] = mine;
+        sync_tile();
+        const float mb = fmaxf(mine, s_x[t][hw ^ 1][r]) * scale_log2;
+        const bool raise = mb > m + kSlack;                // also from -inf
         if (__any_sync(~0u, raise)) {
           const float mn = raise ? mb : m, c = raise ? ex2f(m - mn) : 1.f;
           m = mn;
           l *= c;
           if (i > 0) {
 #pragma unroll 1
-            for (int h = 0; h < D / 16; ++h) {
+            for (int h = 0; h < D / 32; ++h) {             // half of the columns each
               uint32_t o[16];
-              tmem_ld16(o_col + 16 * h, o);
+              tmem_ld16(o_col + hw * (D / 2) + 16 * h, o);
 #pragma unroll
               for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * c);
-              tmem_st16(o_col + 16 * h, o);
+              tmem_st16(o_col + hw * (D / 2) + 16 * h, o);
             }
           }
         }
-        const float ms = m == -INFINITY ? 0.f : m;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          uint32_t p[16];
-#pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            const float x = ex2f(fmaf(__uint_as_float(s[c][2 * k]), a.scale_log2, -ms));
-            const float y = ex2f(fmaf(__uint_as_float(s[c][2 * k + 1]), a.scale_log2, -ms));
-            sum[k & 1] += x;
-            sum[2 + (k & 1)] += y;
-            p[k] = pack_bf16(x, y);
-          }
-          tmem_st16(s_col + 16 * c, p);
-        }
-        l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        if (b == it.b1 - 1 && p0 + BN > it.seq.len) {
+        if (b == b_last && p0 + BN > len) {
           // the last V of the piece lies in its last ring stage; the scores of this block say that every earlier stage of
           // the ring's last round was filled, so the phase waited for is the one that is pending
           const uint32_t last = pos + 2 * it.blocks() - 1, st = stage(last);
           if (ok) ok = wait_bar(&s_full[st], phase(last), abort_flag, a.limit_ns);
-          const int first = max(it.seq.len - p0, 0), rest = (BN - first) * 8;      // 16-byte pieces of a half
-          for (int u = r; u < rest * S::kHalves; u += 128) {
+          const int first = max(len - p0, 0), rest = (BN - first) * 8;      // 16-byte pieces of a half
+          for (int u = hw * 128 + r; u < rest * S::kHalves; u += kTileThreads) {
             const int h = u / rest, x = u - h * rest;
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(ring + st * S::kTileBytes + h * S::kHalfBytes + first * 128 + x * 16),
                          "r"(0)
@@ -346,36 +467,57 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
           fence_async_smem();
           __syncwarp();
         }
+        const float ms = m == -INFINITY ? 0.f : m;
+        const float2 scale = make_float2(scale_log2, scale_log2), minus = make_float2(-ms, -ms);
+        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        // P of this half over scores that both halves have read by now
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          uint32_t p[16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            float2 e = fma2(make_float2(__uint_as_float(x[c][2 * k]), __uint_as_float(x[c][2 * k + 1])), scale, minus);
+            e = k % 8 == 1 || k % 8 == 4 ? ex2_poly(e) : make_float2(ex2f(e.x), ex2f(e.y));
+            sum[k & 1] = add2(sum[k & 1], e);
+            p[k] = pack_bf16(e.x, e.y);
+          }
+          tmem_st16(s_col + 32 * hw + 16 * c, p);
+        }
+        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&s_pfull[t]));
+        if (lane == 0) mbar_arrive(smem_u32(&s_pfull[t][hw]));
       }
-
       pos += 2 * it.blocks();
+      if (m == -INFINITY) l = 0.f;
 
-      // epilogue: a thread writes its row, or, where both tiles hold the same rows, half of the columns of both
-      if (!it.both) s_ml[t * 128 + r] = make_float2(m, l);
-      s_bad[t * 128 + r] = 0;
-      sync_first<kSoftmaxThreads>();
-      const bool row_here = my_row < it.rows;
-      const int row = it.tile * BM + my_row, head = it.kvh * a.g + row - tok * a.g;
-      const int64_t tg = it.seq.q0 + tok;
+      // the row's sum, from both of its threads
+      sync_tile();
+      s_x[t][hw][r] = l;
+      sync_tile();
+      l += s_x[t][hw ^ 1][r];
+
+      // epilogue: a thread writes half of its row, or, where both tiles hold the same rows, a quarter from both of them
       float w0 = t ? 0.f : 1.f, w1 = t ? 1.f : 0.f, inv = 1.f;      // weights of the tiles' sums
-      int c0 = 0, c1 = D;
+      int c0 = hw * (D / 2), c1 = c0 + D / 2;
       if (it.both) {
         if (ok) ok = t ? wait_bar(&s_ofull[1], n_o1 & 1, abort_flag, a.limit_ns) : wait_bar(&s_ofull[0], n_o0 & 1, abort_flag, a.limit_ns);
         ++n_o0;
         ++n_o1;
+        if (m == -INFINITY) w0 = w1 = 0.f;
       } else {
-        const float2 x = s_ml[r], y = s_ml[128 + r];
+        sync_tile();
+        s_x[t][hw][r] = hw ? l : m;
+        sync_both();
+        const float2 x = make_float2(s_x[0][0][r], s_x[0][1][r]), y = make_float2(s_x[1][0][r], s_x[1][1][r]);
         m = fmaxf(x.x, y.x);
         const float ms = m == -INFINITY ? 0.f : m;
         w0 = ex2f(x.x - ms);
         w1 = ex2f(y.x - ms);
         l = w0 * x.y + w1 * y.y;
-        c0 = t * (D / 2);
-        c1 = c0 + D / 2;
+        c0 = D == 128 ? (2 * t + hw) * 32 : t * 32;
+        c1 = D == 128 || hw == 0 ? c0 + 32 : c0;
         if (ok) ok = wait_bar(&s_ofull[0], n_o0 & 1, abort_flag, a.limit_ns);
         ++n_o0;
         if (it.blocks() > 1) {
@@ -383,14 +525,23 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
           ++n_o1;
         }
       }
+      const bool row_here = my_row < it.rows;
+      const int row = it.tile * BM + my_row, head = it.kvh * a.g + row - tok * a.g;
+      const int64_t tg = it.seq.q0 + tok, part_row = (int64_t)it.slot * BM + my_row;
       if (it.whole) inv = l == 0.f ? 0.f : 1.f / l;
-      __syncwarp();
-      tc_fence_after();
+      // the rows of this lane's quad, and its piece of 16 bytes of them
+      uint8_t *my_out = nullptr, *out[4];
+      if (row_here) my_out = it.whole ? (uint8_t *)((__nv_bfloat16 *)a.out + tg * a.out_stride + head * D) : (uint8_t *)(a.part + part_row * D);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        out[k] = (uint8_t *)__shfl_sync(~0u, (unsigned long long)my_out, (lane & ~3) | k);
+        if (out[k]) out[k] += (lane & 3) * 16 + c0 * (it.whole ? 2 : 4);
+      }
       bool finite = true;
-      const int64_t part_row = (int64_t)it.slot * BM + my_row;
 #pragma unroll 1
       for (int c = c0; c < c1; c += 32) {
         __syncwarp();
+        tc_fence_after();
         float o[32];
 #pragma unroll
         for (int k = 0; k < 32; ++k) o[k] = 0.f;
@@ -407,45 +558,70 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
 #pragma unroll
             for (int k = 0; k < 32; ++k) o[k] = fmaf(w, __uint_as_float(x[k]), o[k]);
         }
+        float z = 0.f;                                     // not 0 where some value is not finite
 #pragma unroll
-        for (int k = 0; k < 32; ++k) finite &= fabsf(o[k]) < INFINITY;
-        if (!row_here) continue;
+        for (int k = 0; k < 32; ++k) z = fmaf(o[k], 0.f, z);
+        finite &= z == 0.f;
+        __syncwarp();
+        uint32_t x[16];
         if (it.whole) {
-          __nv_bfloat16 *to = (__nv_bfloat16 *)a.out + tg * a.out_stride + head * D + c;
 #pragma unroll
-          for (int k = 0; k < 32; k += 8)
-            *(uint4 *)(to + k) = make_uint4(pack_bf16(o[k] * inv, o[k + 1] * inv), pack_bf16(o[k + 2] * inv, o[k + 3] * inv),
-                                            pack_bf16(o[k + 4] * inv, o[k + 5] * inv), pack_bf16(o[k + 6] * inv, o[k + 7] * inv));
+          for (int k = 0; k < 16; ++k) x[k] = pack_bf16(o[2 * k] * inv, o[2 * k + 1] * inv);
+          store_quad(x, out);
         } else {
 #pragma unroll
-          for (int k = 0; k < 32; k += 4) *(float4 *)(a.part + part_row * D + c + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+          for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(o[16 * h + k]);
+            store_quad(x, out);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (out[k]) out[k] += 64;
+          }
         }
+        if (it.whole)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if (out[k]) out[k] += 64;
       }
-      if (row_here && c0 == 0) {
+      tc_fence_before();
+      if (row_here && c0 == 0 && c1 > c0) {
         if (!it.whole) *((float2 *)a.part_ml + part_row) = make_float2(m, l);
         else if (a.lse) a.lse[tg * a.hq + head] = l == 0.f ? -INFINITY : m * kLn2f + logf(l);
       }
-      tc_fence_before();
-      if (row_here && !finite) {
-        s_bad[my_row] = 1;
-        s_again = 1;
+      // rows to form again; also: every thread is done with the outputs and with s_x
+      if (row_here && !finite) s_bad[my_row] = 1;
+      if (it.both) sync_tile(); else sync_both();
+      if (hw == 0 && (it.both || t == 0)) {
+        const bool again = s_bad[my_row];
+        if (again) s_bad[my_row] = 0;
+        __syncwarp();
+        for (uint32_t todo = __ballot_sync(~0u, again); todo; todo &= todo - 1) {
+          const int x = (it.both ? t * 128 : 0) + (warp & 3) * 32 + __ffs(todo) - 1;
+          plain_row<D, BM, kCached>(a, it.seq, it.kvh, it.tile, x, it.b0 * BN, it.b1 * BN, it.whole, it.slot);
+        }
       }
-      sync_first<kSoftmaxThreads>();
-      if (s_again) {
-        for (int x = warp; x < it.rows; x += 8)
-          if (s_bad[x]) plain_row<D, BM, kCached>(a, it.seq, it.kvh, it.tile, x, it.b0 * BN, it.b1 * BN, it.whole, it.slot);
-        sync_first<kSoftmaxThreads>();
-        if (tid == 0) s_again = 0;
-        sync_first<kSoftmaxThreads>();
+      if (!it.whole) {
+        // (as last_part, with the barrier between both tiles' warps)
+        __threadfence();
+        sync_both();
+        if (tid == kFirst) {
+          const int old = atomicAdd(&a.counters[it.first_cta], 1);
+          s_flag = ok && old == it.n_parts - 1;
+          if (old == it.n_parts - 1) a.counters[it.first_cta] = 0;
+        }
+        sync_both();
+        const bool last = __all_sync(~0u, s_flag && ok);
+        if (last) {
+          __threadfence();
+          join_parts<__nv_bfloat16, D, BM, kSoftmaxThreads, kFirst>(a, it.seq, it.kvh, it.tile, it.first_cta, it.n_parts);
+        }
+        sync_both();                                       // s_flag has been read
       }
-      if (!it.whole && last_part<kSoftmaxThreads>(a, it.first_cta, it.n_parts, &s_flag))
-        join_parts<__nv_bfloat16, D, BM, kSoftmaxThreads>(a, it.seq, it.kvh, it.tile, it.first_cta, it.n_parts,
-                                                           (float *)(smem_raw + (q_at - smem_u32(smem_raw))), 2 * S::kTileBytes / 4);
       item_done();
     }
   } else {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-    if (warp == 9) {
+    if (warp == 1) {
       // ---- loads: K and V blocks in the order in which the MMAs take them
       bool ok = true;
       for (; __all_sync(~0u, item_ready(ok)); item_done()) {
@@ -480,83 +656,142 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
             ++pos;
           }
       }
-    } else if (warp == 8) {
-      // ---- MMAs, all from one thread
-      uint32_t n_p[2] = {0, 0}, n_q = 0;
+    } else if (warp == 2) {
+      // ---- queries: rows of a tile into the K-major operand layout, rows past the end as zero
+      uint32_t n_q[2] = {0, 0};
       bool ok = true;
-      auto wait = [&](uint64_t *bar, uint32_t ph) { return wait_bar(bar, ph, abort_flag, a.limit_ns); };
-      auto scores = [&](int t, int q, uint32_t st) {      // S_t = Q_q K^T
-        const uint64_t da = umma_desc(q_at + q * S::kTileBytes), db = umma_desc(ring + st * S::kTileBytes);
+      for (; __all_sync(~0u, item_ready(ok)); item_done()) {
+        const Item &it = s_item[n_item & 1];
+        if (it.rows == 0) break;
 #pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-          const uint64_t off = (uint64_t)((k >> 2) * (S::kHalfBytes >> 4) + (k & 3) * 2);
-          mma_ss(tmem + S::kS + t * 128, da + off, db + off, kIdescS, k != 0);
+        for (int q = 0; q < 2; ++q) {
+          if (q && !it.both) continue;
+          ok = ok && wait_bar(&s_qempty[q], (n_q[q] & 1) ^ 1, abort_flag, a.limit_ns);
+          ok = __all_sync(~0u, ok);
+          if (!ok) break;
+          ++n_q[q];
+          if (128 % a.g == 0) {
+            // whole tokens: one box of 128 / g tokens x g heads per half.  Rows past the end are other rows or zero; their
+            // scores are nobody's.
+            if (lane == 0) mbar_arrive_expect_tx(smem_u32(&s_qfull[q]), S::kTileBytes);
+            __syncwarp();
+            if (lane < S::kHalves)
+              tma_load_3d(q_at + q * S::kTileBytes + lane * S::kHalfBytes, &maps.q, lane * 64, it.kvh * a.g, it.seq.q0 + (it.tile * BM + q * 128) / a.g,
+                          smem_u32(&s_qfull[q]));
+            continue;
+          }
+          const int rows = it.rows - q * 128;
+          constexpr int C = D / 8, P = 32 / C;             // pieces of a row; rows that a warp copies side by side
+          const int c = lane % C;
+          const uint32_t to = q_at + q * S::kTileBytes + (c >> 3) * S::kHalfBytes;
+          int tok = (it.tile * BM + q * 128 + lane / C) / a.g, hd = it.tile * BM + q * 128 + lane / C - tok * a.g;
+          for (int qr = lane / C; qr < 128; qr += P) {
+            const bool there = qr < rows;
+            const __nv_bfloat16 *src = (const __nv_bfloat16 *)a.q + (there ? (int64_t)(it.seq.q0 + tok) * a.q_stride + (it.kvh * a.g + hd) * D + c * 8 : 0);
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + qr * 128 + (((c & 7) ^ (qr & 7)) << 4)), "l"(src),
+                         "r"(there ? 16 : 0)
+                         : "memory");
+            for (hd += P; hd >= a.g; hd -= a.g) ++tok;
+          }
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(smem_u32(&s_qfull[q]));
         }
-        umma_commit(smem_u32(&s_sfull[t]));
+      }
+    } else if (warp == 0) {
+      // ---- MMAs.  The whole warp walks along, so that addresses and descriptors stay warp-uniform; one lane issues.
+      uint32_t n_q0 = 0, n_q1 = 0, n_p0 = 0, n_p1 = 0;
+      bool ok = true;
+      uint32_t st = 0, ph = 0;                            // next ring stage and its phase
+      auto advance = [&]() {
+        if (++st == S::kStages) { st = 0; ph ^= 1; }
       };
-      auto output = [&](int t, uint32_t st, bool first) {  // O_t += P_t V
-        const uint64_t dv = mn_desc(ring + st * S::kTileBytes, S::kHalfBytes);
+      auto wait = [&](uint64_t *bar, uint32_t p) { return ok = __all_sync(~0u, wait_bar(bar, p, abort_flag, a.limit_ns)); };
+      const uint64_t q_desc = umma_desc(q_at), k_desc = umma_desc(ring), v_desc = mn_desc(ring, S::kHalfBytes);
+      auto scores = [&](int t, int q, uint32_t at, bool last_q, bool last_k) {      // S_t = Q_q K^T
+        const uint64_t da = q_desc + (uint64_t)(q * (S::kTileBytes >> 4)), db = k_desc + (uint64_t)(at * (S::kTileBytes >> 4));
+        if (elect_lane()) {
 #pragma unroll
-        for (int k = 0; k < BN / 16; ++k)
-          mma_ts(tmem + S::kO + t * D, tmem + S::kS + t * 128 + k * 8, dv + (uint64_t)(k * (2048 >> 4)), kIdescO, !first || k != 0);
+          for (int k = 0; k < D / 16; ++k) {
+            const uint64_t off = (uint64_t)((k >> 2) * (S::kHalfBytes >> 4) + (k & 3) * 2);
+            mma_ss(tmem + S::kS + t * 128, da + off, db + off, kIdescS, k != 0);
+          }
+          umma_commit(smem_u32(&s_sfull[t]));
+          if (last_q) umma_commit(smem_u32(&s_qempty[q]));
+          if (last_k) umma_commit(smem_u32(&s_empty[at]));
+        }
+        __syncwarp();
+      };
+      // O_t += P_t V, as its two halves come
+      auto output = [&](int t, uint32_t at, bool first, bool last_v, bool last_o) {
+        const uint64_t dv = v_desc + (uint64_t)(at * (S::kTileBytes >> 4));
+        const uint32_t p = t ? n_p1++ & 1 : n_p0++ & 1;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          if (!wait(&s_pfull[t][h], p)) return;
+          tc_fence_after();
+          if (elect_lane()) {
+#pragma unroll
+            for (int k = 4 * h; k < 4 * h + 4; ++k)
+              mma_ts(tmem + S::kO + t * D, tmem + S::kS + t * 128 + k * 8, dv + (uint64_t)(k * (2048 >> 4)), kIdescO, !first || k != 0);
+            if (h && last_v) umma_commit(smem_u32(&s_empty[at]));
+            if (h && last_o) umma_commit(smem_u32(&s_ofull[t]));
+          }
+          __syncwarp();
+        }
       };
       for (; __all_sync(~0u, item_ready(ok)); item_done()) {
         const Item &it = s_item[n_item & 1];
         if (it.rows == 0) break;
-        if (lane == 0) {
-          const int n = it.blocks();
+        const int n = it.blocks();
+        if (it.both) {
           const int steps0 = tile_steps<kCached>(a, it, 0);
-          ok = wait(&s_qfull, n_q++ & 1);
-          tc_fence_after();
-          if (it.both) {
-            for (int j = 0; ok && j <= n; ++j) {
-              const uint32_t pv = pos, pk = j ? pos + 1 : pos;
-              pos = pk + (j < n ? 1 : 0);
-              if (j > 0) {
-                ok = wait(&s_full[stage(pv)], phase(pv));
-              }
-              if (ok && j < n) ok = wait(&s_full[stage(pk)], phase(pk));
-#pragma unroll
-              for (int t = 0; t < 2; ++t) {
-                const int steps = t ? n : steps0;
-                if (ok && j > 0 && j - 1 < steps) {
-                  ok = wait(&s_pfull[t], n_p[t]++ & 1);
-                  if (!ok) break;
-                  tc_fence_after();
-                  output(t, stage(pv), j == 1);
-                  if (j == steps) umma_commit(smem_u32(&s_ofull[t]));
-                }
-                if (t == 1 && ok && j > 0) umma_commit(smem_u32(&s_empty[stage(pv)]));
-                if (ok && j < steps) scores(t, t, stage(pk));
-                if (t == 1 && ok && j < n) umma_commit(smem_u32(&s_empty[stage(pk)]));
-              }
+          for (int j = 0; ok && j <= n; ++j) {
+            uint32_t v = st, k = st;
+            if (j > 0) {
+              if (!wait(&s_full[st], ph)) break;
+              advance();
             }
-          } else {
-            for (int i = 0; ok && i < n + 2; ++i) {
-              const int t = i & 1;
-              if (i >= 2) {
-                const uint32_t pv = pos++;
-                ok = wait(&s_full[stage(pv)], phase(pv));
-                if (ok) ok = wait(&s_pfull[t], n_p[t]++ & 1);
-                if (!ok) break;
-                tc_fence_after();
-                output(t, stage(pv), i < 4);
-                umma_commit(smem_u32(&s_empty[stage(pv)]));
-                if (i >= n) umma_commit(smem_u32(&s_ofull[t]));
-              }
-              if (i < n) {
-                const uint32_t pk = pos++;
-                ok = wait(&s_full[stage(pk)], phase(pk));
-                if (!ok) break;
-                scores(t, 0, stage(pk));
-                umma_commit(smem_u32(&s_empty[stage(pk)]));
-              }
+            if (j < n) {
+              k = st;
+              if (!wait(&s_full[st], ph)) break;
+              advance();
+            }
+            if (j > 0 && j - 1 < steps0) output(0, v, j == 1, false, j == steps0);
+            if (ok && j < steps0) {
+              if (j == 0) wait(&s_qfull[0], n_q0++ & 1);
+              if (!ok) break;
+              scores(0, 0, k, j == steps0 - 1, false);
+            }
+            if (ok && j > 0) output(1, v, j == 1, true, j == n);
+            if (ok && j < n) {
+              if (j == 0) wait(&s_qfull[1], n_q1++ & 1);
+              if (!ok) break;
+              scores(1, 1, k, j == n - 1, true);
+            }
+          }
+        } else {
+          wait(&s_qfull[0], n_q0++ & 1);
+          tc_fence_after();
+          for (int i = 0; ok && i < n + 2; ++i) {
+            if (i >= 2) {
+              const uint32_t v = st;
+              if (!wait(&s_full[st], ph)) break;
+              advance();
+              if (i & 1) output(1, v, i < 4, true, i >= n); else output(0, v, i < 4, true, i >= n);
+              if (!ok) break;
+            }
+            if (i < n) {
+              const uint32_t k = st;
+              if (!wait(&s_full[st], ph)) break;
+              advance();
+              scores(i & 1, 0, k, i == n - 1, true);
             }
           }
         }
-        ok = __shfl_sync(~0u, (int)ok, 0);
       }
-    } else if (warp == 11) {
+    } else if (warp == 3) {
       // ---- the pieces of work
       Walk<kCached> walk;
       walk.start(a);
@@ -571,6 +806,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         }
         __syncwarp();
       }
+      walk.finish(a);
     }
   }
   tc_fence_before();
@@ -578,7 +814,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
   tc_fence_after();
   if (s_abort) timeout_record_and_drain(a.status);
   __syncthreads();
-  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+  if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
 bool make_rows_map(CUtensorMap *m, const void *base, uint64_t rows, uint64_t cols, uint64_t stride, uint32_t box_rows) {
@@ -596,10 +832,6 @@ pcomoe_status run(const TcMaps &m, const AttnArgs &a, unsigned grid, cudaStream_
   int dev = -1;
   PCOMOE_CUDA_TRY(cudaGetDevice(&dev));
   if (once.first_use(dev)) {
-    // the register split draws on what the block was launched with: fewer and the larger share would never come
-    cudaFuncAttributes at;
-    PCOMOE_CUDA_TRY(cudaFuncGetAttributes(&at, attn_tc_kernel<D, kCached>));
-    if (at.numRegs < kLaunchRegs) return PCOMOE_ERR_CUDA;
     PCOMOE_CUDA_TRY(cudaFuncSetAttribute(attn_tc_kernel<D, kCached>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem));
     once.done(dev);
   }
@@ -614,6 +846,14 @@ size_t attn_tc_part_rows(int sms) { return (size_t)2 * sms * BM; }
 
 pcomoe_status launch_attn_tc(const AttnArgs &a, int D, int sms, cudaStream_t st) {
   TcMaps m;
+  const int tokens = 128 % a.g ? 1 : 128 / a.g, heads = 128 % a.g ? 1 : a.g;      // of a tile; else the map is not used
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return PCOMOE_ERR_CUDA;
+  cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)a.hq, (cuuint64_t)a.T}, strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)a.q_stride * 2};
+  cuuint32_t box[3] = {BK, (cuuint32_t)heads, (cuuint32_t)tokens}, estr[3] = {1, 1, 1};
+  if (fn(&m.q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(a.q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return PCOMOE_ERR_CUDA;
   if (a.table) {
     const uint64_t rows = (uint64_t)a.pages * a.hkv * a.page;
     if (rows > INT32_MAX) return PCOMOE_ERR_UNSUPPORTED;                 // row numbers of a TMA copy are 32 bits
@@ -623,9 +863,10 @@ pcomoe_status launch_attn_tc(const AttnArgs &a, int D, int sms, cudaStream_t st)
   }
   if (!make_rows_map(&m.k, a.k, a.T, (uint64_t)a.hkv * D, a.k_stride, BN) || !make_rows_map(&m.v, a.v, a.T, (uint64_t)a.hkv * D, a.v_stride, BN))
     return PCOMOE_ERR_CUDA;
-  const int64_t tiles = (int64_t)a.T * a.g / BM + std::min(a.n_seqs, a.T);
-  if (tiles * a.hkv > INT32_MAX) return PCOMOE_ERR_SHAPE;
-  return D == 64 ? run<64, false>(m, a, (unsigned)(tiles * a.hkv), st) : run<128, false>(m, a, (unsigned)(tiles * a.hkv), st);
+  const int64_t tiles = ((int64_t)a.T * a.g / BM + std::min(a.n_seqs, a.T)) * a.hkv;      // no more than that
+  if (tiles > INT32_MAX) return PCOMOE_ERR_SHAPE;
+  const unsigned grid = (unsigned)std::min<int64_t>(tiles, sms);
+  return D == 64 ? run<64, false>(m, a, grid, st) : run<128, false>(m, a, grid, st);
 }
 
 }  // namespace pcomoe
