@@ -552,10 +552,22 @@ class PathMoEStack:
 _TORCH = {PCOMOE_BF16: torch.bfloat16, PCOMOE_FP32: torch.float32}
 
 
-def _ints(t, device, *shape):
-    """A device list of int32 that a call reads: contiguous, of the given shape."""
-    assert t.dtype == torch.int32 and t.is_contiguous() and t.device == device and tuple(t.shape) == shape, (t.dtype, t.shape, shape)
-    return t
+def _ints(t, device, n):
+    """A device list of n int32 that a call reads: contiguous."""
+    assert t.dtype is torch.int32 and t.numel() == n and t.is_contiguous() and t.device == device, (t.dtype, t.shape, t.device, n)
+    return t.data_ptr()
+
+
+def _raw_stream(device) -> int:
+    """The current stream of `device` as an integer."""
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+def _device(device) -> torch.device:
+    d = torch.device(device)
+    d = torch.device("cuda", torch.cuda.current_device()) if d.index is None else d
+    torch.cuda.set_device(d)
+    return d
 
 
 class PagedCache:
@@ -568,8 +580,8 @@ class PagedCache:
 
     def __init__(self, *, layers, pages, page_size, kv_heads, head_dim, max_seqs, max_pages, dtype=PCOMOE_BF16, k=None, v=None,
                  book=None, device="cuda:0"):
-        self.device = k.device if k is not None else torch.device(device)
-        torch.cuda.set_device(self.device)
+        self.device = _device(k.device if k is not None else device)
+        self._lib = load_library()
         shape = (layers, pages, kv_heads, page_size, head_dim)
         n = max_seqs + pages + max_seqs * max_pages
         self.k = torch.zeros(shape, dtype=_TORCH[dtype], device=self.device) if k is None else k
@@ -598,47 +610,44 @@ class PagedCache:
     def reserve(self, seqs, add):
         """Room for add[i] more tokens in sequence seqs[i]."""
         n = seqs.numel()
-        _ints(seqs, self.device, n), _ints(add, self.device, n)
-        _check(load_library().pcomoe_cache_reserve(self._ref, n, seqs.data_ptr(), add.data_ptr(), *self._ws, _stream()),
-               "pcomoe_cache_reserve")
+        _check(self._lib.pcomoe_cache_reserve(self._ref, n, _ints(seqs, self.device, n), _ints(add, self.device, n), *self._ws,
+                                              _raw_stream(self.device)), "pcomoe_cache_reserve")
 
     def write(self, k, v, seqs, cu_len, layer: int = 0):
         """Packed rows k, v [T, kv_heads, head_dim] into the last positions of the sequences in one layer, or
         [n_layers, T, kv_heads, head_dim] into that many layers from `layer` on."""
         n = seqs.numel()
-        _ints(seqs, self.device, n), _ints(cu_len, self.device, n + 1)
-        assert k.dim() in (3, 4) and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype == _TORCH[self.dtype]
-        assert tuple(k.shape[-2:]) == (self.kv_heads, self.head_dim) and k.stride(-1) == 1 and k.stride(-2) == self.head_dim
         many = k.dim() == 4
-        _check(load_library().pcomoe_cache_write(self._ref, layer, k.shape[0] if many else 1, k.shape[-3], n, seqs.data_ptr(),
-                                                 cu_len.data_ptr(), k.data_ptr(), v.data_ptr(), _row_stride(k),
-                                                 k.stride(0) if many else 0, *self._ws, _stream()), "pcomoe_cache_write")
+        assert (many or k.dim() == 3) and k.shape == v.shape and k.stride() == v.stride() and k.dtype is v.dtype is _TORCH[self.dtype]
+        assert k.shape[-2] == self.kv_heads and k.shape[-1] == self.head_dim and k.stride(-1) == 1 and \
+            (self.kv_heads == 1 or k.stride(-2) == self.head_dim) and k.device == v.device == self.device
+        _check(self._lib.pcomoe_cache_write(self._ref, layer, k.shape[0] if many else 1, k.shape[-3], n, _ints(seqs, self.device, n),
+                                            _ints(cu_len, self.device, n + 1), k.data_ptr(), v.data_ptr(), _row_stride(k),
+                                            k.stride(0) if many else 0, *self._ws, _raw_stream(self.device)), "pcomoe_cache_write")
 
     def fork(self, parents, children):
         """Sequence children[i] becomes a copy of parents[i] that shares its pages."""
         n = parents.numel()
-        _ints(parents, self.device, n), _ints(children, self.device, n)
-        _check(load_library().pcomoe_cache_fork(self._ref, n, parents.data_ptr(), children.data_ptr(), *self._ws, _stream()),
-               "pcomoe_cache_fork")
+        _check(self._lib.pcomoe_cache_fork(self._ref, n, _ints(parents, self.device, n), _ints(children, self.device, n), *self._ws,
+                                           _raw_stream(self.device)), "pcomoe_cache_fork")
 
     def keep(self, seqs, cu_len, keep, n_keep):
         """Of the last cu_len[i+1] - cu_len[i] (drafted) positions of seqs[i] those numbered keep[i, :n_keep[i]] stay."""
         n = seqs.numel()
-        _ints(seqs, self.device, n), _ints(cu_len, self.device, n + 1), _ints(n_keep, self.device, n)
-        _ints(keep, self.device, n, keep.shape[1])
-        _check(load_library().pcomoe_cache_keep(self._ref, n, seqs.data_ptr(), cu_len.data_ptr(), keep.data_ptr(), keep.shape[1],
-                                                n_keep.data_ptr(), *self._ws, _stream()), "pcomoe_cache_keep")
+        assert keep.dim() == 2 and keep.shape[0] == n
+        _check(self._lib.pcomoe_cache_keep(self._ref, n, _ints(seqs, self.device, n), _ints(cu_len, self.device, n + 1),
+                                           _ints(keep, self.device, keep.numel()), keep.shape[1], _ints(n_keep, self.device, n), *self._ws,
+                                           _raw_stream(self.device)), "pcomoe_cache_keep")
 
     def trim(self, seqs, lens):
         """Shortens sequence seqs[i] to lens[i] tokens; 0 frees it."""
         n = seqs.numel()
-        _ints(seqs, self.device, n), _ints(lens, self.device, n)
-        _check(load_library().pcomoe_cache_trim(self._ref, n, seqs.data_ptr(), lens.data_ptr(), *self._ws, _stream()),
-               "pcomoe_cache_trim")
+        _check(self._lib.pcomoe_cache_trim(self._ref, n, _ints(seqs, self.device, n), _ints(lens, self.device, n), *self._ws,
+                                           _raw_stream(self.device)), "pcomoe_cache_trim")
 
     def compact(self):
         """Moves the pages in use to the lowest ids."""
-        _check(load_library().pcomoe_cache_compact(self._ref, *self._ws, _stream()), "pcomoe_cache_compact")
+        _check(self._lib.pcomoe_cache_compact(self._ref, *self._ws, _raw_stream(self.device)), "pcomoe_cache_compact")
 
     def device_status(self) -> int:
         return pcomoe_device_status(self.workspace)
@@ -654,44 +663,50 @@ class Attention:
     rows, the default outputs ``out`` [max_tokens, q_heads, head_dim] and ``lse`` [max_tokens, q_heads] fp32."""
 
     def __init__(self, *, q_heads, kv_heads, head_dim, max_tokens, max_seqs, dtype=PCOMOE_BF16, scale=None, device="cuda:0"):
-        self.device = torch.device(device)
-        torch.cuda.set_device(self.device)
+        self.device = _device(device)
+        self._lib = load_library()
         self.q_heads, self.kv_heads, self.head_dim, self.dtype = q_heads, kv_heads, head_dim, dtype
+        self._torch = _TORCH[dtype]
         self.max_tokens, self.max_seqs = max_tokens, max_seqs
         self.cfg = pcomoe_attn_config(ctypes.sizeof(pcomoe_attn_config), q_heads, kv_heads, head_dim, dtype,
                                       head_dim ** -0.5 if scale is None else scale)
         self._cfg = ctypes.byref(self.cfg)
         size = ctypes.c_size_t(0)
-        _check(load_library().pcomoe_attn_workspace_bytes(self._cfg, ctypes.byref(size)), "pcomoe_attn_workspace_bytes")
+        _check(self._lib.pcomoe_attn_workspace_bytes(self._cfg, ctypes.byref(size)), "pcomoe_attn_workspace_bytes")
         self.workspace = torch.empty(size.value, dtype=torch.uint8, device=self.device)
         self.workspace[:PCOMOE_ATTN_ZERO_BYTES].zero_()          # status words and counters start from zero
         self._ws = (self.workspace.data_ptr(), size.value)
         T = max(max_tokens, 1)
         self.out = torch.empty(T, q_heads, head_dim, dtype=_TORCH[dtype], device=self.device)
         self.lse = torch.empty(T, q_heads, dtype=torch.float32, device=self.device)
+        self._own = (T, self.out, self.lse)                      # the outputs as the last batch's size cuts them
 
-    def _rows(self, x, heads):
-        assert x.dim() == 3 and tuple(x.shape[1:]) == (heads, self.head_dim) and x.dtype == _TORCH[self.dtype] and \
-            x.device.type == "cuda" and x.stride(2) == 1 and (heads == 1 or x.stride(1) == self.head_dim), (x.shape, x.stride(), x.dtype)
-        return x.data_ptr(), _row_stride(x)
+    def _rows(self, x, T, heads):
+        """Pointer and row stride of packed rows [T, heads, head_dim]."""
+        shape, (row, head, one) = x.shape, x.stride()
+        assert shape[0] == T and shape[1] == heads and shape[2] == self.head_dim and x.dtype is self._torch and one == 1 and \
+            (head == self.head_dim or heads == 1) and x.device == self.device, (shape, x.stride(), x.dtype, x.device)
+        return x.data_ptr(), row if T > 1 else heads * self.head_dim
 
     def _outputs(self, T, out, lse):
-        assert (out is not None and lse is not None) or T <= self.max_tokens
-        out = self.out[:T] if out is None else out
-        lse = self.lse[:T] if lse is None else lse
-        assert out.shape[0] == T and tuple(lse.shape) == (T, self.q_heads) and lse.is_contiguous() and lse.dtype == torch.float32
+        if out is None or lse is None:
+            assert T <= self.max_tokens
+            if self._own[0] != T:
+                self._own = (T, self.out[:T], self.lse[:T])
+            out = self._own[1] if out is None else out
+            lse = self._own[2] if lse is None else lse
+        assert lse.shape[0] == T and lse.shape[1] == self.q_heads and lse.is_contiguous() and lse.dtype is torch.float32
         return out, lse
 
     def prompt(self, q, k, v, cu_len, out=None, lse=None):
         """Causal attention over packed prompts: q [T, q_heads, D], k and v [T, kv_heads, D] (column ranges of a fused
         projection are fine), cu_len [n+1] int32 on the device.  Returns (out, lse)."""
         T, n = q.shape[0], cu_len.numel() - 1
-        assert n <= self.max_seqs and k.shape[0] == T and v.shape[0] == T
-        _ints(cu_len, self.device, n + 1)
+        assert n <= self.max_seqs
         out, lse = self._outputs(T, out, lse)
-        _check(load_library().pcomoe_attn_prompt(self._cfg, T, n, cu_len.data_ptr(), *self._rows(q, self.q_heads),
-                                                 *self._rows(k, self.kv_heads), *self._rows(v, self.kv_heads),
-                                                 *self._rows(out, self.q_heads), lse.data_ptr(), *self._ws, _stream()),
+        _check(self._lib.pcomoe_attn_prompt(self._cfg, T, n, _ints(cu_len, self.device, n + 1), *self._rows(q, T, self.q_heads),
+                                            *self._rows(k, T, self.kv_heads), *self._rows(v, T, self.kv_heads),
+                                            *self._rows(out, T, self.q_heads), lse.data_ptr(), *self._ws, _raw_stream(self.device)),
                "pcomoe_attn_prompt")
         return out, lse
 
@@ -701,15 +716,14 @@ class Attention:
         is a decode step.  Returns (out, lse)."""
         T, n = q.shape[0], seqs.numel()
         assert n <= self.max_seqs
-        _ints(seqs, self.device, n), _ints(cu_len, self.device, n + 1)
-        words = 0
+        mask, words = None, 0
         if tree_mask is not None:
             words = tree_mask.shape[1]
-            _ints(tree_mask, self.device, T, words)
+            mask = _ints(tree_mask, self.device, T * words)
         out, lse = self._outputs(T, out, lse)
-        _check(load_library().pcomoe_attn_cached(self._cfg, cache._ref, layer, T, n, seqs.data_ptr(), cu_len.data_ptr(),
-                                                 *self._rows(q, self.q_heads), None if tree_mask is None else tree_mask.data_ptr(),
-                                                 words, *self._rows(out, self.q_heads), lse.data_ptr(), *self._ws, _stream()),
+        _check(self._lib.pcomoe_attn_cached(self._cfg, cache._ref, layer, T, n, _ints(seqs, self.device, n),
+                                            _ints(cu_len, self.device, n + 1), *self._rows(q, T, self.q_heads), mask, words,
+                                            *self._rows(out, T, self.q_heads), lse.data_ptr(), *self._ws, _raw_stream(self.device)),
                "pcomoe_attn_cached")
         return out, lse
 
@@ -721,27 +735,29 @@ class TokenScores:
     """pcomoe_token_logprobs for up to `max_tokens` rows.  Owns the outputs."""
 
     def __init__(self, *, max_tokens, top_n=0, device="cuda:0"):
-        self.device = torch.device(device)
-        torch.cuda.set_device(self.device)
+        self.device = _device(device)
+        self._lib = load_library()
         self.max_tokens, self.top_n = max_tokens, top_n
         T = max(max_tokens, 1)
         f32 = dict(dtype=torch.float32, device=self.device)
         self.logprob, self.entropy, self.top_logprob = torch.empty(T, **f32), torch.empty(T, **f32), torch.empty(T, top_n, **f32)
         self.top_ids = torch.empty(T, top_n, dtype=torch.int32, device=self.device)
+        self._out = (self.logprob.data_ptr(), self.entropy.data_ptr(), self.top_ids.data_ptr(), self.top_logprob.data_ptr())
+        self._own = (T, (self.logprob, self.entropy, self.top_ids, self.top_logprob))
 
     def score(self, logits, tokens):
         """logits [T, V] bf16 or fp32, tokens [T] int32.  Returns (logprob [T], entropy [T], top_ids [T, top_n],
         top_logprob [T, top_n])."""
         T, V = logits.shape
-        assert T <= self.max_tokens and logits.stride(1) == 1 and logits.device.type == "cuda"
-        _ints(tokens, self.device, T)
-        dtype = PCOMOE_BF16 if logits.dtype == torch.bfloat16 else PCOMOE_FP32
-        assert logits.dtype == _TORCH[dtype], logits.dtype
-        _check(load_library().pcomoe_token_logprobs(dtype, T, V, logits.data_ptr(), logits.stride(0) if T > 1 else V, tokens.data_ptr(),
-                                                    self.top_n, self.logprob.data_ptr(), self.entropy.data_ptr(),
-                                                    self.top_ids.data_ptr(), self.top_logprob.data_ptr(), _stream()),
-               "pcomoe_token_logprobs")
-        return self.logprob[:T], self.entropy[:T], self.top_ids[:T], self.top_logprob[:T]
+        row, one = logits.stride()
+        assert T <= self.max_tokens and one == 1 and logits.device == self.device
+        dtype = PCOMOE_BF16 if logits.dtype is torch.bfloat16 else PCOMOE_FP32
+        assert logits.dtype is _TORCH[dtype], logits.dtype
+        _check(self._lib.pcomoe_token_logprobs(dtype, T, V, logits.data_ptr(), row if T > 1 else V, _ints(tokens, self.device, T),
+                                               self.top_n, *self._out, _raw_stream(self.device)), "pcomoe_token_logprobs")
+        if self._own[0] != T:
+            self._own = (T, (self.logprob[:T], self.entropy[:T], self.top_ids[:T], self.top_logprob[:T]))
+        return self._own[1]
 
 
 def to_device(arr: np.ndarray | None, device="cuda:0"):

@@ -1,11 +1,12 @@
 // Scores of tokens from logits: log probability of a given token, entropy, the best words, in one read of the logits.
 //
-// Mathematics.  With a reference m and e_i = exp(x_i - m): s = sum e_i and w = sum e_i (x_i - m) give
-//   logZ = m + ln s,   H = logZ - sum p x = ln s - w / s.
-// Moving the reference from m to m' multiplies s by r = exp(m - m') and turns w into r (w + s (m - m')), so both are
-// kept while the maximum grows and partial results of different references join exactly.  The difference x - m is formed
-// before it is scaled for the base-2 exponential, and held above -700 (exp gives 0 from -104 on): rows of the type's
-// lowest value, masked words and NaN need no case of their own.
+// Mathematics, base 2 (c = log2 e).  With a reference word m, M = c m rounded, r = c m - M, and d_i = c x_i - M, formed by one
+// FMA: s = sum 2^d_i and w = sum 2^d_i d_i give
+//   log p_i = (x_i - m) + ln 2 (r - log2 s),   H = ln 2 (log2 s - w / s).
+// Moving the reference by D (from m to m': D = c (m - m') - r + r') multiplies s by 2^D and turns w into 2^D (w + s D), so
+// both are kept while the maximum grows and partial results of different references join.  A d_i far below the reference
+// must not be -inf (0 times it is NaN): words are held above -1e30 first, NaN and -inf with them (two bf16 in one operation).
+// Rows whose maximum is 1e6 or more away from zero (a mask's lowest value, say) take d_i = c (x_i - m) instead, with r = 0.
 //
 // Best words.  A warp reads 512 contiguous bytes of a row at a time (256 bf16 or 128 fp32 words, one 16-byte load per lane): a
 // group.  The n best words under (value descending, id ascending) lie in the n best groups under (largest value
@@ -13,7 +14,9 @@
 // largest value of every group, and afterwards at most n groups are read again (from L2) and ranked.
 //
 // What bounds it: HBM, with the exponentials close behind for bf16 (11.5 words per clock and SM at the copy rate, the
-// special function unit does 16).
+// special function unit does 16).  What comes after the pass over a row is a chain of short steps that few threads take
+// part in, so with many rows a row belongs to two or four warps and other rows' passes fill the gaps; with fewer rows to a
+// block or to a cluster of up to 16 blocks.
 #include <algorithm>
 #include <climits>
 #include <type_traits>
@@ -23,12 +26,9 @@
 namespace pcomoe {
 namespace {
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxTop = 32;
 constexpr int kMaxVocab = 1 << 20;
-constexpr int kMaxCand = 1024;
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLeast = -700.f;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNone = -INFINITY;
 
 // Order of floats as integers (-inf lowest of what occurs here); kNoKey: nothing eligible.
@@ -41,15 +41,56 @@ constexpr int kNoKey = (int)0x807fffff;                  // key_of(-inf)
 
 __device__ __forceinline__ float eligible(float x) { return fabsf(x) < INFINITY ? x : kNone; }
 
-template <typename T> struct Vec;                        // words of one 16-byte load
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(*(uint64_t *)&a), "l"(*(uint64_t *)&b), "l"(*(uint64_t *)&c));
+  return *(float2 *)&d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*(uint64_t *)&a), "l"(*(uint64_t *)&b));
+  return *(float2 *)&d;
+}
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {      // NaN loses
+  uint32_t d;
+  asm("max.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+
+// The words of one 16-byte load.
+template <typename T> struct Vec;
 template <> struct Vec<__nv_bfloat16> {
   static constexpr int N = 8;
+  static __device__ __forceinline__ float lo(uint32_t u) { return __uint_as_float(u << 16); }
+  static __device__ __forceinline__ float hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
   static __device__ __forceinline__ void unpack(const uint4 &v, float *x) {
     const uint32_t u[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = lo(u[i]); x[2 * i + 1] = hi(u[i]); }
+  }
+  static __device__ __forceinline__ uint4 pack(const float *x) {       // exact: words and -inf
+    uint4 v;
+    uint32_t *u = &v.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = (__float_as_uint(x[2 * i]) >> 16) | (__float_as_uint(x[2 * i + 1]) & 0xffff0000u);
+    return v;
+  }
+  static __device__ __forceinline__ float largest(const uint4 &v) {    // of those that are no NaN (NaN if none is)
+    const uint32_t m = max_bf16x2(max_bf16x2(v.x, v.y), max_bf16x2(v.z, v.w));
+    return fmaxf(lo(m), hi(m));
+  }
+  // pairs of words held above -1e30
+  static __device__ __forceinline__ void pairs(const uint4 &v, float2 *x) {
+    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
     for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float(u[i] << 16);
-      x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+      const uint32_t w = max_bf16x2(u[i], 0xf149f149u);                // -1e30 in bf16
+      x[i] = make_float2(lo(w), hi(w));
     }
   }
   static __device__ __forceinline__ float one(const __nv_bfloat16 *p) { return __bfloat162float(*p); }
@@ -59,23 +100,32 @@ template <> struct Vec<float> {
   static __device__ __forceinline__ void unpack(const uint4 &v, float *x) {
     x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y); x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
   }
+  static __device__ __forceinline__ uint4 pack(const float *x) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+  static __device__ __forceinline__ float largest(const uint4 &v) {
+    return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+  }
+  static __device__ __forceinline__ void pairs(const uint4 &v, float2 *x) {
+    x[0] = make_float2(fmaxf(__uint_as_float(v.x), -1e30f), fmaxf(__uint_as_float(v.y), -1e30f));
+    x[1] = make_float2(fmaxf(__uint_as_float(v.z), -1e30f), fmaxf(__uint_as_float(v.w), -1e30f));
+  }
   static __device__ __forceinline__ float one(const float *p) { return *p; }
 };
 
-__device__ __forceinline__ float exp_fast(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * kLog2e));
-  return y;
-}
-
 struct Sums { float m, s, w; };                          // reference, sum, weighted sum
+
+__device__ __forceinline__ bool plain_range(float m) { return fabsf(m) < 1e6f; }
+__device__ __forceinline__ float rest(float m) { return plain_range(m) ? fmaf(m, kLog2e, -(m * kLog2e)) : 0.f; }
+// by how much sums over reference `from` are lower over reference `to` (0 or less, and never -inf)
+__device__ __forceinline__ float shift_of(float from, float to) { return fmaxf(fmaf(from - to, kLog2e, rest(to) - rest(from)), -1000.f); }
 
 __device__ __forceinline__ Sums join(const Sums &a, const Sums &b) {
   if (a.s == 0.f) return b;
   if (b.s == 0.f) return a;
   const float m = fmaxf(a.m, b.m);
-  const float da = fmaxf(a.m - m, kLeast), db = fmaxf(b.m - m, kLeast);
-  const float ra = exp_fast(da), rb = exp_fast(db);
+  const float da = shift_of(a.m, m), db = shift_of(b.m, m);
+  const float ra = ex2(da), rb = ex2(db);
   return {m, a.s * ra + b.s * rb, ra * (a.w + a.s * da) + rb * (b.w + b.s * db)};
 }
 
@@ -83,123 +133,185 @@ struct Args {
   const char *x;
   int64_t row_bytes;
   int T, V, top;
+  int group_room;                                        // places of a team's group list
   const int32_t *tokens;
   float *logprob, *entropy, *top_lp;
   int32_t *top_ids;
 };
 
-// The words of group g that this lane holds.  Word ids begin at -shift: the row starts `shift` words after a 16-byte
-// boundary, and the words before its start or past its end do not exist.
+// The words of group g that this lane holds, as they lie in memory.  Word ids begin at -shift: the row starts `shift` words
+// after a 16-byte boundary, and words before its start or past its end are -inf.
 template <typename T>
-__device__ __forceinline__ void load_words(const T *row, int shift, int V, int g, int lane, float *x) {
+__device__ __forceinline__ uint4 load_raw(const T *row, int shift, int V, int g, int lane) {
   constexpr int N = Vec<T>::N;
   const int i = (g * 32 + lane) * N - shift;
-  if (i >= 0 && i + N <= V) {
-    Vec<T>::unpack(__ldcs((const uint4 *)(row + i)), x);
-  } else {
+  if (i >= 0 && i + N <= V) return __ldcs((const uint4 *)(row + i));
+  float x[N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) x[k] = i + k >= 0 && i + k < V ? Vec<T>::one(row + i + k) : kNone;
-  }
+  for (int k = 0; k < N; ++k) x[k] = i + k >= 0 && i + k < V ? Vec<T>::one(row + i + k) : kNone;
+  return Vec<T>::pack(x);
+}
+template <typename T>
+__device__ __forceinline__ void load_words(const T *row, int shift, int V, int g, int lane, float *x) {
+  Vec<T>::unpack(load_raw<T>(row, shift, V, g, lane), x);
 }
 
-template <typename T, int CL>
-__global__ void __launch_bounds__(kThreads) scores_kernel(Args a) {
+// W warps (a team) per row and block-wide share of it, CL blocks (a cluster) per row; W < kWarps only with CL = 1, where
+// a block holds several teams.
+template <typename T, int kWarps, int W, int CL>
+__global__ void __launch_bounds__(32 * kWarps) scores_kernel(Args a) {
   pdl_grid_wait();
-  constexpr int N = Vec<T>::N, kUnroll = 32 / N;
-  extern __shared__ int s_group[];                       // largest value of every group of this block, as keys
-  __shared__ Sums s_sums[kWarps];
-  __shared__ int s_pick[kMaxTop], s_ckey[kMaxCand], s_cid[kMaxCand], s_nc;
-  __shared__ struct { Sums sums; int key[kMaxTop], id[kMaxTop]; } s_out;      // what the cluster's first block collects
-  __shared__ float s_m, s_lns;                           // log p = (x - m) - ln s: exact where x is near the largest
-  __shared__ int s_count[kWarps];
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  constexpr int N = Vec<T>::N, kLoads = 4, kTeams = kWarps / W, kThreads = 32 * W;      // threads of a team
+  constexpr int kMaxCand = 1024 / kTeams > 512 ? 512 : 1024 / kTeams;
+  static_assert(W == kWarps || CL == 1, "teams or clusters");
+  extern __shared__ int s_all_groups[];                  // largest value of every group of this block's share, as keys
+  struct Team {
+    Sums sums[W];
+    int pick[kMaxTop], ckey[kMaxCand], cid[kMaxCand], nc, count[W];
+    struct { Sums sums; int key[kMaxTop], id[kMaxTop]; } out;      // what the cluster's first block collects
+    float m, tail;                                       // reference, ln 2 (r - log2 s)
+  };
+  __shared__ Team s_team[kTeams];
+  const int lane = threadIdx.x & 31, team = (threadIdx.x >> 5) / W, warp = (threadIdx.x >> 5) % W, tid = warp * 32 + lane;
+  Team &s = s_team[team];
+  auto sync = [&]() {
+    if (W == kWarps) __syncthreads();
+    else asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "n"(kThreads) : "memory");
+  };
   const int rank = CL > 1 ? (int)(blockIdx.x % CL) : 0;
-  const int t = blockIdx.x / CL;
+  const int t = blockIdx.x / CL * kTeams + team;
+  if (t >= a.T) return;                                  // a whole team (never with CL > 1)
   const T *row = (const T *)(a.x + (int64_t)t * a.row_bytes);
   const int shift = (int)(((uintptr_t)row & 15) / sizeof(T));
   const int groups = (a.V + shift + 32 * N - 1) / (32 * N);
   const int per = (groups + CL - 1) / CL;
-  const int g0 = min(rank * per, groups), g1 = min(g0 + per, groups);
+  const int g0 = min(rank * per, groups), g1 = min(g0 + per, groups), G = g1 - g0;
+  int *s_group = s_all_groups + team * a.group_room;
 
   Sums acc = {0.f, 0.f, 0.f};                            // of this lane; the reference is the warp's
-  bool first = true;
-  for (int g = g0 + warp * kUnroll; g < g1; g += kWarps * kUnroll) {
-    float x[kUnroll][N];
+  float most_so_far = kNone;
+  uint4 raw[kLoads];
+  auto fetch = [&](int g) {
+    // all inside the row: no lane looks at its place
+    if (g * 32 * N >= shift && (g + kLoads) * 32 * N - shift <= a.V && g + kLoads <= g1) {
+      const uint4 *p = (const uint4 *)(row - shift) + g * 32 + lane;
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) raw[u] = __ldcs(p + 32 * u);
+    } else {
+      float none[N];
+#pragma unroll
+      for (int k = 0; k < N; ++k) none[k] = kNone;
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) raw[u] = g + u < g1 ? load_raw<T>(row, shift, a.V, g + u, lane) : Vec<T>::pack(none);
+    }
+  };
+  int g = g0 + warp * kLoads;
+  if (g < g1) fetch(g);
+  for (; g < g1; g += W * kLoads) {
+    uint4 v[kLoads];
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) v[u] = raw[u];
+    if (g + W * kLoads < g1) fetch(g + W * kLoads);      // on its way while this one is summed
     int most = kNoKey;
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      if (g + u < g1) {
-        load_words<T>(row, shift, a.V, g + u, lane, x[u]);
-      } else {
-#pragma unroll
-        for (int k = 0; k < N; ++k) x[u][k] = kNone;
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      float mx = x[u][0];
-#pragma unroll
-      for (int k = 1; k < N; ++k) mx = fmaxf(mx, x[u][k]);
+    for (int u = 0; u < kLoads; ++u) {
+      const float mx = Vec<T>::largest(v[u]);
       int key = __reduce_max_sync(~0u, mx == mx ? key_of(mx) : kNoKey);
       if (key >= key_of(INFINITY)) {                     // an infinite logit: it does not count
-        mx = kNone;
+        float x[N];
+        Vec<T>::unpack(v[u], x);
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-          x[u][k] = eligible(x[u][k]);
-          mx = fmaxf(mx, x[u][k]);
-        }
-        key = __reduce_max_sync(~0u, key_of(mx));
+        for (int k = 0; k < N; ++k) x[k] = eligible(x[k]);
+        v[u] = Vec<T>::pack(x);
+        key = __reduce_max_sync(~0u, key_of(Vec<T>::largest(v[u])));
       }
       if (lane == 0 && g + u < g1) s_group[g + u - g0] = key;
       most = max(most, key);
     }
     if (most == kNoKey) continue;
     const float m = of_key(most);
-    if (first || m > acc.m) {
-      if (!first) {
-        const float d = fmaxf(acc.m - m, kLeast), r = exp_fast(d);
+    if (m > most_so_far) {
+      if (acc.s > 0.f) {
+        const float d = shift_of(acc.m, m), r = ex2(d);
         acc.w = r * (acc.w + acc.s * d);
         acc.s *= r;
       }
-      acc.m = m;
-      first = false;
+      acc.m = most_so_far = m;
     }
+    if (plain_range(acc.m)) {
+      const float2 c = make_float2(kLog2e, kLog2e), minus = make_float2(-(acc.m * kLog2e), -(acc.m * kLog2e));
+      float2 s2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)}, w2[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
+      for (int u = 0; u < kLoads; ++u) {
+        float2 x[N / 2];
+        Vec<T>::pairs(v[u], x);
 #pragma unroll
-      for (int k = 0; k < N; ++k) {
-        const float d = fmaxf(x[u][k] - acc.m, kLeast);
-        const float e = exp_fast(d);
-        acc.s += e;
-        acc.w = fmaf(e, d, acc.w);
+        for (int k = 0; k < N / 2; ++k) {
+          const float2 d = fma2(x[k], c, minus);
+          const float2 e = make_float2(ex2(d.x), ex2(d.y));
+          s2[k & 1] = add2(s2[k & 1], e);
+          w2[k & 1] = fma2(e, d, w2[k & 1]);
+        }
       }
+      const float2 st = add2(s2[0], s2[1]), wt = add2(w2[0], w2[1]);
+      acc.s += st.x + st.y;
+      acc.w += wt.x + wt.y;
+    } else {
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {
+        float x[N];
+        Vec<T>::unpack(v[u], x);
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          const float d = fmaxf((eligible(x[k]) - acc.m) * kLog2e, -1000.f);
+          const float e = ex2(d);
+          acc.s += e;
+          acc.w = fmaf(e, d, acc.w);
+        }
+      }
+    }
   }
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
     acc.s += __shfl_xor_sync(~0u, acc.s, o);
     acc.w += __shfl_xor_sync(~0u, acc.w, o);
   }
-  if (lane == 0) s_sums[warp] = acc;
-  if (tid == 0) s_nc = 0;
-  __syncthreads();
+  if (lane == 0) s.sums[warp] = acc;
+  if (tid == 0) s.nc = 0;
+  const int want = a.top;
+  if (tid < want) { s.pick[tid] = -1; s.out.key[tid] = kNoKey; s.out.id[tid] = -1; }
+  sync();
 
-  const int G = g1 - g0, want = a.top;
-  if (warp == 0) {
-    if (lane == 0) {
-      Sums all = s_sums[0];
-      for (int i = 1; i < kWarps; ++i) all = join(all, s_sums[i]);
-      s_out.sums = all;
-    }
-    // the `want` best groups, one after another: every lane knows its best one (lane, lane + 32, ...)
-    if (want) {
+  if (tid == 0) {
+    Sums all = s.sums[0];
+    for (int i = 1; i < W; ++i) all = join(all, s.sums[i]);
+    s.out.sums = all;
+  }
+  if (want) {
+    // the `want` best groups
+    if (W >= 8 && G <= 4 * kThreads) {
+      // by counting the better ones
+      for (int g = tid; g < G; g += kThreads) {
+        const int key = s_group[g];
+        if (key == kNoKey) continue;
+        int r = 0;
+#pragma unroll 8
+        for (int j = 0; j < G; ++j) {
+          const int k = s_group[j];
+          r += k > key || (k == key && j < g);
+        }
+        if (r < want) s.pick[r] = g;
+      }
+    } else if (warp == 0) {
+      // one after another: every lane knows its best one of lane, lane + 32, ...
       int best = kNoKey, at = INT_MAX;
       for (int g = lane; g < G; g += 32)
         if (s_group[g] > best) { best = s_group[g]; at = g; }
       for (int i = 0; i < want; ++i) {
         const int top = __reduce_max_sync(~0u, best);
         const int pick = (int)__reduce_min_sync(~0u, best == top && top != kNoKey ? (unsigned)at : (unsigned)INT_MAX);
-        if (lane == 0) s_pick[i] = pick == INT_MAX ? -1 : pick;
-        if (pick == INT_MAX) continue;
+        if (pick == INT_MAX) break;
+        if (lane == 0) s.pick[i] = pick;
         if (at == pick) {                                // the next best of this lane: lower, or equal and further on
           int b2 = kNoKey, a2 = INT_MAX;
           for (int g = lane; g < G; g += 32) {
@@ -211,24 +323,22 @@ __global__ void __launch_bounds__(kThreads) scores_kernel(Args a) {
         }
       }
     }
-  }
-  if (want) {
-    __syncthreads();
+    sync();
     // every word of the picked groups that reaches the last picked group's largest value may be among the best
     int n_pick = 0;
-    while (n_pick < want && s_pick[n_pick] >= 0) ++n_pick;
-    int floor_key = n_pick ? s_group[s_pick[n_pick - 1]] : INT_MAX;
+    while (n_pick < want && s.pick[n_pick] >= 0) ++n_pick;
+    int floor_key = n_pick ? s_group[s.pick[n_pick - 1]] : INT_MAX;
     if (n_pick && n_pick < want) {
       // fewer groups than ranks: the same bound from single lanes' words, by bisection of the key (the largest key that
       // at least `want` lanes reach)
-      constexpr int kMine = kMaxTop / kWarps;
+      constexpr int kMine = (kMaxTop + W - 1) / W;
       int most[kMine];
 #pragma unroll
       for (int q = 0; q < kMine; ++q) {
         most[q] = kNoKey;
-        if (warp + q * kWarps < n_pick) {
+        if (warp + q * W < n_pick) {
           float x[N];
-          load_words<T>(row, shift, a.V, g0 + s_pick[warp + q * kWarps], lane, x);
+          load_words<T>(row, shift, a.V, g0 + s.pick[warp + q * W], lane, x);
 #pragma unroll
           for (int k = 0; k < N; ++k) most[q] = max(most[q], key_of(eligible(x[k])));
         }
@@ -240,40 +350,40 @@ __global__ void __launch_bounds__(kThreads) scores_kernel(Args a) {
 #pragma unroll
         for (int q = 0; q < kMine; ++q) mine += most[q] >= mid;
         int all = __reduce_add_sync(~0u, mine);
-        if (lane == 0) s_count[warp] = all;
-        __syncthreads();
+        if (lane == 0) s.count[warp] = all;
+        sync();
         all = 0;
-        for (int q = 0; q < kWarps; ++q) all += s_count[q];
-        __syncthreads();
+        for (int q = 0; q < W; ++q) all += s.count[q];
+        sync();
         if (all >= want) lo = mid; else hi = mid;
       }
       floor_key = (int)lo;
     }
-    for (int i = warp; i < n_pick; i += kWarps) {
+#pragma unroll 4
+    for (int i = warp; i < n_pick; i += W) {
       float x[N];
-      const int g = g0 + s_pick[i];
+      const int g = g0 + s.pick[i];
       load_words<T>(row, shift, a.V, g, lane, x);
 #pragma unroll
       for (int k = 0; k < N; ++k) {
         const int key = key_of(eligible(x[k]));
         if (key >= floor_key) {
-          const int c = atomicAdd(&s_nc, 1);
+          const int c = atomicAdd(&s.nc, 1);
           if (c < kMaxCand) {
-            s_ckey[c] = key;
-            s_cid[c] = (g * 32 + lane) * N - shift + k;
+            s.ckey[c] = key;
+            s.cid[c] = (g * 32 + lane) * N - shift + k;
           }
         }
       }
     }
-    if (tid < want) { s_out.key[tid] = kNoKey; s_out.id[tid] = -1; }
-    __syncthreads();
-    const int nc = s_nc;
+    sync();
+    const int nc = s.nc;
     if (nc <= kMaxCand) {
       for (int c = tid; c < nc; c += kThreads) {
-        const int key = s_ckey[c], id = s_cid[c];
+        const int key = s.ckey[c], id = s.cid[c];
         int r = 0;
-        for (int j = 0; j < nc && r < want; ++j) r += s_ckey[j] > key || (s_ckey[j] == key && s_cid[j] < id);
-        if (r < want) { s_out.key[r] = key; s_out.id[r] = id; }
+        for (int j = 0; j < nc; ++j) r += s.ckey[j] > key || (s.ckey[j] == key && s.cid[j] < id);
+        if (r < want) { s.out.key[r] = key; s.out.id[r] = id; }
       }
     } else if (warp == 0) {
       // more equals than there is room for: rank after rank, the best word behind the last one in the order
@@ -282,7 +392,7 @@ __global__ void __launch_bounds__(kThreads) scores_kernel(Args a) {
         int bk = kNoKey, bid = INT_MAX;
         for (int p = 0; p < n_pick; ++p) {
           float x[N];
-          const int g = g0 + s_pick[p];
+          const int g = g0 + s.pick[p];
           load_words<T>(row, shift, a.V, g, lane, x);
 #pragma unroll
           for (int k = 0; k < N; ++k) {
@@ -293,7 +403,7 @@ __global__ void __launch_bounds__(kThreads) scores_kernel(Args a) {
         const int top = __reduce_max_sync(~0u, bk);
         const int id = (int)__reduce_min_sync(~0u, bk == top ? (unsigned)bid : (unsigned)INT_MAX);
         if (top == kNoKey) break;
-        if (lane == 0) { s_out.key[i] = top; s_out.id[i] = id; }
+        if (lane == 0) { s.out.key[i] = top; s.out.id[i] = id; }
         pk = top;
         pid = id;
       }
@@ -304,8 +414,7 @@ __global__ void __launch_bounds__(kThreads) scores_kernel(Args a) {
     asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
     if (rank == 0) {
       // the blocks' sums in rank order; their best words ranked against one another
-      if (tid == 0) s_nc = 0;
-      __syncthreads();
+      static_assert(CL == 1 || (CL * kMaxTop <= kThreads && CL * kMaxTop <= kMaxCand), "a thread per candidate");
       auto remote = [](const void *p, int r) {
         uint32_t l = (uint32_t)__cvta_generic_to_shared(p), q;
         asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(q) : "r"(l), "r"(r));
@@ -316,66 +425,75 @@ __global__ void __launch_bounds__(kThreads) scores_kernel(Args a) {
         asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v) : "r"(p));
         return v;
       };
-      if (tid == 0) {
-        Sums all = s_out.sums;
-        for (int r = 1; r < CL; ++r) {
-          const uint32_t q = remote(&s_out.sums, r);
-          all = join(all, Sums{__int_as_float(ld(q)), __int_as_float(ld(q + 4)), __int_as_float(ld(q + 8))});
+      if (warp == W - 1) {
+        Sums mine = {0.f, 0.f, 0.f};
+        if (lane < CL) {
+          const uint32_t q = remote(&s.out.sums, lane);
+          mine = Sums{__int_as_float(ld(q)), __int_as_float(ld(q + 4)), __int_as_float(ld(q + 8))};
         }
-        s_sums[0] = all;
+#pragma unroll
+        for (int o = 1; o < CL; o <<= 1) mine = join(mine, Sums{__shfl_down_sync(~0u, mine.m, o), __shfl_down_sync(~0u, mine.s, o), __shfl_down_sync(~0u, mine.w, o)});
+        if (lane == 0) s.sums[0] = mine;
       }
       for (int i = tid; i < CL * want; i += kThreads) {
-        s_ckey[i] = ld(remote(&s_out.key[i % want], i / want));
-        s_cid[i] = ld(remote(&s_out.id[i % want], i / want));
+        s.ckey[i] = ld(remote(&s.out.key[i % want], i / want));
+        s.cid[i] = ld(remote(&s.out.id[i % want], i / want));
       }
       __syncthreads();
-      if (tid == 0) s_out.sums = s_sums[0];
+      if (tid == 0) s.out.sums = s.sums[0];
       int key = kNoKey, id = -1, r = want;
-      const int c = tid;
-      static_assert(8 * kMaxTop <= kThreads, "a thread per candidate");
-      if (c < CL * want && (key = s_ckey[c]) != kNoKey) {
-        id = s_cid[c];
+      if (tid < CL * want && (key = s.ckey[tid]) != kNoKey) {
+        id = s.cid[tid];
         r = 0;
-        for (int j = 0; j < CL * want; ++j) r += s_ckey[j] > key || (s_ckey[j] == key && s_cid[j] < id && s_cid[j] >= 0);
+        for (int j = 0; j < CL * want; ++j) r += s.ckey[j] > key || (s.ckey[j] == key && s.cid[j] < id && s.cid[j] >= 0);
       }
       // this block's own list is read by nobody else, and by its own threads before the barrier above
-      if (tid < want) { s_out.key[tid] = kNoKey; s_out.id[tid] = -1; }
+      if (tid < want) { s.out.key[tid] = kNoKey; s.out.id[tid] = -1; }
       __syncthreads();
-      if (r < want) { s_out.key[r] = key; s_out.id[r] = id; }
+      if (r < want) { s.out.key[r] = key; s.out.id[r] = id; }
     }
     asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
     if (rank != 0) return;
   }
-  __syncthreads();
+  sync();
   if (tid == 0) {
-    const Sums all = s_out.sums;
+    const Sums all = s.out.sums;
     const bool any = all.s > 0.f;
-    const float ln_s = logf(all.s);
-    s_m = any ? all.m : 0.f;
-    s_lns = any ? ln_s : 0.f;
-    if (a.entropy) a.entropy[t] = any ? ln_s - all.w / all.s : 0.f;
+    const float log2s = any ? log2f(all.s) : 0.f;
+    s.m = any ? all.m : 0.f;
+    s.tail = any ? kLn2 * (rest(all.m) - log2s) : 0.f;
+    if (a.entropy) a.entropy[t] = any ? kLn2 * (log2s - all.w / all.s) : 0.f;
     if (a.logprob) {
       const int tok = a.tokens[t];
       float lp = 0.f;
       if (tok >= a.V) lp = NAN;
-      else if (tok >= 0) lp = eligible(Vec<T>::one(row + tok)) - s_m - s_lns;
+      else if (tok >= 0) lp = (eligible(Vec<T>::one(row + tok)) - s.m) + s.tail;
       a.logprob[t] = lp;
     }
   }
-  __syncthreads();
+  sync();
   if (tid < want) {
-    const int key = s_out.key[tid];
-    a.top_ids[(int64_t)t * want + tid] = s_out.id[tid];
-    a.top_lp[(int64_t)t * want + tid] = key == kNoKey ? kNone : of_key(key) - s_m - s_lns;
+    const int key = s.out.key[tid];
+    a.top_ids[(int64_t)t * want + tid] = s.out.id[tid];
+    a.top_lp[(int64_t)t * want + tid] = key == kNoKey ? kNone : (of_key(key) - s.m) + s.tail;
   }
 }
 
-template <typename T, int CL>
-cudaError_t launch(const Args &a, size_t smem, cudaStream_t st) {
+template <typename T, int kWarps, int W, int CL>
+pcomoe_status launch(Args a, int groups, cudaStream_t st) {
+  static PerDeviceOnce once;
+  int dev = -1;
+  PCOMOE_CUDA_TRY(cudaGetDevice(&dev));
+  if (CL > 8 && once.first_use(dev)) {
+    PCOMOE_CUDA_TRY(cudaFuncSetAttribute(scores_kernel<T, kWarps, W, CL>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    once.done(dev);
+  }
+  constexpr int kTeams = kWarps / W;
+  a.group_room = (groups + CL - 1) / CL;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)a.T * CL);
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.gridDim = dim3((unsigned)((a.T + kTeams - 1) / kTeams * CL));
+  cfg.blockDim = dim3(32 * kWarps);
+  cfg.dynamicSmemBytes = sizeof(int) * (size_t)a.group_room * kTeams;
   cfg.stream = st;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -384,24 +502,30 @@ cudaError_t launch(const Args &a, size_t smem, cudaStream_t st) {
   attr[1].val.clusterDim = {CL, 1, 1};
   cfg.attrs = attr;
   cfg.numAttrs = CL > 1 ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, scores_kernel<T, CL>, a);
+  PCOMOE_CUDA_TRY((cudaLaunchKernelEx(&cfg, scores_kernel<T, kWarps, W, CL>, a)));
+  count_launch();
+  return PCOMOE_OK;
 }
 
 template <typename T>
 pcomoe_status run(const Args &a, int sms, cudaStream_t st) {
   const int groups = (a.V + 15) / (32 * Vec<T>::N) + 1;
-  // blocks per row: enough rows fill the GPU by themselves; few rows are cut while a block keeps 16 groups
+  // Teams of 2 or 4 warps where there are rows enough to fill the GPU with them (24 warps per SM; 4096 rows of 32000 bf16
+  // words: 74 / 60 / 62 / 77 us with 1 / 2 / 4 / 8 warps, one warp per row leaving a ragged last wave), and no fewer than
+  // keep a team's group list inside 24 KB per block.
+  const auto fills = [&](int64_t warps) { return (int64_t)a.T * warps >= (int64_t)48 * sms; };
+  if (groups <= 1536 && fills(2)) return launch<T, 8, 2, 1>(a, groups, st);
+  if (groups <= 3072 && fills(4)) return launch<T, 8, 4, 1>(a, groups, st);
+  // then blocks of 8 warps, and with few rows clusters of blocks of 16 while a block keeps 16 groups
   int cl = 1;
-  while (cl < 8 && (int64_t)a.T * cl < 2 * sms && groups / (2 * cl) >= 16) cl *= 2;
-  const size_t smem = sizeof(int) * (size_t)((groups + cl - 1) / cl + 1);
+  while (cl < 16 && (int64_t)a.T * 2 * cl <= 2 * sms && groups / (2 * cl) >= 16) cl *= 2;
   switch (cl) {
-    case 1: PCOMOE_CUDA_TRY((launch<T, 1>(a, smem, st))); break;
-    case 2: PCOMOE_CUDA_TRY((launch<T, 2>(a, smem, st))); break;
-    case 4: PCOMOE_CUDA_TRY((launch<T, 4>(a, smem, st))); break;
-    default: PCOMOE_CUDA_TRY((launch<T, 8>(a, smem, st)));
+    case 1: return launch<T, 8, 8, 1>(a, groups, st);
+    case 2: return launch<T, 16, 16, 2>(a, groups, st);
+    case 4: return launch<T, 16, 16, 4>(a, groups, st);
+    case 8: return launch<T, 16, 16, 8>(a, groups, st);
+    default: return launch<T, 16, 16, 16>(a, groups, st);
   }
-  count_launch();
-  return PCOMOE_OK;
 }
 
 }  // namespace
@@ -420,10 +544,10 @@ extern "C" pcomoe_status pcomoe_token_logprobs(int32_t dtype, int32_t T, int32_t
   if (!d_logits || row_stride < V || (top_n > 0 && (!d_top_ids || !d_top_logprob)) || (d_tokens && !d_logprob) ||
       (!d_tokens && d_logprob) || ((uintptr_t)d_logits % e))
     return PCOMOE_ERR_INVALID_ARG;
-  if ((int64_t)T * 8 > INT32_MAX) return PCOMOE_ERR_SHAPE;
+  if ((int64_t)T * 16 > INT32_MAX) return PCOMOE_ERR_SHAPE;
   int sms;
   pcomoe_status st = current_sms(&sms);
   if (st != PCOMOE_OK) return st;
-  const Args a = {(const char *)d_logits, row_stride * e, T, V, top_n, d_tokens, d_logprob, d_entropy, d_top_logprob, d_top_ids};
+  const Args a = {(const char *)d_logits, row_stride * e, T, V, top_n, 0, d_tokens, d_logprob, d_entropy, d_top_logprob, d_top_ids};
   return dtype == PCOMOE_BF16 ? run<__nv_bfloat16>(a, sms, (cudaStream_t)stream) : run<float>(a, sms, (cudaStream_t)stream);
 }
