@@ -39,6 +39,11 @@ __device__ __forceinline__ int key_of(float x) {
 __device__ __forceinline__ float of_key(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7fffffff)); }
 constexpr int kNoKey = (int)0x807fffff;                  // key_of(-inf)
 
+// A word's place in the order: larger is better (value descending, then id ascending).
+__device__ __forceinline__ unsigned long long place_of(int key, int id) { return ((unsigned long long)((uint32_t)key ^ 0x80000000u) << 32) | (uint32_t)~id; }
+__device__ __forceinline__ int place_key(unsigned long long p) { return (int)((uint32_t)(p >> 32) ^ 0x80000000u); }
+__device__ __forceinline__ int place_id(unsigned long long p) { return (int)~(uint32_t)p; }
+
 __device__ __forceinline__ float eligible(float x) { return fabsf(x) < INFINITY ? x : kNone; }
 
 __device__ __forceinline__ float ex2(float x) {
@@ -167,7 +172,8 @@ __global__ void __launch_bounds__(32 * kWarps) scores_kernel(Args a) {
   extern __shared__ int s_all_groups[];                  // largest value of every group of this block's share, as keys
   struct Team {
     Sums sums[W];
-    int pick[kMaxTop], ckey[kMaxCand], cid[kMaxCand], nc, count[W];
+    unsigned long long cand[kMaxCand];
+    int pick[kMaxTop], nc, count[W];
     struct { Sums sums; int key[kMaxTop], id[kMaxTop]; } out;      // what the cluster's first block collects
     float m, tail;                                       // reference, ln 2 (r - log2 s)
   };
@@ -282,10 +288,12 @@ __global__ void __launch_bounds__(32 * kWarps) scores_kernel(Args a) {
   if (tid < want) { s.pick[tid] = -1; s.out.key[tid] = kNoKey; s.out.id[tid] = -1; }
   sync();
 
-  if (tid == 0) {
-    Sums all = s.sums[0];
-    for (int i = 1; i < W; ++i) all = join(all, s.sums[i]);
-    s.out.sums = all;
+  if (warp == W - 1) {
+    // the warps' sums, pairwise in a fixed order
+    Sums all = lane < W ? s.sums[lane] : Sums{0.f, 0.f, 0.f};
+#pragma unroll
+    for (int o = 1; o < W; o <<= 1) all = join(all, Sums{__shfl_down_sync(~0u, all.m, o), __shfl_down_sync(~0u, all.s, o), __shfl_down_sync(~0u, all.w, o)});
+    if (lane == 0) s.out.sums = all;
   }
   if (want) {
     // the `want` best groups
@@ -369,10 +377,7 @@ __global__ void __launch_bounds__(32 * kWarps) scores_kernel(Args a) {
         const int key = key_of(eligible(x[k]));
         if (key >= floor_key) {
           const int c = atomicAdd(&s.nc, 1);
-          if (c < kMaxCand) {
-            s.ckey[c] = key;
-            s.cid[c] = (g * 32 + lane) * N - shift + k;
-          }
+          if (c < kMaxCand) s.cand[c] = place_of(key, (g * 32 + lane) * N - shift + k);
         }
       }
     }
@@ -380,10 +385,11 @@ __global__ void __launch_bounds__(32 * kWarps) scores_kernel(Args a) {
     const int nc = s.nc;
     if (nc <= kMaxCand) {
       for (int c = tid; c < nc; c += kThreads) {
-        const int key = s.ckey[c], id = s.cid[c];
+        const unsigned long long p = s.cand[c];
         int r = 0;
-        for (int j = 0; j < nc; ++j) r += s.ckey[j] > key || (s.ckey[j] == key && s.cid[j] < id);
-        if (r < want) { s.out.key[r] = key; s.out.id[r] = id; }
+#pragma unroll 8
+        for (int j = 0; j < nc; ++j) r += s.cand[j] > p;
+        if (r < want) { s.out.key[r] = place_key(p); s.out.id[r] = place_id(p); }
       }
     } else if (warp == 0) {
       // more equals than there is room for: rank after rank, the best word behind the last one in the order
@@ -435,22 +441,27 @@ __global__ void __launch_bounds__(32 * kWarps) scores_kernel(Args a) {
         for (int o = 1; o < CL; o <<= 1) mine = join(mine, Sums{__shfl_down_sync(~0u, mine.m, o), __shfl_down_sync(~0u, mine.s, o), __shfl_down_sync(~0u, mine.w, o)});
         if (lane == 0) s.sums[0] = mine;
       }
-      for (int i = tid; i < CL * want; i += kThreads) {
-        s.ckey[i] = ld(remote(&s.out.key[i % want], i / want));
-        s.cid[i] = ld(remote(&s.out.id[i % want], i / want));
+      // a thread per candidate; blocks without enough words have (kNoKey, -1) in the rest of their lists
+      unsigned long long place = 0;
+      if (tid < CL * want) {
+        const int r = tid / want, i = tid - r * want;
+        const uint32_t q = remote(&s.out.key[i], r);
+        const int key = ld(q), id = ld(q + (uint32_t)sizeof(s.out.key));
+        place = key == kNoKey ? 0 : place_of(key, id);
+        s.cand[tid] = place;
       }
       __syncthreads();
       if (tid == 0) s.out.sums = s.sums[0];
-      int key = kNoKey, id = -1, r = want;
-      if (tid < CL * want && (key = s.ckey[tid]) != kNoKey) {
-        id = s.cid[tid];
+      int r = want;
+      if (place) {
         r = 0;
-        for (int j = 0; j < CL * want; ++j) r += s.ckey[j] > key || (s.ckey[j] == key && s.cid[j] < id && s.cid[j] >= 0);
+#pragma unroll 8
+        for (int j = 0; j < CL * want; ++j) r += s.cand[j] > place;
       }
       // this block's own list is read by nobody else, and by its own threads before the barrier above
       if (tid < want) { s.out.key[tid] = kNoKey; s.out.id[tid] = -1; }
       __syncthreads();
-      if (r < want) { s.out.key[r] = key; s.out.id[r] = id; }
+      if (r < want) { s.out.key[r] = place_key(place); s.out.id[r] = place_id(place); }
     }
     asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
     if (rank != 0) return;
