@@ -353,7 +353,7 @@ typedef struct {
 /* Bytes of device workspace of the two attention calls.  256-byte aligned; its first PCOMOE_ATTN_ZERO_BYTES must be zero
  * before its first use (status words and counters; the calls leave the counters at zero), the rest may hold anything,
  * and one call at a time may use it.  The size depends on the GPU, not on the batch.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED (head_dim), CUDA. */
-#define PCOMOE_ATTN_ZERO_BYTES (256u + 4u * 4096u)
+#define PCOMOE_ATTN_ZERO_BYTES 512u
 pcomoe_status pcomoe_attn_workspace_bytes(const pcomoe_attn_config *cfg, size_t *bytes);
 
 /*

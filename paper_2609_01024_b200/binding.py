@@ -19,7 +19,7 @@ STATUS_NAMES = {0: "OK", 1: "ERR_INVALID_ARG", 2: "ERR_SHAPE", 3: "ERR_WORKSPACE
                 5: "ERR_CUDA", 6: "ERR_TIMEOUT", 7: "ERR_INDEX",
                 8: "ERR_CACHE_FULL"}
 PCOMOE_BF16, PCOMOE_FP32 = 0, 1
-PCOMOE_ATTN_ZERO_BYTES = 256 + 4 * 4096
+PCOMOE_ATTN_ZERO_BYTES = 512
 PCOMOE_FFN_AUTO, PCOMOE_FFN_SIMT, PCOMOE_FFN_TCGEN05, PCOMOE_FFN_TCGEN05_PAIR = 0, 1, 2, 3
 
 EXPORTS = ["pcomoe_mask_from_bias", "pcomoe_mask_tighten", "pcomoe_layer_create", "pcomoe_layer_destroy", "pcomoe_layer_active_set", "pcomoe_workspace_bytes",

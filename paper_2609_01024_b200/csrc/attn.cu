@@ -17,9 +17,9 @@ pcomoe_status check_config(const pcomoe_attn_config *c) {
   return PCOMOE_OK;
 }
 
-// Workspace: status words, counters, partial results.
-constexpr size_t kCountersAt = 256, kPartAt = kCountersAt + sizeof(int32_t) * kAttnCounters;
-static_assert(kPartAt == PCOMOE_ATTN_ZERO_BYTES, "what the caller clears");
+// Workspace: status words, counters, records of unfinished tiles, partial results.
+constexpr size_t kCountersAt = 256, kRecsAt = 512, kPartAt = kRecsAt + ((sizeof(JoinRec) * kAttnMaxCtas + 255) & ~size_t(255));
+static_assert(kRecsAt == PCOMOE_ATTN_ZERO_BYTES, "what the caller clears");
 
 // rows of partial results: each D sums, a maximum and a sum
 size_t part_rows(const pcomoe_attn_config *c, int sms) {
@@ -34,6 +34,7 @@ pcomoe_status fill(AttnArgs &a, const pcomoe_attn_config *c, int32_t T, int32_t 
   if (n_seqs <= 0 || !cu || !q || !out) return PCOMOE_ERR_INVALID_ARG;
   const int64_t row = (int64_t)c->q_heads * c->head_dim;
   if (q_stride < row || out_stride < row) return PCOMOE_ERR_INVALID_ARG;
+  if (2 * sms > kAttnMaxCtas) return PCOMOE_ERR_UNSUPPORTED;
   if (n_seqs > kAttnMaxSeqs || (int64_t)T * (c->q_heads / c->kv_heads) > INT32_MAX) return PCOMOE_ERR_SHAPE;
   const int64_t e = (int64_t)dtype_size(c->dtype);
   if (!aligned16(q, q_stride, e) || !aligned16(out, out_stride, e)) return PCOMOE_ERR_UNSUPPORTED;
@@ -45,6 +46,7 @@ pcomoe_status fill(AttnArgs &a, const pcomoe_attn_config *c, int32_t T, int32_t 
   a.cu = cu; a.q = q; a.q_stride = q_stride; a.out = out; a.out_stride = out_stride; a.lse = lse;
   a.status = (int32_t *)((char *)ws + offsetof(DevPlan, status_router));
   a.counters = (int32_t *)((char *)ws + kCountersAt);
+  a.recs = (JoinRec *)((char *)ws + kRecsAt);
   a.part = (float *)((char *)ws + kPartAt);
   a.part_ml = a.part + rows * c->head_dim;
   a.limit_ns = wait_limit_ns();

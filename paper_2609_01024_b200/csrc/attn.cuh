@@ -6,7 +6,8 @@
 // Work over a cache.  A tile's blocks of keys are numbered through: (sequence, kv head, tile, block), blocks fastest.  Every
 // block (CTA) of the grid takes an equal, contiguous share of that line, found on the device from the lengths alone (no
 // host copy of them, no plan step), so ragged batches are balanced to one block of keys.  A tile cut by a share's
-// border leaves partial sums; the CTA that finishes last joins them in order of the shares, which fixes the bits.
+// border leaves partial sums, which a second kernel joins in order of the shares.  (Joined by the CTA that finished last
+// instead, the sums of a 192-row tile took 13 us of one SM's time, and fences and counters another 3.)
 #pragma once
 #include "tc_ptx.cuh"
 
@@ -24,16 +25,22 @@ struct AttnArgs {
   int32_t words;
   const int32_t *len, *table;           // the cache's lengths and page tables; NULL: packed prompts
   int32_t pages, page, page_shift, max_seqs, max_pages;
-  int32_t *status, *counters;
+  int32_t *status, *counters;           // counters: next piece of the prompts, CTAs done; zero between calls
+  struct JoinRec *recs;                 // one per CTA of the grid
   float *part, *part_ml;                // [2 * grid][rows][D] and [2 * grid][rows][2]
   uint64_t limit_ns;
 };
 
-constexpr int kAttnCounters = 4096;     // one per CTA of a grid; the last two are the prompts' (next piece, CTAs done)
+// The tile that a CTA of the grid began and did not finish; n_parts = 0: none.
+struct JoinRec {
+  int32_t q0, n, kvh, tile, n_parts;
+};
+constexpr int kAttnMaxCtas = 4096;
 constexpr int kAttnMaxSeqs = 65535;
 constexpr int kAttnMaxWords = 8;
 constexpr float kLn2f = 0.6931471805599453f;
 
+pcomoe_status launch_attn_join(const AttnArgs &a, int head_dim, int dtype, int rows, int ctas, cudaStream_t st);
 pcomoe_status launch_attn_tc(const AttnArgs &a, int head_dim, int sms, cudaStream_t st);
 size_t attn_tc_part_rows(int sms);
 pcomoe_status launch_attn_few(const AttnArgs &a, int head_dim, int sms, cudaStream_t st);
@@ -209,47 +216,17 @@ struct CacheWalk {
     p.n_parts = (int)(w1 / share) - p.first_cta + 1;
     p.whole = p.n_parts == 1;
     at += p.b1 - p.b0;
+    if (p.b0 == 0 && !p.whole) begun = {seq.q0, seq.n, p.kvh, p.tile, p.n_parts};      // then it is the share's last piece
     return p;
   }
+
+  JoinRec begun = {0, 0, 0, 0, 0};
+  __device__ void record(const AttnArgs &a, int cta) const { a.recs[cta] = begun; }      // one thread, at the end
 };
 
 // Place of a partial result: a CTA leaves at most two, of the tile that its share begins inside and of the one that it
 // begins itself and does not finish.
 __device__ __forceinline__ int part_slot(int cta, bool begins_tile) { return 2 * cta + (begins_tile ? 1 : 0); }
-
-// Barrier of N threads of the block (all that use barrier 1).
-template <int N> __device__ __forceinline__ void sync_part() {
-  __syncwarp();
-  asm volatile("bar.sync 1, %0;" ::"n"(N) : "memory");
-}
-
-// The same, and whether `ok` holds in all of them.
-template <int N> __device__ __forceinline__ bool all_part(bool ok) {
-  int r;
-  __syncwarp();
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.aligned.pred q, 1, %2, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
-               : "=r"(r) : "r"((int)ok), "n"(N) : "memory");
-  return r;
-}
-
-// After this CTA's partial result of a tile has been written (N threads from thread F on call): whether it was the last
-// one.  The counter belongs to the tile's first CTA, which begins only one tile that it does not finish, and is left at
-// zero.
-template <int N, int F = 0>
-__device__ __forceinline__ bool last_part(const AttnArgs &a, int first_cta, int n_parts, int *s_flag) {
-  __threadfence();
-  sync_part<N>();
-  if (threadIdx.x == F) {
-    const int old = atomicAdd(&a.counters[first_cta], 1);
-    *s_flag = old == n_parts - 1;
-    if (*s_flag) a.counters[first_cta] = 0;
-  }
-  sync_part<N>();
-  const bool last = *s_flag;
-  if (last) __threadfence();
-  sync_part<N>();
-  return last;
-}
 
 template <typename T> __device__ __forceinline__ void store4(T *p, float4 v);
 template <> __device__ __forceinline__ void store4<float>(float *p, float4 v) { *(float4 *)p = v; }
@@ -258,90 +235,6 @@ template <> __device__ __forceinline__ void store4<__nv_bfloat16>(__nv_bfloat16 
   *(__nv_bfloat162 *)&u.x = __floats2bfloat162_rn(v.x, v.y);
   *(__nv_bfloat162 *)&u.y = __floats2bfloat162_rn(v.z, v.w);
   *(uint2 *)p = u;
-}
-
-template <typename T, int V> __device__ __forceinline__ void store_row(T *p, const float (&x)[V], float by) {
-#pragma unroll
-  for (int k = 0; k < V; k += 2) {
-    if (sizeof(T) == 4) {
-      *(float2 *)(p + k) = make_float2(x[k] * by, x[k + 1] * by);
-    } else {
-      const __nv_bfloat162 v = __floats2bfloat162_rn(x[k] * by, x[k + 1] * by);
-      *(uint32_t *)(p + k) = *(const uint32_t *)&v;
-    }
-  }
-}
-
-// Joins the partial results of a tile and writes its rows.  N threads from thread F on, four rows per warp at a time.  The
-// CTA that finished last does this alone, and all it waits for is L2: eight lanes per row hold the parts' maxima and sums,
-// and the sums of four parts are on their way before the weights are known.  BM: rows of a partial result's place.
-template <typename T, int D, int BM, int N, int F = 0>
-__device__ void join_parts(const AttnArgs &a, const Seq &s, int kvh, int tile, int first_cta, int n_parts) {
-  constexpr int R = 4, U = 4, V = D / 32;                  // rows and parts at a time, columns of a lane
-  const int rows = min(BM, s.n * a.g - tile * BM), lane = threadIdx.x & 31, mine = lane & 7;
-  for (int r0 = ((threadIdx.x - F) >> 5) * R; r0 < rows; r0 += (N / 32) * R) {
-    float x[U][R][V], o[R][V];
-    auto fetch = [&](int i0) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = min(i0 + u, n_parts - 1);
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-          const float *src = a.part + ((int64_t)part_slot(first_cta + i, i == 0) * BM + min(r0 + j, rows - 1)) * D + lane * V;
-          if (V == 4) {
-            const float4 y = __ldcg((const float4 *)src);
-            x[u][j][0] = y.x; x[u][j][1] = y.y; x[u][j][V - 2] = y.z; x[u][j][V - 1] = y.w;
-          } else {
-            const float2 y = __ldcg((const float2 *)src);
-            x[u][j][0] = y.x; x[u][j][1] = y.y;
-          }
-        }
-      }
-    };
-    fetch(0);
-    const int row8 = min(r0 + (lane >> 3), rows - 1);      // the row of this lane's parts (mine, mine + 8, ...)
-    auto stat = [&](int i) { return __ldcg((const float2 *)a.part_ml + (int64_t)part_slot(first_cta + i, i == 0) * BM + row8); };
-    const float2 ml0 = mine < n_parts ? stat(mine) : make_float2(-INFINITY, 0.f);
-    float m = ml0.x;
-    for (int i = mine + 8; i < n_parts; i += 8) m = fmaxf(m, stat(i).x);
-#pragma unroll
-    for (int h = 4; h; h >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, h));
-    const float ms = m == -INFINITY ? 0.f : m;
-    float l = 0.f, w = 0.f;
-#pragma unroll
-    for (int j = 0; j < R; ++j)
-#pragma unroll
-      for (int k = 0; k < V; ++k) o[j][k] = 0.f;
-    for (int i0 = 0; i0 < n_parts; i0 += U) {
-      if ((i0 & 7) == 0) {                                 // the weights of eight parts, one per lane
-        const float2 ml = i0 == 0 ? ml0 : i0 + mine < n_parts ? stat(i0 + mine) : make_float2(-INFINITY, 0.f);
-        w = ex2f(ml.x - ms);
-        if (w != 0.f) l += w * ml.y;                       // 0: a part in which the row saw nothing
-      }
-      if (i0) fetch(i0);
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-          const float wi = __shfl_sync(~0u, w, 8 * j + ((i0 + u) & 7));
-          if (wi != 0.f && i0 + u < n_parts)
-#pragma unroll
-            for (int k = 0; k < V; ++k) o[j][k] = fmaf(wi, x[u][j][k], o[j][k]);
-        }
-    }
-#pragma unroll
-    for (int h = 4; h; h >>= 1) l += __shfl_xor_sync(~0u, l, h);
-#pragma unroll
-    for (int j = 0; j < R; ++j) {
-      const float lj = __shfl_sync(~0u, l, 8 * j), mj = __shfl_sync(~0u, ms, 8 * j);
-      if (r0 + j >= rows) continue;
-      const int row = tile * BM + r0 + j, tok = row / a.g, head = kvh * a.g + row - tok * a.g;
-      const int64_t t = s.q0 + tok;
-      const float inv = lj == 0.f ? 0.f : 1.f / lj;
-      store_row<T, V>((T *)a.out + t * a.out_stride + head * D + lane * V, o[j], inv);
-      if (lane == 0 && a.lse) a.lse[t * a.hq + head] = lj == 0.f ? -INFINITY : mj * kLn2f + logf(lj);
-    }
-  }
 }
 
 // Row of a page pool ([page][head][place in the page]) that holds position p.

@@ -44,13 +44,13 @@ __global__ void __launch_bounds__(kThreads, 2) few_kernel(AttnArgs a) {
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ float2 s_ml[kWarps][BM];
   __shared__ uint8_t s_bad[BM];
-  __shared__ int s_flag, s_again;
+  __shared__ int s_again;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t ring = smem_u32(smem) + warp * kStages * stage_bytes<D>();
   pdl_grid_wait();
   CacheWalk<BM, BN> w;
-  if (!w.start(a, blockIdx.x, gridDim.x, 4)) return;
-  while (w.at < w.end) {
+  const bool some = w.start(a, blockIdx.x, gridDim.x, 4);
+  while (some && w.at < w.end) {
     const auto p = w.next(a);
     const Seq seq = w.seq;
     const int rows = min(BM, seq.n * a.g - p.tile * BM);
@@ -239,9 +239,9 @@ __global__ void __launch_bounds__(kThreads, 2) few_kernel(AttnArgs a) {
         if (s_bad[r]) plain_row<D, BM, true>(a, seq, p.kvh, p.tile, r, p.b0 * BN, p.b1 * BN, p.whole, slot);
       __syncthreads();
     }
-    if (!p.whole && last_part<kThreads>(a, p.first_cta, p.n_parts, &s_flag))
-      join_parts<__nv_bfloat16, D, BM, kThreads>(a, seq, p.kvh, p.tile, p.first_cta, p.n_parts);
+    __syncthreads();                                       // the rings are free again
   }
+  if (tid == 0) w.record(a, blockIdx.x);
 }
 
 template <int D>
@@ -255,7 +255,7 @@ pcomoe_status run(const AttnArgs &a, int sms, cudaStream_t st) {
   }
   PCOMOE_CUDA_TRY(launch_pdl(few_kernel<D>, dim3(2 * sms), dim3(kThreads), smem_bytes<D>(), st, a));
   count_launch();
-  return PCOMOE_OK;
+  return launch_attn_join(a, D, PCOMOE_BF16, BM, 2 * sms, st);
 }
 
 }  // namespace

@@ -174,15 +174,13 @@ template <int D, int BM>
 __global__ void __launch_bounds__(kThreads) simt_cached_kernel(AttnArgs a) {
   pdl_grid_wait();
   extern __shared__ float4 sm4[];
-  __shared__ int s_flag;
   CacheWalk<BM, BN> w;
-  if (!w.start(a, blockIdx.x, gridDim.x, 4)) return;
-  while (w.at < w.end) {
-    const auto p = w.next(a);
-    run_piece<D, BM, true>(a, w.seq, p.kvh, p.tile, p.b0, p.b1, p.whole, part_slot(blockIdx.x, p.b0 == 0), (float *)sm4);
-    if (!p.whole && last_part<kThreads>(a, p.first_cta, p.n_parts, &s_flag))
-      join_parts<float, D, BM, kThreads>(a, w.seq, p.kvh, p.tile, p.first_cta, p.n_parts);
-  }
+  if (w.start(a, blockIdx.x, gridDim.x, 4))
+    while (w.at < w.end) {
+      const auto p = w.next(a);
+      run_piece<D, BM, true>(a, w.seq, p.kvh, p.tile, p.b0, p.b1, p.whole, part_slot(blockIdx.x, p.b0 == 0), (float *)sm4);
+    }
+  if (threadIdx.x == 0) w.record(a, blockIdx.x);
 }
 
 // One tile per block; the tiles are counted from the last one back, so that those with the most keys start first.
@@ -232,7 +230,8 @@ pcomoe_status run(const AttnArgs &a, int sms, cudaStream_t st) {
   const size_t smem = smem_floats<D, BM>() * sizeof(float);
   if (a.table) {
     static PerDeviceOnce once;
-    return launch(simt_cached_kernel<D, BM>, once, dim3(2 * sms), smem, a, st);
+    const pcomoe_status r = launch(simt_cached_kernel<D, BM>, once, dim3(2 * sms), smem, a, st);
+    return r == PCOMOE_OK ? launch_attn_join(a, D, PCOMOE_FP32, BM, 2 * sms, st) : r;
   }
   static PerDeviceOnce once;
   const int64_t tiles = (int64_t)a.T * a.g / BM + std::min(a.n_seqs, a.T);

@@ -196,7 +196,7 @@ struct Item {
   int rows;             // of 256; 0: no more work
   bool both;            // two tiles of rows; else two sets of blocks for one tile
   bool whole;
-  int slot, first_cta, n_parts;
+  int slot;             // place of a partial result
 
   __device__ int blocks() const { return b1 - b0; }
 };
@@ -212,12 +212,14 @@ template <> struct Walk<true> {
     if (!some || w.at >= w.end) return false;
     const auto p = w.next(a);
     it.seq = w.seq; it.kvh = p.kvh; it.tile = p.tile; it.b0 = p.b0; it.b1 = p.b1;
-    it.whole = p.whole; it.slot = part_slot(blockIdx.x, p.b0 == 0); it.first_cta = p.first_cta; it.n_parts = p.n_parts;
+    it.whole = p.whole; it.slot = part_slot(blockIdx.x, p.b0 == 0);
     it.rows = min(BM, it.seq.n * a.g - it.tile * BM);
     it.both = it.rows > 128;
     return true;
   }
-  __device__ void finish(const AttnArgs &) {}
+  __device__ void finish(const AttnArgs &a) {
+    if ((threadIdx.x & 31) == 0) w.record(a, blockIdx.x);
+  }
 };
 
 // Prompts: whole tiles from a counter, longest first.  The order needs every sequence's number of tiles at hand: four per
@@ -244,7 +246,7 @@ template <> struct Walk<false> {
     const int lane = threadIdx.x & 31;
     int w = blockIdx.x;                                    // the first piece needs no counter
     if (!first) {
-      if (lane == 0) w = gridDim.x + atomicAdd(&a.counters[kAttnCounters - 2], 1);
+      if (lane == 0) w = gridDim.x + atomicAdd(&a.counters[0], 1);
       w = __shfl_sync(~0u, w, 0);
     }
     first = false;
@@ -288,15 +290,15 @@ template <> struct Walk<false> {
     }
     it.seq = load_seq<false>(a, s);
     it.b0 = 0; it.b1 = tile_blocks<false, BM, BN>(a, it.seq, it.tile);
-    it.whole = true; it.slot = it.first_cta = 0; it.n_parts = 1;
+    it.whole = true; it.slot = 0;
     it.rows = min(BM, it.seq.n * a.g - it.tile * BM);
     it.both = it.rows > 128;
     return true;
   }
   // the last CTA to leave sets the counter back
   __device__ void finish(const AttnArgs &a) {
-    if ((threadIdx.x & 31) == 0 && atomicAdd(&a.counters[kAttnCounters - 1], 1) == (int)gridDim.x - 1)
-      a.counters[kAttnCounters - 2] = a.counters[kAttnCounters - 1] = 0;
+    if ((threadIdx.x & 31) == 0 && atomicAdd(&a.counters[1], 1) == (int)gridDim.x - 1)
+      a.counters[0] = a.counters[1] = 0;
   }
 };
 
@@ -321,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
   __shared__ float s_x[2][2][128];                        // between the threads of a row: [tile][half of the keys][row]
   __shared__ uint8_t s_bad[BM];
   __shared__ uint32_t s_tmem;
-  __shared__ int s_abort, s_flag;
+  __shared__ int s_abort;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t q_at = smem_u32(smem), ring = q_at + 2 * S::kTileBytes;
   volatile int *abort_flag = &s_abort;
@@ -601,23 +603,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
           plain_row<D, BM, kCached>(a, it.seq, it.kvh, it.tile, x, it.b0 * BN, it.b1 * BN, it.whole, it.slot);
         }
       }
-      if (!it.whole) {
-        // (as last_part, with the barrier between both tiles' warps)
-        __threadfence();
-        sync_both();
-        if (tid == kFirst) {
-          const int old = atomicAdd(&a.counters[it.first_cta], 1);
-          s_flag = ok && old == it.n_parts - 1;
-          if (old == it.n_parts - 1) a.counters[it.first_cta] = 0;
-        }
-        sync_both();
-        const bool last = __all_sync(~0u, s_flag && ok);
-        if (last) {
-          __threadfence();
-          join_parts<__nv_bfloat16, D, BM, kSoftmaxThreads, kFirst>(a, it.seq, it.kvh, it.tile, it.first_cta, it.n_parts);
-        }
-        sync_both();                                       // s_flag has been read
-      }
       item_done();
     }
   } else {
@@ -859,7 +844,8 @@ pcomoe_status launch_attn_tc(const AttnArgs &a, int D, int sms, cudaStream_t st)
     if (rows > INT32_MAX) return PCOMOE_ERR_UNSUPPORTED;                 // row numbers of a TMA copy are 32 bits
     const uint32_t box = std::min(BN, a.page);
     if (!make_rows_map(&m.k, a.k, rows, D, D, box) || !make_rows_map(&m.v, a.v, rows, D, D, box)) return PCOMOE_ERR_CUDA;
-    return D == 64 ? run<64, true>(m, a, sms, st) : run<128, true>(m, a, sms, st);
+    const pcomoe_status r = D == 64 ? run<64, true>(m, a, sms, st) : run<128, true>(m, a, sms, st);
+    return r == PCOMOE_OK ? launch_attn_join(a, D, PCOMOE_BF16, BM, sms, st) : r;
   }
   if (!make_rows_map(&m.k, a.k, a.T, (uint64_t)a.hkv * D, a.k_stride, BN) || !make_rows_map(&m.v, a.v, a.T, (uint64_t)a.hkv * D, a.v_stride, BN))
     return PCOMOE_ERR_CUDA;
