@@ -125,12 +125,14 @@ __device__ __forceinline__ uint32_t seen_bits(const AttnArgs &a, const Seq &s, i
   return bits;
 }
 
-// A CTA's share of the line of blocks, and its walk along it.  All of it is the same in every thread of a warp.
-template <int BM, int BN>
+// A CTA's share of the line of blocks, and its walk along it.  All of it is the same in every thread of a warp.  A tile
+// counts for its blocks and kExtra more, which stand for what a piece of work costs besides (a sequence of one block of keys
+// is no cheaper to begin than one of a thousand): without them the CTA that met the shortest sequences finished last.
+template <int BM, int BN, int kExtra>
 struct CacheWalk {
-  int64_t at, end;      // blocks of this share still to do
-  int64_t share;
-  int64_t seq_at;       // number of the current sequence's first block
+  uint32_t at, end;     // units of this share still to do
+  uint32_t share;
+  uint32_t seq_at;      // number of the current sequence's first unit
   int s;                // sequence
   Seq seq;
   int tiles, blocks;    // of the current sequence: row tiles, blocks of a tile
@@ -140,33 +142,41 @@ struct CacheWalk {
     tiles = (seq.n * a.g + BM - 1) / BM;
     blocks = max(1, (seq.len + BN - 1) / BN);
   }
+  __device__ uint32_t units() const { return (uint32_t)(blocks + kExtra); }
+  __device__ uint64_t weight(const AttnArgs &a) const { return (uint64_t)((int64_t)tiles * a.hkv) * units(); }
 
-  // One warp, all lanes.  Returns false when the share is empty.
-  __device__ bool start(const AttnArgs &a, int cta, int ctas, int least) {
+  // One warp, all lanes.  An empty share gives no piece.
+  __device__ void start(const AttnArgs &a, int cta, int ctas, int least) {
     const int lane = threadIdx.x & 31;
-    int64_t total = 0, w0 = 0;                             // w0: of this lane's sequence among the first 32
+    uint64_t total = 0, w0 = 0;                            // w0: of this lane's sequence among the first 32
+    begun.n_parts = 0;
     for (int s0 = 0; s0 < a.n_seqs; s0 += 32) {
       s = s0 + lane;
-      int64_t w = 0;
-      if (s < a.n_seqs) { measure(a); w = (int64_t)tiles * blocks * a.hkv; }
+      uint64_t w = 0;
+      if (s < a.n_seqs) { measure(a); w = weight(a); }
       if (s0 == 0) w0 = w;
 #pragma unroll
       for (int o = 16; o; o >>= 1) w += __shfl_xor_sync(~0u, w, o);
       total += w;
     }
-    share = max((total + ctas - 1) / ctas, (int64_t)least);
+    at = end = 0;
+    if (total > (uint64_t)INT32_MAX) {                     // more than any memory holds, unless a sequence is named very often
+      atomicCAS(a.status, 0, (int)PCOMOE_ERR_SHAPE);
+      return;
+    }
+    share = max(((uint32_t)total + ctas - 1) / ctas, (uint32_t)(least + kExtra));
+    if ((uint64_t)cta * share >= total) return;
     at = cta * share;
-    end = min(at + share, total);
-    if (at >= end) return false;
-    int64_t before = 0;
+    end = min(at + share, (uint32_t)total);
+    uint32_t before = 0;
     for (int s0 = 0; s0 < a.n_seqs; s0 += 32) {
       s = s0 + lane;
-      int64_t w = s0 == 0 ? w0 : 0;
-      if (s0 && s < a.n_seqs) { measure(a); w = (int64_t)tiles * blocks * a.hkv; }
-      int64_t upto = w;
+      uint32_t w = s0 == 0 ? (uint32_t)w0 : 0;
+      if (s0 && s < a.n_seqs) { measure(a); w = (uint32_t)weight(a); }
+      uint32_t upto = w;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const int64_t y = __shfl_up_sync(~0u, upto, o);
+        const uint32_t y = __shfl_up_sync(~0u, upto, o);
         if (lane >= o) upto += y;
       }
       const uint32_t hit = __ballot_sync(~0u, before + upto > at);
@@ -182,45 +192,46 @@ struct CacheWalk {
           seq.id = __shfl_sync(~0u, seq.id, l);
           tiles = __shfl_sync(~0u, tiles, l);
           blocks = __shfl_sync(~0u, blocks, l);
-          return true;
+          return;
         }
         break;
       }
       before += __shfl_sync(~0u, upto, 31);
     }
     measure(a);
-    return true;
   }
 
   struct Piece {
     int kvh, tile, b0, b1;     // blocks [b0, b1) of a tile of `blocks`
-    int first_cta, n_parts;    // shares that the tile is cut into
     bool whole;
   };
 
-  __device__ Piece next(const AttnArgs &a) {
-    while (at >= seq_at + (int64_t)tiles * blocks * a.hkv) {
-      seq_at += (int64_t)tiles * blocks * a.hkv;
-      ++s;
-      measure(a);
+  __device__ bool next(const AttnArgs &a, Piece &p) {
+    while (at < end) {
+      while (at >= seq_at + (uint32_t)(tiles * a.hkv) * units()) {
+        seq_at += (uint32_t)(tiles * a.hkv) * units();
+        ++s;
+        measure(a);
+      }
+      const uint32_t t = (at - seq_at) / units(), tile_at = seq_at + t * units();
+      const uint32_t upto = min(end, tile_at + units());
+      p.b0 = max((int)(at - tile_at) - kExtra, 0);
+      p.b1 = (int)(upto - tile_at) - kExtra;
+      at = upto;
+      if (p.b1 <= p.b0) continue;                          // of this tile only what stands for its cost
+      p.kvh = (int)t / tiles;
+      p.tile = (int)t - p.kvh * tiles;
+      p.whole = p.b0 == 0 && p.b1 == blocks;
+      if (p.b0 == 0 && !p.whole) {                         // then it is the share's last piece
+        const uint32_t first = tile_at + kExtra;
+        begun = {seq.q0, seq.n, p.kvh, p.tile, (int)((first + blocks - 1) / share - first / share) + 1};
+      }
+      return true;
     }
-    Piece p;
-    const int64_t off = at - seq_at;
-    const int t = (int)(off / blocks);
-    p.b0 = (int)(off - (int64_t)t * blocks);
-    p.kvh = t / tiles;
-    p.tile = t - p.kvh * tiles;
-    p.b1 = (int)min((int64_t)blocks, p.b0 + (end - at));
-    const int64_t w0 = at - p.b0, w1 = w0 + blocks - 1;
-    p.first_cta = (int)(w0 / share);
-    p.n_parts = (int)(w1 / share) - p.first_cta + 1;
-    p.whole = p.n_parts == 1;
-    at += p.b1 - p.b0;
-    if (p.b0 == 0 && !p.whole) begun = {seq.q0, seq.n, p.kvh, p.tile, p.n_parts};      // then it is the share's last piece
-    return p;
+    return false;
   }
 
-  JoinRec begun = {0, 0, 0, 0, 0};
+  JoinRec begun;
   __device__ void record(const AttnArgs &a, int cta) const { a.recs[cta] = begun; }      // one thread, at the end
 };
 

@@ -15,6 +15,7 @@ namespace pcomoe {
 namespace {
 
 constexpr int BM = 16, BN = 64, kWarps = 4, kThreads = 32 * kWarps, kStages = 3, kKeys = 16;
+constexpr int kExtra = 3;              // blocks of 64 keys that a piece of work costs besides its own
 
 template <int D> constexpr int stage_bytes() { return 2 * kKeys * D * 2; }
 template <int D> constexpr int smem_bytes() { return kWarps * kStages * stage_bytes<D>(); }
@@ -48,32 +49,16 @@ __global__ void __launch_bounds__(kThreads, 2) few_kernel(AttnArgs a) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t ring = smem_u32(smem) + warp * kStages * stage_bytes<D>();
   pdl_grid_wait();
-  CacheWalk<BM, BN> w;
-  const bool some = w.start(a, blockIdx.x, gridDim.x, 4);
-  while (some && w.at < w.end) {
-    const auto p = w.next(a);
+  CacheWalk<BM, BN, kExtra> w;
+  CacheWalk<BM, BN, kExtra>::Piece p;
+  w.start(a, blockIdx.x, gridDim.x, 4);
+  while (w.next(a, p)) {
     const Seq seq = w.seq;
     const int rows = min(BM, seq.n * a.g - p.tile * BM);
     const int r0 = lane >> 2, r1 = r0 + 8;                // the rows of this lane's fragments
     int tok[2];
     tok[0] = (p.tile * BM + min(r0, rows - 1)) / a.g;
     tok[1] = (p.tile * BM + min(r1, rows - 1)) / a.g;
-    uint32_t q[D / 16][4];                                // A fragments of the queries
-    {
-      const __nv_bfloat16 *row[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int rr = p.tile * BM + min(i ? r1 : r0, rows - 1);
-        row[i] = (const __nv_bfloat16 *)a.q + (int64_t)(seq.q0 + tok[i]) * a.q_stride + (p.kvh * a.g + rr - tok[i] * a.g) * D + (lane & 3) * 2;
-      }
-#pragma unroll
-      for (int k = 0; k < D / 16; ++k) {
-        q[k][0] = *(const uint32_t *)(row[0] + k * 16);
-        q[k][1] = *(const uint32_t *)(row[1] + k * 16);
-        q[k][2] = *(const uint32_t *)(row[0] + k * 16 + 8);
-        q[k][3] = *(const uint32_t *)(row[1] + k * 16 + 8);
-      }
-    }
     float o[D / 8][4];
 #pragma unroll
     for (int n = 0; n < D / 8; ++n) o[n][0] = o[n][1] = o[n][2] = o[n][3] = 0.f;
@@ -103,6 +88,22 @@ __global__ void __launch_bounds__(kThreads, 2) few_kernel(AttnArgs a) {
     };
 #pragma unroll
     for (int i = 0; i < kStages - 1; ++i) load(i);
+    uint32_t q[D / 16][4];                                // A fragments of the queries
+    {
+      const __nv_bfloat16 *row[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int rr = p.tile * BM + min(i ? r1 : r0, rows - 1);
+        row[i] = (const __nv_bfloat16 *)a.q + (int64_t)(seq.q0 + tok[i]) * a.q_stride + (p.kvh * a.g + rr - tok[i] * a.g) * D + (lane & 3) * 2;
+      }
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        q[k][0] = *(const uint32_t *)(row[0] + k * 16);
+        q[k][1] = *(const uint32_t *)(row[1] + k * 16);
+        q[k][2] = *(const uint32_t *)(row[0] + k * 16 + 8);
+        q[k][3] = *(const uint32_t *)(row[1] + k * 16 + 8);
+      }
+    }
     for (int i = 0; i < steps; ++i) {
       load(i + kStages - 1);
       asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 1) : "memory");

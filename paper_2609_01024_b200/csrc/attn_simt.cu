@@ -174,12 +174,11 @@ template <int D, int BM>
 __global__ void __launch_bounds__(kThreads) simt_cached_kernel(AttnArgs a) {
   pdl_grid_wait();
   extern __shared__ float4 sm4[];
-  CacheWalk<BM, BN> w;
-  if (w.start(a, blockIdx.x, gridDim.x, 4))
-    while (w.at < w.end) {
-      const auto p = w.next(a);
-      run_piece<D, BM, true>(a, w.seq, p.kvh, p.tile, p.b0, p.b1, p.whole, part_slot(blockIdx.x, p.b0 == 0), (float *)sm4);
-    }
+  CacheWalk<BM, BN, 2> w;
+  typename CacheWalk<BM, BN, 2>::Piece p;
+  w.start(a, blockIdx.x, gridDim.x, 2);
+  while (w.next(a, p))
+    run_piece<D, BM, true>(a, w.seq, p.kvh, p.tile, p.b0, p.b1, p.whole, part_slot(blockIdx.x, p.b0 == 0), (float *)sm4);
   if (threadIdx.x == 0) w.record(a, blockIdx.x);
 }
 

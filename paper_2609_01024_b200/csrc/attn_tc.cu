@@ -205,12 +205,11 @@ struct Item {
 template <bool kCached> struct Walk;
 
 template <> struct Walk<true> {
-  CacheWalk<BM, BN> w;
-  bool some;
-  __device__ void start(const AttnArgs &a) { some = w.start(a, blockIdx.x, gridDim.x, 4); }
+  CacheWalk<BM, BN, 2> w;
+  __device__ void start(const AttnArgs &a) { w.start(a, blockIdx.x, gridDim.x, 4); }
   __device__ bool next(const AttnArgs &a, Item &it) {
-    if (!some || w.at >= w.end) return false;
-    const auto p = w.next(a);
+    CacheWalk<BM, BN, 2>::Piece p;
+    if (!w.next(a, p)) return false;
     it.seq = w.seq; it.kvh = p.kvh; it.tile = p.tile; it.b0 = p.b0; it.b1 = p.b1;
     it.whole = p.whole; it.slot = part_slot(blockIdx.x, p.b0 == 0);
     it.rows = min(BM, it.seq.n * a.g - it.tile * BM);
