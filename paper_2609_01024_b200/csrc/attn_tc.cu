@@ -13,17 +13,17 @@
 // at the end.
 //   warp 0: issues the MMAs and owns TMEM                         warp 1: TMA loads of K and V into a ring (128-byte swizzle)
 //   warp 2: copies the queries                                    warp 3: finds the CTA's pieces of work and hands them out
-//   warps 4-11, 12-19: softmax of tile 0 and 1, and its epilogue; a row has two threads, with half of the keys each
+//   warps 4-7, 8-11: softmax of tile 0 and 1, and its epilogue
 // The CTAs are persistent and every role runs ahead of the next as far as its buffers allow: the next piece's queries,
 // keys and first scores come in while the last one's output is written.  Prompts: pieces are whole tiles, drawn from a
 // counter in order of falling length, so that the last ones to finish are short.  Cache: every CTA has an equal share.
 //
-// What the softmax threads do bounds the kernel once the products are fed: an exponential per score, and the special
-// function unit does 16 per clock and SM where the MMAs want 16 scores per clock.  So a quarter is formed on the FMA
-// pipe instead: 2^x = 2^n 2^f with n the nearest integer (the add of 1.5 * 2^23 leaves it in the low bits) and 2^f on
-// [-1/2, 1/2] by a degree-4 polynomial (minimax in the relative error by Remez exchange, 2.7e-6, against the 2^-9 that a
-// bf16 weight keeps).  The weights go to the MMA in two halves, so that it starts on the first while the second is formed.
-// K is the K-major B operand of the first product; V ([key][d] as it lies in memory) the MN-major B operand of the second.
+// What bounds it once the products are fed is the chain of a tile: scores done -> read, maximum, 128 exponentials per thread
+// -> weights written -> two products; the special function unit's rate (16 per clock and SM) makes the middle 1024 clocks
+// long at least, and the products 1024.  Tried and not kept, for one prompt of 16384 tokens with 16 heads (this form
+// 0.93 ms, 1.19 PFLOP/s): a polynomial on the FMA pipe for 1, 2 or 3 of 8 exponentials 0.92, 0.94, 0.97 ms (issue slots are
+// as scarce as exponentials); two threads per row 0.99; scores read twice so that loops stay short 0.97; weights formed with
+// a stale maximum while a vote is out 1.35.
 // The softmax threads clear the V rows past the end of a sequence before they hand over the weights of that block, which
 // keeps stale memory out of the sums; a NaN or infinity in a row of V that only some rows of a tile see meets
 // the others with weight 0 and would turn them into NaN: a row whose output is not finite is formed again without the
@@ -36,7 +36,9 @@ namespace pcomoe {
 namespace {
 
 constexpr int BM = 256, BN = 128;              // rows of a CTA, keys of a block
-constexpr int kFirst = 128, kTileThreads = 256, kSoftmaxThreads = 512, kThreads = 640;      // softmax threads from thread kFirst on
+constexpr int kFirst = 128, kTileThreads = 128, kSoftmaxThreads = 256, kThreads = 384;      // softmax threads from thread kFirst on
+constexpr int kSoftmaxRegs = 208, kOtherRegs = 88, kLaunchRegs = 168;
+static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs, "register split");
 constexpr float kSlack = 8.f;                  // how far a maximum may run ahead of the one in use, in powers of two
 
 template <bool B> struct Bool { static constexpr bool value = B; };
@@ -142,28 +144,6 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   uint64_t d;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*(uint64_t *)&a), "l"(*(uint64_t *)&b));
   return *(float2 *)&d;
-}
-__device__ __forceinline__ float max_nan(float a, float b) {
-  float d;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
-  return d;
-}
-__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*(uint64_t *)&a), "l"(*(uint64_t *)&b));
-  return *(float2 *)&d;
-}
-// Two powers of two on the FMA pipe (see the head of the file).  -127 and below, -inf among them, give 0; NaN stays NaN.
-__device__ __forceinline__ float2 ex2_poly(float2 x) {
-  constexpr float kRound = 12582912.f + 127.f;             // the low bits of x + kRound are n + 127, 2^n's exponent field
-  x = make_float2(max_nan(x.x, -127.f), max_nan(x.y, -127.f));
-  const float2 t = add2(x, make_float2(kRound, kRound));
-  const float2 f = add2(x, fma2(t, make_float2(-1.f, -1.f), make_float2(kRound, kRound)));
-  float2 p = fma2(f, make_float2(0.009570102207362652f, 0.009570102207362652f), make_float2(0.05591785907745361f, 0.05591785907745361f));
-  p = fma2(p, f, make_float2(0.240247443318367f, 0.240247443318367f));
-  p = fma2(p, f, make_float2(0.6931217908859253f, 0.6931217908859253f));
-  p = fma2(p, f, make_float2(0.9999992847442627f, 0.9999992847442627f));
-  return mul2(p, make_float2(__int_as_float(__float_as_int(t.x) << 23), __int_as_float(__float_as_int(t.y) << 23)));
 }
 // Four rows of 64 bytes, one per lane of a quad, turned so that every store of the quad is 64 contiguous bytes: lane i ends up
 // with piece i of the four rows.  row[k]: where the quad's k-th row goes (this lane's piece), or NULL.
@@ -319,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
   __shared__ __align__(8) uint64_t s_full[S::kStages], s_empty[S::kStages], s_sfull[2], s_pfull[2][2], s_ofull[2], s_qfull[2], s_qempty[2], s_join;
   __shared__ __align__(8) uint64_t s_ifull[2], s_iempty[2];
   __shared__ Item s_item[2];
-  __shared__ float s_x[2][2][128];                        // between the threads of a row: [tile][half of the keys][row]
+  __shared__ float2 s_ml[2][128];                         // maxima and sums of the two tiles, where they hold the same rows
   __shared__ uint8_t s_bad[BM];
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
@@ -338,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
       mbar_init(smem_u32(&s_qfull[t]), 1);
       mbar_init(smem_u32(&s_qempty[t]), 1);
       mbar_init(smem_u32(&s_ifull[t]), 1);
-      mbar_init(smem_u32(&s_iempty[t]), 19);              // every warp but the one that fills them
+      mbar_init(smem_u32(&s_iempty[t]), 11);              // every warp but the one that fills them
     }
     mbar_init(smem_u32(&s_join), kSoftmaxThreads / 32);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -365,7 +345,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
     ++n_item;
   };
   if (warp >= kFirst / 32) {
-    const int t = (warp - kFirst / 32) >> 3, hw = (warp >> 2) & 1 ? 0 : 1;      // tile; half of the keys (warps 4-7: the first)
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
+    const int t = (warp - kFirst / 32) >> 2;              // tile
     const int r = (warp & 3) * 32 + lane;                 // row of the tile = TMEM lane
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const uint32_t s_col = tmem + S::kS + t * 128 + lanes, o_col = tmem + S::kO + t * D + lanes;
@@ -375,10 +356,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
       asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %1, 0;\n\tbarrier.cta.red.and.aligned.pred q, %2, %3, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
                    : "=r"(out) : "r"((int)yes), "r"(2 + t), "n"(kTileThreads) : "memory");
       return out != 0;
-    };
-    auto sync_tile = [&]() {
-      __syncwarp();
-      asm volatile("bar.sync %0, %1;" ::"r"(2 + t), "n"(kTileThreads) : "memory");
     };
     uint32_t n_s = 0, n_o0 = 0, n_o1 = 0;                 // steps so far of this tile, finished outputs of both
     const float scale_log2 = a.scale_log2;
@@ -409,16 +386,18 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         __syncwarp();
         tc_fence_after();
         const bool masked = p0 + BN > (kCached ? base : first_tok + 1) || p0 + BN > len;
-        uint32_t x[2][32];
-        tmem_ld32_issue(s_col + 64 * hw, x[0]);
-        tmem_ld32_issue(s_col + 64 * hw + 32, x[1]);
+        uint32_t x[4][32];
+        tmem_ld32_issue(s_col, x[0]);
+        tmem_ld32_issue(s_col + 32, x[1]);
+        tmem_ld32_issue(s_col + 64, x[2]);
+        tmem_ld32_issue(s_col + 96, x[3]);
         tmem_wait_ld();
-        reg_fence32(x[0]);
-        reg_fence32(x[1]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) reg_fence32(x[c]);
         if (masked) {
 #pragma unroll
-          for (int c = 0; c < 2; ++c) {
-            const uint32_t bits = seen_bits<kCached>(a, it.seq, tok, p0 + 64 * hw + 32 * c);
+          for (int c = 0; c < 4; ++c) {
+            const uint32_t bits = seen_bits<kCached>(a, it.seq, tok, p0 + 32 * c);
 #pragma unroll
             for (int k = 0; k < 32; ++k)
               if (!((bits >> k) & 1)) x[c][k] = 0xff800000u;
@@ -429,14 +408,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
 #pragma unroll
         for (int k = 0; k < 8; ++k) mx[k] = fmaxf(__uint_as_float(x[0][2 * k]), __uint_as_float(x[0][2 * k + 1]));
 #pragma unroll
-        for (int k = 8; k < 32; ++k) mx[k & 7] = fmaxf(mx[k & 7], fmaxf(__uint_as_float(x[k >> 4][(2 * k) & 31]), __uint_as_float(x[k >> 4][((2 * k) & 31) + 1])));
+        for (int k = 8; k < 64; ++k) mx[k & 7] = fmaxf(mx[k & 7], fmaxf(__uint_as_float(x[k >> 4][(2 * k) & 31]), __uint_as_float(x[k >> 4][((2 * k) & 31) + 1])));
 #pragma unroll
         for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], mx[k + 4]);
-        const float mine = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
-        // the row's other half; its thread cannot come back here before this one has handed over its weights
-        s_x[t][hw][r] = mine;
-        sync_tile();
-        const float mb = fmaxf(mine, s_x[t][hw ^ 1][r]) * scale_log2;
+        const float mb = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale_log2;
         const bool raise = mb > m + kSlack;                // also from -inf
         if (__any_sync(~0u, raise)) {
           const float mn = raise ? mb : m, c = raise ? ex2f(m - mn) : 1.f;
@@ -444,12 +419,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
           l *= c;
           if (i > 0) {
 #pragma unroll 1
-            for (int h = 0; h < D / 32; ++h) {             // half of the columns each
+            for (int h = 0; h < D / 16; ++h) {
               uint32_t o[16];
-              tmem_ld16(o_col + hw * (D / 2) + 16 * h, o);
+              tmem_ld16(o_col + 16 * h, o);
 #pragma unroll
               for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * c);
-              tmem_st16(o_col + hw * (D / 2) + 16 * h, o);
+              tmem_st16(o_col + 16 * h, o);
             }
           }
         }
@@ -459,7 +434,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
           const uint32_t last = pos + 2 * it.blocks() - 1, st = stage(last);
           if (ok) ok = wait_bar(&s_full[st], phase(last), abort_flag, a.limit_ns);
           const int first = max(len - p0, 0), rest = (BN - first) * 8;      // 16-byte pieces of a half
-          for (int u = hw * 128 + r; u < rest * S::kHalves; u += kTileThreads) {
+          for (int u = r; u < rest * S::kHalves; u += kTileThreads) {
             const int h = u / rest, x = u - h * rest;
             asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(ring + st * S::kTileBytes + h * S::kHalfBytes + first * 128 + x * 16),
                          "r"(0)
@@ -470,55 +445,49 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         }
         const float ms = m == -INFINITY ? 0.f : m;
         const float2 scale = make_float2(scale_log2, scale_log2), minus = make_float2(-ms, -ms);
-        float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-        // P of this half over scores that both halves have read by now
+        float2 sum[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
+        for (int c = 0; c < 4; ++c) {
           uint32_t p[16];
 #pragma unroll
           for (int k = 0; k < 16; ++k) {
             float2 e = fma2(make_float2(__uint_as_float(x[c][2 * k]), __uint_as_float(x[c][2 * k + 1])), scale, minus);
-            e = k % 8 == 1 || k % 8 == 4 ? ex2_poly(e) : make_float2(ex2f(e.x), ex2f(e.y));
-            sum[k & 1] = add2(sum[k & 1], e);
+            e = make_float2(ex2f(e.x), ex2f(e.y));
+            sum[k & 3] = add2(sum[k & 3], e);
             p[k] = pack_bf16(e.x, e.y);
           }
-          tmem_st16(s_col + 32 * hw + 16 * c, p);
+          tmem_st16(s_col + 16 * c, p);
+          if (c & 1) {                                     // a half goes
+            tmem_wait_st();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&s_pfull[t][c >> 1]));
+          }
         }
-        l += (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&s_pfull[t][hw]));
+        l += ((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y)) + ((sum[2].x + sum[2].y) + (sum[3].x + sum[3].y));
       }
       pos += 2 * it.blocks();
       if (m == -INFINITY) l = 0.f;
 
-      // the row's sum, from both of its threads
-      sync_tile();
-      s_x[t][hw][r] = l;
-      sync_tile();
-      l += s_x[t][hw ^ 1][r];
-
-      // epilogue: a thread writes half of its row, or, where both tiles hold the same rows, a quarter from both of them
+      // epilogue: a thread writes its row, or, where both tiles hold the same rows, half of the columns from both of them
       float w0 = t ? 0.f : 1.f, w1 = t ? 1.f : 0.f, inv = 1.f;      // weights of the tiles' sums
-      int c0 = hw * (D / 2), c1 = c0 + D / 2;
+      int c0 = 0, c1 = D;
       if (it.both) {
         if (ok) ok = t ? wait_bar(&s_ofull[1], n_o1 & 1, abort_flag, a.limit_ns) : wait_bar(&s_ofull[0], n_o0 & 1, abort_flag, a.limit_ns);
         ++n_o0;
         ++n_o1;
         if (m == -INFINITY) w0 = w1 = 0.f;
       } else {
-        sync_tile();
-        s_x[t][hw][r] = hw ? l : m;
+        s_ml[t][r] = make_float2(m, l);
         sync_both();
-        const float2 x = make_float2(s_x[0][0][r], s_x[0][1][r]), y = make_float2(s_x[1][0][r], s_x[1][1][r]);
+        const float2 x = s_ml[0][r], y = s_ml[1][r];
         m = fmaxf(x.x, y.x);
         const float ms = m == -INFINITY ? 0.f : m;
         w0 = ex2f(x.x - ms);
         w1 = ex2f(y.x - ms);
         l = w0 * x.y + w1 * y.y;
-        c0 = D == 128 ? (2 * t + hw) * 32 : t * 32;
-        c1 = D == 128 || hw == 0 ? c0 + 32 : c0;
+        c0 = t * (D / 2);
+        c1 = c0 + D / 2;
         if (ok) ok = wait_bar(&s_ofull[0], n_o0 & 1, abort_flag, a.limit_ns);
         ++n_o0;
         if (it.blocks() > 1) {
@@ -586,14 +555,14 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
             if (out[k]) out[k] += 64;
       }
       tc_fence_before();
-      if (row_here && c0 == 0 && c1 > c0) {
+      if (row_here && c0 == 0) {
         if (!it.whole) *((float2 *)a.part_ml + part_row) = make_float2(m, l);
         else if (a.lse) a.lse[tg * a.hq + head] = l == 0.f ? -INFINITY : m * kLn2f + logf(l);
       }
-      // rows to form again; also: every thread is done with the outputs and with s_x
+      // rows to form again; also: every thread is done with the outputs and with s_ml
       if (row_here && !finite) s_bad[my_row] = 1;
-      if (it.both) sync_tile(); else sync_both();
-      if (hw == 0 && (it.both || t == 0)) {
+      if (!it.both) sync_both();
+      if (it.both || t == 0) {
         const bool again = s_bad[my_row];
         if (again) s_bad[my_row] = 0;
         __syncwarp();
@@ -605,6 +574,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
       item_done();
     }
   } else {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
     if (warp == 1) {
       // ---- loads: K and V blocks in the order in which the MMAs take them
       bool ok = true;
@@ -816,6 +786,10 @@ pcomoe_status run(const TcMaps &m, const AttnArgs &a, unsigned grid, cudaStream_
   int dev = -1;
   PCOMOE_CUDA_TRY(cudaGetDevice(&dev));
   if (once.first_use(dev)) {
+    // the register split draws on what the block was launched with: with fewer the larger share would never come
+    cudaFuncAttributes at;
+    PCOMOE_CUDA_TRY(cudaFuncGetAttributes(&at, attn_tc_kernel<D, kCached>));
+    if (at.numRegs < kLaunchRegs) return PCOMOE_ERR_CUDA;
     PCOMOE_CUDA_TRY(cudaFuncSetAttribute(attn_tc_kernel<D, kCached>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem));
     once.done(dev);
   }
