@@ -145,28 +145,11 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*(uint64_t *)&a), "l"(*(uint64_t *)&b));
   return *(float2 *)&d;
 }
-// Four rows of 64 bytes, one per lane of a quad, turned so that every store of the quad is 64 contiguous bytes: lane i ends up
-// with piece i of the four rows.  row[k]: where the quad's k-th row goes (this lane's piece), or NULL.
-__device__ __forceinline__ void store_quad(uint32_t (&x)[16], uint8_t *const (&row)[4]) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int h = 1; h <= 2; h <<= 1) {
-    const bool up = lane & h;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      if (c & h) continue;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        // the pieces that belong on the other side of this bit change places
-        uint32_t &lo = x[4 * c + k], &hi = x[4 * (c | h) + k];
-        const uint32_t got = __shfl_xor_sync(~0u, up ? lo : hi, h);
-        if (up) lo = got; else hi = got;
-      }
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < 4; ++k)
-    if (row[k]) *(uint4 *)row[k] = make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+// 32 bytes at once, a whole sector: rows are a thread each, so a warp's stores lie far apart
+__device__ __forceinline__ void store32(void *p, const uint32_t (&x)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]), "r"(x[4]), "r"(x[5]),
+               "r"(x[6]), "r"(x[7])
+               : "memory");
 }
 
 // A piece of work: blocks [b0, b1) of keys for the rows of one tile of 256.
@@ -304,6 +287,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
   __shared__ uint32_t s_tmem;
   __shared__ int s_abort;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const bool wide = (((uintptr_t)a.out | (uintptr_t)(a.out_stride * 2)) & 31) == 0;      // rows begin on whole sectors
   const uint32_t q_at = smem_u32(smem), ring = q_at + 2 * S::kTileBytes;
   volatile int *abort_flag = &s_abort;
 
@@ -470,13 +454,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
       if (m == -INFINITY) l = 0.f;
 
       // epilogue: a thread writes its row, or, where both tiles hold the same rows, half of the columns from both of them
-      float w0 = t ? 0.f : 1.f, w1 = t ? 1.f : 0.f, inv = 1.f;      // weights of the tiles' sums
+      float w0 = 0.f, w1 = 0.f, inv = 1.f;                 // weights of the tiles' sums, where they hold the same rows
       int c0 = 0, c1 = D;
       if (it.both) {
         if (ok) ok = t ? wait_bar(&s_ofull[1], n_o1 & 1, abort_flag, a.limit_ns) : wait_bar(&s_ofull[0], n_o0 & 1, abort_flag, a.limit_ns);
         ++n_o0;
         ++n_o1;
-        if (m == -INFINITY) w0 = w1 = 0.f;
       } else {
         s_ml[t][r] = make_float2(m, l);
         sync_both();
@@ -499,60 +482,71 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
       const int row = it.tile * BM + my_row, head = it.kvh * a.g + row - tok * a.g;
       const int64_t tg = it.seq.q0 + tok, part_row = (int64_t)it.slot * BM + my_row;
       if (it.whole) inv = l == 0.f ? 0.f : 1.f / l;
-      // the rows of this lane's quad, and its piece of 16 bytes of them
-      uint8_t *my_out = nullptr, *out[4];
-      if (row_here) my_out = it.whole ? (uint8_t *)((__nv_bfloat16 *)a.out + tg * a.out_stride + head * D) : (uint8_t *)(a.part + part_row * D);
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        out[k] = (uint8_t *)__shfl_sync(~0u, (unsigned long long)my_out, (lane & ~3) | k);
-        if (out[k]) out[k] += (lane & 3) * 16 + c0 * (it.whole ? 2 : 4);
-      }
       bool finite = true;
-#pragma unroll 1
-      for (int c = c0; c < c1; c += 32) {
-        __syncwarp();
-        tc_fence_after();
-        float o[32];
+      __nv_bfloat16 *out = (__nv_bfloat16 *)a.out + tg * a.out_stride + head * D;
+      float *part = a.part + part_row * D;
+      auto write = [&](uint32_t (&o)[32], int c) {         // columns [c, c + 32) of this thread's row
+        float2 z = make_float2(0.f, 0.f);                  // not 0 where some value is not finite
 #pragma unroll
-        for (int k = 0; k < 32; ++k) o[k] = 0.f;
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          if (it.both ? q != t : q >= it.blocks()) continue;
-          uint32_t x[32];
-          tmem_ld32_issue(tmem + S::kO + q * D + lanes + c, x);
-          tmem_wait_ld();
-          reg_fence32(x);
-          // a tile in which the row saw nothing has no say, whatever its sums hold
-          const float w = q ? w1 : w0;
-          if (w != 0.f)
-#pragma unroll
-            for (int k = 0; k < 32; ++k) o[k] = fmaf(w, __uint_as_float(x[k]), o[k]);
-        }
-        float z = 0.f;                                     // not 0 where some value is not finite
-#pragma unroll
-        for (int k = 0; k < 32; ++k) z = fmaf(o[k], 0.f, z);
-        finite &= z == 0.f;
-        __syncwarp();
-        uint32_t x[16];
+        for (int k = 0; k < 32; k += 2) z = fma2(make_float2(__uint_as_float(o[k]), __uint_as_float(o[k + 1])), make_float2(0.f, 0.f), z);
+        finite &= z.x + z.y == 0.f;
+        if (!row_here) return;
         if (it.whole) {
 #pragma unroll
-          for (int k = 0; k < 16; ++k) x[k] = pack_bf16(o[2 * k] * inv, o[2 * k + 1] * inv);
-          store_quad(x, out);
+          for (int h = 0; h < 2; ++h) {
+            uint32_t x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = pack_bf16(__uint_as_float(o[16 * h + 2 * k]) * inv, __uint_as_float(o[16 * h + 2 * k + 1]) * inv);
+            if (wide) {
+              store32(out + c + 16 * h, x);
+            } else {
+              *(uint4 *)(out + c + 16 * h) = make_uint4(x[0], x[1], x[2], x[3]);
+              *(uint4 *)(out + c + 16 * h + 8) = make_uint4(x[4], x[5], x[6], x[7]);
+            }
+          }
         } else {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
+          for (int h = 0; h < 4; ++h) {
+            uint32_t x[8];
 #pragma unroll
-            for (int k = 0; k < 16; ++k) x[k] = __float_as_uint(o[16 * h + k]);
-            store_quad(x, out);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              if (out[k]) out[k] += 64;
+            for (int k = 0; k < 8; ++k) x[k] = o[8 * h + k];
+            store32(part + c + 8 * h, x);
           }
         }
-        if (it.whole)
+      };
+      tc_fence_after();
+      if (it.both) {
+        if (m == -INFINITY) inv = 0.f;
+#pragma unroll 1
+        for (int c = 0; c < D; c += 32) {
+          uint32_t o[32];
+          __syncwarp();
+          tmem_ld32_issue(o_col + c, o);
+          tmem_wait_ld();
+          reg_fence32(o);
+          if (m == -INFINITY)                              // a row that saw nothing: whatever the sums hold
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            if (out[k]) out[k] += 64;
+            for (int k = 0; k < 32; ++k) o[k] = 0;
+          write(o, c);
+        }
+      } else {
+#pragma unroll 1
+        for (int c = c0; c < c1; c += 32) {
+          uint32_t o[32], y[32];
+          __syncwarp();
+          tmem_ld32_issue(tmem + S::kO + lanes + c, o);
+          if (it.blocks() > 1) tmem_ld32_issue(tmem + S::kO + D + lanes + c, y);
+          tmem_wait_ld();
+          reg_fence32(o);
+          reg_fence32(y);
+          // a tile in which the row saw nothing has no say, whatever its sums hold
+#pragma unroll
+          for (int k = 0; k < 32; ++k) {
+            const float v = w0 != 0.f ? w0 * __uint_as_float(o[k]) : 0.f;
+            o[k] = __float_as_uint(w1 != 0.f ? fmaf(w1, __uint_as_float(y[k]), v) : v);
+          }
+          write(o, c);
+        }
       }
       tc_fence_before();
       if (row_here && c0 == 0) {
