@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(kThreads) simt_cached_kernel(AttnArgs a) {
   extern __shared__ float4 sm4[];
   CacheWalk<BM, BN, 2> w;
   typename CacheWalk<BM, BN, 2>::Piece p;
-  w.start(a, blockIdx.x, gridDim.x, 2);
+  w.start(a, blockIdx.x, gridDim.x, 1);
   while (w.next(a, p))
     run_piece<D, BM, true>(a, w.seq, p.kvh, p.tile, p.b0, p.b1, p.whole, part_slot(blockIdx.x, p.b0 == 0), (float *)sm4);
   if (threadIdx.x == 0) w.record(a, blockIdx.x);
@@ -243,7 +243,9 @@ pcomoe_status run(const AttnArgs &a, int sms, cudaStream_t st) {
 size_t attn_simt_part_rows(int sms) { return (size_t)4 * sms * 64; }
 
 pcomoe_status launch_attn_simt(const AttnArgs &a, int D, int sms, cudaStream_t st) {
-  const bool narrow = (int64_t)a.T * a.g <= (int64_t)16 * a.n_seqs;
+  // Narrow tiles: where a sequence has at most 16 rows on average, and for prompts also where wide ones would not give every
+  // SM a tile (their number is what counts then).
+  const bool narrow = (int64_t)a.T * a.g <= (int64_t)16 * a.n_seqs || (!a.table && ((int64_t)a.T * a.g / 64 + a.n_seqs) * a.hkv < sms);
   if (D == 64) return narrow ? run<64, 16>(a, sms, st) : run<64, 64>(a, sms, st);
   return narrow ? run<128, 16>(a, sms, st) : run<128, 64>(a, sms, st);
 }

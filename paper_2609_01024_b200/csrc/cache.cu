@@ -217,9 +217,17 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(CacheDev c, 
 // Whole pages from src to dst in every layer, K and V.  A block moves 16 KB pieces: four 16-byte loads per thread in
 // flight before the first store.
 constexpr int kPiece = 16384;
+template <bool kRemap>
 __global__ void __launch_bounds__(256) move_pages_kernel(CacheDev c, CacheWs w) {
   pdl_grid_wait();
   const int n = w.head->n_moves;
+  if (kRemap && n) {                                      // the page tables follow the pages
+    const int64_t entries = (int64_t)c.max_seqs * c.max_pages;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < entries; i += (int64_t)gridDim.x * blockDim.x) {
+      const int p = c.table[i];
+      if (p >= 0 && p < c.pages) c.table[i] = w.list[p];
+    }
+  }
   const int pieces = (int)((c.page_bytes + kPiece - 1) / kPiece);
   const int64_t units = (int64_t)n * 2 * c.layers * pieces;
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
@@ -452,20 +460,11 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(CacheDev c, 
   if (tid == 0) w.head->n_moves = moves;
 }
 
-__global__ void __launch_bounds__(256) remap_tables_kernel(CacheDev c, CacheWs w) {
-  pdl_grid_wait();
-  if (w.head->n_moves == 0) return;
-  const int64_t n = (int64_t)c.max_seqs * c.max_pages;
-  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
-    const int p = c.table[i];
-    if (p >= 0 && p < c.pages) c.table[i] = w.list[p];
-  }
-}
-
+template <bool kRemap>
 pcomoe_status launch_moves(const CacheDev &c, const CacheWs &w, int64_t most, int sms, cudaStream_t st) {
   const int64_t units = most * 2 * c.layers * ((c.page_bytes + kPiece - 1) / kPiece);
   const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(units, (int64_t)sms * 8));
-  PCOMOE_CUDA_TRY(launch_pdl(move_pages_kernel, dim3(grid), dim3(256), 0, st, c, w));
+  PCOMOE_CUDA_TRY(launch_pdl(move_pages_kernel<kRemap>, dim3(grid), dim3(256), 0, st, c, w));
   count_launch();
   return PCOMOE_OK;
 }
@@ -524,7 +523,7 @@ pcomoe_status pcomoe_cache_reserve(const pcomoe_cache *cache, int32_t n, const i
   const CacheWs w = cache_ws(cache, d_workspace);
   PCOMOE_CUDA_TRY(launch_pdl(reserve_plan_kernel, dim3(1), dim3(kPlanThreads), 0, (cudaStream_t)stream, c, n, d_seqs, d_add, w));
   count_launch();
-  return launch_moves(c, w, n, sms, (cudaStream_t)stream);
+  return launch_moves<false>(c, w, n, sms, (cudaStream_t)stream);
 }
 
 pcomoe_status pcomoe_cache_write(const pcomoe_cache *cache, int32_t first_layer, int32_t n_layers, int32_t T, int32_t n,
@@ -595,12 +594,7 @@ pcomoe_status pcomoe_cache_compact(const pcomoe_cache *cache, void *d_workspace,
   const CacheWs w = cache_ws(cache, d_workspace);
   PCOMOE_CUDA_TRY(launch_pdl(compact_plan_kernel, dim3(1), dim3(kPlanThreads), 0, (cudaStream_t)stream, c, w));
   count_launch();
-  if ((st = launch_moves(c, w, (c.pages + 1) / 2, sms, (cudaStream_t)stream)) != PCOMOE_OK) return st;
-  const int64_t n = (int64_t)c.max_seqs * c.max_pages;
-  const int grid = (int)std::min<int64_t>((n + 255) / 256, (int64_t)sms * 8);
-  PCOMOE_CUDA_TRY(launch_pdl(remap_tables_kernel, dim3(grid), dim3(256), 0, (cudaStream_t)stream, c, w));
-  count_launch();
-  return PCOMOE_OK;
+  return launch_moves<true>(c, w, (c.pages + 1) / 2, sms, (cudaStream_t)stream);
 }
 
 }  // extern "C"
