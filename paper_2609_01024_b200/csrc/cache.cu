@@ -120,7 +120,14 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(CacheDev c, 
   __shared__ int s_first[kMaxSeqs];             // pages given to the entries before i
   __shared__ uint32_t s_seen[kMaxSeqs / 32], s_copy[kMaxSeqs / 32];
   __shared__ int s_scan[33], s_bad, s_copies;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31, wp = tid >> 5;
+  // the free pages of each warp's contiguous run of the reference counts: their loads are under way while the chain list
+  // -> length -> table -> count below is followed
+  const int run = ((c.pages + 1023) / 1024) * 32;      // pages of a warp, a multiple of 32
+  const int lo = min(wp * run, c.pages), hi = min(lo + run, c.pages);
+  int mine = 0;
+#pragma unroll 4
+  for (int p = lo + lane; p < hi; p += 32) mine += c.ref[p] == 0;
   for (int i = tid; i < kMaxSeqs / 32; i += kPlanThreads) s_seen[i] = s_copy[i] = 0;
   if (tid == 0) { s_bad = 0; s_copies = 0; w.head->n_moves = 0; }
   __syncthreads();
@@ -169,12 +176,7 @@ __global__ void __launch_bounds__(kPlanThreads) reserve_plan_kernel(CacheDev c, 
     if (i < n) s_first[i] = total + first;
     total += sum;
   }
-  // the free pages in order: a warp takes a contiguous run of the reference counts
-  const int lane = tid & 31, wp = tid >> 5;
-  const int run = ((c.pages + 1023) / 1024) * 32;      // pages of a warp, a multiple of 32
-  const int lo = min(wp * run, c.pages), hi = min(lo + run, c.pages);
-  int mine = 0;
-  for (int p = lo + lane; p < hi; p += 32) mine += c.ref[p] == 0;
+  // the free pages in order
 #pragma unroll
   for (int o = 16; o; o >>= 1) mine += __shfl_xor_sync(~0u, mine, o);
   int free_pages;

@@ -218,23 +218,26 @@ __global__ void __launch_bounds__(32 * kWarps) scores_kernel(Args a) {
 #pragma unroll
     for (int u = 0; u < kLoads; ++u) v[u] = raw[u];
     if (g + W * kLoads < g1) fetch(g + W * kLoads);      // on its way while this one is summed
-    int most = kNoKey;
+    int key[kLoads];
 #pragma unroll
-    for (int u = 0; u < kLoads; ++u) {
-      const float mx = Vec<T>::largest(v[u]);
-      int key = __reduce_max_sync(~0u, mx == mx ? key_of(mx) : kNoKey);
-      if (key >= key_of(INFINITY)) {                     // an infinite logit: it does not count
+    for (int u = 0; u < kLoads; ++u) key[u] = __reduce_max_sync(~0u, key_of(Vec<T>::largest(v[u])));
+    int most = max(max(key[0], key[1]), max(key[2], key[3]));
+    if (most >= key_of(INFINITY)) {                      // infinite logits (or nothing but NaN in a lane): they do not count
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {
         float x[N];
         Vec<T>::unpack(v[u], x);
 #pragma unroll
         for (int k = 0; k < N; ++k) x[k] = eligible(x[k]);
         v[u] = Vec<T>::pack(x);
-        key = __reduce_max_sync(~0u, key_of(Vec<T>::largest(v[u])));
+        key[u] = __reduce_max_sync(~0u, key_of(Vec<T>::largest(v[u])));
       }
-      if (lane == 0 && g + u < g1) s_group[g + u - g0] = key;
-      most = max(most, key);
+      most = max(max(key[0], key[1]), max(key[2], key[3]));
     }
-    if (most == kNoKey) continue;
+    static_assert(kLoads == 4, "a lane per group of the iteration");
+    if (lane < kLoads && g + lane < g1)                  // (a NaN's key may lie below -inf's)
+      s_group[g + lane - g0] = max(lane < 2 ? (lane ? key[1] : key[0]) : (lane == 2 ? key[2] : key[3]), kNoKey);
+    if (most <= kNoKey) continue;
     const float m = of_key(most);
     if (m > most_so_far) {
       if (acc.s > 0.f) {
