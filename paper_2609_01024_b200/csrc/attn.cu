@@ -42,6 +42,7 @@ pcomoe_status fill(AttnArgs &a, const pcomoe_attn_config *c, int32_t T, int32_t 
   if (!ws || ((uintptr_t)ws & 255) || ws_bytes < kPartAt + rows * (c->head_dim + 2) * sizeof(float)) return PCOMOE_ERR_WORKSPACE;
   a = AttnArgs{};
   a.T = T; a.n_seqs = n_seqs; a.hq = c->q_heads; a.hkv = c->kv_heads; a.g = c->q_heads / c->kv_heads;
+  a.sms = sms;
   a.scale_log2 = c->scale * 1.4426950408889634f;
   a.cu = cu; a.q = q; a.q_stride = q_stride; a.out = out; a.out_stride = out_stride; a.lse = lse;
   a.status = (int32_t *)((char *)ws + offsetof(DevPlan, status_router));

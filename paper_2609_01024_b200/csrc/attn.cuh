@@ -14,7 +14,7 @@
 namespace pcomoe {
 
 struct AttnArgs {
-  int32_t T, n_seqs, hq, hkv, g;
+  int32_t T, n_seqs, hq, hkv, g, sms;
   float scale_log2;                     // scale * log2(e)
   const int32_t *cu, *seqs;
   const void *q, *k, *v;                // k, v: packed rows, or the layer's page pools
@@ -93,12 +93,12 @@ __device__ __forceinline__ Seq load_seq(const AttnArgs &a, int s) {
   return r;
 }
 
-// Blocks of BN keys that tile `tile` (BM rows) of a sequence looks at; at least one, so that rows that see nothing are
+// Blocks of BN keys that the rows before `row_end` of a sequence look at; at least one, so that rows that see nothing are
 // still written.
-template <bool kCached, int BM, int BN>
-__device__ __forceinline__ int tile_blocks(const AttnArgs &a, const Seq &s, int tile) {
+template <bool kCached, int BN>
+__device__ __forceinline__ int key_blocks(const AttnArgs &a, const Seq &s, int row_end) {
   int keys = s.len;
-  if (!kCached) keys = min(keys, (min((tile + 1) * BM, s.n * a.g) - 1) / a.g + 1);
+  if (!kCached) keys = min(keys, (min(row_end, s.n * a.g) - 1) / a.g + 1);
   return max(1, (keys + BN - 1) / BN);
 }
 
@@ -261,10 +261,10 @@ __device__ __forceinline__ int64_t page_row(const AttnArgs &a, const int32_t *ta
 // One bf16 row without the tensor cores, by a warp, each lane its columns of the head: positions [p0, p1) that the row
 // sees.  For rows that met a NaN or infinity they do not see (weight 0 times it); rare, so plain.
 template <int D, int BM, bool kCached>
-__device__ __forceinline__ void plain_row(const AttnArgs &a, const Seq &s, int kvh, int tile, int r, int p0, int p1, bool whole, int slot) {
+__device__ __forceinline__ void plain_row(const AttnArgs &a, const Seq &s, int kvh, int row0, int r, int p0, int p1, bool whole, int slot) {
   constexpr int N = D / 32;
   const int lane = threadIdx.x & 31;
-  const int row = tile * BM + r, tok = row / a.g, head = kvh * a.g + row - tok * a.g;
+  const int row = row0 + r, tok = row / a.g, head = kvh * a.g + row - tok * a.g;
   const int64_t t = s.q0 + tok;
   float q[N], o[N], m = -INFINITY, l = 0.f;
 #pragma unroll

@@ -237,7 +237,7 @@ __global__ void __launch_bounds__(kThreads, 2) few_kernel(AttnArgs a) {
     __syncthreads();
     if (s_again) {
       for (int r = warp; r < rows; r += kWarps)
-        if (s_bad[r]) plain_row<D, BM, true>(a, seq, p.kvh, p.tile, r, p.b0 * BN, p.b1 * BN, p.whole, slot);
+        if (s_bad[r]) plain_row<D, BM, true>(a, seq, p.kvh, p.tile * BM, r, p.b0 * BN, p.b1 * BN, p.whole, slot);
       __syncthreads();
     }
     __syncthreads();                                       // the rings are free again

@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(kThreads) simt_prompt_kernel(AttnArgs a) {
   }
   if (tile < 0) return;
   const Seq seq = load_seq<false>(a, s);
-  run_piece<D, BM, false>(a, seq, blockIdx.y, tile, 0, tile_blocks<false, BM, BN>(a, seq, tile), true, 0, (float *)sm4);
+  run_piece<D, BM, false>(a, seq, blockIdx.y, tile, 0, key_blocks<false, BN>(a, seq, (tile + 1) * BM), true, 0, (float *)sm4);
 }
 
 template <typename F>

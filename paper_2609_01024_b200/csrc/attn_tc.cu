@@ -152,11 +152,11 @@ __device__ __forceinline__ void store32(void *p, const uint32_t (&x)[8]) {
                : "memory");
 }
 
-// A piece of work: blocks [b0, b1) of keys for the rows of one tile of 256.
+// A piece of work: blocks [b0, b1) of keys for the rows of one tile.
 struct Item {
   Seq seq;
-  int kvh, tile, b0, b1;
-  int rows;             // of 256; 0: no more work
+  int kvh, row0, b0, b1;
+  int rows;             // up to 256 from row0 on; 0: no more work
   bool both;            // two tiles of rows; else two sets of blocks for one tile
   bool whole;
   int slot;             // place of a partial result
@@ -173,9 +173,9 @@ template <> struct Walk<true> {
   __device__ bool next(const AttnArgs &a, Item &it) {
     CacheWalk<BM, BN, 2>::Piece p;
     if (!w.next(a, p)) return false;
-    it.seq = w.seq; it.kvh = p.kvh; it.tile = p.tile; it.b0 = p.b0; it.b1 = p.b1;
+    it.seq = w.seq; it.kvh = p.kvh; it.row0 = p.tile * BM; it.b0 = p.b0; it.b1 = p.b1;
     it.whole = p.whole; it.slot = part_slot(blockIdx.x, p.b0 == 0);
-    it.rows = min(BM, it.seq.n * a.g - it.tile * BM);
+    it.rows = min(BM, it.seq.n * a.g - it.row0);
     it.both = it.rows > 128;
     return true;
   }
@@ -191,10 +191,13 @@ template <> struct Walk<false> {
   int mine[4];
   int total;
   bool first;
-  __device__ static int tiles_of(const AttnArgs &a, int s) { return s < a.n_seqs ? (load_seq<false>(a, s).n * a.g + BM - 1) / BM : 0; }
+  int rows;             // of a tile: 256, or 128 where that leaves SMs idle (its keys then go to both halves of the CTA)
+  __device__ int tiles_of(const AttnArgs &a, int s) const { return s < a.n_seqs ? (load_seq<false>(a, s).n * a.g + rows - 1) / rows : 0; }
   __device__ static int sum(int x) { return (int)__reduce_add_sync(~0u, (unsigned)x); }
   __device__ void start(const AttnArgs &a) {
     const int lane = threadIdx.x & 31;
+    // (a bound of the host's kind: every sequence may end in a part of a tile)
+    rows = ((int64_t)a.T * a.g / BM + a.n_seqs) * a.hkv < a.sms ? 128 : BM;
     total = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k) total += mine[k] = tiles_of(a, 32 * k + lane);
@@ -214,7 +217,7 @@ template <> struct Walk<false> {
     first = false;
     if (w >= total * a.hkv) return false;
     it.kvh = w % a.hkv;
-    int want = w / a.hkv, s = 0;
+    int want = w / a.hkv, s = 0, tile = 0;
     if (a.n_seqs <= 128) {
       int lo = 0, hi = (int)__reduce_max_sync(~0u, (unsigned)max(max(mine[0], mine[1]), max(mine[2], mine[3])));
       while (hi - lo > 1) {                                // the largest number with more than `want` tiles from it on
@@ -222,7 +225,7 @@ template <> struct Walk<false> {
         if (from(mid) > want) lo = mid; else hi = mid;
       }
       want -= from(lo + 1);                                // the want-th of the sequences that have tile lo
-      it.tile = lo;
+      tile = lo;
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         const uint32_t b = __ballot_sync(~0u, mine[k] > lo);
@@ -244,16 +247,17 @@ template <> struct Walk<false> {
         if (hit) {
           const int l = __ffs(hit) - 1;
           s = s0 + l;
-          it.tile = want - __shfl_sync(~0u, upto - n, l);
+          tile = want - __shfl_sync(~0u, upto - n, l);
           break;
         }
         want -= __shfl_sync(~0u, upto, 31);
       }
     }
     it.seq = load_seq<false>(a, s);
-    it.b0 = 0; it.b1 = tile_blocks<false, BM, BN>(a, it.seq, it.tile);
+    it.row0 = tile * rows;
+    it.b0 = 0; it.b1 = key_blocks<false, BN>(a, it.seq, it.row0 + rows);
     it.whole = true; it.slot = 0;
-    it.rows = min(BM, it.seq.n * a.g - it.tile * BM);
+    it.rows = min(rows, it.seq.n * a.g - it.row0);
     it.both = it.rows > 128;
     return true;
   }
@@ -270,7 +274,7 @@ __device__ __forceinline__ int tile_steps(const AttnArgs &a, const Item &it, int
   const int n = it.blocks();
   if (!it.both) return (n + 1 - t) >> 1;
   if (kCached || t) return n;
-  return min(n, tile_blocks<false, 128, BN>(a, it.seq, 2 * it.tile) - it.b0);
+  return min(n, key_blocks<false, BN>(a, it.seq, it.row0 + 128) - it.b0);
 }
 
 template <int D, bool kCached>
@@ -359,7 +363,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
       const Item &it = s_item[n_item & 1];
       if (it.rows == 0) break;
       const int my_row = it.both ? t * 128 + r : r;       // of the item's rows
-      const int tok = (it.tile * BM + min(my_row, it.rows - 1)) / a.g;
+      const int tok = (it.row0 + min(my_row, it.rows - 1)) / a.g;
       const int first_tok = __shfl_sync(~0u, tok, 0);
       const int steps = tile_steps<kCached>(a, it, t), len = it.seq.len, base = it.seq.base, b0 = it.b0, b_last = it.b1 - 1;
       const bool both = it.both;                           // (in registers: shared memory is busy feeding the MMAs)
@@ -479,7 +483,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         }
       }
       const bool row_here = my_row < it.rows;
-      const int row = it.tile * BM + my_row, head = it.kvh * a.g + row - tok * a.g;
+      const int row = it.row0 + my_row, head = it.kvh * a.g + row - tok * a.g;
       const int64_t tg = it.seq.q0 + tok, part_row = (int64_t)it.slot * BM + my_row;
       if (it.whole) inv = l == 0.f ? 0.f : 1.f / l;
       bool finite = true;
@@ -562,7 +566,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         __syncwarp();
         for (uint32_t todo = __ballot_sync(~0u, again); todo; todo &= todo - 1) {
           const int x = (it.both ? t * 128 : 0) + (warp & 3) * 32 + __ffs(todo) - 1;
-          plain_row<D, BM, kCached>(a, it.seq, it.kvh, it.tile, x, it.b0 * BN, it.b1 * BN, it.whole, it.slot);
+          plain_row<D, BM, kCached>(a, it.seq, it.kvh, it.row0, x, it.b0 * BN, it.b1 * BN, it.whole, it.slot);
         }
       }
       item_done();
@@ -624,7 +628,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
             if (lane == 0) mbar_arrive_expect_tx(smem_u32(&s_qfull[q]), S::kTileBytes);
             __syncwarp();
             if (lane < S::kHalves)
-              tma_load_3d(q_at + q * S::kTileBytes + lane * S::kHalfBytes, &maps.q, lane * 64, it.kvh * a.g, it.seq.q0 + (it.tile * BM + q * 128) / a.g,
+              tma_load_3d(q_at + q * S::kTileBytes + lane * S::kHalfBytes, &maps.q, lane * 64, it.kvh * a.g, it.seq.q0 + (it.row0 + q * 128) / a.g,
                           smem_u32(&s_qfull[q]));
             continue;
           }
@@ -632,7 +636,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
           constexpr int C = D / 8, P = 32 / C;             // pieces of a row; rows that a warp copies side by side
           const int c = lane % C;
           const uint32_t to = q_at + q * S::kTileBytes + (c >> 3) * S::kHalfBytes;
-          int tok = (it.tile * BM + q * 128 + lane / C) / a.g, hd = it.tile * BM + q * 128 + lane / C - tok * a.g;
+          int tok = (it.row0 + q * 128 + lane / C) / a.g, hd = it.row0 + q * 128 + lane / C - tok * a.g;
           for (int qr = lane / C; qr < 128; qr += P) {
             const bool there = qr < rows;
             const __nv_bfloat16 *src = (const __nv_bfloat16 *)a.q + (there ? (int64_t)(it.seq.q0 + tok) * a.q_stride + (it.kvh * a.g + hd) * D + c * 8 : 0);
@@ -816,7 +820,7 @@ pcomoe_status launch_attn_tc(const AttnArgs &a, int D, int sms, cudaStream_t st)
   }
   if (!make_rows_map(&m.k, a.k, a.T, (uint64_t)a.hkv * D, a.k_stride, BN) || !make_rows_map(&m.v, a.v, a.T, (uint64_t)a.hkv * D, a.v_stride, BN))
     return PCOMOE_ERR_CUDA;
-  const int64_t tiles = ((int64_t)a.T * a.g / BM + std::min(a.n_seqs, a.T)) * a.hkv;      // no more than that
+  const int64_t tiles = ((int64_t)a.T * a.g / 128 + std::min(a.n_seqs, a.T)) * a.hkv;      // no more than that
   if (tiles > INT32_MAX) return PCOMOE_ERR_SHAPE;
   const unsigned grid = (unsigned)std::min<int64_t>(tiles, sms);
   return D == 64 ? run<64, false>(m, a, grid, st) : run<128, false>(m, a, grid, st);

@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(32 * kWarps) scores_kernel(Args a) {
   struct Team {
     Sums sums[W];
     unsigned long long cand[kMaxCand];
-    int pick[kMaxTop], nc, count[W];
+    int pick[kMaxTop], nc, count[2][W];
     struct { Sums sums; int key[kMaxTop], id[kMaxTop]; } out;      // what the cluster's first block collects
     float m, tail;                                       // reference, ln 2 (r - log2 s)
   };
@@ -339,7 +339,9 @@ __global__ void __launch_bounds__(32 * kWarps) scores_kernel(Args a) {
     int n_pick = 0;
     while (n_pick < want && s.pick[n_pick] >= 0) ++n_pick;
     int floor_key = n_pick ? s_group[s.pick[n_pick - 1]] : INT_MAX;
-    if (n_pick && n_pick < want) {
+    if (n_pick && n_pick < want && n_pick * 32 * N <= kMaxCand) {
+      floor_key = kNoKey + 1;                            // there is room for all their words
+    } else if (n_pick && n_pick < want) {
       // fewer groups than ranks: the same bound from single lanes' words, by bisection of the key (the largest key that
       // at least `want` lanes reach)
       constexpr int kMine = (kMaxTop + W - 1) / W;
@@ -354,18 +356,17 @@ __global__ void __launch_bounds__(32 * kWarps) scores_kernel(Args a) {
           for (int k = 0; k < N; ++k) most[q] = max(most[q], key_of(eligible(x[k])));
         }
       }
-      int64_t lo = kNoKey + 1, hi = (int64_t)key_of(INFINITY);          // reached by enough lanes (or the least); not reached
-      while (hi - lo > 1) {
+      int64_t lo = kNoKey + 1, hi = (int64_t)s_group[s.pick[0]] + 1;      // reached by enough lanes (or the least); not reached
+      for (int turn = 0; hi - lo > 1; turn ^= 1) {
         const int64_t mid = (lo + hi) >> 1;
         int mine = 0;
 #pragma unroll
         for (int q = 0; q < kMine; ++q) mine += most[q] >= mid;
         int all = __reduce_add_sync(~0u, mine);
-        if (lane == 0) s.count[warp] = all;
+        if (lane == 0) s.count[turn][warp] = all;
         sync();
         all = 0;
-        for (int q = 0; q < W; ++q) all += s.count[q];
-        sync();
+        for (int q = 0; q < W; ++q) all += s.count[turn][q];
         if (all >= want) lo = mid; else hi = mid;
       }
       floor_key = (int)lo;
