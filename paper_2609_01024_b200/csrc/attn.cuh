@@ -57,6 +57,11 @@ __device__ __forceinline__ float ex2f(float x) {
   return y;
 }
 
+// 16 bytes to shared memory; zeros where there is nothing to copy
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+
 struct Seq {
   int q0, n;            // first packed row and their number
   int len, base;        // keys; those before `base` are seen by every row, the others by mask or order

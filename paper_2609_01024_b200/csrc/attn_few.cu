@@ -20,9 +20,6 @@ constexpr int kExtra = 3;              // blocks of 64 keys that a piece of work
 template <int D> constexpr int stage_bytes() { return 2 * kKeys * D * 2; }
 template <int D> constexpr int smem_bytes() { return kWarps * kStages * stage_bytes<D>(); }
 
-__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
 __device__ __forceinline__ void ldsm4(uint32_t at, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }

@@ -15,23 +15,26 @@ namespace {
 
 constexpr int BN = 64, kThreads = 256;
 
-template <int D, int BM> constexpr int smem_floats() { return (BM + 2 * BN) * (D + 4) + BM * (BN + 4); }
+template <int D, int BM> constexpr int smem_floats() { return (BM + 2 * BN) * (D + 4); }
 
-template <int D, int BM, bool kCached>
-__device__ void run_piece(const AttnArgs &a, const Seq &s, int kvh, int tile, int b0, int b1, bool whole, int slot, float *sm) {
-  constexpr int RM = BM / 16, DP = D + 4, PP = BN + 4, NC = D / 64;
-  float *Q = sm, *K = Q + BM * DP, *V = K + BN * DP, *P = V + BN * DP;
+// RM: rows of a thread; a tile with few rows left takes fewer of them.
+
+template <int D, int BM, int RM, bool kCached>
+__device__ __forceinline__ void run_rows(const AttnArgs &a, const Seq &s, int kvh, int tile, int b0, int b1, bool whole, int slot, float *sm) {
+  constexpr int DP = D + 4, PP = BN + 4, NC = D / 64;
+  static_assert(BM * PP <= BN * DP, "the weights fit over the keys");
+  float *Q = sm, *K = Q + BM * DP, *V = K + BN * DP, *P = K;      // weights over the keys, once every thread has its scores
   const int tid = threadIdx.x, ty = tid >> 4, tx = tid & 15;
-  const int rows = min(BM, s.n * a.g - tile * BM);
+  const int rows = min(16 * RM, s.n * a.g - tile * BM);
+  // Everything comes in by asynchronous copies: the page lookups of all of a thread's rows are under way at once, and the
+  // values arrive while the scores are formed.
+  constexpr int kRowChunks = D / 4;
   __syncthreads();                                        // the last piece's readers are done
-  for (int u = tid; u < BM * (D / 4); u += kThreads) {
-    const int r = u / (D / 4), c = u - r * (D / 4);
-    float4 x = {0.f, 0.f, 0.f, 0.f};
-    if (r < rows) {
-      const int row = tile * BM + r, tok = row / a.g, head = kvh * a.g + row - tok * a.g;
-      x = *(const float4 *)((const float *)a.q + (int64_t)(s.q0 + tok) * a.q_stride + head * D + 4 * c);
-    }
-    *(float4 *)(Q + r * DP + 4 * c) = x;
+#pragma unroll
+  for (int i = 0; i < 16 * RM * kRowChunks / kThreads; ++i) {
+    const int u = tid + i * kThreads, r = u / kRowChunks, c = u - r * kRowChunks;
+    const int row = tile * BM + min(r, rows - 1), t = row / a.g, head = kvh * a.g + row - t * a.g;
+    copy16(smem_u32(Q + r * DP + 4 * c), (const float *)a.q + (int64_t)(s.q0 + t) * a.q_stride + head * D + 4 * c, r < rows);
   }
   float m[RM], l[RM];
   float4 o[RM][NC];
@@ -48,22 +51,28 @@ __device__ void run_piece(const AttnArgs &a, const Seq &s, int kvh, int tile, in
   for (int b = b0; b < b1; ++b) {
     const int p0 = b * BN;
     __syncthreads();
-    for (int u = tid; u < BN * (D / 4); u += kThreads) {
-      const int r = u / (D / 4), c = u - r * (D / 4), p = p0 + r;
-      float4 x = {0.f, 0.f, 0.f, 0.f}, y = x;               // past the end: zero, so that no stale value can matter
-      if (p < s.len) {
-        if (kCached) {
-          const int64_t at = page_row(a, table, kvh, p) * D + 4 * c;
-          x = *(const float4 *)((const float *)a.k + at);
-          y = *(const float4 *)((const float *)a.v + at);
-        } else {
-          x = *(const float4 *)((const float *)a.k + (int64_t)(s.q0 + p) * a.k_stride + kvh * D + 4 * c);
-          y = *(const float4 *)((const float *)a.v + (int64_t)(s.q0 + p) * a.v_stride + kvh * D + 4 * c);
-        }
-      }
-      *(float4 *)(K + r * DP + 4 * c) = x;
-      *(float4 *)(V + r * DP + 4 * c) = y;
+    constexpr int kCopies = BN * kRowChunks / kThreads;
+    const int c4 = 4 * (tid % kRowChunks);
+    int64_t from[kCopies];
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      const int p = p0 + (tid + i * kThreads) / kRowChunks;
+      from[i] = p >= s.len ? -1 : kCached ? page_row(a, table, kvh, p) : s.q0 + p;
     }
+    // past the end: zero, so that no stale value can matter
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      const int64_t at = max(from[i], (int64_t)0) * (kCached ? D : a.k_stride) + (kCached ? 0 : kvh * D) + c4;
+      copy16(smem_u32(K + (tid + i * kThreads) / kRowChunks * DP + c4), (const float *)a.k + at, from[i] >= 0);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < kCopies; ++i) {
+      const int64_t at = max(from[i], (int64_t)0) * (kCached ? D : a.v_stride) + (kCached ? 0 : kvh * D) + c4;
+      copy16(smem_u32(V + (tid + i * kThreads) / kRowChunks * DP + c4), (const float *)a.v + at, from[i] >= 0);
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    asm volatile("cp.async.wait_group 1;" ::: "memory");
     __syncthreads();
     float acc[RM][4];
 #pragma unroll
@@ -85,6 +94,15 @@ __device__ void run_piece(const AttnArgs &a, const Seq &s, int kvh, int tile, in
     }
     // some row of the tile may not see all of the block
     const bool masked = p0 + BN > s.base || p0 + BN > s.len;
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    float odd = 0.f;                                         // NaN once a value that this thread copied is NaN or infinite
+    if (masked)
+#pragma unroll
+      for (int i = 0; i < kCopies; ++i) {
+        const float4 y = *(const float4 *)(V + (tid + i * kThreads) / kRowChunks * DP + c4);
+        odd = fmaf(0.f, y.x, fmaf(0.f, y.y, fmaf(0.f, y.z, fmaf(0.f, y.w, odd))));
+      }
+    const bool careful = __syncthreads_or(odd != 0.f);       // the values are there, and every thread is done with the keys
 #pragma unroll
     for (int i = 0; i < RM; ++i) {
       float x[4], mx = -INFINITY;
@@ -118,7 +136,7 @@ __device__ void run_piece(const AttnArgs &a, const Seq &s, int kvh, int tile, in
       for (int c = 0; c < NC; ++c) { o[i][c].x *= r; o[i][c].y *= r; o[i][c].z *= r; o[i][c].w *= r; }
     }
     __syncwarp();                                            // a row's weights are written and read by one warp
-    if (!masked) {
+    if (!careful) {
 #pragma unroll 4
       for (int n = 0; n < BN; ++n)
 #pragma unroll
@@ -170,8 +188,19 @@ __device__ void run_piece(const AttnArgs &a, const Seq &s, int kvh, int tile, in
   }
 }
 
+template <int D, int BM, bool kCached>
+__device__ __forceinline__ void run_piece(const AttnArgs &a, const Seq &s, int kvh, int tile, int b0, int b1, bool whole, int slot, float *sm) {
+  const int rows = s.n * a.g - tile * BM;
+  if (BM == 16 || rows <= 16)
+    run_rows<D, BM, 1, kCached>(a, s, kvh, tile, b0, b1, whole, slot, sm);
+  else if (rows <= 32)
+    run_rows<D, BM, 2, kCached>(a, s, kvh, tile, b0, b1, whole, slot, sm);
+  else
+    run_rows<D, BM, 4, kCached>(a, s, kvh, tile, b0, b1, whole, slot, sm);
+}
+
 template <int D, int BM>
-__global__ void __launch_bounds__(kThreads) simt_cached_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) simt_cached_kernel(AttnArgs a) {
   pdl_grid_wait();
   extern __shared__ float4 sm4[];
   CacheWalk<BM, BN, 2> w;
@@ -184,7 +213,7 @@ __global__ void __launch_bounds__(kThreads) simt_cached_kernel(AttnArgs a) {
 
 // One tile per block; the tiles are counted from the last one back, so that those with the most keys start first.
 template <int D, int BM>
-__global__ void __launch_bounds__(kThreads) simt_prompt_kernel(AttnArgs a) {
+__global__ void __launch_bounds__(kThreads, 2) simt_prompt_kernel(AttnArgs a) {
   pdl_grid_wait();
   extern __shared__ float4 sm4[];
   const int lane = threadIdx.x & 31;
