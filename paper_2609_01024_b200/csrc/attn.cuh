@@ -133,7 +133,10 @@ __device__ __forceinline__ uint32_t seen_bits(const AttnArgs &a, const Seq &s, i
 // A CTA's share of the line of blocks, and its walk along it.  All of it is the same in every thread of a warp.  A tile
 // counts for its blocks and kExtra more, which stand for what a piece of work costs besides (a sequence of one block of keys
 // is no cheaper to begin than one of a thousand): without them the CTA that met the shortest sequences finished last.
-template <int BM, int BN, int kExtra>
+// (A share is never less than one block, so that short sequences still spread over the GPU: with shares of four blocks and
+// more a draft tree over 100 to 400 keys took 20 us instead of 14.)  Where every tile can have a CTA of its own and none
+// is longer than kFlat blocks, tiles are not cut: parts would cost more to write and join than they save.
+template <int BM, int BN, int kExtra, int kFlat>
 struct CacheWalk {
   uint32_t at, end;     // units of this share still to do
   uint32_t share;
@@ -141,43 +144,56 @@ struct CacheWalk {
   int s;                // sequence
   Seq seq;
   int tiles, blocks;    // of the current sequence: row tiles, blocks of a tile
+  bool flat;            // a CTA per tile: a tile is one unit
 
   __device__ void measure(const AttnArgs &a) {
     seq = load_seq<true>(a, s);
     tiles = (seq.n * a.g + BM - 1) / BM;
     blocks = max(1, (seq.len + BN - 1) / BN);
   }
-  __device__ uint32_t units() const { return (uint32_t)(blocks + kExtra); }
+  __device__ uint32_t units() const { return flat ? 1u : (uint32_t)(blocks + kExtra); }
   __device__ uint64_t weight(const AttnArgs &a) const { return (uint64_t)((int64_t)tiles * a.hkv) * units(); }
 
   // One warp, all lanes.  An empty share gives no piece.
-  __device__ void start(const AttnArgs &a, int cta, int ctas, int least) {
+  __device__ void start(const AttnArgs &a, int cta, int ctas) {
     const int lane = threadIdx.x & 31;
-    uint64_t total = 0, w0 = 0;                            // w0: of this lane's sequence among the first 32
+    uint64_t total = 0;
+    int own = 0, longest = 0;                              // tiles, up to one more than CTAs; blocks of the longest
     begun.n_parts = 0;
+    flat = false;
     for (int s0 = 0; s0 < a.n_seqs; s0 += 32) {
       s = s0 + lane;
       uint64_t w = 0;
-      if (s < a.n_seqs) { measure(a); w = weight(a); }
-      if (s0 == 0) w0 = w;
+      if (s < a.n_seqs) {
+        measure(a);
+        w = weight(a);
+        own = (int)min((int64_t)ctas + 1, own + (int64_t)tiles * a.hkv);
+        longest = max(longest, tiles ? blocks : 0);
+      }
 #pragma unroll
       for (int o = 16; o; o >>= 1) w += __shfl_xor_sync(~0u, w, o);
       total += w;
     }
+    const uint32_t all = __reduce_add_sync(~0u, (unsigned)own);
+    flat = all <= (uint32_t)ctas && __reduce_max_sync(~0u, (unsigned)longest) <= kFlat;
+    if (flat) total = all;
     at = end = 0;
     if (total > (uint64_t)INT32_MAX) {                     // more than any memory holds, unless a sequence is named very often
       atomicCAS(a.status, 0, (int)PCOMOE_ERR_SHAPE);
       return;
     }
-    share = max(((uint32_t)total + ctas - 1) / ctas, (uint32_t)(least + kExtra));
+    share = flat ? 1 : max(((uint32_t)total + ctas - 1) / ctas, (uint32_t)(1 + kExtra));
     if ((uint64_t)cta * share >= total) return;
     at = cta * share;
     end = min(at + share, (uint32_t)total);
     uint32_t before = 0;
     for (int s0 = 0; s0 < a.n_seqs; s0 += 32) {
       s = s0 + lane;
-      uint32_t w = s0 == 0 ? (uint32_t)w0 : 0;
-      if (s0 && s < a.n_seqs) { measure(a); w = (uint32_t)weight(a); }
+      uint32_t w = 0;
+      if (s < a.n_seqs) {
+        if (a.n_seqs > 32) measure(a);                     // else it is what the lane has
+        w = (uint32_t)weight(a);
+      }
       uint32_t upto = w;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -219,6 +235,11 @@ struct CacheWalk {
         measure(a);
       }
       const uint32_t t = (at - seq_at) / units(), tile_at = seq_at + t * units();
+      if (flat) {
+        at = tile_at + 1;
+        p = {(int)t / tiles, (int)t % tiles, 0, blocks, true};
+        return true;
+      }
       const uint32_t upto = min(end, tile_at + units());
       p.b0 = max((int)(at - tile_at) - kExtra, 0);
       p.b1 = (int)(upto - tile_at) - kExtra;

@@ -46,9 +46,9 @@ __global__ void __launch_bounds__(kThreads, 2) few_kernel(AttnArgs a) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t ring = smem_u32(smem) + warp * kStages * stage_bytes<D>();
   pdl_grid_wait();
-  CacheWalk<BM, BN, kExtra> w;
-  CacheWalk<BM, BN, kExtra>::Piece p;
-  w.start(a, blockIdx.x, gridDim.x, 4);
+  CacheWalk<BM, BN, kExtra, 8> w;
+  CacheWalk<BM, BN, kExtra, 8>::Piece p;
+  w.start(a, blockIdx.x, gridDim.x);
   while (w.next(a, p)) {
     const Seq seq = w.seq;
     const int rows = min(BM, seq.n * a.g - p.tile * BM);

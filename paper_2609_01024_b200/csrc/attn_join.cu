@@ -105,17 +105,14 @@ pcomoe_status run(const AttnArgs &a, int ctas, cudaStream_t st) {
   return PCOMOE_OK;
 }
 
-template <typename T, int D>
-pcomoe_status by_rows(const AttnArgs &a, int rows, int ctas, cudaStream_t st) {
-  return rows == 16 ? run<T, D, 16>(a, ctas, st) : rows == 64 ? run<T, D, 64>(a, ctas, st) : run<T, D, 256>(a, ctas, st);
-}
-
 }  // namespace
 
-// rows: of a partial result's place (16, 64 or 256)
+// rows: of a partial result's place: 64 for fp32, 16 or 256 for bf16
 pcomoe_status launch_attn_join(const AttnArgs &a, int D, int dtype, int rows, int ctas, cudaStream_t st) {
-  if (dtype == PCOMOE_BF16) return D == 64 ? by_rows<__nv_bfloat16, 64>(a, rows, ctas, st) : by_rows<__nv_bfloat16, 128>(a, rows, ctas, st);
-  return D == 64 ? by_rows<float, 64>(a, rows, ctas, st) : by_rows<float, 128>(a, rows, ctas, st);
+  using bf16 = __nv_bfloat16;
+  if (dtype == PCOMOE_FP32) return D == 64 ? run<float, 64, 64>(a, ctas, st) : run<float, 128, 64>(a, ctas, st);
+  if (rows == 16) return D == 64 ? run<bf16, 64, 16>(a, ctas, st) : run<bf16, 128, 16>(a, ctas, st);
+  return D == 64 ? run<bf16, 64, 256>(a, ctas, st) : run<bf16, 128, 256>(a, ctas, st);
 }
 
 }  // namespace pcomoe

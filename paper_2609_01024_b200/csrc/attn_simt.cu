@@ -2,10 +2,14 @@
 //
 // One pass over the keys with the running maximum m and sum l of each row's softmax (in the base-2 domain):
 //   m' = max(m, max s),  o <- 2^(m-m') o + sum 2^(s-m') v,  l <- 2^(m-m') l + sum 2^(s-m').
-// A block of 256 threads owns BM rows and walks blocks of 64 keys through shared memory; a thread holds BM/16 rows x 4
-// columns of the scores and BM/16 rows x D/16 columns of the output, both in registers.  What bounds it: the FMA pipe for
-// prompts; for a few rows over a cache shared-memory reads and HBM, hence the narrow form (BM 16, a quarter of the score
-// work of BM 64) where a sequence has at most 16 rows on average.
+// A block of 256 threads owns a tile of 64 rows (prompts too small to fill the GPU with them: 16) and walks blocks of 64 keys
+// through shared memory; a thread holds up to 4 rows x 4 columns of the scores and 4 rows x D/16 columns of the output in
+// registers.  The weights lie over the keys, so that two blocks of threads fit on an SM at D = 128 and one computes
+// while the other's copies are on their way (31 sequences of about 300 tokens with 5 to 63 drafts, 8 heads on 4: 117 us; one
+// per SM 157).
+// What bounds it: the FMA pipe and the shared-memory reads that feed it, half and half (8 loads of 16 bytes to 64 FMA);
+// with few rows over a long cache the shared-memory reads alone (32 x 2048 tokens, 4 heads of 128, up to 16 rows each:
+// 187 us, 1.4 TB/s).  A causal prompt pair of 1024 with 8 heads on 2: 247 us, 8.7 TFLOP/s, the last tiles' chains of 16 blocks.
 #include <algorithm>
 
 #include "attn.cuh"
@@ -199,15 +203,15 @@ __device__ __forceinline__ void run_piece(const AttnArgs &a, const Seq &s, int k
     run_rows<D, BM, 4, kCached>(a, s, kvh, tile, b0, b1, whole, slot, sm);
 }
 
-template <int D, int BM>
+template <int D>
 __global__ void __launch_bounds__(kThreads, 2) simt_cached_kernel(AttnArgs a) {
   pdl_grid_wait();
   extern __shared__ float4 sm4[];
-  CacheWalk<BM, BN, 2> w;
-  typename CacheWalk<BM, BN, 2>::Piece p;
-  w.start(a, blockIdx.x, gridDim.x, 1);
+  CacheWalk<64, BN, 2, 1> w;
+  CacheWalk<64, BN, 2, 1>::Piece p;
+  w.start(a, blockIdx.x, gridDim.x);
   while (w.next(a, p))
-    run_piece<D, BM, true>(a, w.seq, p.kvh, p.tile, p.b0, p.b1, p.whole, part_slot(blockIdx.x, p.b0 == 0), (float *)sm4);
+    run_piece<D, 64, true>(a, w.seq, p.kvh, p.tile, p.b0, p.b1, p.whole, part_slot(blockIdx.x, p.b0 == 0), (float *)sm4);
   if (threadIdx.x == 0) w.record(a, blockIdx.x);
 }
 
@@ -253,18 +257,19 @@ pcomoe_status launch(F *kernel, PerDeviceOnce &once, dim3 grid, size_t smem, con
   return PCOMOE_OK;
 }
 
+template <int D>
+pcomoe_status run_cached(const AttnArgs &a, int sms, cudaStream_t st) {
+  static PerDeviceOnce once;
+  const pcomoe_status r = launch(simt_cached_kernel<D>, once, dim3(2 * sms), smem_floats<D, 64>() * sizeof(float), a, st);
+  return r == PCOMOE_OK ? launch_attn_join(a, D, PCOMOE_FP32, 64, 2 * sms, st) : r;
+}
+
 template <int D, int BM>
-pcomoe_status run(const AttnArgs &a, int sms, cudaStream_t st) {
-  const size_t smem = smem_floats<D, BM>() * sizeof(float);
-  if (a.table) {
-    static PerDeviceOnce once;
-    const pcomoe_status r = launch(simt_cached_kernel<D, BM>, once, dim3(2 * sms), smem, a, st);
-    return r == PCOMOE_OK ? launch_attn_join(a, D, PCOMOE_FP32, BM, 2 * sms, st) : r;
-  }
+pcomoe_status run_prompt(const AttnArgs &a, cudaStream_t st) {
   static PerDeviceOnce once;
   const int64_t tiles = (int64_t)a.T * a.g / BM + std::min(a.n_seqs, a.T);
   if (tiles > INT32_MAX) return PCOMOE_ERR_SHAPE;
-  return launch(simt_prompt_kernel<D, BM>, once, dim3((unsigned)tiles, a.hkv), smem, a, st);
+  return launch(simt_prompt_kernel<D, BM>, once, dim3((unsigned)tiles, a.hkv), smem_floats<D, BM>() * sizeof(float), a, st);
 }
 
 }  // namespace
@@ -272,11 +277,11 @@ pcomoe_status run(const AttnArgs &a, int sms, cudaStream_t st) {
 size_t attn_simt_part_rows(int sms) { return (size_t)4 * sms * 64; }
 
 pcomoe_status launch_attn_simt(const AttnArgs &a, int D, int sms, cudaStream_t st) {
-  // Narrow tiles: where a sequence has at most 16 rows on average, and for prompts also where wide ones would not give every
-  // SM a tile (their number is what counts then).
-  const bool narrow = (int64_t)a.T * a.g <= (int64_t)16 * a.n_seqs || (!a.table && ((int64_t)a.T * a.g / 64 + a.n_seqs) * a.hkv < sms);
-  if (D == 64) return narrow ? run<64, 16>(a, sms, st) : run<64, 64>(a, sms, st);
-  return narrow ? run<128, 16>(a, sms, st) : run<128, 64>(a, sms, st);
+  if (a.table) return D == 64 ? run_cached<64>(a, sms, st) : run_cached<128>(a, sms, st);
+  // Prompts: tiles of 16 rows where each of them gets an SM of its own (head size 128, 8 heads on 2: 4 prompts of 64 tokens
+  // 10.5 us, with 64 rows 12.3 us), else of 64 (4 prompts of 256: 52 us, with 16 rows 68 us).
+  if (((int64_t)a.T * a.g / 16 + std::min(a.n_seqs, a.T)) * a.hkv <= sms) return D == 64 ? run_prompt<64, 16>(a, st) : run_prompt<128, 16>(a, st);
+  return D == 64 ? run_prompt<64, 64>(a, st) : run_prompt<128, 64>(a, st);
 }
 
 }  // namespace pcomoe

@@ -41,8 +41,6 @@ constexpr int kSoftmaxRegs = 208, kOtherRegs = 88, kLaunchRegs = 168;
 static_assert(256 * kSoftmaxRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs, "register split");
 constexpr float kSlack = 8.f;                  // how far a maximum may run ahead of the one in use, in powers of two
 
-template <bool B> struct Bool { static constexpr bool value = B; };
-
 template <int D> struct Shape {
   static constexpr int kHalves = D / 64;                    // 64-column halves, one 128-byte swizzle row each
   static constexpr int kHalfBytes = 128 * 128;
@@ -168,10 +166,10 @@ struct Item {
 template <bool kCached> struct Walk;
 
 template <> struct Walk<true> {
-  CacheWalk<BM, BN, 2> w;
-  __device__ void start(const AttnArgs &a) { w.start(a, blockIdx.x, gridDim.x, 4); }
+  CacheWalk<BM, BN, 2, 4> w;
+  __device__ void start(const AttnArgs &a) { w.start(a, blockIdx.x, gridDim.x); }
   __device__ bool next(const AttnArgs &a, Item &it) {
-    CacheWalk<BM, BN, 2>::Piece p;
+    CacheWalk<BM, BN, 2, 4>::Piece p;
     if (!w.next(a, p)) return false;
     it.seq = w.seq; it.kvh = p.kvh; it.row0 = p.tile * BM; it.b0 = p.b0; it.b1 = p.b1;
     it.whole = p.whole; it.slot = part_slot(blockIdx.x, p.b0 == 0);
@@ -640,9 +638,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
           for (int qr = lane / C; qr < 128; qr += P) {
             const bool there = qr < rows;
             const __nv_bfloat16 *src = (const __nv_bfloat16 *)a.q + (there ? (int64_t)(it.seq.q0 + tok) * a.q_stride + (it.kvh * a.g + hd) * D + c * 8 : 0);
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + qr * 128 + (((c & 7) ^ (qr & 7)) << 4)), "l"(src),
-                         "r"(there ? 16 : 0)
-                         : "memory");
+            copy16(to + qr * 128 + (((c & 7) ^ (qr & 7)) << 4), src, there);
             for (hd += P; hd >= a.g; hd -= a.g) ++tok;
           }
           asm volatile("cp.async.wait_all;" ::: "memory");

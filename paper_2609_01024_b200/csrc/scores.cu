@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(32 * kWarps) scores_kernel(Args a) {
   struct Team {
     Sums sums[W];
     unsigned long long cand[kMaxCand];
-    int pick[kMaxTop], nc, count[2][W];
+    int pick[kMaxTop], nc, floor_key;
     struct { Sums sums; int key[kMaxTop], id[kMaxTop]; } out;      // what the cluster's first block collects
     float m, tail;                                       // reference, ln 2 (r - log2 s)
   };
@@ -339,37 +339,33 @@ __global__ void __launch_bounds__(32 * kWarps) scores_kernel(Args a) {
     int n_pick = 0;
     while (n_pick < want && s.pick[n_pick] >= 0) ++n_pick;
     int floor_key = n_pick ? s_group[s.pick[n_pick - 1]] : INT_MAX;
-    if (n_pick && n_pick < want && n_pick * 32 * N <= kMaxCand) {
-      floor_key = kNoKey + 1;                            // there is room for all their words
-    } else if (n_pick && n_pick < want) {
-      // fewer groups than ranks: the same bound from single lanes' words, by bisection of the key (the largest key that
-      // at least `want` lanes reach)
-      constexpr int kMine = (kMaxTop + W - 1) / W;
-      int most[kMine];
+    if (n_pick && n_pick < want) {
+      // fewer groups than ranks: the same bound from parts of the groups, 65 to 128 of them (or single lanes'), by counting
+      int per_group = 32;
+      while (n_pick * per_group > 128) per_group >>= 1;
+      int *part = (int *)s.cand;                         // not in use yet
+      static_assert(sizeof(s.cand) >= 128 * sizeof(int), "room for the parts");
+      for (int i = warp; i < n_pick; i += W) {
+        float x[N];
+        load_words<T>(row, shift, a.V, g0 + s.pick[i], lane, x);
+        int most = kNoKey;
 #pragma unroll
-      for (int q = 0; q < kMine; ++q) {
-        most[q] = kNoKey;
-        if (warp + q * W < n_pick) {
-          float x[N];
-          load_words<T>(row, shift, a.V, g0 + s.pick[warp + q * W], lane, x);
-#pragma unroll
-          for (int k = 0; k < N; ++k) most[q] = max(most[q], key_of(eligible(x[k])));
-        }
+        for (int k = 0; k < N; ++k) most = max(most, key_of(eligible(x[k])));
+        for (int o = 32 / per_group / 2; o; o >>= 1) most = max(most, __shfl_xor_sync(~0u, most, o));
+        const int lanes = 32 / per_group;
+        if (lane % lanes == 0) part[i * per_group + lane / lanes] = most;
       }
-      int64_t lo = kNoKey + 1, hi = (int64_t)s_group[s.pick[0]] + 1;      // reached by enough lanes (or the least); not reached
-      for (int turn = 0; hi - lo > 1; turn ^= 1) {
-        const int64_t mid = (lo + hi) >> 1;
-        int mine = 0;
-#pragma unroll
-        for (int q = 0; q < kMine; ++q) mine += most[q] >= mid;
-        int all = __reduce_add_sync(~0u, mine);
-        if (lane == 0) s.count[turn][warp] = all;
-        sync();
-        all = 0;
-        for (int q = 0; q < W; ++q) all += s.count[turn][q];
-        if (all >= want) lo = mid; else hi = mid;
+      if (tid == 0) s.floor_key = kNoKey + 1;            // where fewer parts than ranks have an eligible word: all words
+      sync();
+      for (int e = tid; e < n_pick * per_group; e += kThreads) {
+        const int key = part[e];
+        int r = 0;
+#pragma unroll 8
+        for (int j = 0; j < n_pick * per_group; ++j) r += part[j] > key || (part[j] == key && j < e);
+        if (r == want - 1 && key != kNoKey) s.floor_key = key;
       }
-      floor_key = (int)lo;
+      sync();
+      floor_key = s.floor_key;
     }
 #pragma unroll 4
     for (int i = warp; i < n_pick; i += W) {
@@ -525,15 +521,25 @@ pcomoe_status launch(Args a, int groups, cudaStream_t st) {
 template <typename T>
 pcomoe_status run(const Args &a, int sms, cudaStream_t st) {
   const int groups = (a.V + 15) / (32 * Vec<T>::N) + 1;
-  // Teams of 2 or 4 warps where there are rows enough to fill the GPU with them (24 warps per SM; 4096 rows of 32000 bf16
-  // words: 74 / 60 / 62 / 77 us with 1 / 2 / 4 / 8 warps, one warp per row leaving a ragged last wave), and no fewer than
-  // keep a team's group list inside 24 KB per block.
-  const auto fills = [&](int64_t warps) { return (int64_t)a.T * warps >= (int64_t)48 * sms; };
-  if (groups <= 1536 && fills(2)) return launch<T, 8, 2, 1>(a, groups, st);
-  if (groups <= 3072 && fills(4)) return launch<T, 8, 4, 1>(a, groups, st);
-  // then blocks of 8 warps, and with few rows clusters of blocks of 16 while a block keeps 16 groups
+  // Teams of 1, 2 or 4 warps where there are rows enough to fill the GPU with them (a team's group list stays inside 24 KB
+  // per block).  bf16, 5 best words:
+  //   rows of at most 16 groups, where what follows the pass over a row counts most: one warp (2400 rows of 2000 words:
+  //   11.9 us, two warps 15.2; of 8000 words 22.5 us, two warps 19.8);
+  //   48 warps per SM with teams of two: these (4000 rows of 32000 words: 55 us, one warp 63; 3000 rows, teams of four 47, of
+  //   two 49);
+  //   18 warps per SM with teams of four: these (1000 rows of 128000 words: 58 us, blocks of 8 warps 97; 600 rows of 32000
+  //   words: 19 us, blocks 17).
+  // Blocks of 8 warps, four teams to a block: blocks of 4 or 2 warps take 72 and 61 us instead of 57 for 4096 rows of 32000.
+  const auto fills = [&](int64_t warps, int64_t per_sm) { return (int64_t)a.T * warps >= per_sm * sms; };
+  if (groups <= 16 && a.top <= 8 && fills(1, 16)) return launch<T, 8, 1, 1>(a, groups, st);
+  if (groups <= 1536 && fills(2, 48)) return launch<T, 8, 2, 1>(a, groups, st);
+  if (groups <= 2 * 1536 && fills(4, 18)) return launch<T, 8, 4, 1>(a, groups, st);
+  // Fewer rows: a block of 8 warps each, or clusters of blocks of 16 while these find room and keep 16 groups each (a row of
+  // 32000 words: 5.6 us, one block 6.7; of 128000: 6.2, one block 22; but 8000 words, 32 groups, 5.3 and one block 4.3).
+  // Rows of 256 groups and more never go to one block (400 rows of 128000 words: 42 us, one block 57).
   int cl = 1;
-  while (cl < 16 && (int64_t)a.T * 2 * cl <= 2 * sms && groups / (2 * cl) >= 16) cl *= 2;
+  while (cl < 16 && (int64_t)a.T * 2 * cl <= 2 * sms && groups >= 64 && groups / (2 * cl) >= 16) cl *= 2;
+  if (cl == 1 && groups >= 256) cl = 2;
   switch (cl) {
     case 1: return launch<T, 8, 8, 1>(a, groups, st);
     case 2: return launch<T, 16, 16, 2>(a, groups, st);
