@@ -352,7 +352,8 @@ typedef struct {
 
 /* Bytes of device workspace of the two attention calls.  256-byte aligned; its first PCOMOE_ATTN_ZERO_BYTES must be zero
  * before its first use (status words and counters; the calls leave the counters at zero), the rest may hold anything,
- * and one call at a time may use it.  The size depends on the GPU, not on the batch.  Errors: INVALID_ARG, SHAPE, UNSUPPORTED (head_dim), CUDA. */
+ * and one call at a time may use it.  The size depends on the GPU, not on the batch.  Errors: INVALID_ARG, SHAPE
+ * (q_heads > 4096), UNSUPPORTED (head_dim), CUDA. */
 #define PCOMOE_ATTN_ZERO_BYTES 512u
 pcomoe_status pcomoe_attn_workspace_bytes(const pcomoe_attn_config *cfg, size_t *bytes);
 
@@ -368,9 +369,9 @@ pcomoe_status pcomoe_attn_workspace_bytes(const pcomoe_attn_config *cfg, size_t 
  * bf16: tensor cores, scores, maxima, sums and outputs accumulated in fp32, the weights a_p rounded to bf16 before they
  * meet v, the result rounded once.  fp32: plain FMA kernels.
  * Bits do not change from call to call.  Asynchronous on `stream`, allocates nothing.
- * Errors: INVALID_ARG (NULL, n_seqs <= 0 with T > 0, stride below a row, bad config), SHAPE (T < 0), UNSUPPORTED
- * (head_dim; base or stride not a multiple of 16 bytes), WORKSPACE, CUDA.  Device: INDEX (d_cu_len not ascending or past
- * T: the offending sequences are skipped), TIMEOUT.
+ * Errors: INVALID_ARG (NULL, n_seqs <= 0 with T > 0, stride below a row, bad config), SHAPE (T < 0, n_seqs > 65535,
+ * T * Hq / Hkv above 2^31 - 1), UNSUPPORTED (head_dim; base or stride not a multiple of 16 bytes), WORKSPACE, CUDA.
+ * Device: INDEX (d_cu_len not ascending or past T: the offending sequences are skipped), TIMEOUT.
  */
 pcomoe_status pcomoe_attn_prompt(const pcomoe_attn_config *cfg, int32_t T, int32_t n_seqs, const int32_t *d_cu_len,
                                  const void *d_q, int64_t q_stride, const void *d_k, int64_t k_stride, const void *d_v,
@@ -449,8 +450,10 @@ pcomoe_status pcomoe_cache_compact(const pcomoe_cache *cache, void *d_workspace,
  * (bits from n_i on are ignored).  d_tree_mask = NULL: the rows are a chain and row j sees m <= j; one row per sequence
  * is a decode step.  A row that sees nothing gets o = 0 and lse = -inf.
  * d_seqs may name a sequence more than once.  Formula, arrays, types, bits and errors as in pcomoe_attn_prompt; also
- * INVALID_ARG (cache and config disagree, layer out of range), SHAPE (mask_words < 0 or > 8).  Device: INDEX (sequence
- * or page out of range, more query rows than cached positions or than 32 * mask_words: o = 0, lse = -inf there).
+ * INVALID_ARG (cache and config disagree, layer out of range), SHAPE (mask_words < 0 or > 8), UNSUPPORTED (bf16: a
+ * layer's pool of 2^31 rows of a head or more).  Device: INDEX (sequence out of range, more query rows than cached
+ * positions or than 32 * mask_words: o = 0, lse = -inf there; a table entry that is no page: page 0 is read in its
+ * place and those results mean nothing), SHAPE (tiles times key blocks above 2^31: nothing is written).
  */
 pcomoe_status pcomoe_attn_cached(const pcomoe_attn_config *cfg, const pcomoe_cache *cache, int32_t layer, int32_t T,
                                  int32_t n_seqs, const int32_t *d_seqs, const int32_t *d_cu_len, const void *d_q,

@@ -121,9 +121,9 @@ pcomoe_status pcomoe_attn_cached(const pcomoe_attn_config *cfg, const pcomoe_cac
   // At most 32 rows (tokens x heads of a group) per sequence on average: the kernel whose tile has 16.  16 heads on 4, head
   // size 128; us with it and with the other, whose tile has 256 and whose pieces of work cost more to begin:
   //   rows per sequence              4           32          64
-  //   64 sequences of 512      17.8, 32.5  30.7, 34.4  49.7, 36.4
-  //   32 sequences of 4096     49.3, 55.9  62.3, 60.3   166, 63.0
-  //   4 sequences of 16384     33.6, 36.6  37.8, 39.5  60.5, 41.4
+  //   64 sequences of 512      18.1, 33.3  30.9, 34.8  49.9, 37.0
+  //   32 sequences of 4096     49.0, 55.9  62.1, 60.5   165, 62.6
+  //   4 sequences of 16384     33.4, 37.1  37.5, 39.8  58.4, 40.9
   if (cfg->dtype == PCOMOE_BF16 && (int64_t)T * a.g <= (int64_t)32 * n_seqs) return launch_attn_few(a, cfg->head_dim, sms, (cudaStream_t)stream);
   return cfg->dtype == PCOMOE_BF16 ? launch_attn_tc(a, cfg->head_dim, sms, (cudaStream_t)stream)
                                    : launch_attn_simt(a, cfg->head_dim, sms, (cudaStream_t)stream);

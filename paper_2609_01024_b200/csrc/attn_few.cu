@@ -1,4 +1,4 @@
-// Attention of a few rows over the paged cache, bf16: decode steps and small drafts (at most 16 rows per kv head and sequence).
+// Attention of a few rows over the paged cache, bf16: decode steps and small drafts (tiles of 16 rows per kv head and sequence).
 //
 // Mathematics as in the other attention kernels: one pass over the keys with a running maximum and sum per row, base 2.
 // What bounds it: reading the cache once (HBM).  With g heads on a kv head a byte of K or V takes part in g
@@ -7,6 +7,9 @@
 // with 16-byte asynchronous copies, and takes every fourth piece of the CTA's share; nothing in the loop waits for
 // another warp.  16 keys never cross a page (pages hold a multiple of 16), so a piece is one page lookup and one
 // contiguous run per K and V.  Two CTAs per SM: while one joins its warps' results the other one's loads go on.
+// Measured with the joining launch, 32 heads on 8 of 128: 32 sequences of 1 to 4095 tokens 46 us for 243 MB, 5.2 TB/s (ends and
+// beginnings of pieces and the second launch); two of 131071 and 100003 tokens 155 us for 946 MB, 6.1 TB/s, 0.93 of a
+// plain copy's rate; two sequences of 4 tokens 5.4 us.
 #include <algorithm>
 
 #include "attn.cuh"

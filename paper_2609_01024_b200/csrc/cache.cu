@@ -8,7 +8,9 @@
 // What bounds them: the bookkeeping is a chain of a few dependent loads (latency); the data movement is a copy, each
 // moved row read and written once (HBM).  So the bookkeeping of a call is one block where an order over the call's
 // sequences is needed (reserve, compact) and a block per sequence elsewhere, and the copies that follow are spread over
-// the whole GPU by a second launch that finds its list in the workspace.
+// the whole GPU by a second launch that finds its list in the workspace.  Measured (cold caches): reserving for 8
+// sequences 8 us; writing 10 MB of new rows 10 us; compaction that moves 97 MB of pages 30 us, 6.4 TB/s read and
+// written; accepting up to 9 drafts in each of 8 sequences 13 us.
 #include <algorithm>
 
 #include "common.cuh"
