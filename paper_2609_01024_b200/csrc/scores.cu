@@ -32,9 +32,9 @@ constexpr int kMaxVocab = 1 << 20;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kNone = -INFINITY;
 
-// Order of floats as integers (-inf lowest of what occurs here); kNoKey: nothing eligible.
+// Order of floats as integers (-inf lowest of what occurs here, -0 as 0); kNoKey: nothing eligible.
 __device__ __forceinline__ int key_of(float x) {
-  const int b = __float_as_int(x);
+  const int b = __float_as_int(x + 0.f);
   return b ^ ((b >> 31) & 0x7fffffff);
 }
 __device__ __forceinline__ float of_key(int k) { return __int_as_float(k ^ ((k >> 31) & 0x7fffffff)); }
