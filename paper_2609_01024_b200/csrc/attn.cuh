@@ -62,6 +62,10 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 
+// Weight of a partial sum l over the maximum m when the whole's is `to` (finite): 0 for a part in which the row saw nothing, and
+// NaN where l is (scores that are NaN raise no maximum).
+__device__ __forceinline__ float part_weight(float m, float l, float to) { return l == l ? ex2f(m - to) : l; }
+
 struct Seq {
   int q0, n;            // first packed row and their number
   int len, base;        // keys; those before `base` are seen by every row, the others by mask or order

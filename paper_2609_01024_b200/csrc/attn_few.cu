@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(kThreads, 2) few_kernel(AttnArgs a) {
 #pragma unroll
       for (int i = 0; i < kWarps; ++i) {
         const float2 ml = s_ml[i][r];
-        const float wt = ex2f(ml.x - ms);
+        const float wt = part_weight(ml.x, ml.y, ms);
         if (wt == 0.f) continue;                           // a warp in which the row saw nothing
         const float4 y = *(const float4 *)(so + (i * BM + r) * kPad + 4 * c);
         ll += wt * ml.y;

@@ -70,7 +70,7 @@ __global__ void __launch_bounds__(32 * kWarps) join_kernel(AttnArgs a) {
     for (int i0 = 0; i0 < n_parts; i0 += U) {
       if ((i0 & 7) == 0) {                                 // the weights of eight parts, one per lane
         const float2 ml = i0 == 0 ? ml0 : i0 + mine < n_parts ? stat(i0 + mine) : make_float2(-INFINITY, 0.f);
-        w = ex2f(ml.x - ms);
+        w = part_weight(ml.x, ml.y, ms);
         if (w != 0.f) l += w * ml.y;                       // 0: a part in which the row saw nothing
       }
       if (i0) fetch(i0);

@@ -457,7 +457,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         l += ((sum[0].x + sum[0].y) + (sum[1].x + sum[1].y)) + ((sum[2].x + sum[2].y) + (sum[3].x + sum[3].y));
       }
       pos += 2 * it.blocks();
-      if (m == -INFINITY) l = 0.f;
 
       // epilogue: a thread writes its row, or, where both tiles hold the same rows, half of the columns from both of them
       float w0 = 0.f, w1 = 0.f, inv = 1.f;                 // weights of the tiles' sums, where they hold the same rows
@@ -472,8 +471,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         const float2 x = s_ml[0][r], y = s_ml[1][r];
         m = fmaxf(x.x, y.x);
         const float ms = m == -INFINITY ? 0.f : m;
-        w0 = ex2f(x.x - ms);
-        w1 = ex2f(y.x - ms);
+        w0 = part_weight(x.x, x.y, ms);
+        w1 = part_weight(y.x, y.y, ms);
         l = w0 * x.y + w1 * y.y;
         c0 = t * (D / 2);
         c1 = c0 + D / 2;
@@ -522,7 +521,6 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
       };
       tc_fence_after();
       if (it.both) {
-        if (m == -INFINITY) inv = 0.f;
 #pragma unroll 1
         for (int c = 0; c < D; c += 32) {
           uint32_t o[32];
@@ -530,7 +528,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
           tmem_ld32_issue(o_col + c, o);
           tmem_wait_ld();
           reg_fence32(o);
-          if (m == -INFINITY)                              // a row that saw nothing: whatever the sums hold
+          if (l == 0.f)                                    // a row that saw nothing: whatever the sums hold
 #pragma unroll
             for (int k = 0; k < 32; ++k) o[k] = 0;
           write(o, c);

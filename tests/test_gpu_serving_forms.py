@@ -73,3 +73,34 @@ def test_cached_values_nobody_sees_fp32_rest_tiles(n):
     out, lse = at.cached(q.to(DEV), cache, 1, ints([0]), cu_of([n]), R.pack_bits([tree], 2).to(DEV))
     assert torch.isfinite(out[:n - 1]).all() and torch.isnan(out[n - 1, :, 5]).all()
     check_attention(out, lse, R.cached(q, keys, values, [n], [seen_of(70 + n, n, tree)], d ** -0.5), "f32")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prompt_nan_is_not_hidden(dtype):
+    """A NaN in a query, and in a first key, which is all that its own row sees, gives NaN there and nowhere else."""
+    hq, hkv, d, lens = 4, 2, 64, [150, 1, 20]
+    T = sum(lens)
+    q, k, v = (randn(i, T, h, d, dtype=TYPES[dtype][1], std=1.2) for i, h in enumerate((hq, hkv, hkv)))
+    q[7, 1, 3] = q[149, 2, 0] = q[165, 0, 9] = float("nan")
+    k[150, 0, 5] = float("nan")
+    at = make(dtype, hq, hkv, d, T, len(lens))
+    out, lse = at.prompt(q.to(DEV), k.to(DEV), v.to(DEV), cu_of(lens))
+    ref = R.prompt(q, k, v, lens, d ** -0.5)
+    assert torch.isnan(ref[0][7, 1]).all() and torch.isnan(ref[0][150, :2]).all() and torch.isfinite(ref[0][150, 2:]).all()
+    check_attention(out, lse, ref, dtype)
+
+
+@pytest.mark.parametrize("ctx,add", [([50, 0], [2, 1]), ([60, 9], [40, 17]), ([4000, 30], [2, 2]), ([4000, 30], [40, 40])], ids=str)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_cached_nan_is_not_hidden(dtype, ctx, add):
+    """The same over the cache, where a tile may be whole or cut into many parts."""
+    hq, hkv, d, page = 4, 1, 64, 64
+    full, T = [c + a for c, a in zip(ctx, add)], sum(add)
+    cache, keys, values = fill_cache(dtype, hkv, d, page, full, seed=5)
+    q = randn(3, T, hq, d, dtype=TYPES[dtype][1], std=1.2)
+    q[0, 1, 3] = q[T - 1, 0, 63] = float("nan")
+    at = make(dtype, hq, hkv, d, T, len(ctx))
+    out, lse = at.cached(q.to(DEV), cache, 1, ints(range(len(ctx))), cu_of(add))
+    ref = R.cached(q, keys, values, add, [seen_of(n, a, None) for n, a in zip(full, add)], d ** -0.5)
+    assert int(torch.isnan(ref[1]).sum()) == 2
+    check_attention(out, lse, ref, dtype)
