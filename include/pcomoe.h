@@ -365,8 +365,9 @@ pcomoe_status pcomoe_attn_workspace_bytes(const pcomoe_attn_config *cfg, size_t 
  *   d_q [T,Hq,D], d_k, d_v [T,Hkv,D], d_out [T,Hq,D] in cfg->dtype: a row's heads are contiguous, rows are *_stride
  *   ELEMENTS apart (column ranges of one fused projection output are fine)
  *   d_lse [T,Hq] fp32 or NULL.
- * A value that no row sees (another sequence's, a later row's) never reaches a result, NaN and infinities included; a
- * NaN score that a row sees makes its o and lse NaN.
+ * A value that a row does not see (another sequence's, a later row's) never reaches its result, NaN and infinities
+ * included; one that it sees does however small its weight is (0 in fp32 times NaN or an infinity is NaN), and a NaN score
+ * that a row sees makes its o and lse NaN.
  * bf16: tensor cores, scores, maxima, sums and outputs accumulated in fp32, the weights a_p rounded to bf16 before they
  * meet v, the result rounded once.  fp32: plain FMA kernels.
  * Bits do not change from call to call.  Asynchronous on `stream`, allocates nothing.

@@ -62,9 +62,12 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
 }
 
-// Weight of a partial sum l over the maximum m when the whole's is `to` (finite): 0 for a part in which the row saw nothing, and
-// NaN where l is (scores that are NaN raise no maximum).
-__device__ __forceinline__ float part_weight(float m, float l, float to) { return l == l ? ex2f(m - to) : l; }
+// Weight of a partial sum l over the maximum m when the whole's is `to` (finite): NaN where l is (scores that are NaN raise no
+// maximum), and kNoPart for a part in which the row saw nothing, whose sums may hold anything.  A part's largest weight is
+// 2^-8 or more, so l is 0 for no other; a part that the row saw counts even with a weight that is 0 in fp32, as a single
+// key does: 0 times a NaN is NaN, wherever the cut falls.
+constexpr float kNoPart = -1.f;
+__device__ __forceinline__ float part_weight(float m, float l, float to) { return l == 0.f ? kNoPart : l == l ? ex2f(m - to) : l; }
 
 struct Seq {
   int q0, n;            // first packed row and their number

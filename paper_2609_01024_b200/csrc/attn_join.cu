@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(32 * kWarps) join_kernel(AttnArgs a) {
       if ((i0 & 7) == 0) {                                 // the weights of eight parts, one per lane
         const float2 ml = i0 == 0 ? ml0 : i0 + mine < n_parts ? stat(i0 + mine) : make_float2(-INFINITY, 0.f);
         w = part_weight(ml.x, ml.y, ms);
-        if (w != 0.f) l += w * ml.y;                       // 0: a part in which the row saw nothing
+        if (w != kNoPart) l += w * ml.y;
       }
       if (i0) fetch(i0);
 #pragma unroll
@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(32 * kWarps) join_kernel(AttnArgs a) {
 #pragma unroll
         for (int j = 0; j < R; ++j) {
           const float wi = __shfl_sync(~0u, w, 8 * j + ((i0 + u) & 7));
-          if (wi != 0.f && i0 + u < n_parts)
+          if (wi != kNoPart && i0 + u < n_parts)
 #pragma unroll
             for (int k = 0; k < V; ++k) o[j][k] = fmaf(wi, x[u][j][k], o[j][k]);
         }

@@ -130,7 +130,7 @@ __device__ __forceinline__ void run_rows(const AttnArgs &a, const Seq &s, int kv
       for (int j = 0; j < 4; ++j) {
         const float p = ex2f(x[j] - ms);
         sum += p;
-        P[(ty * RM + i) * PP + tx + 16 * j] = p;
+        P[(ty * RM + i) * PP + tx + 16 * j] = ((j < 2 ? lo : hi) >> (tx + 16 * (j & 1))) & 1u ? p : -0.f;
       }
 #pragma unroll
       for (int q = 8; q; q >>= 1) sum += __shfl_xor_sync(~0u, sum, q);
@@ -154,7 +154,8 @@ __device__ __forceinline__ void run_rows(const AttnArgs &a, const Seq &s, int kv
           }
         }
     } else {
-      // a value that a row does not see (weight 0) does not touch it, NaN and infinities included
+      // a value that a row does not see (weight -0) does not touch it, NaN and infinities included; one that it sees does,
+      // with a weight that is 0 in fp32 too
       for (int n = 0; n < BN; ++n)
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
@@ -162,7 +163,7 @@ __device__ __forceinline__ void run_rows(const AttnArgs &a, const Seq &s, int kv
 #pragma unroll
           for (int i = 0; i < RM; ++i) {
             const float p = P[(ty * RM + i) * PP + n];
-            if (p != 0.f) {
+            if (__float_as_int(p) != (int)0x80000000) {
               o[i][c].x = fmaf(p, vv.x, o[i][c].x); o[i][c].y = fmaf(p, vv.y, o[i][c].y);
               o[i][c].z = fmaf(p, vv.z, o[i][c].z); o[i][c].w = fmaf(p, vv.w, o[i][c].w);
             }

@@ -473,7 +473,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         const float ms = m == -INFINITY ? 0.f : m;
         w0 = part_weight(x.x, x.y, ms);
         w1 = part_weight(y.x, y.y, ms);
-        l = w0 * x.y + w1 * y.y;
+        l = w0 * x.y + w1 * y.y;                           // kNoPart times 0 adds nothing
         c0 = t * (D / 2);
         c1 = c0 + D / 2;
         if (ok) ok = wait_bar(&s_ofull[0], n_o0 & 1, abort_flag, a.limit_ns);
@@ -546,8 +546,8 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
           // a tile in which the row saw nothing has no say, whatever its sums hold
 #pragma unroll
           for (int k = 0; k < 32; ++k) {
-            const float v = w0 != 0.f ? w0 * __uint_as_float(o[k]) : 0.f;
-            o[k] = __float_as_uint(w1 != 0.f ? fmaf(w1, __uint_as_float(y[k]), v) : v);
+            const float v = w0 != kNoPart ? w0 * __uint_as_float(o[k]) : 0.f;
+            o[k] = __float_as_uint(w1 != kNoPart ? fmaf(w1, __uint_as_float(y[k]), v) : v);
           }
           write(o, c);
         }
