@@ -415,8 +415,10 @@ pcomoe_status pcomoe_cache_reserve(const pcomoe_cache *cache, int32_t n, const i
 
 /* Rows into the cache: the last d_cu_len[i+1] - d_cu_len[i] positions of sequence d_seqs[i] receive the packed rows
  * [d_cu_len[i], d_cu_len[i+1]) of d_k and d_v [n_layers, T, kv_heads, head_dim] (rows `row_stride` and layers
- * `layer_stride` elements apart, for both), into the layers first_layer .. first_layer + n_layers - 1.
- * Device: INDEX (no such position, or its page is shared: that row is not written). */
+ * `layer_stride` elements apart, for both), into the layers first_layer .. first_layer + n_layers - 1.  0 <= d_cu_len[0],
+ * d_cu_len[n] <= T; rows outside of [d_cu_len[0], d_cu_len[n]) are not used.  T = 0: nothing is done.
+ * Device: INDEX (no such position, or its page is shared: that row is not written; a list that names rows outside of
+ * [0, T): the positions of those keep what they hold). */
 pcomoe_status pcomoe_cache_write(const pcomoe_cache *cache, int32_t first_layer, int32_t n_layers, int32_t T, int32_t n,
                                  const int32_t *d_seqs, const int32_t *d_cu_len, const void *d_k, const void *d_v,
                                  int64_t row_stride, int64_t layer_stride, void *d_workspace, size_t ws_bytes,

@@ -260,6 +260,8 @@ __global__ void __launch_bounds__(256) cache_write_kernel(CacheDev c, int first_
   pdl_grid_wait();
   __shared__ int s_page[kWriteRows], s_slot[kWriteRows];
   const int t0 = blockIdx.x * kWriteRows, layer = blockIdx.y;
+  // positions without a row: they keep what their page held
+  if (blockIdx.x == 0 && layer == 0 && threadIdx.x == kWriteRows && (cu[n] > T || cu[0] < 0)) flag(head, PCOMOE_ERR_INDEX);
   if (threadIdx.x < kWriteRows) {
     const int t = t0 + threadIdx.x;
     int page = -1, slot = 0;
