@@ -338,6 +338,7 @@ pcomoe_status pcomoe_residual_cast(const pcomoe_layer *layer, int32_t T, const v
  * What stands around the layer when a model is served: attention over packed prompts, a paged cache of keys and values
  * with its page operations, attention of new or drafted tokens over that cache, and scores of tokens from logits.
  * (The paper evaluates whole models and writes out none of these.)  Types are the layer's: bf16 or fp32.
+ * The calls launch on the current device, which has to be the one that their arrays and stream belong to.
  * --------------------------------------------------------------------------------------------------------------- */
 
 /* Plain data; set struct_size = sizeof(pcomoe_attn_config).  Query head h reads kv head h / (q_heads / kv_heads). */

@@ -552,22 +552,48 @@ class PathMoEStack:
 _TORCH = {PCOMOE_BF16: torch.bfloat16, PCOMOE_FP32: torch.float32}
 
 
-def _ints(t, device, n):
-    """A device list of n int32 that a call reads: contiguous."""
-    assert t.dtype is torch.int32 and t.numel() == n and t.is_contiguous() and t.device == device, (t.dtype, t.shape, t.device, n)
+_I32 = torch.int32
+
+
+def _ints(t, gpu, n):
+    """A list of n int32 on GPU number `gpu` that a call reads: contiguous."""
+    assert t.dtype is _I32 and t.numel() == n and t.is_contiguous() and t.get_device() == gpu, (t.dtype, t.shape, t.device, n)
     return t.data_ptr()
-
-
-def _raw_stream(device) -> int:
-    """The current stream of `device` as an integer."""
-    return torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _device(device) -> torch.device:
     d = torch.device(device)
-    d = torch.device("cuda", torch.cuda.current_device()) if d.index is None else d
-    torch.cuda.set_device(d)
-    return d
+    return torch.device("cuda", torch.cuda.current_device()) if d.index is None else d
+
+
+_current_device = torch._C._cuda_getDevice                    # an object's constructor has brought CUDA up
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _call(gpu, call, *args):
+    """One call of the library on the current stream of GPU number `gpu`, which is the current device while it is made: the
+    library launches there, whatever device the pointers and the stream belong to (the default stream's handle is 0 on
+    every device)."""
+    if _current_device() == gpu:
+        status = call(*args, _raw_stream(gpu))
+    else:
+        with torch.cuda.device(gpu):
+            status = call(*args, _raw_stream(gpu))
+    if status:
+        raise PcomoeError(status, call.__name__)
+
+
+def _bytes(device, name, config) -> int:
+    """What a *_workspace_bytes call answers for `device`."""
+    size = ctypes.c_size_t(0)
+    with torch.cuda.device(device):
+        _check(getattr(load_library(), name)(config, ctypes.byref(size)), name)
+    return size.value
+
+
+def _status(device, workspace) -> int:
+    with torch.cuda.device(device):
+        return pcomoe_device_status(workspace)
 
 
 class PagedCache:
@@ -581,7 +607,7 @@ class PagedCache:
     def __init__(self, *, layers, pages, page_size, kv_heads, head_dim, max_seqs, max_pages, dtype=PCOMOE_BF16, k=None, v=None,
                  book=None, device="cuda:0"):
         self.device = _device(k.device if k is not None else device)
-        self._lib = load_library()
+        self.gpu, self._lib = self.device.index, load_library()
         shape = (layers, pages, kv_heads, page_size, head_dim)
         n = max_seqs + pages + max_seqs * max_pages
         self.k = torch.zeros(shape, dtype=_TORCH[dtype], device=self.device) if k is None else k
@@ -590,7 +616,7 @@ class PagedCache:
         self.book = torch.zeros(n, dtype=torch.int32, device=self.device) if fresh else book
         for t in (self.k, self.v):
             assert tuple(t.shape) == shape and t.dtype == _TORCH[dtype] and t.is_contiguous() and t.device == self.device
-        _ints(self.book, self.device, n)
+        _ints(self.book, self.gpu, n)
         self.seq_len = self.book[:max_seqs]
         self.page_ref = self.book[max_seqs:max_seqs + pages]
         self.page_table = self.book[max_seqs + pages:].view(max_seqs, max_pages)
@@ -601,17 +627,15 @@ class PagedCache:
                               self.k.data_ptr(), self.v.data_ptr(), self.seq_len.data_ptr(), self.page_ref.data_ptr(),
                               self.page_table.data_ptr())
         self._ref = ctypes.byref(self.c)
-        size = ctypes.c_size_t(0)
-        _check(load_library().pcomoe_cache_workspace_bytes(self._ref, ctypes.byref(size)), "pcomoe_cache_workspace_bytes")
-        self.workspace = torch.empty(size.value, dtype=torch.uint8, device=self.device)
+        size = _bytes(self.device, "pcomoe_cache_workspace_bytes", self._ref)
+        self.workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
         self.workspace[:256].zero_()          # the status words start from zero
-        self._ws = (self.workspace.data_ptr(), size.value)
+        self._ws = (self.workspace.data_ptr(), size)
 
     def reserve(self, seqs, add):
         """Room for add[i] more tokens in sequence seqs[i]."""
         n = seqs.numel()
-        _check(self._lib.pcomoe_cache_reserve(self._ref, n, _ints(seqs, self.device, n), _ints(add, self.device, n), *self._ws,
-                                              _raw_stream(self.device)), "pcomoe_cache_reserve")
+        _call(self.gpu, self._lib.pcomoe_cache_reserve, self._ref, n, _ints(seqs, self.gpu, n), _ints(add, self.gpu, n), *self._ws)
 
     def write(self, k, v, seqs, cu_len, layer: int = 0):
         """Packed rows k, v [T, kv_heads, head_dim] into the last positions of the sequences in one layer, or
@@ -621,36 +645,33 @@ class PagedCache:
         assert (many or k.dim() == 3) and k.shape == v.shape and k.stride() == v.stride() and k.dtype is v.dtype is _TORCH[self.dtype]
         assert k.shape[-2] == self.kv_heads and k.shape[-1] == self.head_dim and k.stride(-1) == 1 and \
             (self.kv_heads == 1 or k.stride(-2) == self.head_dim) and k.device == v.device == self.device
-        _check(self._lib.pcomoe_cache_write(self._ref, layer, k.shape[0] if many else 1, k.shape[-3], n, _ints(seqs, self.device, n),
-                                            _ints(cu_len, self.device, n + 1), k.data_ptr(), v.data_ptr(), _row_stride(k),
-                                            k.stride(0) if many else 0, *self._ws, _raw_stream(self.device)), "pcomoe_cache_write")
+        _call(self.gpu, self._lib.pcomoe_cache_write, self._ref, layer, k.shape[0] if many else 1, k.shape[-3], n, _ints(seqs, self.gpu, n),
+              _ints(cu_len, self.gpu, n + 1), k.data_ptr(), v.data_ptr(), _row_stride(k),
+              k.stride(0) if many else 0, *self._ws)
 
     def fork(self, parents, children):
         """Sequence children[i] becomes a copy of parents[i] that shares its pages."""
         n = parents.numel()
-        _check(self._lib.pcomoe_cache_fork(self._ref, n, _ints(parents, self.device, n), _ints(children, self.device, n), *self._ws,
-                                           _raw_stream(self.device)), "pcomoe_cache_fork")
+        _call(self.gpu, self._lib.pcomoe_cache_fork, self._ref, n, _ints(parents, self.gpu, n), _ints(children, self.gpu, n), *self._ws)
 
     def keep(self, seqs, cu_len, keep, n_keep):
         """Of the last cu_len[i+1] - cu_len[i] (drafted) positions of seqs[i] those numbered keep[i, :n_keep[i]] stay."""
         n = seqs.numel()
         assert keep.dim() == 2 and keep.shape[0] == n
-        _check(self._lib.pcomoe_cache_keep(self._ref, n, _ints(seqs, self.device, n), _ints(cu_len, self.device, n + 1),
-                                           _ints(keep, self.device, keep.numel()), keep.shape[1], _ints(n_keep, self.device, n), *self._ws,
-                                           _raw_stream(self.device)), "pcomoe_cache_keep")
+        _call(self.gpu, self._lib.pcomoe_cache_keep, self._ref, n, _ints(seqs, self.gpu, n), _ints(cu_len, self.gpu, n + 1),
+              _ints(keep, self.gpu, keep.numel()), keep.shape[1], _ints(n_keep, self.gpu, n), *self._ws)
 
     def trim(self, seqs, lens):
         """Shortens sequence seqs[i] to lens[i] tokens; 0 frees it."""
         n = seqs.numel()
-        _check(self._lib.pcomoe_cache_trim(self._ref, n, _ints(seqs, self.device, n), _ints(lens, self.device, n), *self._ws,
-                                           _raw_stream(self.device)), "pcomoe_cache_trim")
+        _call(self.gpu, self._lib.pcomoe_cache_trim, self._ref, n, _ints(seqs, self.gpu, n), _ints(lens, self.gpu, n), *self._ws)
 
     def compact(self):
         """Moves the pages in use to the lowest ids."""
-        _check(self._lib.pcomoe_cache_compact(self._ref, *self._ws, _raw_stream(self.device)), "pcomoe_cache_compact")
+        _call(self.gpu, self._lib.pcomoe_cache_compact, self._ref, *self._ws)
 
     def device_status(self) -> int:
-        return pcomoe_device_status(self.workspace)
+        return _status(self.device, self.workspace)
 
 
 def _row_stride(x):
@@ -664,22 +685,21 @@ class Attention:
 
     def __init__(self, *, q_heads, kv_heads, head_dim, max_tokens, max_seqs, dtype=PCOMOE_BF16, scale=None, device="cuda:0"):
         self.device = _device(device)
-        self._lib = load_library()
+        self.gpu, self._lib = self.device.index, load_library()
         self.q_heads, self.kv_heads, self.head_dim, self.dtype = q_heads, kv_heads, head_dim, dtype
         self._torch = _TORCH[dtype]
         self.max_tokens, self.max_seqs = max_tokens, max_seqs
         self.cfg = pcomoe_attn_config(ctypes.sizeof(pcomoe_attn_config), q_heads, kv_heads, head_dim, dtype,
                                       head_dim ** -0.5 if scale is None else scale)
         self._cfg = ctypes.byref(self.cfg)
-        size = ctypes.c_size_t(0)
-        _check(self._lib.pcomoe_attn_workspace_bytes(self._cfg, ctypes.byref(size)), "pcomoe_attn_workspace_bytes")
-        self.workspace = torch.empty(size.value, dtype=torch.uint8, device=self.device)
+        size = _bytes(self.device, "pcomoe_attn_workspace_bytes", self._cfg)
+        self.workspace = torch.empty(size, dtype=torch.uint8, device=self.device)
         self.workspace[:PCOMOE_ATTN_ZERO_BYTES].zero_()          # status words and counters start from zero
-        self._ws = (self.workspace.data_ptr(), size.value)
+        self._ws = (self.workspace.data_ptr(), size)
         T = max(max_tokens, 1)
         self.out = torch.empty(T, q_heads, head_dim, dtype=_TORCH[dtype], device=self.device)
         self.lse = torch.empty(T, q_heads, dtype=torch.float32, device=self.device)
-        self._own = (T, self.out, self.lse)                      # the outputs as the last batch's size cuts them
+        self._own = (None,)                                      # rows of the last batch, and the outputs as they cut them
 
     def _rows(self, x, T, heads):
         """Pointer and row stride of packed rows [T, heads, head_dim]."""
@@ -689,25 +709,28 @@ class Attention:
         return x.data_ptr(), row if T > 1 else heads * self.head_dim
 
     def _outputs(self, T, out, lse):
+        """out, lse and what a call takes of them: pointer and row stride of out, pointer of lse."""
         if out is None or lse is None:
             assert T <= self.max_tokens
             if self._own[0] != T:
-                self._own = (T, self.out[:T], self.lse[:T])
+                own_out, own_lse = self.out[:T], self.lse[:T]
+                self._own = (T, own_out, own_lse, (own_out.data_ptr(), self.q_heads * self.head_dim, own_lse.data_ptr()))
+            if out is None and lse is None:
+                return self._own[1:]
             out = self._own[1] if out is None else out
             lse = self._own[2] if lse is None else lse
-        assert lse.shape[0] == T and lse.shape[1] == self.q_heads and lse.is_contiguous() and lse.dtype is torch.float32
-        return out, lse
+        assert lse.shape[0] == T and lse.shape[1] == self.q_heads and lse.is_contiguous() and lse.dtype is torch.float32 and \
+            lse.device == self.device
+        return out, lse, (*self._rows(out, T, self.q_heads), lse.data_ptr())
 
     def prompt(self, q, k, v, cu_len, out=None, lse=None):
         """Causal attention over packed prompts: q [T, q_heads, D], k and v [T, kv_heads, D] (column ranges of a fused
         projection are fine), cu_len [n+1] int32 on the device.  Returns (out, lse)."""
         T, n = q.shape[0], cu_len.numel() - 1
         assert n <= self.max_seqs
-        out, lse = self._outputs(T, out, lse)
-        _check(self._lib.pcomoe_attn_prompt(self._cfg, T, n, _ints(cu_len, self.device, n + 1), *self._rows(q, T, self.q_heads),
-                                            *self._rows(k, T, self.kv_heads), *self._rows(v, T, self.kv_heads),
-                                            *self._rows(out, T, self.q_heads), lse.data_ptr(), *self._ws, _raw_stream(self.device)),
-               "pcomoe_attn_prompt")
+        out, lse, places = self._outputs(T, out, lse)
+        _call(self.gpu, self._lib.pcomoe_attn_prompt, self._cfg, T, n, _ints(cu_len, self.gpu, n + 1), *self._rows(q, T, self.q_heads),
+              *self._rows(k, T, self.kv_heads), *self._rows(v, T, self.kv_heads), *places, *self._ws)
         return out, lse
 
     def cached(self, q, cache: PagedCache, layer: int, seqs, cu_len, tree_mask=None, out=None, lse=None):
@@ -715,20 +738,19 @@ class Attention:
         rows' own.  tree_mask [T, words] int32 (bit m: the row sees the m-th of them) or None: a chain; one row per sequence
         is a decode step.  Returns (out, lse)."""
         T, n = q.shape[0], seqs.numel()
-        assert n <= self.max_seqs
+        assert n <= self.max_seqs and cache.device == self.device, (n, cache.device)
         mask, words = None, 0
         if tree_mask is not None:
             words = tree_mask.shape[1]
-            mask = _ints(tree_mask, self.device, T * words)
-        out, lse = self._outputs(T, out, lse)
-        _check(self._lib.pcomoe_attn_cached(self._cfg, cache._ref, layer, T, n, _ints(seqs, self.device, n),
-                                            _ints(cu_len, self.device, n + 1), *self._rows(q, T, self.q_heads), mask, words,
-                                            *self._rows(out, T, self.q_heads), lse.data_ptr(), *self._ws, _raw_stream(self.device)),
-               "pcomoe_attn_cached")
+            mask = _ints(tree_mask, self.gpu, T * words)
+        out, lse, places = self._outputs(T, out, lse)
+        _call(self.gpu, self._lib.pcomoe_attn_cached, self._cfg, cache._ref, layer, T, n, _ints(seqs, self.gpu, n),
+              _ints(cu_len, self.gpu, n + 1), *self._rows(q, T, self.q_heads), mask, words,
+              *places, *self._ws)
         return out, lse
 
     def device_status(self) -> int:
-        return pcomoe_device_status(self.workspace)
+        return _status(self.device, self.workspace)
 
 
 class TokenScores:
@@ -736,7 +758,7 @@ class TokenScores:
 
     def __init__(self, *, max_tokens, top_n=0, device="cuda:0"):
         self.device = _device(device)
-        self._lib = load_library()
+        self.gpu, self._lib = self.device.index, load_library()
         self.max_tokens, self.top_n = max_tokens, top_n
         T = max(max_tokens, 1)
         f32 = dict(dtype=torch.float32, device=self.device)
@@ -753,8 +775,8 @@ class TokenScores:
         assert T <= self.max_tokens and one == 1 and logits.device == self.device
         dtype = PCOMOE_BF16 if logits.dtype is torch.bfloat16 else PCOMOE_FP32
         assert logits.dtype is _TORCH[dtype], logits.dtype
-        _check(self._lib.pcomoe_token_logprobs(dtype, T, V, logits.data_ptr(), row if T > 1 else V, _ints(tokens, self.device, T),
-                                               self.top_n, *self._out, _raw_stream(self.device)), "pcomoe_token_logprobs")
+        _call(self.gpu, self._lib.pcomoe_token_logprobs, dtype, T, V, logits.data_ptr(), row if T > 1 else V, _ints(tokens, self.gpu, T),
+              self.top_n, *self._out)
         if self._own[0] != T:
             self._own = (T, (self.logprob[:T], self.entropy[:T], self.top_ids[:T], self.top_logprob[:T]))
         return self._own[1]
