@@ -291,58 +291,173 @@ __device__ __forceinline__ int64_t page_row(const AttnArgs &a, const int32_t *ta
   return ((int64_t)page * a.hkv + kvh) * a.page + (p & (a.page - 1));
 }
 
-// One bf16 row without the tensor cores, by a warp, each lane its columns of the head: positions [p0, p1) that the row
-// sees.  For rows that met a NaN or infinity they do not see (weight 0 times it); rare, so plain.
-template <int D, int BM, bool kCached>
-__device__ __forceinline__ void plain_row(const AttnArgs &a, const Seq &s, int kvh, int row0, int r, int p0, int p1, bool whole, int slot) {
-  constexpr int N = D / 32;
+// Place of position p's row of K or V, in elements; bf16 kernels.
+template <int D, bool kCached>
+__device__ __forceinline__ int64_t row_at(const AttnArgs &a, const Seq &s, int kvh, int p, int64_t stride) {
+  return kCached ? page_row(a, a.table + (int64_t)s.id * a.max_pages, kvh, p) * D : (int64_t)(s.q0 + p) * stride + kvh * D;
+}
+
+// Rows whose sums are not finite.  The products of a tile take every row through every value, with weight 0 where the row does not
+// see it, and 0 times a NaN or an infinity is NaN.  So such a row is right as it stands, unless one of the values that it does
+// not see is NaN or infinite: only then it is formed again (plain_rows).  Each lane asks for its own row, of token tok; p0 to
+// p1 are the positions that went into the sums, and every row of the warp sees those before `from`.  A warp.
+template <int D, bool kCached>
+__device__ __forceinline__ bool met_unseen(const AttnArgs &a, const Seq &s, int kvh, int tok, int p0, int p1, int from, bool asks) {
+  constexpr int C = D / 8, P = 32 / C;                   // lanes of a row, rows side by side
   const int lane = threadIdx.x & 31;
-  const int row = row0 + r, tok = row / a.g, head = kvh * a.g + row - tok * a.g;
-  const int64_t t = s.q0 + tok;
-  float q[N], o[N], m = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    q[i] = __bfloat162float(((const __nv_bfloat16 *)a.q)[t * a.q_stride + head * D + lane * N + i]);
-    o[i] = 0.f;
-  }
+  bool met = false;
   p1 = min(p1, s.len);
-  const int32_t *table = kCached ? a.table + (int64_t)s.id * a.max_pages : nullptr;
-  uint32_t bits = 0;
-  for (int p = p0; p < p1; ++p) {
-    if (p == p0 || (p & 31) == 0) bits = seen_bits<kCached>(a, s, tok, p & ~31);
-    if (!((bits >> (p & 31)) & 1)) continue;
-    const __nv_bfloat16 *k, *v;
-    if (kCached) {
-      const int64_t at = page_row(a, table, kvh, p) * D;
-      k = (const __nv_bfloat16 *)a.k + at;
-      v = (const __nv_bfloat16 *)a.v + at;
-    } else {
-      k = (const __nv_bfloat16 *)a.k + (s.q0 + p) * a.k_stride + kvh * D;
-      v = (const __nv_bfloat16 *)a.v + (s.q0 + p) * a.v_stride + kvh * D;
+  for (int g = max(p0, from) & ~31; g < p1; g += 32) {
+    uint32_t odd = 0;                                    // which of the 32 positions hold such a value
+#pragma unroll 4
+    for (int k = 0; k < 32; k += P) {
+      const int p = g + k + lane / C;
+      uint4 x = make_uint4(0, 0, 0, 0);
+      if (p < p1) x = *(const uint4 *)((const __nv_bfloat16 *)a.v + row_at<D, kCached>(a, s, kvh, p, a.v_stride) + (lane % C) * 8);
+      auto not_finite = [](uint32_t u) { return (u & 0x7f80u) == 0x7f80u || (u & 0x7f800000u) == 0x7f800000u; };
+      const uint32_t b = __ballot_sync(~0u, not_finite(x.x) || not_finite(x.y) || not_finite(x.z) || not_finite(x.w));
+#pragma unroll
+      for (int j = 0; j < P; ++j)
+        if ((b >> (j * C)) & ((1u << C) - 1u)) odd |= 1u << (k + j);
     }
-    float x = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) x = fmaf(q[i], __bfloat162float(k[lane * N + i]), x);
-#pragma unroll
-    for (int h = 16; h; h >>= 1) x += __shfl_xor_sync(~0u, x, h);
-    x *= a.scale_log2;
-    const float mn = fmaxf(m, x), ms = mn == -INFINITY ? 0.f : mn;
-    const float c = ex2f(m - ms), w = ex2f(x - ms);
-    l = l * c + w;
-    m = mn;
-#pragma unroll
-    for (int i = 0; i < N; ++i) o[i] = fmaf(w, __bfloat162float(v[lane * N + i]), o[i] * c);
+    if (odd && asks) met |= (odd & ~seen_bits<kCached>(a, s, tok, g)) != 0;
+    if (__all_sync(~0u, met || !asks)) break;
   }
-  if (whole) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
+  return met;
+}
+
+// bf16 rows without the tensor cores, by a warp: the rows r0 + i of bits i of `todo`, four at a time, over the positions [p0, p1)
+// that each of them sees, 32 at a time: a lane per key for the scores, and every lane its columns of the head for the sums.
+// Once all columns of a row are NaN nothing can change them, and the maximum and sum of the first pass, which come from the
+// scores alone, stay.  Rare, so plain: in a prompt of 16384 tokens (16 heads of 128, 0.94 ms) an infinity at row 12543, the last
+// of its tile, sends 255 rows of every head here and makes it 30 ms; one at row 0, which every row sees, sends none (1.13 ms).
+template <int D, int BM, bool kCached>
+__device__ __forceinline__ void plain_rows(const AttnArgs &a, const Seq &s, int kvh, int row0, int r0, uint32_t todo, int p0, int p1, bool whole, int slot) {
+  constexpr int N = D / 32, U = 8, R = 4;                 // columns of a lane; values under way; rows at a time
+  const int lane = threadIdx.x & 31;
+  p1 = min(p1, s.len);
+  while (todo) {
+    int r[R];                                             // the last one again where there are fewer
+    int n = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) ((__nv_bfloat16 *)a.out)[t * a.out_stride + head * D + lane * N + i] = __float2bfloat16_rn(o[i] * inv);
-    if (lane == 0 && a.lse) a.lse[t * a.hq + head] = l == 0.f ? -INFINITY : m * kLn2f + logf(l);
-  } else {
-    const int64_t at = (int64_t)slot * BM + r;
+    for (int i = 0; i < R; ++i) {
+      r[i] = todo ? r0 + __ffs(todo) - 1 : r[max(i - 1, 0)];
+      n += todo != 0;
+      todo &= todo - 1;
+    }
+    float o[R][N], m[R], l[R];
 #pragma unroll
-    for (int i = 0; i < N; ++i) a.part[at * D + lane * N + i] = o[i];
-    if (lane == 0) *((float2 *)a.part_ml + at) = make_float2(m, l);
+    for (int i = 0; i < R; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+#pragma unroll
+      for (int k = 0; k < N; ++k) o[i][k] = 0.f;
+    }
+    auto q_row = [&](int i) {
+      const int row = row0 + r[i], tok = row / a.g;
+      return (const uint4 *)((const __nv_bfloat16 *)a.q + (int64_t)(s.q0 + tok) * a.q_stride + (kvh * a.g + row - tok * a.g) * D);
+    };
+    uint32_t lost = 0;                                    // rows whose columns are all NaN
+    for (int g = p0; g < p1 && lost != (1u << R) - 1u; g += 32) {
+      uint32_t bits[R], any = 0;
+#pragma unroll
+      for (int i = 0; i < R; ++i) any |= bits[i] = seen_bits<kCached>(a, s, (row0 + r[i]) / a.g, g);       // none past the end of the sequence
+      const int p = g + lane;
+      float x[R];
+#pragma unroll
+      for (int i = 0; i < R; ++i) x[i] = 0.f;
+      int64_t v_at = 0;
+      if ((any >> lane) & 1) {
+        const uint4 *k = (const uint4 *)((const __nv_bfloat16 *)a.k + row_at<D, kCached>(a, s, kvh, p, a.k_stride));
+        v_at = row_at<D, kCached>(a, s, kvh, p, a.v_stride);
+#pragma unroll 1
+        for (int c0 = 0; c0 < D / 8; c0 += 4) {
+          uint4 y[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) y[c] = k[c0 + c];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const uint32_t u[4] = {y[c].x, y[c].y, y[c].z, y[c].w};
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+              const uint4 z = q_row(i)[c0 + c];
+              const uint32_t w[4] = {z.x, z.y, z.z, z.w};
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                x[i] = fmaf(__uint_as_float(u[e] << 16), __uint_as_float(w[e] << 16), x[i]);
+                x[i] = fmaf(__uint_as_float(u[e] & 0xffff0000u), __uint_as_float(w[e] & 0xffff0000u), x[i]);
+              }
+            }
+          }
+        }
+      }
+      __syncwarp();
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        x[i] = (bits[i] >> lane) & 1 ? x[i] * a.scale_log2 : -INFINITY;
+        float mn = x[i];
+#pragma unroll
+        for (int h = 16; h; h >>= 1) mn = fmaxf(mn, __shfl_xor_sync(~0u, mn, h));
+        mn = fmaxf(mn, m[i]);
+        const float ms = mn == -INFINITY ? 0.f : mn, c = ex2f(m[i] - ms);
+        x[i] = ex2f(x[i] - ms);                           // the weight
+        float sum = x[i];
+#pragma unroll
+        for (int h = 16; h; h >>= 1) sum += __shfl_xor_sync(~0u, sum, h);
+        l[i] = l[i] * c + sum;
+        m[i] = mn;
+#pragma unroll
+        for (int k = 0; k < N; ++k) o[i][k] *= c;
+      }
+#pragma unroll 1
+      for (int j0 = 0; j0 < 32; j0 += U) {
+        uint32_t v[U][N / 2];
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+          const int64_t at = __shfl_sync(~0u, v_at, j0 + j);
+#pragma unroll
+          for (int k = 0; k < N / 2; ++k)
+            v[j][k] = (any >> (j0 + j)) & 1 ? ((const uint32_t *)((const __nv_bfloat16 *)a.v + at + lane * N))[k] : 0u;
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j)
+#pragma unroll
+          for (int i = 0; i < R; ++i) {
+            const float w = __shfl_sync(~0u, x[i], j0 + j);
+            if ((bits[i] >> (j0 + j)) & 1)
+#pragma unroll
+              for (int k = 0; k < N / 2; ++k) {
+                o[i][2 * k] = fmaf(w, __uint_as_float(v[j][k] << 16), o[i][2 * k]);
+                o[i][2 * k + 1] = fmaf(w, __uint_as_float(v[j][k] & 0xffff0000u), o[i][2 * k + 1]);
+              }
+          }
+      }
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        bool all = true;
+#pragma unroll
+        for (int k = 0; k < N; ++k) all &= o[i][k] != o[i][k];
+        lost |= (uint32_t)__all_sync(~0u, all) << i;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      if (i >= n) continue;
+      const bool keep = (lost >> i) & 1;                  // what the first pass left of the maximum and sum
+      if (whole) {
+        const int row = row0 + r[i], tok = row / a.g, head = kvh * a.g + row - tok * a.g;
+        const int64_t t = s.q0 + tok;
+        const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
+#pragma unroll
+        for (int k = 0; k < N; ++k) ((__nv_bfloat16 *)a.out)[t * a.out_stride + head * D + lane * N + k] = __float2bfloat16_rn(o[i][k] * inv);
+        if (lane == 0 && a.lse && !keep) a.lse[t * a.hq + head] = l[i] == 0.f ? -INFINITY : m[i] * kLn2f + logf(l[i]);
+      } else {
+        const int64_t at = (int64_t)slot * BM + r[i];
+#pragma unroll
+        for (int k = 0; k < N; ++k) a.part[at * D + lane * N + k] = o[i][k];
+        if (lane == 0 && !keep) *((float2 *)a.part_ml + at) = make_float2(m[i], l[i]);
+      }
+    }
   }
 }
 

@@ -39,8 +39,17 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   return *(const uint32_t *)&v;
 }
 
+// Rows of a tile that may have to be formed again, every fourth to a warp.
 template <int D>
-__global__ void __launch_bounds__(kThreads, 2) few_kernel(AttnArgs a) {
+__device__ __noinline__ void form_again(const AttnArgs &a, Seq seq, int kvh, int tile, int b0, int b1, int rows, bool whole, int slot, const uint8_t *bad) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, mine = lane % BM;      // row of this lane
+  const bool met = met_unseen<D, true>(a, seq, kvh, (tile * BM + min(mine, rows - 1)) / a.g, b0 * BN, b1 * BN, seq.base, bad[mine]);
+  const uint32_t todo = __ballot_sync(~0u, met && lane < BM && lane % kWarps == warp);
+  plain_rows<D, BM, true>(a, seq, kvh, tile * BM, 0, todo, b0 * BN, b1 * BN, whole, slot);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 2) few_kernel(const __grid_constant__ AttnArgs a) {
   constexpr int kChunks = D / 8;                          // 16-byte pieces of a row
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ float2 s_ml[kWarps][BM];
@@ -218,8 +227,8 @@ __global__ void __launch_bounds__(kThreads, 2) few_kernel(AttnArgs a) {
         ll += wt * ml.y;
         x.x += wt * y.x; x.y += wt * y.y; x.z += wt * y.z; x.w += wt * y.w;
       }
-      if (!(fabsf(x.x) < INFINITY && fabsf(x.y) < INFINITY && fabsf(x.z) < INFINITY && fabsf(x.w) < INFINITY)) {
-        s_bad[r] = 1;
+      if (!(fabsf(x.x) < INFINITY && fabsf(x.y) < INFINITY && fabsf(x.z) < INFINITY && fabsf(x.w) < INFINITY) && ll == ll) {
+        s_bad[r] = 1;                                      // (with a NaN score the row is NaN whatever the values are)
         s_again = 1;
       }
       if (p.whole) {
@@ -236,8 +245,7 @@ __global__ void __launch_bounds__(kThreads, 2) few_kernel(AttnArgs a) {
     }
     __syncthreads();
     if (s_again) {
-      for (int r = warp; r < rows; r += kWarps)
-        if (s_bad[r]) plain_row<D, BM, true>(a, seq, p.kvh, p.tile * BM, r, p.b0 * BN, p.b1 * BN, p.whole, slot);
+      form_again<D>(a, seq, p.kvh, p.tile, p.b0, p.b1, rows, p.whole, slot, s_bad);
       __syncthreads();
     }
     __syncthreads();                                       // the rings are free again

@@ -29,8 +29,8 @@
 // a stale maximum while a vote is out 1.35.
 // The softmax threads clear the V rows past the end of a sequence before they hand over the weights of that block, which
 // keeps stale memory out of the sums; a NaN or infinity in a row of V that only some rows of a tile see meets
-// the others with weight 0 and would turn them into NaN: a row whose output is not finite is formed again without the
-// tensor cores, from what it sees alone.
+// the others with weight 0 and turns them into NaN: a row that met such a value is formed again without the tensor cores,
+// from what it sees alone.
 #include <algorithm>
 
 #include "attn.cuh"
@@ -69,17 +69,23 @@ __device__ __forceinline__ bool pause_bar(uint32_t bar, uint32_t parity) {
   asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
   return ok;
 }
-__device__ __forceinline__ bool wait_bar(uint64_t *bar_ptr, uint32_t parity, volatile int *abort_flag, uint64_t limit_ns) {
+// flags: [0] this CTA gives up, [1] warps that are forming rows again (plain_rows): what they hold up is late, not lost, and they
+// come to an end by themselves, so that time does not count.
+__device__ __forceinline__ bool wait_bar(uint64_t *bar_ptr, uint32_t parity, volatile int *flags, uint64_t limit_ns) {
   const uint32_t bar = smem_u32(bar_ptr);
   if (probe_bar(bar, parity)) return true;
   if (pause_bar(bar, parity)) return true;
-  const uint64_t t0 = global_ns();
+  uint64_t t0 = global_ns();
   for (uint32_t it = 1; it < (1u << 28); ++it) {
     if (pause_bar(bar, parity)) return true;
-    if (*abort_flag) return false;
+    if (flags[0]) return false;
+    if (flags[1]) {
+      t0 = global_ns();
+      it = 0;
+    }
     if (global_ns() - t0 > limit_ns) break;
   }
-  *abort_flag = 1;
+  flags[0] = 1;
   return false;
 }
 
@@ -279,6 +285,21 @@ __device__ __forceinline__ int tile_steps(const AttnArgs &a, const Item &it, int
   return min(n, key_blocks<false, BN>(a, it.seq, it.row0 + 128) - it.b0);
 }
 
+// Rows of a warp (my_row: this lane's) that may have to be formed again.  Not in line: the registers that it takes are those of
+// the softmax (in line, and with the counter outside, prompts took 2 % longer and trees over the cache 4 %).
+template <int D, bool kCached>
+__device__ __noinline__ void form_again(const AttnArgs &a, const Item &it, int my_row, uint8_t *bad_rows, int *flags) {
+  const int lane = threadIdx.x & 31;
+  if (lane == 0) atomicAdd(&flags[1], 1);
+  const bool bad = bad_rows[my_row];
+  if (bad) bad_rows[my_row] = 0;
+  const int tok = (it.row0 + min(my_row, it.rows - 1)) / a.g, first_tok = __shfl_sync(~0u, tok, 0);
+  const uint32_t todo = __ballot_sync(~0u, met_unseen<D, kCached>(a, it.seq, it.kvh, tok, it.b0 * BN, it.b1 * BN, kCached ? it.seq.base : first_tok + 1, bad));
+  plain_rows<D, BM, kCached>(a, it.seq, it.kvh, it.row0, my_row - lane, todo, it.b0 * BN, it.b1 * BN, it.whole, it.slot);
+  __syncwarp();
+  if (lane == 0) atomicSub(&flags[1], 1);
+}
+
 template <int D, bool kCached>
 __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_constant__ TcMaps maps, const __grid_constant__ AttnArgs a) {
   using S = Shape<D>;
@@ -291,14 +312,15 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
   __shared__ float2 s_ml[2][128];                         // maxima and sums of the two tiles, where they hold the same rows
   __shared__ uint8_t s_bad[BM];
   __shared__ uint32_t s_tmem;
-  __shared__ int s_abort;
+  __shared__ int s_flags[2];                              // see wait_bar
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const bool wide = (((uintptr_t)a.out | (uintptr_t)(a.out_stride * 2)) & 31) == 0;      // rows begin on whole sectors
   const uint32_t q_at = smem_u32(smem), ring = q_at + 2 * S::kTileBytes;
-  volatile int *abort_flag = &s_abort;
+  volatile int *flags = s_flags;
 
   if (tid == 0) {
-    s_abort = q_at & 1023 ? 1 : 0;                        // the swizzle needs it; nothing would be right otherwise
+    s_flags[0] = q_at & 1023 ? 1 : 0;                     // the swizzle needs it; nothing would be right otherwise
+    s_flags[1] = 0;
     for (int i = 0; i < S::kStages; ++i) { mbar_init(smem_u32(&s_full[i]), 1); mbar_init(smem_u32(&s_empty[i]), 1); }
     for (int t = 0; t < 2; ++t) {
       mbar_init(smem_u32(&s_sfull[t]), 1);
@@ -328,7 +350,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
   auto stage = [&](uint32_t p) { return p % S::kStages; };
   auto phase = [&](uint32_t p) { return (p / S::kStages) & 1; };
   uint32_t n_item = 0;                                    // pieces so far
-  auto item_ready = [&](bool ok) { return ok && wait_bar(&s_ifull[n_item & 1], (n_item >> 1) & 1, abort_flag, a.limit_ns); };
+  auto item_ready = [&](bool ok) { return ok && wait_bar(&s_ifull[n_item & 1], (n_item >> 1) & 1, flags, a.limit_ns); };
   auto item_done = [&]() {
     __syncwarp();
     if (lane == 0) mbar_arrive(smem_u32(&s_iempty[n_item & 1]));
@@ -355,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
     auto sync_both = [&]() {
       __syncwarp();
       if (lane == 0) mbar_arrive(smem_u32(&s_join));
-      if (ok) ok = wait_bar(&s_join, n_join & 1, abort_flag, a.limit_ns);
+      if (ok) ok = wait_bar(&s_join, n_join & 1, flags, a.limit_ns);
       ++n_join;
       __syncwarp();
     };
@@ -372,7 +394,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
       float m = -INFINITY, l = 0.f;
       for (int i = 0; i < steps; ++i, ++n_s) {
         const int b = b0 + (both ? i : 2 * i + t), p0 = b * BN;
-        if (ok) ok = wait_bar(&s_sfull[t], n_s & 1, abort_flag, a.limit_ns);
+        if (ok) ok = wait_bar(&s_sfull[t], n_s & 1, flags, a.limit_ns);
         __syncwarp();
         tc_fence_after();
         const bool masked = p0 + BN > (kCached ? base : first_tok + 1) || p0 + BN > len;
@@ -422,7 +444,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
           // the last V of the piece lies in its last ring stage; the scores of this block say that every earlier stage of
           // the ring's last round was filled, so the phase waited for is the one that is pending
           const uint32_t last = pos + 2 * it.blocks() - 1, st = stage(last);
-          if (ok) ok = wait_bar(&s_full[st], phase(last), abort_flag, a.limit_ns);
+          if (ok) ok = wait_bar(&s_full[st], phase(last), flags, a.limit_ns);
           const int first = max(len - p0, 0), rest = (BN - first) * 8;      // 16-byte pieces of a half
           for (int u = r; u < rest * S::kHalves; u += kTileThreads) {
             const int h = u / rest, x = u - h * rest;
@@ -462,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
       float w0 = 0.f, w1 = 0.f, inv = 1.f;                 // weights of the tiles' sums, where they hold the same rows
       int c0 = 0, c1 = D;
       if (it.both) {
-        if (ok) ok = t ? wait_bar(&s_ofull[1], n_o1 & 1, abort_flag, a.limit_ns) : wait_bar(&s_ofull[0], n_o0 & 1, abort_flag, a.limit_ns);
+        if (ok) ok = t ? wait_bar(&s_ofull[1], n_o1 & 1, flags, a.limit_ns) : wait_bar(&s_ofull[0], n_o0 & 1, flags, a.limit_ns);
         ++n_o0;
         ++n_o1;
       } else {
@@ -476,10 +498,10 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         l = w0 * x.y + w1 * y.y;                           // kNoPart times 0 adds nothing
         c0 = t * (D / 2);
         c1 = c0 + D / 2;
-        if (ok) ok = wait_bar(&s_ofull[0], n_o0 & 1, abort_flag, a.limit_ns);
+        if (ok) ok = wait_bar(&s_ofull[0], n_o0 & 1, flags, a.limit_ns);
         ++n_o0;
         if (it.blocks() > 1) {
-          if (ok) ok = wait_bar(&s_ofull[1], n_o1 & 1, abort_flag, a.limit_ns);
+          if (ok) ok = wait_bar(&s_ofull[1], n_o1 & 1, flags, a.limit_ns);
           ++n_o1;
         }
       }
@@ -557,17 +579,12 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         if (!it.whole) *((float2 *)a.part_ml + part_row) = make_float2(m, l);
         else if (a.lse) a.lse[tg * a.hq + head] = l == 0.f ? -INFINITY : m * kLn2f + logf(l);
       }
-      // rows to form again; also: every thread is done with the outputs and with s_ml
-      if (row_here && !finite) s_bad[my_row] = 1;
+      // rows that may have to be formed again (with a NaN score a row is NaN whatever the values are); also: every thread is
+      // done with the outputs and with s_ml
+      if (row_here && !finite && l == l) s_bad[my_row] = 1;
       if (!it.both) sync_both();
       if (it.both || t == 0) {
-        const bool again = s_bad[my_row];
-        if (again) s_bad[my_row] = 0;
-        __syncwarp();
-        for (uint32_t todo = __ballot_sync(~0u, again); todo; todo &= todo - 1) {
-          const int x = (it.both ? t * 128 : 0) + (warp & 3) * 32 + __ffs(todo) - 1;
-          plain_row<D, BM, kCached>(a, it.seq, it.kvh, it.row0, x, it.b0 * BN, it.b1 * BN, it.whole, it.slot);
-        }
+        if (__any_sync(~0u, s_bad[my_row])) form_again<D, kCached>(a, it, my_row, s_bad, s_flags);
       }
       item_done();
     }
@@ -586,7 +603,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
             const int j = kv ? i - lag : i;
             if (j < 0 || j >= n) continue;
             const uint32_t st = stage(pos);
-            ok = wait_bar(&s_empty[st], phase(pos) ^ 1, abort_flag, a.limit_ns);
+            ok = wait_bar(&s_empty[st], phase(pos) ^ 1, flags, a.limit_ns);
             ok = __all_sync(~0u, ok);
             if (!ok) break;
             const uint32_t bar = smem_u32(&s_full[st]), to = ring + st * S::kTileBytes;
@@ -618,7 +635,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
           if (q && !it.both) continue;
-          ok = ok && wait_bar(&s_qempty[q], (n_q[q] & 1) ^ 1, abort_flag, a.limit_ns);
+          ok = ok && wait_bar(&s_qempty[q], (n_q[q] & 1) ^ 1, flags, a.limit_ns);
           ok = __all_sync(~0u, ok);
           if (!ok) break;
           ++n_q[q];
@@ -657,7 +674,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
       auto advance = [&]() {
         if (++st == S::kStages) { st = 0; ph ^= 1; }
       };
-      auto wait = [&](uint64_t *bar, uint32_t p) { return ok = __all_sync(~0u, wait_bar(bar, p, abort_flag, a.limit_ns)); };
+      auto wait = [&](uint64_t *bar, uint32_t p) { return ok = __all_sync(~0u, wait_bar(bar, p, flags, a.limit_ns)); };
       const uint64_t q_desc = umma_desc(q_at), k_desc = umma_desc(ring), v_desc = mn_desc(ring, S::kHalfBytes);
       auto scores = [&](int t, int q, uint32_t at, bool last_q, bool last_k) {      // S_t = Q_q K^T
         const uint64_t da = q_desc + (uint64_t)(q * (S::kTileBytes >> 4)), db = k_desc + (uint64_t)(at * (S::kTileBytes >> 4));
@@ -749,7 +766,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
         Item it;
         more = walk.next(a, it);
         if (!more) it.rows = 0;
-        if (!__all_sync(~0u, wait_bar(&s_iempty[n_item & 1], ((n_item >> 1) & 1) ^ 1, abort_flag, a.limit_ns))) break;
+        if (!__all_sync(~0u, wait_bar(&s_iempty[n_item & 1], ((n_item >> 1) & 1) ^ 1, flags, a.limit_ns))) break;
         if (lane == 0) {
           s_item[n_item & 1] = it;
           mbar_arrive(smem_u32(&s_ifull[n_item & 1]));
@@ -762,7 +779,7 @@ __global__ void __launch_bounds__(kThreads, 1) attn_tc_kernel(const __grid_const
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (s_abort) timeout_record_and_drain(a.status);
+  if (s_flags[0]) timeout_record_and_drain(a.status);
   __syncthreads();
   if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }

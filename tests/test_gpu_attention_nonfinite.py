@@ -9,6 +9,7 @@ import pytest
 import torch
 
 import serving_reference as R
+from paper_2609_01024_b200 import binding as B
 from test_gpu_attention import DEV, TYPES, check, cu_of, fill_cache, ints, make, randn, seen_of
 
 pytestmark = pytest.mark.gpu
@@ -62,3 +63,104 @@ def test_cached_seen_nan_of_weight_zero(dtype, d, n, nan):
     ref = R.cached(q, keys, values, [n, n], [seen_of(5000 + n, n, None), seen_of(90 + n, n, None)], SCALE)
     assert torch.isnan(ref[0][:n, :, 3]).all() and torch.isfinite(ref[0][n:]).all()
     check(out, lse, ref, dtype)
+
+
+def check_values(out, lse, ref, dtype):
+    """`check`, and infinities are the reference's own."""
+    inf = torch.isinf(ref[0])
+    assert torch.equal(out.double().cpu()[inf], ref[0][inf])
+    check(out, lse, ref, dtype)
+
+
+def spoil(v, kind, T):
+    """Values of one kv head and column, or of all of them, made NaN or infinite; returns v."""
+    nan, inf = float("nan"), float("inf")
+    if kind == "first":
+        v[0, :, 3] = inf
+    elif kind == "middle":
+        v[T // 2, 0, 5], v[min(T // 2 + 1, T - 1), -1, 0] = nan, -inf
+    elif kind == "last":
+        v[T - 1] = nan
+    elif kind == "everywhere":                                        # a value in every block of keys, in other columns
+        for i, p in enumerate(range(5, T, 61)):
+            v[p, i % v.shape[1], (7 * i) % v.shape[2]] = nan if i % 3 else inf
+    elif kind == "all":
+        v[:] = nan
+    return v
+
+
+KINDS = ["first", "middle", "last", "everywhere", "all"]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("heads,lens", [((2, 2), [300, 64]), ((7, 1), [210]), ((32, 8), [1100, 90])], ids=str)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prompt_values(dtype, d, heads, lens, kind):
+    """Every row against the definition, in tiles of 128 and 256 rows; of 32 heads three."""
+    hq, hkv = heads
+    T, g = sum(lens), hq // hkv
+    q, k, v = (randn(i, T, h, d, dtype=TYPES[dtype][1]) for i, h in enumerate((hq, hkv, hkv)))
+    spoil(v, kind, lens[0])
+    a = make(dtype, hq, hkv, d, T, len(lens))
+    out, lse = a.prompt(q.to(DEV), k.to(DEV), v.to(DEV), cu_of(lens))
+    assert a.device_status() == 0
+    for h in sorted({0, hq // 2, hq - 1}):
+        one = lambda x, i: x[:, i:i + 1]
+        check_values(one(out, h), one(lse, h), R.prompt(one(q, h), one(k, h // g), one(v, h // g), lens, d ** -0.5), dtype)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n", [1, 7, 40, 90])
+@pytest.mark.parametrize("tree", [False, True], ids=["chain", "tree"])
+@pytest.mark.parametrize("dtype,d", [("bf16", 64), ("bf16", 128), ("f32", 128)])
+def test_cached_values(dtype, d, tree, n, kind):
+    """The same among drafted tokens and their contexts, whole and cut tiles."""
+    hq, hkv, page, full = 4, 2, 32, [700 + n, 0 + n]
+    cache, keys, values = fill_cache(dtype, hkv, d, page, full, seed=4)
+    for s, m in enumerate(full):
+        new = values[s][-n:]
+        spoil(values[s] if kind == "first" else new, kind, n)
+        for slot in range(-(-m // page)):
+            rows = values[s][slot * page:(slot + 1) * page]
+            cache.v[1, int(cache.page_table[s, slot]), :, :rows.shape[0]] = rows.transpose(0, 1).to(DEV)
+    q = randn(1, 2 * n, hq, d, dtype=TYPES[dtype][1])
+    trees = [R.tree_bits(np.random.default_rng(s), n) if tree else None for s in range(2)]
+    a = make(dtype, hq, hkv, d, 2 * n, 2)
+    out, lse = a.cached(q.to(DEV), cache, 1, ints([0, 1]), cu_of([n, n]), R.pack_bits(trees, 3).to(DEV) if tree else None)
+    assert a.device_status() == 0
+    check_values(out, lse, R.cached(q, keys, values, [n, n], [seen_of(m, n, t) for m, t in zip(full, trees)], d ** -0.5), dtype)
+
+
+@pytest.mark.parametrize("at", [0, 2900, 4095])
+def test_rows_formed_again_run_into_no_wait_limit(at):
+    """A prompt of 4096 tokens with an infinity in one value, under a wait limit of 1 ms (a tile takes some 20 us): forming rows again
+    is not a wait that ran out, and where every row sees the value (at 0) none is formed again."""
+    T, h, d = 4096, 16, 128
+    q, k, v = (randn(i, T, h, d, dtype=torch.bfloat16).to(DEV) for i in range(3))
+    clean, cu = v.clone(), cu_of([T])
+    v[at, :, 3] = float("inf")
+    a = make("bf16", h, h, d, T, 1)
+    want = a.prompt(q, k, clean, cu)[0].clone()
+
+    def time(values):
+        begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        begin.record()
+        a.prompt(q, k, values, cu)
+        end.record()
+        end.synchronize()
+        return begin.elapsed_time(end)
+    plain = min(time(clean) for _ in range(5))
+    try:
+        B.pcomoe_set_wait_limit_us(1000)
+        again = min(time(v) for _ in range(3))
+        assert a.device_status() == 0
+    finally:
+        B.pcomoe_set_wait_limit_us(0)
+    assert torch.isposinf(a.out[at:, :, 3]).all()
+    keep = [c for c in range(d) if c != 3]
+    assert torch.equal(a.out[:at], want[:at]) or float((a.out[:at].float() - want[:at].float()).abs().max()) <= 2 * 2.0 ** -8 * float(want.float().abs().max())
+    assert torch.isfinite(a.out[:at]).all() and torch.isfinite(a.out[:, :, keep]).all()
+    if at == 0:
+        assert torch.equal(a.out[:, :, keep], want[:, :, keep])
+        assert again < 20 * plain, (again, plain)
