@@ -492,31 +492,49 @@ __global__ void __launch_bounds__(32 * kWarps) scores_kernel(Args a) {
 }
 
 template <typename T, int kWarps, int W, int CL>
-pcomoe_status launch(Args a, int groups, cudaStream_t st) {
-  static PerDeviceOnce once;
-  int dev = -1;
-  PCOMOE_CUDA_TRY(cudaGetDevice(&dev));
-  if (CL > 8 && once.first_use(dev)) {
-    PCOMOE_CUDA_TRY(cudaFuncSetAttribute(scores_kernel<T, kWarps, W, CL>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
-    once.done(dev);
-  }
-  constexpr int kTeams = kWarps / W;
-  a.group_room = (groups + CL - 1) / CL;
+struct Launch {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((a.T + kTeams - 1) / kTeams * CL));
-  cfg.blockDim = dim3(32 * kWarps);
-  cfg.dynamicSmemBytes = sizeof(int) * (size_t)a.group_room * kTeams;
-  cfg.stream = st;
   cudaLaunchAttribute attr[2];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim = {CL, 1, 1};
-  cfg.attrs = attr;
-  cfg.numAttrs = CL > 1 ? 2 : 1;
-  PCOMOE_CUDA_TRY((cudaLaunchKernelEx(&cfg, scores_kernel<T, kWarps, W, CL>, a)));
+  Launch(int rows, int group_room, cudaStream_t st) {
+    constexpr int kTeams = kWarps / W;
+    cfg.gridDim = dim3((unsigned)((rows + kTeams - 1) / kTeams * CL));
+    cfg.blockDim = dim3(32 * kWarps);
+    cfg.dynamicSmemBytes = sizeof(int) * (size_t)group_room * kTeams;
+    cfg.stream = st;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim = {CL, 1, 1};
+    cfg.attrs = attr;
+    cfg.numAttrs = CL > 1 ? 2 : 1;
+  }
+};
+
+template <typename T, int kWarps, int W, int CL>
+pcomoe_status launch(Args a, int groups, cudaStream_t st) {
+  a.group_room = (groups + CL - 1) / CL;
+  const Launch<T, kWarps, W, CL> l(a.T, a.group_room, st);
+  PCOMOE_CUDA_TRY((cudaLaunchKernelEx(&l.cfg, scores_kernel<T, kWarps, W, CL>, a)));
   count_launch();
   return PCOMOE_OK;
+}
+
+// Whether clusters of 16 blocks find room on the current device, which 8 always do: asked once for each device.
+template <typename T>
+bool room_for_16() {
+  static std::atomic<uint64_t> asked{0}, room{0};
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
+  if (asked.load(std::memory_order_acquire) & bit) return (room.load(std::memory_order_relaxed) & bit) != 0;
+  const Launch<T, 16, 16, 16> l(1, kMaxVocab / (32 * Vec<T>::N) / 16 + 1, nullptr);
+  int clusters = 0;
+  const bool ok = cudaFuncSetAttribute(scores_kernel<T, 16, 16, 16>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                  cudaOccupancyMaxActiveClusters(&clusters, scores_kernel<T, 16, 16, 16>, &l.cfg) == cudaSuccess && clusters > 0;
+  if (!ok) cudaGetLastError();                             // the answer is no, not an error of a later call
+  if (ok) room.fetch_or(bit, std::memory_order_relaxed);
+  asked.fetch_or(bit, std::memory_order_release);
+  return ok;
 }
 
 template <typename T>
@@ -541,6 +559,7 @@ pcomoe_status run(const Args &a, int sms, cudaStream_t st) {
   int cl = 1;
   while (cl < 16 && (int64_t)a.T * 2 * cl <= 2 * sms && groups >= 64 && groups / (2 * cl) >= 16) cl *= 2;
   if (cl == 1 && groups >= 256) cl = 2;
+  if (cl == 16 && !room_for_16<T>()) cl = 8;
   switch (cl) {
     case 1: return launch<T, 8, 8, 1>(a, groups, st);
     case 2: return launch<T, 16, 16, 2>(a, groups, st);
