@@ -492,9 +492,9 @@ pcomoe_status pcomoe_device_status(const void *d_workspace, void *stream);
  * this level.)
  *   pcomoe_set_wait_limit_us   sets the limit for kernels launched afterwards, process-wide; 0 restores the
  *                              default of 2 s; more than 60 s is INVALID_ARG.
- *   pcomoe_selftest_wait_timeout  enqueues a one-warp kernel that waits, with the same routine and limit, on a
- *                              barrier nothing will complete (no copy or MMA is involved), and so ends through the
- *                              give-up path: afterwards pcomoe_device_status(d_workspace) returns TIMEOUT, and the
+ *   pcomoe_selftest_wait_timeout  enqueues a two-warp kernel that waits, with the same routines (the layer's and the
+ *                              attention calls') and limit, on barriers nothing will complete (no copy or MMA is
+ *                              involved), and so ends, once both have given up, through the give-up path: afterwards pcomoe_device_status(d_workspace) returns TIMEOUT, and the
  *                              next pcomoe_build_path_groups on that workspace clears the word again.  d_workspace
  *                              needs room for the status header only (256 bytes, 256-byte aligned).
  * Errors: INVALID_ARG, WORKSPACE, CUDA. */

@@ -62,24 +62,24 @@ __global__ void __launch_bounds__(256) cast_y_bf16_kernel(const float4 *acc, uin
     out_s[i] = __float2bfloat16_rn(acc_s[i]);
 }
 
-// Self-test of the bounded wait: one warp waits, with the same helper and limit as the GEMM kernels, on an
-// mbarrier that nothing will ever arrive on (no copy, MMA or other CTA is involved), and then takes the same
-// give-up path: the status word receives PCOMOE_ERR_TIMEOUT and the kernel returns.
-__global__ void __launch_bounds__(32) wait_probe_kernel(int32_t *status_word, uint64_t limit_ns) {
+// Self-test of the bounded waits: two warps wait, one with the routine and limit of the GEMM kernels and one with the attention
+// kernels', on mbarriers that nothing will ever arrive on (no copy, MMA or other CTA is involved).  Where both give up,
+// the kernel takes the same path as theirs: the status word receives PCOMOE_ERR_TIMEOUT and it returns.
+__global__ void __launch_bounds__(64) wait_probe_kernel(int32_t *status_word, uint64_t limit_ns) {
   pdl_grid_wait();
-  __shared__ __align__(8) uint64_t s_bar;
-  __shared__ int s_abort;
+  __shared__ __align__(8) uint64_t s_bar[2];
+  __shared__ int s_abort, s_flags[2];
   if (threadIdx.x == 0) {
-    s_abort = 0;
-    mbar_init(smem_u32(&s_bar), 1);
+    s_abort = s_flags[0] = s_flags[1] = 0;
+    mbar_init(smem_u32(&s_bar[0]), 1);
+    mbar_init(smem_u32(&s_bar[1]), 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  __syncwarp();
-  bool done = true;
-  if (threadIdx.x == 0) done = mbar_wait(smem_u32(&s_bar), 0, &s_abort, limit_ns);
-  __syncwarp();
-  if (s_abort) timeout_record_and_drain(status_word);
-  (void)done;
+  __syncthreads();
+  if (threadIdx.x == 0) mbar_wait(smem_u32(&s_bar[0]), 0, &s_abort, limit_ns);
+  if (threadIdx.x == 32) wait_bar(&s_bar[1], 0, s_flags, limit_ns);
+  __syncthreads();
+  if (s_abort && s_flags[0]) timeout_record_and_drain(status_word);
 }
 
 }  // namespace
@@ -96,7 +96,7 @@ pcomoe_status launch_cast_y(const pcomoe_layer *L, int32_t T, const float *y_acc
 }
 
 pcomoe_status launch_wait_probe(int32_t *status_word, cudaStream_t st) {
-  PCOMOE_CUDA_TRY(launch_pdl(wait_probe_kernel, dim3(1), dim3(32), 0, st, status_word, wait_limit_ns()));
+  PCOMOE_CUDA_TRY(launch_pdl(wait_probe_kernel, dim3(1), dim3(64), 0, st, status_word, wait_limit_ns()));
   count_launch();
   return PCOMOE_OK;
 }

@@ -71,6 +71,38 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
   return mbar_wait_slow(bar, parity, abort_flag, limit_ns);
 }
 
+// The attention kernels' bounded wait: mbar_wait in line (where it stands registers are scarce), and without the long
+// suspend hint, whose wake-up short waits would feel.
+__device__ __forceinline__ bool probe_bar(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok;
+}
+__device__ __forceinline__ bool pause_bar(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok;
+}
+// flags: [0] this CTA gives up, [1] warps that are forming rows again (plain_rows): what they hold up is late, not lost, and they
+// come to an end by themselves, so that time does not count.
+__device__ __forceinline__ bool wait_bar(uint64_t *bar_ptr, uint32_t parity, volatile int *flags, uint64_t limit_ns) {
+  const uint32_t bar = smem_u32(bar_ptr);
+  if (probe_bar(bar, parity)) return true;
+  if (pause_bar(bar, parity)) return true;
+  uint64_t t0 = global_ns();
+  for (uint32_t it = 1; it < (1u << 28); ++it) {
+    if (pause_bar(bar, parity)) return true;
+    if (flags[0]) return false;
+    if (flags[1]) {
+      t0 = global_ns();
+      it = 0;
+    }
+    if (global_ns() - t0 > limit_ns) break;
+  }
+  flags[0] = 1;
+  return false;
+}
+
 // What a CTA does once one of its waits has run out: record the timeout in the status word, then give the
 // copies and MMAs already issued time to finish before shared memory and TMEM are given back.  All threads
 // of the CTA call it.
