@@ -130,7 +130,7 @@ __device__ __forceinline__ void run_rows(const AttnArgs &a, const Seq &s, int kv
       for (int j = 0; j < 4; ++j) {
         const float p = ex2f(x[j] - ms);
         sum += p;
-        P[(ty * RM + i) * PP + tx + 16 * j] = ((j < 2 ? lo : hi) >> (tx + 16 * (j & 1))) & 1u ? p : -0.f;
+        P[(ty * RM + i) * PP + tx + 16 * j] = p;
       }
 #pragma unroll
       for (int q = 8; q; q >>= 1) sum += __shfl_xor_sync(~0u, sum, q);
@@ -154,21 +154,26 @@ __device__ __forceinline__ void run_rows(const AttnArgs &a, const Seq &s, int kv
           }
         }
     } else {
-      // a value that a row does not see (weight -0) does not touch it, NaN and infinities included; one that it sees does,
-      // with a weight that is 0 in fp32 too
-      for (int n = 0; n < BN; ++n)
+      // a value that a row does not see does not touch it, NaN and infinities included; one that it sees does, with a weight
+      // that is 0 in fp32 too
+#pragma unroll 1
+      for (int n = 0; n < BN; ++n) {
+        uint32_t sees = 0;
+#pragma unroll
+        for (int i = 0; i < RM; ++i) sees |= ((seen_bits<kCached>(a, s, tok[i], p0 + (n & 32)) >> (n & 31)) & 1u) << i;
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
           const float4 vv = *(const float4 *)(V + n * DP + 4 * tx + 64 * c);
 #pragma unroll
           for (int i = 0; i < RM; ++i) {
             const float p = P[(ty * RM + i) * PP + n];
-            if (__float_as_int(p) != (int)0x80000000) {
+            if ((sees >> i) & 1) {
               o[i][c].x = fmaf(p, vv.x, o[i][c].x); o[i][c].y = fmaf(p, vv.y, o[i][c].y);
               o[i][c].z = fmaf(p, vv.z, o[i][c].z); o[i][c].w = fmaf(p, vv.w, o[i][c].w);
             }
           }
         }
+      }
     }
   }
 #pragma unroll
