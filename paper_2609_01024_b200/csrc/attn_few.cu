@@ -221,8 +221,8 @@ __global__ void __launch_bounds__(kThreads, 2) few_kernel(const __grid_constant_
 #pragma unroll
       for (int i = 0; i < kWarps; ++i) {
         const float2 ml = s_ml[i][r];
+        if (ml.y == 0.f) continue;                         // a warp in which the row saw nothing (kNoPart)
         const float wt = part_weight(ml.x, ml.y, ms);
-        if (wt == kNoPart) continue;                       // a warp in which the row saw nothing
         const float4 y = *(const float4 *)(so + (i * BM + r) * kPad + 4 * c);
         ll += wt * ml.y;
         x.x += wt * y.x; x.y += wt * y.y; x.z += wt * y.z; x.w += wt * y.w;
