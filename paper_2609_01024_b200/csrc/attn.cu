@@ -120,10 +120,14 @@ pcomoe_status pcomoe_attn_cached(const pcomoe_attn_config *cfg, const pcomoe_cac
   for (a.page_shift = 0; (1 << a.page_shift) < cache->page_size;) ++a.page_shift;
   // At most 32 rows (tokens x heads of a group) per sequence on average: the kernel whose tile has 16.  16 heads on 4, head
   // size 128; us with it and with the other, whose tile has 256 and whose pieces of work cost more to begin:
-  //   rows per sequence              4           32          64
-  //   64 sequences of 512      18.1, 33.3  30.9, 34.8  49.9, 37.0
-  //   32 sequences of 4096     49.0, 55.9  62.1, 60.5   165, 62.6
-  //   4 sequences of 16384     33.4, 37.1  37.5, 39.8  58.4, 40.9
+  //   rows per sequence              4          16          32          64
+  //   64 sequences of 512      14.2, 28.8  16.6, 29.3  31.4, 30.6  50.2, 31.6
+  //   32 sequences of 4096     49.3, 54.7  52.2, 56.6  63.6, 58.7   168, 62.0
+  //   4 sequences of 16384     34.0, 35.4  35.6, 36.0  39.1, 37.7  68.7, 39.0
+  // 48 ragged batches of 17 to 32 rows on average (1 to 64 sequences, up to 16 to 16000 tokens, 1 to 8 kv heads): 0.69 of the
+  // other's time in the mean, 0.52 to 1.12.  What the average does not see is a batch that mixes: 255 decode rows (32 heads
+  // on 8, 100 to 2000 tokens) and a chunk of 1000 on 3000 tokens take 507 us here and 460 there, as two calls 197 and 94;
+  // 63 and a chunk of 440 182 and 130, as two calls 55 and 46.
   if (cfg->dtype == PCOMOE_BF16 && (int64_t)T * a.g <= (int64_t)32 * n_seqs) return launch_attn_few(a, cfg->head_dim, sms, (cudaStream_t)stream);
   return cfg->dtype == PCOMOE_BF16 ? launch_attn_tc(a, cfg->head_dim, sms, (cudaStream_t)stream)
                                    : launch_attn_simt(a, cfg->head_dim, sms, (cudaStream_t)stream);

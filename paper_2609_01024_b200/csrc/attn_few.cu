@@ -2,14 +2,15 @@
 //
 // Mathematics as in the other attention kernels: one pass over the keys with a running maximum and sum per row, base 2.
 // What bounds it: reading the cache once (HBM).  With g heads on a kv head a byte of K or V takes part in g
-// multiply-adds, so 16-row warp MMAs (m16n8k16) do the products with most of their time to spare, and the kernel is
-// built around loads in flight: every warp has its own ring of three pieces of 16 keys (K and V, 8 KB at D = 128), filled
-// with 16-byte asynchronous copies, and takes every fourth piece of the CTA's share; nothing in the loop waits for
-// another warp.  16 keys never cross a page (pages hold a multiple of 16), so a piece is one page lookup and one
+// multiply-adds, so 16-row warp MMAs (m16n8k16) do the products with most of their time to spare (the second one takes the
+// weights in bf16, the type of its other operand, an error of at most 2^-8 of each; their sum takes them unrounded), and the
+// kernel is built around loads in flight: every warp has its own ring of three pieces of 16 keys (K and V, 8 KB at D =
+// 128), filled with 16-byte asynchronous copies, and takes every fourth piece of the CTA's share; nothing in the loop waits
+// for another warp.  16 keys never cross a page (pages hold a multiple of 16), so a piece is one page lookup and one
 // contiguous run per K and V.  Two CTAs per SM: while one joins its warps' results the other one's loads go on.
 // Measured with the joining launch, 32 heads on 8 of 128: 32 sequences of 1 to 4095 tokens 46 us for 243 MB, 5.2 TB/s (ends and
 // beginnings of pieces and the second launch); two of 131071 and 100003 tokens 155 us for 946 MB, 6.1 TB/s, 0.93 of a
-// plain copy's rate; two sequences of 4 tokens 5.4 us.
+// plain copy's rate; two sequences of 4 tokens 5.7 us.
 #include <algorithm>
 
 #include "attn.cuh"

@@ -7,9 +7,11 @@
 // registers.  The weights lie over the keys, so that two blocks of threads fit on an SM at D = 128 and one computes
 // while the other's copies are on their way (31 sequences of about 300 tokens with 5 to 63 drafts, 8 heads on 4: 117 us; one
 // per SM 157).
-// What bounds it: the FMA pipe and the shared-memory reads that feed it, half and half (8 loads of 16 bytes to 64 FMA);
-// with few rows over a long cache the shared-memory reads alone (32 x 2048 tokens, 4 heads of 128, up to 16 rows each:
-// 187 us, 1.4 TB/s).  A causal prompt pair of 1024 with 8 heads on 2: 247 us, 8.7 TFLOP/s, the last tiles' chains of 16 blocks.
+// What bounds it: the shared-memory reads that feed the FMA pipe (with four rows to a thread 8 reads of 16 bytes to 64 FMA in the
+// first product, and in the second, where a weight is a read of its own, 5 to 16 at D = 64 and 6 to 32 at 128; with one
+// row 5 to 16 in the first), each block's wait for its own copies, and few tiles.  Two causal prompts of 1024 with 8 heads
+// on 2: of 64 141 us, 15.3 TFLOP/s, the FMA pipe 45 % busy, of 128 248 us, 17.3 TFLOP/s, the last tiles' chains of 16
+// blocks; 32 sequences of 2048 tokens with a token each, 16 heads on 4 of 128: 176 us, 1.5 TB/s.
 #include <algorithm>
 
 #include "attn.cuh"

@@ -7,7 +7,8 @@
 //
 // A CTA owns 256 rows (tokens x heads of one kv head's group) as two tiles of 128, one TMEM lane and one thread per row.
 // Scores S = Q K^T (128 x 128 fp32) of a tile sit in TMEM; its 128 threads read them, and write the weights back as bf16
-// over them, where the second product O += P V takes them as its A operand.  The two tiles take turns: while one's
+// over them, where the second product O += P V takes them as its A operand (its operands have one type: an error of at most
+// 2^-8 of each weight, as of the output's own rounding; the sums l take the weights unrounded).  The two tiles take turns: while one's
 // weights are formed, the tensor cores work for the other.  With at most 128 rows both tiles hold the same rows and
 // take alternate blocks of keys, so a few drafted tokens over a long cache still keep both busy; the halves are joined
 // at the end.
@@ -17,14 +18,16 @@
 // The CTAs are persistent and every role runs ahead of the next as far as its buffers allow: the next piece's queries,
 // keys and first scores come in while the last one's output is written.  Prompts: pieces are whole tiles, drawn from a
 // counter in order of falling length, so that the last ones to finish are short.  Cache: every CTA has an equal share.
-// Measured: one prompt of 16384 tokens, 16 heads of 128: 0.94 ms, 1.17 PFLOP/s, 0.72 of a library matrix product's rate;
-// prompts of 1531, 1523, 977, 64 and 1 tokens, 32 heads on 8: 67 us (a third of it the pieces' beginnings and ends); 17
-// to 48 drafts over 8 sequences of 905 to 4050 tokens, 32 heads on 8: 43 us with the joining launch, 85 MB.
+// Measured: one prompt of 16384 tokens, 16 heads of 128: 0.93 ms in runs of a few milliseconds, 1.18 PFLOP/s, and 1.07 ms in runs
+// of seconds, where the power limit lowers the clock, 1.03 PFLOP/s: 0.73 and 0.75 of a library matrix product's rate in
+// the same regime; prompts of 1531, 1523, 977, 64 and 1 tokens, 32 heads on 8: 67 us (a third of it the pieces'
+// beginnings and ends); 17 to 48 drafts over 8 sequences of 905 to 4050 tokens, 32 heads on 8: 42 us with the joining
+// launch, 85 MB.  (168 registers at launch; 36 bytes a thread spilled in the prompt forms, 72 in the cached ones.)
 //
 // What bounds it once the products are fed is the chain of a tile: scores done -> read, maximum, 128 exponentials per thread
 // -> weights written -> two products; the special function unit's rate (16 per clock and SM) makes the middle 1024 clocks
 // long at least, and the products 1024.  Tried and not kept, for one prompt of 16384 tokens with 16 heads (this form
-// 0.93 ms, 1.19 PFLOP/s): a polynomial on the FMA pipe for 1, 2 or 3 of 8 exponentials 0.92, 0.94, 0.97 ms (issue slots are
+// 0.93 ms): a polynomial on the FMA pipe for 1, 2 or 3 of 8 exponentials 0.92, 0.94, 0.97 ms (issue slots are
 // as scarce as exponentials); two threads per row 0.99; scores read twice so that loops stay short 0.97; weights formed with
 // a stale maximum while a vote is out 1.35.
 // The softmax threads clear the V rows past the end of a sequence before they hand over the weights of that block, which

@@ -10,7 +10,8 @@
 // sequences is needed (reserve, compact) and a block per sequence elsewhere, and the copies that follow are spread over
 // the whole GPU by a second launch that finds its list in the workspace.  Measured (cold caches): reserving for 8
 // sequences 8 us; writing 10 MB of new rows 10 us; compaction that moves 97 MB of pages 30 us, 6.4 TB/s read and
-// written; accepting up to 9 drafts in each of 8 sequences 13 us.
+// written; accepting up to 9 drafts in each of 8 sequences 13 us.  In a steady loop, call by call: reserve 5.7, write 4.4, keep
+// 8.3 (two launches), trim 1.6, fork 2.3, compaction of a compact pool 4.1 us.
 #include <algorithm>
 
 #include "common.cuh"

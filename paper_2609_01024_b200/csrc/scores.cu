@@ -17,7 +17,8 @@
 // special function unit does 16).  What comes after the pass over a row is a chain of short steps that few threads take
 // part in, so with many rows a row belongs to two or four warps and other rows' passes fill the gaps; with fewer rows to a
 // block or to a cluster of up to 16 blocks.  Measured, bf16: 4096 rows of 32000 words 57 us, 4.6 TB/s (the issue slots 70 %
-// busy, the special function unit 56 %, and teams that wait for the last rows); 4 rows of 128000 words 6.2 us.
+// busy, the special function unit 56 %, and teams that wait for the last rows); 4 rows of 128000 words 6.4 us; fp32: 1000
+// rows of 128000 words 84 us, 6.1 TB/s.
 #include <algorithm>
 #include <climits>
 #include <type_traits>
