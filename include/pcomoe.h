@@ -488,8 +488,9 @@ pcomoe_status pcomoe_device_status(const void *d_workspace, void *stream);
 /* Failure detection on the device.  Every wait of the tensor-core kernels (on an mbarrier that a TMA copy, an MMA
  * or the partner CTA completes) is bounded: when the limit runs out the CTA records PCOMOE_ERR_TIMEOUT in the
  * workspace's status word, lets its copies land, frees its tensor memory and returns, so the context stays usable
- * and pcomoe_device_status reports the failure.  (The paper has no counterpart; its engine is not described at
- * this level.)
+ * and pcomoe_device_status reports the failure.  Time in which a bf16 attention kernel forms rows again, because a NaN or
+ * infinity that they do not see lies in their tile, counts for no wait.  (The paper has no counterpart; its engine is
+ * not described at this level.)
  *   pcomoe_set_wait_limit_us   sets the limit for kernels launched afterwards, process-wide; 0 restores the
  *                              default of 2 s; more than 60 s is INVALID_ARG.
  *   pcomoe_selftest_wait_timeout  enqueues a two-warp kernel that waits, with the same routines (the layer's and the
