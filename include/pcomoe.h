@@ -1,6 +1,7 @@
 /*
  * pcomoe.h - C ABI of the path-composed MoE FFN layer for NVIDIA B200 (sm_100a), and of what serves a model around it:
- * attention over prompts and over a paged cache, the cache's page operations, token scores.
+ * head norms with rotation, attention over prompts and over a paged cache, the cache's page operations, weights of cached
+ * positions and eviction by them, token scores, verification of drafted tokens.
  *
  * The layer (PCoMoE, Sec. 4): every SwiGLU expert e is split into an expansion-side
  * operator U_e(h) = SiLU(W_gate h) (.) (W_up h) and a projection-side operator
@@ -479,9 +480,118 @@ pcomoe_status pcomoe_token_logprobs(int32_t dtype, int32_t T, int32_t V, const v
                                     const int32_t *d_tokens, int32_t top_n, float *d_logprob, float *d_entropy,
                                     int32_t *d_top_ids, float *d_top_logprob, void *stream);
 
+/*
+ * Norm and rotation of the heads of queries and keys, in one pass.  Set struct_size = sizeof(pcomoe_rotate_config).
+ * A head x of D elements with a weight w becomes  y = x w / sqrt(mean x^2 + eps)  (without a weight y = x; squares are summed
+ * in fp32, so elements beyond 1e18 overflow them), and pair i < rot_dim / 2 of y becomes
+ *     (a cos t - b sin t, a sin t + b cos t),   t = position * inv_freq[i],
+ * where the pair is (y[i], y[i + rot_dim / 2]) or (y[2 i], y[2 i + 1]); elements from rot_dim on are not rotated.
+ */
+typedef enum { PCOMOE_ROTATE_HALVES = 0, PCOMOE_ROTATE_NEIGHBOURS = 1 } pcomoe_rotate_pairs;
+typedef struct {
+  int32_t struct_size;
+  int32_t q_heads, kv_heads;
+  int32_t head_dim;     /* D: 64 or 128                                                       */
+  int32_t rot_dim;      /* 0 .. D, a multiple of 16; 0: norm only                             */
+  int32_t pairs;        /* pcomoe_rotate_pairs                                                */
+  int32_t dtype;        /* pcomoe_dtype of all rows and of the weights                        */
+  float eps;            /* finite, >= 0                                                       */
+} pcomoe_rotate_config;
+
+/* All T rows of d_q [T,Hq,D] and d_k [T,Hkv,D] into d_q_out and d_k_out (rows of contiguous heads, *_stride ELEMENTS apart;
+ * an output may be its input's own array, and must not overlap it otherwise).  d_position [T] int32, any value (a row's
+ * position in its text, which is not its place in a cache once rows were evicted); d_inv_freq [rot_dim / 2] fp64;
+ * d_q_weight, d_k_weight [D] in dtype or NULL (that part is not normed).  The angle is formed in 64 bits, everything else
+ * in fp32, the result is rounded once.  Bits do not depend on the batch.
+ * Errors: INVALID_ARG (NULL, bad config, stride below a row), SHAPE (T < 0 or too large), UNSUPPORTED (head_dim, rot_dim;
+ * base or stride not a multiple of 16 bytes), CUDA. */
+pcomoe_status pcomoe_heads_rotate(const pcomoe_rotate_config *cfg, int32_t T, const int32_t *d_position, const double *d_inv_freq, const void *d_q_weight,
+                                  const void *d_k_weight, const void *d_q, int64_t q_stride, const void *d_k, int64_t k_stride, void *d_q_out,
+                                  int64_t q_out_stride, void *d_k_out, int64_t k_out_stride, void *stream);
+
+/* The same for the rows [d_cu_len[0], d_cu_len[n]), of which the last d_cu_len[i+1] - d_cu_len[i] cached positions of sequence
+ * d_seqs[i] are the packed rows' own: the keys, normed and rotated, and the values d_v [T,Hkv,D] as they are go into these
+ * positions of one layer (reserve them first).  d_k_out may be NULL.  Rows outside of the list are neither read nor written.
+ * Also INVALID_ARG (cache and config disagree, layer out of range), WORKSPACE (256 bytes are enough: a status word; the
+ * cache's own will do).  Device: INDEX as in pcomoe_cache_write (that row's key and value are not cached). */
+pcomoe_status pcomoe_heads_rotate_cached(const pcomoe_rotate_config *cfg, const pcomoe_cache *cache, int32_t layer, int32_t T, int32_t n, const int32_t *d_seqs,
+                                         const int32_t *d_cu_len, const int32_t *d_position, const double *d_inv_freq, const void *d_q_weight,
+                                         const void *d_k_weight, const void *d_q, int64_t q_stride, const void *d_k, int64_t k_stride, const void *d_v,
+                                         int64_t v_stride, void *d_q_out, int64_t q_out_stride, void *d_k_out, int64_t k_out_stride, void *d_workspace,
+                                         size_t ws_bytes, void *stream);
+
+/*
+ * How much each cached position was attended to.  The last m_i cached positions of sequence d_seqs[i] are counted rows' own, and
+ * the k-th of them sees every position up to its own; with the log sums lse that the attention call left for it,
+ *     d_weight[d_seqs[i]][p] += sum over counted rows and query heads of exp(scale q.k_p - lse)     for every p < seq_len.
+ * Counted are all packed rows [d_cu_len[i], d_cu_len[i+1]), or, where d_keep is given, those numbered
+ * d_keep[i][0 .. d_n_keep[i]) of them: the lists of pcomoe_cache_keep, after that call.
+ *   fresh        not 0: the counted rows' own positions hold nothing yet and are set, not added to (the first layer of a step)
+ *   d_q [T,Hq,D] as in pcomoe_attn_cached, d_lse [T,Hq] fp32; d_keep [n, keep_stride] int32, d_n_keep [n], or both NULL
+ *   d_weight     [max_seqs] rows of fp32, weight_stride >= max_pages * page_size elements apart.  Only positions below seq_len
+ *                of the listed sequences are written.
+ * Weights belong to a sequence and its positions: a fork's are its parent's (copy the row), a shortened sequence's go with it.
+ * A key that a row does not see adds nothing, whatever it holds; a row with lse = -inf adds nothing; a NaN score that a row
+ * sees makes that position's weight NaN.  Scores are accumulated in fp32 and summed in fp32, in an order that the shapes fix:
+ * bits do not change from call to call.
+ * Errors: as pcomoe_attn_cached without a mask; INVALID_ARG also (one of d_keep and d_n_keep, weight_stride too small), SHAPE
+ * (n > max_seqs).  WORKSPACE: pcomoe_weigh_workspace_bytes, 256-byte aligned, its first 256 bytes zero before the first
+ * use.  Device: INDEX (a sequence out of range or repeated, more counted rows than cached positions, a list past T: the
+ * sequence is skipped; a number of d_keep out of range: that row counts nothing; a table entry that is no page: page 0 is
+ * read in its place).
+ */
+pcomoe_status pcomoe_weigh_workspace_bytes(const pcomoe_attn_config *cfg, const pcomoe_cache *cache, size_t *bytes);
+pcomoe_status pcomoe_cache_weigh(const pcomoe_attn_config *cfg, const pcomoe_cache *cache, int32_t layer, int32_t T, int32_t n, const int32_t *d_seqs,
+                                 const int32_t *d_cu_len, const void *d_q, int64_t q_stride, const float *d_lse, const int32_t *d_keep,
+                                 int32_t keep_stride, const int32_t *d_n_keep, int32_t fresh, float *d_weight, int64_t weight_stride,
+                                 void *d_workspace, size_t ws_bytes, void *stream);
+
+/* Shortens every listed sequence that is longer than d_budget[i] to it: its first `sinks` positions, its last `recent` ones and,
+ * of those between, the ones with the largest weight (ties: the lower position; a NaN is the smallest) stay, in order, in
+ * every layer; their weights move with them and the pages behind them are freed.  (Keys keep the rotation of their old
+ * positions: what is next in the text is for the caller to count.)
+ * The workspace (pcomoe_evict_workspace_bytes for n listed sequences, 256-byte aligned, first 256 bytes zero before the first
+ * use) holds the list of the places; one call at a time.
+ * Errors: those of a cache call; INVALID_ARG also (sinks or recent < 0, weight_stride below max_pages * page_size).
+ * Device: INDEX (a sequence out of range or repeated, a budget below 0 or, where it matters, below sinks + recent, a row to be
+ * written in a shared page, a table entry that is no page: that sequence stays as it is). */
+pcomoe_status pcomoe_evict_workspace_bytes(const pcomoe_cache *cache, int32_t n, size_t *bytes);
+pcomoe_status pcomoe_cache_evict(const pcomoe_cache *cache, int32_t n, const int32_t *d_seqs, const int32_t *d_budget, int32_t sinks, int32_t recent,
+                                 float *d_weight, int64_t weight_stride, void *d_workspace, size_t ws_bytes, void *stream);
+
+/*
+ * Verification of drafted tokens from given random numbers, and the token that follows.  Sequence i owns the packed rows
+ * [d_cu_len[i], d_cu_len[i+1]); its row 0 is a token that stands already, the others are drafts, row j behind the row d_parent[j]
+ * < j of its sequence (NULL: j - 1, a chain).  Row j's logits x are the target's for the token behind it.  With
+ * p = softmax(x / temperature) over the finite logits of a row (the rule for token scores: others have probability 0) and q the
+ * distribution that its drafts were drawn from, each on its own, the drafts behind a row are tested in order:
+ *     taken iff u[j] * q(token) * sum r < r(token);  refused: r <- max(r - q * sum r, 0), and r = p again if that is 0 everywhere
+ * from r = p on.  The walk goes on behind the first taken draft.  Where it ends, the next token is the first one whose sum of
+ * r over the ids up to it is above u_next * sum r.  (So for uniform numbers the tokens are distributed as the target's own.)
+ * One row per sequence is plain sampling.
+ *   d_tokens [T] int32, d_logits [T,V] in dtype, rows row_stride elements apart (any alignment)
+ *   d_draft_probs [T,V] fp32, rows draft_stride apart, or NULL.  Row j is the drafter's distribution behind row j, read only where
+ *                a draft hangs on it; what is negative, infinite or NaN counts as 0.  NULL: every draft was given, q is all on it.
+ *   d_temperature [n] fp32 or NULL (1); anything but a positive finite number: greedy, p is all on the lowest of the best ids
+ *   d_u [T] fp32 in [0, 1), a number per draft (row 0's is not used), d_u_next [n]
+ *   d_keep [n, keep_stride] int32, d_n_keep [n]: the walk's rows, row 0 first, ready for pcomoe_cache_keep; the rest of d_keep is -1;
+ *                a walk ends after keep_stride rows.
+ *   d_next [n] int32: -1 where no word is eligible.  A sequence without rows gets n_keep = 0 and next = -1.
+ * All that decides a token is formed in 64 bits.  Results are a function of the arguments.
+ * Workspace: pcomoe_verify_workspace_bytes(T), 256-byte aligned, first 256 bytes zero before the first use, one call at a time.
+ * Errors: INVALID_ARG, SHAPE (T < 0, V <= 0, n < 0 or > 65535, keep_stride < 0), UNSUPPORTED (V > 2^20), WORKSPACE, CUDA.
+ * Device: INDEX (d_cu_len not ascending or past T: that sequence counts as empty; a draft whose parent or token is out of range
+ * is passed over).
+ */
+pcomoe_status pcomoe_verify_workspace_bytes(int32_t max_tokens, size_t *bytes);
+pcomoe_status pcomoe_verify_drafts(int32_t dtype, int32_t T, int32_t V, int32_t n, const int32_t *d_cu_len, const int32_t *d_tokens, const int32_t *d_parent,
+                                   const void *d_logits, int64_t row_stride, const float *d_draft_probs, int64_t draft_stride, const float *d_temperature,
+                                   const float *d_u, const float *d_u_next, int32_t *d_keep, int32_t keep_stride, int32_t *d_n_keep, int32_t *d_next,
+                                   void *d_workspace, size_t ws_bytes, void *stream);
+
 /* Synchronises `stream`, reads the workspace's status words and returns the first error a kernel
  * recorded (PCOMOE_OK if none): the layer's word is cleared by the next pcomoe_build_path_groups, the
- * router's by this call once it has been read.  A workspace of the attention or cache calls has one word, kept like the
+ * router's by this call once it has been read.  A workspace of the calls around the layer has one word, kept like the
  * router's. */
 pcomoe_status pcomoe_device_status(const void *d_workspace, void *stream);
 

@@ -14,12 +14,13 @@ import torch
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libpcomoe.so")
 
-PCOMOE_OK = 0
+PCOMOE_OK, PCOMOE_ERR_UNSUPPORTED = 0, 4
 STATUS_NAMES = {0: "OK", 1: "ERR_INVALID_ARG", 2: "ERR_SHAPE", 3: "ERR_WORKSPACE", 4: "ERR_UNSUPPORTED",
                 5: "ERR_CUDA", 6: "ERR_TIMEOUT", 7: "ERR_INDEX",
                 8: "ERR_CACHE_FULL"}
 PCOMOE_BF16, PCOMOE_FP32 = 0, 1
 PCOMOE_ATTN_ZERO_BYTES = 512
+PCOMOE_ROTATE_HALVES, PCOMOE_ROTATE_NEIGHBOURS = 0, 1
 PCOMOE_FFN_AUTO, PCOMOE_FFN_SIMT, PCOMOE_FFN_TCGEN05, PCOMOE_FFN_TCGEN05_PAIR = 0, 1, 2, 3
 
 EXPORTS = ["pcomoe_mask_from_bias", "pcomoe_mask_tighten", "pcomoe_layer_create", "pcomoe_layer_destroy", "pcomoe_layer_active_set", "pcomoe_workspace_bytes",
@@ -29,7 +30,9 @@ EXPORTS = ["pcomoe_mask_from_bias", "pcomoe_mask_tighten", "pcomoe_layer_create"
            "pcomoe_host_pipe_destroy",
            "pcomoe_attn_workspace_bytes", "pcomoe_attn_prompt", "pcomoe_attn_cached", "pcomoe_cache_workspace_bytes",
            "pcomoe_cache_reserve", "pcomoe_cache_write", "pcomoe_cache_fork", "pcomoe_cache_keep", "pcomoe_cache_trim",
-           "pcomoe_cache_compact", "pcomoe_token_logprobs",
+           "pcomoe_cache_compact", "pcomoe_token_logprobs", "pcomoe_heads_rotate", "pcomoe_heads_rotate_cached",
+           "pcomoe_weigh_workspace_bytes", "pcomoe_cache_weigh", "pcomoe_evict_workspace_bytes", "pcomoe_cache_evict",
+           "pcomoe_verify_workspace_bytes", "pcomoe_verify_drafts",
            "pcomoe_device_status", "pcomoe_set_wait_limit_us", "pcomoe_selftest_wait_timeout",
            "pcomoe_launch_count", "pcomoe_status_string"]
 
@@ -56,6 +59,10 @@ class pcomoe_groups(ctypes.Structure):
 class pcomoe_attn_config(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_int32), ("q_heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class pcomoe_rotate_config(ctypes.Structure):
+    _fields_ = [(k, ctypes.c_int32) for k in ("struct_size", "q_heads", "kv_heads", "head_dim", "rot_dim", "pairs", "dtype")] + [("eps", ctypes.c_float)]
 
 
 class pcomoe_cache(ctypes.Structure):
@@ -112,6 +119,15 @@ def load_library(path: str | None = None):
     lib.pcomoe_cache_trim.argtypes = [pc, i32, vp, vp, vp, sz, vp]
     lib.pcomoe_cache_compact.argtypes = [pc, vp, sz, vp]
     lib.pcomoe_token_logprobs.argtypes = [i32, i32, i32, vp, i64, vp, i32, vp, vp, vp, vp, vp]
+    pr = ctypes.POINTER(pcomoe_rotate_config)
+    lib.pcomoe_heads_rotate.argtypes = [pr, i32, vp, vp, vp, vp] + [vp, i64] * 4 + [vp]
+    lib.pcomoe_heads_rotate_cached.argtypes = [pr, pc, i32, i32, i32, vp, vp, vp, vp, vp, vp] + [vp, i64] * 5 + [vp, sz, vp]
+    lib.pcomoe_weigh_workspace_bytes.argtypes = [pa, pc, ctypes.POINTER(sz)]
+    lib.pcomoe_cache_weigh.argtypes = [pa, pc, i32, i32, i32, vp, vp, vp, i64, vp, vp, i32, vp, i32, vp, i64, vp, sz, vp]
+    lib.pcomoe_evict_workspace_bytes.argtypes = [pc, i32, ctypes.POINTER(sz)]
+    lib.pcomoe_cache_evict.argtypes = [pc, i32, vp, vp, i32, i32, vp, i64, vp, sz, vp]
+    lib.pcomoe_verify_workspace_bytes.argtypes = [i32, ctypes.POINTER(sz)]
+    lib.pcomoe_verify_drafts.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, vp, i32, vp, vp, vp, sz, vp]
     lib.pcomoe_launch_count.restype = ctypes.c_int64
     lib.pcomoe_status_string.restype = ctypes.c_char_p
     lib.pcomoe_status_string.argtypes = [i32]
@@ -780,6 +796,158 @@ class TokenScores:
         if self._own[0] != T:
             self._own = (T, (self.logprob[:T], self.entropy[:T], self.top_ids[:T], self.top_logprob[:T]))
         return self._own[1]
+
+
+def _f32(t, gpu, n):
+    """A list of n fp32 on GPU number `gpu` that a call reads: contiguous."""
+    assert t.dtype is torch.float32 and t.numel() == n and t.is_contiguous() and t.get_device() == gpu, (t.dtype, t.shape, t.device, n)
+    return t.data_ptr()
+
+
+class HeadRotation:
+    """pcomoe_heads_rotate and pcomoe_heads_rotate_cached for one head layout: RMS norm of each head with q_weight and k_weight [head_dim] (None: not
+    normed), then the rotation of its first rot_dim elements by position * inv_freq (inv_freq: [rot_dim / 2], kept in fp64 on the device; None:
+    no rotation).  Pairs are the halves of the rotated part, or neighbours."""
+
+    def __init__(self, *, q_heads, kv_heads, head_dim, inv_freq=None, rot_dim=None, neighbours=False, q_weight=None, k_weight=None, eps=1e-6,
+                 dtype=PCOMOE_BF16, device="cuda:0"):
+        self.device = _device(device)
+        self.gpu, self._lib = self.device.index, load_library()
+        self.q_heads, self.kv_heads, self.head_dim, self.dtype, self._torch = q_heads, kv_heads, head_dim, dtype, _TORCH[dtype]
+        self.rot_dim = (0 if inv_freq is None else 2 * len(inv_freq)) if rot_dim is None else rot_dim
+        self.inv_freq = None
+        if self.rot_dim:
+            self.inv_freq = torch.as_tensor(inv_freq, dtype=torch.float64, device=self.device).contiguous()
+            assert self.inv_freq.shape == (self.rot_dim // 2,), (self.inv_freq.shape, self.rot_dim)
+        self.q_weight, self.k_weight = q_weight, k_weight
+        for w in (q_weight, k_weight):
+            assert w is None or (w.shape == (head_dim,) and w.dtype is self._torch and w.is_contiguous() and w.device == self.device), (w.shape, w.dtype, w.device)
+        self.cfg = pcomoe_rotate_config(ctypes.sizeof(pcomoe_rotate_config), q_heads, kv_heads, head_dim, self.rot_dim,
+                                        PCOMOE_ROTATE_NEIGHBOURS if neighbours else PCOMOE_ROTATE_HALVES, dtype, eps)
+        self._cfg = ctypes.byref(self.cfg)
+        self._fixed = tuple(None if x is None else x.data_ptr() for x in (self.inv_freq, q_weight, k_weight))
+
+    def _rows(self, x, T, heads):
+        """Pointer and row stride of packed rows [T, heads, head_dim]."""
+        shape, (row, head, one) = x.shape, x.stride()
+        assert shape[0] == T and shape[1] == heads and shape[2] == self.head_dim and x.dtype is self._torch and one == 1 and \
+            (head == self.head_dim or heads == 1) and x.device == self.device, (shape, x.stride(), x.dtype, x.device)
+        return x.data_ptr(), row if T > 1 else heads * self.head_dim
+
+    def rotate(self, q, k, position, q_out=None, k_out=None):
+        """q [T, q_heads, head_dim], k [T, kv_heads, head_dim] (column ranges of a fused projection are fine), position [T] int32.  Without outputs
+        the inputs are overwritten.  Returns (q_out, k_out)."""
+        T = q.shape[0]
+        q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
+        _call(self.gpu, self._lib.pcomoe_heads_rotate, self._cfg, T, _ints(position, self.gpu, T), *self._fixed, *self._rows(q, T, self.q_heads),
+              *self._rows(k, T, self.kv_heads), *self._rows(q_out, T, self.q_heads), *self._rows(k_out, T, self.kv_heads))
+        return q_out, k_out
+
+    def rotate_cached(self, q, k, v, position, cache: PagedCache, layer: int, seqs, cu_len, q_out=None, k_out=None):
+        """The same, and the keys with the values v [T, kv_heads, head_dim] go into one layer of the cache: the last cu_len[i+1] - cu_len[i] positions of
+        seqs[i] (reserved before) are the packed rows' own.  Without q_out q is overwritten; without k_out the keys go into the cache alone.
+        Returns q_out."""
+        T, n = q.shape[0], seqs.numel()
+        assert cache.device == self.device, cache.device
+        q_out = q if q_out is None else q_out
+        _call(self.gpu, self._lib.pcomoe_heads_rotate_cached, self._cfg, cache._ref, layer, T, n, _ints(seqs, self.gpu, n), _ints(cu_len, self.gpu, n + 1),
+              _ints(position, self.gpu, T), *self._fixed, *self._rows(q, T, self.q_heads), *self._rows(k, T, self.kv_heads),
+              *self._rows(v, T, self.kv_heads), *self._rows(q_out, T, self.q_heads), *((None, 0) if k_out is None else self._rows(k_out, T, self.kv_heads)), *cache._ws)
+        return q_out
+
+
+class CacheWeights:
+    """How much each cached position was attended to (pcomoe_cache_weigh) and eviction by it (pcomoe_cache_evict).  ``weight`` [max_seqs, max_pages *
+    page_size] fp32, by sequence and position; memory that the caller has already is used in place.  Up to `max_listed` sequences can be
+    evicted from in a call (all of them by default; the lists of places take 4 bytes per position and listed sequence)."""
+
+    def __init__(self, cache: PagedCache, *, q_heads, scale=None, weight=None, max_listed=None):
+        self.cache, self.device, self.gpu, self._lib = cache, cache.device, cache.gpu, cache._lib
+        c = cache.c
+        self.q_heads = q_heads
+        shape = (c.max_seqs, c.max_pages * c.page_size)
+        self.weight = torch.zeros(shape, dtype=torch.float32, device=self.device) if weight is None else weight
+        assert tuple(self.weight.shape) == shape and self.weight.dtype is torch.float32 and self.weight.device == self.device and self.weight.stride(1) == 1
+        self.cfg = pcomoe_attn_config(ctypes.sizeof(pcomoe_attn_config), q_heads, c.kv_heads, c.head_dim, c.dtype, c.head_dim ** -0.5 if scale is None else scale)
+        self._cfg = ctypes.byref(self.cfg)
+        self._place = (self.weight.data_ptr(), self.weight.stride(0) if shape[0] > 1 else shape[1])
+        self.max_listed = c.max_seqs if max_listed is None else max_listed
+        size = ctypes.c_size_t(0)
+        # (a head size that add() refuses can still be evicted from)
+        status = self._lib.pcomoe_weigh_workspace_bytes(self._cfg, cache._ref, ctypes.byref(size))
+        if status != PCOMOE_ERR_UNSUPPORTED:
+            _check(status, "pcomoe_weigh_workspace_bytes")
+        need = size.value
+        _check(self._lib.pcomoe_evict_workspace_bytes(cache._ref, self.max_listed, ctypes.byref(size)), "pcomoe_evict_workspace_bytes")
+        need = max(need, size.value)
+        self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+        self.workspace[:256].zero_()          # the status words start from zero
+        self._ws = (self.workspace.data_ptr(), need)
+
+    def add(self, q, lse, layer: int, seqs, cu_len, keep=None, n_keep=None, fresh: bool = False):
+        """After Attention.cached or prompt: q [T, q_heads, head_dim] and lse [T, q_heads] of the packed rows, whose keys are the last cached positions
+        of their sequences.  After PagedCache.keep pass its lists, and only the kept rows count.  fresh: this is the first layer of the step."""
+        T, n = q.shape[0], seqs.numel()
+        shape, (row, head, one) = q.shape, q.stride()
+        assert shape[1] == self.q_heads and shape[2] == self.cache.head_dim and q.dtype is _TORCH[self.cache.dtype] and one == 1 and \
+            (head == shape[2] or shape[1] == 1) and q.device == self.device, (shape, q.stride(), q.dtype, q.device)
+        lists = (None, 0, None)
+        if keep is not None:
+            assert keep.dim() == 2 and keep.shape[0] == n
+            lists = (_ints(keep, self.gpu, keep.numel()), keep.shape[1], _ints(n_keep, self.gpu, n))
+        _call(self.gpu, self._lib.pcomoe_cache_weigh, self._cfg, self.cache._ref, layer, T, n, _ints(seqs, self.gpu, n), _ints(cu_len, self.gpu, n + 1),
+              q.data_ptr(), row if T > 1 else self.q_heads * shape[2], _f32(lse, self.gpu, T * self.q_heads), *lists, int(fresh), *self._place, *self._ws)
+
+    def evict(self, seqs, budget, sinks: int = 0, recent: int = 0):
+        """Sequences longer than budget[i] (int32 on the device) keep their first `sinks`, their last `recent` and the heaviest other positions."""
+        n = seqs.numel()
+        assert n <= self.max_listed
+        _call(self.gpu, self._lib.pcomoe_cache_evict, self.cache._ref, n, _ints(seqs, self.gpu, n), _ints(budget, self.gpu, n), sinks, recent, *self._place, *self._ws)
+
+    def device_status(self) -> int:
+        return _status(self.device, self.workspace)
+
+
+class DraftVerifier:
+    """pcomoe_verify_drafts for up to `max_seqs` sequences, whose walks end after `max_path` rows, and up to `max_tokens` packed rows (max_seqs *
+    max_path by default).  Owns the workspace and the outputs."""
+
+    def __init__(self, *, max_seqs, max_path, max_tokens=None, device="cuda:0"):
+        self.device = _device(device)
+        self.gpu, self._lib = self.device.index, load_library()
+        self.max_seqs, self.max_path = max_seqs, max_path
+        self.max_tokens = max_seqs * max_path if max_tokens is None else max_tokens
+        i32 = dict(dtype=torch.int32, device=self.device)
+        n = max(max_seqs, 1)
+        self.keep, self.n_keep, self.next = torch.empty(n, max_path, **i32), torch.empty(n, **i32), torch.empty(n, **i32)
+        self._out = (self.keep.data_ptr(), max_path, self.n_keep.data_ptr(), self.next.data_ptr())
+        size = ctypes.c_size_t(0)
+        _check(self._lib.pcomoe_verify_workspace_bytes(self.max_tokens, ctypes.byref(size)), "pcomoe_verify_workspace_bytes")
+        self.workspace = torch.empty(size.value, dtype=torch.uint8, device=self.device)
+        self.workspace[:256].zero_()          # the status words start from zero
+        self._ws = (self.workspace.data_ptr(), size.value)
+
+    def verify(self, logits, tokens, cu_len, u, u_next, parent=None, draft_probs=None, temperature=None):
+        """logits [T, V] bf16 or fp32, tokens [T] int32 (row 0 of a sequence stands already), cu_len [n+1] int32, parent [T] int32 (None: chains),
+        draft_probs [T, V] fp32 (None: the drafts were given), temperature [n] (None: 1), u [T] and u_next [n] in [0, 1).  Returns (keep
+        [n, max_path], n_keep [n], next [n]): the first two are PagedCache.keep's lists."""
+        T, V = logits.shape
+        n = cu_len.numel() - 1
+        row, one = logits.stride()
+        assert n <= self.max_seqs and T <= self.max_tokens and one == 1 and logits.device == self.device
+        dtype = PCOMOE_BF16 if logits.dtype is torch.bfloat16 else PCOMOE_FP32
+        assert logits.dtype is _TORCH[dtype], logits.dtype
+        near = (None, 0)
+        if draft_probs is not None:
+            assert draft_probs.shape == (T, V) and draft_probs.dtype is torch.float32 and draft_probs.stride(1) == 1 and draft_probs.device == self.device
+            near = (draft_probs.data_ptr(), draft_probs.stride(0) if T > 1 else V)
+        _call(self.gpu, self._lib.pcomoe_verify_drafts, dtype, T, V, n, _ints(cu_len, self.gpu, n + 1), _ints(tokens, self.gpu, T),
+              None if parent is None else _ints(parent, self.gpu, T), logits.data_ptr(), row if T > 1 else V, *near,
+              None if temperature is None else _f32(temperature, self.gpu, n), _f32(u, self.gpu, T), _f32(u_next, self.gpu, n), *self._out, *self._ws)
+        return self.keep[:n], self.n_keep[:n], self.next[:n]
+
+    def device_status(self) -> int:
+        return _status(self.device, self.workspace)
 
 
 def to_device(arr: np.ndarray | None, device="cuda:0"):

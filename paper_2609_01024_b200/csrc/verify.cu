@@ -1,0 +1,715 @@
+// Verification of drafted tokens against the target's probabilities, from given random numbers, and the token that follows.
+//
+// Mathematics.  p = softmax(x / temperature) of a row's logits x, q the distribution that the drafts behind the row were drawn
+// from (the drafter's row; all of it on the draft where none is given).  At a row whose drafts are c1, c2, ... with tokens t1,
+// t2, ...: ci is taken iff u q(ti) R < r(ti), where r = p and R = 1 before the first, and a refusal leaves r <- max(r - R q, 0),
+// R <- sum r.  With A the sum of the R so far that is r = max(p - A q, 0) at once, since q >= 0; where q is all on the draft it
+// is p without the refused tokens.  The next token is the first one whose sum of r, in the order of ids, exceeds u_next times
+// all of it.  Whatever decides an integer (exponentials, sums, products with random numbers) is formed in 64 bits: in 32 a
+// sum over a vocabulary is off by 1e-7 of itself, and with 10^4 to 10^5 borders between words that changes a token in every few
+// thousand.
+//
+// Two launches.  The first forms the largest logit and the sum of the exponentials of every row that has a draft behind it,
+// rows side by side.  In the second a cluster of blocks per sequence first gathers what each draft's test needs, walks over
+// the drafts (they are numbered behind their parents, so one ascending pass meets every test in order), and reads the row
+// that the walk ended at once more: sums of its groups of 512 bytes, from which the group of the next token and in it the token
+// follow.  What bounds them: the rows' one read (HBM), the 64-bit pipe (64 lanes per clock and SM, about 12 of its operations
+// per word), and with few rows the chain of both launches.
+#include <algorithm>
+
+#include "words.cuh"
+
+namespace pcomoe {
+namespace {
+
+struct VerifyHeader {
+  int32_t reserved[8];
+  int32_t status;                         // the place of the router's word
+};
+static_assert(offsetof(VerifyHeader, status) == offsetof(DevPlan, status_router), "status word");
+
+struct RowSums {                          // of a row with drafts behind it
+  double s;                               // sum of 2^(c (x - m)), c = log2 e / temperature
+  float m;                                // largest logit; -inf: nothing eligible
+  int32_t best;                           // its lowest id (greedy rows only)
+};
+
+struct VerifyArgs {
+  int32_t T, V, n;
+  const int32_t *cu, *tokens, *parent;    // parent NULL: chains
+  const char *x;
+  int64_t row_bytes;
+  const float *near;                      // the drafter's probabilities or NULL
+  int64_t near_stride;
+  const float *temperature, *u, *u_next;
+  int32_t *keep, *n_keep, *next;
+  int32_t keep_stride;
+  VerifyHeader *head;
+  RowSums *sums;
+};
+
+constexpr int kTable = 64;
+constexpr int kMaxGroups = 1040;          // of a block: 2^20 fp32 words over 8 blocks, and one
+
+// 2^d for d <= 0 (or a little above), 64 bits: the nearest 64th apart, Taylor's series of the rest (at most 1/128, so the first
+// term left out is below 4e-17) and a table of 2^(k/64).  Below 2^-1000 it is 0.
+__device__ __forceinline__ double pow2(double d, const double *table) {
+  const double magic = 105553116266496.0;                  // 1.5 * 2^46: its last place is 1/64
+  const double t = fmax(d, -1100.0) + magic;
+  const int k = __double2loint(t);
+  const double y = (fmax(d, -1100.0) - (t - magic)) * 0.69314718055994530942;
+  double p = fma(y, 1.0 / 120, 1.0 / 24);
+  p = fma(p, y, 1.0 / 6);
+  p = fma(p, y, 0.5);
+  p = fma(p, y, 1.0);
+  p = fma(p, y, 1.0) * table[k & (kTable - 1)];
+  return d < -1000.0 ? 0.0 : __hiloint2double(__double2hiint(p) + ((k >> 6) << 20), __double2loint(p));
+}
+__device__ __forceinline__ void fill_table(double *table) {
+  for (int i = threadIdx.x; i < kTable; i += blockDim.x) table[i] = exp2(i * (1.0 / kTable));
+}
+
+__device__ __forceinline__ float real(float q) { return q > 0.f && q < INFINITY ? q : 0.f; }      // what is no probability counts as 0
+
+template <typename T> __device__ __forceinline__ const T *row_of(const VerifyArgs &a, int t) { return (const T *)(a.x + (int64_t)t * a.row_bytes); }
+template <typename T> __device__ __forceinline__ int shift_of(const T *row) { return (int)(((uintptr_t)row & 15) / sizeof(T)); }
+
+// log2 e / temperature, where the row is not greedy
+__device__ __forceinline__ double rate_of(const VerifyArgs &a, int s) {
+  const float t = a.temperature ? a.temperature[s] : 1.f;
+  return 1.4426950408889634074 / (double)t;
+}
+__device__ __forceinline__ bool greedy_of(const VerifyArgs &a, int s) { return a.temperature && !(a.temperature[s] > 0.f && a.temperature[s] < INFINITY); }
+
+// Rows of sequence s; empty and reported where the list is no list.
+__device__ __forceinline__ int2 rows_of(const VerifyArgs &a, int s) {
+  const int from = a.cu[s], to = a.cu[s + 1];
+  if (from < 0 || to < from || to > a.T) {
+    atomicCAS(&a.head->status, 0, (int)PCOMOE_ERR_INDEX);
+    return make_int2(0, 0);
+  }
+  return make_int2(from, to - from);
+}
+
+// A block's sum and largest place, joined over the cluster in the order of the blocks.  Places hold a key of a logit in the upper
+// half.  `slot` alternates so that one barrier is enough.
+struct Joined {
+  double s;
+  unsigned long long place;
+};
+template <int CL>
+struct Cluster {
+  Joined (*box)[2];                       // [CL] of this block
+  int slot;
+  __device__ int rank() const { return CL > 1 ? (int)(blockIdx.x % CL) : 0; }
+  __device__ static void barrier() {
+    if (CL > 1) asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+    else __syncthreads();
+  }
+  // every block's pair, in `all`; thread 0 gives this block's
+  __device__ void gather(Joined mine, Joined (&all)[CL]) {
+    slot ^= 1;
+    if (threadIdx.x == 0) box[0][slot] = mine;
+    barrier();
+#pragma unroll
+    for (int r = 0; r < CL; ++r) {
+      if (CL == 1) {
+        all[r] = box[0][slot];
+      } else {
+        const uint32_t at = (uint32_t)__cvta_generic_to_shared(&box[0][slot]);
+        uint32_t q;
+        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(q) : "r"(at), "r"(r));
+        asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(all[r].s) : "r"(q) : "memory");
+        asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(all[r].place) : "r"(q + 8) : "memory");
+      }
+    }
+    if (CL == 1) __syncthreads();         // the box may be written again
+  }
+};
+
+__device__ __forceinline__ double warp_sum(double x) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
+  return x;
+}
+__device__ __forceinline__ unsigned long long warp_max(unsigned long long x) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x = max(x, __shfl_xor_sync(~0u, x, o));
+  return x;
+}
+
+// The lowest id of a group whose word has the key; a warp.
+template <typename T>
+__device__ __forceinline__ int id_in_group(const T *row, int shift, int V, int g, int key) {
+  constexpr int N = Vec<T>::N;
+  const int lane = threadIdx.x & 31;
+  float x[N];
+  load_words<T>(row, shift, V, g, lane, x);
+  unsigned id = INT_MAX;
+#pragma unroll
+  for (int k = N - 1; k >= 0; --k)
+    if (key_of(eligible(x[k])) == key) id = (g * 32 + lane) * N - shift + k;
+  return (int)__reduce_min_sync(~0u, id);
+}
+
+// Sums of rows with drafts behind them.  kWarps warps, CL blocks per row.
+constexpr int kSumWarps = 8;
+template <typename T, int CL>
+__global__ void __launch_bounds__(32 * kSumWarps) row_sums_kernel(const __grid_constant__ VerifyArgs a) {
+  pdl_grid_wait();
+  constexpr int N = Vec<T>::N, kLoads = 4;
+  __shared__ double s_table[kTable], s_sum[kSumWarps];
+  __shared__ unsigned long long s_place[kSumWarps];
+  __shared__ Joined s_box[2];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int t = blockIdx.x / CL;
+  Cluster<CL> cl = {&s_box, 0};
+  // the row's sequence, and whether a draft hangs on it
+  int s = 0;
+  {
+    int hi = a.n;
+    while (hi - s > 1) {
+      const int step = (hi - s + 31) / 32, i = s + (lane + 1) * step;
+      const int k = __popc(__ballot_sync(~0u, i < hi && a.cu[min(i, hi)] <= t));
+      hi = min(s + (k + 1) * step, hi);
+      s += k * step;
+    }
+  }
+  const int2 rows = rows_of(a, s);
+  const int at = t - rows.x;
+  if (at < 0 || at >= rows.y) return;                      // (every block of the cluster, like the next one)
+  bool wanted = false;
+  if (!a.parent) wanted = at + 1 < rows.y;
+  else
+    for (int j = at + 1; j < rows.y && !wanted; j += 32) wanted = __any_sync(~0u, j + lane < rows.y && a.parent[rows.x + j + lane] == at);
+  if (!wanted) return;
+  fill_table(s_table);
+  __syncthreads();
+  const bool greedy = greedy_of(a, s);
+  const double c = rate_of(a, s);
+  const T *row = row_of<T>(a, t);
+  const int shift = shift_of(row), groups = (a.V + shift + 32 * N - 1) / (32 * N), per = (groups + CL - 1) / CL;
+  const int g0 = min(cl.rank() * per, groups), g1 = min(g0 + per, groups);
+  // sums over the warp's largest logit so far
+  double sum = 0.0;
+  int key = kNoKey, best_g = 0;
+  for (int g = g0 + warp * kLoads; g < g1; g += kSumWarps * kLoads) {
+    uint4 raw[kLoads];
+    float none[N];
+#pragma unroll
+    for (int k = 0; k < N; ++k) none[k] = kNone;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) raw[i] = g + i < g1 ? load_raw<T>(row, shift, a.V, g + i, lane) : Vec<T>::pack(none);
+    float x[kLoads][N];
+    int k4[kLoads], most = kNoKey;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      Vec<T>::unpack(raw[i], x[i]);
+      int k1 = kNoKey;
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        x[i][k] = eligible(x[i][k]);
+        k1 = max(k1, key_of(x[i][k]));
+      }
+      k4[i] = __reduce_max_sync(~0u, k1);
+      most = max(most, k4[i]);
+    }
+    if (most > key) {
+      if (sum > 0.0) sum *= pow2(c * ((double)of_key(key) - (double)of_key(most)), s_table);
+#pragma unroll
+      for (int i = kLoads - 1; i >= 0; --i)
+        if (k4[i] == most) best_g = g + i;
+      key = most;
+    }
+    if (greedy || key == kNoKey) continue;
+    const double m = (double)of_key(key);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+      for (int k = 0; k < N; ++k) sum += pow2(((double)x[i][k] - m) * c, s_table);
+  }
+  sum = warp_sum(sum);
+  if (lane == 0) { s_sum[warp] = sum; s_place[warp] = place_of(key, best_g); }
+  __syncthreads();
+  // the warps', then the blocks', over the largest of all; ties go to the lowest group
+  unsigned long long place = 0;
+#pragma unroll
+  for (int w = 0; w < kSumWarps; ++w) place = max(place, s_place[w]);
+  double total = 0.0;
+  const auto join = [&](double part, int from, int to) { return part > 0.0 ? part * pow2(c * ((double)of_key(from) - (double)of_key(to)), s_table) : 0.0; };
+#pragma unroll
+  for (int w = 0; w < kSumWarps; ++w) total += join(s_sum[w], place_key(s_place[w]), place_key(place));
+  Joined all[CL];
+  cl.gather({total, place}, all);
+  if (cl.rank() == 0 && warp == 0) {
+#pragma unroll
+    for (int r = 0; r < CL; ++r) place = max(place, all[r].place);
+    total = 0.0;
+#pragma unroll
+    for (int r = 0; r < CL; ++r) total += join(all[r].s, place_key(all[r].place), place_key(place));
+    const int k = place_key(place);
+    const int best = greedy && k != kNoKey ? id_in_group<T>(row, shift, a.V, place_id(place), k) : -1;
+    if (lane == 0) a.sums[t] = {total, of_key(k), best};
+  }
+  Cluster<CL>::barrier();                                  // nobody leaves while others read its box
+}
+
+// The walk and the next token.  CL blocks per sequence.
+constexpr int kWalkWarps = 16, kWalkThreads = 32 * kWalkWarps, kChunk = kWalkThreads;
+template <typename T, int CL>
+__global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constant__ VerifyArgs a, int room) {
+  pdl_grid_wait();
+  constexpr int N = Vec<T>::N, kLoads = 4;
+  extern __shared__ __align__(16) uint8_t smem[];
+  double *s_group = (double *)smem;                        // sums of this block's groups
+  float *s_most = (float *)(s_group + room);               // what they are relative to
+  uint8_t *s_out = (uint8_t *)(s_most + room);             // refused words of given drafts, a bit each: a byte per lane and group
+  __shared__ double s_table[kTable], s_p[kChunk], s_q[kChunk], s_warp[kWalkWarps];
+  __shared__ int s_parent[kChunk];
+  __shared__ float s_u[kChunk];
+  __shared__ unsigned long long s_place[kWalkWarps];
+  __shared__ Joined s_box[2];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int seq = blockIdx.x / CL;
+  Cluster<CL> cl = {&s_box, 0};
+  const bool first_block = cl.rank() == 0;
+  const int2 rows = rows_of(a, seq);
+  if (rows.y == 0) {
+    if (first_block) {
+      for (int i = tid; i < a.keep_stride; i += kWalkThreads) a.keep[(int64_t)seq * a.keep_stride + i] = -1;
+      if (tid == 0) { a.n_keep[seq] = 0; a.next[seq] = -1; }
+    }
+    return;
+  }
+  fill_table(s_table);
+  const bool greedy = greedy_of(a, seq);
+  const double c = rate_of(a, seq);
+  __syncthreads();
+
+  int cur = 0, length = 1;
+  double A = 0.0, R = 1.0;                                 // r = max(p - A q, 0), R = sum r (unless it is due)
+  int refused = 0;                                         // drafts refused at cur
+  bool due = false;
+  const T *row;
+  int shift, groups, per, g0, g1;
+  auto enter = [&](int at) {
+    row = row_of<T>(a, rows.x + at);
+    shift = shift_of(row);
+    groups = (a.V + shift + 32 * N - 1) / (32 * N);
+    per = (groups + CL - 1) / CL;
+    g0 = min(cl.rank() * per, groups);
+    g1 = min(g0 + per, groups);
+  };
+
+  // Sums of the groups of row cur into s_group.  `rest`: of max(2^(c (x - m)) - cut q, 0) with the given m; else of
+  // 2^(c (x - m)), m the group's own largest (s_most), without the words marked in s_out if `marked`.
+  auto sum_groups = [&](bool rest, bool marked, float m_row, double cut) {
+    const float *near = rest ? a.near + (int64_t)(rows.x + cur) * a.near_stride : nullptr;
+    for (int g = g0 + warp * kLoads; g < g1; g += kWalkWarps * kLoads) {
+      uint4 raw[kLoads];
+      float none[N];
+#pragma unroll
+      for (int k = 0; k < N; ++k) none[k] = kNone;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) raw[i] = g + i < g1 ? load_raw<T>(row, shift, a.V, g + i, lane) : Vec<T>::pack(none);
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        if (g + i >= g1) break;
+        float x[N];
+        Vec<T>::unpack(raw[i], x);
+        const uint32_t out = marked ? s_out[(g + i - g0) * 32 + lane] : 0u;
+        int k1 = kNoKey;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          x[k] = (out >> k) & 1 ? kNone : eligible(x[k]);
+          k1 = max(k1, key_of(x[k]));
+        }
+        const float m = rest ? m_row : of_key(__reduce_max_sync(~0u, k1));
+        double sum = 0.0;
+        if (m != kNone && !greedy) {
+          const int id = ((g + i) * 32 + lane) * N - shift;
+#pragma unroll
+          for (int k = 0; k < N; ++k) {
+            double e = pow2(((double)x[k] - (double)m) * c, s_table);
+            if (rest) e = fmax(e - cut * (double)(id + k >= 0 && id + k < a.V ? real(near[id + k]) : 0.f), 0.0);
+            sum += e;
+          }
+          sum = warp_sum(sum);
+        }
+        if (lane == 0) { s_group[g + i - g0] = sum; s_most[g + i - g0] = m; }
+      }
+    }
+    __syncthreads();
+  };
+  // this block's sum of s_group, the same in every thread
+  auto block_sum = [&]() {
+    double x = 0.0;
+    for (int i = tid; i < g1 - g0; i += kWalkThreads) x += s_group[i];
+    x = warp_sum(x);
+    if (lane == 0) s_warp[warp] = x;
+    __syncthreads();
+    x = 0.0;
+#pragma unroll
+    for (int w = 0; w < kWalkWarps; ++w) x += s_warp[w];
+    __syncthreads();
+    return x;
+  };
+  Joined all[CL];
+
+  enter(0);
+  for (int c0 = 0; c0 < rows.y && length < a.keep_stride; c0 += kChunk) {
+    // what the tests of the next drafts need: p and q of each one's token at its parent's row
+    __syncthreads();
+    if (c0 + tid < rows.y && c0 + tid > 0) {
+      const int j = c0 + tid, t = rows.x + j, up = a.parent ? a.parent[t] : j - 1, token = a.tokens[t];
+      bool ok = up >= 0 && up < j && token >= 0 && token < a.V;
+      if (!ok) atomicCAS(&a.head->status, 0, (int)PCOMOE_ERR_INDEX);
+      double p = 0.0, q = 1.0;
+      if (ok) {
+        const RowSums sums = a.sums[rows.x + up];
+        if (greedy) {
+          p = token == sums.best ? 1.0 : 0.0;
+        } else {
+          const float x = eligible(Vec<T>::one(row_of<T>(a, rows.x + up) + token));
+          if (x != kNone && sums.s > 0.0) p = pow2(c * ((double)x - (double)sums.m), s_table) / sums.s;
+        }
+        if (a.near) q = (double)real(a.near[(int64_t)(rows.x + up) * a.near_stride + token]);
+      }
+      s_p[tid] = p;
+      s_q[tid] = q;
+      s_u[tid] = a.u[t];
+      s_parent[tid] = ok ? up : -1;
+    } else {
+      s_parent[tid] = -1;
+    }
+    __syncthreads();
+    // every warp of every block takes the same way
+    int j = 0;
+    while (length < a.keep_stride) {
+      int hit = kChunk;
+      for (int b = j & ~31; b < kChunk; b += 32) {
+        const uint32_t m = __ballot_sync(~0u, b + lane >= j && s_parent[b + lane] == cur);
+        if (m) {
+          hit = b + __ffs(m) - 1;
+          break;
+        }
+      }
+      if (hit == kChunk) break;
+      double r = s_p[hit];
+      if (a.near) {
+        if (due) {
+          const RowSums sums = a.sums[rows.x + cur];
+          double left = 0.0;
+          if (greedy) {
+            // all of p lies on one word
+            left = sums.best >= 0 ? fmax(1.0 - A * (double)real(a.near[(int64_t)(rows.x + cur) * a.near_stride + sums.best]), 0.0) : 0.0;
+          } else if (sums.s > 0.0) {
+            sum_groups(true, false, sums.m, A * sums.s);
+            const double mine = block_sum();
+            cl.gather({mine, 0ull}, all);
+#pragma unroll
+            for (int k = 0; k < CL; ++k) left += all[k].s;
+            left /= sums.s;
+          }
+          R = left;
+          due = false;
+          if (!(R > 0.0)) { A = 0.0; R = 1.0; }            // nothing is left: the target's own distribution again
+        }
+        r = fmax(r - A * s_q[hit], 0.0);
+      } else if (refused) {
+        // a token that an earlier draft here had is gone
+        const int token = a.tokens[rows.x + c0 + hit];
+        bool again = false;
+        for (int b = cur + 1; b < c0 + hit && !again; b += 32) {
+          const int k = b + lane;
+          again = __any_sync(~0u, k < c0 + hit && (a.parent ? a.parent[rows.x + k] : k - 1) == cur && a.tokens[rows.x + k] == token);
+        }
+        if (again) r = 0.0;
+      }
+      if ((double)s_u[hit] * R * s_q[hit] < r) {
+        cur = c0 + hit;
+        enter(cur);
+        if (first_block && tid == 0) a.keep[(int64_t)seq * a.keep_stride + length] = cur;
+        ++length;
+        A = 0.0;
+        R = 1.0;
+        refused = 0;
+        due = false;
+      } else {
+        ++refused;
+        if (a.near) {
+          A += R;
+          due = true;
+        } else {
+          R = fmax(R - r, 0.0);
+          if (!(R > 0.0)) R = 1.0;
+        }
+      }
+      j = hit + 1;
+    }
+  }
+  if (first_block) {
+    if (tid == 0) { a.keep[(int64_t)seq * a.keep_stride] = 0; a.n_keep[seq] = length; }
+    for (int i = length + tid; i < a.keep_stride; i += kWalkThreads) a.keep[(int64_t)seq * a.keep_stride + i] = -1;
+  }
+
+  // the next token from row cur
+  const int mine = g1 - g0;
+  bool rest = a.near && A > 0.0 && !greedy;
+  bool marked = !a.near && refused > 0 && !greedy;
+  RowSums sums = {0.0, 0.f, -1};
+  if (rest) {
+    sums = a.sums[rows.x + cur];
+    rest = sums.s > 0.0;
+  }
+  if (marked) {
+    for (int i = tid; i < mine * 8; i += kWalkThreads) ((uint32_t *)s_out)[i] = 0u;
+    __syncthreads();
+    for (int k = cur + 1 + tid; k < rows.y; k += kWalkThreads) {
+      const int token = a.tokens[rows.x + k];
+      if ((a.parent ? a.parent[rows.x + k] : k - 1) == cur && token >= 0 && token < a.V) {
+        const int w = token + shift - g0 * 32 * N;         // place in this block's words
+        if (w >= 0 && w < mine * 32 * N) atomicOr((uint32_t *)s_out + (w / N) / 4, 1u << (((w / N) & 3) * 8 + w % N));
+      }
+    }
+    __syncthreads();
+  }
+  double block_scale = 1.0, total = 0.0;
+  unsigned long long place = 0;
+  for (;;) {
+    sum_groups(rest, marked, sums.m, A * sums.s);
+    if (!rest) {
+      // over the block's largest
+      unsigned long long best = place_of(kNoKey, 0);
+      for (int i = tid; i < mine; i += kWalkThreads) best = max(best, place_of(key_of(s_most[i]), g0 + i));
+      best = warp_max(best);
+      if (lane == 0) s_place[warp] = best;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kWalkWarps; ++w) best = max(best, s_place[w]);
+      place = best;
+      const double top = (double)of_key(place_key(best));
+      if (!greedy)
+        for (int i = tid; i < mine; i += kWalkThreads)
+          if (s_group[i] > 0.0) s_group[i] *= pow2(c * ((double)s_most[i] - top), s_table);
+      __syncthreads();
+    }
+    const double part = greedy ? 0.0 : block_sum();
+    cl.gather({part, place}, all);
+    unsigned long long whole = 0;
+#pragma unroll
+    for (int r = 0; r < CL; ++r) whole = max(whole, all[r].place);
+    total = 0.0;
+#pragma unroll
+    for (int r = 0; r < CL; ++r) {
+      if (!rest && all[r].s > 0.0) all[r].s *= pow2(c * ((double)of_key(place_key(all[r].place)) - (double)of_key(place_key(whole))), s_table);
+      if (r == cl.rank() && !rest && part > 0.0) block_scale = all[r].s / part;
+      total += all[r].s;
+    }
+    if (greedy) place = whole;
+    if (greedy || total > 0.0 || !(rest || marked)) break;
+    rest = marked = false;                                 // nothing is left: the target's own distribution
+  }
+  if (greedy) {
+    const int key = place_key(place);
+    if (first_block && warp == 0) {
+      const int id = key == kNoKey ? -1 : id_in_group<T>(row, shift, a.V, place_id(place), key);
+      if (lane == 0) a.next[seq] = id;
+    }
+  } else if (!(total > 0.0)) {
+    if (first_block && tid == 0) a.next[seq] = -1;
+  } else {
+    // the block, the group and the word in which the sum passes the target
+    const double target = (double)a.u_next[seq] * total;
+    double before = 0.0;
+    int owner = -1;
+#pragma unroll
+    for (int r = 0; r < CL; ++r) {
+      if (owner < 0 && before + all[r].s > target) owner = r;
+      if (owner < 0) before += all[r].s;
+    }
+    if (owner < 0) {                                       // rounding, or u_next at 1: the last word with any weight
+      before = INFINITY;
+#pragma unroll
+      for (int r = 0; r < CL; ++r)
+        if (all[r].s > 0.0) owner = r;
+    }
+    if (owner == cl.rank() && warp == 0) {
+      const double goal = before == INFINITY ? INFINITY : (target - before) / (rest ? 1.0 : block_scale);
+      const int each = (mine + 31) / 32;
+      double sum = 0.0;
+      int last = -1;                                       // the last group with any weight
+      for (int i = lane * each; i < min((lane + 1) * each, mine); ++i) {
+        sum += s_group[i];
+        if (s_group[i] > 0.0) last = i;
+      }
+      double upto = sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const double y = __shfl_up_sync(~0u, upto, o);
+        if (lane >= o) upto += y;
+      }
+      const uint32_t past = __ballot_sync(~0u, upto > goal);
+      int g = __reduce_max_sync(~0u, last);
+      double base = INFINITY;                              // all of that group
+      if (past) {
+        const int l = __ffs(past) - 1;
+        base = __shfl_sync(~0u, upto - sum, l);
+        int found = -1;
+        for (int i = l * each; i < min((l + 1) * each, mine); ++i) {
+          if (base + s_group[i] > goal) {
+            found = i;
+            break;
+          }
+          base += s_group[i];
+        }
+        if (found >= 0) g = found;
+        else base = INFINITY;
+      }
+      const float m = s_most[g];
+      const double scale = rest ? 1.0 : pow2(c * ((double)m - (double)of_key(place_key(place))), s_table);
+      const double left = base == INFINITY ? INFINITY : (goal - base) / scale;
+      float x[N];
+      load_words<T>(row, shift, a.V, g0 + g, lane, x);
+      const uint32_t out = marked ? s_out[g * 32 + lane] : 0u;
+      const float *near = rest ? a.near + (int64_t)(rows.x + cur) * a.near_stride : nullptr;
+      const int id = ((g0 + g) * 32 + lane) * N - shift;
+      double e[N], lane_sum = 0.0;
+      int last_word = -1;
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        const float y = (out >> k) & 1 ? kNone : eligible(x[k]);
+        e[k] = pow2(((double)y - (double)m) * c, s_table);
+        if (rest) e[k] = fmax(e[k] - A * sums.s * (double)(id + k >= 0 && id + k < a.V ? real(near[id + k]) : 0.f), 0.0);
+        lane_sum += e[k];
+        if (e[k] > 0.0) last_word = id + k;
+      }
+      double incl = lane_sum;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const double y = __shfl_up_sync(~0u, incl, o);
+        if (lane >= o) incl += y;
+      }
+      int pick = INT_MAX;
+      double run = incl - lane_sum;
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        run += e[k];
+        if (e[k] > 0.0 && run > left && pick == INT_MAX) pick = id + k;
+      }
+      const int lowest = (int)__reduce_min_sync(~0u, (unsigned)pick);
+      const int highest = __reduce_max_sync(~0u, last_word);
+      if (lane == 0) a.next[seq] = lowest == INT_MAX ? highest : lowest;
+    }
+  }
+  Cluster<CL>::barrier();                                  // nobody leaves while others read its box
+}
+
+template <typename... K, typename... A>
+cudaError_t launch_clusters(void (*kernel)(K...), int items, int cl, int threads, size_t smem, cudaStream_t st, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(items * cl));
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = (unsigned)cl;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = cl > 1 ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, K(args)...);
+}
+
+template <typename T, int CL>
+pcomoe_status launch_sums(const VerifyArgs &a, cudaStream_t st) {
+  PCOMOE_CUDA_TRY(launch_clusters(row_sums_kernel<T, CL>, a.T, CL, 32 * kSumWarps, 0, st, a));
+  count_launch();
+  return PCOMOE_OK;
+}
+template <typename T, int CL>
+pcomoe_status launch_walk(const VerifyArgs &a, int groups, cudaStream_t st) {
+  const int room = ((groups + CL - 1) / CL + 1) & ~1;
+  static PerDeviceOnce once;
+  int dev = -1;
+  PCOMOE_CUDA_TRY(cudaGetDevice(&dev));
+  if (once.first_use(dev)) {
+    PCOMOE_CUDA_TRY(cudaFuncSetAttribute(walk_kernel<T, CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxGroups * (8 + 4 + 32)));
+    once.done(dev);
+  }
+  PCOMOE_CUDA_TRY(launch_clusters(walk_kernel<T, CL>, a.n, CL, kWalkThreads, (size_t)room * (8 + 4 + 32), st, a, room));
+  count_launch();
+  return PCOMOE_OK;
+}
+
+template <typename T>
+pcomoe_status run(const VerifyArgs &a, int sms, cudaStream_t st) {
+  const int groups = (a.V + 15) / (32 * Vec<T>::N) + 1;    // at any alignment
+  // blocks per row and per sequence: while there is an SM for each and enough groups for its warps
+  const auto blocks = [&](int items, int warps) {
+    int cl = 1;
+    while (cl < 8 && ((int64_t)items * 2 * cl <= sms || groups > cl * (kMaxGroups - 2)) && groups >= 2 * cl * warps) cl *= 2;
+    return cl;
+  };
+  pcomoe_status s = PCOMOE_OK;
+  if (a.T > 0) switch (blocks(a.T, kSumWarps)) {
+    case 1: s = launch_sums<T, 1>(a, st); break;
+    case 2: s = launch_sums<T, 2>(a, st); break;
+    case 4: s = launch_sums<T, 4>(a, st); break;
+    default: s = launch_sums<T, 8>(a, st); break;
+  }
+  if (s != PCOMOE_OK) return s;
+  switch (blocks(a.n, kWalkWarps)) {
+    case 1: return launch_walk<T, 1>(a, groups, st);
+    case 2: return launch_walk<T, 2>(a, groups, st);
+    case 4: return launch_walk<T, 4>(a, groups, st);
+    default: return launch_walk<T, 8>(a, groups, st);
+  }
+}
+
+}  // namespace
+}  // namespace pcomoe
+
+using namespace pcomoe;
+
+extern "C" {
+
+pcomoe_status pcomoe_verify_workspace_bytes(int32_t max_tokens, size_t *bytes) {
+  if (!bytes) return PCOMOE_ERR_INVALID_ARG;
+  if (max_tokens < 0) return PCOMOE_ERR_SHAPE;
+  *bytes = 256 + sizeof(RowSums) * (size_t)max_tokens;
+  return PCOMOE_OK;
+}
+
+pcomoe_status pcomoe_verify_drafts(int32_t dtype, int32_t T, int32_t V, int32_t n, const int32_t *d_cu_len, const int32_t *d_tokens, const int32_t *d_parent,
+                                   const void *d_logits, int64_t row_stride, const float *d_draft_probs, int64_t draft_stride, const float *d_temperature,
+                                   const float *d_u, const float *d_u_next, int32_t *d_keep, int32_t keep_stride, int32_t *d_n_keep, int32_t *d_next,
+                                   void *d_workspace, size_t ws_bytes, void *stream) {
+  if (dtype != PCOMOE_BF16 && dtype != PCOMOE_FP32) return PCOMOE_ERR_INVALID_ARG;
+  if (T < 0 || V <= 0 || n < 0 || n > 65535 || keep_stride < 0) return PCOMOE_ERR_SHAPE;
+  if (V > kMaxVocab) return PCOMOE_ERR_UNSUPPORTED;
+  if (n == 0) return PCOMOE_OK;
+  const int64_t e = (int64_t)dtype_size(dtype);
+  if (!d_cu_len || !d_keep || keep_stride == 0 || !d_n_keep || !d_next || !d_u_next || (T > 0 && (!d_tokens || !d_u || !d_logits))) return PCOMOE_ERR_INVALID_ARG;
+  if (T > 0 && (row_stride < V || (uintptr_t)d_logits % e || (d_draft_probs && (draft_stride < V || (uintptr_t)d_draft_probs % 4)))) return PCOMOE_ERR_INVALID_ARG;
+  if ((int64_t)T * 8 > INT32_MAX) return PCOMOE_ERR_SHAPE;
+  if (!d_workspace || ((uintptr_t)d_workspace & 255) || ws_bytes < 256 + sizeof(RowSums) * (size_t)T) return PCOMOE_ERR_WORKSPACE;
+  int sms;
+  const pcomoe_status st = current_sms(&sms);
+  if (st != PCOMOE_OK) return st;
+  VerifyArgs a = {};
+  a.T = T; a.V = V; a.n = n;
+  a.cu = d_cu_len; a.tokens = d_tokens; a.parent = d_parent;
+  a.x = (const char *)d_logits; a.row_bytes = row_stride * e;
+  a.near = d_draft_probs; a.near_stride = draft_stride;
+  a.temperature = d_temperature; a.u = d_u; a.u_next = d_u_next;
+  a.keep = d_keep; a.n_keep = d_n_keep; a.next = d_next; a.keep_stride = keep_stride;
+  a.head = (VerifyHeader *)d_workspace;
+  a.sums = (RowSums *)((char *)d_workspace + 256);
+  return dtype == PCOMOE_BF16 ? run<__nv_bfloat16>(a, sms, (cudaStream_t)stream) : run<float>(a, sms, (cudaStream_t)stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,340 @@
+// Accumulated attention weight of cached positions: host side, and the kernel of few counted rows.
+//
+// Mathematics.  w_p += sum over counted rows and heads of 2^(c q.k_p - c' lse), c = scale log2 e, c' = log2 e: the products of
+// attention's first matrix product again, with the log sums that attention has left instead of a running maximum, so one
+// pass over the keys and no pass over the values.  A position is a row of the product here and the counted rows are its
+// columns, so that a position's sum stays inside a few lanes.
+//
+// What bounds it with few rows: one read of the keys (HBM).  A warp takes 16 keys of one head at a time (no piece crosses a
+// page); its lanes load whole 16-byte pieces straight into the fragments of the warp MMAs (m16n8k16): the order of the
+// inner dimension is free as long as both operands have the same one, so the keys need no shared memory, and the
+// queries are laid out once per sequence in the same order.  All heads of a block of keys are taken by one block of
+// threads and added in order, so nothing is added across blocks and no atomics are needed.
+#include <algorithm>
+#include <cmath>
+
+#include "weigh.cuh"
+
+namespace pcomoe {
+namespace {
+
+constexpr int kWarps = 8, kThreads = 32 * kWarps, kKeys = 16;
+constexpr int kItems = 32;              // pieces of 16 keys of a head in a block of keys, about
+constexpr int kMaxSubs = 16;            // pieces of 16 keys of one head in it
+constexpr int kQBytes = 48 * 1024;      // queries held at a time
+constexpr int kExtra = 2;               // cost of a block of keys besides its columns, in tiles of 8 columns
+
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// 16 keys of a head in registers, and their weights over the columns [0, tiles * 8) at q, lse, lim (lim: the last position that
+// a column sees).  key0: position of the first.  Lane 0..15 of the result: key0 + lane.
+template <typename T, int D> struct Piece;
+
+template <int D> struct Piece<__nv_bfloat16, D> {
+  uint4 x[2][D / 32];
+  __device__ __forceinline__ void load(const __nv_bfloat16 *k) {
+    const int lane = threadIdx.x & 31;
+    const char *p = (const char *)(k + (lane >> 2) * D) + (lane & 3) * 16;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+      x[0][i] = *(const uint4 *)(p + 64 * i);
+      x[1][i] = *(const uint4 *)(p + 64 * i + 16 * D);
+    }
+  }
+  // place of the 16 bytes c of column col in the layout that sums() reads: a tile of 8 columns, step by step, lane by lane
+  static __device__ __forceinline__ int place(int col, int c) { return (((col >> 3) * (D / 32) + (c >> 2)) * 32 + (col & 7) * 4 + (c & 3)) * 16; }
+  __device__ __forceinline__ float sums(const char *q, const float *lse, const int *lim, int tiles, int key0, float scale) const {
+    const int lane = threadIdx.x & 31;
+    const int p0 = key0 + (lane >> 2), p1 = p0 + 8;
+    float w0 = 0.f, w1 = 0.f;
+    for (int t = 0; t < tiles; ++t) {
+      float c[4] = {0.f, 0.f, 0.f, 0.f};
+      const uint4 *b = (const uint4 *)q + t * (D / 32) * 32 + lane;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        const uint4 y = b[32 * i];
+        mma(c, x[0][i].x, x[1][i].x, x[0][i].y, x[1][i].y, y.x, y.y);
+        mma(c, x[0][i].z, x[1][i].z, x[0][i].w, x[1][i].w, y.z, y.w);
+      }
+      const float2 l = *(const float2 *)(lse + t * 8 + (lane & 3) * 2);
+      const int2 m = *(const int2 *)(lim + t * 8 + (lane & 3) * 2);
+      // chosen, not multiplied: what is not seen adds nothing whatever it is
+      w0 += (p0 <= m.x ? exp2_fast(fmaf(c[0], scale, -l.x)) : 0.f) + (p0 <= m.y ? exp2_fast(fmaf(c[1], scale, -l.y)) : 0.f);
+      w1 += (p1 <= m.x ? exp2_fast(fmaf(c[2], scale, -l.x)) : 0.f) + (p1 <= m.y ? exp2_fast(fmaf(c[3], scale, -l.y)) : 0.f);
+    }
+    w0 += __shfl_xor_sync(~0u, w0, 1);
+    w1 += __shfl_xor_sync(~0u, w1, 1);
+    w0 += __shfl_xor_sync(~0u, w0, 2);
+    w1 += __shfl_xor_sync(~0u, w1, 2);
+    // lane r holds key r
+    const float lo = __shfl_sync(~0u, w0, (lane & 7) * 4), hi = __shfl_sync(~0u, w1, (lane & 7) * 4);
+    return lane & 8 ? hi : lo;
+  }
+};
+
+// fp32: a lane holds half of a key's row
+template <int D> struct Piece<float, D> {
+  float4 x[D / 8];
+  __device__ __forceinline__ void load(const float *k) {
+    const int lane = threadIdx.x & 31;
+    const float4 *p = (const float4 *)(k + (lane & 15) * D + (lane >> 4) * (D / 2));
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) x[i] = p[i];
+  }
+  static __device__ __forceinline__ int place(int col, int c) { return (col * (D / 4) + c) * 16; }
+  __device__ __forceinline__ float sums(const char *q, const float *lse, const int *lim, int tiles, int key0, float scale) const {
+    const int lane = threadIdx.x & 31, p = key0 + (lane & 15);
+    const float4 *b = (const float4 *)q + (lane >> 4) * (D / 8);
+    float w = 0.f;
+    for (int c = 0; c < 8 * tiles; ++c) {
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) {
+        const float4 y = b[c * (D / 4) + i];
+        s[0] = fmaf(x[i].x, y.x, s[0]);
+        s[1] = fmaf(x[i].y, y.y, s[1]);
+        s[2] = fmaf(x[i].z, y.z, s[2]);
+        s[3] = fmaf(x[i].w, y.w, s[3]);
+      }
+      float t = (s[0] + s[1]) + (s[2] + s[3]);
+      t += __shfl_xor_sync(~0u, t, 16);
+      w += p <= lim[c] ? exp2_fast(fmaf(t, scale, -lse[c])) : 0.f;
+    }
+    return w;
+  }
+};
+
+// Heads and columns of a head that are held at a time, and pieces of 16 keys of one head in a block of keys.
+struct Cut {
+  int heads, cols, subs;
+};
+template <typename T, int D>
+__host__ __device__ inline Cut cut_of(int hkv, int hq, int64_t most_cols) {
+  constexpr int kCols = kQBytes / (D * (int)sizeof(T));
+  Cut c;
+  c.heads = hkv * 8 <= kCols ? hkv : kCols / 8;
+  c.heads = c.heads < kItems ? c.heads : kItems;
+  const int64_t fit = (int64_t)(kCols / c.heads) & ~int64_t(7), need = (most_cols + 7) & ~int64_t(7);
+  c.cols = (int)(fit < need ? fit : need);
+  c.subs = kItems / c.heads < kMaxSubs ? kItems / c.heads : kMaxSubs;
+  return c;
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads, 2) weigh_kernel(const __grid_constant__ WeighArgs a) {
+  constexpr int kCols = kQBytes / (D * (int)sizeof(T)), kPieces = D * (int)sizeof(T) / 16;
+  extern __shared__ __align__(16) char s_q[];
+  __shared__ float s_lse[kCols];
+  __shared__ int s_lim[kCols];
+  __shared__ float s_part[2][kItems][kKeys];
+  __shared__ uint32_t s_bits[2 * (kMaxSeqs / 32)];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  pdl_grid_wait();
+  const uint32_t *twice = find_repeats(a.seqs, a.n, a.max_seqs, s_bits);
+
+  // This block's share of the line of all sequences' blocks of keys, which count for their columns; every warp finds it.
+  const Cut fixed = cut_of<T, D>(a.hkv, a.hq, 8);
+  const int keys = fixed.subs * kKeys;
+  auto blocks_of = [&](const WeighSeq &s) { return (s.len + keys - 1) / keys; };
+  auto cost_of = [&](const WeighSeq &s) { return (uint64_t)(kExtra + ((int64_t)s.m * a.g + 7) / 8); };
+  uint64_t total = 0;
+  for (int s0 = 0; s0 < a.n; s0 += 32) {
+    uint64_t w = 0;
+    if (s0 + lane < a.n) {
+      const WeighSeq s = weigh_seq(a, s0 + lane, twice);
+      w = blocks_of(s) * cost_of(s);
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) w += __shfl_xor_sync(~0u, w, o);
+    total += w;
+  }
+  const uint64_t share = (total + gridDim.x - 1) / gridDim.x, x0 = share * blockIdx.x, x1 = min(x0 + share, total);
+  if (x0 >= x1) return;
+  uint64_t at = 0;                                         // of the line: where sequence list begins
+  int parity = 0;
+  for (int s0 = 0; s0 < a.n && at < x1; s0 += 32) {
+    WeighSeq mine = {};
+    uint64_t w = 0;
+    if (s0 + lane < a.n) {
+      mine = weigh_seq(a, s0 + lane, twice);
+      w = blocks_of(mine) * cost_of(mine);
+    }
+    uint64_t upto = w;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint64_t y = __shfl_up_sync(~0u, upto, o);
+      if (lane >= o) upto += y;
+    }
+    const uint32_t ours = __ballot_sync(~0u, w > 0 && at + upto > x0 && at + upto - w < x1);
+    for (uint32_t left = ours; left; left &= left - 1) {
+      const int l = __ffs(left) - 1, list = s0 + l;
+      WeighSeq s;
+      s.q0 = __shfl_sync(~0u, mine.q0, l);
+      s.n = __shfl_sync(~0u, mine.n, l);
+      s.m = __shfl_sync(~0u, mine.m, l);
+      s.len = __shfl_sync(~0u, mine.len, l);
+      s.base = s.len - s.m;
+      s.id = __shfl_sync(~0u, mine.id, l);
+      const uint64_t begin = at + __shfl_sync(~0u, upto - w, l), cost = cost_of(s);
+      // the blocks that begin inside of the share
+      const int b0 = begin >= x0 ? 0 : (int)((x0 - begin + cost - 1) / cost);
+      const int b1 = (int)min((uint64_t)blocks_of(s), (x1 - begin + cost - 1) / cost);
+      if (b0 >= b1) continue;
+      const int32_t *table = a.table + (int64_t)s.id * a.max_pages;
+      float *weight = a.weight + s.id * a.weight_stride;
+      const int64_t all_cols = (int64_t)s.m * a.g;
+      const Cut cut = cut_of<T, D>(a.hkv, a.hq, all_cols);
+      bool first = true;
+      for (int h0 = 0; h0 < a.hkv; h0 += cut.heads)
+        for (int64_t c0 = 0; c0 < all_cols; c0 += cut.cols) {
+          const int heads = min(cut.heads, a.hkv - h0);
+          const int cols = (int)min((int64_t)cut.cols, all_cols - c0), tiles = (cols + 7) >> 3;
+          __syncthreads();                                 // the last ones are done with what is replaced
+          for (int u = tid; u < heads * tiles * 8 * kPieces; u += kThreads) {
+            const int c = u % kPieces, hc = u / kPieces, col = hc % (tiles * 8), h = hc / (tiles * 8);
+            uint4 x = make_uint4(0, 0, 0, 0);
+            int lim = -1;
+            float lse = 0.f;
+            if (col < cols) {
+              const int64_t at_col = c0 + col;
+              const int k = (int)(at_col / a.g), head = (h0 + h) * a.g + (int)(at_col - (int64_t)k * a.g), row = counted_row(a, s, list, k);
+              if (row >= 0) {
+                x = *(const uint4 *)((const char *)((const T *)a.q + row * a.q_stride + (int64_t)head * D) + c * 16);
+                if (c == 0) {
+                  lse = a.lse[(int64_t)row * a.hq + head];
+                  if (lse != -INFINITY) lim = s.base + k;  // a row that saw nothing adds nothing
+                }
+              }
+            }
+            *(uint4 *)(s_q + (size_t)h * tiles * 8 * kPieces * 16 + Piece<T, D>::place(col, c)) = x;
+            if (c == 0) { s_lse[h * tiles * 8 + col] = lse * kLog2ef; s_lim[h * tiles * 8 + col] = lim; }
+          }
+          __syncthreads();
+          // pieces of 16 keys of a head, a block of keys after another: the keys of a warp's next piece come in while it works, and the
+          // page of the one after that is looked up
+          const int per = cut.subs * heads;
+          int nb = b0, ni = warp;                          // the piece that is looked up
+          auto look = [&]() -> const T * {
+            const int key0 = nb * keys + (ni / heads) * kKeys;
+            if (ni >= per || nb >= b1 || key0 >= s.len) return nullptr;
+            return (const T *)a.k + (weigh_page_row(a, table, key0) + (int64_t)(h0 + ni % heads) * a.page) * D;
+          };
+          auto advance = [&]() {
+            ni += kWarps;
+            if (ni >= per) { ni = warp; ++nb; }
+          };
+          Piece<T, D> now, next;
+          const T *from = look();
+          if (from) next.load(from);
+          advance();
+          from = look();
+          for (int b = b0; b < b1; ++b) {
+            for (int i = warp; i < per; i += kWarps) {
+              now = next;
+              if (from) next.load(from);
+              advance();
+              from = look();
+              const int key0 = b * keys + (i / heads) * kKeys, h = i % heads;
+              if (key0 < s.len) {
+                const float w16 = now.sums(s_q + (size_t)h * tiles * 8 * kPieces * 16, s_lse + h * tiles * 8, s_lim + h * tiles * 8, tiles, key0, a.scale_log2);
+                if (lane < kKeys) s_part[parity][i][lane] = w16;
+              }
+            }
+            __syncthreads();
+            const int p = b * keys + tid;
+            if (tid < keys && p < s.len) {
+              float sum = 0.f;
+              for (int h = 0; h < heads; ++h) sum += s_part[parity][(tid / kKeys) * heads + h][tid % kKeys];
+              weight[p] = first && a.fresh && p >= s.base ? sum : weight[p] + sum;
+            }
+            parity ^= 1;
+          }
+          first = false;
+        }
+    }
+    at += __shfl_sync(~0u, upto, 31);
+  }
+}
+
+template <typename T, int D>
+pcomoe_status run(const WeighArgs &a, int sms, cudaStream_t st) {
+  static PerDeviceOnce once;
+  int dev = -1;
+  PCOMOE_CUDA_TRY(cudaGetDevice(&dev));
+  if (once.first_use(dev)) {
+    PCOMOE_CUDA_TRY(cudaFuncSetAttribute(weigh_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kQBytes));
+    once.done(dev);
+  }
+  PCOMOE_CUDA_TRY(launch_pdl(weigh_kernel<T, D>, dim3(2 * sms), dim3(kThreads), kQBytes, st, a));
+  count_launch();
+  return PCOMOE_OK;
+}
+
+pcomoe_status check_config(const pcomoe_attn_config *c, const pcomoe_cache *cache) {
+  if (!c || c->struct_size != (int32_t)sizeof(pcomoe_attn_config)) return PCOMOE_ERR_INVALID_ARG;
+  if (c->q_heads <= 0 || c->kv_heads <= 0 || c->q_heads % c->kv_heads || c->head_dim <= 0 || !(c->scale > 0.f) || !std::isfinite(c->scale))
+    return PCOMOE_ERR_INVALID_ARG;
+  if (c->dtype != PCOMOE_BF16 && c->dtype != PCOMOE_FP32) return PCOMOE_ERR_INVALID_ARG;
+  if (c->head_dim != 64 && c->head_dim != 128) return PCOMOE_ERR_UNSUPPORTED;
+  if (c->q_heads > 4096) return PCOMOE_ERR_SHAPE;
+  const pcomoe_status st = check_cache(cache);
+  if (st != PCOMOE_OK) return st;
+  if (cache->kv_heads != c->kv_heads || cache->head_dim != c->head_dim || cache->dtype != c->dtype) return PCOMOE_ERR_INVALID_ARG;
+  return PCOMOE_OK;
+}
+
+constexpr size_t kWorkspace = 256;       // a status word
+
+}  // namespace
+}  // namespace pcomoe
+
+using namespace pcomoe;
+
+extern "C" {
+
+pcomoe_status pcomoe_weigh_workspace_bytes(const pcomoe_attn_config *cfg, const pcomoe_cache *cache, size_t *bytes) {
+  if (!bytes) return PCOMOE_ERR_INVALID_ARG;
+  const pcomoe_status st = check_config(cfg, cache);
+  if (st != PCOMOE_OK) return st;
+  *bytes = kWorkspace;
+  return PCOMOE_OK;
+}
+
+pcomoe_status pcomoe_cache_weigh(const pcomoe_attn_config *cfg, const pcomoe_cache *cache, int32_t layer, int32_t T, int32_t n, const int32_t *d_seqs,
+                                 const int32_t *d_cu_len, const void *d_q, int64_t q_stride, const float *d_lse, const int32_t *d_keep,
+                                 int32_t keep_stride, const int32_t *d_n_keep, int32_t fresh, float *d_weight, int64_t weight_stride,
+                                 void *d_workspace, size_t ws_bytes, void *stream) {
+  pcomoe_status st = check_config(cfg, cache);
+  if (st != PCOMOE_OK) return st;
+  if (layer < 0 || layer >= cache->layers || n < 0) return PCOMOE_ERR_INVALID_ARG;
+  if (T < 0 || n > cache->max_seqs) return PCOMOE_ERR_SHAPE;
+  if (T == 0 || n == 0) return PCOMOE_OK;
+  if (!d_seqs || !d_cu_len || !d_q || !d_lse || !d_weight || !d_keep != !d_n_keep || (d_keep && keep_stride <= 0)) return PCOMOE_ERR_INVALID_ARG;
+  if (q_stride < (int64_t)cfg->q_heads * cfg->head_dim || weight_stride < (int64_t)cache->max_pages * cache->page_size) return PCOMOE_ERR_INVALID_ARG;
+  const int64_t e = (int64_t)dtype_size(cfg->dtype);
+  if (((uintptr_t)d_q & 15) || (q_stride * e) % 16) return PCOMOE_ERR_UNSUPPORTED;
+  if ((int64_t)T * (cfg->q_heads / cfg->kv_heads) > INT32_MAX) return PCOMOE_ERR_SHAPE;
+  if (!d_workspace || ((uintptr_t)d_workspace & 255) || ws_bytes < kWorkspace) return PCOMOE_ERR_WORKSPACE;
+  int sms;
+  if ((st = current_sms(&sms)) != PCOMOE_OK) return st;
+  WeighArgs a = {};
+  a.T = T; a.n = n; a.hq = cfg->q_heads; a.hkv = cfg->kv_heads; a.g = cfg->q_heads / cfg->kv_heads;
+  a.scale_log2 = cfg->scale * 1.4426950408889634f;
+  a.seqs = d_seqs; a.cu = d_cu_len; a.keep = d_keep; a.n_keep = d_n_keep; a.keep_stride = keep_stride; a.fresh = fresh != 0;
+  a.q = d_q; a.q_stride = q_stride; a.lse = d_lse;
+  a.k = (const char *)cache->d_k + (int64_t)layer * cache->pages * cache->kv_heads * cache->page_size * cache->head_dim * e;
+  a.len = cache->d_seq_len; a.table = cache->d_page_table;
+  a.pages = cache->pages; a.page = cache->page_size; a.max_seqs = cache->max_seqs; a.max_pages = cache->max_pages;
+  for (a.page_shift = 0; (1 << a.page_shift) < cache->page_size;) ++a.page_shift;
+  a.weight = d_weight; a.weight_stride = weight_stride;
+  a.status = (int32_t *)((char *)d_workspace + offsetof(DevPlan, status_router));
+  a.limit_ns = wait_limit_ns();
+  if (cfg->dtype == PCOMOE_BF16) return cfg->head_dim == 64 ? run<__nv_bfloat16, 64>(a, sms, (cudaStream_t)stream) : run<__nv_bfloat16, 128>(a, sms, (cudaStream_t)stream);
+  return cfg->head_dim == 64 ? run<float, 64>(a, sms, (cudaStream_t)stream) : run<float, 128>(a, sms, (cudaStream_t)stream);
+}
+
+}  // extern "C"
