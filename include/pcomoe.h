@@ -535,12 +535,12 @@ pcomoe_status pcomoe_heads_rotate_cached(const pcomoe_rotate_config *cfg, const 
  * sees makes that position's weight NaN.  Scores are accumulated in fp32 and summed in fp32, in an order that the shapes fix:
  * bits do not change from call to call.
  * Errors: as pcomoe_attn_cached without a mask; INVALID_ARG also (one of d_keep and d_n_keep, weight_stride too small), SHAPE
- * (n > max_seqs).  WORKSPACE: pcomoe_weigh_workspace_bytes, 256-byte aligned, its first 256 bytes zero before the first
- * use.  Device: INDEX (a sequence out of range or repeated, more counted rows than cached positions, a list past T: the
+ * (n > max_seqs).  WORKSPACE: pcomoe_weigh_workspace_bytes for n listed sequences, 256-byte aligned, its first 256 bytes
+ * zero before the first use, one call at a time.  Device: INDEX (a sequence out of range or repeated, more counted rows than cached positions, a list past T: the
  * sequence is skipped; a number of d_keep out of range: that row counts nothing; a table entry that is no page: page 0 is
  * read in its place).
  */
-pcomoe_status pcomoe_weigh_workspace_bytes(const pcomoe_attn_config *cfg, const pcomoe_cache *cache, size_t *bytes);
+pcomoe_status pcomoe_weigh_workspace_bytes(const pcomoe_attn_config *cfg, const pcomoe_cache *cache, int32_t n, size_t *bytes);
 pcomoe_status pcomoe_cache_weigh(const pcomoe_attn_config *cfg, const pcomoe_cache *cache, int32_t layer, int32_t T, int32_t n, const int32_t *d_seqs,
                                  const int32_t *d_cu_len, const void *d_q, int64_t q_stride, const float *d_lse, const int32_t *d_keep,
                                  int32_t keep_stride, const int32_t *d_n_keep, int32_t fresh, float *d_weight, int64_t weight_stride,

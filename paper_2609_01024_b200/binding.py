@@ -122,7 +122,7 @@ def load_library(path: str | None = None):
     pr = ctypes.POINTER(pcomoe_rotate_config)
     lib.pcomoe_heads_rotate.argtypes = [pr, i32, vp, vp, vp, vp] + [vp, i64] * 4 + [vp]
     lib.pcomoe_heads_rotate_cached.argtypes = [pr, pc, i32, i32, i32, vp, vp, vp, vp, vp, vp] + [vp, i64] * 5 + [vp, sz, vp]
-    lib.pcomoe_weigh_workspace_bytes.argtypes = [pa, pc, ctypes.POINTER(sz)]
+    lib.pcomoe_weigh_workspace_bytes.argtypes = [pa, pc, i32, ctypes.POINTER(sz)]
     lib.pcomoe_cache_weigh.argtypes = [pa, pc, i32, i32, i32, vp, vp, vp, i64, vp, vp, i32, vp, i32, vp, i64, vp, sz, vp]
     lib.pcomoe_evict_workspace_bytes.argtypes = [pc, i32, ctypes.POINTER(sz)]
     lib.pcomoe_cache_evict.argtypes = [pc, i32, vp, vp, i32, i32, vp, i64, vp, sz, vp]
@@ -859,7 +859,7 @@ class HeadRotation:
 class CacheWeights:
     """How much each cached position was attended to (pcomoe_cache_weigh) and eviction by it (pcomoe_cache_evict).  ``weight`` [max_seqs, max_pages *
     page_size] fp32, by sequence and position; memory that the caller has already is used in place.  Up to `max_listed` sequences can be
-    evicted from in a call (all of them by default; the lists of places take 4 bytes per position and listed sequence)."""
+    listed in a call (all of them by default; the workspace takes 4 bytes times the kv heads, at least 8, per position and listed sequence)."""
 
     def __init__(self, cache: PagedCache, *, q_heads, scale=None, weight=None, max_listed=None):
         self.cache, self.device, self.gpu, self._lib = cache, cache.device, cache.gpu, cache._lib
@@ -874,7 +874,7 @@ class CacheWeights:
         self.max_listed = c.max_seqs if max_listed is None else max_listed
         size = ctypes.c_size_t(0)
         # (a head size that add() refuses can still be evicted from)
-        status = self._lib.pcomoe_weigh_workspace_bytes(self._cfg, cache._ref, ctypes.byref(size))
+        status = self._lib.pcomoe_weigh_workspace_bytes(self._cfg, cache._ref, self.max_listed, ctypes.byref(size))
         if status != PCOMOE_ERR_UNSUPPORTED:
             _check(status, "pcomoe_weigh_workspace_bytes")
         need = size.value
@@ -889,7 +889,7 @@ class CacheWeights:
         of their sequences.  After PagedCache.keep pass its lists, and only the kept rows count.  fresh: this is the first layer of the step."""
         T, n = q.shape[0], seqs.numel()
         shape, (row, head, one) = q.shape, q.stride()
-        assert shape[1] == self.q_heads and shape[2] == self.cache.head_dim and q.dtype is _TORCH[self.cache.dtype] and one == 1 and \
+        assert n <= self.max_listed and shape[1] == self.q_heads and shape[2] == self.cache.head_dim and q.dtype is _TORCH[self.cache.dtype] and one == 1 and \
             (head == shape[2] or shape[1] == 1) and q.device == self.device, (shape, q.stride(), q.dtype, q.device)
         lists = (None, 0, None)
         if keep is not None:

@@ -22,6 +22,7 @@ constexpr int kWarps = 8, kThreads = 32 * kWarps, kKeys = 16;
 constexpr int kItems = 32;              // pieces of 16 keys of a head in a block of keys, about
 constexpr int kMaxSubs = 16;            // pieces of 16 keys of one head in it
 constexpr int kQBytes = 48 * 1024;      // queries held at a time
+constexpr int kManyColumns = 96;        // of a sequence on average, from which on the tensor-core kernel is taken
 constexpr int kExtra = 2;               // cost of a block of keys besides its columns, in tiles of 8 columns
 
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -287,7 +288,10 @@ pcomoe_status check_config(const pcomoe_attn_config *c, const pcomoe_cache *cach
   return PCOMOE_OK;
 }
 
-constexpr size_t kWorkspace = 256;       // a status word
+// Workspace: a status word, partial sums of the kernel of many rows.
+size_t workspace_of(const pcomoe_attn_config *c, const pcomoe_cache *cache, int n) {
+  return 256 + (c->dtype == PCOMOE_BF16 ? weigh_tc_bytes(c->kv_heads, (int64_t)cache->max_pages * cache->page_size, n) : 0);
+}
 
 }  // namespace
 }  // namespace pcomoe
@@ -296,11 +300,13 @@ using namespace pcomoe;
 
 extern "C" {
 
-pcomoe_status pcomoe_weigh_workspace_bytes(const pcomoe_attn_config *cfg, const pcomoe_cache *cache, size_t *bytes) {
+pcomoe_status pcomoe_weigh_workspace_bytes(const pcomoe_attn_config *cfg, const pcomoe_cache *cache, int32_t n, size_t *bytes) {
   if (!bytes) return PCOMOE_ERR_INVALID_ARG;
   const pcomoe_status st = check_config(cfg, cache);
   if (st != PCOMOE_OK) return st;
-  *bytes = kWorkspace;
+  if (n < 0) return PCOMOE_ERR_INVALID_ARG;
+  if (n > cache->max_seqs) return PCOMOE_ERR_SHAPE;
+  *bytes = workspace_of(cfg, cache, n);
   return PCOMOE_OK;
 }
 
@@ -318,7 +324,7 @@ pcomoe_status pcomoe_cache_weigh(const pcomoe_attn_config *cfg, const pcomoe_cac
   const int64_t e = (int64_t)dtype_size(cfg->dtype);
   if (((uintptr_t)d_q & 15) || (q_stride * e) % 16) return PCOMOE_ERR_UNSUPPORTED;
   if ((int64_t)T * (cfg->q_heads / cfg->kv_heads) > INT32_MAX) return PCOMOE_ERR_SHAPE;
-  if (!d_workspace || ((uintptr_t)d_workspace & 255) || ws_bytes < kWorkspace) return PCOMOE_ERR_WORKSPACE;
+  if (!d_workspace || ((uintptr_t)d_workspace & 255) || ws_bytes < workspace_of(cfg, cache, n)) return PCOMOE_ERR_WORKSPACE;
   int sms;
   if ((st = current_sms(&sms)) != PCOMOE_OK) return st;
   WeighArgs a = {};
@@ -333,6 +339,9 @@ pcomoe_status pcomoe_cache_weigh(const pcomoe_attn_config *cfg, const pcomoe_cac
   a.weight = d_weight; a.weight_stride = weight_stride;
   a.status = (int32_t *)((char *)d_workspace + offsetof(DevPlan, status_router));
   a.limit_ns = wait_limit_ns();
+  // Many counted rows (columns, with the heads of a group) per sequence: the tensor-core kernel.
+  if (cfg->dtype == PCOMOE_BF16 && (int64_t)T * a.g >= (int64_t)kManyColumns * n)
+    return launch_weigh_tc(a, cfg->head_dim, (float *)((char *)d_workspace + 256), (int64_t)cache->max_pages * cache->page_size, sms, (cudaStream_t)stream);
   if (cfg->dtype == PCOMOE_BF16) return cfg->head_dim == 64 ? run<__nv_bfloat16, 64>(a, sms, (cudaStream_t)stream) : run<__nv_bfloat16, 128>(a, sms, (cudaStream_t)stream);
   return cfg->head_dim == 64 ? run<float, 64>(a, sms, (cudaStream_t)stream) : run<float, 128>(a, sms, (cudaStream_t)stream);
 }

@@ -1,5 +1,7 @@
 // What the kernels that weigh cached positions share: arguments and the sequences of a call.
 #pragma once
+#include <climits>
+
 #include "cache.cuh"
 
 namespace pcomoe {
@@ -19,6 +21,9 @@ struct WeighArgs {
   int32_t *status;
   uint64_t limit_ns;
 };
+
+pcomoe_status launch_weigh_tc(const WeighArgs &a, int head_dim, float *partial, int64_t room, int sms, cudaStream_t st);
+size_t weigh_tc_bytes(int hkv, int64_t room, int n);       // of partial sums of n listed sequences of up to `room` positions
 
 #ifdef __CUDACC__
 namespace {

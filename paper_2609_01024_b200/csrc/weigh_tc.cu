@@ -1,0 +1,538 @@
+// Weights of cached positions from many counted rows, bf16, on the tensor cores (tcgen05).
+//
+// Mathematics as in the kernel of few rows: w_p += sum over columns 2^(c q.k_p - c' lse); a column is a counted row and a query head.
+// A unit of work is 128 keys of one kv head: S^T = K Q^T with the keys as the accumulator's rows, so a position is a TMEM lane and one
+// thread's, its sum over the columns never leaves that thread, and the log sums are the same for all lanes (shared memory, one
+// broadcast load for four columns).  There is no second product and nothing is written back.
+//   warp 0: MMAs (128 keys x 128 columns a step), owner of TMEM     warps 1, 2: copies of keys and queries, log sums
+//   warp 3: finds the CTA's units                                   warps 4-7, 8-11: exponentials and sums of every other step
+// Four accumulators of 128 columns fill TMEM, the queries come through four stages, the keys of the next unit into a second
+// buffer while this one is worked on.  Queries are copied with 16-byte asynchronous copies, not as boxes, since counted rows may
+// be any of the packed ones and a group of heads need not divide a tile.
+// Units leave partial sums, one for each head (or each share of a head's columns, where there are fewer than 8 heads), which a
+// second launch adds in order: no atomics, and the bits do not depend on which CTA took which unit.  CTAs take units from both
+// ends of rounds of the grid's size in turn, so that in a prompt, whose later keys are seen by fewer rows, all get the same work.
+//
+// What bounds it: the special function unit, 16 exponentials per clock and SM: 1024 clocks a step, in which the tensor cores work 512.
+#include <algorithm>
+
+#include "tc_ptx.cuh"
+#include "weigh.cuh"
+
+namespace pcomoe {
+namespace {
+
+constexpr int BK_ROWS = 128, BC = 128;          // keys of a unit, columns of a step
+constexpr int kThreads = 384, kFirst = 128;
+constexpr int kSumRegs = 208, kOtherRegs = 88, kLaunchRegs = 168;
+static_assert(256 * kSumRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs, "register split");
+constexpr int kStages = 4, kBuffers = 4, kSlots = 16;      // of queries, of accumulators, of log sums
+// A slot of log sums is filled again 16 steps later.  By then its step is done: the copies run at most kStages steps ahead of the
+// MMAs, these at most kBuffers ahead of the sums, and a warp group takes a step only after its last one.
+
+template <int D> struct Shape {
+  static constexpr int kHalves = D / 64;
+  static constexpr int kHalfBytes = 128 * 128;
+  static constexpr int kTileBytes = kHalves * kHalfBytes;
+  static constexpr int kSmem = (kStages + 2) * kTileBytes;
+};
+
+struct Unit {
+  WeighSeq seq;
+  int list, head, part;
+  int p0;               // first key; -1: no more work
+  int first, steps;     // column tile of the first step, and their number; tiles are `parts` apart
+};
+
+struct TcArgs {
+  WeighArgs w;
+  float *partial;       // [n][hkv * parts][room]
+  int64_t room;
+  int32_t parts;
+};
+
+__device__ __forceinline__ bool elect_lane() {
+  uint32_t e;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
+  return e;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
+               "l"(b), "r"(idesc), "r"(acc)
+               : "memory");
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  uint64_t d;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(*(uint64_t *)&a), "l"(*(uint64_t *)&b), "l"(*(uint64_t *)&c));
+  return *(float2 *)&d;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*(uint64_t *)&a), "l"(*(uint64_t *)&b));
+  return *(float2 *)&d;
+}
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map),
+               "r"(x), "r"(y), "r"(z), "r"(bar)
+               : "memory");
+}
+
+// The units of a call, in one line: sequence, keys, head and part, the last fastest.  One warp.
+struct Line {
+  int s0;               // sequences s0 + lane are in hand
+  int64_t before;       // units before them
+  WeighSeq mine;
+  int64_t upto;
+  bool held;
+
+  __device__ __forceinline__ void hold(const TcArgs &a, const uint32_t *twice) {
+    const int lane = threadIdx.x & 31;
+    mine = {};
+    if (s0 + lane < a.w.n) mine = weigh_seq(a.w, s0 + lane, twice);
+    upto = (int64_t)((mine.len + BK_ROWS - 1) / BK_ROWS) * (a.w.hkv * a.parts);
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(~0u, upto, o);
+      if (lane >= o) upto += y;
+    }
+    held = true;
+  }
+  // unit u, no smaller than any asked for before
+  __device__ __forceinline__ void get(const TcArgs &a, const uint32_t *twice, int64_t u, Unit &it) {
+    it.p0 = -1;
+    while (s0 < a.w.n) {
+      if (!held) hold(a, twice);
+      const uint32_t hit = __ballot_sync(~0u, before + upto > u);
+      if (hit) {
+        const int l = __ffs(hit) - 1;
+        const int64_t upto_l = __shfl_sync(~0u, upto, l);
+        const int lanes_len = __shfl_sync(~0u, mine.len, l), P = a.w.hkv * a.parts;
+        const int64_t count = (int64_t)((lanes_len + BK_ROWS - 1) / BK_ROWS) * P, at = u - (before + upto_l - count);
+        it.seq.q0 = __shfl_sync(~0u, mine.q0, l);
+        it.seq.n = __shfl_sync(~0u, mine.n, l);
+        it.seq.m = __shfl_sync(~0u, mine.m, l);
+        it.seq.len = lanes_len;
+        it.seq.base = it.seq.len - it.seq.m;
+        it.seq.id = __shfl_sync(~0u, mine.id, l);
+        it.list = s0 + l;
+        const int r = (int)(at % P);
+        it.head = r % a.w.hkv;
+        it.part = r / a.w.hkv;
+        it.p0 = (int)(at / P) * BK_ROWS;
+        const int64_t cols = (int64_t)it.seq.m * a.w.g, from = (int64_t)max(0, it.p0 - it.seq.base) * a.w.g;
+        const int tiles = (int)((cols + BC - 1) / BC);
+        it.first = (int)(from / BC) + it.part;
+        it.steps = max(0, (tiles - it.first + a.parts - 1) / a.parts);
+        return;
+      }
+      before += __shfl_sync(~0u, upto, 31);
+      s0 += 32;
+      held = false;
+    }
+  }
+};
+
+// kBoxes: all packed rows are counted and a tile holds whole rows, so a tile of queries is one box per 64 columns of the head.
+template <int D, bool kBoxes>
+__global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ TcArgs a) {
+  using S = Shape<D>;
+  constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+  constexpr int C = D / 8, kSide = 32 / C;                // 16-byte pieces of a row; rows that a warp copies side by side
+  extern __shared__ __align__(1024) uint8_t smem[];
+  __shared__ __align__(8) uint64_t s_qfull[kStages], s_qempty[kStages], s_kfull[2], s_kempty[2], s_sfull[kBuffers], s_sempty[kBuffers], s_lfull[kSlots], s_ifull[2],
+      s_iempty[2], s_join[2];
+  __shared__ Unit s_item[2];
+  __shared__ __align__(16) float s_lse[kSlots][BC];
+  __shared__ __align__(16) int s_lim[kSlots][BC];
+  __shared__ int s_least[kSlots][2];                      // the smallest limit of either half of a step's columns
+  __shared__ int64_t s_at[2][64];                         // of the copying warps: where rows are, -1: nowhere
+  __shared__ float s_sum[2][BK_ROWS];
+  __shared__ uint32_t s_bits[2 * (kMaxSeqs / 32)];
+  __shared__ uint32_t s_tmem;
+  __shared__ int s_flags[2];
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t q_at = smem_u32(smem), k_at = q_at + kStages * S::kTileBytes;
+  volatile int *flags = s_flags;
+
+  if (tid == 0) {
+    s_flags[0] = q_at & 1023 ? 1 : 0;                     // the swizzle needs it
+    s_flags[1] = 0;
+    for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&s_qfull[i]), 2); mbar_init(smem_u32(&s_qempty[i]), 1); }
+    for (int i = 0; i < kBuffers; ++i) { mbar_init(smem_u32(&s_sfull[i]), 1); mbar_init(smem_u32(&s_sempty[i]), 4); }
+    for (int i = 0; i < kSlots; ++i) mbar_init(smem_u32(&s_lfull[i]), 2);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(smem_u32(&s_kfull[i]), 2);
+      mbar_init(smem_u32(&s_kempty[i]), 1);
+      mbar_init(smem_u32(&s_ifull[i]), 1);
+      mbar_init(smem_u32(&s_iempty[i]), 11);              // every warp but the one that fills them
+      mbar_init(smem_u32(&s_join[i]), 4);
+    }
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 0) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&s_tmem)), "r"(512) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = s_tmem;
+  pdl_grid_wait();
+  const uint32_t *twice = find_repeats(a.w.seqs, a.w.n, a.w.max_seqs, s_bits);
+
+  uint32_t n_item = 0, step = 0;                          // units and steps so far
+  auto item_ready = [&](bool ok) { return __all_sync(~0u, ok && wait_bar(&s_ifull[n_item & 1], (n_item >> 1) & 1, flags, a.w.limit_ns)); };
+  auto item_done = [&]() {
+    __syncwarp();
+    if (lane == 0) mbar_arrive(smem_u32(&s_iempty[n_item & 1]));
+    ++n_item;
+  };
+  if (warp >= kFirst / 32) {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSumRegs));
+    const int group = (warp - kFirst / 32) >> 2, key = (warp & 3) * 32 + lane;
+    const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+    const float scale = a.w.scale_log2;
+    bool ok = true;
+    uint32_t n_unit = 0;
+    while (item_ready(ok)) {
+      const Unit &it = s_item[n_item & 1];
+      if (it.p0 < 0) break;
+      const int p = it.p0 + key, last = it.p0 + BK_ROWS - 1, steps = it.steps, len = it.seq.len;
+      float total = 0.f;
+      for (int i = 0; i < steps; ++i) {
+        const uint32_t at = step + i, b = at % kBuffers, slot = at % kSlots;
+        if ((int)(at & 1) != group) continue;
+        if (ok) ok = wait_bar(&s_sfull[b], (at / kBuffers) & 1, flags, a.w.limit_ns) && wait_bar(&s_lfull[slot], (at / kSlots) & 1, flags, a.w.limit_ns);
+        __syncwarp();
+        tc_fence_after();
+        uint32_t x[4][32];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) tmem_ld32_issue(tmem + b * BC + 32 * c + lanes, x[c]);
+        tmem_wait_ld();
+#pragma unroll
+        for (int c = 0; c < 4; ++c) reg_fence32(x[c]);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&s_sempty[b]));
+        float2 sum[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        const float2 scale2 = make_float2(scale, scale);
+        const bool masked = last > min(s_least[slot][0], s_least[slot][1]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+#pragma unroll
+          for (int k = 0; k < 32; k += 4) {
+            const float4 l = *(const float4 *)&s_lse[slot][32 * c + k];          // minus the log sum
+            float2 e = fma2(make_float2(__uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1])), scale2, make_float2(l.x, l.y));
+            float2 f = fma2(make_float2(__uint_as_float(x[c][k + 2]), __uint_as_float(x[c][k + 3])), scale2, make_float2(l.z, l.w));
+            e = make_float2(exp2_fast(e.x), exp2_fast(e.y));
+            f = make_float2(exp2_fast(f.x), exp2_fast(f.y));
+            if (masked) {                                  // chosen, not multiplied
+              const int4 m = *(const int4 *)&s_lim[slot][32 * c + k];
+              e = make_float2(p <= m.x ? e.x : 0.f, p <= m.y ? e.y : 0.f);
+              f = make_float2(p <= m.z ? f.x : 0.f, p <= m.w ? f.y : 0.f);
+            }
+            sum[(k >> 2) & 1] = add2(sum[(k >> 2) & 1], e);
+            sum[2 + ((k >> 2) & 1)] = add2(sum[2 + ((k >> 2) & 1)], f);
+          }
+        }
+        const float2 s = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
+        total += s.x + s.y;
+      }
+      step += steps;
+      // the second group hands its sums to the first.  (It gets to the unit after the next, which takes the same place and barrier,
+      // only when both are done with this one.)
+      if (group) {
+        s_sum[n_unit & 1][key] = total;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&s_join[n_unit & 1]));
+      } else {
+        if (ok) ok = wait_bar(&s_join[n_unit & 1], (n_unit >> 1) & 1, flags, a.w.limit_ns);
+        __syncwarp();
+        if (p < len) a.partial[((int64_t)it.list * (a.w.hkv * a.parts) + it.part * a.w.hkv + it.head) * a.room + p] = total + s_sum[n_unit & 1][key];
+      }
+      ++n_unit;
+      item_done();
+    }
+  } else {
+  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
+  if (warp == 1 || warp == 2) {
+    // ---- copies: keys of a unit, then the columns of its steps; each of the two warps takes 64 rows.  Up to two copies are under way
+    // before the oldest is waited for and handed on.
+    const int half = warp - 1;
+    uint64_t *wait0[2] = {nullptr, nullptr}, *wait1[2] = {nullptr, nullptr};       // barriers of the copies under way, oldest last
+    bool ok = true;
+    uint32_t n_k = 0;
+    auto hand_on = [&](int i) {
+      if (!wait0[i]) return;
+      if (lane == 0) {
+        mbar_arrive(smem_u32(wait0[i]));
+        if (wait1[i]) mbar_arrive(smem_u32(wait1[i]));
+      }
+      wait0[i] = nullptr;
+    };
+    auto flush = [&]() {
+      if (!wait0[0] && !wait0[1]) return;
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      hand_on(1);
+      hand_on(0);
+    };
+    auto begun = [&](uint64_t *b0, uint64_t *b1) {
+      asm volatile("cp.async.commit_group;" ::: "memory");
+      if (wait0[1]) {
+        asm volatile("cp.async.wait_group 2;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        hand_on(1);
+      }
+      wait0[1] = wait0[0]; wait1[1] = wait1[0];
+      wait0[0] = b0; wait1[0] = b1;
+    };
+    auto wait = [&](uint64_t *bar, uint32_t parity) {
+      if (!__all_sync(~0u, probe_bar(smem_u32(bar), parity))) {
+        flush();                                           // nobody waits for a copy that waits for this
+        ok = __all_sync(~0u, ok && wait_bar(bar, parity, flags, a.w.limit_ns));
+      }
+      return ok;
+    };
+    // 64 rows whose places are in s_at, to rows half * 64 .. of the tile at `to`
+    auto copy_rows = [&](const void *base, uint32_t to) {
+      const int c = lane % C;
+      const uint32_t dst = to + (c >> 3) * S::kHalfBytes;
+#pragma unroll 8
+      for (int r0 = 0; r0 < 64; r0 += kSide) {
+        const int r = r0 + lane / C, row = half * 64 + r;
+        const int64_t at = s_at[half][r];
+        copy16(dst + row * 128 + (((c & 7) ^ (row & 7)) << 4), (const __nv_bfloat16 *)base + (at < 0 ? 0 : at) + c * 8, at >= 0);
+      }
+    };
+    for (; item_ready(ok); item_done()) {
+      const Unit it = s_item[n_item & 1];
+      if (it.p0 < 0) break;
+      if (it.steps == 0) continue;
+      if (!wait(&s_kempty[n_k & 1], ((n_k >> 1) & 1) ^ 1)) break;
+      const int32_t *table = a.w.table + (int64_t)it.seq.id * a.w.max_pages;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int r = 32 * j + lane, p = it.p0 + half * 64 + r;
+        s_at[half][r] = p < it.seq.len ? (weigh_page_row(a.w, table, p) + (int64_t)it.head * a.w.page) * D : -1;
+      }
+      __syncwarp();
+      copy_rows(a.w.k, k_at + (n_k & 1) * S::kTileBytes);
+      __syncwarp();
+      begun(&s_kfull[n_k & 1], nullptr);
+      ++n_k;
+      if (kBoxes) {
+        // the first warp sends for the queries; the second has the log sums, a step ahead of their use
+        const int cols = it.seq.m * a.w.g;
+        float lse[4], following[4];
+        auto fetch = [&](int i, float (&to)[4]) {
+          const int c0 = (it.first + i * a.parts) * BC + 4 * lane;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int col = c0 + j, k = col / a.w.g;
+            to[j] = i < it.steps && col < cols ? a.w.lse[(int64_t)(it.seq.q0 + k) * a.w.hq + it.head * a.w.g + col - k * a.w.g] : -INFINITY;
+          }
+        };
+        if (half) fetch(0, lse);
+        for (int i = 0; i < it.steps; ++i, ++step) {
+          const uint32_t st = step % kStages, slot = step % kSlots;
+          const int c0 = (it.first + i * a.parts) * BC;
+          if (half) fetch(i + 1, following);
+          if (!wait(&s_qempty[st], ((step / kStages) & 1) ^ 1)) break;
+          if (!half) {
+            if (lane == 0) {
+              mbar_arrive_expect_tx(smem_u32(&s_qfull[st]), S::kTileBytes);
+              mbar_arrive(smem_u32(&s_lfull[slot]));
+#pragma unroll
+              for (int h = 0; h < S::kHalves; ++h)
+                tma_load_3d(q_at + st * S::kTileBytes + h * S::kHalfBytes, &q_map, h * 64, it.head * a.w.g, it.seq.q0 + c0 / a.w.g, smem_u32(&s_qfull[st]));
+            }
+            __syncwarp();
+          } else {
+            int lim[4], least = INT32_MAX;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              lim[j] = lse[j] != -INFINITY ? it.seq.base + (c0 + 4 * lane + j) / a.w.g : -1;
+              least = min(least, lim[j]);
+              lse[j] = lim[j] >= 0 ? -lse[j] * kLog2ef : 0.f;
+            }
+            *(float4 *)&s_lse[slot][4 * lane] = make_float4(lse[0], lse[1], lse[2], lse[3]);
+            *(int4 *)&s_lim[slot][4 * lane] = make_int4(lim[0], lim[1], lim[2], lim[3]);
+            least = __reduce_min_sync(~0u, least);
+            if (lane < 2) s_least[slot][lane] = least;
+            __syncwarp();
+            if (lane == 0) {
+              mbar_arrive(smem_u32(&s_qfull[st]));
+              mbar_arrive(smem_u32(&s_lfull[slot]));
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) lse[j] = following[j];
+          }
+          if (i == 0) flush();                             // the keys, while the first queries come in
+        }
+      } else
+      for (int i = 0; i < it.steps; ++i, ++step) {
+        const uint32_t st = step % kStages, slot = step % kSlots;
+        if (!wait(&s_qempty[st], ((step / kStages) & 1) ^ 1)) break;
+        const int64_t c0 = (int64_t)(it.first + i * a.parts) * BC + half * 64, cols = (int64_t)it.seq.m * a.w.g;
+        int least = INT32_MAX;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const int r = 32 * j + lane;
+          const int64_t col = c0 + r;
+          int64_t at = -1;
+          float lse = 0.f;
+          int lim = -1;
+          if (col < cols) {
+            const int k = (int)col / a.w.g, head = it.head * a.w.g + (int)col - k * a.w.g, row = counted_row(a.w, it.seq, it.list, k);
+            if (row >= 0) {
+              at = row * a.w.q_stride + (int64_t)head * D;
+              lse = a.w.lse[(int64_t)row * a.w.hq + head];
+              if (lse != -INFINITY) lim = it.seq.base + k;
+            }
+          }
+          s_at[half][r] = at;
+          s_lse[slot][half * 64 + r] = lim >= 0 ? -lse * kLog2ef : 0.f;
+          s_lim[slot][half * 64 + r] = lim;
+          least = min(least, lim);
+        }
+        least = __reduce_min_sync(~0u, least);
+        if (lane == 0) s_least[slot][half] = least;
+        __syncwarp();
+        copy_rows(a.w.q, q_at + st * S::kTileBytes);
+        __syncwarp();
+        begun(&s_qfull[st], &s_lfull[slot]);
+      }
+      if (!ok) break;
+    }
+    flush();
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  } else if (warp == 0) {
+    // ---- MMAs; the whole warp walks along, one lane issues
+    bool ok = true;
+    uint32_t n_k = 0;
+    auto wait = [&](uint64_t *bar, uint32_t p) { return ok = __all_sync(~0u, wait_bar(bar, p, flags, a.w.limit_ns)); };
+    const uint64_t q_desc = umma_desc(q_at), k_desc = umma_desc(k_at);
+    for (; item_ready(ok); item_done()) {
+      const int p0 = s_item[n_item & 1].p0, steps = s_item[n_item & 1].steps;
+      if (p0 < 0) break;
+      if (steps == 0) continue;
+      if (!wait(&s_kfull[n_k & 1], (n_k >> 1) & 1)) break;
+      const uint64_t da = k_desc + (uint64_t)((n_k & 1) * (S::kTileBytes >> 4));
+      for (int i = 0; i < steps; ++i, ++step) {
+        const uint32_t st = step % kStages, b = step % kBuffers;
+        if (!wait(&s_sempty[b], ((step / kBuffers) & 1) ^ 1)) break;
+        if (!wait(&s_qfull[st], (step / kStages) & 1)) break;
+        tc_fence_after();
+        const uint64_t db = q_desc + (uint64_t)(st * (S::kTileBytes >> 4));
+        if (elect_lane()) {
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            const uint64_t off = (uint64_t)((k >> 2) * (S::kHalfBytes >> 4) + (k & 3) * 2);
+            mma_ss(tmem + b * BC, da + off, db + off, kIdesc, k != 0);
+          }
+          umma_commit(smem_u32(&s_sfull[b]));
+          umma_commit(smem_u32(&s_qempty[st]));
+          if (i == steps - 1) umma_commit(smem_u32(&s_kempty[n_k & 1]));
+        }
+        __syncwarp();
+      }
+      if (!ok) break;
+      ++n_k;
+    }
+  } else {
+    // ---- the units: from both ends of rounds of two grids
+    Line line = {0, 0, {}, 0, false};
+    for (uint32_t r = 0;; ++r, ++n_item) {
+      Unit it = {};
+      const int64_t u = (int64_t)r * gridDim.x + (r & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+      line.get(a, twice, u, it);
+      if (!__all_sync(~0u, wait_bar(&s_iempty[n_item & 1], ((n_item >> 1) & 1) ^ 1, flags, a.w.limit_ns))) break;
+      if (lane == 0) {
+        s_item[n_item & 1] = it;
+        mbar_arrive(smem_u32(&s_ifull[n_item & 1]));
+      }
+      __syncwarp();
+      if (it.p0 < 0) break;
+    }
+  }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (s_flags[0]) timeout_record_and_drain(a.w.status);
+  __syncthreads();
+  if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
+}
+
+// Partial sums added in order.  blockIdx.y: sequences, a grid's height apart.
+__global__ void __launch_bounds__(256) weigh_join_kernel(const __grid_constant__ TcArgs a) {
+  __shared__ uint32_t s_bits[2 * (kMaxSeqs / 32)];
+  pdl_grid_wait();
+  const uint32_t *twice = find_repeats(a.w.seqs, a.w.n, a.w.max_seqs, s_bits);
+  const int P = a.w.hkv * a.parts;
+  for (int i = blockIdx.y; i < a.w.n; i += gridDim.y) {
+    const WeighSeq s = weigh_seq(a.w, i, twice);
+    float *w = a.w.weight + s.id * a.w.weight_stride;
+    const float *part = a.partial + (int64_t)i * P * a.room;
+    for (int p = blockIdx.x * 256 + threadIdx.x; p < s.len; p += gridDim.x * 256) {
+      float sum = 0.f;
+#pragma unroll 8
+      for (int r = 0; r < P; ++r) sum += part[r * a.room + p];
+      w[p] = a.w.fresh && p >= s.base ? sum : w[p] + sum;
+    }
+  }
+}
+
+template <int D, bool kBoxes>
+pcomoe_status run(const CUtensorMap &q_map, const TcArgs &a, int sms, cudaStream_t st) {
+  static PerDeviceOnce once;
+  int dev = -1;
+  PCOMOE_CUDA_TRY(cudaGetDevice(&dev));
+  if (once.first_use(dev)) {
+    // the register split draws on what the block was launched with: with fewer the larger share would never come
+    cudaFuncAttributes at;
+    PCOMOE_CUDA_TRY(cudaFuncGetAttributes(&at, weigh_tc_kernel<D, kBoxes>));
+    if (at.numRegs < kLaunchRegs) return PCOMOE_ERR_CUDA;
+    PCOMOE_CUDA_TRY(cudaFuncSetAttribute(weigh_tc_kernel<D, kBoxes>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem));
+    once.done(dev);
+  }
+  PCOMOE_CUDA_TRY(launch_pdl(weigh_tc_kernel<D, kBoxes>, dim3(sms), dim3(kThreads), Shape<D>::kSmem, st, q_map, a));
+  const unsigned wide = (unsigned)std::max<int64_t>(1, std::min<int64_t>((a.room + 1023) / 1024, 4 * sms));
+  PCOMOE_CUDA_TRY(launch_pdl(weigh_join_kernel, dim3(wide, (unsigned)std::min(a.w.n, 65535)), dim3(256), 0, st, a));
+  count_launch(2);
+  return PCOMOE_OK;
+}
+
+// Shares of a head's columns: enough units where there are few heads.
+int parts_of(int hkv) { return hkv >= 8 ? 1 : 8 / hkv; }
+
+}  // namespace
+
+size_t weigh_tc_bytes(int hkv, int64_t room, int n) { return sizeof(float) * (size_t)n * (size_t)(hkv * parts_of(hkv)) * (size_t)room; }
+
+pcomoe_status launch_weigh_tc(const WeighArgs &w, int D, float *partial, int64_t room, int sms, cudaStream_t st) {
+  TcArgs a = {};
+  a.w = w;
+  a.partial = partial;
+  a.room = room;
+  a.parts = parts_of(w.hkv);
+  CUtensorMap q = {};
+  if (w.n_keep || BC % w.g) return D == 64 ? run<64, false>(q, a, sms, st) : run<128, false>(q, a, sms, st);
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return PCOMOE_ERR_CUDA;
+  cuuint64_t dims[3] = {(cuuint64_t)D, (cuuint64_t)w.hq, (cuuint64_t)w.T}, strides[2] = {(cuuint64_t)D * 2, (cuuint64_t)w.q_stride * 2};
+  cuuint32_t box[3] = {BK, (cuuint32_t)w.g, (cuuint32_t)(BC / w.g)}, estr[3] = {1, 1, 1};
+  if (fn(&q, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(w.q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+         CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+    return PCOMOE_ERR_CUDA;
+  return D == 64 ? run<64, true>(q, a, sms, st) : run<128, true>(q, a, sms, st);
+}
+
+}  // namespace pcomoe

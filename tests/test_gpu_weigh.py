@@ -213,3 +213,67 @@ def test_after_attention():
     total = c.weights.weight.double().sum(1).cpu().numpy()
     # every term of a row has the same relative error of its log sum (|lse| up to 60: 60 * 2^-23) and its own of its score
     assert np.allclose(total, [3 * hq, 200 * hq], rtol=2e-5)
+
+
+@pytest.mark.parametrize("hq,hkv,d,page,ctx,add", [(32, 8, 128, 64, [0], [700]), (8, 8, 64, 16, [130, 0, 1000], [257, 128, 90]), (28, 4, 128, 32, [5], [300]), (6, 2, 128, 128, [0, 0, 0, 60], [200, 0, 1, 333]),
+                                                   (4, 1, 64, 16, [2000], [150]), (10, 10, 128, 16, [77], [129]), (7, 1, 128, 64, [0], [1000])])
+def test_many_rows(hq, hkv, d, page, ctx, add):
+    """Column tiles that groups of heads do not divide, units without columns, more steps than there are places for log sums."""
+    c = Case("bf16", hq, hkv, d, page, ctx, add, seed=hq + d, behind=5)
+    c.check()
+    c.check(fresh=False)
+
+
+def test_many_kept_rows():
+    """Lists of many rows, some numbers left out, beside sequences with none."""
+    rng = np.random.default_rng(1)
+    kept = [sorted(rng.permutation(400)[:300].tolist()), [], [0, 2], list(range(150))]
+    Case("bf16", 8, 2, 128, 32, [40, 30, 0, 500], [400, 3, 3, 150], kept, seed=2, order=[3, 2, 1, 0]).check()
+
+
+def test_many_rows_spoiled():
+    """In the tensor-core kernel too a key spoils its own position alone and rows that saw nothing, or are no rows, add nothing."""
+    c = Case("bf16", 8, 2, 128, 16, [50], [300], seed=13)
+    clean = c.weights.weight.clone()
+    c.add_up()
+    want, c.weights.weight[:] = c.weights.weight.clone(), clean
+    page = lambda p: (0, int(c.cache.page_table[0, p // 16]), 0, p % 16)
+    c.cache.k[page(7)] = float("nan")
+    c.cache.k[page(349)] = float("nan")
+    c.cache.k[page(200)] = float("inf")
+    c.add_up()
+    got = c.weights.weight
+    spoiled = torch.isnan(got[0]) | torch.isinf(got[0]) | (got[0] != want[0])
+    assert spoiled.nonzero().flatten().tolist() == [7, 200, 349]
+    c.weights.weight[:] = clean
+    for p in (7, 200, 349):
+        c.cache.k[page(p)] = 1.0
+    c.q[10] = float("nan")                      # a row that saw nothing, whatever it holds
+    c.lse[10] = float("-inf")
+    c.add_up()
+    assert torch.isfinite(c.weights.weight).all()
+    rows = torch.arange(300, device="cuda") != 10
+    keep = ints([[i if i != 10 else 1000 for i in range(300)]])
+    c.weights.weight[:] = clean
+    c.weights.add(c.q, c.lse, 0, ints([0]), ints([0, 300]), keep=keep, n_keep=ints([300]), fresh=True)
+    assert c.weights.device_status() == 7 and torch.isfinite(c.weights.weight).all()
+
+
+def test_many_rows_bits_and_graph():
+    c = Case("bf16", 16, 4, 128, 64, [300, 0], [200, 400], seed=14)
+    before = c.weights.weight.clone()
+    c.add_up()
+    want = c.weights.weight.clone()
+    args = (c.q, c.lse, 0, ints([0, 1]), ints([0, 200, 600]))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            c.weights.add(*args, fresh=True)
+        for _ in range(5):
+            c.weights.weight.copy_(before)
+            graph.replay()
+            assert torch.equal(c.weights.weight, want)
+    side.synchronize()
+    assert c.weights.device_status() == 0
