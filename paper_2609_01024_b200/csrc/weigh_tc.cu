@@ -15,6 +15,7 @@
 //
 // What bounds it: the special function unit, 16 exponentials per clock and SM: 1024 clocks a step, in which the tensor cores work 512.
 #include <algorithm>
+#include <type_traits>
 
 #include "tc_ptx.cuh"
 #include "weigh.cuh"
@@ -220,25 +221,29 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
         if (lane == 0) mbar_arrive(smem_u32(&s_sempty[b]));
         float2 sum[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
         const float2 scale2 = make_float2(scale, scale);
-        const bool masked = last > min(s_least[slot][0], s_least[slot][1]);
+        // (two loops, so that the one without a mask is one stretch of code: with the question inside of it a step took twice as long)
+        const auto sums = [&](auto masked) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
+          for (int c = 0; c < 4; ++c) {
 #pragma unroll
-          for (int k = 0; k < 32; k += 4) {
-            const float4 l = *(const float4 *)&s_lse[slot][32 * c + k];          // minus the log sum
-            float2 e = fma2(make_float2(__uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1])), scale2, make_float2(l.x, l.y));
-            float2 f = fma2(make_float2(__uint_as_float(x[c][k + 2]), __uint_as_float(x[c][k + 3])), scale2, make_float2(l.z, l.w));
-            e = make_float2(exp2_fast(e.x), exp2_fast(e.y));
-            f = make_float2(exp2_fast(f.x), exp2_fast(f.y));
-            if (masked) {                                  // chosen, not multiplied
-              const int4 m = *(const int4 *)&s_lim[slot][32 * c + k];
-              e = make_float2(p <= m.x ? e.x : 0.f, p <= m.y ? e.y : 0.f);
-              f = make_float2(p <= m.z ? f.x : 0.f, p <= m.w ? f.y : 0.f);
+            for (int k = 0; k < 32; k += 4) {
+              const float4 l = *(const float4 *)&s_lse[slot][32 * c + k];        // minus the log sum
+              float2 e = fma2(make_float2(__uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1])), scale2, make_float2(l.x, l.y));
+              float2 f = fma2(make_float2(__uint_as_float(x[c][k + 2]), __uint_as_float(x[c][k + 3])), scale2, make_float2(l.z, l.w));
+              e = make_float2(exp2_fast(e.x), exp2_fast(e.y));
+              f = make_float2(exp2_fast(f.x), exp2_fast(f.y));
+              if (masked.value) {                          // chosen, not multiplied
+                const int4 m = *(const int4 *)&s_lim[slot][32 * c + k];
+                e = make_float2(p <= m.x ? e.x : 0.f, p <= m.y ? e.y : 0.f);
+                f = make_float2(p <= m.z ? f.x : 0.f, p <= m.w ? f.y : 0.f);
+              }
+              sum[(k >> 2) & 1] = add2(sum[(k >> 2) & 1], e);
+              sum[2 + ((k >> 2) & 1)] = add2(sum[2 + ((k >> 2) & 1)], f);
             }
-            sum[(k >> 2) & 1] = add2(sum[(k >> 2) & 1], e);
-            sum[2 + ((k >> 2) & 1)] = add2(sum[2 + ((k >> 2) & 1)], f);
           }
-        }
+        };
+        if (last > min(s_least[slot][0], s_least[slot][1])) sums(std::true_type());
+        else sums(std::false_type());
         const float2 s = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
         total += s.x + s.y;
       }
@@ -328,22 +333,24 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
       begun(&s_kfull[n_k & 1], nullptr);
       ++n_k;
       if (kBoxes) {
-        // the first warp sends for the queries; the second has the log sums, a step ahead of their use
-        const int cols = it.seq.m * a.w.g;
-        float lse[4], following[4];
+        // the first warp sends for the queries; the second has the log sums on their way kAhead steps before they are used
+        constexpr int kAhead = 3;
+        const int cols = it.seq.m * a.w.g, gs = __ffs(a.w.g) - 1;          // a tile holds whole rows: g is a power of 2
+        float ahead[kAhead][4];
         auto fetch = [&](int i, float (&to)[4]) {
           const int c0 = (it.first + i * a.parts) * BC + 4 * lane;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const int col = c0 + j, k = col / a.w.g;
-            to[j] = i < it.steps && col < cols ? a.w.lse[(int64_t)(it.seq.q0 + k) * a.w.hq + it.head * a.w.g + col - k * a.w.g] : -INFINITY;
+            const int col = c0 + j, k = col >> gs;
+            to[j] = i < it.steps && col < cols ? a.w.lse[(int64_t)(it.seq.q0 + k) * a.w.hq + (it.head << gs) + col - (k << gs)] : -INFINITY;
           }
         };
-        if (half) fetch(0, lse);
+        if (half)
+#pragma unroll
+          for (int k = 0; k < kAhead; ++k) fetch(k, ahead[k]);
         for (int i = 0; i < it.steps; ++i, ++step) {
           const uint32_t st = step % kStages, slot = step % kSlots;
           const int c0 = (it.first + i * a.parts) * BC;
-          if (half) fetch(i + 1, following);
           if (!wait(&s_qempty[st], ((step / kStages) & 1) ^ 1)) break;
           if (!half) {
             if (lane == 0) {
@@ -351,14 +358,22 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
               mbar_arrive(smem_u32(&s_lfull[slot]));
 #pragma unroll
               for (int h = 0; h < S::kHalves; ++h)
-                tma_load_3d(q_at + st * S::kTileBytes + h * S::kHalfBytes, &q_map, h * 64, it.head * a.w.g, it.seq.q0 + c0 / a.w.g, smem_u32(&s_qfull[st]));
+                tma_load_3d(q_at + st * S::kTileBytes + h * S::kHalfBytes, &q_map, h * 64, it.head << gs, it.seq.q0 + (c0 >> gs), smem_u32(&s_qfull[st]));
             }
             __syncwarp();
           } else {
+            float lse[4];
             int lim[4], least = INT32_MAX;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              lim[j] = lse[j] != -INFINITY ? it.seq.base + (c0 + 4 * lane + j) / a.w.g : -1;
+              lse[j] = ahead[0][j];
+#pragma unroll
+              for (int k = 0; k + 1 < kAhead; ++k) ahead[k][j] = ahead[k + 1][j];
+            }
+            fetch(i + kAhead, ahead[kAhead - 1]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              lim[j] = lse[j] != -INFINITY ? it.seq.base + ((c0 + 4 * lane + j) >> gs) : -1;
               least = min(least, lim[j]);
               lse[j] = lim[j] >= 0 ? -lse[j] * kLog2ef : 0.f;
             }
@@ -371,8 +386,6 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
               mbar_arrive(smem_u32(&s_qfull[st]));
               mbar_arrive(smem_u32(&s_lfull[slot]));
             }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) lse[j] = following[j];
           }
           if (i == 0) flush();                             // the keys, while the first queries come in
         }
