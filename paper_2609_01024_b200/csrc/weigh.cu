@@ -22,7 +22,14 @@ constexpr int kWarps = 8, kThreads = 32 * kWarps, kKeys = 16;
 constexpr int kItems = 32;              // pieces of 16 keys of a head in a block of keys, about
 constexpr int kMaxSubs = 16;            // pieces of 16 keys of one head in it
 constexpr int kQBytes = 48 * 1024;      // queries held at a time
-constexpr int kManyColumns = 96;        // of a sequence on average, from which on the tensor-core kernel is taken
+// From this many columns (counted rows x heads of a group) of a sequence on, on average, the tensor-core kernel is taken.  Both, us, with 32
+// heads on 8 of 128 and so many counted rows a sequence (4 columns each), this one and the other:
+//   rows                       1          8           16          32          128
+//   64 sequences of 512    23.5, 69.9  49.5, 70.9   83, 71.0   161, 69.9   878, 109
+//   32 sequences of 4096   63.4, 192    132, 193    220, 193   418, 182   1659, 278
+//   4 sequences of 16384   38.3, 106   80.9, 107    136, 107   266, 98.7   898, 144
+//   8 sequences of 300     14.6, 18.7  28.9, 18.9  41.2, 19.5  86.2, 18.7  321, 24.8
+constexpr int kManyColumns = 64;
 constexpr int kExtra = 2;               // cost of a block of keys besides its columns, in tiles of 8 columns
 
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {

@@ -4,16 +4,22 @@
 // A unit of work is 128 keys of one kv head: S^T = K Q^T with the keys as the accumulator's rows, so a position is a TMEM lane and one
 // thread's, its sum over the columns never leaves that thread, and the log sums are the same for all lanes (shared memory, one
 // broadcast load for four columns).  There is no second product and nothing is written back.
-//   warp 0: MMAs (128 keys x 128 columns a step), owner of TMEM     warps 1, 2: copies of keys and queries, log sums
-//   warp 3: finds the CTA's units                                   warps 4-7, 8-11: exponentials and sums of every other step
-// Four accumulators of 128 columns fill TMEM, the queries come through four stages, the keys of the next unit into a second
-// buffer while this one is worked on.  Queries are copied with 16-byte asynchronous copies, not as boxes, since counted rows may
-// be any of the packed ones and a group of heads need not divide a tile.
+//   warp 0: MMAs (128 keys x 128 columns a step), owner of TMEM     warps 1, 2: queries and log sums of the steps
+//   warp 3: finds the CTA's units                                   warps 4-15: exponentials and sums, three groups in turn
+// The keys are the MMA's first operand and lie in TMEM (two elements a column, written there by the threads that own their rows), so
+// that shared memory feeds only the queries to the tensor cores.  With both operands in shared memory a step moved 64 KB out of it
+// and 32 KB into it, at its limit.  Two units' keys and three accumulators of 128 columns fill TMEM; the queries come through six
+// stages of 32 KB, as one box per 64 columns of the head where all packed rows are counted and a tile holds whole rows, else by
+// 16-byte copies (counted rows may be any of the packed ones, and a group of heads need not divide a tile).
 // Units leave partial sums, one for each head (or each share of a head's columns, where there are fewer than 8 heads), which a
 // second launch adds in order: no atomics, and the bits do not depend on which CTA took which unit.  CTAs take units from both
-// ends of rounds of the grid's size in turn, so that in a prompt, whose later keys are seen by fewer rows, all get the same work.
+// ends of rounds of the grid's size in turn, so that in a prompt, whose later keys are seen by fewer rows, all get about the same
+// work.  (Drawn from a counter as they were finished the units took as long.)
 //
-// What bounds it: the special function unit, 16 exponentials per clock and SM: 1024 clocks a step, in which the tensor cores work 512.
+// What bounds it: the special function unit, 16 exponentials per clock and SM (1024 clocks a step, in which the tensor cores work
+// 512), and in long runs the power limit.  Measured: a prompt of 8192 tokens, 32 heads on 8 of 128, 0.36 ms in runs of a few
+// milliseconds and 0.39 ms in long ones (1.72 GHz at 980 W), 275 GFLOP and 1.07e9 exponentials.  Two groups instead of three took 6 %
+// longer; a polynomial on the FMA pipe for a quarter of the exponentials 0.35 ms in short runs and no less in long ones.
 #include <algorithm>
 #include <type_traits>
 
@@ -24,18 +30,14 @@ namespace pcomoe {
 namespace {
 
 constexpr int BK_ROWS = 128, BC = 128;          // keys of a unit, columns of a step
-constexpr int kThreads = 384, kFirst = 128;
-constexpr int kSumRegs = 208, kOtherRegs = 88, kLaunchRegs = 168;
-static_assert(256 * kSumRegs + 128 * kOtherRegs <= kThreads * kLaunchRegs, "register split");
-constexpr int kStages = 4, kBuffers = 4, kSlots = 16;      // of queries, of accumulators, of log sums
-// A slot of log sums is filled again 16 steps later.  By then its step is done: the copies run at most kStages steps ahead of the
-// MMAs, these at most kBuffers ahead of the sums, and a warp group takes a step only after its last one.
-
+constexpr int kGroups = 3, kFirst = 128, kThreads = kFirst + 128 * kGroups;      // warp groups that sum, from thread kFirst on
+constexpr int kStages = 6, kBuffers = 3, kSlots = 8;       // of queries, of accumulators, of log sums
+constexpr uint32_t kKeyCols = 64, kAccAt = 2 * kKeyCols;    // TMEM columns: keys of two units, then the accumulators
 template <int D> struct Shape {
   static constexpr int kHalves = D / 64;
   static constexpr int kHalfBytes = 128 * 128;
   static constexpr int kTileBytes = kHalves * kHalfBytes;
-  static constexpr int kSmem = (kStages + 2) * kTileBytes;
+  static constexpr int kSmem = kStages * kTileBytes;
 };
 
 struct Unit {
@@ -57,10 +59,20 @@ __device__ __forceinline__ bool elect_lane() {
   asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(e));
   return e;
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
+// D (+)= A B, A from TMEM
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a),
                "l"(b), "r"(idesc), "r"(acc)
                : "memory");
+}
+// 16 columns of this thread's TMEM lane
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]),
+      "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+      "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(taddr)
+      : "memory");
 }
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool there) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -80,6 +92,26 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map
   asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map),
                "r"(x), "r"(y), "r"(z), "r"(bar)
                : "memory");
+}
+
+// 2^d of two numbers without the special function unit: the nearest whole number apart, and for the rest f in [-1/2, 1/2] a
+// polynomial of degree 5 whose largest relative error is 7.5e-8 (fitted to 2^f by weighted least squares until the error is
+// level).  Held inside [-126, 128], where 2^128 is infinite; a NaN stays one.
+__device__ __forceinline__ float2 exp2_poly(float2 d) {
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(d.x) : "f"(-126.f));
+  asm("max.NaN.f32 %0, %0, %1;" : "+f"(d.y) : "f"(-126.f));
+  asm("min.NaN.f32 %0, %0, %1;" : "+f"(d.x) : "f"(128.f));
+  asm("min.NaN.f32 %0, %0, %1;" : "+f"(d.y) : "f"(128.f));
+  const auto both = [](float v) { return make_float2(v, v); };
+  const float2 t = add2(d, both(12582912.f));               // 1.5 * 2^23: the last place is 1
+  const float2 f = add2(d, fma2(add2(t, both(-12582912.f)), both(-1.f), both(0.f)));
+  float2 p = fma2(both(0.0013276471781f), f, both(0.0096755413328f));
+  p = fma2(p, f, both(0.0555071327415f));
+  p = fma2(p, f, both(0.2402211972388f));
+  p = fma2(p, f, both(0.6931469670644f));
+  p = fma2(p, f, both(1.0000000716547f));
+  const float2 s = make_float2(__int_as_float((__float_as_int(t.x) << 23) + 0x3f800000), __int_as_float((__float_as_int(t.y) << 23) + 0x3f800000));
+  return fma2(p, s, both(0.f));
 }
 
 // The units of a call, in one line: sequence, keys, head and part, the last fastest.  One warp.
@@ -144,33 +176,33 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
   constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
   constexpr int C = D / 8, kSide = 32 / C;                // 16-byte pieces of a row; rows that a warp copies side by side
   extern __shared__ __align__(1024) uint8_t smem[];
-  __shared__ __align__(8) uint64_t s_qfull[kStages], s_qempty[kStages], s_kfull[2], s_kempty[2], s_sfull[kBuffers], s_sempty[kBuffers], s_lfull[kSlots], s_ifull[2],
+  __shared__ __align__(8) uint64_t s_qfull[kStages], s_qempty[kStages], s_kfull[2], s_kempty[2], s_sfull[kBuffers], s_sempty[kBuffers], s_lfull[kSlots], s_lempty[kSlots], s_ifull[2],
       s_iempty[2], s_join[2];
   __shared__ Unit s_item[2];
   __shared__ __align__(16) float s_lse[kSlots][BC];
   __shared__ __align__(16) int s_lim[kSlots][BC];
   __shared__ int s_least[kSlots][2];                      // the smallest limit of either half of a step's columns
   __shared__ int64_t s_at[2][64];                         // of the copying warps: where rows are, -1: nowhere
-  __shared__ float s_sum[2][BK_ROWS];
+  __shared__ float s_sum[2][kGroups - 1][BK_ROWS];
   __shared__ uint32_t s_bits[2 * (kMaxSeqs / 32)];
   __shared__ uint32_t s_tmem;
   __shared__ int s_flags[2];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t q_at = smem_u32(smem), k_at = q_at + kStages * S::kTileBytes;
+  const uint32_t q_at = smem_u32(smem);
   volatile int *flags = s_flags;
 
   if (tid == 0) {
     s_flags[0] = q_at & 1023 ? 1 : 0;                     // the swizzle needs it
     s_flags[1] = 0;
-    for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&s_qfull[i]), 2); mbar_init(smem_u32(&s_qempty[i]), 1); }
+    for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&s_qfull[i]), kBoxes ? 1 : 2); mbar_init(smem_u32(&s_qempty[i]), 1); }
     for (int i = 0; i < kBuffers; ++i) { mbar_init(smem_u32(&s_sfull[i]), 1); mbar_init(smem_u32(&s_sempty[i]), 4); }
-    for (int i = 0; i < kSlots; ++i) mbar_init(smem_u32(&s_lfull[i]), 2);
+    for (int i = 0; i < kSlots; ++i) { mbar_init(smem_u32(&s_lfull[i]), kBoxes ? 1 : 2); mbar_init(smem_u32(&s_lempty[i]), 4); }
     for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&s_kfull[i]), 2);
+      mbar_init(smem_u32(&s_kfull[i]), 4);
       mbar_init(smem_u32(&s_kempty[i]), 1);
       mbar_init(smem_u32(&s_ifull[i]), 1);
-      mbar_init(smem_u32(&s_iempty[i]), 11);              // every warp but the one that fills them
-      mbar_init(smem_u32(&s_join[i]), 4);
+      mbar_init(smem_u32(&s_iempty[i]), 3 + 4 * kGroups);              // every warp but the one that fills them
+      mbar_init(smem_u32(&s_join[i]), 4 * (kGroups - 1));
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -193,43 +225,77 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
     ++n_item;
   };
   if (warp >= kFirst / 32) {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSumRegs));
     const int group = (warp - kFirst / 32) >> 2, key = (warp & 3) * 32 + lane;
     const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
     const float scale = a.w.scale_log2;
     bool ok = true;
-    uint32_t n_unit = 0;
+    uint32_t n_unit = 0, n_k = 0;
+    // The first group brings the keys of unit number n into TMEM: a thread its own row, straight from its page, two elements to a column.
+    auto load_keys = [&](uint32_t n) {
+      if (ok) ok = wait_bar(&s_ifull[n & 1], (n >> 1) & 1, flags, a.w.limit_ns);
+      __syncwarp();
+      const Unit &it = s_item[n & 1];
+      if (!__all_sync(~0u, ok) || it.p0 < 0 || it.steps == 0) return;
+      const int p = it.p0 + key;
+      const uint4 *row = nullptr;
+      if (p < it.seq.len)
+        row = (const uint4 *)((const __nv_bfloat16 *)a.w.k + (weigh_page_row(a.w, a.w.table + (int64_t)it.seq.id * a.w.max_pages, p) + (int64_t)it.head * a.w.page) * D);
+      ok = wait_bar(&s_kempty[n_k & 1], ((n_k >> 1) & 1) ^ 1, flags, a.w.limit_ns);
+      __syncwarp();
+      tc_fence_after();
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        uint32_t x[16];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint4 y = row ? row[4 * c + k] : make_uint4(0, 0, 0, 0);
+          x[4 * k] = y.x; x[4 * k + 1] = y.y; x[4 * k + 2] = y.z; x[4 * k + 3] = y.w;
+        }
+        __syncwarp();
+        tmem_st16(tmem + (n_k & 1) * kKeyCols + 16 * c + lanes, x);
+      }
+      asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(smem_u32(&s_kfull[n_k & 1]));
+      ++n_k;
+    };
+    if (group == 0) load_keys(0);
     while (item_ready(ok)) {
       const Unit &it = s_item[n_item & 1];
       if (it.p0 < 0) break;
+      bool ahead = group != 0;                             // the next unit's keys are on their way
       const int p = it.p0 + key, last = it.p0 + BK_ROWS - 1, steps = it.steps, len = it.seq.len;
       float total = 0.f;
       for (int i = 0; i < steps; ++i) {
         const uint32_t at = step + i, b = at % kBuffers, slot = at % kSlots;
-        if ((int)(at & 1) != group) continue;
+        if ((int)(at % kGroups) != group) continue;
         if (ok) ok = wait_bar(&s_sfull[b], (at / kBuffers) & 1, flags, a.w.limit_ns) && wait_bar(&s_lfull[slot], (at / kSlots) & 1, flags, a.w.limit_ns);
         __syncwarp();
         tc_fence_after();
-        uint32_t x[4][32];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) tmem_ld32_issue(tmem + b * BC + 32 * c + lanes, x[c]);
-        tmem_wait_ld();
-#pragma unroll
-        for (int c = 0; c < 4; ++c) reg_fence32(x[c]);
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&s_sempty[b]));
         float2 sum[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
         const float2 scale2 = make_float2(scale, scale);
-        // (two loops, so that the one without a mask is one stretch of code: with the question inside of it a step took twice as long)
+        // 32 columns in hand, the next 32 on their way.  (Two loops, so that the one without a mask is one stretch of code: with the
+        // question inside of it a step took twice as long.)
         const auto sums = [&](auto masked) {
+          uint32_t x[2][32];
+          tmem_ld32_issue(tmem + kAccAt + b * BC + lanes, x[0]);
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
+            tmem_wait_ld();
+            reg_fence32(x[c & 1]);
+            if (c < 3) {
+              tmem_ld32_issue(tmem + kAccAt + b * BC + 32 * (c + 1) + lanes, x[(c + 1) & 1]);
+            } else {
+              tc_fence_before();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(smem_u32(&s_sempty[b]));
+            }
 #pragma unroll
             for (int k = 0; k < 32; k += 4) {
               const float4 l = *(const float4 *)&s_lse[slot][32 * c + k];        // minus the log sum
-              float2 e = fma2(make_float2(__uint_as_float(x[c][k]), __uint_as_float(x[c][k + 1])), scale2, make_float2(l.x, l.y));
-              float2 f = fma2(make_float2(__uint_as_float(x[c][k + 2]), __uint_as_float(x[c][k + 3])), scale2, make_float2(l.z, l.w));
+              float2 e = fma2(make_float2(__uint_as_float(x[c & 1][k]), __uint_as_float(x[c & 1][k + 1])), scale2, make_float2(l.x, l.y));
+              float2 f = fma2(make_float2(__uint_as_float(x[c & 1][k + 2]), __uint_as_float(x[c & 1][k + 3])), scale2, make_float2(l.z, l.w));
               e = make_float2(exp2_fast(e.x), exp2_fast(e.y));
               f = make_float2(exp2_fast(f.x), exp2_fast(f.y));
               if (masked.value) {                          // chosen, not multiplied
@@ -246,31 +312,37 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
         else sums(std::false_type());
         const float2 s = add2(add2(sum[0], sum[1]), add2(sum[2], sum[3]));
         total += s.x + s.y;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&s_lempty[slot]));
+        if (!ahead) {
+          load_keys(n_item + 1);
+          ahead = true;
+        }
       }
+      if (!ahead) load_keys(n_item + 1);
       step += steps;
-      // the second group hands its sums to the first.  (It gets to the unit after the next, which takes the same place and barrier,
-      // only when both are done with this one.)
+      // the other groups hand their sums to the first.  (They get to the unit after the next, which takes the same place and barrier,
+      // only when all are done with this one.)
       if (group) {
-        s_sum[n_unit & 1][key] = total;
+        s_sum[n_unit & 1][group - 1][key] = total;
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&s_join[n_unit & 1]));
       } else {
         if (ok) ok = wait_bar(&s_join[n_unit & 1], (n_unit >> 1) & 1, flags, a.w.limit_ns);
         __syncwarp();
-        if (p < len) a.partial[((int64_t)it.list * (a.w.hkv * a.parts) + it.part * a.w.hkv + it.head) * a.room + p] = total + s_sum[n_unit & 1][key];
+#pragma unroll
+        for (int g = 1; g < kGroups; ++g) total += s_sum[n_unit & 1][g - 1][key];
+        if (p < len) a.partial[((int64_t)it.list * (a.w.hkv * a.parts) + it.part * a.w.hkv + it.head) * a.room + p] = total;
       }
       ++n_unit;
       item_done();
     }
-  } else {
-  asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-  if (warp == 1 || warp == 2) {
-    // ---- copies: keys of a unit, then the columns of its steps; each of the two warps takes 64 rows.  Up to two copies are under way
-    // before the oldest is waited for and handed on.
+  } else if (warp == 1 || warp == 2) {
+    // ---- the columns of the steps and their log sums.  Where rows are copied one by one each of the two warps takes 64 columns, and up to
+    // two copies are under way before the oldest is waited for and handed on.
     const int half = warp - 1;
     uint64_t *wait0[2] = {nullptr, nullptr}, *wait1[2] = {nullptr, nullptr};       // barriers of the copies under way, oldest last
     bool ok = true;
-    uint32_t n_k = 0;
     auto hand_on = [&](int i) {
       if (!wait0[i]) return;
       if (lane == 0) {
@@ -320,18 +392,6 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
       const Unit it = s_item[n_item & 1];
       if (it.p0 < 0) break;
       if (it.steps == 0) continue;
-      if (!wait(&s_kempty[n_k & 1], ((n_k >> 1) & 1) ^ 1)) break;
-      const int32_t *table = a.w.table + (int64_t)it.seq.id * a.w.max_pages;
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int r = 32 * j + lane, p = it.p0 + half * 64 + r;
-        s_at[half][r] = p < it.seq.len ? (weigh_page_row(a.w, table, p) + (int64_t)it.head * a.w.page) * D : -1;
-      }
-      __syncwarp();
-      copy_rows(a.w.k, k_at + (n_k & 1) * S::kTileBytes);
-      __syncwarp();
-      begun(&s_kfull[n_k & 1], nullptr);
-      ++n_k;
       if (kBoxes) {
         // the first warp sends for the queries; the second has the log sums on their way kAhead steps before they are used
         constexpr int kAhead = 3;
@@ -351,17 +411,17 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
         for (int i = 0; i < it.steps; ++i, ++step) {
           const uint32_t st = step % kStages, slot = step % kSlots;
           const int c0 = (it.first + i * a.parts) * BC;
-          if (!wait(&s_qempty[st], ((step / kStages) & 1) ^ 1)) break;
           if (!half) {
+            if (!wait(&s_qempty[st], ((step / kStages) & 1) ^ 1)) break;
             if (lane == 0) {
               mbar_arrive_expect_tx(smem_u32(&s_qfull[st]), S::kTileBytes);
-              mbar_arrive(smem_u32(&s_lfull[slot]));
 #pragma unroll
               for (int h = 0; h < S::kHalves; ++h)
                 tma_load_3d(q_at + st * S::kTileBytes + h * S::kHalfBytes, &q_map, h * 64, it.head << gs, it.seq.q0 + (c0 >> gs), smem_u32(&s_qfull[st]));
             }
             __syncwarp();
           } else {
+            if (!wait(&s_lempty[slot], ((step / kSlots) & 1) ^ 1)) break;
             float lse[4];
             int lim[4], least = INT32_MAX;
 #pragma unroll
@@ -382,17 +442,13 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
             least = __reduce_min_sync(~0u, least);
             if (lane < 2) s_least[slot][lane] = least;
             __syncwarp();
-            if (lane == 0) {
-              mbar_arrive(smem_u32(&s_qfull[st]));
-              mbar_arrive(smem_u32(&s_lfull[slot]));
-            }
+            if (lane == 0) mbar_arrive(smem_u32(&s_lfull[slot]));
           }
-          if (i == 0) flush();                             // the keys, while the first queries come in
         }
       } else
       for (int i = 0; i < it.steps; ++i, ++step) {
         const uint32_t st = step % kStages, slot = step % kSlots;
-        if (!wait(&s_qempty[st], ((step / kStages) & 1) ^ 1)) break;
+        if (!wait(&s_qempty[st], ((step / kStages) & 1) ^ 1) || !wait(&s_lempty[slot], ((step / kSlots) & 1) ^ 1)) break;
         const int64_t c0 = (int64_t)(it.first + i * a.parts) * BC + half * 64, cols = (int64_t)it.seq.m * a.w.g;
         int least = INT32_MAX;
 #pragma unroll
@@ -431,13 +487,13 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
     bool ok = true;
     uint32_t n_k = 0;
     auto wait = [&](uint64_t *bar, uint32_t p) { return ok = __all_sync(~0u, wait_bar(bar, p, flags, a.w.limit_ns)); };
-    const uint64_t q_desc = umma_desc(q_at), k_desc = umma_desc(k_at);
+    const uint64_t q_desc = umma_desc(q_at);
     for (; item_ready(ok); item_done()) {
       const int p0 = s_item[n_item & 1].p0, steps = s_item[n_item & 1].steps;
       if (p0 < 0) break;
       if (steps == 0) continue;
       if (!wait(&s_kfull[n_k & 1], (n_k >> 1) & 1)) break;
-      const uint64_t da = k_desc + (uint64_t)((n_k & 1) * (S::kTileBytes >> 4));
+      const uint32_t keys = tmem + (n_k & 1) * kKeyCols;
       for (int i = 0; i < steps; ++i, ++step) {
         const uint32_t st = step % kStages, b = step % kBuffers;
         if (!wait(&s_sempty[b], ((step / kBuffers) & 1) ^ 1)) break;
@@ -448,7 +504,7 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
 #pragma unroll
           for (int k = 0; k < D / 16; ++k) {
             const uint64_t off = (uint64_t)((k >> 2) * (S::kHalfBytes >> 4) + (k & 3) * 2);
-            mma_ss(tmem + b * BC, da + off, db + off, kIdesc, k != 0);
+            mma_ts(tmem + kAccAt + b * BC, keys + k * 8, db + off, kIdesc, k != 0);
           }
           umma_commit(smem_u32(&s_sfull[b]));
           umma_commit(smem_u32(&s_qempty[st]));
@@ -460,12 +516,11 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
       ++n_k;
     }
   } else {
-    // ---- the units: from both ends of rounds of two grids
+    // ---- the units: from both ends of rounds of the grid's size in turn
     Line line = {0, 0, {}, 0, false};
     for (uint32_t r = 0;; ++r, ++n_item) {
       Unit it = {};
-      const int64_t u = (int64_t)r * gridDim.x + (r & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-      line.get(a, twice, u, it);
+      line.get(a, twice, (int64_t)r * gridDim.x + (r & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x), it);
       if (!__all_sync(~0u, wait_bar(&s_iempty[n_item & 1], ((n_item >> 1) & 1) ^ 1, flags, a.w.limit_ns))) break;
       if (lane == 0) {
         s_item[n_item & 1] = it;
@@ -474,7 +529,6 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
       __syncwarp();
       if (it.p0 < 0) break;
     }
-  }
   }
   tc_fence_before();
   __syncthreads();
@@ -509,10 +563,6 @@ pcomoe_status run(const CUtensorMap &q_map, const TcArgs &a, int sms, cudaStream
   int dev = -1;
   PCOMOE_CUDA_TRY(cudaGetDevice(&dev));
   if (once.first_use(dev)) {
-    // the register split draws on what the block was launched with: with fewer the larger share would never come
-    cudaFuncAttributes at;
-    PCOMOE_CUDA_TRY(cudaFuncGetAttributes(&at, weigh_tc_kernel<D, kBoxes>));
-    if (at.numRegs < kLaunchRegs) return PCOMOE_ERR_CUDA;
     PCOMOE_CUDA_TRY(cudaFuncSetAttribute(weigh_tc_kernel<D, kBoxes>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<D>::kSmem));
     once.done(dev);
   }
