@@ -9,12 +9,13 @@
 // sum over a vocabulary is off by 1e-7 of itself, and with 10^4 to 10^5 borders between words that changes a token in every few
 // thousand.
 //
-// Two launches.  The first forms the largest logit and the sum of the exponentials of every row that has a draft behind it,
-// rows side by side.  In the second a cluster of blocks per sequence first gathers what each draft's test needs, walks over
-// the drafts (they are numbered behind their parents, so one ascending pass meets every test in order), and reads the row
-// that the walk ended at once more: sums of its groups of 512 bytes, from which the group of the next token and in it the token
-// follow.  What bounds them: the rows' one read (HBM), the 64-bit pipe (64 lanes per clock and SM, about 12 of its operations
-// per word), and with few rows the chain of both launches.
+// Two launches.  The first forms the largest logit and, in 32 bits, the sum of the exponentials of every row that has a draft
+// behind it, rows side by side.  In the second a cluster of blocks per sequence first gathers what each draft's test needs,
+// walks over the drafts (they are numbered behind their parents, so one ascending pass meets every test in order; a test that lies too
+// near its border for 32 bits gets the row's sum in 64 first), and reads the row that the walk ended at once or twice more: sums
+// of its groups of 512 bytes, from which the group of the next token and in it the token follow.  What bounds them: the rows' one
+// read (HBM) in the first; in the second the chain of its steps and the 64-bit pipe (64 lanes per clock and SM, 14 of its operations
+// per word).
 #include <algorithm>
 
 #include "words.cuh"
@@ -48,25 +49,46 @@ struct VerifyArgs {
   RowSums *sums;
 };
 
-constexpr int kTable = 64;
+constexpr int kTable = 16;
 constexpr int kMaxGroups = 1040;          // of a block: 2^20 fp32 words over 8 blocks, and one
 
-// 2^d for d <= 0 (or a little above), 64 bits: the nearest 64th apart, Taylor's series of the rest (at most 1/128, so the first
-// term left out is below 4e-17) and a table of 2^(k/64).  Below 2^-1000 it is 0.
-__device__ __forceinline__ double pow2(double d, const double *table) {
-  const double magic = 105553116266496.0;                  // 1.5 * 2^46: its last place is 1/64
-  const double t = fmax(d, -1100.0) + magic;
+// 2^((x - m) c) in 64 bits for x <= m.  c16 = 16 c.  The nearest 16th apart, Taylor's series of the rest y / 16, |y| <= 1/2, up to the 5th
+// power (the first term left out is below 2e-13 of the result) and a table of 2^(k/16): 16 entries of 8 bytes lie in as many pairs
+// of banks, so that lanes that ask for different ones do not wait for one another.  0 below 2^-1000 and where x is -inf.
+__device__ __forceinline__ double pow2(float x, float m, double c16, float least, const double *table) {
+  const double magic = 6755399441055744.0;                 // 1.5 * 2^52: its last place is 1
+  const double d = (double)fmaxf(x, least) - (double)m, t = fma(d, c16, magic);
   const int k = __double2loint(t);
-  const double y = (fmax(d, -1100.0) - (t - magic)) * 0.69314718055994530942;
-  double p = fma(y, 1.0 / 120, 1.0 / 24);
-  p = fma(p, y, 1.0 / 6);
-  p = fma(p, y, 0.5);
-  p = fma(p, y, 1.0);
-  p = fma(p, y, 1.0) * table[k & (kTable - 1)];
-  return d < -1000.0 ? 0.0 : __hiloint2double(__double2hiint(p) + ((k >> 6) << 20), __double2loint(p));
+  const double y = fma(d, c16, magic - t);
+  constexpr double u = 0.69314718055994530942 / 16;
+  double p = fma(y, u * u * u * u * u / 120, u * u * u * u / 24);
+  p = fma(p, y, u * u * u / 6);
+  p = fma(p, y, u * u / 2);
+  p = fma(p, y, u) * y;
+  const double w = table[k & (kTable - 1)], r = fma(w, p, w);
+  return x < least ? 0.0 : __hiloint2double(__double2hiint(r) + ((k >> 4) << 20), __double2loint(r));
 }
+// the smallest x that pow2 takes
+__device__ __forceinline__ float least_of(float m, double c) { return (float)fmax((double)m - 990.0 / c, -3.4e38); }
+// 2^d for any d <= 0; 64 bits
+__device__ __forceinline__ double scale_of(float from, float to, double c) { return exp2(((double)from - (double)to) * c); }
 __device__ __forceinline__ void fill_table(double *table) {
   for (int i = threadIdx.x; i < kTable; i += blockDim.x) table[i] = exp2(i * (1.0 / kTable));
+}
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*(uint64_t *)&a), "l"(*(uint64_t *)&b));
+  return *(float2 *)&d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(*(uint64_t *)&a), "l"(*(uint64_t *)&b));
+  return *(float2 *)&d;
 }
 
 __device__ __forceinline__ float real(float q) { return q > 0.f && q < INFINITY ? q : 0.f; }      // what is no probability counts as 0
@@ -152,13 +174,13 @@ __device__ __forceinline__ int id_in_group(const T *row, int shift, int V, int g
   return (int)__reduce_min_sync(~0u, id);
 }
 
-// Sums of rows with drafts behind them.  kWarps warps, CL blocks per row.
+// Sums of rows with drafts behind them, in 32 bits.  kSumWarps warps, CL blocks per row.
 constexpr int kSumWarps = 8;
 template <typename T, int CL>
 __global__ void __launch_bounds__(32 * kSumWarps) row_sums_kernel(const __grid_constant__ VerifyArgs a) {
   pdl_grid_wait();
   constexpr int N = Vec<T>::N, kLoads = 4;
-  __shared__ double s_table[kTable], s_sum[kSumWarps];
+  __shared__ float s_sum[kSumWarps];
   __shared__ unsigned long long s_place[kSumWarps];
   __shared__ Joined s_box[2];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -183,73 +205,108 @@ __global__ void __launch_bounds__(32 * kSumWarps) row_sums_kernel(const __grid_c
   else
     for (int j = at + 1; j < rows.y && !wanted; j += 32) wanted = __any_sync(~0u, j + lane < rows.y && a.parent[rows.x + j + lane] == at);
   if (!wanted) return;
-  fill_table(s_table);
-  __syncthreads();
   const bool greedy = greedy_of(a, s);
-  const double c = rate_of(a, s);
+  const float c = (float)fmin(rate_of(a, s), 3e38);
   const T *row = row_of<T>(a, t);
   const int shift = shift_of(row), groups = (a.V + shift + 32 * N - 1) / (32 * N), per = (groups + CL - 1) / CL;
   const int g0 = min(cl.rank() * per, groups), g1 = min(g0 + per, groups);
   // sums over the warp's largest logit so far
-  double sum = 0.0;
+  float sum = 0.f;
   int key = kNoKey, best_g = 0;
-  for (int g = g0 + warp * kLoads; g < g1; g += kSumWarps * kLoads) {
-    uint4 raw[kLoads];
-    float none[N];
+  uint4 raw[kLoads];
+  auto fetch = [&](int g) {
+    if (g * 32 * N >= shift && (g + kLoads) * 32 * N - shift <= a.V && g + kLoads <= g1) {      // all inside the row
+      const uint4 *p = (const uint4 *)(row - shift) + g * 32 + lane;
 #pragma unroll
-    for (int k = 0; k < N; ++k) none[k] = kNone;
+      for (int u = 0; u < kLoads; ++u) raw[u] = __ldcs(p + 32 * u);
+    } else {
+      float none[N];
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) raw[i] = g + i < g1 ? load_raw<T>(row, shift, a.V, g + i, lane) : Vec<T>::pack(none);
-    float x[kLoads][N];
-    int k4[kLoads], most = kNoKey;
+      for (int k = 0; k < N; ++k) none[k] = kNone;
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      Vec<T>::unpack(raw[i], x[i]);
-      int k1 = kNoKey;
+      for (int u = 0; u < kLoads; ++u) raw[u] = g + u < g1 ? load_raw<T>(row, shift, a.V, g + u, lane) : Vec<T>::pack(none);
+    }
+  };
+  int g = g0 + warp * kLoads;
+  if (g < g1) fetch(g);
+  for (; g < g1; g += kSumWarps * kLoads) {
+    uint4 v[kLoads];
 #pragma unroll
-      for (int k = 0; k < N; ++k) {
-        x[i][k] = eligible(x[i][k]);
-        k1 = max(k1, key_of(x[i][k]));
+    for (int u = 0; u < kLoads; ++u) v[u] = raw[u];
+    if (g + kSumWarps * kLoads < g1) fetch(g + kSumWarps * kLoads);      // on its way while this one is summed
+    int k4[kLoads];
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) k4[u] = __reduce_max_sync(~0u, key_of(Vec<T>::largest(v[u])));
+    int most = max(max(k4[0], k4[1]), max(k4[2], k4[3]));
+    if (most >= key_of(INFINITY)) {                        // infinite logits (or nothing but NaN in a lane): they do not count
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {
+        float x[N];
+        Vec<T>::unpack(v[u], x);
+#pragma unroll
+        for (int k = 0; k < N; ++k) x[k] = eligible(x[k]);
+        v[u] = Vec<T>::pack(x);
+        k4[u] = __reduce_max_sync(~0u, key_of(Vec<T>::largest(v[u])));
       }
-      k4[i] = __reduce_max_sync(~0u, k1);
-      most = max(most, k4[i]);
+      most = max(max(k4[0], k4[1]), max(k4[2], k4[3]));
     }
     if (most > key) {
-      if (sum > 0.0) sum *= pow2(c * ((double)of_key(key) - (double)of_key(most)), s_table);
+      if (sum > 0.f) sum *= ex2((of_key(key) - of_key(most)) * c);
 #pragma unroll
-      for (int i = kLoads - 1; i >= 0; --i)
-        if (k4[i] == most) best_g = g + i;
+      for (int u = kLoads - 1; u >= 0; --u)
+        if (k4[u] == most) best_g = g + u;
       key = most;
     }
-    if (greedy || key == kNoKey) continue;
-    const double m = (double)of_key(key);
+    if (greedy || key <= kNoKey) continue;
+    const float m = of_key(key);
+    if (fabsf(m) < 1e6f) {                                 // (words held above -1e30, NaN and -inf with them: their weight is 0)
+      const float2 c2 = make_float2(c, c), minus = make_float2(-m, -m);
+      float2 s2[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i)
+      for (int u = 0; u < kLoads; ++u) {
+        float2 x[N / 2];
+        Vec<T>::pairs(v[u], x);
 #pragma unroll
-      for (int k = 0; k < N; ++k) sum += pow2(((double)x[i][k] - m) * c, s_table);
+        for (int k = 0; k < N / 2; ++k) {
+          const float2 d = mul2(add2(x[k], minus), c2);
+          s2[u] = add2(s2[u], make_float2(ex2(d.x), ex2(d.y)));
+        }
+      }
+      const float2 st = add2(add2(s2[0], s2[1]), add2(s2[2], s2[3]));
+      sum += st.x + st.y;
+    } else {
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {
+        float x[N];
+        Vec<T>::unpack(v[u], x);
+#pragma unroll
+        for (int k = 0; k < N; ++k) sum += ex2(fmaxf((eligible(x[k]) - m) * c, -1000.f));
+      }
+    }
   }
-  sum = warp_sum(sum);
-  if (lane == 0) { s_sum[warp] = sum; s_place[warp] = place_of(key, best_g); }
+#pragma unroll
+  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+  if (lane == 0) { s_sum[warp] = sum; s_place[warp] = place_of(max(key, kNoKey), best_g); }
   __syncthreads();
   // the warps', then the blocks', over the largest of all; ties go to the lowest group
   unsigned long long place = 0;
 #pragma unroll
   for (int w = 0; w < kSumWarps; ++w) place = max(place, s_place[w]);
-  double total = 0.0;
-  const auto join = [&](double part, int from, int to) { return part > 0.0 ? part * pow2(c * ((double)of_key(from) - (double)of_key(to)), s_table) : 0.0; };
+  const auto join = [&](float part, int from, int to) { return part > 0.f ? part * ex2((of_key(from) - of_key(to)) * c) : 0.f; };
+  float total = 0.f;
 #pragma unroll
   for (int w = 0; w < kSumWarps; ++w) total += join(s_sum[w], place_key(s_place[w]), place_key(place));
   Joined all[CL];
-  cl.gather({total, place}, all);
+  cl.gather({(double)total, place}, all);
   if (cl.rank() == 0 && warp == 0) {
 #pragma unroll
     for (int r = 0; r < CL; ++r) place = max(place, all[r].place);
-    total = 0.0;
+    total = 0.f;
 #pragma unroll
-    for (int r = 0; r < CL; ++r) total += join(all[r].s, place_key(all[r].place), place_key(place));
+    for (int r = 0; r < CL; ++r) total += join((float)all[r].s, place_key(all[r].place), place_key(place));
     const int k = place_key(place);
     const int best = greedy && k != kNoKey ? id_in_group<T>(row, shift, a.V, place_id(place), k) : -1;
-    if (lane == 0) a.sums[t] = {total, of_key(k), best};
+    if (lane == 0) a.sums[t] = {(double)total, of_key(k), best};
   }
   Cluster<CL>::barrier();                                  // nobody leaves while others read its box
 }
@@ -283,16 +340,23 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
   }
   fill_table(s_table);
   const bool greedy = greedy_of(a, seq);
-  const double c = rate_of(a, seq);
+  const double c = rate_of(a, seq), c16 = 16 * c;
   __syncthreads();
 
   int cur = 0, length = 1;
+  RowSums sums = {0.0, 0.f, -1};                           // of row cur, where drafts hang on it
+  bool exact = greedy;                                     // sums.s is formed in 64 bits
+  double ratio = 1.0;                                      // what the p in hand are multiplied by: the sum that they were formed with to the exact one
   double A = 0.0, R = 1.0;                                 // r = max(p - A q, 0), R = sum r (unless it is due)
+  double gone = 0.0;                                       // p of the refused tokens, where drafts are given
   int refused = 0;                                         // drafts refused at cur
   bool due = false;
   const T *row;
   int shift, groups, per, g0, g1;
   auto enter = [&](int at) {
+    sums = a.sums[rows.x + at];                            // (not formed, and not used, where no draft hangs on the row)
+    exact = greedy;
+    ratio = 1.0;
     row = row_of<T>(a, rows.x + at);
     shift = shift_of(row);
     groups = (a.V + shift + 32 * N - 1) / (32 * N);
@@ -327,10 +391,11 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
         const float m = rest ? m_row : of_key(__reduce_max_sync(~0u, k1));
         double sum = 0.0;
         if (m != kNone && !greedy) {
+          const float least = least_of(m, c);
           const int id = ((g + i) * 32 + lane) * N - shift;
 #pragma unroll
           for (int k = 0; k < N; ++k) {
-            double e = pow2(((double)x[k] - (double)m) * c, s_table);
+            double e = pow2(x[k], m, c16, least, s_table);
             if (rest) e = fmax(e - cut * (double)(id + k >= 0 && id + k < a.V ? real(near[id + k]) : 0.f), 0.0);
             sum += e;
           }
@@ -355,6 +420,51 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
     return x;
   };
   Joined all[CL];
+  double block_scale = 1.0;                                // of this block's s_group, to the whole's reference
+  unsigned long long place = 0;                            // this block's largest logit and its group
+  // What sum_groups has left, over all blocks; `rest` as there.
+  auto collect = [&](bool rest) {
+    if (!rest) {
+      // over the block's largest
+      unsigned long long best = place_of(kNoKey, 0);
+      for (int i = tid; i < g1 - g0; i += kWalkThreads) best = max(best, place_of(key_of(s_most[i]), g0 + i));
+      best = warp_max(best);
+      if (lane == 0) s_place[warp] = best;
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < kWalkWarps; ++w) best = max(best, s_place[w]);
+      place = best;
+      const float top = of_key(place_key(best));
+      if (!greedy)
+        for (int i = tid; i < g1 - g0; i += kWalkThreads)
+          if (s_group[i] > 0.0) s_group[i] *= scale_of(s_most[i], top, c);
+      __syncthreads();
+    }
+    const double part = greedy ? 0.0 : block_sum();
+    cl.gather({part, place}, all);
+    unsigned long long whole = 0;
+#pragma unroll
+    for (int r = 0; r < CL; ++r) whole = max(whole, all[r].place);
+    double total = 0.0;
+#pragma unroll
+    for (int r = 0; r < CL; ++r) {
+      if (!rest && all[r].s > 0.0) all[r].s *= scale_of(of_key(place_key(all[r].place)), of_key(place_key(whole)), c);
+      if (r == cl.rank() && !rest && part > 0.0) block_scale = all[r].s / part;
+      total += all[r].s;
+    }
+    if (greedy) place = whole;
+    return total;
+  };
+  // The sum of row cur in 64 bits, where its 32 do not decide.
+  auto refine = [&]() {
+    if (!exact && sums.s > 0.0) {
+      sum_groups(false, false, 0.f, 0.0);
+      const double total = collect(false);
+      ratio = sums.s / total;
+      sums.s = total;
+    }
+    exact = true;
+  };
 
   enter(0);
   for (int c0 = 0; c0 < rows.y && length < a.keep_stride; c0 += kChunk) {
@@ -366,12 +476,12 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
       if (!ok) atomicCAS(&a.head->status, 0, (int)PCOMOE_ERR_INDEX);
       double p = 0.0, q = 1.0;
       if (ok) {
-        const RowSums sums = a.sums[rows.x + up];
+        const RowSums sums = a.sums[rows.x + up];          // in 32 bits, see test()
         if (greedy) {
           p = token == sums.best ? 1.0 : 0.0;
         } else {
           const float x = eligible(Vec<T>::one(row_of<T>(a, rows.x + up) + token));
-          if (x != kNone && sums.s > 0.0) p = pow2(c * ((double)x - (double)sums.m), s_table) / sums.s;
+          if (x != kNone && sums.s > 0.0) p = pow2(x, sums.m, c16, least_of(sums.m, c), s_table) / sums.s;
         }
         if (a.near) q = (double)real(a.near[(int64_t)(rows.x + up) * a.near_stride + token]);
       }
@@ -395,43 +505,49 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
         }
       }
       if (hit == kChunk) break;
-      double r = s_p[hit];
-      if (a.near) {
-        if (due) {
-          const RowSums sums = a.sums[rows.x + cur];
-          double left = 0.0;
-          if (greedy) {
-            // all of p lies on one word
-            left = sums.best >= 0 ? fmax(1.0 - A * (double)real(a.near[(int64_t)(rows.x + cur) * a.near_stride + sums.best]), 0.0) : 0.0;
-          } else if (sums.s > 0.0) {
-            sum_groups(true, false, sums.m, A * sums.s);
-            const double mine = block_sum();
-            cl.gather({mine, 0ull}, all);
-#pragma unroll
-            for (int k = 0; k < CL; ++k) left += all[k].s;
-            left /= sums.s;
-          }
-          R = left;
-          due = false;
-          if (!(R > 0.0)) { A = 0.0; R = 1.0; }            // nothing is left: the target's own distribution again
-        }
-        r = fmax(r - A * s_q[hit], 0.0);
-      } else if (refused) {
-        // a token that an earlier draft here had is gone
+      bool again = false;                                  // a given token that an earlier draft here had is gone
+      if (!a.near && refused) {
         const int token = a.tokens[rows.x + c0 + hit];
-        bool again = false;
         for (int b = cur + 1; b < c0 + hit && !again; b += 32) {
           const int k = b + lane;
           again = __any_sync(~0u, k < c0 + hit && (a.parent ? a.parent[rows.x + k] : k - 1) == cur && a.tokens[rows.x + k] == token);
         }
-        if (again) r = 0.0;
       }
-      if ((double)s_u[hit] * R * s_q[hit] < r) {
+      if (a.near && due) {
+        refine();
+        double left = 0.0;
+        if (greedy) {
+          // all of p lies on one word
+          left = sums.best >= 0 ? fmax(1.0 - A * (double)real(a.near[(int64_t)(rows.x + cur) * a.near_stride + sums.best]), 0.0) : 0.0;
+        } else if (sums.s > 0.0) {
+          sum_groups(true, false, sums.m, A * sums.s);
+          left = collect(true) / sums.s;
+        }
+        R = left;
+        due = false;
+        if (!(R > 0.0)) { A = 0.0; R = 1.0; }              // nothing is left: the target's own distribution again
+      }
+      double r, want;
+      const auto test = [&]() {
+        const double p = s_p[hit] * ratio;
+        if (!a.near) R = ratio * gone < 1.0 ? 1.0 - ratio * gone : 1.0;
+        r = again ? 0.0 : fmax(p - A * s_q[hit], 0.0);
+        want = (double)s_u[hit] * R * s_q[hit];
+        return want < r;
+      };
+      // A sum in 32 bits is off by at most 2^-14 of itself (20 times 2^-23 from the products' rounding where the words' own logarithms
+      // average 20 bits, and a step of 2^-24 for each of the additions of a lane): where that could turn the answer, 64 bits give it.
+      bool taken = test();
+      if (!exact && fabs(want - r) <= (1.0 / 8192) * ((double)s_u[hit] * s_q[hit] + s_p[hit])) {
+        refine();
+        taken = test();
+      }
+      if (taken) {
         cur = c0 + hit;
         enter(cur);
         if (first_block && tid == 0) a.keep[(int64_t)seq * a.keep_stride + length] = cur;
         ++length;
-        A = 0.0;
+        A = gone = 0.0;
         R = 1.0;
         refused = 0;
         due = false;
@@ -440,9 +556,8 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
         if (a.near) {
           A += R;
           due = true;
-        } else {
-          R = fmax(R - r, 0.0);
-          if (!(R > 0.0)) R = 1.0;
+        } else if (!again) {
+          gone += s_p[hit];
         }
       }
       j = hit + 1;
@@ -457,9 +572,8 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
   const int mine = g1 - g0;
   bool rest = a.near && A > 0.0 && !greedy;
   bool marked = !a.near && refused > 0 && !greedy;
-  RowSums sums = {0.0, 0.f, -1};
   if (rest) {
-    sums = a.sums[rows.x + cur];
+    refine();
     rest = sums.s > 0.0;
   }
   if (marked) {
@@ -474,39 +588,10 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
     }
     __syncthreads();
   }
-  double block_scale = 1.0, total = 0.0;
-  unsigned long long place = 0;
+  double total;
   for (;;) {
     sum_groups(rest, marked, sums.m, A * sums.s);
-    if (!rest) {
-      // over the block's largest
-      unsigned long long best = place_of(kNoKey, 0);
-      for (int i = tid; i < mine; i += kWalkThreads) best = max(best, place_of(key_of(s_most[i]), g0 + i));
-      best = warp_max(best);
-      if (lane == 0) s_place[warp] = best;
-      __syncthreads();
-#pragma unroll
-      for (int w = 0; w < kWalkWarps; ++w) best = max(best, s_place[w]);
-      place = best;
-      const double top = (double)of_key(place_key(best));
-      if (!greedy)
-        for (int i = tid; i < mine; i += kWalkThreads)
-          if (s_group[i] > 0.0) s_group[i] *= pow2(c * ((double)s_most[i] - top), s_table);
-      __syncthreads();
-    }
-    const double part = greedy ? 0.0 : block_sum();
-    cl.gather({part, place}, all);
-    unsigned long long whole = 0;
-#pragma unroll
-    for (int r = 0; r < CL; ++r) whole = max(whole, all[r].place);
-    total = 0.0;
-#pragma unroll
-    for (int r = 0; r < CL; ++r) {
-      if (!rest && all[r].s > 0.0) all[r].s *= pow2(c * ((double)of_key(place_key(all[r].place)) - (double)of_key(place_key(whole))), s_table);
-      if (r == cl.rank() && !rest && part > 0.0) block_scale = all[r].s / part;
-      total += all[r].s;
-    }
-    if (greedy) place = whole;
+    total = collect(rest);
     if (greedy || total > 0.0 || !(rest || marked)) break;
     rest = marked = false;                                 // nothing is left: the target's own distribution
   }
@@ -567,19 +652,20 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
         else base = INFINITY;
       }
       const float m = s_most[g];
-      const double scale = rest ? 1.0 : pow2(c * ((double)m - (double)of_key(place_key(place))), s_table);
+      const double scale = rest ? 1.0 : scale_of(m, of_key(place_key(place)), c);
       const double left = base == INFINITY ? INFINITY : (goal - base) / scale;
       float x[N];
       load_words<T>(row, shift, a.V, g0 + g, lane, x);
       const uint32_t out = marked ? s_out[g * 32 + lane] : 0u;
       const float *near = rest ? a.near + (int64_t)(rows.x + cur) * a.near_stride : nullptr;
       const int id = ((g0 + g) * 32 + lane) * N - shift;
+      const float least = least_of(m, c);
       double e[N], lane_sum = 0.0;
       int last_word = -1;
 #pragma unroll
       for (int k = 0; k < N; ++k) {
         const float y = (out >> k) & 1 ? kNone : eligible(x[k]);
-        e[k] = pow2(((double)y - (double)m) * c, s_table);
+        e[k] = pow2(y, m, c16, least, s_table);
         if (rest) e[k] = fmax(e[k] - A * sums.s * (double)(id + k >= 0 && id + k < a.V ? real(near[id + k]) : 0.f), 0.0);
         lane_sum += e[k];
         if (e[k] > 0.0) last_word = id + k;
