@@ -17,6 +17,7 @@
 // read (HBM) in the first; in the second the chain of its steps and the 64-bit pipe (64 lanes per clock and SM, 14 of its operations
 // per word).
 #include <algorithm>
+#include <type_traits>
 
 #include "words.cuh"
 
@@ -70,8 +71,6 @@ __device__ __forceinline__ double pow2(float x, float m, double c16, float least
 }
 // the smallest x that pow2 takes
 __device__ __forceinline__ float least_of(float m, double c) { return (float)fmax((double)m - 990.0 / c, -3.4e38); }
-// 2^d for any d <= 0; 64 bits
-__device__ __forceinline__ double scale_of(float from, float to, double c) { return exp2(((double)from - (double)to) * c); }
 __device__ __forceinline__ void fill_table(double *table) {
   for (int i = threadIdx.x; i < kTable; i += blockDim.x) table[i] = exp2(i * (1.0 / kTable));
 }
@@ -314,8 +313,9 @@ __global__ void __launch_bounds__(32 * kSumWarps) row_sums_kernel(const __grid_c
 // The walk and the next token.  CL blocks per sequence.
 constexpr int kWalkWarps = 16, kWalkThreads = 32 * kWalkWarps, kChunk = kWalkThreads;
 template <typename T, int CL>
-__global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constant__ VerifyArgs a, int room) {
-  pdl_grid_wait();
+__global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_constant__ VerifyArgs a, int room) {
+  // The launch before this one in the stream is row_sums_kernel's, which let this one begin only after all earlier work was
+  // done: the arguments can be read before waiting for it, its sums and the caller's outputs not.
   constexpr int N = Vec<T>::N, kLoads = 4;
   extern __shared__ __align__(16) uint8_t smem[];
   double *s_group = (double *)smem;                        // sums of this block's groups
@@ -332,6 +332,7 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
   const bool first_block = cl.rank() == 0;
   const int2 rows = rows_of(a, seq);
   if (rows.y == 0) {
+    pdl_grid_wait();
     if (first_block) {
       for (int i = tid; i < a.keep_stride; i += kWalkThreads) a.keep[(int64_t)seq * a.keep_stride + i] = -1;
       if (tid == 0) { a.n_keep[seq] = 0; a.next[seq] = -1; }
@@ -354,7 +355,6 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
   const T *row;
   int shift, groups, per, g0, g1;
   auto enter = [&](int at) {
-    sums = a.sums[rows.x + at];                            // (not formed, and not used, where no draft hangs on the row)
     exact = greedy;
     ratio = 1.0;
     row = row_of<T>(a, rows.x + at);
@@ -366,45 +366,63 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
   };
 
   // Sums of the groups of row cur into s_group.  `rest`: of max(2^(c (x - m)) - cut q, 0) with the given m; else of
-  // 2^(c (x - m)), m the group's own largest (s_most), without the words marked in s_out if `marked`.
-  auto sum_groups = [&](bool rest, bool marked, float m_row, double cut) {
-    const float *near = rest ? a.near + (int64_t)(rows.x + cur) * a.near_stride : nullptr;
-    for (int g = g0 + warp * kLoads; g < g1; g += kWalkWarps * kLoads) {
+  // 2^(c (x - m)), m the group's own largest (s_most), without the words marked in s_out if `marked`.  (Two stretches of code without
+  // questions inside: eight words' chains of 64-bit operations then run side by side.)
+  auto group_sums = [&](auto rest, bool marked, float m_row, double cut) {
+    const float *near = rest.value ? a.near + (int64_t)(rows.x + cur) * a.near_stride : nullptr;
+    for (int g = g0 + warp; g < g1; g += kWalkWarps * kLoads) {
       uint4 raw[kLoads];
-      float none[N];
+      if (g * 32 * N >= shift && (g + kWalkWarps * (kLoads - 1) + 1) * 32 * N - shift <= a.V && g + kWalkWarps * (kLoads - 1) < g1) {
+        const uint4 *p = (const uint4 *)(row - shift) + g * 32 + lane;                  // all inside the row
 #pragma unroll
-      for (int k = 0; k < N; ++k) none[k] = kNone;
+        for (int i = 0; i < kLoads; ++i) raw[i] = p[32 * kWalkWarps * i];
+      } else {
+        float none[N];
 #pragma unroll
-      for (int i = 0; i < kLoads; ++i) raw[i] = g + i < g1 ? load_raw<T>(row, shift, a.V, g + i, lane) : Vec<T>::pack(none);
+        for (int k = 0; k < N; ++k) none[k] = kNone;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i)
+          raw[i] = g + kWalkWarps * i < g1 ? load_raw<T>(row, shift, a.V, g + kWalkWarps * i, lane) : Vec<T>::pack(none);
+      }
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        if (g + i >= g1) break;
+        const int gi = g + kWalkWarps * i;
+        if (gi >= g1) break;
         float x[N];
         Vec<T>::unpack(raw[i], x);
-        const uint32_t out = marked ? s_out[(g + i - g0) * 32 + lane] : 0u;
+        const uint32_t out = !rest.value && marked ? s_out[(gi - g0) * 32 + lane] : 0u;
         int k1 = kNoKey;
 #pragma unroll
         for (int k = 0; k < N; ++k) {
           x[k] = (out >> k) & 1 ? kNone : eligible(x[k]);
           k1 = max(k1, key_of(x[k]));
         }
-        const float m = rest ? m_row : of_key(__reduce_max_sync(~0u, k1));
+        const float m = rest.value ? m_row : of_key(__reduce_max_sync(~0u, k1));
         double sum = 0.0;
         if (m != kNone && !greedy) {
           const float least = least_of(m, c);
-          const int id = ((g + i) * 32 + lane) * N - shift;
+          double e[N];
 #pragma unroll
-          for (int k = 0; k < N; ++k) {
-            double e = pow2(x[k], m, c16, least, s_table);
-            if (rest) e = fmax(e - cut * (double)(id + k >= 0 && id + k < a.V ? real(near[id + k]) : 0.f), 0.0);
-            sum += e;
+          for (int k = 0; k < N; ++k) e[k] = pow2(x[k], m, c16, least, s_table);
+          if (rest.value) {
+            const int id = (gi * 32 + lane) * N - shift;
+#pragma unroll
+            for (int k = 0; k < N; ++k) e[k] = fmax(e[k] - cut * (double)(id + k >= 0 && id + k < a.V ? real(near[id + k]) : 0.f), 0.0);
           }
-          sum = warp_sum(sum);
+#pragma unroll
+          for (int o = 1; o < N; o <<= 1)
+#pragma unroll
+            for (int k = 0; k < N; k += 2 * o) e[k] += e[k + o];
+          sum = warp_sum(e[0]);
         }
-        if (lane == 0) { s_group[g + i - g0] = sum; s_most[g + i - g0] = m; }
+        if (lane == 0) { s_group[gi - g0] = sum; s_most[gi - g0] = m; }
       }
     }
     __syncthreads();
+  };
+  auto sum_groups = [&](bool rest, bool marked, float m_row, double cut) {
+    if (rest) group_sums(std::true_type(), false, m_row, cut);
+    else group_sums(std::false_type(), marked, 0.f, 0.0);
   };
   // this block's sum of s_group, the same in every thread
   auto block_sum = [&]() {
@@ -434,10 +452,10 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
 #pragma unroll
       for (int w = 0; w < kWalkWarps; ++w) best = max(best, s_place[w]);
       place = best;
-      const float top = of_key(place_key(best));
+      const float top = of_key(place_key(best)), least = least_of(top, c);
       if (!greedy)
         for (int i = tid; i < g1 - g0; i += kWalkThreads)
-          if (s_group[i] > 0.0) s_group[i] *= scale_of(s_most[i], top, c);
+          if (s_group[i] > 0.0) s_group[i] *= pow2(s_most[i], top, c16, least, s_table);
       __syncthreads();
     }
     const double part = greedy ? 0.0 : block_sum();
@@ -446,9 +464,10 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
 #pragma unroll
     for (int r = 0; r < CL; ++r) whole = max(whole, all[r].place);
     double total = 0.0;
+    const float top = of_key(place_key(whole)), least = least_of(top, c);
 #pragma unroll
     for (int r = 0; r < CL; ++r) {
-      if (!rest && all[r].s > 0.0) all[r].s *= scale_of(of_key(place_key(all[r].place)), of_key(place_key(whole)), c);
+      if (!rest && all[r].s > 0.0) all[r].s *= pow2(of_key(place_key(all[r].place)), top, c16, least, s_table);
       if (r == cl.rank() && !rest && part > 0.0) block_scale = all[r].s / part;
       total += all[r].s;
     }
@@ -457,7 +476,9 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
   };
   // The sum of row cur in 64 bits, where its 32 do not decide.
   auto refine = [&]() {
-    if (!exact && sums.s > 0.0) {
+    if (exact) return;
+    sums = a.sums[rows.x + cur];
+    if (sums.s > 0.0) {
       sum_groups(false, false, 0.f, 0.0);
       const double total = collect(false);
       ratio = sums.s / total;
@@ -467,38 +488,45 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
   };
 
   enter(0);
-  for (int c0 = 0; c0 < rows.y && length < a.keep_stride; c0 += kChunk) {
+  if (rows.y == 1 || a.keep_stride == 1) pdl_grid_wait();
+  for (int c0 = 0; c0 < rows.y && rows.y > 1 && length < a.keep_stride; c0 += kChunk) {
     // what the tests of the next drafts need: p and q of each one's token at its parent's row
     __syncthreads();
-    if (c0 + tid < rows.y && c0 + tid > 0) {
-      const int j = c0 + tid, t = rows.x + j, up = a.parent ? a.parent[t] : j - 1, token = a.tokens[t];
-      bool ok = up >= 0 && up < j && token >= 0 && token < a.V;
-      if (!ok) atomicCAS(&a.head->status, 0, (int)PCOMOE_ERR_INDEX);
-      double p = 0.0, q = 1.0;
-      if (ok) {
-        const RowSums sums = a.sums[rows.x + up];          // in 32 bits, see test()
-        if (greedy) {
-          p = token == sums.best ? 1.0 : 0.0;
-        } else {
-          const float x = eligible(Vec<T>::one(row_of<T>(a, rows.x + up) + token));
-          if (x != kNone && sums.s > 0.0) p = pow2(x, sums.m, c16, least_of(sums.m, c), s_table) / sums.s;
-        }
+    const int j = c0 + tid, t = rows.x + j;
+    const bool mine = j < rows.y && j > 0;
+    int up = -1, token = -1;
+    float x = kNone;
+    double q = 1.0;
+    if (mine) {
+      up = a.parent ? a.parent[t] : j - 1;
+      token = a.tokens[t];
+      s_u[tid] = a.u[t];
+      if (up < 0 || up >= j || token < 0 || token >= a.V) {
+        atomicCAS(&a.head->status, 0, (int)PCOMOE_ERR_INDEX);
+        up = -1;
+      } else {
+        x = eligible(Vec<T>::one(row_of<T>(a, rows.x + up) + token));
         if (a.near) q = (double)real(a.near[(int64_t)(rows.x + up) * a.near_stride + token]);
       }
-      s_p[tid] = p;
-      s_q[tid] = q;
-      s_u[tid] = a.u[t];
-      s_parent[tid] = ok ? up : -1;
-    } else {
-      s_parent[tid] = -1;
     }
+    s_parent[tid] = up;
+    s_q[tid] = q;
+    if (c0 == 0) pdl_grid_wait();
+    double p = 0.0;
+    if (up >= 0) {
+      const RowSums at = a.sums[rows.x + up];              // in 32 bits, see test()
+      if (greedy) p = token == at.best ? 1.0 : 0.0;
+      else if (x != kNone && at.s > 0.0) p = pow2(x, at.m, c16, least_of(at.m, c), s_table) / at.s;
+    }
+    s_p[tid] = p;
     __syncthreads();
+    const int in_chunk = min(kChunk, rows.y - c0);
     // every warp of every block takes the same way
-    int j = 0;
+    int next = 0;
     while (length < a.keep_stride) {
       int hit = kChunk;
-      for (int b = j & ~31; b < kChunk; b += 32) {
-        const uint32_t m = __ballot_sync(~0u, b + lane >= j && s_parent[b + lane] == cur);
+      for (int b = next & ~31; b < in_chunk; b += 32) {
+        const uint32_t m = __ballot_sync(~0u, b + lane >= next && s_parent[b + lane] == cur);
         if (m) {
           hit = b + __ffs(m) - 1;
           break;
@@ -518,6 +546,7 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
         double left = 0.0;
         if (greedy) {
           // all of p lies on one word
+          sums = a.sums[rows.x + cur];
           left = sums.best >= 0 ? fmax(1.0 - A * (double)real(a.near[(int64_t)(rows.x + cur) * a.near_stride + sums.best]), 0.0) : 0.0;
         } else if (sums.s > 0.0) {
           sum_groups(true, false, sums.m, A * sums.s);
@@ -560,7 +589,7 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
           gone += s_p[hit];
         }
       }
-      j = hit + 1;
+      next = hit + 1;
     }
   }
   if (first_block) {
@@ -652,7 +681,8 @@ __global__ void __launch_bounds__(kWalkThreads) walk_kernel(const __grid_constan
         else base = INFINITY;
       }
       const float m = s_most[g];
-      const double scale = rest ? 1.0 : scale_of(m, of_key(place_key(place)), c);
+      const float top = of_key(place_key(place));
+      const double scale = rest ? 1.0 : pow2(m, top, c16, least_of(top, c), s_table);
       const double left = base == INFINITY ? INFINITY : (goal - base) / scale;
       float x[N];
       load_words<T>(row, shift, a.V, g0 + g, lane, x);
@@ -712,7 +742,7 @@ cudaError_t launch_clusters(void (*kernel)(K...), int items, int cl, int threads
 
 template <typename T, int CL>
 pcomoe_status launch_sums(const VerifyArgs &a, cudaStream_t st) {
-  PCOMOE_CUDA_TRY(launch_clusters(row_sums_kernel<T, CL>, a.T, CL, 32 * kSumWarps, 0, st, a));
+  PCOMOE_CUDA_TRY(launch_clusters(row_sums_kernel<T, CL>, std::max(a.T, 1), CL, 32 * kSumWarps, 0, st, a));
   count_launch();
   return PCOMOE_OK;
 }
@@ -741,7 +771,7 @@ pcomoe_status run(const VerifyArgs &a, int sms, cudaStream_t st) {
     return cl;
   };
   pcomoe_status s = PCOMOE_OK;
-  if (a.T > 0) switch (blocks(a.T, kSumWarps)) {
+  switch (blocks(std::max(a.T, 1), kSumWarps)) {           // (launched for no rows too: the second launch leans on the first)
     case 1: s = launch_sums<T, 1>(a, st); break;
     case 2: s = launch_sums<T, 2>(a, st); break;
     case 4: s = launch_sums<T, 4>(a, st); break;
