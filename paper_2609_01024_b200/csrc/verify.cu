@@ -9,13 +9,15 @@
 // sum over a vocabulary is off by 1e-7 of itself, and with 10^4 to 10^5 borders between words that changes a token in every few
 // thousand.
 //
-// Two launches.  The first forms the largest logit and, in 32 bits, the sum of the exponentials of every row that has a draft
-// behind it, rows side by side.  In the second a cluster of blocks per sequence first gathers what each draft's test needs,
-// walks over the drafts (they are numbered behind their parents, so one ascending pass meets every test in order; a test that lies too
-// near its border for 32 bits gets the row's sum in 64 first), and reads the row that the walk ended at once or twice more: sums
-// of its groups of 512 bytes, from which the group of the next token and in it the token follow.  What bounds them: the rows' one
-// read (HBM) in the first; in the second the chain of its steps and the 64-bit pipe (64 lanes per clock and SM, 14 of its operations
-// per word).
+// Two launches.  The first forms the largest logit, its lowest id and, in 32 bits, the sum of the exponentials of every row, rows
+// side by side.  In the second a cluster of blocks per sequence has gathered meanwhile what each draft's test needs, walks over the
+// drafts (they are numbered behind their parents, so one ascending pass meets every test in order) and reads the row that the walk
+// ended at once more, for the sums of its groups of 512 bytes in 64 bits, from which the group of the next token and in it the token
+// follow.  A test is made in 32 bits first, and in 64, with the row's sum formed again, where it lies within 2^-13 of its border.
+// After a refusal the sums of max(p - A q, 0) are taken as those of p and q over the words where p > A q: which words these are
+// the sum in 32 bits tells well enough (a word that it takes wrongly lies so near the border that it adds 1e-12 of itself).
+// What bounds them: the rows' one read (HBM) in the first; in the second a chain of dependent steps, since an operation in 64
+// bits takes some 45 clocks until the next one can use it.
 #include <algorithm>
 #include <type_traits>
 
@@ -30,10 +32,10 @@ struct VerifyHeader {
 };
 static_assert(offsetof(VerifyHeader, status) == offsetof(DevPlan, status_router), "status word");
 
-struct RowSums {                          // of a row with drafts behind it
-  double s;                               // sum of 2^(c (x - m)), c = log2 e / temperature
+struct RowSums {                          // of a row
+  double s;                               // sum of 2^(c (x - m)), c = log2 e / temperature (not of greedy rows)
   float m;                                // largest logit; -inf: nothing eligible
-  int32_t best;                           // its lowest id (greedy rows only)
+  int32_t best;                           // its lowest id, -1
 };
 
 struct VerifyArgs {
@@ -173,8 +175,8 @@ __device__ __forceinline__ int id_in_group(const T *row, int shift, int V, int g
   return (int)__reduce_min_sync(~0u, id);
 }
 
-// Sums of rows with drafts behind them, in 32 bits.  kSumWarps warps, CL blocks per row.
-constexpr int kSumWarps = 8;
+// Largest logit, its lowest id and sums of all rows, in 32 bits.  kSumWarps warps, CL blocks per row.
+constexpr int kSumWarps = 16;
 template <typename T, int CL>
 __global__ void __launch_bounds__(32 * kSumWarps) row_sums_kernel(const __grid_constant__ VerifyArgs a) {
   pdl_grid_wait();
@@ -185,7 +187,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) row_sums_kernel(const __grid_c
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t = blockIdx.x / CL;
   Cluster<CL> cl = {&s_box, 0};
-  // the row's sequence, and whether a draft hangs on it
+  // the row's sequence
   int s = 0;
   {
     int hi = a.n;
@@ -196,14 +198,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) row_sums_kernel(const __grid_c
       s += k * step;
     }
   }
-  const int2 rows = rows_of(a, s);
-  const int at = t - rows.x;
-  if (at < 0 || at >= rows.y) return;                      // (every block of the cluster, like the next one)
-  bool wanted = false;
-  if (!a.parent) wanted = at + 1 < rows.y;
-  else
-    for (int j = at + 1; j < rows.y && !wanted; j += 32) wanted = __any_sync(~0u, j + lane < rows.y && a.parent[rows.x + j + lane] == at);
-  if (!wanted) return;
+  if (t >= a.T || t < a.cu[s] || t >= a.cu[s + 1]) return; // (every block of the cluster)
   const bool greedy = greedy_of(a, s);
   const float c = (float)fmin(rate_of(a, s), 3e38);
   const T *row = row_of<T>(a, t);
@@ -288,48 +283,56 @@ __global__ void __launch_bounds__(32 * kSumWarps) row_sums_kernel(const __grid_c
   if (lane == 0) { s_sum[warp] = sum; s_place[warp] = place_of(max(key, kNoKey), best_g); }
   __syncthreads();
   // the warps', then the blocks', over the largest of all; ties go to the lowest group
+  const auto join = [&](float part, unsigned long long from, unsigned long long to) {
+    return part > 0.f ? part * ex2((of_key(place_key(from)) - of_key(place_key(to))) * c) : 0.f;
+  };
   unsigned long long place = 0;
-#pragma unroll
-  for (int w = 0; w < kSumWarps; ++w) place = max(place, s_place[w]);
-  const auto join = [&](float part, int from, int to) { return part > 0.f ? part * ex2((of_key(from) - of_key(to)) * c) : 0.f; };
   float total = 0.f;
+  if (warp == 0) {
+    static_assert(kSumWarps == 16, "half a warp's lanes");
+    const unsigned long long mine = s_place[lane & 15];
+    place = warp_max(mine);
+    total = join(s_sum[lane & 15], mine, place);
 #pragma unroll
-  for (int w = 0; w < kSumWarps; ++w) total += join(s_sum[w], place_key(s_place[w]), place_key(place));
-  Joined all[CL];
-  cl.gather({(double)total, place}, all);
+    for (int o = 8; o; o >>= 1) total += __shfl_xor_sync(~0u, total, o);
+  }
+  if (CL > 1) {
+    Joined all[CL];
+    cl.gather({(double)total, place}, all);
+    if (cl.rank() == 0 && warp == 0) {
+#pragma unroll
+      for (int r = 0; r < CL; ++r) place = max(place, all[r].place);
+      total = 0.f;
+#pragma unroll
+      for (int r = 0; r < CL; ++r) total += join((float)all[r].s, all[r].place, place);
+    }
+  }
   if (cl.rank() == 0 && warp == 0) {
-#pragma unroll
-    for (int r = 0; r < CL; ++r) place = max(place, all[r].place);
-    total = 0.f;
-#pragma unroll
-    for (int r = 0; r < CL; ++r) total += join((float)all[r].s, place_key(all[r].place), place_key(place));
-    const int k = place_key(place);
-    const int best = greedy && k != kNoKey ? id_in_group<T>(row, shift, a.V, place_id(place), k) : -1;
+    const int k = place_key(place), best = k == kNoKey ? -1 : id_in_group<T>(row, shift, a.V, place_id(place), k);
     if (lane == 0) a.sums[t] = {(double)total, of_key(k), best};
   }
-  Cluster<CL>::barrier();                                  // nobody leaves while others read its box
+  if (CL > 1) Cluster<CL>::barrier();                      // nobody leaves while others read its box
 }
 
 // The walk and the next token.  CL blocks per sequence.
 constexpr int kWalkWarps = 16, kWalkThreads = 32 * kWalkWarps, kChunk = kWalkThreads;
+constexpr float kMargin = 1.f / 8192;     // of a test in 32 bits
 template <typename T, int CL>
 __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_constant__ VerifyArgs a, int room) {
   // The launch before this one in the stream is row_sums_kernel's, which let this one begin only after all earlier work was
   // done: the arguments can be read before waiting for it, its sums and the caller's outputs not.
-  constexpr int N = Vec<T>::N, kLoads = 4;
+  constexpr int N = Vec<T>::N, kLoads = 16 / N;            // groups of a warp at a time: 16 words of a lane
   extern __shared__ __align__(16) uint8_t smem[];
-  double *s_group = (double *)smem;                        // sums of this block's groups
-  float *s_most = (float *)(s_group + room);               // what they are relative to
-  uint8_t *s_out = (uint8_t *)(s_most + room);             // refused words of given drafts, a bit each: a byte per lane and group
-  __shared__ double s_table[kTable], s_p[kChunk], s_q[kChunk], s_warp[kWalkWarps];
+  double *s_group = (double *)smem;                        // sums of this block's groups: of 2^(c (x - m)), where p > A q after a refusal
+  double *s_near = s_group + room;                         // and of q there
+  uint8_t *s_out = (uint8_t *)(s_near + room);             // refused words of given drafts, a bit each: a byte per lane and group
+  __shared__ double s_table[kTable];
+  __shared__ double s_warp[2][3][kWalkWarps];              // what the warps hand to the cluster, in turn
+  __shared__ float s_p[kChunk], s_q[kChunk], s_u[kChunk];
   __shared__ int s_parent[kChunk];
-  __shared__ float s_u[kChunk];
-  __shared__ unsigned long long s_place[kWalkWarps];
-  __shared__ Joined s_box[2];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int seq = blockIdx.x / CL;
-  Cluster<CL> cl = {&s_box, 0};
-  const bool first_block = cl.rank() == 0;
+  const int seq = blockIdx.x / CL, rank = CL > 1 ? (int)(blockIdx.x % CL) : 0;
+  const bool first_block = rank == 0;
   const int2 rows = rows_of(a, seq);
   if (rows.y == 0) {
     pdl_grid_wait();
@@ -342,162 +345,201 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
   fill_table(s_table);
   const bool greedy = greedy_of(a, seq);
   const double c = rate_of(a, seq), c16 = 16 * c;
+  const float c32 = (float)fmin(c, 3e38);
   __syncthreads();
+  auto parent_of = [&](int k) { return a.parent ? a.parent[rows.x + k] : k - 1; };
 
   int cur = 0, length = 1;
-  RowSums sums = {0.0, 0.f, -1};                           // of row cur, where drafts hang on it
-  bool exact = greedy;                                     // sums.s is formed in 64 bits
-  double ratio = 1.0;                                      // what the p in hand are multiplied by: the sum that they were formed with to the exact one
-  double A = 0.0, R = 1.0;                                 // r = max(p - A q, 0), R = sum r (unless it is due)
-  double gone = 0.0;                                       // p of the refused tokens, where drafts are given
   int refused = 0;                                         // drafts refused at cur
-  bool due = false;
+  float gone = 0.f;                                        // p of the refused tokens, where drafts are given
+  double A = 0.0, R = 1.0;                                 // where they were drawn: r = max(p - A q, 0), R = sum r (unless it is due)
+  bool due = false, exact = false;                         // exact: sums.s is formed in 64 bits
+  RowSums sums = {0.0, 0.f, -1};                           // of row cur, once asked for
   const T *row;
-  int shift, groups, per, g0, g1;
-  auto enter = [&](int at) {
-    exact = greedy;
-    ratio = 1.0;
-    row = row_of<T>(a, rows.x + at);
+  int shift, groups, per, g0, g1, slot = 0;
+
+  // Sums of row cur's groups, of this block in s_group (and s_near), of every block in every thread.
+  double all_e[CL], all_p[CL], all_q[CL];                  // blocks: of 2^(c (x - m)); of it and of q where p > A q
+  auto pass = [&](auto rest, bool marked) {
+    sums = a.sums[rows.x + cur];
+    row = row_of<T>(a, rows.x + cur);
     shift = shift_of(row);
     groups = (a.V + shift + 32 * N - 1) / (32 * N);
     per = (groups + CL - 1) / CL;
-    g0 = min(cl.rank() * per, groups);
+    g0 = min(rank * per, groups);
     g1 = min(g0 + per, groups);
-  };
-
-  // Sums of the groups of row cur into s_group.  `rest`: of max(2^(c (x - m)) - cut q, 0) with the given m; else of
-  // 2^(c (x - m)), m the group's own largest (s_most), without the words marked in s_out if `marked`.  (Two stretches of code without
-  // questions inside: eight words' chains of 64-bit operations then run side by side.)
-  auto group_sums = [&](auto rest, bool marked, float m_row, double cut) {
+    const float m = sums.m, least = least_of(m, c);
+    const double cut = A * sums.s;
     const float *near = rest.value ? a.near + (int64_t)(rows.x + cur) * a.near_stride : nullptr;
+    double we = 0.0, wp = 0.0, wq = 0.0;
     for (int g = g0 + warp; g < g1; g += kWalkWarps * kLoads) {
       uint4 raw[kLoads];
+      float y[kLoads][N];
       if (g * 32 * N >= shift && (g + kWalkWarps * (kLoads - 1) + 1) * 32 * N - shift <= a.V && g + kWalkWarps * (kLoads - 1) < g1) {
         const uint4 *p = (const uint4 *)(row - shift) + g * 32 + lane;                  // all inside the row
 #pragma unroll
         for (int i = 0; i < kLoads; ++i) raw[i] = p[32 * kWalkWarps * i];
+        if (rest.value) {
+          const float *q = near + (g * 32 + lane) * N - shift;
+          if (((uintptr_t)q & 15) == 0) {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+              for (int k = 0; k < N; k += 4) *(float4 *)&y[i][k] = *(const float4 *)(q + 32 * kWalkWarps * N * i + k);
+          } else {
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+              for (int k = 0; k < N; ++k) y[i][k] = q[32 * kWalkWarps * N * i + k];
+          }
+        }
       } else {
         float none[N];
 #pragma unroll
         for (int k = 0; k < N; ++k) none[k] = kNone;
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-          raw[i] = g + kWalkWarps * i < g1 ? load_raw<T>(row, shift, a.V, g + kWalkWarps * i, lane) : Vec<T>::pack(none);
+        for (int i = 0; i < kLoads; ++i) {
+          const bool there = g + kWalkWarps * i < g1;
+          const int id = ((g + kWalkWarps * i) * 32 + lane) * N - shift;
+          raw[i] = there ? load_raw<T>(row, shift, a.V, g + kWalkWarps * i, lane) : Vec<T>::pack(none);
+          if (rest.value)
+#pragma unroll
+            for (int k = 0; k < N; ++k) y[i][k] = there && id + k >= 0 && id + k < a.V ? near[id + k] : 0.f;
+        }
       }
+      double e[kLoads][N], ep[kLoads], eq[kLoads];
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        const int gi = g + kWalkWarps * i;
-        if (gi >= g1) break;
         float x[N];
         Vec<T>::unpack(raw[i], x);
-        const uint32_t out = !rest.value && marked ? s_out[(gi - g0) * 32 + lane] : 0u;
-        int k1 = kNoKey;
+        const uint32_t out = !rest.value && marked && g + kWalkWarps * i < g1 ? s_out[(g + kWalkWarps * i - g0) * 32 + lane] : 0u;
 #pragma unroll
-        for (int k = 0; k < N; ++k) {
-          x[k] = (out >> k) & 1 ? kNone : eligible(x[k]);
-          k1 = max(k1, key_of(x[k]));
-        }
-        const float m = rest.value ? m_row : of_key(__reduce_max_sync(~0u, k1));
-        double sum = 0.0;
-        if (m != kNone && !greedy) {
-          const float least = least_of(m, c);
-          double e[N];
+        for (int k = 0; k < N; ++k) e[i][k] = pow2((out >> k) & 1 ? kNone : eligible(x[k]), m, c16, least, s_table);
+      }
+      if (rest.value) {
 #pragma unroll
-          for (int k = 0; k < N; ++k) e[k] = pow2(x[k], m, c16, least, s_table);
-          if (rest.value) {
-            const int id = (gi * 32 + lane) * N - shift;
+        for (int i = 0; i < kLoads; ++i) {
+          double p[N], q[N];
 #pragma unroll
-            for (int k = 0; k < N; ++k) e[k] = fmax(e[k] - cut * (double)(id + k >= 0 && id + k < a.V ? real(near[id + k]) : 0.f), 0.0);
+          for (int k = 0; k < N; ++k) {
+            const double z = (double)real(y[i][k]);
+            const bool over = e[i][k] > cut * z;
+            p[k] = over ? e[i][k] : 0.0;
+            q[k] = over ? z : 0.0;
           }
 #pragma unroll
           for (int o = 1; o < N; o <<= 1)
 #pragma unroll
-            for (int k = 0; k < N; k += 2 * o) e[k] += e[k + o];
-          sum = warp_sum(e[0]);
+            for (int k = 0; k < N; k += 2 * o) { p[k] += p[k + o]; q[k] += q[k + o]; }
+          ep[i] = p[0];
+          eq[i] = q[0];
         }
-        if (lane == 0) { s_group[gi - g0] = sum; s_most[gi - g0] = m; }
+      }
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+        for (int o = 1; o < N; o <<= 1)
+#pragma unroll
+          for (int k = 0; k < N; k += 2 * o) e[i][k] += e[i][k + o];
+#pragma unroll
+      for (int o = 16; o; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+          e[i][0] += __shfl_xor_sync(~0u, e[i][0], o);
+          if (rest.value) {
+            ep[i] += __shfl_xor_sync(~0u, ep[i], o);
+            eq[i] += __shfl_xor_sync(~0u, eq[i], o);
+          }
+        }
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        if (g + kWalkWarps * i >= g1) break;
+        if (lane == 0) {
+          s_group[g + kWalkWarps * i - g0] = rest.value ? ep[i] : e[i][0];
+          if (rest.value) s_near[g + kWalkWarps * i - g0] = eq[i];
+        }
+        we += e[i][0];
+        if (rest.value) { wp += ep[i]; wq += eq[i]; }
       }
     }
-    __syncthreads();
-  };
-  auto sum_groups = [&](bool rest, bool marked, float m_row, double cut) {
-    if (rest) group_sums(std::true_type(), false, m_row, cut);
-    else group_sums(std::false_type(), marked, 0.f, 0.0);
-  };
-  // this block's sum of s_group, the same in every thread
-  auto block_sum = [&]() {
-    double x = 0.0;
-    for (int i = tid; i < g1 - g0; i += kWalkThreads) x += s_group[i];
-    x = warp_sum(x);
-    if (lane == 0) s_warp[warp] = x;
-    __syncthreads();
-    x = 0.0;
-#pragma unroll
-    for (int w = 0; w < kWalkWarps; ++w) x += s_warp[w];
-    __syncthreads();
-    return x;
-  };
-  Joined all[CL];
-  double block_scale = 1.0;                                // of this block's s_group, to the whole's reference
-  unsigned long long place = 0;                            // this block's largest logit and its group
-  // What sum_groups has left, over all blocks; `rest` as there.
-  auto collect = [&](bool rest) {
-    if (!rest) {
-      // over the block's largest
-      unsigned long long best = place_of(kNoKey, 0);
-      for (int i = tid; i < g1 - g0; i += kWalkThreads) best = max(best, place_of(key_of(s_most[i]), g0 + i));
-      best = warp_max(best);
-      if (lane == 0) s_place[warp] = best;
-      __syncthreads();
-#pragma unroll
-      for (int w = 0; w < kWalkWarps; ++w) best = max(best, s_place[w]);
-      place = best;
-      const float top = of_key(place_key(best)), least = least_of(top, c);
-      if (!greedy)
-        for (int i = tid; i < g1 - g0; i += kWalkThreads)
-          if (s_group[i] > 0.0) s_group[i] *= pow2(s_most[i], top, c16, least, s_table);
-      __syncthreads();
+    slot ^= 1;
+    if (lane == 0) {
+      s_warp[slot][0][warp] = we;
+      if (rest.value) { s_warp[slot][1][warp] = wp; s_warp[slot][2][warp] = wq; }
     }
-    const double part = greedy ? 0.0 : block_sum();
-    cl.gather({part, place}, all);
-    unsigned long long whole = 0;
+    Cluster<CL>::barrier();                                // (the next pass writes to the other slot, the one after that behind its barrier)
+    constexpr int kRounds = (CL + 1) / 2;
+    double v[kRounds][3];
 #pragma unroll
-    for (int r = 0; r < CL; ++r) whole = max(whole, all[r].place);
-    double total = 0.0;
-    const float top = of_key(place_key(whole)), least = least_of(top, c);
+    for (int i = 0; i < kRounds; ++i)
+#pragma unroll
+      for (int k = 0; k < (rest.value ? 3 : 1); ++k) {
+        const double *from = &s_warp[slot][k][lane & 15];
+        if (CL == 1) {
+          v[i][k] = *from;
+        } else {
+          uint32_t q;
+          asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(q) : "r"((uint32_t)__cvta_generic_to_shared(from)), "r"(2 * i + (lane >> 4)));
+          asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v[i][k]) : "r"(q) : "memory");
+        }
+      }
+#pragma unroll
+    for (int o = 8; o; o >>= 1)
+#pragma unroll
+      for (int i = 0; i < kRounds; ++i)
+#pragma unroll
+        for (int k = 0; k < (rest.value ? 3 : 1); ++k) v[i][k] += __shfl_xor_sync(~0u, v[i][k], o);
 #pragma unroll
     for (int r = 0; r < CL; ++r) {
-      if (!rest && all[r].s > 0.0) all[r].s *= pow2(of_key(place_key(all[r].place)), top, c16, least, s_table);
-      if (r == cl.rank() && !rest && part > 0.0) block_scale = all[r].s / part;
-      total += all[r].s;
+      all_e[r] = __shfl_sync(~0u, v[r / 2][0], (r & 1) * 16);
+      if (rest.value) {
+        all_p[r] = __shfl_sync(~0u, v[r / 2][1], (r & 1) * 16);
+        all_q[r] = __shfl_sync(~0u, v[r / 2][2], (r & 1) * 16);
+      }
     }
-    if (greedy) place = whole;
-    return total;
   };
-  // The sum of row cur in 64 bits, where its 32 do not decide.
+  auto sum_of = [&](const double (&x)[CL]) {
+    double s = 0.0;
+#pragma unroll
+    for (int r = 0; r < CL; ++r) s += x[r];
+    return s;
+  };
+  // sums.s of row cur in 64 bits
   auto refine = [&]() {
     if (exact) return;
-    sums = a.sums[rows.x + cur];
-    if (sums.s > 0.0) {
-      sum_groups(false, false, 0.f, 0.0);
-      const double total = collect(false);
-      ratio = sums.s / total;
-      sums.s = total;
-    }
+    pass(std::false_type(), false);
+    sums.s = sum_of(all_e);
     exact = true;
   };
+  // the row's sum and what is left of it after the refusals so far, in units of 2^(c m)
+  auto left_over = [&]() {
+    pass(std::true_type(), false);
+    sums.s = sum_of(all_e);
+    exact = true;
+    const double left = sum_of(all_p) - A * sums.s * sum_of(all_q);
+    return left > 0.0 ? left : 0.0;
+  };
+  // p of a token at row cur, in 64 bits
+  auto p_of = [&](int token) {
+    if (greedy) return token == sums.best ? 1.0 : 0.0;
+    const float x = eligible(Vec<T>::one(row_of<T>(a, rows.x + cur) + token));
+    return x != kNone && sums.s > 0.0 ? pow2(x, sums.m, c16, least_of(sums.m, c), s_table) / sums.s : 0.0;
+  };
+  // whether one of the drafts [from, to) hangs on cur and has this token
+  auto named = [&](int from, int to, int token) {
+    bool yes = false;
+    for (int b = from; b < to && !yes; b += 32) yes = __any_sync(~0u, b + lane < to && parent_of(b + lane) == cur && a.tokens[rows.x + b + lane] == token);
+    return yes;
+  };
 
-  enter(0);
   if (rows.y == 1 || a.keep_stride == 1) pdl_grid_wait();
   for (int c0 = 0; c0 < rows.y && rows.y > 1 && length < a.keep_stride; c0 += kChunk) {
-    // what the tests of the next drafts need: p and q of each one's token at its parent's row
+    // what the tests of the next drafts need: p and q of each one's token at its parent's row, in 32 bits
     __syncthreads();
     const int j = c0 + tid, t = rows.x + j;
-    const bool mine = j < rows.y && j > 0;
     int up = -1, token = -1;
-    float x = kNone;
-    double q = 1.0;
-    if (mine) {
+    float x = kNone, q = 1.f, p = 0.f;
+    if (j < rows.y && j > 0) {
       up = a.parent ? a.parent[t] : j - 1;
       token = a.tokens[t];
       s_u[tid] = a.u[t];
@@ -506,17 +548,16 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
         up = -1;
       } else {
         x = eligible(Vec<T>::one(row_of<T>(a, rows.x + up) + token));
-        if (a.near) q = (double)real(a.near[(int64_t)(rows.x + up) * a.near_stride + token]);
+        if (a.near) q = real(a.near[(int64_t)(rows.x + up) * a.near_stride + token]);
       }
     }
     s_parent[tid] = up;
     s_q[tid] = q;
     if (c0 == 0) pdl_grid_wait();
-    double p = 0.0;
     if (up >= 0) {
-      const RowSums at = a.sums[rows.x + up];              // in 32 bits, see test()
-      if (greedy) p = token == at.best ? 1.0 : 0.0;
-      else if (x != kNone && at.s > 0.0) p = pow2(x, at.m, c16, least_of(at.m, c), s_table) / at.s;
+      const RowSums at = a.sums[rows.x + up];
+      if (greedy) p = token == at.best ? 1.f : 0.f;
+      else if (x != kNone && at.s > 0.0) p = ex2((x - at.m) * c32) / (float)at.s;
     }
     s_p[tid] = p;
     __syncthreads();
@@ -533,53 +574,58 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
         }
       }
       if (hit == kChunk) break;
-      bool again = false;                                  // a given token that an earlier draft here had is gone
-      if (!a.near && refused) {
-        const int token = a.tokens[rows.x + c0 + hit];
-        for (int b = cur + 1; b < c0 + hit && !again; b += 32) {
-          const int k = b + lane;
-          again = __any_sync(~0u, k < c0 + hit && (a.parent ? a.parent[rows.x + k] : k - 1) == cur && a.tokens[rows.x + k] == token);
-        }
-      }
-      if (a.near && due) {
-        refine();
-        double left = 0.0;
+      const bool again = !a.near && refused && named(cur + 1, c0 + hit, a.tokens[rows.x + c0 + hit]);      // a given token that is gone
+      if (due) {
+        double left;
         if (greedy) {
           // all of p lies on one word
           sums = a.sums[rows.x + cur];
+          exact = true;
           left = sums.best >= 0 ? fmax(1.0 - A * (double)real(a.near[(int64_t)(rows.x + cur) * a.near_stride + sums.best]), 0.0) : 0.0;
-        } else if (sums.s > 0.0) {
-          sum_groups(true, false, sums.m, A * sums.s);
-          left = collect(true) / sums.s;
+        } else {
+          left = left_over();
+          left = sums.s > 0.0 ? left / sums.s : 0.0;
         }
         R = left;
         due = false;
         if (!(R > 0.0)) { A = 0.0; R = 1.0; }              // nothing is left: the target's own distribution again
       }
-      double r, want;
-      const auto test = [&]() {
-        const double p = s_p[hit] * ratio;
-        if (!a.near) R = ratio * gone < 1.0 ? 1.0 - ratio * gone : 1.0;
-        r = again ? 0.0 : fmax(p - A * s_q[hit], 0.0);
-        want = (double)s_u[hit] * R * s_q[hit];
-        return want < r;
-      };
-      // A sum in 32 bits is off by at most 2^-14 of itself (20 times 2^-23 from the products' rounding where the words' own logarithms
-      // average 20 bits, and a step of 2^-24 for each of the additions of a lane): where that could turn the answer, 64 bits give it.
-      bool taken = test();
-      if (!exact && fabs(want - r) <= (1.0 / 8192) * ((double)s_u[hit] * s_q[hit] + s_p[hit])) {
-        refine();
-        taken = test();
+      // In 32 bits a row's sum is off by at most 2^-14 of itself (20 times 2^-23 from the products' rounding where the words' own logarithms
+      // average 20 bits, and a step of 2^-24 for each addition of a lane): where that could turn the answer, 64 bits give it.
+      bool taken;
+      {
+        const float p = s_p[hit], q = s_q[hit], u = s_u[hit], aq = (float)A * q;
+        const float rr = a.near ? (float)R : 1.f - gone;
+        const float r = again ? 0.f : p - aq, want = u * q * rr;
+        taken = want < r;
+        if (!(fabsf(want - r) > kMargin * (u * q * (a.near ? rr : 1.f) + p + aq)) || fmaxf(want, r) < 1e-30f) {
+          const int token = a.tokens[rows.x + c0 + hit];
+          if (greedy) {
+            sums = a.sums[rows.x + cur];
+            exact = true;
+          }
+          refine();
+          const double p64 = p_of(token), q64 = (double)q;
+          double r64 = again ? 0.0 : fmax(p64 - A * q64, 0.0), R64 = R;
+          if (!a.near) {
+            for (int k = cur + 1; k < c0 + hit; ++k) {     // without the refused tokens, each once
+              const int other = a.tokens[rows.x + k];
+              if (parent_of(k) == cur && other >= 0 && other < a.V && !named(cur + 1, k, other)) R64 -= p_of(other);
+            }
+            if (!(R64 > 0.0)) R64 = 1.0;
+          }
+          taken = (double)u * R64 * q64 < r64;
+        }
       }
       if (taken) {
         cur = c0 + hit;
-        enter(cur);
         if (first_block && tid == 0) a.keep[(int64_t)seq * a.keep_stride + length] = cur;
         ++length;
-        A = gone = 0.0;
+        A = 0.0;
         R = 1.0;
+        gone = 0.f;
         refused = 0;
-        due = false;
+        due = exact = false;
       } else {
         ++refused;
         if (a.near) {
@@ -598,127 +644,134 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
   }
 
   // the next token from row cur
-  const int mine = g1 - g0;
-  bool rest = a.near && A > 0.0 && !greedy;
-  bool marked = !a.near && refused > 0 && !greedy;
-  if (rest) {
-    refine();
-    rest = sums.s > 0.0;
-  }
-  if (marked) {
-    for (int i = tid; i < mine * 8; i += kWalkThreads) ((uint32_t *)s_out)[i] = 0u;
-    __syncthreads();
-    for (int k = cur + 1 + tid; k < rows.y; k += kWalkThreads) {
-      const int token = a.tokens[rows.x + k];
-      if ((a.parent ? a.parent[rows.x + k] : k - 1) == cur && token >= 0 && token < a.V) {
-        const int w = token + shift - g0 * 32 * N;         // place in this block's words
-        if (w >= 0 && w < mine * 32 * N) atomicOr((uint32_t *)s_out + (w / N) / 4, 1u << (((w / N) & 3) * 8 + w % N));
-      }
-    }
-    __syncthreads();
-  }
-  double total;
-  for (;;) {
-    sum_groups(rest, marked, sums.m, A * sums.s);
-    total = collect(rest);
-    if (greedy || total > 0.0 || !(rest || marked)) break;
-    rest = marked = false;                                 // nothing is left: the target's own distribution
-  }
   if (greedy) {
-    const int key = place_key(place);
-    if (first_block && warp == 0) {
-      const int id = key == kNoKey ? -1 : id_in_group<T>(row, shift, a.V, place_id(place), key);
-      if (lane == 0) a.next[seq] = id;
-    }
-  } else if (!(total > 0.0)) {
-    if (first_block && tid == 0) a.next[seq] = -1;
+    if (first_block && tid == 0) a.next[seq] = a.sums[rows.x + cur].best;
   } else {
-    // the block, the group and the word in which the sum passes the target
-    const double target = (double)a.u_next[seq] * total;
-    double before = 0.0;
-    int owner = -1;
-#pragma unroll
-    for (int r = 0; r < CL; ++r) {
-      if (owner < 0 && before + all[r].s > target) owner = r;
-      if (owner < 0) before += all[r].s;
-    }
-    if (owner < 0) {                                       // rounding, or u_next at 1: the last word with any weight
-      before = INFINITY;
-#pragma unroll
-      for (int r = 0; r < CL; ++r)
-        if (all[r].s > 0.0) owner = r;
-    }
-    if (owner == cl.rank() && warp == 0) {
-      const double goal = before == INFINITY ? INFINITY : (target - before) / (rest ? 1.0 : block_scale);
-      const int each = (mine + 31) / 32;
-      double sum = 0.0;
-      int last = -1;                                       // the last group with any weight
-      for (int i = lane * each; i < min((lane + 1) * each, mine); ++i) {
-        sum += s_group[i];
-        if (s_group[i] > 0.0) last = i;
-      }
-      double upto = sum;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const double y = __shfl_up_sync(~0u, upto, o);
-        if (lane >= o) upto += y;
-      }
-      const uint32_t past = __ballot_sync(~0u, upto > goal);
-      int g = __reduce_max_sync(~0u, last);
-      double base = INFINITY;                              // all of that group
-      if (past) {
-        const int l = __ffs(past) - 1;
-        base = __shfl_sync(~0u, upto - sum, l);
-        int found = -1;
-        for (int i = l * each; i < min((l + 1) * each, mine); ++i) {
-          if (base + s_group[i] > goal) {
-            found = i;
-            break;
-          }
-          base += s_group[i];
+    bool rest = a.near && A > 0.0, marked = !a.near && refused > 0;
+    if (marked) {
+      row = row_of<T>(a, rows.x + cur);
+      shift = shift_of(row);
+      per = ((a.V + shift + 32 * N - 1) / (32 * N) + CL - 1) / CL;
+      for (int i = tid; i < per * 8; i += kWalkThreads) ((uint32_t *)s_out)[i] = 0u;
+      __syncthreads();
+      for (int k = cur + 1 + tid; k < rows.y; k += kWalkThreads) {
+        const int token = a.tokens[rows.x + k];
+        if (parent_of(k) == cur && token >= 0 && token < a.V) {
+          const int w = token + shift - rank * per * 32 * N;         // place in this block's words
+          if (w >= 0 && w < per * 32 * N) atomicOr((uint32_t *)s_out + (w / N) / 4, 1u << (((w / N) & 3) * 8 + w % N));
         }
-        if (found >= 0) g = found;
-        else base = INFINITY;
       }
-      const float m = s_most[g];
-      const float top = of_key(place_key(place));
-      const double scale = rest ? 1.0 : pow2(m, top, c16, least_of(top, c), s_table);
-      const double left = base == INFINITY ? INFINITY : (goal - base) / scale;
-      float x[N];
-      load_words<T>(row, shift, a.V, g0 + g, lane, x);
-      const uint32_t out = marked ? s_out[g * 32 + lane] : 0u;
-      const float *near = rest ? a.near + (int64_t)(rows.x + cur) * a.near_stride : nullptr;
-      const int id = ((g0 + g) * 32 + lane) * N - shift;
-      const float least = least_of(m, c);
-      double e[N], lane_sum = 0.0;
-      int last_word = -1;
+      __syncthreads();
+    }
+    double part[CL], total;                                // what the token is drawn from, block by block
+    if (rest) {
+      total = left_over();
 #pragma unroll
-      for (int k = 0; k < N; ++k) {
-        const float y = (out >> k) & 1 ? kNone : eligible(x[k]);
-        e[k] = pow2(y, m, c16, least, s_table);
-        if (rest) e[k] = fmax(e[k] - A * sums.s * (double)(id + k >= 0 && id + k < a.V ? real(near[id + k]) : 0.f), 0.0);
-        lane_sum += e[k];
-        if (e[k] > 0.0) last_word = id + k;
+      for (int r = 0; r < CL; ++r) part[r] = fmax(all_p[r] - A * sums.s * all_q[r], 0.0);
+      if (!(total > 0.0)) rest = false;                    // nothing is left: the target's own distribution
+    }
+    if (!rest) {
+      pass(std::false_type(), marked);
+      total = sum_of(all_e);
+      if (marked && !(total > 0.0)) {
+        marked = false;
+        __syncthreads();                                   // the sums are read before they are formed again
+        pass(std::false_type(), false);
       }
-      double incl = lane_sum;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const double y = __shfl_up_sync(~0u, incl, o);
-        if (lane >= o) incl += y;
-      }
-      int pick = INT_MAX;
-      double run = incl - lane_sum;
+      for (int r = 0; r < CL; ++r) part[r] = all_e[r];
+    }
+    total = sum_of(part);
+    if (!(total > 0.0)) {
+      if (first_block && tid == 0) a.next[seq] = -1;
+    } else {
+      // the block, the group and the word in which the sum passes the target
+      const double target = (double)a.u_next[seq] * total;
+      double before = 0.0;
+      int owner = -1;
 #pragma unroll
-      for (int k = 0; k < N; ++k) {
-        run += e[k];
-        if (e[k] > 0.0 && run > left && pick == INT_MAX) pick = id + k;
+      for (int r = 0; r < CL; ++r) {
+        if (owner < 0 && before + part[r] > target) owner = r;
+        if (owner < 0) before += part[r];
       }
-      const int lowest = (int)__reduce_min_sync(~0u, (unsigned)pick);
-      const int highest = __reduce_max_sync(~0u, last_word);
-      if (lane == 0) a.next[seq] = lowest == INT_MAX ? highest : lowest;
+      if (owner < 0) {                                     // rounding, or u_next at 1: the last word with any weight
+        before = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < CL; ++r)
+          if (part[r] > 0.0) owner = r;
+      }
+      if (owner == rank && warp == 0) {
+        const double goal = target - before, cut = A * sums.s;      // +inf: all of it
+        const int mine = g1 - g0, each = (mine + 31) / 32;
+        auto group_at = [&](int i) { return rest ? fmax(s_group[i] - cut * s_near[i], 0.0) : s_group[i]; };
+        double sum = 0.0;
+        int last = -1;                                     // the last group with any weight
+        for (int i = lane * each; i < min((lane + 1) * each, mine); ++i) {
+          const double x = group_at(i);
+          sum += x;
+          if (x > 0.0) last = i;
+        }
+        double upto = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const double y = __shfl_up_sync(~0u, upto, o);
+          if (lane >= o) upto += y;
+        }
+        const uint32_t past = __ballot_sync(~0u, upto > goal);
+        int g = __reduce_max_sync(~0u, last);
+        double left = INFINITY;                            // what is to be passed inside of the group
+        if (past) {
+          const int l = __ffs(past) - 1;
+          double base = __shfl_sync(~0u, upto - sum, l);
+          int found = -1;
+          for (int i = l * each; i < min((l + 1) * each, mine); ++i) {
+            const double x = group_at(i);
+            if (base + x > goal) {
+              found = i;
+              break;
+            }
+            base += x;
+          }
+          if (found >= 0) {
+            g = found;
+            left = goal - base;
+          }
+        }
+        float x[N];
+        load_words<T>(row, shift, a.V, g0 + g, lane, x);
+        const uint32_t out = marked ? s_out[g * 32 + lane] : 0u;
+        const float *near = rest ? a.near + (int64_t)(rows.x + cur) * a.near_stride : nullptr;
+        const int id = ((g0 + g) * 32 + lane) * N - shift;
+        const float least = least_of(sums.m, c);
+        double e[N], lane_sum = 0.0;
+        int last_word = -1;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          e[k] = pow2((out >> k) & 1 ? kNone : eligible(x[k]), sums.m, c16, least, s_table);
+          if (rest) e[k] = fmax(e[k] - cut * (double)(id + k >= 0 && id + k < a.V ? real(near[id + k]) : 0.f), 0.0);
+          lane_sum += e[k];
+          if (e[k] > 0.0) last_word = id + k;
+        }
+        double incl = lane_sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const double y = __shfl_up_sync(~0u, incl, o);
+          if (lane >= o) incl += y;
+        }
+        int pick = INT_MAX;
+        double run = incl - lane_sum;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+          run += e[k];
+          if (e[k] > 0.0 && run > left && pick == INT_MAX) pick = id + k;
+        }
+        const int lowest = (int)__reduce_min_sync(~0u, (unsigned)pick);
+        const int highest = __reduce_max_sync(~0u, last_word);
+        if (lane == 0) a.next[seq] = lowest == INT_MAX ? highest : lowest;
+      }
     }
   }
-  Cluster<CL>::barrier();                                  // nobody leaves while others read its box
+  Cluster<CL>::barrier();                                  // nobody leaves while others read its sums
 }
 
 template <typename... K, typename... A>
@@ -753,10 +806,10 @@ pcomoe_status launch_walk(const VerifyArgs &a, int groups, cudaStream_t st) {
   int dev = -1;
   PCOMOE_CUDA_TRY(cudaGetDevice(&dev));
   if (once.first_use(dev)) {
-    PCOMOE_CUDA_TRY(cudaFuncSetAttribute(walk_kernel<T, CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxGroups * (8 + 4 + 32)));
+    PCOMOE_CUDA_TRY(cudaFuncSetAttribute(walk_kernel<T, CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxGroups * (8 + 8 + 32)));
     once.done(dev);
   }
-  PCOMOE_CUDA_TRY(launch_clusters(walk_kernel<T, CL>, a.n, CL, kWalkThreads, (size_t)room * (8 + 4 + 32), st, a, room));
+  PCOMOE_CUDA_TRY(launch_clusters(walk_kernel<T, CL>, a.n, CL, kWalkThreads, (size_t)room * (8 + 8 + 32), st, a, room));
   count_launch();
   return PCOMOE_OK;
 }
