@@ -1,10 +1,11 @@
 // Eviction from the paged cache by accumulated weight: which positions stay, their rows moved up in order, pages freed.
 //
-// Three launches.  The first, a block per sequence, finds the weight of the last position that stays by four rounds over its
-// bits (a histogram of 256 bins each, from the top), lists the places that stay in order and moves the weights.  The second moves the
-// rows: a block owns a column of 64 bytes of one head's rows in one layer, K or V, and walks over them in ascending windows; the
-// places ascend and a row never moves up past itself, so a window only has to be read whole before it is written, and
-// nothing that a later window reads is overwritten.  The third gives back the pages.
+// Three launches.  The first, a cluster of blocks per sequence, finds the weight of the last position that stays by four rounds
+// over its bits (a histogram of 256 bins each, from the top, added over the blocks), lists the places that stay in order, as rows of
+// the pool, and moves the weights.  The second moves the rows: a block owns a column of 64 bytes of one head's rows in one layer, K
+// or V, and walks over them in ascending windows; the places ascend and a row never moves up past itself, so a window only has
+// to be read whole before it is written, and nothing that a later window reads is overwritten: the next window's rows come in
+// while this one's are stored.  The third gives back the pages.
 // What bounds it: the moved rows, read and written once (HBM); few sequences in few layers leave few columns to walk over.
 #include <algorithm>
 
@@ -23,7 +24,8 @@ struct EvictSeq {                          // what the first launch leaves for t
 struct EvictWs {
   CacheHeader *head;
   EvictSeq *seq;                           // [n]
-  int32_t *list;                           // [n][room] places that stay
+  int32_t *list;                           // [n][room] rows that stay: page * page_size + place in it
+  float *kept;                             // [n][room] their weights
   int64_t room;
   size_t total;
 };
@@ -34,8 +36,10 @@ EvictWs evict_ws(const pcomoe_cache *c, int32_t n, void *ws) {
   const size_t seqs = align256(sizeof(EvictSeq) * (size_t)n);
   w.head = (CacheHeader *)ws;
   w.seq = (EvictSeq *)((char *)ws + 256);
+  const size_t lists = align256(4 * (size_t)n * (size_t)w.room);
   w.list = (int32_t *)((char *)ws + 256 + seqs);
-  w.total = 256 + seqs + align256(4 * (size_t)n * (size_t)w.room);
+  w.kept = (float *)((char *)ws + 256 + seqs + lists);
+  w.total = 256 + seqs + 2 * lists;
   return w;
 }
 
@@ -46,30 +50,39 @@ __device__ __forceinline__ uint32_t heaviness(float w) {
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 
-// Exclusive prefix over the warps of one value per warp.  s: 33 ints.
-__device__ __forceinline__ int warps_before(int x, int *s) {
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  if (lane == 0) s[w] = x;
-  __syncthreads();
-  const int y = __reduce_add_sync(~0u, lane < w ? s[lane] : 0);
-  __syncthreads();
-  return y;
+// A word of another block of the cluster, and the cluster's barrier; one block: its own.
+template <int CL>
+__device__ __forceinline__ int of_block(const int *p, int rank) {
+  if (CL == 1) return *p;
+  uint32_t q;
+  int v;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(q) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(q) : "memory");
+  return v;
+}
+template <int CL>
+__device__ __forceinline__ void all_blocks() {
+  if (CL > 1) asm volatile("barrier.cluster.arrive.aligned;\n\tbarrier.cluster.wait.aligned;" ::: "memory");
+  else __syncthreads();
 }
 
+template <int CL>
 __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(CacheDev c, int n, const int32_t *seqs, const int32_t *budget, int sinks, int recent,
                                                                       float *weight, int64_t weight_stride, EvictWs ws) {
   pdl_grid_wait();
-  static_assert(kSelectThreads == 1024, "a warp's lanes stand for the warps");
-  __shared__ int s_bin[256], s_scan[33], s_pick, s_rest, s_first;
-  const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  constexpr int kWarps = kSelectThreads / 32;
+  static_assert(kWarps == 32, "a warp's lanes stand for the warps");
+  __shared__ int s_bin[2][256], s_all[256], s_warp[2][kWarps], s_pick, s_rest, s_first;
+  const int i = blockIdx.x / CL, rank = CL > 1 ? (int)(blockIdx.x % CL) : 0, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   EvictSeq *out = ws.seq + i;
+  // (every block of the cluster comes to the same answers)
   bool ok = alone(seqs, n, i, c.max_seqs);
   const int id = seqs[i], L = ok ? c.len[id] : 0, B = budget[i];
   ok = ok && B >= 0 && L >= 0 && pages_of(c, L) <= c.max_pages;
   const bool cuts = ok && L > B;
   if (cuts && (int64_t)sinks + recent > B) ok = false;
   if (!ok || !cuts) {
-    if (tid == 0) {
+    if (tid == 0 && rank == 0) {
       out->left = -1;
       if (!ok) flag(ws.head, PCOMOE_ERR_INDEX);
     }
@@ -77,6 +90,8 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(CacheDev c
   }
   float *w = weight + id * weight_stride;
   const int lo = sinks, hi = L - recent, need = B - sinks - recent;      // `need` of the positions [lo, hi) stay, fewer than there are
+  // a run of positions for every warp of the cluster, in order
+  const int run = ((L + 1024 * CL - 1) / (1024 * CL)) * 32, p0 = min((rank * kWarps + warp) * run, L), p1 = min(p0 + run, L);
   // the key of the last one that stays, from its upper bits down, and how many with this key stay
   uint32_t key = 0xffffffffu;
   int equal = 0;
@@ -85,17 +100,26 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(CacheDev c
     equal = need;
     for (int round = 0; round < 4; ++round) {
       const int sh = 24 - 8 * round;
-      for (int b = tid; b < 256; b += kSelectThreads) s_bin[b] = 0;
+      int *bin = s_bin[round & 1];
+      for (int b = tid; b < 256; b += kSelectThreads) bin[b] = 0;
       __syncthreads();
-      for (int p = lo + tid; p < hi; p += kSelectThreads) {
+#pragma unroll 4
+      for (int p = max(p0, lo) + lane; p < min(p1, hi); p += 32) {
         const uint32_t k = heaviness(w[p]);
-        if (round == 0 || (k >> (sh + 8)) == (key >> (sh + 8))) atomicAdd(&s_bin[(k >> sh) & 255], 1);
+        if (round == 0 || (k >> (sh + 8)) == (key >> (sh + 8))) atomicAdd(&bin[(k >> sh) & 255], 1);
+      }
+      all_blocks<CL>();                                    // (two rounds on the bins are cleared again: all have read them by then)
+      if (tid < 256) {
+        int sum = 0;
+#pragma unroll
+        for (int r = 0; r < CL; ++r) sum += of_block<CL>(&bin[tid], r);
+        s_all[tid] = sum;
       }
       __syncthreads();
       if (warp == 0) {
         // lane l: bins 255 - 8 l down; the bin in which the count passes `equal`
         int mine = 0;
-        for (int b = 0; b < 8; ++b) mine += s_bin[255 - 8 * lane - b];
+        for (int b = 0; b < 8; ++b) mine += s_all[255 - 8 * lane - b];
         int upto = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -105,7 +129,7 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(CacheDev c
         const uint32_t past = __ballot_sync(~0u, upto >= equal);
         if (lane == __ffs(past) - 1) {
           int before = upto - mine, b = 0;
-          while (before + s_bin[255 - 8 * lane - b] < equal) before += s_bin[255 - 8 * lane - b++];
+          while (before + s_all[255 - 8 * lane - b] < equal) before += s_all[255 - 8 * lane - b++];
           s_pick = 255 - 8 * lane - b;
           s_rest = equal - before;
         }
@@ -113,11 +137,9 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(CacheDev c
       __syncthreads();
       key |= (uint32_t)s_pick << sh;
       equal = s_rest;
-      __syncthreads();
     }
   }
-  // the places that stay: every warp has a run of positions, counts its own, then lists them
-  const int run = ((L + 1023) / 1024) * 32, p0 = min(warp * run, L), p1 = min(p0 + run, L);
+  // the places that stay: every warp counts those of its run, then lists them
   int sure = 0, ties = 0;
   auto look = [&](int p, bool &stays, bool &tie) {
     stays = tie = false;
@@ -131,19 +153,31 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(CacheDev c
       }
     }
   };
+#pragma unroll 4
   for (int p = p0; p < p1; p += 32) {
     bool stays, tie;
     look(p + lane, stays, tie);
     sure += __popc(__ballot_sync(~0u, stays));
     ties += __popc(__ballot_sync(~0u, tie));
   }
-  int tie_at = warps_before(ties, s_scan);
+  // what the warps before this one of the whole cluster have
+  auto before = [&](int (&box)[kWarps], int x) {
+    if (lane == 0) box[warp] = x;
+    all_blocks<CL>();
+    int y = 0;
+#pragma unroll
+    for (int r = 0; r < CL; ++r)
+      if (r < rank || (r == rank && lane < warp)) y += of_block<CL>(&box[lane], r);
+    return (int)__reduce_add_sync(~0u, y);
+  };
+  int tie_at = before(s_warp[0], ties);
   const int own_ties = min(max(equal - tie_at, 0), ties);
-  int at = warps_before(sure + own_ties, s_scan);
-  int32_t *list = ws.list + i * ws.room;
   if (tid == 0) s_first = B;
-  __syncthreads();
-  int first = B;
+  int at = before(s_warp[1], sure + own_ties);
+  const int32_t *row = c.table + (int64_t)id * c.max_pages;
+  int32_t *list = ws.list + i * ws.room;
+  float *kept = ws.kept + i * ws.room;
+  int first = B, bad = 0;
   for (int p = p0; p < p1; p += 32) {
     bool stays, tie;
     look(p + lane, stays, tie);
@@ -153,75 +187,93 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(CacheDev c
     const uint32_t b = __ballot_sync(~0u, stays);
     const int j = at + __popc(b & below);
     if (stays) {
-      list[j] = p + lane;
-      if (j != p + lane) first = min(first, j);
+      const int page = row[(p + lane) >> c.shift];
+      bad |= page < 0 || page >= c.pages;
+      list[j] = page * c.page + ((p + lane) & (c.page - 1));
+      kept[j] = w[p + lane];
+      if (j != p + lane) {
+        first = min(first, j);
+        // a page that is written to is this sequence's alone
+        const int to = row[j >> c.shift];
+        bad |= to < 0 || to >= c.pages || c.ref[min(max(to, 0), c.pages - 1)] != 1;
+      }
     }
     at += __popc(b);
   }
+  // and all pages that are given back are pages
+  for (int s = pages_of(c, B) + rank * kSelectThreads + tid; s < pages_of(c, L); s += CL * kSelectThreads) bad |= row[s] < 0 || row[s] >= c.pages;
   first = __reduce_min_sync(~0u, first);
-  if (lane == 0) atomicMin(&s_first, first);
-  __syncthreads();
-  first = s_first;
-  // the pages written to are this sequence's alone, and all are pages
-  const int32_t *row = c.table + (int64_t)id * c.max_pages;
-  int bad = 0;
-  for (int s = (first >> c.shift) + tid; s < pages_of(c, L); s += kSelectThreads) {
-    const int page = row[s];
-    bad |= page < 0 || page >= c.pages || (s < pages_of(c, B) && first < B && c.ref[page] != 1);
+  bad = __any_sync(~0u, bad);
+  if (lane == 0) {
+    atomicMin(&s_first, first);
+    if (bad) atomicMin(&s_first, -1);
   }
-  if (__syncthreads_or(bad)) {
-    if (tid == 0) {
-      out->left = -1;
-      flag(ws.head, PCOMOE_ERR_INDEX);
-    }
-    return;
-  }
-  // the weights move as the rows do: a window is read before it is written
-  for (int j0 = first; j0 < B; j0 += 4 * kSelectThreads) {
-    float x[4];
+  all_blocks<CL>();
+  first = B;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int j = j0 + k * kSelectThreads + tid;
-      if (j < B) x[k] = w[list[j]];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int j = j0 + k * kSelectThreads + tid;
-      if (j < B) w[j] = x[k];
-    }
-    __syncthreads();
+  for (int r = 0; r < CL; ++r) first = min(first, of_block<CL>(&s_first, r));
+  if (rank == 0 && tid == 0) {
+    out->left = first < 0 ? -1 : B;
+    out->first = first;
+    if (first < 0) flag(ws.head, PCOMOE_ERR_INDEX);
   }
-  if (tid == 0) { out->left = B; out->first = first; }
+  all_blocks<CL>();                                        // nobody leaves while others read its first
 }
 
-// blockIdx: (head and column, layer and K or V, sequence)
+// blockIdx: (head and column, layer and K or V, sequence); one column more, for the first layer's K, moves the weights.
 constexpr int kColumn = 4;                                 // 16-byte pieces of a row that a block moves
-__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(CacheDev c, const int32_t *seqs, EvictWs ws) {
+__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(CacheDev c, const int32_t *seqs, float *weight, int64_t weight_stride, EvictWs ws) {
   pdl_grid_wait();
-  constexpr int kRows = kMoveThreads / kColumn, U = 8;
+  constexpr int kRows = kMoveThreads / kColumn, U = 8, kWindow = kRows * U;
   const int i = blockIdx.z;
   const EvictSeq s = ws.seq[i];
   if (s.left < 0 || s.first >= s.left) return;
+  const int id = seqs[i];
   const int parts = (c.chunks + kColumn - 1) / kColumn, head = blockIdx.x / parts, chunk = (blockIdx.x % parts) * kColumn + threadIdx.x % kColumn;
+  if (head >= c.kv_heads) {
+    if (blockIdx.y) return;
+    for (int j = s.first + threadIdx.x; j < s.left; j += kMoveThreads) weight[id * weight_stride + j] = ws.kept[i * ws.room + j];
+    return;
+  }
   const bool has = chunk < c.chunks;
   const int layer = blockIdx.y >> 1;
   char *pool = (blockIdx.y & 1 ? c.v : c.k) + (int64_t)layer * c.pages * c.page_bytes + ((int64_t)head * c.page * c.chunks + chunk) * 16;
-  const int32_t *row = c.table + (int64_t)seqs[i] * c.max_pages, *list = ws.list + i * ws.room;
-  auto place = [&](int p) { return (uint4 *)(pool + (int64_t)row[p >> c.shift] * c.page_bytes + (int64_t)(p & (c.page - 1)) * c.chunks * 16); };
+  const int32_t *row = c.table + (int64_t)id * c.max_pages, *list = ws.list + i * ws.room;
+  const int64_t row_bytes = (int64_t)c.chunks * 16;
+  auto place = [&](int page, int slot) { return pool + (int64_t)page * c.page_bytes + slot * row_bytes; };
   const int r = threadIdx.x / kColumn;
-  for (int j0 = s.first; j0 < s.left; j0 += kRows * U) {
-    uint4 x[U];
+  // Three windows at work: the places of one are asked for, the rows of the one before come in, those of the one before that are stored.
+  int from[U], to[U], to_next[U];
+  uint4 x[U];
+  auto ask = [&](int j0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int j = j0 + u * kRows + r;
-      if (has && j < s.left) x[u] = *place(list[j]);
+      from[u] = has && j < s.left ? list[j] : -1;
+      to_next[u] = has && j < s.left ? row[j >> c.shift] : 0;
     }
+  };
+  auto fetch = [&]() {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (from[u] >= 0) x[u] = *(const uint4 *)place(from[u] >> c.shift, from[u] & (c.page - 1));
+      to[u] = to_next[u];
+    }
+  };
+  ask(s.first);
+  fetch();
+  for (int j0 = s.first; j0 < s.left; j0 += kWindow) {
+    ask(j0 + kWindow);
     __syncthreads();                                       // the window is read
+    uint4 y[U];
+    int at[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) { y[u] = x[u]; at[u] = to[u]; }
+    fetch();                                               // of the next one: its rows lie behind all that is written now
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int j = j0 + u * kRows + r;
-      if (has && j < s.left) *place(j) = x[u];
+      if (has && j < s.left) *(uint4 *)place(at[u], j & (c.page - 1)) = y[u];
     }
   }
 }
@@ -234,6 +286,26 @@ __global__ void __launch_bounds__(256) evict_book_kernel(CacheDev c, const int32
   drop_pages(c, id, c.len[id], left);
   __syncthreads();
   if (threadIdx.x == 0) c.len[id] = left;
+}
+
+template <int CL>
+pcomoe_status launch_select(const CacheDev &c, int n, const int32_t *seqs, const int32_t *budget, int sinks, int recent, float *weight, int64_t weight_stride,
+                            const EvictWs &ws, cudaStream_t st) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)n * CL);
+  cfg.blockDim = dim3(kSelectThreads);
+  cfg.stream = st;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  attr[1].id = cudaLaunchAttributeClusterDimension;
+  attr[1].val.clusterDim.x = CL;
+  attr[1].val.clusterDim.y = 1;
+  attr[1].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = CL > 1 ? 2 : 1;
+  PCOMOE_CUDA_TRY(cudaLaunchKernelEx(&cfg, evict_select_kernel<CL>, c, n, seqs, budget, sinks, recent, weight, weight_stride, ws));
+  return PCOMOE_OK;
 }
 
 }  // namespace
@@ -255,7 +327,7 @@ pcomoe_status pcomoe_evict_workspace_bytes(const pcomoe_cache *cache, int32_t n,
 
 pcomoe_status pcomoe_cache_evict(const pcomoe_cache *cache, int32_t n, const int32_t *d_seqs, const int32_t *d_budget, int32_t sinks, int32_t recent,
                                  float *d_weight, int64_t weight_stride, void *d_workspace, size_t ws_bytes, void *stream) {
-  const pcomoe_status st = check_cache(cache);
+  pcomoe_status st = check_cache(cache);
   if (st != PCOMOE_OK) return st;
   if (n < 0 || sinks < 0 || recent < 0) return PCOMOE_ERR_INVALID_ARG;
   if (n > cache->max_seqs || cache->layers > 32767) return PCOMOE_ERR_SHAPE;
@@ -264,12 +336,23 @@ pcomoe_status pcomoe_cache_evict(const pcomoe_cache *cache, int32_t n, const int
   if (!d_seqs || !d_budget || !d_weight || weight_stride < (int64_t)cache->max_pages * cache->page_size) return PCOMOE_ERR_INVALID_ARG;
   const CacheDev c = cache_dev(cache);
   const EvictWs w = evict_ws(cache, n, d_workspace);
-  const int64_t columns = (int64_t)c.kv_heads * ((c.chunks + kColumn - 1) / kColumn);
+  const int64_t columns = (int64_t)c.kv_heads * ((c.chunks + kColumn - 1) / kColumn) + 1;
   if (columns > INT32_MAX) return PCOMOE_ERR_SHAPE;
-  PCOMOE_CUDA_TRY(launch_pdl(evict_select_kernel, dim3(n), dim3(kSelectThreads), 0, (cudaStream_t)stream, c, n, d_seqs, d_budget, sinks, recent, d_weight,
-                             weight_stride, w));
-  PCOMOE_CUDA_TRY(launch_pdl(evict_move_kernel, dim3((unsigned)columns, 2 * c.layers, n), dim3(kMoveThreads), 0, (cudaStream_t)stream, c, d_seqs, w));
-  PCOMOE_CUDA_TRY(launch_pdl(evict_book_kernel, dim3(n), dim3(256), 0, (cudaStream_t)stream, c, d_seqs, w));
+  int sms;
+  if ((st = current_sms(&sms)) != PCOMOE_OK) return st;
+  // Blocks of a cluster: a sequence may have more than 4096 positions for each, and the GPU two blocks for every SM.
+  int cl = 1;
+  while (cl < 8 && w.room > 4096 * cl && (int64_t)n * 2 * cl <= 2 * sms) cl *= 2;
+  const cudaStream_t s = (cudaStream_t)stream;
+  switch (cl) {
+    case 1: st = launch_select<1>(c, n, d_seqs, d_budget, sinks, recent, d_weight, weight_stride, w, s); break;
+    case 2: st = launch_select<2>(c, n, d_seqs, d_budget, sinks, recent, d_weight, weight_stride, w, s); break;
+    case 4: st = launch_select<4>(c, n, d_seqs, d_budget, sinks, recent, d_weight, weight_stride, w, s); break;
+    default: st = launch_select<8>(c, n, d_seqs, d_budget, sinks, recent, d_weight, weight_stride, w, s); break;
+  }
+  if (st != PCOMOE_OK) return st;
+  PCOMOE_CUDA_TRY(launch_pdl(evict_move_kernel, dim3((unsigned)columns, 2 * c.layers, n), dim3(kMoveThreads), 0, s, c, d_seqs, d_weight, weight_stride, w));
+  PCOMOE_CUDA_TRY(launch_pdl(evict_book_kernel, dim3(n), dim3(256), 0, s, c, d_seqs, w));
   count_launch(3);
   return PCOMOE_OK;
 }

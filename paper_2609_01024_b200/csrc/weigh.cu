@@ -30,6 +30,7 @@ constexpr int kQBytes = 48 * 1024;      // queries held at a time
 //   4 sequences of 16384   38.3, 106   80.9, 107    136, 107   266, 98.7   898, 144
 //   8 sequences of 300     14.6, 18.7  28.9, 18.9  41.2, 19.5  86.2, 18.7  321, 24.8
 constexpr int kManyColumns = 64;
+constexpr int kDeep = 2;                // blocks of keys for each block of the grid that make larger ones worth it
 constexpr int kExtra = 2;               // cost of a block of keys besides its columns, in tiles of 8 columns
 
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -38,7 +39,7 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// 16 keys of a head in registers, and their weights over the columns [0, tiles * 8) at q, lse, lim (lim: the last position that
+// 16 keys of a head in registers, and their weights over the columns [0, cols) at q, lse, lim (laid out in tiles of 8) (lim: the last position that
 // a column sees).  key0: position of the first.  Lane 0..15 of the result: key0 + lane.
 template <typename T, int D> struct Piece;
 
@@ -55,11 +56,11 @@ template <int D> struct Piece<__nv_bfloat16, D> {
   }
   // place of the 16 bytes c of column col in the layout that sums() reads: a tile of 8 columns, step by step, lane by lane
   static __device__ __forceinline__ int place(int col, int c) { return (((col >> 3) * (D / 32) + (c >> 2)) * 32 + (col & 7) * 4 + (c & 3)) * 16; }
-  __device__ __forceinline__ float sums(const char *q, const float *lse, const int *lim, int tiles, int key0, float scale) const {
+  __device__ __forceinline__ float sums(const char *q, const float *lse, const int *lim, int cols, int key0, float scale) const {
     const int lane = threadIdx.x & 31;
     const int p0 = key0 + (lane >> 2), p1 = p0 + 8;
     float w0 = 0.f, w1 = 0.f;
-    for (int t = 0; t < tiles; ++t) {
+    for (int t = 0; t < (cols + 7) / 8; ++t) {
       float c[4] = {0.f, 0.f, 0.f, 0.f};
       const uint4 *b = (const uint4 *)q + t * (D / 32) * 32 + lane;
 #pragma unroll
@@ -94,11 +95,11 @@ template <int D> struct Piece<float, D> {
     for (int i = 0; i < D / 8; ++i) x[i] = p[i];
   }
   static __device__ __forceinline__ int place(int col, int c) { return (col * (D / 4) + c) * 16; }
-  __device__ __forceinline__ float sums(const char *q, const float *lse, const int *lim, int tiles, int key0, float scale) const {
+  __device__ __forceinline__ float sums(const char *q, const float *lse, const int *lim, int cols, int key0, float scale) const {
     const int lane = threadIdx.x & 31, p = key0 + (lane & 15);
     const float4 *b = (const float4 *)q + (lane >> 4) * (D / 8);
     float w = 0.f;
-    for (int c = 0; c < 8 * tiles; ++c) {
+    for (int c = 0; c < cols; ++c) {
       float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int i = 0; i < D / 8; ++i) {
@@ -145,7 +146,16 @@ __global__ void __launch_bounds__(kThreads, 2) weigh_kernel(const __grid_constan
   const uint32_t *twice = find_repeats(a.seqs, a.n, a.max_seqs, s_bits);
 
   // This block's share of the line of all sequences' blocks of keys, which count for their columns; every warp finds it.
-  const Cut fixed = cut_of<T, D>(a.hkv, a.hq, 8);
+  // (Small blocks of keys where that gives all of the grid something to do.)
+  Cut fixed = cut_of<T, D>(a.hkv, a.hq, 8);
+  {
+    int pieces = 0;                                        // of 16 keys
+    for (int s0 = 0; s0 < a.n; s0 += 32) {
+      const int len = s0 + lane < a.n ? weigh_seq(a, s0 + lane, twice).len : 0;
+      pieces += (int)__reduce_add_sync(~0u, (unsigned)((len + kKeys - 1) / kKeys));
+    }
+    while (fixed.subs > 1 && pieces / fixed.subs < kDeep * (int)gridDim.x) fixed.subs >>= 1;
+  }
   const int keys = fixed.subs * kKeys;
   auto blocks_of = [&](const WeighSeq &s) { return (s.len + keys - 1) / keys; };
   auto cost_of = [&](const WeighSeq &s) { return (uint64_t)(kExtra + ((int64_t)s.m * a.g + 7) / 8); };
@@ -195,7 +205,8 @@ __global__ void __launch_bounds__(kThreads, 2) weigh_kernel(const __grid_constan
       const int32_t *table = a.table + (int64_t)s.id * a.max_pages;
       float *weight = a.weight + s.id * a.weight_stride;
       const int64_t all_cols = (int64_t)s.m * a.g;
-      const Cut cut = cut_of<T, D>(a.hkv, a.hq, all_cols);
+      Cut cut = cut_of<T, D>(a.hkv, a.hq, all_cols);
+      cut.subs = fixed.subs;
       bool first = true;
       for (int h0 = 0; h0 < a.hkv; h0 += cut.heads)
         for (int64_t c0 = 0; c0 < all_cols; c0 += cut.cols) {
@@ -248,7 +259,7 @@ __global__ void __launch_bounds__(kThreads, 2) weigh_kernel(const __grid_constan
               from = look();
               const int key0 = b * keys + (i / heads) * kKeys, h = i % heads;
               if (key0 < s.len) {
-                const float w16 = now.sums(s_q + (size_t)h * tiles * 8 * kPieces * 16, s_lse + h * tiles * 8, s_lim + h * tiles * 8, tiles, key0, a.scale_log2);
+                const float w16 = now.sums(s_q + (size_t)h * tiles * 8 * kPieces * 16, s_lse + h * tiles * 8, s_lim + h * tiles * 8, cols, key0, a.scale_log2);
                 if (lane < kKeys) s_part[parity][i][lane] = w16;
               }
             }
