@@ -6,9 +6,9 @@
 // columns, so that a position's sum stays inside a few lanes.
 //
 // What bounds it with few rows: one read of the keys (HBM).  A warp takes 16 keys of one head at a time (no piece crosses a
-// page); its lanes load whole 16-byte pieces straight into the fragments of the warp MMAs (m16n8k16): the order of the
-// inner dimension is free as long as both operands have the same one, so the keys need no shared memory, and the
-// queries are laid out once per sequence in the same order.  All heads of a block of keys are taken by one block of
+// page) through a ring of its own, filled with 16-byte asynchronous copies.  Its lanes read 16 bytes at a time as the fragments of the
+// warp MMAs (m16n8k16): the order of the inner dimension is free as long as both operands have the same one, and the queries
+// are laid out once per sequence in that order.  All heads of a block of keys are taken by one block of
 // threads and added in order, so nothing is added across blocks and no atomics are needed.
 #include <algorithm>
 #include <cmath>
@@ -18,10 +18,9 @@
 namespace pcomoe {
 namespace {
 
-constexpr int kWarps = 8, kThreads = 32 * kWarps, kKeys = 16;
-constexpr int kItems = 32;              // pieces of 16 keys of a head in a block of keys, about
+constexpr int kWarps = 12, kThreads = 32 * kWarps, kKeys = 16;
+constexpr int kItems = 48;              // pieces of 16 keys of a head in a block of keys, about
 constexpr int kMaxSubs = 16;            // pieces of 16 keys of one head in it
-constexpr int kQBytes = 48 * 1024;      // queries held at a time
 // From this many columns (counted rows x heads of a group) of a sequence on, on average, the tensor-core kernel is taken.  Both, us, with 32
 // heads on 8 of 128 and so many counted rows a sequence (4 columns each), this one and the other:
 //   rows                       1          8           16          32          128
@@ -30,8 +29,8 @@ constexpr int kQBytes = 48 * 1024;      // queries held at a time
 //   4 sequences of 16384   38.3, 106   80.9, 107    136, 107   266, 98.7   898, 144
 //   8 sequences of 300     14.6, 18.7  28.9, 18.9  41.2, 19.5  86.2, 18.7  321, 24.8
 constexpr int kManyColumns = 64;
-constexpr int kDeep = 2;                // blocks of keys for each block of the grid that make larger ones worth it
-constexpr int kExtra = 2;               // cost of a block of keys besides its columns, in tiles of 8 columns
+constexpr int kStart = 8;               // cost of a sequence's beginning, in pieces of 16 keys
+constexpr int kExtra = 6;               // cost of a piece of 16 keys besides its columns, in tiles of 8 columns
 
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -39,19 +38,31 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// 16 keys of a head in registers, and their weights over the columns [0, cols) at q, lse, lim (laid out in tiles of 8) (lim: the last position that
-// a column sees).  key0: position of the first.  Lane 0..15 of the result: key0 + lane.
+// 16 keys of a head in registers, and their weights over the columns [0, cols) at q, lse, lim (laid out in tiles of 8; lim: the last
+// position that a column sees).  key0: position of the first.  Lane 0..15 of the result: key0 + lane.
 template <typename T, int D> struct Piece;
 
 template <int D> struct Piece<__nv_bfloat16, D> {
+  // Keys come through a ring of the warp's own in shared memory, two pieces under way while one is worked on.  Odd rows have the two
+  // halves of their 128 bytes exchanged, so that lanes of two rows read from different banks.
+  static constexpr int kStages = 3, kBytes = kKeys * D * 2, kQBytes = 64 * 1024;      // stages, bytes of one; queries held at a time
   uint4 x[2][D / 32];
-  __device__ __forceinline__ void load(const __nv_bfloat16 *k) {
+  static __device__ __forceinline__ void fetch(const __nv_bfloat16 *k, uint32_t to) {
+    constexpr int C = D / 8;
     const int lane = threadIdx.x & 31;
-    const char *p = (const char *)(k + (lane >> 2) * D) + (lane & 3) * 16;
+#pragma unroll
+    for (int j = 0; j < kKeys * C / 32; ++j) {
+      const int u = j * 32 + lane, r = u / C, c = u % C;
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + r * (D * 2) + ((c ^ ((r & 1) << 2)) << 4)), "l"((const char *)k + u * 16) : "memory");
+    }
+  }
+  __device__ __forceinline__ void load(const char *from) {
+    const int lane = threadIdx.x & 31, r = lane >> 2;
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) {
-      x[0][i] = *(const uint4 *)(p + 64 * i);
-      x[1][i] = *(const uint4 *)(p + 64 * i + 16 * D);
+      const int at = r * (D * 2) + (((4 * i + (lane & 3)) ^ ((r & 1) << 2)) << 4);
+      x[0][i] = *(const uint4 *)(from + at);
+      x[1][i] = *(const uint4 *)(from + at + 8 * D * 2);
     }
   }
   // place of the 16 bytes c of column col in the layout that sums() reads: a tile of 8 columns, step by step, lane by lane
@@ -85,12 +96,22 @@ template <int D> struct Piece<__nv_bfloat16, D> {
   }
 };
 
-// fp32: a lane holds half of a key's row
+// fp32: a lane holds half of a key's row; rows are copied with 16 bytes between them
 template <int D> struct Piece<float, D> {
+  static constexpr int kStages = 2, kBytes = kKeys * (D * 4 + 16), kQBytes = 16 * 1024;
   float4 x[D / 8];
-  __device__ __forceinline__ void load(const float *k) {
+  static __device__ __forceinline__ void fetch(const float *k, uint32_t to) {
+    constexpr int C = D / 4;
     const int lane = threadIdx.x & 31;
-    const float4 *p = (const float4 *)(k + (lane & 15) * D + (lane >> 4) * (D / 2));
+#pragma unroll
+    for (int j = 0; j < kKeys * C / 32; ++j) {
+      const int u = j * 32 + lane, r = u / C, c = u % C;
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + r * (D * 4 + 16) + c * 16), "l"((const char *)k + u * 16) : "memory");
+    }
+  }
+  __device__ __forceinline__ void load(const char *from) {
+    const int lane = threadIdx.x & 31;
+    const float4 *p = (const float4 *)(from + (lane & 15) * (D * 4 + 16)) + (lane >> 4) * (D / 8);
 #pragma unroll
     for (int i = 0; i < D / 8; ++i) x[i] = p[i];
   }
@@ -123,7 +144,7 @@ struct Cut {
 };
 template <typename T, int D>
 __host__ __device__ inline Cut cut_of(int hkv, int hq, int64_t most_cols) {
-  constexpr int kCols = kQBytes / (D * (int)sizeof(T));
+  constexpr int kCols = Piece<T, D>::kQBytes / (D * (int)sizeof(T));
   Cut c;
   c.heads = hkv * 8 <= kCols ? hkv : kCols / 8;
   c.heads = c.heads < kItems ? c.heads : kItems;
@@ -134,38 +155,31 @@ __host__ __device__ inline Cut cut_of(int hkv, int hq, int64_t most_cols) {
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, 2) weigh_kernel(const __grid_constant__ WeighArgs a) {
-  constexpr int kCols = kQBytes / (D * (int)sizeof(T)), kPieces = D * (int)sizeof(T) / 16;
-  extern __shared__ __align__(16) char s_q[];
+__global__ void __launch_bounds__(kThreads, 1) weigh_kernel(const __grid_constant__ WeighArgs a) {
+  constexpr int kCols = Piece<T, D>::kQBytes / (D * (int)sizeof(T)), kPieces = D * (int)sizeof(T) / 16;
+  using P = Piece<T, D>;
+  extern __shared__ __align__(16) char s_q[];            // queries, then a ring for every warp
   __shared__ float s_lse[kCols];
-  __shared__ int s_lim[kCols];
+  __shared__ int s_lim[kCols], s_row[kCols];
   __shared__ float s_part[2][kItems][kKeys];
   __shared__ uint32_t s_bits[2 * (kMaxSeqs / 32)];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const char *ring = s_q + P::kQBytes + warp * P::kStages * P::kBytes;
+  const uint32_t q_at = (uint32_t)__cvta_generic_to_shared(s_q), ring_at = (uint32_t)__cvta_generic_to_shared(ring);
   pdl_grid_wait();
   const uint32_t *twice = find_repeats(a.seqs, a.n, a.max_seqs, s_bits);
 
-  // This block's share of the line of all sequences' blocks of keys, which count for their columns; every warp finds it.
-  // (Small blocks of keys where that gives all of the grid something to do.)
-  Cut fixed = cut_of<T, D>(a.hkv, a.hq, 8);
-  {
-    int pieces = 0;                                        // of 16 keys
-    for (int s0 = 0; s0 < a.n; s0 += 32) {
-      const int len = s0 + lane < a.n ? weigh_seq(a, s0 + lane, twice).len : 0;
-      pieces += (int)__reduce_add_sync(~0u, (unsigned)((len + kKeys - 1) / kKeys));
-    }
-    while (fixed.subs > 1 && pieces / fixed.subs < kDeep * (int)gridDim.x) fixed.subs >>= 1;
-  }
-  const int keys = fixed.subs * kKeys;
-  auto blocks_of = [&](const WeighSeq &s) { return (s.len + keys - 1) / keys; };
+  // This block's share of the line of all sequences' pieces of 16 keys, which count for their columns; every warp finds it.  (Up to 32
+  // sequences a lane keeps what it has read.)
+  auto pieces_of = [&](const WeighSeq &s) { return (s.len + kKeys - 1) / kKeys; };
+  auto units_of = [&](const WeighSeq &s) { return (uint64_t)(s.len ? kStart + pieces_of(s) : 0); };
   auto cost_of = [&](const WeighSeq &s) { return (uint64_t)(kExtra + ((int64_t)s.m * a.g + 7) / 8); };
+  WeighSeq mine = {};
   uint64_t total = 0;
   for (int s0 = 0; s0 < a.n; s0 += 32) {
-    uint64_t w = 0;
-    if (s0 + lane < a.n) {
-      const WeighSeq s = weigh_seq(a, s0 + lane, twice);
-      w = blocks_of(s) * cost_of(s);
-    }
+    mine = {};
+    if (s0 + lane < a.n) mine = weigh_seq(a, s0 + lane, twice);
+    uint64_t w = units_of(mine) * cost_of(mine);
 #pragma unroll
     for (int o = 16; o; o >>= 1) w += __shfl_xor_sync(~0u, w, o);
     total += w;
@@ -175,12 +189,11 @@ __global__ void __launch_bounds__(kThreads, 2) weigh_kernel(const __grid_constan
   uint64_t at = 0;                                         // of the line: where sequence list begins
   int parity = 0;
   for (int s0 = 0; s0 < a.n && at < x1; s0 += 32) {
-    WeighSeq mine = {};
-    uint64_t w = 0;
-    if (s0 + lane < a.n) {
-      mine = weigh_seq(a, s0 + lane, twice);
-      w = blocks_of(mine) * cost_of(mine);
+    if (a.n > 32) {
+      mine = {};
+      if (s0 + lane < a.n) mine = weigh_seq(a, s0 + lane, twice);
     }
+    const uint64_t w = units_of(mine) * cost_of(mine);
     uint64_t upto = w;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -198,74 +211,86 @@ __global__ void __launch_bounds__(kThreads, 2) weigh_kernel(const __grid_constan
       s.base = s.len - s.m;
       s.id = __shfl_sync(~0u, mine.id, l);
       const uint64_t begin = at + __shfl_sync(~0u, upto - w, l), cost = cost_of(s);
-      // the blocks that begin inside of the share
-      const int b0 = begin >= x0 ? 0 : (int)((x0 - begin + cost - 1) / cost);
-      const int b1 = (int)min((uint64_t)blocks_of(s), (x1 - begin + cost - 1) / cost);
+      // the pieces that begin inside of the share
+      const int b0 = begin >= x0 ? 0 : (int)max((int64_t)((x0 - begin + cost - 1) / cost) - kStart, (int64_t)0);
+      const int b1 = (int)min((int64_t)pieces_of(s), (int64_t)((x1 - begin + cost - 1) / cost) - kStart);
       if (b0 >= b1) continue;
       const int32_t *table = a.table + (int64_t)s.id * a.max_pages;
       float *weight = a.weight + s.id * a.weight_stride;
-      const int64_t all_cols = (int64_t)s.m * a.g;
-      Cut cut = cut_of<T, D>(a.hkv, a.hq, all_cols);
-      cut.subs = fixed.subs;
+      const int all_cols = s.m * a.g;
+      const Cut cut = cut_of<T, D>(a.hkv, a.hq, all_cols);
       bool first = true;
       for (int h0 = 0; h0 < a.hkv; h0 += cut.heads)
-        for (int64_t c0 = 0; c0 < all_cols; c0 += cut.cols) {
+        for (int c0 = 0; c0 < all_cols; c0 += cut.cols) {
           const int heads = min(cut.heads, a.hkv - h0);
-          const int cols = (int)min((int64_t)cut.cols, all_cols - c0), tiles = (cols + 7) >> 3;
+          const int cols = min(cut.cols, all_cols - c0), tiles = (cols + 7) >> 3;
+          // A block of keys, cut.subs pieces, after another, the warps in turn its (piece, head) pairs; the page of a pair is looked
+          // up one pair ahead of its copies.
+          int nb = b0, ni = warp;                          // the pair that is looked up
+          auto pairs_of = [&](int b) { return min(cut.subs, b1 - b) * heads; };
+          auto look = [&]() -> const T * {
+            if (ni >= pairs_of(nb)) { ni = warp; nb += cut.subs; }       // (a later block has no more pairs than this one)
+            if (ni >= pairs_of(nb)) nb = b1;
+            if (nb >= b1) return nullptr;
+            return (const T *)a.k + (weigh_page_row(a, table, (nb + ni / heads) * kKeys) + (int64_t)(h0 + ni % heads) * a.page) * D;
+          };
+          uint32_t in = 0, out = 0;                        // pairs sent for, pairs done
+          const T *from = look();
+          auto fetch = [&]() {
+            if (from) {
+              P::fetch(from, ring_at + (in % P::kStages) * P::kBytes);
+              ni += kWarps;
+              from = look();
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            ++in;
+          };
+#pragma unroll
+          for (int i = 0; i < P::kStages - 1; ++i) fetch();
           __syncthreads();                                 // the last ones are done with what is replaced
-          for (int u = tid; u < heads * tiles * 8 * kPieces; u += kThreads) {
-            const int c = u % kPieces, hc = u / kPieces, col = hc % (tiles * 8), h = hc / (tiles * 8);
-            uint4 x = make_uint4(0, 0, 0, 0);
-            int lim = -1;
+          // the columns, then their queries
+          for (int u = tid; u < heads * tiles * 8; u += kThreads) {
+            const int col = u % (tiles * 8), h = u / (tiles * 8);
+            int lim = -1, row = -1;
             float lse = 0.f;
             if (col < cols) {
-              const int64_t at_col = c0 + col;
-              const int k = (int)(at_col / a.g), head = (h0 + h) * a.g + (int)(at_col - (int64_t)k * a.g), row = counted_row(a, s, list, k);
+              const int k = (c0 + col) / a.g, head = (h0 + h) * a.g + c0 + col - k * a.g;
+              row = counted_row(a, s, list, k);
               if (row >= 0) {
-                x = *(const uint4 *)((const char *)((const T *)a.q + row * a.q_stride + (int64_t)head * D) + c * 16);
-                if (c == 0) {
-                  lse = a.lse[(int64_t)row * a.hq + head];
-                  if (lse != -INFINITY) lim = s.base + k;  // a row that saw nothing adds nothing
-                }
+                lse = a.lse[(int64_t)row * a.hq + head];
+                if (lse != -INFINITY) lim = s.base + k;    // a row that saw nothing adds nothing
               }
             }
-            *(uint4 *)(s_q + (size_t)h * tiles * 8 * kPieces * 16 + Piece<T, D>::place(col, c)) = x;
-            if (c == 0) { s_lse[h * tiles * 8 + col] = lse * kLog2ef; s_lim[h * tiles * 8 + col] = lim; }
+            s_lse[u] = lse * kLog2ef;
+            s_lim[u] = lim;
+            s_row[u] = row;
           }
           __syncthreads();
-          // pieces of 16 keys of a head, a block of keys after another: the keys of a warp's next piece come in while it works, and the
-          // page of the one after that is looked up
-          const int per = cut.subs * heads;
-          int nb = b0, ni = warp;                          // the piece that is looked up
-          auto look = [&]() -> const T * {
-            const int key0 = nb * keys + (ni / heads) * kKeys;
-            if (ni >= per || nb >= b1 || key0 >= s.len) return nullptr;
-            return (const T *)a.k + (weigh_page_row(a, table, key0) + (int64_t)(h0 + ni % heads) * a.page) * D;
-          };
-          auto advance = [&]() {
-            ni += kWarps;
-            if (ni >= per) { ni = warp; ++nb; }
-          };
-          Piece<T, D> now, next;
-          const T *from = look();
-          if (from) next.load(from);
-          advance();
-          from = look();
-          for (int b = b0; b < b1; ++b) {
-            for (int i = warp; i < per; i += kWarps) {
-              now = next;
-              if (from) next.load(from);
-              advance();
-              from = look();
-              const int key0 = b * keys + (i / heads) * kKeys, h = i % heads;
-              if (key0 < s.len) {
-                const float w16 = now.sums(s_q + (size_t)h * tiles * 8 * kPieces * 16, s_lse + h * tiles * 8, s_lim + h * tiles * 8, cols, key0, a.scale_log2);
-                if (lane < kKeys) s_part[parity][i][lane] = w16;
-              }
+          for (int u = tid; u < heads * tiles * 8 * kPieces; u += kThreads) {
+            const int c = u % kPieces, hc = u / kPieces, col = hc % (tiles * 8), h = hc / (tiles * 8), row = s_row[hc];
+            const int head = (h0 + h) * a.g + (c0 + col) % a.g;
+            const char *from = (const char *)((const T *)a.q + (row < 0 ? 0 : row * a.q_stride + (int64_t)head * D)) + c * 16;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(q_at + h * tiles * 8 * kPieces * 16 + P::place(col, c)), "l"(from), "r"(row < 0 ? 0 : 16) : "memory");
+          }
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          __syncthreads();
+          for (int b = b0; b < b1; b += cut.subs) {
+            const int pairs = pairs_of(b);
+            for (int i = warp; i < pairs; i += kWarps) {
+              fetch();
+              asm volatile("cp.async.wait_group %0;" ::"n"(P::kStages - 1) : "memory");
+              __syncwarp();
+              P now;
+              now.load(ring + (out % P::kStages) * P::kBytes);
+              ++out;
+              const int h = i % heads;
+              const float w16 = now.sums(s_q + (size_t)h * tiles * 8 * kPieces * 16, s_lse + h * tiles * 8, s_lim + h * tiles * 8, cols, (b + i / heads) * kKeys, a.scale_log2);
+              if (lane < kKeys) s_part[parity][i][lane] = w16;
+              __syncwarp();                                // the stage is read before it is filled again
             }
             __syncthreads();
-            const int p = b * keys + tid;
-            if (tid < keys && p < s.len) {
+            const int p = b * kKeys + tid;
+            if (tid < min(cut.subs, b1 - b) * kKeys && p < s.len) {
               float sum = 0.f;
               for (int h = 0; h < heads; ++h) sum += s_part[parity][(tid / kKeys) * heads + h][tid % kKeys];
               weight[p] = first && a.fresh && p >= s.base ? sum : weight[p] + sum;
@@ -273,6 +298,7 @@ __global__ void __launch_bounds__(kThreads, 2) weigh_kernel(const __grid_constan
             parity ^= 1;
           }
           first = false;
+          asm volatile("cp.async.wait_all;" ::: "memory");
         }
     }
     at += __shfl_sync(~0u, upto, 31);
@@ -281,14 +307,15 @@ __global__ void __launch_bounds__(kThreads, 2) weigh_kernel(const __grid_constan
 
 template <typename T, int D>
 pcomoe_status run(const WeighArgs &a, int sms, cudaStream_t st) {
+  constexpr int kSmem = Piece<T, D>::kQBytes + kWarps * Piece<T, D>::kStages * Piece<T, D>::kBytes;
   static PerDeviceOnce once;
   int dev = -1;
   PCOMOE_CUDA_TRY(cudaGetDevice(&dev));
   if (once.first_use(dev)) {
-    PCOMOE_CUDA_TRY(cudaFuncSetAttribute(weigh_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kQBytes));
+    PCOMOE_CUDA_TRY(cudaFuncSetAttribute(weigh_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem));
     once.done(dev);
   }
-  PCOMOE_CUDA_TRY(launch_pdl(weigh_kernel<T, D>, dim3(2 * sms), dim3(kThreads), kQBytes, st, a));
+  PCOMOE_CUDA_TRY(launch_pdl(weigh_kernel<T, D>, dim3(sms), dim3(kThreads), kSmem, st, a));
   count_launch();
   return PCOMOE_OK;
 }
@@ -341,7 +368,7 @@ pcomoe_status pcomoe_cache_weigh(const pcomoe_attn_config *cfg, const pcomoe_cac
   if (q_stride < (int64_t)cfg->q_heads * cfg->head_dim || weight_stride < (int64_t)cache->max_pages * cache->page_size) return PCOMOE_ERR_INVALID_ARG;
   const int64_t e = (int64_t)dtype_size(cfg->dtype);
   if (((uintptr_t)d_q & 15) || (q_stride * e) % 16) return PCOMOE_ERR_UNSUPPORTED;
-  if ((int64_t)T * (cfg->q_heads / cfg->kv_heads) > INT32_MAX) return PCOMOE_ERR_SHAPE;
+  if ((int64_t)T * (cfg->q_heads / cfg->kv_heads) > INT32_MAX - 1024) return PCOMOE_ERR_SHAPE;
   if (!d_workspace || ((uintptr_t)d_workspace & 255) || ws_bytes < workspace_of(cfg, cache, n)) return PCOMOE_ERR_WORKSPACE;
   int sms;
   if ((st = current_sms(&sms)) != PCOMOE_OK) return st;
