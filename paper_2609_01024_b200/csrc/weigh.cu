@@ -226,13 +226,19 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_kernel(const __grid_constan
           const int cols = min(cut.cols, all_cols - c0), tiles = (cols + 7) >> 3;
           // A block of keys, cut.subs pieces, after another, the warps in turn its (piece, head) pairs; the page of a pair is looked
           // up one pair ahead of its copies.
-          int nb = b0, ni = warp;                          // the pair that is looked up
+          const int up = kWarps / heads, over = kWarps % heads, sub0 = warp / heads, head0 = warp % heads;
+          auto on = [&](int &sub, int &h) {                // to a warp's next pair: piece of the block, head
+            sub += up;
+            h += over;
+            if (h >= heads) { h -= heads; ++sub; }
+          };
+          int nb = b0, ni = warp, nsub = sub0, nh = head0; // the pair that is looked up
           auto pairs_of = [&](int b) { return min(cut.subs, b1 - b) * heads; };
           auto look = [&]() -> const T * {
-            if (ni >= pairs_of(nb)) { ni = warp; nb += cut.subs; }       // (a later block has no more pairs than this one)
+            if (ni >= pairs_of(nb)) { ni = warp; nsub = sub0; nh = head0; nb += cut.subs; }       // (a later block has no more pairs than this one)
             if (ni >= pairs_of(nb)) nb = b1;
             if (nb >= b1) return nullptr;
-            return (const T *)a.k + (weigh_page_row(a, table, (nb + ni / heads) * kKeys) + (int64_t)(h0 + ni % heads) * a.page) * D;
+            return (const T *)a.k + (weigh_page_row(a, table, (nb + nsub) * kKeys) + (int64_t)(h0 + nh) * a.page) * D;
           };
           uint32_t in = 0, out = 0;                        // pairs sent for, pairs done
           const T *from = look();
@@ -240,6 +246,7 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_kernel(const __grid_constan
             if (from) {
               P::fetch(from, ring_at + (in % P::kStages) * P::kBytes);
               ni += kWarps;
+              on(nsub, nh);
               from = look();
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
@@ -276,15 +283,15 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_kernel(const __grid_constan
           __syncthreads();
           for (int b = b0; b < b1; b += cut.subs) {
             const int pairs = pairs_of(b);
-            for (int i = warp; i < pairs; i += kWarps) {
+            int sub = sub0, h = head0;
+            for (int i = warp; i < pairs; i += kWarps, on(sub, h)) {
               fetch();
               asm volatile("cp.async.wait_group %0;" ::"n"(P::kStages - 1) : "memory");
               __syncwarp();
               P now;
               now.load(ring + (out % P::kStages) * P::kBytes);
               ++out;
-              const int h = i % heads;
-              const float w16 = now.sums(s_q + (size_t)h * tiles * 8 * kPieces * 16, s_lse + h * tiles * 8, s_lim + h * tiles * 8, cols, (b + i / heads) * kKeys, a.scale_log2);
+              const float w16 = now.sums(s_q + (size_t)h * tiles * 8 * kPieces * 16, s_lse + h * tiles * 8, s_lim + h * tiles * 8, cols, (b + sub) * kKeys, a.scale_log2);
               if (lane < kKeys) s_part[parity][i][lane] = w16;
               __syncwarp();                                // the stage is read before it is filled again
             }
