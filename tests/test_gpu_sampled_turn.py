@@ -1,0 +1,77 @@
+"""Rotation, attention over the cache, verification, kept rows, weights and eviction together, as a serving loop runs them."""
+import importlib.util
+import os
+
+import numpy as np
+import pytest
+import torch
+
+import turn_reference as ref
+
+pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def example():
+    spec = importlib.util.spec_from_file_location("sample_in_budget", os.path.join(ROOT, "examples", "sample_in_budget.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m
+
+
+def test_sampling_in_a_budget():
+    m = example()
+    model, prompts, out, held = m.main()
+    for o, p in zip(out, prompts):
+        assert o[:len(p)] == p and len(o) >= len(p) + 13 and all(0 <= t < model.vocab for t in o)
+    assert all(k <= 48 for row in held for k in row) and max(held[-1]) == 48
+    pages = sum(-(-k // model.cache.page_size) for k in held[-1])
+    assert int((model.cache.page_ref > 0).sum()) == pages
+
+
+def test_one_turn_step_by_step():
+    """Every step of a turn against plain forms of the step before: cached keys, the walk, the weights, what is evicted."""
+    m = example()
+    B = m.B
+    model, rng = m.Decoder(blocks=1, seed=3), np.random.default_rng(3)
+    prompt = rng.integers(0, model.vocab, size=70).tolist()
+    seqs = m.ints([0])
+    model.cache.reserve(seqs, m.ints([70]))
+    cu = m.cu_of([70])
+    logits, left = model.run(m.ints(prompt), m.ints(range(70)), seqs, cu, prompt=True)
+    model.weigh(left, seqs, cu)
+    # every row's attention adds up to one a head
+    total = float(model.weights.weight[0, :70].double().sum())
+    assert abs(total - 70 * model.heads) <= 2e-5 * total
+    drafter = m.Drafter(model.vocab, rng)
+    tokens, parents = drafter.tree(5, (3, 2, 1))
+    n = len(tokens)
+    cu = m.cu_of([n])
+    mask = torch.tensor(np.asarray([[b] for b in m.ancestors(parents)], np.uint32).view(np.int32), device="cuda")
+    model.cache.reserve(seqs, m.ints([n]))
+    logits, left = model.run(m.ints(tokens), m.ints([70 + d for d in m.depths(parents)]), seqs, cu, mask)
+    u, u_next = rng.random(n).astype(np.float32), rng.random(1).astype(np.float32)
+    near = drafter.rows(tokens)
+    keep, n_keep, nxt = model.verifier.verify(logits, m.ints(tokens), cu, m.floats(u), m.floats(u_next), parent=m.ints(parents), draft_probs=near)
+    path, want = ref.verify(logits.double().cpu().numpy(), tokens, [0, n], u, u_next, parents, near.cpu().numpy())
+    assert keep[0, :int(n_keep[0])].tolist() == path[0] and nxt.tolist() == want
+    model.cache.keep(seqs, cu, keep, n_keep)
+    before = model.weights.weight[0].double().cpu().numpy()
+    model.weigh(left, seqs, cu, keep, n_keep)
+    length, base = int(model.cache.seq_len[0]), 70
+    assert length == base + len(path[0])
+    k = ref.rows_of(model.cache.k[0], model.cache.page_table[0].tolist(), model.cache.page_size, length).double().cpu().numpy()
+    q, lse = left[0][0].double().cpu().numpy(), left[0][1].double().cpu().numpy()
+    add, err = ref.weigh(q, lse, k, model.d ** -0.5, path[0], base)
+    got = model.weights.weight[0, :length].double().cpu().numpy()
+    old = np.concatenate([before[:base], np.zeros(length - base)])
+    assert (np.abs(got - old - add) <= err + (old + add) * 2.0 ** -23).all()
+    # the log sums came from the attention over the tree, which saw these positions alone: the kept rows' weights add up to one a head
+    assert abs(float(add.sum()) - len(path[0]) * model.heads) <= 2e-5 * len(path[0]) * model.heads
+    stays = ref.evict(got, length, 40, 2, 10)
+    kept = torch.tensor(k)[stays]
+    model.weights.evict(seqs, m.ints([40]), sinks=2, recent=10)
+    assert int(model.cache.seq_len[0]) == 40
+    now = ref.rows_of(model.cache.k[0], model.cache.page_table[0].tolist(), model.cache.page_size, 40).double().cpu()
+    assert torch.equal(now, kept)
+    assert [model.cache.device_status(), model.attn.device_status(), model.weights.device_status(), model.verifier.device_status()] == [0] * 4
