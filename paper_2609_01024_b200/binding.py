@@ -829,9 +829,11 @@ class HeadRotation:
 
     def _rows(self, x, T, heads):
         """Pointer and row stride of packed rows [T, heads, head_dim]."""
-        shape, (row, head, one) = x.shape, x.stride()
-        assert shape[0] == T and shape[1] == heads and shape[2] == self.head_dim and x.dtype is self._torch and one == 1 and \
-            (head == self.head_dim or heads == 1) and x.device == self.device, (shape, x.stride(), x.dtype, x.device)
+        assert x.shape == (T, heads, self.head_dim) and x.dtype is self._torch and x.get_device() == self.gpu, (x.shape, x.dtype, x.device)
+        if x.is_contiguous():
+            return x.data_ptr(), heads * self.head_dim
+        row, head, one = x.stride()
+        assert one == 1 and (head == self.head_dim or heads == 1), x.stride()
         return x.data_ptr(), row if T > 1 else heads * self.head_dim
 
     def rotate(self, q, k, position, q_out=None, k_out=None):

@@ -12,6 +12,7 @@
 // threads and added in order, so nothing is added across blocks and no atomics are needed.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "weigh.cuh"
 
@@ -23,12 +24,12 @@ constexpr int kItems = 48;              // pieces of 16 keys of a head in a bloc
 constexpr int kMaxSubs = 16;            // pieces of 16 keys of one head in it
 // From this many columns (counted rows x heads of a group) of a sequence on, on average, the tensor-core kernel is taken.  Both, us, with 32
 // heads on 8 of 128 and so many counted rows a sequence (4 columns each), this one and the other:
-//   rows                       1          8           16          32          128
-//   64 sequences of 512    23.5, 69.9  49.5, 70.9   83, 71.0   161, 69.9   878, 109
-//   32 sequences of 4096   63.4, 192    132, 193    220, 193   418, 182   1659, 278
-//   4 sequences of 16384   38.3, 106   80.9, 107    136, 107   266, 98.7   898, 144
-//   8 sequences of 300     14.6, 18.7  28.9, 18.9  41.2, 19.5  86.2, 18.7  321, 24.8
-constexpr int kManyColumns = 64;
+//   rows                       1          8           16          24          32          128
+//   64 sequences of 512    21.0, 56.7  30.1, 57.0  51.0, 57.6  74.2, 60.5  96.3, 58.1  392, 103
+//   32 sequences of 4096   53.3, 177   70.6, 178    128, 179    186, 179    242, 163   954, 274
+//   4 sequences of 16384   32.9, 99.1  42.9, 100   73.6, 101    104, 101    133, 93.4  511, 148
+//   8 sequences of 300     10.5, 17.8  13.3, 18.0  18.8, 18.7  24.9, 17.4  31.0, 17.0  105, 22.8
+constexpr int kManyColumns = 96;
 constexpr int kStart = 8;               // cost of a sequence's beginning, in pieces of 16 keys
 constexpr int kExtra = 6;               // cost of a piece of 16 keys besides its columns, in tiles of 8 columns
 
@@ -71,21 +72,35 @@ template <int D> struct Piece<__nv_bfloat16, D> {
     const int lane = threadIdx.x & 31;
     const int p0 = key0 + (lane >> 2), p1 = p0 + 8;
     float w0 = 0.f, w1 = 0.f;
-    for (int t = 0; t < (cols + 7) / 8; ++t) {
-      float c[4] = {0.f, 0.f, 0.f, 0.f};
+    const auto form = [&](int t, auto many) {              // that many tiles of columns from t on, whose chains of products run side by side
+      constexpr int M = many.value;
+      float c[M][4];
+#pragma unroll
+      for (int k = 0; k < M; ++k) c[k][0] = c[k][1] = c[k][2] = c[k][3] = 0.f;
       const uint4 *b = (const uint4 *)q + t * (D / 32) * 32 + lane;
 #pragma unroll
       for (int i = 0; i < D / 32; ++i) {
-        const uint4 y = b[32 * i];
-        mma(c, x[0][i].x, x[1][i].x, x[0][i].y, x[1][i].y, y.x, y.y);
-        mma(c, x[0][i].z, x[1][i].z, x[0][i].w, x[1][i].w, y.z, y.w);
+        uint4 y[M];
+#pragma unroll
+        for (int k = 0; k < M; ++k) y[k] = b[(k * (D / 32) + i) * 32];
+#pragma unroll
+        for (int k = 0; k < M; ++k) mma(c[k], x[0][i].x, x[1][i].x, x[0][i].y, x[1][i].y, y[k].x, y[k].y);
+#pragma unroll
+        for (int k = 0; k < M; ++k) mma(c[k], x[0][i].z, x[1][i].z, x[0][i].w, x[1][i].w, y[k].z, y[k].w);
       }
-      const float2 l = *(const float2 *)(lse + t * 8 + (lane & 3) * 2);
-      const int2 m = *(const int2 *)(lim + t * 8 + (lane & 3) * 2);
-      // chosen, not multiplied: what is not seen adds nothing whatever it is
-      w0 += (p0 <= m.x ? exp2_fast(fmaf(c[0], scale, -l.x)) : 0.f) + (p0 <= m.y ? exp2_fast(fmaf(c[1], scale, -l.y)) : 0.f);
-      w1 += (p1 <= m.x ? exp2_fast(fmaf(c[2], scale, -l.x)) : 0.f) + (p1 <= m.y ? exp2_fast(fmaf(c[3], scale, -l.y)) : 0.f);
-    }
+#pragma unroll
+      for (int k = 0; k < M; ++k) {
+        const float2 l = *(const float2 *)(lse + (t + k) * 8 + (lane & 3) * 2);
+        const int2 m = *(const int2 *)(lim + (t + k) * 8 + (lane & 3) * 2);
+        // chosen, not multiplied: what is not seen adds nothing whatever it is
+        w0 += (p0 <= m.x ? exp2_fast(fmaf(c[k][0], scale, -l.x)) : 0.f) + (p0 <= m.y ? exp2_fast(fmaf(c[k][1], scale, -l.y)) : 0.f);
+        w1 += (p1 <= m.x ? exp2_fast(fmaf(c[k][2], scale, -l.x)) : 0.f) + (p1 <= m.y ? exp2_fast(fmaf(c[k][3], scale, -l.y)) : 0.f);
+      }
+    };
+    const int tiles = (cols + 7) / 8;
+    int t = 0;
+    for (; t + 4 <= tiles; t += 4) form(t, std::integral_constant<int, 4>());
+    for (; t < tiles; ++t) form(t, std::integral_constant<int, 1>());
     w0 += __shfl_xor_sync(~0u, w0, 1);
     w1 += __shfl_xor_sync(~0u, w1, 1);
     w0 += __shfl_xor_sync(~0u, w0, 2);

@@ -32,6 +32,7 @@ namespace {
 constexpr int BK_ROWS = 128, BC = 128;          // keys of a unit, columns of a step
 constexpr int kGroups = 3, kFirst = 128, kThreads = kFirst + 128 * kGroups;      // warp groups that sum, from thread kFirst on
 constexpr int kStages = 6, kBuffers = 3, kSlots = 8;       // of queries, of accumulators, of log sums
+constexpr int kUnits = 4;                       // units in hand
 constexpr uint32_t kKeyCols = 64, kAccAt = 2 * kKeyCols;    // TMEM columns: keys of two units, then the accumulators
 template <int D> struct Shape {
   static constexpr int kHalves = D / 64;
@@ -176,14 +177,14 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
   constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
   constexpr int C = D / 8, kSide = 32 / C;                // 16-byte pieces of a row; rows that a warp copies side by side
   extern __shared__ __align__(1024) uint8_t smem[];
-  __shared__ __align__(8) uint64_t s_qfull[kStages], s_qempty[kStages], s_kfull[2], s_kempty[2], s_sfull[kBuffers], s_sempty[kBuffers], s_lfull[kSlots], s_lempty[kSlots], s_ifull[2],
-      s_iempty[2], s_join[2];
-  __shared__ Unit s_item[2];
+  __shared__ __align__(8) uint64_t s_qfull[kStages], s_qempty[kStages], s_kfull[2], s_kempty[2], s_sfull[kBuffers], s_sempty[kBuffers], s_lfull[kSlots], s_lempty[kSlots], s_ifull[kUnits],
+      s_iempty[kUnits], s_join[kUnits];
+  __shared__ Unit s_item[kUnits];
   __shared__ __align__(16) float s_lse[kSlots][BC];
   __shared__ __align__(16) int s_lim[kSlots][BC];
   __shared__ int s_least[kSlots][2];                      // the smallest limit of either half of a step's columns
   __shared__ int64_t s_at[2][64];                         // of the copying warps: where rows are, -1: nowhere
-  __shared__ float s_sum[2][kGroups - 1][BK_ROWS];
+  __shared__ float s_sum[kUnits][kGroups - 1][BK_ROWS];
   __shared__ uint32_t s_bits[2 * (kMaxSeqs / 32)];
   __shared__ uint32_t s_tmem;
   __shared__ int s_flags[2];
@@ -197,11 +198,10 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
     for (int i = 0; i < kStages; ++i) { mbar_init(smem_u32(&s_qfull[i]), kBoxes ? 1 : 2); mbar_init(smem_u32(&s_qempty[i]), 1); }
     for (int i = 0; i < kBuffers; ++i) { mbar_init(smem_u32(&s_sfull[i]), 1); mbar_init(smem_u32(&s_sempty[i]), 4); }
     for (int i = 0; i < kSlots; ++i) { mbar_init(smem_u32(&s_lfull[i]), kBoxes ? 1 : 2); mbar_init(smem_u32(&s_lempty[i]), 4); }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&s_kfull[i]), 4);
-      mbar_init(smem_u32(&s_kempty[i]), 1);
+    for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&s_kfull[i]), 4); mbar_init(smem_u32(&s_kempty[i]), 1); }
+    for (int i = 0; i < kUnits; ++i) {
       mbar_init(smem_u32(&s_ifull[i]), 1);
-      mbar_init(smem_u32(&s_iempty[i]), 3 + 4 * kGroups);              // every warp but the one that fills them
+      mbar_init(smem_u32(&s_iempty[i]), 3 + 4 * kGroups);  // every warp but the one that fills them
       mbar_init(smem_u32(&s_join[i]), 4 * (kGroups - 1));
     }
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -218,10 +218,10 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
   const uint32_t *twice = find_repeats(a.w.seqs, a.w.n, a.w.max_seqs, s_bits);
 
   uint32_t n_item = 0, step = 0;                          // units and steps so far
-  auto item_ready = [&](bool ok) { return __all_sync(~0u, ok && wait_bar(&s_ifull[n_item & 1], (n_item >> 1) & 1, flags, a.w.limit_ns)); };
+  auto item_ready = [&](bool ok) { return __all_sync(~0u, ok && wait_bar(&s_ifull[n_item % kUnits], (n_item / kUnits) & 1, flags, a.w.limit_ns)); };
   auto item_done = [&]() {
     __syncwarp();
-    if (lane == 0) mbar_arrive(smem_u32(&s_iempty[n_item & 1]));
+    if (lane == 0) mbar_arrive(smem_u32(&s_iempty[n_item % kUnits]));
     ++n_item;
   };
   if (warp >= kFirst / 32) {
@@ -230,29 +230,37 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
     const float scale = a.w.scale_log2;
     bool ok = true;
     uint32_t n_unit = 0, n_k = 0;
-    // The first group brings the keys of unit number n into TMEM: a thread its own row, straight from its page, two elements to a column.
+    // The groups in turn bring a unit's keys into TMEM: a thread its own row, straight from its page, two elements to a column.  Unit
+    // number n's are brought while the one before it is worked on; n_k units with steps came before it.
     auto load_keys = [&](uint32_t n) {
-      if (ok) ok = wait_bar(&s_ifull[n & 1], (n >> 1) & 1, flags, a.w.limit_ns);
+      if (ok) ok = wait_bar(&s_ifull[n % kUnits], (n / kUnits) & 1, flags, a.w.limit_ns);
       __syncwarp();
-      const Unit &it = s_item[n & 1];
+      const Unit &it = s_item[n % kUnits];
       if (!__all_sync(~0u, ok) || it.p0 < 0 || it.steps == 0) return;
+      if ((int)(n_k % kGroups) != group) {
+        ++n_k;
+        return;
+      }
       const int p = it.p0 + key;
       const uint4 *row = nullptr;
       if (p < it.seq.len)
         row = (const uint4 *)((const __nv_bfloat16 *)a.w.k + (weigh_page_row(a.w, a.w.table + (int64_t)it.seq.id * a.w.max_pages, p) + (int64_t)it.head * a.w.page) * D);
+      // (all of the row is asked for before any of it is used)
+      uint32_t x[D / 32][16];
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint4 y = row ? row[4 * c + k] : make_uint4(0, 0, 0, 0);
+          x[c][4 * k] = y.x; x[c][4 * k + 1] = y.y; x[c][4 * k + 2] = y.z; x[c][4 * k + 3] = y.w;
+        }
       ok = wait_bar(&s_kempty[n_k & 1], ((n_k >> 1) & 1) ^ 1, flags, a.w.limit_ns);
       __syncwarp();
       tc_fence_after();
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
-        uint32_t x[16];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint4 y = row ? row[4 * c + k] : make_uint4(0, 0, 0, 0);
-          x[4 * k] = y.x; x[4 * k + 1] = y.y; x[4 * k + 2] = y.z; x[4 * k + 3] = y.w;
-        }
         __syncwarp();
-        tmem_st16(tmem + (n_k & 1) * kKeyCols + 16 * c + lanes, x);
+        tmem_st16(tmem + (n_k & 1) * kKeyCols + 16 * c + lanes, x[c]);
       }
       asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
       tc_fence_before();
@@ -260,11 +268,12 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
       if (lane == 0) mbar_arrive(smem_u32(&s_kfull[n_k & 1]));
       ++n_k;
     };
-    if (group == 0) load_keys(0);
+    load_keys(0);
     while (item_ready(ok)) {
-      const Unit &it = s_item[n_item & 1];
+      const Unit &it = s_item[n_item % kUnits];
       if (it.p0 < 0) break;
-      bool ahead = group != 0;                             // the next unit's keys are on their way
+      // (before the group's own steps: those wait for this unit's products, and the next unit's keys would wait behind them)
+      load_keys(n_item + 1);
       const int p = it.p0 + key, last = it.p0 + BK_ROWS - 1, steps = it.steps, len = it.seq.len;
       float total = 0.f;
       for (int i = 0; i < steps; ++i) {
@@ -314,24 +323,19 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
         total += s.x + s.y;
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&s_lempty[slot]));
-        if (!ahead) {
-          load_keys(n_item + 1);
-          ahead = true;
-        }
       }
-      if (!ahead) load_keys(n_item + 1);
       step += steps;
-      // the other groups hand their sums to the first.  (They get to the unit after the next, which takes the same place and barrier,
-      // only when all are done with this one.)
+      // the other groups hand their sums to the first.  (They get to the unit that takes the same place and barrier only when all are
+      // done with this one.)
       if (group) {
-        s_sum[n_unit & 1][group - 1][key] = total;
+        s_sum[n_unit % kUnits][group - 1][key] = total;
         __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&s_join[n_unit & 1]));
+        if (lane == 0) mbar_arrive(smem_u32(&s_join[n_unit % kUnits]));
       } else {
-        if (ok) ok = wait_bar(&s_join[n_unit & 1], (n_unit >> 1) & 1, flags, a.w.limit_ns);
+        if (ok) ok = wait_bar(&s_join[n_unit % kUnits], (n_unit / kUnits) & 1, flags, a.w.limit_ns);
         __syncwarp();
 #pragma unroll
-        for (int g = 1; g < kGroups; ++g) total += s_sum[n_unit & 1][g - 1][key];
+        for (int g = 1; g < kGroups; ++g) total += s_sum[n_unit % kUnits][g - 1][key];
         if (p < len) a.partial[((int64_t)it.list * (a.w.hkv * a.parts) + it.part * a.w.hkv + it.head) * a.room + p] = total;
       }
       ++n_unit;
@@ -389,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
       }
     };
     for (; item_ready(ok); item_done()) {
-      const Unit it = s_item[n_item & 1];
+      const Unit it = s_item[n_item % kUnits];
       if (it.p0 < 0) break;
       if (it.steps == 0) continue;
       if (kBoxes) {
@@ -489,7 +493,7 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
     auto wait = [&](uint64_t *bar, uint32_t p) { return ok = __all_sync(~0u, wait_bar(bar, p, flags, a.w.limit_ns)); };
     const uint64_t q_desc = umma_desc(q_at);
     for (; item_ready(ok); item_done()) {
-      const int p0 = s_item[n_item & 1].p0, steps = s_item[n_item & 1].steps;
+      const int p0 = s_item[n_item % kUnits].p0, steps = s_item[n_item % kUnits].steps;
       if (p0 < 0) break;
       if (steps == 0) continue;
       if (!wait(&s_kfull[n_k & 1], (n_k >> 1) & 1)) break;
@@ -521,10 +525,10 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
     for (uint32_t r = 0;; ++r, ++n_item) {
       Unit it = {};
       line.get(a, twice, (int64_t)r * gridDim.x + (r & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x), it);
-      if (!__all_sync(~0u, wait_bar(&s_iempty[n_item & 1], ((n_item >> 1) & 1) ^ 1, flags, a.w.limit_ns))) break;
+      if (!__all_sync(~0u, wait_bar(&s_iempty[n_item % kUnits], ((n_item / kUnits) & 1) ^ 1, flags, a.w.limit_ns))) break;
       if (lane == 0) {
-        s_item[n_item & 1] = it;
-        mbar_arrive(smem_u32(&s_ifull[n_item & 1]));
+        s_item[n_item % kUnits] = it;
+        mbar_arrive(smem_u32(&s_ifull[n_item % kUnits]));
       }
       __syncwarp();
       if (it.p0 < 0) break;
