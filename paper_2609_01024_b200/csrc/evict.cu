@@ -14,7 +14,7 @@
 namespace pcomoe {
 namespace {
 
-constexpr int kSelectThreads = 1024, kMoveThreads = 256;
+constexpr int kSelectThreads = 1024, kMoveThreads = 512;
 
 struct EvictSeq {                          // what the first launch leaves for the others
   int32_t left;                            // new length; -1: the sequence stays as it is
@@ -224,7 +224,7 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(CacheDev c
 constexpr int kColumn = 4;                                 // 16-byte pieces of a row that a block moves
 __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(CacheDev c, const int32_t *seqs, float *weight, int64_t weight_stride, EvictWs ws) {
   pdl_grid_wait();
-  constexpr int kRows = kMoveThreads / kColumn, U = 8, kWindow = kRows * U;
+  constexpr int kRows = kMoveThreads / kColumn, U = 4, kWindow = kRows * U;
   const int i = blockIdx.z;
   const EvictSeq s = ws.seq[i];
   if (s.left < 0 || s.first >= s.left) return;
