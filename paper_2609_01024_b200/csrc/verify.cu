@@ -71,8 +71,8 @@ __device__ __forceinline__ double pow2(float x, float m, double c16, float least
   const double w = table[k & (kTable - 1)], r = fma(w, p, w);
   return x < least ? 0.0 : __hiloint2double(__double2hiint(r) + ((k >> 4) << 20), __double2loint(r));
 }
-// the smallest x that pow2 takes
-__device__ __forceinline__ float least_of(float m, double c) { return (float)fmax((double)m - 990.0 / c, -3.4e38); }
+// the smallest x that pow2 takes; span = 990 / c
+__device__ __forceinline__ float least_of(float m, double span) { return (float)fmax((double)m - span, -3.4e38); }
 __device__ __forceinline__ void fill_table(double *table) {
   for (int i = threadIdx.x; i < kTable; i += blockDim.x) table[i] = exp2(i * (1.0 / kTable));
 }
@@ -150,11 +150,6 @@ struct Cluster {
   }
 };
 
-__device__ __forceinline__ double warp_sum(double x) {
-#pragma unroll
-  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
-  return x;
-}
 __device__ __forceinline__ unsigned long long warp_max(unsigned long long x) {
 #pragma unroll
   for (int o = 16; o; o >>= 1) x = max(x, __shfl_xor_sync(~0u, x, o));
@@ -187,20 +182,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) row_sums_kernel(const __grid_c
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int t = blockIdx.x / CL;
   Cluster<CL> cl = {&s_box, 0};
-  // the row's sequence
-  int s = 0;
-  {
-    int hi = a.n;
-    while (hi - s > 1) {
-      const int step = (hi - s + 31) / 32, i = s + (lane + 1) * step;
-      const int k = __popc(__ballot_sync(~0u, i < hi && a.cu[min(i, hi)] <= t));
-      hi = min(s + (k + 1) * step, hi);
-      s += k * step;
-    }
-  }
-  if (t >= a.T || t < a.cu[s] || t >= a.cu[s + 1]) return; // (every block of the cluster)
-  const bool greedy = greedy_of(a, s);
-  const float c = (float)fmin(rate_of(a, s), 3e38);
+  if (t >= a.T) return;                                    // (there is a block for no rows)
   const T *row = row_of<T>(a, t);
   const int shift = shift_of(row), groups = (a.V + shift + 32 * N - 1) / (32 * N), per = (groups + CL - 1) / CL;
   const int g0 = min(cl.rank() * per, groups), g1 = min(g0 + per, groups);
@@ -222,7 +204,21 @@ __global__ void __launch_bounds__(32 * kSumWarps) row_sums_kernel(const __grid_c
     }
   };
   int g = g0 + warp * kLoads;
-  if (g < g1) fetch(g);
+  if (g < g1) fetch(g);                                    // on its way while the sequence is looked up
+  // the row's sequence
+  int s = 0;
+  {
+    int hi = a.n;
+    while (hi - s > 1) {
+      const int step = (hi - s + 31) / 32, i = s + (lane + 1) * step;
+      const int k = __popc(__ballot_sync(~0u, i < hi && a.cu[min(i, hi)] <= t));
+      hi = min(s + (k + 1) * step, hi);
+      s += k * step;
+    }
+  }
+  if (t < a.cu[s] || t >= a.cu[s + 1]) return;             // (every block of the cluster)
+  const bool greedy = greedy_of(a, s);
+  const float c = (float)fmin(rate_of(a, s), 3e38);
   for (; g < g1; g += kSumWarps * kLoads) {
     uint4 v[kLoads];
 #pragma unroll
@@ -316,7 +312,11 @@ __global__ void __launch_bounds__(32 * kSumWarps) row_sums_kernel(const __grid_c
 
 // The walk and the next token.  CL blocks per sequence.
 constexpr int kWalkWarps = 16, kWalkThreads = 32 * kWalkWarps, kChunk = kWalkThreads;
-constexpr float kMargin = 1.f / 8192;     // of a test in 32 bits
+// Whether 32 bits may not decide want < r.  A row's sum is off by at most 2^-14 of itself (20 times 2^-23 from the products' rounding
+// where the words' own logarithms average 20 bits, and a step of 2^-24 for each addition of a lane); `size`: what want and r were formed from.
+__device__ __forceinline__ bool near_border(float want, float r, float size) {
+  return !(fabsf(want - r) > (1.f / 8192) * size) || fmaxf(want, r) < 1e-30f;
+}
 template <typename T, int CL>
 __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_constant__ VerifyArgs a, int room) {
   // The launch before this one in the stream is row_sums_kernel's, which let this one begin only after all earlier work was
@@ -330,6 +330,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
   __shared__ double s_warp[2][3][kWalkWarps];              // what the warps hand to the cluster, in turn
   __shared__ float s_p[kChunk], s_q[kChunk], s_u[kChunk];
   __shared__ int s_parent[kChunk];
+  __shared__ uint8_t s_first[kChunk];                      // the test where a draft is the first at its parent: 1 taken, 2 near its border
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int seq = blockIdx.x / CL, rank = CL > 1 ? (int)(blockIdx.x % CL) : 0;
   const bool first_block = rank == 0;
@@ -344,7 +345,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
   }
   fill_table(s_table);
   const bool greedy = greedy_of(a, seq);
-  const double c = rate_of(a, seq), c16 = 16 * c;
+  const double c = rate_of(a, seq), c16 = 16 * c, span = 990.0 / c;
   const float c32 = (float)fmin(c, 3e38);
   __syncthreads();
   auto parent_of = [&](int k) { return a.parent ? a.parent[rows.x + k] : k - 1; };
@@ -368,7 +369,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
     per = (groups + CL - 1) / CL;
     g0 = min(rank * per, groups);
     g1 = min(g0 + per, groups);
-    const float m = sums.m, least = least_of(m, c);
+    const float m = sums.m, least = least_of(m, span);
     const double cut = A * sums.s;
     const float *near = rest.value ? a.near + (int64_t)(rows.x + cur) * a.near_stride : nullptr;
     double we = 0.0, wp = 0.0, wq = 0.0;
@@ -523,7 +524,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
   auto p_of = [&](int token) {
     if (greedy) return token == sums.best ? 1.0 : 0.0;
     const float x = eligible(Vec<T>::one(row_of<T>(a, rows.x + cur) + token));
-    return x != kNone && sums.s > 0.0 ? pow2(x, sums.m, c16, least_of(sums.m, c), s_table) / sums.s : 0.0;
+    return x != kNone && sums.s > 0.0 ? pow2(x, sums.m, c16, least_of(sums.m, span), s_table) / sums.s : 0.0;
   };
   // whether one of the drafts [from, to) hangs on cur and has this token
   auto named = [&](int from, int to, int token) {
@@ -560,6 +561,10 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
       else if (x != kNone && at.s > 0.0) p = ex2((x - at.m) * c32) / (float)at.s;
     }
     s_p[tid] = p;
+    {
+      const float want = (j < rows.y && j > 0 ? s_u[tid] : 0.f) * q;
+      s_first[tid] = near_border(want, p, want + p) ? 2 : want < p;
+    }
     __syncthreads();
     const int in_chunk = min(kChunk, rows.y - c0);
     // every warp of every block takes the same way
@@ -590,32 +595,34 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
         due = false;
         if (!(R > 0.0)) { A = 0.0; R = 1.0; }              // nothing is left: the target's own distribution again
       }
-      // In 32 bits a row's sum is off by at most 2^-14 of itself (20 times 2^-23 from the products' rounding where the words' own logarithms
-      // average 20 bits, and a step of 2^-24 for each addition of a lane): where that could turn the answer, 64 bits give it.
-      bool taken;
-      {
-        const float p = s_p[hit], q = s_q[hit], u = s_u[hit], aq = (float)A * q;
-        const float rr = a.near ? (float)R : 1.f - gone;
+      bool taken, close;
+      const float q = s_q[hit], u = s_u[hit];
+      if (!refused) {
+        taken = s_first[hit] & 1;
+        close = s_first[hit] & 2;
+      } else {
+        const float p = s_p[hit], aq = (float)A * q, rr = a.near ? (float)R : 1.f - gone;
         const float r = again ? 0.f : p - aq, want = u * q * rr;
         taken = want < r;
-        if (!(fabsf(want - r) > kMargin * (u * q * (a.near ? rr : 1.f) + p + aq)) || fmaxf(want, r) < 1e-30f) {
-          const int token = a.tokens[rows.x + c0 + hit];
-          if (greedy) {
-            sums = a.sums[rows.x + cur];
-            exact = true;
-          }
-          refine();
-          const double p64 = p_of(token), q64 = (double)q;
-          double r64 = again ? 0.0 : fmax(p64 - A * q64, 0.0), R64 = R;
-          if (!a.near) {
-            for (int k = cur + 1; k < c0 + hit; ++k) {     // without the refused tokens, each once
-              const int other = a.tokens[rows.x + k];
-              if (parent_of(k) == cur && other >= 0 && other < a.V && !named(cur + 1, k, other)) R64 -= p_of(other);
-            }
-            if (!(R64 > 0.0)) R64 = 1.0;
-          }
-          taken = (double)u * R64 * q64 < r64;
+        close = near_border(want, r, u * q * (a.near ? rr : 1.f) + p + aq);
+      }
+      if (close) {                                         // 64 bits give the answer
+        const int token = a.tokens[rows.x + c0 + hit];
+        if (greedy) {
+          sums = a.sums[rows.x + cur];
+          exact = true;
         }
+        refine();
+        const double p64 = p_of(token), r64 = again ? 0.0 : fmax(p64 - A * (double)q, 0.0);
+        double R64 = R;
+        if (!a.near) {
+          for (int k = cur + 1; k < c0 + hit; ++k) {       // without the refused tokens, each once
+            const int other = a.tokens[rows.x + k];
+            if (parent_of(k) == cur && other >= 0 && other < a.V && !named(cur + 1, k, other)) R64 -= p_of(other);
+          }
+          if (!(R64 > 0.0)) R64 = 1.0;
+        }
+        taken = (double)u * R64 * (double)q < r64;
       }
       if (taken) {
         cur = c0 + hit;
@@ -742,7 +749,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
         const uint32_t out = marked ? s_out[g * 32 + lane] : 0u;
         const float *near = rest ? a.near + (int64_t)(rows.x + cur) * a.near_stride : nullptr;
         const int id = ((g0 + g) * 32 + lane) * N - shift;
-        const float least = least_of(sums.m, c);
+        const float least = least_of(sums.m, span);
         double e[N], lane_sum = 0.0;
         int last_word = -1;
 #pragma unroll
@@ -774,6 +781,8 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
   Cluster<CL>::barrier();                                  // nobody leaves while others read its sums
 }
 
+constexpr int kGroupBytes = 8 + 8 + 32;   // of shared memory for each group of a block: two sums, a byte per lane
+
 template <typename... K, typename... A>
 cudaError_t launch_clusters(void (*kernel)(K...), int items, int cl, int threads, size_t smem, cudaStream_t st, A... args) {
   cudaLaunchConfig_t cfg = {};
@@ -799,6 +808,34 @@ pcomoe_status launch_sums(const VerifyArgs &a, cudaStream_t st) {
   count_launch();
   return PCOMOE_OK;
 }
+// Whether clusters of 16 blocks find room on the current device, which 8 always do: asked once for each device.
+template <typename T>
+bool room_for_16() {
+  static std::atomic<uint64_t> asked{0}, there{0};
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
+  const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
+  if (asked.load(std::memory_order_acquire) & bit) return (there.load(std::memory_order_relaxed) & bit) != 0;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(16);
+  cfg.blockDim = dim3(kWalkThreads);
+  cfg.dynamicSmemBytes = kMaxGroups * kGroupBytes;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = 16;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int clusters = 0;
+  const bool ok = cudaFuncSetAttribute(walk_kernel<T, 16>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                  cudaFuncSetAttribute(walk_kernel<T, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxGroups * kGroupBytes) == cudaSuccess &&
+                  cudaOccupancyMaxActiveClusters(&clusters, walk_kernel<T, 16>, &cfg) == cudaSuccess && clusters > 0;
+  if (!ok) cudaGetLastError();                             // the answer is no, not an error of a later call
+  if (ok) there.fetch_or(bit, std::memory_order_relaxed);
+  asked.fetch_or(bit, std::memory_order_release);
+  return ok;
+}
+
 template <typename T, int CL>
 pcomoe_status launch_walk(const VerifyArgs &a, int groups, cudaStream_t st) {
   const int room = ((groups + CL - 1) / CL + 1) & ~1;
@@ -806,10 +843,10 @@ pcomoe_status launch_walk(const VerifyArgs &a, int groups, cudaStream_t st) {
   int dev = -1;
   PCOMOE_CUDA_TRY(cudaGetDevice(&dev));
   if (once.first_use(dev)) {
-    PCOMOE_CUDA_TRY(cudaFuncSetAttribute(walk_kernel<T, CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxGroups * (8 + 8 + 32)));
+    PCOMOE_CUDA_TRY(cudaFuncSetAttribute(walk_kernel<T, CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxGroups * kGroupBytes));
     once.done(dev);
   }
-  PCOMOE_CUDA_TRY(launch_clusters(walk_kernel<T, CL>, a.n, CL, kWalkThreads, (size_t)room * (8 + 8 + 32), st, a, room));
+  PCOMOE_CUDA_TRY(launch_clusters(walk_kernel<T, CL>, a.n, CL, kWalkThreads, (size_t)room * kGroupBytes, st, a, room));
   count_launch();
   return PCOMOE_OK;
 }
@@ -818,20 +855,23 @@ template <typename T>
 pcomoe_status run(const VerifyArgs &a, int sms, cudaStream_t st) {
   const int groups = (a.V + 15) / (32 * Vec<T>::N) + 1;    // at any alignment
   // blocks per row and per sequence: while there is an SM for each and enough groups for its warps
-  const auto blocks = [&](int items, int warps) {
+  const auto blocks = [&](int items, int warps, int most) {
     int cl = 1;
-    while (cl < 8 && ((int64_t)items * 2 * cl <= sms || groups > cl * (kMaxGroups - 2)) && groups >= 2 * cl * warps) cl *= 2;
+    while (cl < most && ((int64_t)items * 2 * cl <= sms || groups > cl * (kMaxGroups - 2)) && groups >= 2 * cl * warps) cl *= 2;
     return cl;
   };
   pcomoe_status s = PCOMOE_OK;
-  switch (blocks(std::max(a.T, 1), kSumWarps)) {           // (launched for no rows too: the second launch leans on the first)
+  switch (blocks(std::max(a.T, 1), kSumWarps, 8)) {           // (launched for no rows too: the second launch leans on the first)
     case 1: s = launch_sums<T, 1>(a, st); break;
     case 2: s = launch_sums<T, 2>(a, st); break;
     case 4: s = launch_sums<T, 4>(a, st); break;
     default: s = launch_sums<T, 8>(a, st); break;
   }
   if (s != PCOMOE_OK) return s;
-  switch (blocks(a.n, kWalkWarps)) {
+  int cl = blocks(a.n, kWalkWarps, 16);
+  if (cl == 16 && !room_for_16<T>()) cl = 8;
+  switch (cl) {
+    case 16: return launch_walk<T, 16>(a, groups, st);
     case 1: return launch_walk<T, 1>(a, groups, st);
     case 2: return launch_walk<T, 2>(a, groups, st);
     case 4: return launch_walk<T, 4>(a, groups, st);

@@ -75,3 +75,41 @@ def test_one_turn_step_by_step():
     now = ref.rows_of(model.cache.k[0], model.cache.page_table[0].tolist(), model.cache.page_size, 40).double().cpu()
     assert torch.equal(now, kept)
     assert [model.cache.device_status(), model.attn.device_status(), model.weights.device_status(), model.verifier.device_status()] == [0] * 4
+
+
+def test_two_objects_at_the_same_time():
+    """Two loops' objects on two streams, their calls interleaved, give what each gives alone."""
+    m = example()
+    B = m.B
+    rng = np.random.default_rng(7)
+    work = []
+    for i, (V, rows, lens) in enumerate(((3000, 7, [900, 40]), (32000, 4, [60, 2500]))):
+        n = len(lens)
+        T = n * rows
+        c = ref.cache_of(B, B.PCOMOE_BF16, page=16, kv_heads=2, head_dim=64, lens=lens, seed=i)
+        w = dict(logits=torch.randn(T, V, device="cuda").bfloat16(), tokens=m.ints(rng.integers(0, V, T)), cu=m.cu_of([rows] * n), u=m.floats(rng.random(T)),
+                 u_next=m.floats(rng.random(n)), near=torch.softmax(torch.randn(T, V, device="cuda"), 1), seqs=m.ints(range(n)), cache=c, weights=B.CacheWeights(c, q_heads=8),
+                 q=torch.randn(T, 8, 64, device="cuda").bfloat16(), lse=torch.full((T, 8), 6.0, device="cuda"), verifier=B.DraftVerifier(max_seqs=n, max_path=rows),
+                 rotation=B.HeadRotation(q_heads=8, kv_heads=2, head_dim=64, inv_freq=np.linspace(1, 0.001, 32)), k=torch.randn(T, 2, 64, device="cuda").bfloat16(),
+                 position=m.ints(rng.integers(0, 9999, T)), stream=torch.cuda.Stream())
+        work.append(w)
+
+    def turn(w):
+        w["weights"].weight.zero_()
+        q = torch.empty_like(w["q"])
+        w["rotation"].rotate_cached(w["q"], w["k"], w["k"], w["position"], w["cache"], 0, w["seqs"], w["cu"], q)
+        out = [x.clone() for x in w["verifier"].verify(w["logits"], w["tokens"], w["cu"], w["u"], w["u_next"], draft_probs=w["near"])]
+        w["weights"].add(q, w["lse"], 0, w["seqs"], w["cu"], fresh=True)
+        return out + [q, w["weights"].weight.clone()]
+
+    want = [turn(w) for w in work]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for i, w in enumerate(work):
+            with torch.cuda.stream(w["stream"]):
+                got[i] = turn(w)
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
+    assert [w[k].device_status() for w in work for k in ("cache", "weights", "verifier")] == [0] * 6

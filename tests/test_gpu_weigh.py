@@ -216,9 +216,11 @@ def test_after_attention():
 
 
 @pytest.mark.parametrize("hq,hkv,d,page,ctx,add", [(32, 8, 128, 64, [0], [700]), (8, 8, 64, 16, [130, 0, 1000], [257, 128, 90]), (28, 4, 128, 32, [5], [300]), (6, 2, 128, 128, [0, 0, 0, 60], [200, 0, 1, 333]),
-                                                   (4, 1, 64, 16, [2000], [150]), (10, 10, 128, 16, [77], [129]), (7, 1, 128, 64, [0], [1000])])
+                                                   (4, 1, 64, 16, [2000], [150]), (10, 10, 128, 16, [77], [129]), (7, 1, 128, 64, [0], [1000]), (32, 8, 128, 16, [500], [30]),
+                                                   (8, 2, 64, 32, [9] * 40, [24] * 39 + [100])])
 def test_many_rows(hq, hkv, d, page, ctx, add):
-    """Column tiles that groups of heads do not divide, units without columns, more steps than there are places for log sums."""
+    """Column tiles that groups of heads do not divide, units without columns, more steps than there are places for log sums, fewer rows
+    than a tile holds, more sequences than a warp has lanes."""
     c = Case("bf16", hq, hkv, d, page, ctx, add, seed=hq + d, behind=5)
     c.check()
     c.check(fresh=False)
