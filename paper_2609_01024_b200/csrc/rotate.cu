@@ -8,8 +8,8 @@
 // What bounds it: HBM, every row read and written once (with few rows the latency of one chain position -> angle and list ->
 // length -> page).  D / 16 lanes hold a head, two 16-byte pieces each, chosen so that both elements of a pair lie in one lane
 // and a lane's angles are the same for all heads of its token: a warp forms a token's angles once and walks over its
-// heads, the next heads' loads under way.  Measured, 16384 tokens of 16 + 16 + 16 heads of 128 into packed rows and pages: 88 us, 5.3
-// TB/s read and written, 0.82 of a plain copy's rate.  (Four heads' loads ahead and half the warps per SM took 111 us, no load
+// heads, the next heads' loads under way.  Measured, 16384 tokens of 16 + 16 + 16 heads of 128 into packed rows and pages: 86 us, 5.5
+// TB/s read and written, 0.85 of a plain copy's rate.  (Four heads' loads ahead and half the warps per SM took 111 us, no load
 // ahead and 32 warps 94, packed two-element arithmetic 93.)  32 decode rows of 32 + 8 + 8 heads: 4 us.
 #include <algorithm>
 #include <cmath>
@@ -19,7 +19,7 @@
 namespace pcomoe {
 namespace {
 
-constexpr int kWarps = 4;
+constexpr int kWarps = 2;
 
 struct RotateArgs {
   int32_t T, hq, hkv, rot, neighbours;
@@ -103,7 +103,7 @@ __device__ __forceinline__ int64_t place_of(const RotateArgs &a, int t) {
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(32 * kWarps, 6) rotate_kernel(const __grid_constant__ RotateArgs a) {
+__global__ void __launch_bounds__(32 * kWarps, 12) rotate_kernel(const __grid_constant__ RotateArgs a) {
   constexpr int G = D / 16, kHeads = 32 / G, E = (int)sizeof(T);
   pdl_grid_wait();
   const int lane = threadIdx.x & 31, l = lane % G, sub = lane / G;
