@@ -14,7 +14,7 @@
 namespace pcomoe {
 namespace {
 
-constexpr int kSelectThreads = 1024, kMoveThreads = 512;
+constexpr int kSelectThreads = 1024;
 
 struct EvictSeq {                          // what the first launch leaves for the others
   int32_t left;                            // new length; -1: the sequence stays as it is
@@ -222,9 +222,10 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(CacheDev c
 
 // blockIdx: (head and column, layer and K or V, sequence); one column more, for the first layer's K, moves the weights.
 constexpr int kColumn = 4;                                 // 16-byte pieces of a row that a block moves
+template <int kMoveThreads>
 __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(CacheDev c, const int32_t *seqs, float *weight, int64_t weight_stride, EvictWs ws) {
   pdl_grid_wait();
-  constexpr int kRows = kMoveThreads / kColumn, U = 4, kWindow = kRows * U;
+  constexpr int kRows = kMoveThreads / kColumn, U = 8, kWindow = kRows * U;
   const int i = blockIdx.z;
   const EvictSeq s = ws.seq[i];
   if (s.left < 0 || s.first >= s.left) return;
@@ -242,33 +243,39 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(CacheDev c, co
   const int64_t row_bytes = (int64_t)c.chunks * 16;
   auto place = [&](int page, int slot) { return pool + (int64_t)page * c.page_bytes + slot * row_bytes; };
   const int r = threadIdx.x / kColumn;
-  // Three windows at work: the places of one are asked for, the rows of the one before come in, those of the one before that are stored.
-  int from[U], to[U], to_next[U];
+  // Windows at work: the places of one are asked for, those of the one before are at hand, the rows of the one before that come in, and
+  // the first one's are stored.
+  int from[U], to[U], from_next[U], to_next[U];
   uint4 x[U];
   auto ask = [&](int j0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int j = j0 + u * kRows + r;
-      from[u] = has && j < s.left ? list[j] : -1;
+      from_next[u] = has && j < s.left ? list[j] : -1;
       to_next[u] = has && j < s.left ? row[j >> c.shift] : 0;
     }
   };
+  auto take = [&]() {
+#pragma unroll
+    for (int u = 0; u < U; ++u) { from[u] = from_next[u]; to[u] = to_next[u]; }
+  };
   auto fetch = [&]() {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
+    for (int u = 0; u < U; ++u)
       if (from[u] >= 0) x[u] = *(const uint4 *)place(from[u] >> c.shift, from[u] & (c.page - 1));
-      to[u] = to_next[u];
-    }
   };
   ask(s.first);
+  take();
+  ask(s.first + kWindow);
   fetch();
   for (int j0 = s.first; j0 < s.left; j0 += kWindow) {
-    ask(j0 + kWindow);
     __syncthreads();                                       // the window is read
     uint4 y[U];
     int at[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) { y[u] = x[u]; at[u] = to[u]; }
+    take();
+    ask(j0 + 2 * kWindow);
     fetch();                                               // of the next one: its rows lie behind all that is written now
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -351,7 +358,12 @@ pcomoe_status pcomoe_cache_evict(const pcomoe_cache *cache, int32_t n, const int
     default: st = launch_select<8>(c, n, d_seqs, d_budget, sinks, recent, d_weight, weight_stride, w, s); break;
   }
   if (st != PCOMOE_OK) return st;
-  PCOMOE_CUDA_TRY(launch_pdl(evict_move_kernel, dim3((unsigned)columns, 2 * c.layers, n), dim3(kMoveThreads), 0, s, c, d_seqs, d_weight, weight_stride, w));
+  // A column each for few blocks is walked over with 512 threads, more of its rows under way; many blocks have 256 (one sequence of 131071
+  // tokens cut to a quarter in 2 layers: the whole pass 492 us, with 256 threads 527; 8 sequences of 905 to 4050 in 4 layers 171, with
+  // 512 threads 186).
+  const dim3 grid((unsigned)columns, 2 * c.layers, n);
+  if (columns * 2 * c.layers * n <= 2 * sms) PCOMOE_CUDA_TRY(launch_pdl(evict_move_kernel<512>, grid, dim3(512), 0, s, c, d_seqs, d_weight, weight_stride, w));
+  else PCOMOE_CUDA_TRY(launch_pdl(evict_move_kernel<256>, grid, dim3(256), 0, s, c, d_seqs, d_weight, weight_stride, w));
   PCOMOE_CUDA_TRY(launch_pdl(evict_book_kernel, dim3(n), dim3(256), 0, s, c, d_seqs, w));
   count_launch(3);
   return PCOMOE_OK;
