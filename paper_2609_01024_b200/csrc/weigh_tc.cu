@@ -95,26 +95,6 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map
                : "memory");
 }
 
-// 2^d of two numbers without the special function unit: the nearest whole number apart, and for the rest f in [-1/2, 1/2] a
-// polynomial of degree 5 whose largest relative error is 7.5e-8 (fitted to 2^f by weighted least squares until the error is
-// level).  Held inside [-126, 128], where 2^128 is infinite; a NaN stays one.
-__device__ __forceinline__ float2 exp2_poly(float2 d) {
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(d.x) : "f"(-126.f));
-  asm("max.NaN.f32 %0, %0, %1;" : "+f"(d.y) : "f"(-126.f));
-  asm("min.NaN.f32 %0, %0, %1;" : "+f"(d.x) : "f"(128.f));
-  asm("min.NaN.f32 %0, %0, %1;" : "+f"(d.y) : "f"(128.f));
-  const auto both = [](float v) { return make_float2(v, v); };
-  const float2 t = add2(d, both(12582912.f));               // 1.5 * 2^23: the last place is 1
-  const float2 f = add2(d, fma2(add2(t, both(-12582912.f)), both(-1.f), both(0.f)));
-  float2 p = fma2(both(0.0013276471781f), f, both(0.0096755413328f));
-  p = fma2(p, f, both(0.0555071327415f));
-  p = fma2(p, f, both(0.2402211972388f));
-  p = fma2(p, f, both(0.6931469670644f));
-  p = fma2(p, f, both(1.0000000716547f));
-  const float2 s = make_float2(__int_as_float((__float_as_int(t.x) << 23) + 0x3f800000), __int_as_float((__float_as_int(t.y) << 23) + 0x3f800000));
-  return fma2(p, s, both(0.f));
-}
-
 // The units of a call, in one line: sequence, keys, head and part, the last fastest.  One warp.
 struct Line {
   int s0;               // sequences s0 + lane are in hand
