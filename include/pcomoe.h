@@ -483,7 +483,7 @@ pcomoe_status pcomoe_token_logprobs(int32_t dtype, int32_t T, int32_t V, const v
 /*
  * Norm and rotation of the heads of queries and keys, in one pass.  Set struct_size = sizeof(pcomoe_rotate_config).
  * A head x of D elements with a weight w becomes  y = x w / sqrt(mean x^2 + eps)  (without a weight y = x; squares are summed
- * in fp32, so elements beyond 1e18 overflow them), and pair i < rot_dim / 2 of y becomes
+ * in fp32, so elements beyond 1e18 overflow them and those below 1e-23 count for nothing beside eps), and pair i < rot_dim / 2 of y becomes
  *     (a cos t - b sin t, a sin t + b cos t),   t = position * inv_freq[i],
  * where the pair is (y[i], y[i + rot_dim / 2]) or (y[2 i], y[2 i + 1]); elements from rot_dim on are not rotated.
  */
@@ -577,11 +577,12 @@ pcomoe_status pcomoe_cache_evict(const pcomoe_cache *cache, int32_t n, const int
  *   d_keep [n, keep_stride] int32, d_n_keep [n]: the walk's rows, row 0 first, ready for pcomoe_cache_keep; the rest of d_keep is -1;
  *                a walk ends after keep_stride rows.
  *   d_next [n] int32: -1 where no word is eligible.  A sequence without rows gets n_keep = 0 and next = -1.
- * All that decides a token is formed in 64 bits.  Results are a function of the arguments.
+ * All that decides a token is formed in 64 bits.  Results are a function of the arguments.  Outputs are no inputs (INVALID_ARG), but
+ * where all sequences have one row d_tokens, d_parent and d_u may be outputs' (a longer one counts as empty then: INDEX).
  * Workspace: pcomoe_verify_workspace_bytes(T), 256-byte aligned, first 256 bytes zero before the first use, one call at a time.
  * Errors: INVALID_ARG, SHAPE (T < 0, V <= 0, n < 0 or > 65535, keep_stride < 0), UNSUPPORTED (V > 2^20), WORKSPACE, CUDA.
- * Device: INDEX (d_cu_len not ascending or past T: that sequence counts as empty; a draft whose parent or token is out of range
- * is passed over).
+ * Device: INDEX (d_cu_len not ascending or past T: that sequence counts as empty, and rows of others that lie in it too may count
+ * as rows without eligible words; a draft whose parent or token is out of range is passed over).
  */
 pcomoe_status pcomoe_verify_workspace_bytes(int32_t max_tokens, size_t *bytes);
 pcomoe_status pcomoe_verify_drafts(int32_t dtype, int32_t T, int32_t V, int32_t n, const int32_t *d_cu_len, const int32_t *d_tokens, const int32_t *d_parent,

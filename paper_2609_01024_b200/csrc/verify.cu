@@ -19,6 +19,7 @@
 // What bounds them: the rows' one read (HBM) in the first; in the second a chain of dependent steps, since an operation in 64
 // bits takes some 45 clocks until the next one can use it.
 #include <algorithm>
+#include <cfloat>
 #include <type_traits>
 
 #include "words.cuh"
@@ -48,6 +49,7 @@ struct VerifyArgs {
   const float *temperature, *u, *u_next;
   int32_t *keep, *n_keep, *next;
   int32_t keep_stride;
+  int32_t most_rows;                      // of a sequence
   VerifyHeader *head;
   RowSums *sums;
 };
@@ -72,7 +74,7 @@ __device__ __forceinline__ double pow2(float x, float m, double c16, float least
   return x < least ? 0.0 : __hiloint2double(__double2hiint(r) + ((k >> 4) << 20), __double2loint(r));
 }
 // the smallest x that pow2 takes; span = 990 / c
-__device__ __forceinline__ float least_of(float m, double span) { return (float)fmax((double)m - span, -3.4e38); }
+__device__ __forceinline__ float least_of(float m, double span) { return (float)fmax((double)m - span, -(double)FLT_MAX); }
 __device__ __forceinline__ void fill_table(double *table) {
   for (int i = threadIdx.x; i < kTable; i += blockDim.x) table[i] = exp2(i * (1.0 / kTable));
 }
@@ -92,6 +94,9 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
   return *(float2 *)&d;
 }
 
+// 2^((x - m) c) in 32 bits for x <= m, any of them finite (their difference need not be) or x = -inf
+__device__ __forceinline__ float weight_of(float x, float m, float c) { return ex2(fmaxf((0.5f * x - 0.5f * m) * c * 2.f, -1000.f)); }
+
 __device__ __forceinline__ float real(float q) { return q > 0.f && q < INFINITY ? q : 0.f; }      // what is no probability counts as 0
 
 template <typename T> __device__ __forceinline__ const T *row_of(const VerifyArgs &a, int t) { return (const T *)(a.x + (int64_t)t * a.row_bytes); }
@@ -107,7 +112,7 @@ __device__ __forceinline__ bool greedy_of(const VerifyArgs &a, int s) { return a
 // Rows of sequence s; empty and reported where the list is no list.
 __device__ __forceinline__ int2 rows_of(const VerifyArgs &a, int s) {
   const int from = a.cu[s], to = a.cu[s + 1];
-  if (from < 0 || to < from || to > a.T) {
+  if (from < 0 || to < from || to > a.T || to - from > a.most_rows) {
     atomicCAS(&a.head->status, 0, (int)PCOMOE_ERR_INDEX);
     return make_int2(0, 0);
   }
@@ -216,7 +221,11 @@ __global__ void __launch_bounds__(32 * kSumWarps) row_sums_kernel(const __grid_c
       s += k * step;
     }
   }
-  if (t < a.cu[s] || t >= a.cu[s + 1]) return;             // (every block of the cluster)
+  if (t < a.cu[s] || t >= a.cu[s + 1]) {                   // (every block of the cluster)
+    // nothing to draw from, should a list that does not ascend bring a walk here
+    if (cl.rank() == 0 && threadIdx.x == 0) a.sums[t] = {0.0, -INFINITY, -1};
+    return;
+  }
   const bool greedy = greedy_of(a, s);
   const float c = (float)fmin(rate_of(a, s), 3e38);
   for (; g < g1; g += kSumWarps * kLoads) {
@@ -241,7 +250,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) row_sums_kernel(const __grid_c
       most = max(max(k4[0], k4[1]), max(k4[2], k4[3]));
     }
     if (most > key) {
-      if (sum > 0.f) sum *= ex2((of_key(key) - of_key(most)) * c);
+      if (sum > 0.f) sum *= weight_of(of_key(key), of_key(most), c);
 #pragma unroll
       for (int u = kLoads - 1; u >= 0; --u)
         if (k4[u] == most) best_g = g + u;
@@ -249,7 +258,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) row_sums_kernel(const __grid_c
     }
     if (greedy || key <= kNoKey) continue;
     const float m = of_key(key);
-    if (fabsf(m) < 1e6f) {                                 // (words held above -1e30, NaN and -inf with them: their weight is 0)
+    if (fabsf(m) < 1e6f && c > 1e-20f) {                   // (words held above -1e30, NaN and -inf with them: their weight is 0)
       const float2 c2 = make_float2(c, c), minus = make_float2(-m, -m);
       float2 s2[4] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
@@ -270,7 +279,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) row_sums_kernel(const __grid_c
         float x[N];
         Vec<T>::unpack(v[u], x);
 #pragma unroll
-        for (int k = 0; k < N; ++k) sum += ex2(fmaxf((eligible(x[k]) - m) * c, -1000.f));
+        for (int k = 0; k < N; ++k) sum += weight_of(eligible(x[k]), m, c);
       }
     }
   }
@@ -280,7 +289,7 @@ __global__ void __launch_bounds__(32 * kSumWarps) row_sums_kernel(const __grid_c
   __syncthreads();
   // the warps', then the blocks', over the largest of all; ties go to the lowest group
   const auto join = [&](float part, unsigned long long from, unsigned long long to) {
-    return part > 0.f ? part * ex2((of_key(place_key(from)) - of_key(place_key(to))) * c) : 0.f;
+    return part > 0.f ? part * weight_of(of_key(place_key(from)), of_key(place_key(to)), c) : 0.f;
   };
   unsigned long long place = 0;
   float total = 0.f;
@@ -558,7 +567,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
     if (up >= 0) {
       const RowSums at = a.sums[rows.x + up];
       if (greedy) p = token == at.best ? 1.f : 0.f;
-      else if (x != kNone && at.s > 0.0) p = ex2((x - at.m) * c32) / (float)at.s;
+      else if (x != kNone && at.s > 0.0) p = weight_of(x, at.m, c32) / (float)at.s;
     }
     s_p[tid] = p;
     {
@@ -716,7 +725,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
         for (int i = lane * each; i < min((lane + 1) * each, mine); ++i) {
           const double x = group_at(i);
           sum += x;
-          if (x > 0.0) last = i;
+          if (s_group[i] > 0.0) last = i;                  // (a difference of sums may round to 0)
         }
         double upto = sum;
 #pragma unroll
@@ -879,6 +888,15 @@ pcomoe_status run(const VerifyArgs &a, int sms, cudaStream_t st) {
   }
 }
 
+struct Range {                            // of memory; NULL: none
+  const void *at;
+  int64_t bytes;
+  bool meets(const Range &o) const {
+    const uintptr_t a = (uintptr_t)at, b = (uintptr_t)o.at;
+    return at && o.at && bytes > 0 && o.bytes > 0 && a < b + (uintptr_t)o.bytes && b < a + (uintptr_t)bytes;
+  }
+};
+
 }  // namespace
 }  // namespace pcomoe
 
@@ -906,10 +924,23 @@ pcomoe_status pcomoe_verify_drafts(int32_t dtype, int32_t T, int32_t V, int32_t 
   if (T > 0 && (row_stride < V || (uintptr_t)d_logits % e || (d_draft_probs && (draft_stride < V || (uintptr_t)d_draft_probs % 4)))) return PCOMOE_ERR_INVALID_ARG;
   if ((int64_t)T * 8 > INT32_MAX) return PCOMOE_ERR_SHAPE;
   if (!d_workspace || ((uintptr_t)d_workspace & 255) || ws_bytes < 256 + sizeof(RowSums) * (size_t)T) return PCOMOE_ERR_WORKSPACE;
+  // An output among the inputs: the blocks of a cluster would read different things.  What only drafts need (tokens, parents, u) may be
+  // an output's where there are none.
+  const Range out[3] = {{d_keep, 4 * (int64_t)n * keep_stride}, {d_n_keep, 4 * (int64_t)n}, {d_next, 4 * (int64_t)n}};
+  const Range in[5] = {{d_cu_len, 4 * ((int64_t)n + 1)}, {d_temperature, 4 * (int64_t)n}, {d_u_next, 4 * (int64_t)n},
+                       {d_logits, T ? (((int64_t)T - 1) * row_stride + V) * e : 0}, {d_draft_probs, T ? (((int64_t)T - 1) * draft_stride + V) * 4 : 0}};
+  const Range of_drafts[3] = {{d_tokens, 4 * (int64_t)T}, {d_parent, 4 * (int64_t)T}, {d_u, 4 * (int64_t)T}};
+  bool shared = false;
+  for (const Range &o : out) {
+    for (const Range &i : in)
+      if (o.meets(i)) return PCOMOE_ERR_INVALID_ARG;
+    for (const Range &i : of_drafts) shared |= o.meets(i);
+  }
   int sms;
   const pcomoe_status st = current_sms(&sms);
   if (st != PCOMOE_OK) return st;
   VerifyArgs a = {};
+  a.most_rows = shared ? 1 : INT_MAX;
   a.T = T; a.V = V; a.n = n;
   a.cu = d_cu_len; a.tokens = d_tokens; a.parent = d_parent;
   a.x = (const char *)d_logits; a.row_bytes = row_stride * e;

@@ -142,6 +142,23 @@ def test_temperatures(temperature):
     same(c, [temperature] * 3)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_words_ruled_out_at_large_temperatures(dtype):
+    """At a temperature of 1e30 the eligible words are all but equally likely, and -inf still has no weight; the type's largest logits apart."""
+    rng = np.random.default_rng(2)
+    n, V = 200, 4
+    x = np.tile(np.array([0.0, -np.inf, 1.0, -np.inf]), (2 * n, 1))
+    c = dict(x=torch.tensor(x).to(TYPES[dtype]).cuda(), tokens=rng.choice([0, 2], 2 * n).tolist(), cu=np.arange(n + 1) * 2, parent=None, near=None,
+             u=rng.random(2 * n).astype(np.float32), u_next=rng.random(n).astype(np.float32))
+    got, _, _ = same(c, [1e30] * n)
+    assert 0.3 * n < sum(len(g) > 1 for g in got) < 0.7 * n
+    big = float(torch.finfo(TYPES[dtype]).max)
+    c["x"] = torch.tensor(np.tile(np.array([-big, -np.inf, big, 0.0]), (2 * n, 1))).to(TYPES[dtype]).cuda()
+    got, nxt, _ = same(c, [1e38] * n)
+    assert len(set(nxt)) == 3 or min(len(g) for g in got) == 1
+    same(c, [1.0] * n)
+
+
 def test_greedy_takes_the_lowest_of_the_best():
     x = torch.zeros((3, 4000), device="cuda")
     x[:, [17, 900, 3999]] = 2.0
@@ -209,6 +226,32 @@ def test_reported_and_passed_over():
         broken = 0 if cu[0] < 0 else 1
         assert int(n_keep[broken]) == 0 and int(nxt[broken]) == -1 and (keep[broken] == -1).all()
         assert v.device_status() == 7
+
+
+def test_lists_that_overlap():
+    """A list that does not ascend: that sequence is empty, the others stay inside of their rows, whatever the workspace held before."""
+    c = case(6, 64, [4, 4], True, True, "f32")
+    for temperature in ([1.0] * 3, [0.0] * 3):
+        v = B.DraftVerifier(max_seqs=3, max_path=8, max_tokens=8)
+        v.workspace[256:] = 0x7f
+        keep, n_keep, nxt = v.verify(c["x"], ints(c["tokens"]), ints([0, 5, 3, 8]), floats(c["u"]), floats([.1, .5, .9]), parent=ints([-1, 0, 0, 1, 1, -1, 0, 1]),
+                                     draft_probs=torch.tensor(c["near"], device="cuda"), temperature=floats(temperature))
+        assert n_keep.tolist()[1] == 0 and nxt.tolist()[1] == -1 and v.device_status() == 7
+        assert all(-1 <= t < 64 for t in nxt.tolist()) and all(m >= 1 for m in n_keep.tolist()[::2])
+
+
+def test_tokens_that_are_an_earlier_result():
+    """Plain sampling may be given the object's own `next` as tokens; sequences of several rows then count as empty."""
+    V, n = 500, 6
+    c = case(9, V, [1] * n, False, False, "f32")
+    v = B.DraftVerifier(max_seqs=n, max_path=2)
+    _, want, _, _ = run(c, verifier=v)
+    out = v.verify(c["x"], v.next, ints(range(n + 1)), floats(c["u"]), floats(c["u_next"]))
+    assert out[2].tolist() == want and v.device_status() == 0
+    out = v.verify(c["x"], v.next, ints([0, 2, 2, 3, 4, 5, 6]), floats(c["u"]), floats(c["u_next"]))
+    assert out[1].tolist() == [0, 0, 1, 1, 1, 1] and out[2].tolist()[:2] == [-1, -1] and v.device_status() == 7
+    with pytest.raises(Exception):
+        v.verify(c["x"], ints([0] * n), v.keep.flatten()[:n + 1], floats(c["u"]), floats(c["u_next"]))
 
 
 def test_no_rows():

@@ -106,3 +106,18 @@ def test_verify(lib):
         assert f(**{missing: None}) == 1
     assert f(ks=0) == 1 and f(stride=99) == 1 and f(x=p + 1) == 1 and f(near=p, ns=99) == 1 and f(near=p + 2, ns=100) == 1
     assert f(ws=None) == 3 and f(ws=257) == 3 and f(size=size - 1) == 3
+
+
+def test_verify_outputs_among_inputs(lib):
+    """Each array at a place of its own; then an output at or inside of an input."""
+    names = ("cu", "x", "near", "temperature", "u_next", "tokens", "parent", "u", "keep", "n_keep", "nxt")
+    place = {k: 4096 * (i + 1) for i, k in enumerate(names)}
+
+    def f(**at):
+        a = dict(place, **at)
+        return lib.pcomoe_verify_drafts(1, 10, 100, 2, a["cu"], a["tokens"], a["parent"], a["x"], 100, a["near"], 100, a["temperature"], a["u"], a["u_next"], a["keep"], 4,
+                                        a["n_keep"], a["nxt"], 1 << 20, 4096, None)
+    for out in ("keep", "n_keep", "nxt"):
+        for i in ("cu", "temperature", "u_next", "x", "near"):
+            assert f(**{out: place[i]}) == 1 and f(**{out: place[i] + 4}) == 1, (out, i)
+        assert f(**{out: place["x"] + 3996}) == 1 and f(**{out: place["near"] + 3996}) == 1
