@@ -946,6 +946,8 @@ class DraftVerifier:
         _call(self.gpu, self._lib.pcomoe_verify_drafts, dtype, T, V, n, _ints(cu_len, self.gpu, n + 1), _ints(tokens, self.gpu, T),
               None if parent is None else _ints(parent, self.gpu, T), logits.data_ptr(), row if T > 1 else V, *near,
               None if temperature is None else _f32(temperature, self.gpu, n), _f32(u, self.gpu, T), _f32(u_next, self.gpu, n), *self._out, *self._ws)
+        if n == self.next.numel():
+            return self.keep, self.n_keep, self.next
         return self.keep[:n], self.n_keep[:n], self.next[:n]
 
     def device_status(self) -> int:

@@ -52,9 +52,10 @@ __device__ inline bool alone(const int32_t *seqs, int n, int i, int max_seqs) {
   return !__syncthreads_or(bad);
 }
 
-__device__ inline void drop_pages(const CacheDev &c, int id, int old_len, int new_len) {
+// (by one block, or by several that start and step as far apart)
+__device__ inline void drop_pages(const CacheDev &c, int id, int old_len, int new_len, int start = 0, int step = 0) {
   const int m = min(pages_of(c, old_len), c.max_pages);
-  for (int s = pages_of(c, new_len) + threadIdx.x; s < m; s += blockDim.x) {
+  for (int s = pages_of(c, new_len) + start + threadIdx.x; s < m; s += step ? step : blockDim.x) {
     int32_t *e = &c.table[(int64_t)id * c.max_pages + s];
     if (*e >= 0 && *e < c.pages) atomicSub(&c.ref[*e], 1);
     *e = -1;
