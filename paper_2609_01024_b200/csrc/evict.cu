@@ -2,11 +2,15 @@
 //
 // Three launches.  The first, a cluster of blocks per sequence, finds the weight of the last position that stays by four rounds
 // over its bits (a histogram of 256 bins each, from the top, added over the blocks), lists the places that stay in order, as rows of
-// the pool, and moves the weights.  The second moves the rows: a block owns a column of 64 bytes of one head's rows in one layer, K
+// the pool, with their weights.  The second moves rows and weights: a block owns a column of 64 bytes of one head's rows in one layer, K
 // or V, and walks over them in ascending windows; the places ascend and a row never moves up past itself, so a window only has
 // to be read whole before it is written, and nothing that a later window reads is overwritten: the next window's rows come in
 // while this one's are stored.  The third gives back the pages.
-// What bounds it: the moved rows, read and written once (HBM); few sequences in few layers leave few columns to walk over.
+// What bounds it: the moved rows, read and written once (HBM); few sequences in few layers leave few columns to walk over.  Measured: one
+// sequence of 131071 tokens cut to a quarter in 2 layers of 8 heads of 128, the move 107 us for 492 MB (4.6 TB/s; 128 blocks have a
+// column), the choice 35 us; 8 sequences of 905 to 4050 tokens in 4 layers, the move 51 us, the choice 12.  Columns of 32 bytes took the
+// whole pass over the long sequence from 478 to 508 us, of 128 bytes (half as many blocks) to 524; loads that bring 128 or 256 bytes into
+// L2 583 and 527.
 #include <algorithm>
 
 #include "cache.cuh"
@@ -178,7 +182,7 @@ __global__ void __launch_bounds__(kSelectThreads) evict_select_kernel(CacheDev c
   int32_t *list = ws.list + i * ws.room;
   float *kept = ws.kept + i * ws.room;
   int first = B, bad = 0;
-  // (four steps together, so that the chains weight -> place -> page -> its count run side by side: one long sequence's pass 41 -> XX us)
+  // (four steps together, so that the chains weight -> place -> page -> its count run side by side)
   constexpr int U = 4;
   for (int p = p0; p < p1; p += 32 * U) {
     bool stays[U], tie[U];
@@ -365,7 +369,8 @@ pcomoe_status pcomoe_cache_evict(const pcomoe_cache *cache, int32_t n, const int
   if (columns > INT32_MAX) return PCOMOE_ERR_SHAPE;
   int sms;
   if ((st = current_sms(&sms)) != PCOMOE_OK) return st;
-  // Blocks of a cluster: a sequence may have more than 4096 positions for each, and the GPU two blocks for every SM.
+  // Blocks of a cluster: a sequence may have more than 4096 positions for each, and the GPU two blocks for every SM.  The whole pass with 1, 2, 4
+  // and 8: one sequence of 131071 tokens 608, 536, 497, 478 us; 8 of up to 4050 171, 174, 174, 175.
   int cl = 1;
   while (cl < 8 && w.room > 4096 * cl && (int64_t)n * 2 * cl <= 2 * sms) cl *= 2;
   const cudaStream_t s = (cudaStream_t)stream;
@@ -377,7 +382,7 @@ pcomoe_status pcomoe_cache_evict(const pcomoe_cache *cache, int32_t n, const int
   }
   if (st != PCOMOE_OK) return st;
   // A column each for few blocks is walked over with 512 threads, more of its rows under way; many blocks have 256 (one sequence of 131071
-  // tokens cut to a quarter in 2 layers: the whole pass 492 us, with 256 threads 527; 8 sequences of 905 to 4050 in 4 layers 171, with
+  // tokens cut to a quarter in 2 layers: the whole pass 478 us, with 256 threads 513; 8 sequences of 905 to 4050 in 4 layers 171, with
   // 512 threads 186).
   const dim3 grid((unsigned)columns, 2 * c.layers, n);
   if (columns * 2 * c.layers * n <= 2 * sms) PCOMOE_CUDA_TRY(launch_pdl(evict_move_kernel<512>, grid, dim3(512), 0, s, c, d_seqs, d_weight, weight_stride, w));

@@ -17,7 +17,8 @@
 // After a refusal the sums of max(p - A q, 0) are taken as those of p and q over the words where p > A q: which words these are
 // the sum in 32 bits tells well enough (a word that it takes wrongly lies so near the border that it adds 1e-12 of itself).
 // What bounds them: the rows' one read (HBM) in the first; in the second a chain of dependent steps, since an operation in 64
-// bits takes some 45 clocks until the next one can use it.
+// bits takes some 45 clocks until the next one can use it.  Measured, both together: 32 sequences of 9 rows of 32000 words in bf16 21 us (18
+// MB; the first launch about 8), 8 trees of 17 to 48 rows 18.5, 5 sequences of 1 to 5 rows of 151936 words in fp32 20.6.
 #include <algorithm>
 #include <cfloat>
 #include <type_traits>
