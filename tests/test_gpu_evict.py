@@ -84,6 +84,50 @@ def test_long_sequences():
         check(c, w, [0, 1], [b, 699], 4, 64)
 
 
+def test_many_pages():
+    """More pages are given back than one block has threads, by sequences of very different lengths."""
+    c, w = make("bf16", [30000, 10, 9000, 16400], page=16, layers=1, hkv=1, seed=21)
+    check(c, w, [2, 0, 3, 1], [40, 20, 16399, 0], 4, 8, untouched=(1,))
+    assert w.device_status() == 7               # a budget of 0 leaves no room for 4 + 8
+    held = [t[t >= 0].tolist() for t in c.page_table]
+    assert sorted(sum(held, [])) == c.page_ref.nonzero().flatten().tolist()
+
+
+def test_weights_in_a_wider_array_and_few_listed():
+    """Rows of weights that the caller has, further apart than they are long, and a workspace for two sequences at a time."""
+    c, w0 = make("bf16", [300, 200, 100, 50], seed=22)
+    wide = torch.full((w0.weight.shape[0], w0.weight.shape[1] + 96), 7.0, device="cuda")
+    w = B.CacheWeights(c, q_heads=2, weight=wide[:, 32:32 + w0.weight.shape[1]], max_listed=2)
+    w.weight.copy_(w0.weight)
+    check(c, w, [3, 0], [20, 133], 2, 9)
+    check(c, w, [2, 1], [99, 17], 2, 9)
+    assert w.device_status() == 0 and (wide[:, :32] == 7).all() and (wide[:, -64:] == 7).all()
+    with pytest.raises(AssertionError):
+        w.evict(ints([0, 1, 2]), ints([5, 5, 5]))
+
+
+def test_two_objects_at_once():
+    """Two caches are cut down on two streams at the same time, again and again."""
+    pairs = [make("bf16", [5000, 3000, 0, 700], page=16, layers=2, seed=s) for s in (23, 24)]
+    want = []
+    for c, w in pairs:
+        state = [c.k.clone(), c.v.clone(), w.weight.clone(), c.seq_len.clone(), c.page_ref.clone(), c.page_table.clone()]
+        w.evict(ints([1, 0, 3]), ints([900, 901, 902]), sinks=3, recent=50)
+        want.append((state, [x.clone() for x in (c.k, c.v, w.weight, c.seq_len, c.page_ref, c.page_table)]))
+    seqs, budget = ints([1, 0, 3]), ints([900, 901, 902])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in pairs]
+    for _ in range(5):
+        for st, (c, w), (state, _) in zip(streams, pairs, want):
+            with torch.cuda.stream(st):
+                for x, y in zip((c.k, c.v, w.weight, c.seq_len, c.page_ref, c.page_table), state):
+                    x.copy_(y)
+                w.evict(seqs, budget, sinks=3, recent=50)
+    torch.cuda.synchronize()
+    for (c, w), (_, after) in zip(pairs, want):
+        assert all(torch.equal(x, y) for x, y in zip((c.k, c.v, w.weight, c.seq_len, c.page_ref, c.page_table), after)) and w.device_status() == 0
+
+
 def test_shared_pages():
     """A fork's pages: a sequence that would write into them stays as it is and is reported; one that only gives them back is cut."""
     c, w = make("bf16", [100, 0, 60], seed=6)

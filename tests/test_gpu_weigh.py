@@ -279,3 +279,37 @@ def test_many_rows_bits_and_graph():
             assert torch.equal(c.weights.weight, want)
     side.synchronize()
     assert c.weights.device_status() == 0
+
+
+def test_two_objects_at_once():
+    """Both kernels, on two streams at the same time, give the bits that they give alone."""
+    cases = [Case("bf16", 16, 4, 128, 64, [300, 0], [200, 400], seed=15), Case("bf16", 32, 8, 128, 16, [500, 90, 1300], [1, 4, 2], seed=16), Case("bf16", 8, 8, 64, 16, [70], [500], seed=17),
+             Case("f32", 8, 2, 64, 16, [400, 33], [3, 1], seed=18)]
+    before = [c.weights.weight.clone() for c in cases]
+    want, args = [], []
+    for c in cases:
+        c.add_up()
+        want.append(c.weights.weight.clone())
+        args.append((ints(c.order), ints(c.cu)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(10):
+        for st, c, b, a in zip(streams, cases, before, args):
+            with torch.cuda.stream(st):
+                c.weights.weight.copy_(b)
+                c.weights.add(c.q, c.lse, 0, *a, fresh=True)
+    torch.cuda.synchronize()
+    assert all(torch.equal(c.weights.weight, w) and c.weights.device_status() == 0 for c, w in zip(cases, want))
+
+
+def test_weights_in_a_wider_array_and_few_listed():
+    c = Case("bf16", 8, 2, 128, 16, [100, 60, 40], [2, 120, 1], seed=19, order=[1, 2])
+    before = c.weights.weight.clone()
+    c.add_up()
+    want = c.weights.weight.clone()
+    room = c.weights.weight.shape[1]
+    wide = torch.full((before.shape[0], room + 40), 3.0, device="cuda")
+    w = B.CacheWeights(c.cache, q_heads=8, weight=wide[:, 8:8 + room], max_listed=2)
+    w.weight.copy_(before)
+    w.add(c.q, c.lse, 0, ints(c.order), ints(c.cu), fresh=True)
+    assert torch.equal(w.weight, want) and (wide[:, :8] == 3).all() and (wide[:, 8 + room:] == 3).all() and w.device_status() == 0
