@@ -551,7 +551,8 @@ pcomoe_status run(const CUtensorMap &q_map, const TcArgs &a, int sms, cudaStream
     once.done(dev);
   }
   PCOMOE_CUDA_TRY(launch_pdl(weigh_tc_kernel<D, kBoxes>, dim3(sms), dim3(kThreads), Shape<D>::kSmem, st, q_map, a));
-  const unsigned wide = (unsigned)std::max<int64_t>(1, std::min<int64_t>((a.room + 1023) / 1024, 4 * sms));
+  // a position per thread, while that makes no more than 16 blocks for every SM
+  const unsigned wide = (unsigned)std::min<int64_t>((a.room + 255) / 256, std::max(1, 16 * sms / a.w.n));
   PCOMOE_CUDA_TRY(launch_pdl(weigh_join_kernel, dim3(wide, (unsigned)std::min(a.w.n, 65535)), dim3(256), 0, st, a));
   count_launch(2);
   return PCOMOE_OK;
