@@ -32,6 +32,12 @@ constexpr int kMaxSubs = 16;            // pieces of 16 keys of one head in it
 //   4 sequences of 16384   32.9, 99.1  42.9, 100   73.6, 101    104, 101    133, 93.4  511, 148
 //   8 sequences of 300     10.5, 17.8  13.3, 18.0  18.8, 18.7  24.9, 17.4  31.0, 17.0  105, 22.8
 constexpr int kManyColumns = 96;
+// And in fp32 from this many on:
+//   rows                                         1            4            8            16          32          128
+//   16 sequences of 512                    19.6, 47.6  41.1, 48.2  73.8, 49.3  140, 49.9   272, 80.9  1193, 311
+//   8 sequences of 4096                    41.0, 154   90.4, 155    170, 158   328, 160    643, 264   2534, 970
+//   8 sequences of 300, 8 heads on 2 of 64  8.5, 14.6  10.5, 14.5  12.5, 14.6  18.0, 14.6  28.8, 16.1  92.9, 27.8
+constexpr int kManyColumnsF32 = 32;
 constexpr int kStart = 8;               // cost of a sequence's beginning, in pieces of 16 keys
 constexpr int kExtra = 6;               // cost of a piece of 16 keys besides its columns, in tiles of 8 columns
 
@@ -359,7 +365,7 @@ pcomoe_status check_config(const pcomoe_attn_config *c, const pcomoe_cache *cach
 
 // Workspace: a status word, partial sums of the kernel of many rows.
 size_t workspace_of(const pcomoe_attn_config *c, const pcomoe_cache *cache, int n) {
-  return 256 + (c->dtype == PCOMOE_BF16 ? weigh_tc_bytes(c->kv_heads, (int64_t)cache->max_pages * cache->page_size, n) : 0);
+  return 256 + weigh_part_bytes(c->kv_heads, (int64_t)cache->max_pages * cache->page_size, n);
 }
 
 }  // namespace
@@ -408,9 +414,12 @@ pcomoe_status pcomoe_cache_weigh(const pcomoe_attn_config *cfg, const pcomoe_cac
   a.weight = d_weight; a.weight_stride = weight_stride;
   a.status = (int32_t *)((char *)d_workspace + offsetof(DevPlan, status_router));
   a.limit_ns = wait_limit_ns();
-  // Many counted rows (columns, with the heads of a group) per sequence: the tensor-core kernel.
-  if (cfg->dtype == PCOMOE_BF16 && (int64_t)T * a.g >= (int64_t)kManyColumns * n)
-    return launch_weigh_tc(a, cfg->head_dim, (float *)((char *)d_workspace + 256), (int64_t)cache->max_pages * cache->page_size, sms, (cudaStream_t)stream);
+  // Many counted rows (columns, with the heads of a group) per sequence: the kernels that divide them into tiles.
+  float *partial = (float *)((char *)d_workspace + 256);
+  const int64_t room = (int64_t)cache->max_pages * cache->page_size;
+  if ((int64_t)T * a.g >= (int64_t)(cfg->dtype == PCOMOE_BF16 ? kManyColumns : kManyColumnsF32) * n)
+    return cfg->dtype == PCOMOE_BF16 ? launch_weigh_tc(a, cfg->head_dim, partial, room, sms, (cudaStream_t)stream)
+                                     : launch_weigh_simt(a, cfg->head_dim, partial, room, sms, (cudaStream_t)stream);
   if (cfg->dtype == PCOMOE_BF16) return cfg->head_dim == 64 ? run<__nv_bfloat16, 64>(a, sms, (cudaStream_t)stream) : run<__nv_bfloat16, 128>(a, sms, (cudaStream_t)stream);
   return cfg->head_dim == 64 ? run<float, 64>(a, sms, (cudaStream_t)stream) : run<float, 128>(a, sms, (cudaStream_t)stream);
 }

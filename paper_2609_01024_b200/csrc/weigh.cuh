@@ -22,8 +22,9 @@ struct WeighArgs {
   uint64_t limit_ns;
 };
 
+pcomoe_status launch_weigh_simt(const WeighArgs &a, int head_dim, float *partial, int64_t room, int sms, cudaStream_t st);
 pcomoe_status launch_weigh_tc(const WeighArgs &a, int head_dim, float *partial, int64_t room, int sms, cudaStream_t st);
-size_t weigh_tc_bytes(int hkv, int64_t room, int n);       // of partial sums of n listed sequences of up to `room` positions
+size_t weigh_part_bytes(int hkv, int64_t room, int n);       // of partial sums of n listed sequences of up to `room` positions
 
 #ifdef __CUDACC__
 namespace {

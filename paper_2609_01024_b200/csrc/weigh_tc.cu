@@ -24,7 +24,7 @@
 #include <type_traits>
 
 #include "tc_ptx.cuh"
-#include "weigh.cuh"
+#include "weigh_parts.cuh"
 
 namespace pcomoe {
 namespace {
@@ -39,20 +39,6 @@ template <int D> struct Shape {
   static constexpr int kHalfBytes = 128 * 128;
   static constexpr int kTileBytes = kHalves * kHalfBytes;
   static constexpr int kSmem = kStages * kTileBytes;
-};
-
-struct Unit {
-  WeighSeq seq;
-  int list, head, part;
-  int p0;               // first key; -1: no more work
-  int first, steps;     // column tile of the first step, and their number; tiles are `parts` apart
-};
-
-struct TcArgs {
-  WeighArgs w;
-  float *partial;       // [n][hkv * parts][room]
-  int64_t room;
-  int32_t parts;
 };
 
 __device__ __forceinline__ bool elect_lane() {
@@ -95,64 +81,9 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map
                : "memory");
 }
 
-// The units of a call, in one line: sequence, keys, head and part, the last fastest.  One warp.
-struct Line {
-  int s0;               // sequences s0 + lane are in hand
-  int64_t before;       // units before them
-  WeighSeq mine;
-  int64_t upto;
-  bool held;
-
-  __device__ __forceinline__ void hold(const TcArgs &a, const uint32_t *twice) {
-    const int lane = threadIdx.x & 31;
-    mine = {};
-    if (s0 + lane < a.w.n) mine = weigh_seq(a.w, s0 + lane, twice);
-    upto = (int64_t)((mine.len + BK_ROWS - 1) / BK_ROWS) * (a.w.hkv * a.parts);
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t y = __shfl_up_sync(~0u, upto, o);
-      if (lane >= o) upto += y;
-    }
-    held = true;
-  }
-  // unit u, no smaller than any asked for before
-  __device__ __forceinline__ void get(const TcArgs &a, const uint32_t *twice, int64_t u, Unit &it) {
-    it.p0 = -1;
-    while (s0 < a.w.n) {
-      if (!held) hold(a, twice);
-      const uint32_t hit = __ballot_sync(~0u, before + upto > u);
-      if (hit) {
-        const int l = __ffs(hit) - 1;
-        const int64_t upto_l = __shfl_sync(~0u, upto, l);
-        const int lanes_len = __shfl_sync(~0u, mine.len, l), P = a.w.hkv * a.parts;
-        const int64_t count = (int64_t)((lanes_len + BK_ROWS - 1) / BK_ROWS) * P, at = u - (before + upto_l - count);
-        it.seq.q0 = __shfl_sync(~0u, mine.q0, l);
-        it.seq.n = __shfl_sync(~0u, mine.n, l);
-        it.seq.m = __shfl_sync(~0u, mine.m, l);
-        it.seq.len = lanes_len;
-        it.seq.base = it.seq.len - it.seq.m;
-        it.seq.id = __shfl_sync(~0u, mine.id, l);
-        it.list = s0 + l;
-        const int r = (int)(at % P);
-        it.head = r % a.w.hkv;
-        it.part = r / a.w.hkv;
-        it.p0 = (int)(at / P) * BK_ROWS;
-        const int64_t cols = (int64_t)it.seq.m * a.w.g, from = (int64_t)max(0, it.p0 - it.seq.base) * a.w.g;
-        const int tiles = (int)((cols + BC - 1) / BC);
-        it.first = (int)(from / BC) + it.part;
-        it.steps = max(0, (tiles - it.first + a.parts - 1) / a.parts);
-        return;
-      }
-      before += __shfl_sync(~0u, upto, 31);
-      s0 += 32;
-      held = false;
-    }
-  }
-};
-
 // kBoxes: all packed rows are counted and a tile holds whole rows, so a tile of queries is one box per 64 columns of the head.
 template <int D, bool kBoxes>
-__global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ TcArgs a) {
+__global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_constant__ CUtensorMap q_map, const __grid_constant__ PartArgs a) {
   using S = Shape<D>;
   constexpr uint32_t kIdesc = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
   constexpr int C = D / 8, kSide = 32 / C;                // 16-byte pieces of a row; rows that a warp copies side by side
@@ -501,7 +432,7 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
     }
   } else {
     // ---- the units: from both ends of rounds of the grid's size in turn
-    Line line = {0, 0, {}, 0, false};
+    Line<BK_ROWS, BC> line = {0, 0, {}, 0, false};
     for (uint32_t r = 0;; ++r, ++n_item) {
       Unit it = {};
       line.get(a, twice, (int64_t)r * gridDim.x + (r & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x), it);
@@ -522,27 +453,8 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
   if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
 }
 
-// Partial sums added in order.  blockIdx.y: sequences, a grid's height apart.
-__global__ void __launch_bounds__(256) weigh_join_kernel(const __grid_constant__ TcArgs a) {
-  __shared__ uint32_t s_bits[2 * (kMaxSeqs / 32)];
-  pdl_grid_wait();
-  const uint32_t *twice = find_repeats(a.w.seqs, a.w.n, a.w.max_seqs, s_bits);
-  const int P = a.w.hkv * a.parts;
-  for (int i = blockIdx.y; i < a.w.n; i += gridDim.y) {
-    const WeighSeq s = weigh_seq(a.w, i, twice);
-    float *w = a.w.weight + s.id * a.w.weight_stride;
-    const float *part = a.partial + (int64_t)i * P * a.room;
-    for (int p = blockIdx.x * 256 + threadIdx.x; p < s.len; p += gridDim.x * 256) {
-      float sum = 0.f;
-#pragma unroll 8
-      for (int r = 0; r < P; ++r) sum += part[r * a.room + p];
-      w[p] = a.w.fresh && p >= s.base ? sum : w[p] + sum;
-    }
-  }
-}
-
 template <int D, bool kBoxes>
-pcomoe_status run(const CUtensorMap &q_map, const TcArgs &a, int sms, cudaStream_t st) {
+pcomoe_status run(const CUtensorMap &q_map, const PartArgs &a, int sms, cudaStream_t st) {
   static PerDeviceOnce once;
   int dev = -1;
   PCOMOE_CUDA_TRY(cudaGetDevice(&dev));
@@ -551,22 +463,18 @@ pcomoe_status run(const CUtensorMap &q_map, const TcArgs &a, int sms, cudaStream
     once.done(dev);
   }
   PCOMOE_CUDA_TRY(launch_pdl(weigh_tc_kernel<D, kBoxes>, dim3(sms), dim3(kThreads), Shape<D>::kSmem, st, q_map, a));
-  // a position per thread, while that makes no more than 16 blocks for every SM
-  const unsigned wide = (unsigned)std::min<int64_t>((a.room + 255) / 256, std::max(1, 16 * sms / a.w.n));
-  PCOMOE_CUDA_TRY(launch_pdl(weigh_join_kernel, dim3(wide, (unsigned)std::min(a.w.n, 65535)), dim3(256), 0, st, a));
-  count_launch(2);
+  const pcomoe_status s = launch_join(a, sms, st);
+  if (s != PCOMOE_OK) return s;
+  count_launch();
   return PCOMOE_OK;
 }
 
-// Shares of a head's columns: enough units where there are few heads.
-int parts_of(int hkv) { return hkv >= 8 ? 1 : 8 / hkv; }
-
 }  // namespace
 
-size_t weigh_tc_bytes(int hkv, int64_t room, int n) { return sizeof(float) * (size_t)n * (size_t)(hkv * parts_of(hkv)) * (size_t)room; }
+size_t weigh_part_bytes(int hkv, int64_t room, int n) { return sizeof(float) * (size_t)n * (size_t)(hkv * parts_of(hkv)) * (size_t)room; }
 
 pcomoe_status launch_weigh_tc(const WeighArgs &w, int D, float *partial, int64_t room, int sms, cudaStream_t st) {
-  TcArgs a = {};
+  PartArgs a = {};
   a.w = w;
   a.partial = partial;
   a.room = room;

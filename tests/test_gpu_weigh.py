@@ -313,3 +313,40 @@ def test_weights_in_a_wider_array_and_few_listed():
     w.weight.copy_(before)
     w.add(c.q, c.lse, 0, ints(c.order), ints(c.cu), fresh=True)
     assert torch.equal(w.weight, want) and (wide[:, :8] == 3).all() and (wide[:, 8 + room:] == 3).all() and w.device_status() == 0
+
+
+@pytest.mark.parametrize("hq,hkv,d,page,ctx,add", [(32, 8, 128, 64, [0], [150]), (8, 8, 64, 16, [130, 0, 300], [57, 128, 33]), (28, 4, 128, 32, [5], [80]), (6, 2, 128, 128, [0, 0, 0, 60], [200, 0, 1, 133]),
+                                                   (4, 1, 64, 16, [700], [65]), (7, 1, 128, 64, [0], [300]), (3, 3, 64, 32, [9] * 40, [50] * 39 + [64])])
+def test_many_rows_f32(hq, hkv, d, page, ctx, add):
+    """Tiles of 64 columns and keys that end everywhere, sequences without rows, more sequences than a warp has lanes."""
+    c = Case("f32", hq, hkv, d, page, ctx, add, seed=hq + d, behind=5)
+    c.check()
+    c.check(fresh=False)
+
+
+def test_many_kept_rows_f32():
+    rng = np.random.default_rng(1)
+    kept = [sorted(rng.permutation(200)[:150].tolist()), [], [0, 2], list(range(90))]
+    Case("f32", 8, 2, 128, 32, [40, 30, 0, 100], [200, 3, 3, 90], kept, seed=2, order=[3, 2, 1, 0]).check()
+
+
+def test_many_rows_spoiled_f32():
+    c = Case("f32", 8, 2, 128, 16, [50], [300], seed=13)
+    clean = c.weights.weight.clone()
+    c.add_up()
+    want, c.weights.weight[:] = c.weights.weight.clone(), clean
+    page = lambda p: (0, int(c.cache.page_table[0, p // 16]), 0, p % 16)
+    for p, x in ((7, float("nan")), (349, float("nan")), (200, float("inf"))):
+        c.cache.k[page(p)] = x
+    c.cache.k[(0, int(c.cache.page_table[0, 21]), slice(None), slice(14, None))] = float("nan")      # behind the end
+    c.q[10] = float("nan")                      # a row that saw nothing, whatever it holds
+    c.lse[10] = float("-inf")
+    c.add_up()
+    first, c.weights.weight[:] = c.weights.weight.clone(), clean
+    c.add_up()
+    assert torch.equal(torch.nan_to_num(first, nan=-1.0, posinf=-2.0), torch.nan_to_num(c.weights.weight, nan=-1.0, posinf=-2.0))
+    bad = ~torch.isfinite(first[0])
+    assert bad[[7, 349]].all() and bad.nonzero().flatten().tolist() in ([7, 349], [7, 200, 349])
+    keep = ~bad & (torch.arange(first.shape[1], device="cuda") != 200)
+    # a row less: no more than before at every other position
+    assert (first[0][keep] <= want[0][keep]).all()
