@@ -34,9 +34,9 @@ constexpr int kMaxSubs = 16;            // pieces of 16 keys of one head in it
 constexpr int kManyColumns = 96;
 // And in fp32 from this many on:
 //   rows                                         1            4            8            16          32          128
-//   16 sequences of 512                    19.6, 47.6  41.1, 48.2  73.8, 49.3  140, 49.9   272, 80.9  1193, 311
-//   8 sequences of 4096                    41.0, 154   90.4, 155    170, 158   328, 160    643, 264   2534, 970
-//   8 sequences of 300, 8 heads on 2 of 64  8.5, 14.6  10.5, 14.5  12.5, 14.6  18.0, 14.6  28.8, 16.1  92.9, 27.8
+//   16 sequences of 512                    19.6, 47.3  41.1, 47.3  73.8, 47.6  140, 49.4   272, 78.8  1193, 298
+//   8 sequences of 4096                    41.0, 148   90.4, 148    170, 149   328, 149    643, 255   2534, 935
+//   8 sequences of 300, 8 heads on 2 of 64  8.5, 14.6  10.5, 14.5  12.5, 14.6  18.0, 14.6  28.8, 15.3  92.9, 27.2
 constexpr int kManyColumnsF32 = 32;
 constexpr int kStart = 8;               // cost of a sequence's beginning, in pieces of 16 keys
 constexpr int kExtra = 6;               // cost of a piece of 16 keys besides its columns, in tiles of 8 columns

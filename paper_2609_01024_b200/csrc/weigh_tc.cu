@@ -303,7 +303,13 @@ __global__ void __launch_bounds__(kThreads, 1) weigh_tc_kernel(const __grid_cons
         copy16(dst + row * 128 + (((c & 7) ^ (row & 7)) << 4), (const __nv_bfloat16 *)base + (at < 0 ? 0 : at) + c * 8, at >= 0);
       }
     };
-    for (; item_ready(ok); item_done()) {
+    // The next unit comes when the groups are done with one before it, which may wait for a copy that is not handed on yet (units
+    // without steps lie between).
+    auto next_item = [&]() {
+      if (!__all_sync(~0u, probe_bar(smem_u32(&s_ifull[n_item % kUnits]), (n_item / kUnits) & 1))) flush();
+      return item_ready(ok);
+    };
+    for (; next_item(); item_done()) {
       const Unit it = s_item[n_item % kUnits];
       if (it.p0 < 0) break;
       if (it.steps == 0) continue;

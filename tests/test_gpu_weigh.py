@@ -350,3 +350,14 @@ def test_many_rows_spoiled_f32():
     keep = ~bad & (torch.arange(first.shape[1], device="cuda") != 200)
     # a row less: no more than before at every other position
     assert (first[0][keep] <= want[0][keep]).all()
+
+
+@pytest.mark.parametrize("hq,hkv,d,ctx,add", [(6, 2, 64, [3000, 10, 2500, 700] * 2, [40, 1, 42, 60] * 2), (3, 1, 128, [4000, 3999], [50, 43]), (7, 1, 64, [6000], [20]),
+                                              (6, 2, 64, [1500] * 19, [106, 3, 212] * 6 + [90]), (12, 4, 128, [2000] * 3, [33, 90, 1])])
+def test_units_without_columns(hq, hkv, d, ctx, add):
+    """Few tiles of columns and several shares of them: many units have nothing to do, and the copies of the units around them are still
+    handed on (groups of heads that do not divide a tile)."""
+    c = Case("bf16", hq, hkv, d, 32, ctx, add, seed=len(ctx) + hq)
+    c.check()
+    kept = [list(range(0, a, 1 + i % 2)) for i, a in enumerate(add)]
+    Case("bf16", hq, hkv, d, 32, ctx, add, kept, seed=hq).check()
