@@ -74,8 +74,9 @@ __device__ __forceinline__ double pow2(float x, float m, double c16, float least
   const double w = table[k & (kTable - 1)], r = fma(w, p, w);
   return x < least ? 0.0 : __hiloint2double(__double2hiint(r) + ((k >> 4) << 20), __double2loint(r));
 }
-// the smallest x that pow2 takes; span = 990 / c
-__device__ __forceinline__ float least_of(float m, double span) { return (float)fmax((double)m - span, -(double)FLT_MAX); }
+// the smallest x that pow2 takes; span = 990 / c.  Rounded up: where the steps of fp32 at m are not small beside the span, a value below m - span
+// may have a power that the exponent of 64 bits has no room for.
+__device__ __forceinline__ float least_of(float m, double span) { return __double2float_ru(fmax((double)m - span, -(double)FLT_MAX)); }
 __device__ __forceinline__ void fill_table(double *table) {
   for (int i = threadIdx.x; i < kTable; i += blockDim.x) table[i] = exp2(i * (1.0 / kTable));
 }

@@ -304,3 +304,24 @@ def test_repeated_calls_and_graph():
             graph.replay()
             want = ref.verify(c["x"].double().cpu().numpy(), c["tokens"], c["cu"], u, u_next, None, c["near"], None, 12)
             assert [k[:m] for k, m in zip(out[0].tolist(), out[1].tolist())] == want[0] and out[2].tolist() == want[1]
+
+
+@pytest.mark.parametrize("best", [20.0, 40.0, 100.0, 2000.0, 1e4, -30.0])
+@pytest.mark.parametrize("temperature", [1e-9, 2e-9, 1e-8, 1e-7, 1e-6, 1e-5, 1e-4])
+def test_words_a_few_steps_below_the_best(best, temperature):
+    """Small temperatures, where the steps of fp32 at the largest logit are as far apart as the powers of 2 that 64 bits hold: words 1 to 20 steps below
+    it, as next tokens and as the rest beside a draft that 64 bits decide on."""
+    n, V, best, temperature = 40, 60, np.float32(best), float(np.float32(temperature))
+    below = [best]
+    for _ in range(40):
+        below.append(np.nextafter(below[-1], np.float32(-np.inf)))
+    x = np.full((2 * n, V), best - np.float32(50), np.float32)
+    for r in range(2 * n):
+        x[r, 37] = best
+        x[r, 5] = below[1 + r % 20]
+        if r >= n:
+            x[r, 50] = below[2 * (1 + r % 20)]
+    rng = np.random.default_rng(0)
+    u = np.where(np.arange(2 * n) % 3, np.float32(1 - 2.0 ** -24), rng.random(2 * n)).astype(np.float32)
+    same(dict(x=torch.tensor(x, device="cuda"), tokens=[37] * (2 * n), cu=np.arange(n + 1) * 2, parent=None, near=None, u=u, u_next=rng.random(n).astype(np.float32)),
+         [temperature] * n)
