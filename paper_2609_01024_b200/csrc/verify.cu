@@ -14,8 +14,8 @@
 // drafts (they are numbered behind their parents, so one ascending pass meets every test in order) and reads the row that the walk
 // ended at once more, for the sums of its groups of 512 bytes in 64 bits, from which the group of the next token and in it the token
 // follow.  A test is made in 32 bits first, and in 64, with the row's sum formed again, where it lies within 2^-13 of its border.
-// After a refusal the sums of max(p - A q, 0) are taken as those of p and q over the words where p > A q: which words these are
-// the sum in 32 bits tells well enough (a word that it takes wrongly lies so near the border that it adds 1e-12 of itself).
+// After a refusal of a drawn draft the row's sum is formed in 64 bits before the sums of max(p - A q, 0) are: where the drafter's probabilities are nearly
+// the target's, the rest is made of words so near p = A q that the sum in 32 bits says nothing about them.
 // What bounds them: the rows' one read (HBM) in the first; in the second a chain of dependent steps, since an operation in 64
 // bits takes some 45 clocks until the next one can use it.  Measured, both together: 32 sequences of 9 rows of 32000 words in bf16 21 us (18
 // MB; the first launch about 8), 8 trees of 17 to 48 rows 18.5, 5 sequences of 1 to 5 rows of 151936 words in fp32 20.6.
@@ -98,6 +98,10 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
 
 // 2^((x - m) c) in 32 bits for x <= m, any of them finite (their difference need not be) or x = -inf
 __device__ __forceinline__ float weight_of(float x, float m, float c) { return ex2(fmaxf((0.5f * x - 0.5f * m) * c * 2.f, -1000.f)); }
+
+// max(e - cut q, 0), the same bits wherever it is formed (the compiler may not join the product with the difference): a sum of these is
+// above 0 where one of them is
+__device__ __forceinline__ double rest_of(double e, double cut, double q) { return fmax(__dsub_rn(e, __dmul_rn(cut, q)), 0.0); }
 
 __device__ __forceinline__ float real(float q) { return q > 0.f && q < INFINITY ? q : 0.f; }      // what is no probability counts as 0
 
@@ -334,11 +338,10 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
   // done: the arguments can be read before waiting for it, its sums and the caller's outputs not.
   constexpr int N = Vec<T>::N, kLoads = 16 / N;            // groups of a warp at a time: 16 words of a lane
   extern __shared__ __align__(16) uint8_t smem[];
-  double *s_group = (double *)smem;                        // sums of this block's groups: of 2^(c (x - m)), where p > A q after a refusal
-  double *s_near = s_group + room;                         // and of q there
-  uint8_t *s_out = (uint8_t *)(s_near + room);             // refused words of given drafts, a bit each: a byte per lane and group
+  double *s_group = (double *)smem;                        // sums of this block's groups: of 2^(c (x - m)), or of what is left of it
+  uint8_t *s_out = (uint8_t *)(s_group + room);            // refused words of given drafts, a bit each: a byte per lane and group
   __shared__ double s_table[kTable];
-  __shared__ double s_warp[2][3][kWalkWarps];              // what the warps hand to the cluster, in turn
+  __shared__ double s_warp[2][kWalkWarps];                 // what the warps hand to the cluster, in turn
   __shared__ float s_p[kChunk], s_q[kChunk], s_u[kChunk];
   __shared__ int s_parent[kChunk];
   __shared__ uint8_t s_first[kChunk];                      // the test where a draft is the first at its parent: 1 taken, 2 near its border
@@ -370,10 +373,11 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
   const T *row;
   int shift, groups, per, g0, g1, slot = 0;
 
-  // Sums of row cur's groups, of this block in s_group (and s_near), of every block in every thread.
-  double all_e[CL], all_p[CL], all_q[CL];                  // blocks: of 2^(c (x - m)); of it and of q where p > A q
+  // Sums of row cur's groups, of this block in s_group, of every block in every thread: of e = 2^(c (x - m)), or (rest) of max(e - A s q, 0) with s
+  // the sum of e over the row in 64 bits.
+  double part[CL];
   auto pass = [&](auto rest, bool marked) {
-    sums = a.sums[rows.x + cur];
+    if (!exact) sums = a.sums[rows.x + cur];
     row = row_of<T>(a, rows.x + cur);
     shift = shift_of(row);
     groups = (a.V + shift + 32 * N - 1) / (32 * N);
@@ -383,7 +387,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
     const float m = sums.m, least = least_of(m, span);
     const double cut = A * sums.s;
     const float *near = rest.value ? a.near + (int64_t)(rows.x + cur) * a.near_stride : nullptr;
-    double we = 0.0, wp = 0.0, wq = 0.0;
+    double we = 0.0;
     for (int g = g0 + warp; g < g1; g += kWalkWarps * kLoads) {
       uint4 raw[kLoads];
       float y[kLoads][N];
@@ -419,7 +423,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
             for (int k = 0; k < N; ++k) y[i][k] = there && id + k >= 0 && id + k < a.V ? near[id + k] : 0.f;
         }
       }
-      double e[kLoads][N], ep[kLoads], eq[kLoads];
+      double e[kLoads][N];
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         float x[N];
@@ -430,22 +434,9 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
       }
       if (rest.value) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-          double p[N], q[N];
+        for (int i = 0; i < kLoads; ++i)
 #pragma unroll
-          for (int k = 0; k < N; ++k) {
-            const double z = (double)real(y[i][k]);
-            const bool over = e[i][k] > cut * z;
-            p[k] = over ? e[i][k] : 0.0;
-            q[k] = over ? z : 0.0;
-          }
-#pragma unroll
-          for (int o = 1; o < N; o <<= 1)
-#pragma unroll
-            for (int k = 0; k < N; k += 2 * o) { p[k] += p[k + o]; q[k] += q[k + o]; }
-          ep[i] = p[0];
-          eq[i] = q[0];
-        }
+          for (int k = 0; k < N; ++k) e[i][k] = rest_of(e[i][k], cut, (double)real(y[i][k]));
       }
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
@@ -456,80 +447,55 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
 #pragma unroll
       for (int o = 16; o; o >>= 1)
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-          e[i][0] += __shfl_xor_sync(~0u, e[i][0], o);
-          if (rest.value) {
-            ep[i] += __shfl_xor_sync(~0u, ep[i], o);
-            eq[i] += __shfl_xor_sync(~0u, eq[i], o);
-          }
-        }
+        for (int i = 0; i < kLoads; ++i) e[i][0] += __shfl_xor_sync(~0u, e[i][0], o);
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
         if (g + kWalkWarps * i >= g1) break;
-        if (lane == 0) {
-          s_group[g + kWalkWarps * i - g0] = rest.value ? ep[i] : e[i][0];
-          if (rest.value) s_near[g + kWalkWarps * i - g0] = eq[i];
-        }
+        if (lane == 0) s_group[g + kWalkWarps * i - g0] = e[i][0];
         we += e[i][0];
-        if (rest.value) { wp += ep[i]; wq += eq[i]; }
       }
     }
     slot ^= 1;
-    if (lane == 0) {
-      s_warp[slot][0][warp] = we;
-      if (rest.value) { s_warp[slot][1][warp] = wp; s_warp[slot][2][warp] = wq; }
-    }
+    if (lane == 0) s_warp[slot][warp] = we;
     Cluster<CL>::barrier();                                // (the next pass writes to the other slot, the one after that behind its barrier)
     constexpr int kRounds = (CL + 1) / 2;
-    double v[kRounds][3];
+    double v[kRounds];
 #pragma unroll
-    for (int i = 0; i < kRounds; ++i)
-#pragma unroll
-      for (int k = 0; k < (rest.value ? 3 : 1); ++k) {
-        const double *from = &s_warp[slot][k][lane & 15];
-        if (CL == 1) {
-          v[i][k] = *from;
-        } else {
-          uint32_t q;
-          asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(q) : "r"((uint32_t)__cvta_generic_to_shared(from)), "r"(2 * i + (lane >> 4)));
-          asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v[i][k]) : "r"(q) : "memory");
-        }
+    for (int i = 0; i < kRounds; ++i) {
+      const double *from = &s_warp[slot][lane & 15];
+      if (CL == 1) {
+        v[i] = *from;
+      } else {
+        uint32_t q;
+        asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(q) : "r"((uint32_t)__cvta_generic_to_shared(from)), "r"(2 * i + (lane >> 4)));
+        asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v[i]) : "r"(q) : "memory");
       }
+    }
 #pragma unroll
     for (int o = 8; o; o >>= 1)
 #pragma unroll
-      for (int i = 0; i < kRounds; ++i)
+      for (int i = 0; i < kRounds; ++i) v[i] += __shfl_xor_sync(~0u, v[i], o);
 #pragma unroll
-        for (int k = 0; k < (rest.value ? 3 : 1); ++k) v[i][k] += __shfl_xor_sync(~0u, v[i][k], o);
-#pragma unroll
-    for (int r = 0; r < CL; ++r) {
-      all_e[r] = __shfl_sync(~0u, v[r / 2][0], (r & 1) * 16);
-      if (rest.value) {
-        all_p[r] = __shfl_sync(~0u, v[r / 2][1], (r & 1) * 16);
-        all_q[r] = __shfl_sync(~0u, v[r / 2][2], (r & 1) * 16);
-      }
-    }
+    for (int r = 0; r < CL; ++r) part[r] = __shfl_sync(~0u, v[r / 2], (r & 1) * 16);
   };
-  auto sum_of = [&](const double (&x)[CL]) {
+  auto sum_of_parts = [&]() {
     double s = 0.0;
 #pragma unroll
-    for (int r = 0; r < CL; ++r) s += x[r];
+    for (int r = 0; r < CL; ++r) s += part[r];
     return s;
   };
   // sums.s of row cur in 64 bits
   auto refine = [&]() {
     if (exact) return;
     pass(std::false_type(), false);
-    sums.s = sum_of(all_e);
+    sums.s = sum_of_parts();
     exact = true;
   };
-  // the row's sum and what is left of it after the refusals so far, in units of 2^(c m)
+  // what is left of the row after the refusals so far, in units of 2^(c m)
   auto left_over = [&]() {
+    refine();
     pass(std::true_type(), false);
-    sums.s = sum_of(all_e);
-    exact = true;
-    const double left = sum_of(all_p) - A * sums.s * sum_of(all_q);
-    return left > 0.0 ? left : 0.0;
+    return sum_of_parts();
   };
   // p of a token at row cur, in 64 bits
   auto p_of = [&](int token) {
@@ -681,25 +647,21 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
       }
       __syncthreads();
     }
-    double part[CL], total;                                // what the token is drawn from, block by block
+    double total = 0.0;                                    // what the token is drawn from, block by block in `part`
     if (rest) {
       total = left_over();
-#pragma unroll
-      for (int r = 0; r < CL; ++r) part[r] = fmax(all_p[r] - A * sums.s * all_q[r], 0.0);
       if (!(total > 0.0)) rest = false;                    // nothing is left: the target's own distribution
     }
     if (!rest) {
       pass(std::false_type(), marked);
-      total = sum_of(all_e);
+      total = sum_of_parts();
       if (marked && !(total > 0.0)) {
         marked = false;
         __syncthreads();                                   // the sums are read before they are formed again
         pass(std::false_type(), false);
+        total = sum_of_parts();
       }
-#pragma unroll
-      for (int r = 0; r < CL; ++r) part[r] = all_e[r];
     }
-    total = sum_of(part);
     if (!(total > 0.0)) {
       if (first_block && tid == 0) a.next[seq] = -1;
     } else {
@@ -721,13 +683,12 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
       if (owner == rank && warp == 0) {
         const double goal = target - before, cut = A * sums.s;      // +inf: all of it
         const int mine = g1 - g0, each = (mine + 31) / 32;
-        auto group_at = [&](int i) { return rest ? fmax(s_group[i] - cut * s_near[i], 0.0) : s_group[i]; };
         double sum = 0.0;
         int last = -1;                                     // the last group with any weight
         for (int i = lane * each; i < min((lane + 1) * each, mine); ++i) {
-          const double x = group_at(i);
+          const double x = s_group[i];
           sum += x;
-          if (s_group[i] > 0.0) last = i;                  // (a difference of sums may round to 0)
+          if (x > 0.0) last = i;
         }
         double upto = sum;
 #pragma unroll
@@ -743,7 +704,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
           double base = __shfl_sync(~0u, upto - sum, l);
           int found = -1;
           for (int i = l * each; i < min((l + 1) * each, mine); ++i) {
-            const double x = group_at(i);
+            const double x = s_group[i];
             if (base + x > goal) {
               found = i;
               break;
@@ -766,7 +727,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
 #pragma unroll
         for (int k = 0; k < N; ++k) {
           e[k] = pow2((out >> k) & 1 ? kNone : eligible(x[k]), sums.m, c16, least, s_table);
-          if (rest) e[k] = fmax(e[k] - cut * (double)(id + k >= 0 && id + k < a.V ? real(near[id + k]) : 0.f), 0.0);
+          if (rest) e[k] = rest_of(e[k], cut, id + k >= 0 && id + k < a.V ? (double)real(near[id + k]) : 0.0);
           lane_sum += e[k];
           if (e[k] > 0.0) last_word = id + k;
         }
@@ -792,7 +753,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
   Cluster<CL>::barrier();                                  // nobody leaves while others read its sums
 }
 
-constexpr int kGroupBytes = 8 + 8 + 32;   // of shared memory for each group of a block: two sums, a byte per lane
+constexpr int kGroupBytes = 8 + 32;       // of shared memory for each group of a block: a sum, a byte per lane
 
 template <typename... K, typename... A>
 cudaError_t launch_clusters(void (*kernel)(K...), int items, int cl, int threads, size_t smem, cudaStream_t st, A... args) {

@@ -325,3 +325,65 @@ def test_words_a_few_steps_below_the_best(best, temperature):
     u = np.where(np.arange(2 * n) % 3, np.float32(1 - 2.0 ** -24), rng.random(2 * n)).astype(np.float32)
     same(dict(x=torch.tensor(x, device="cuda"), tokens=[37] * (2 * n), cu=np.arange(n + 1) * 2, parent=None, near=None, u=u, u_next=rng.random(n).astype(np.float32)),
          [temperature] * n)
+
+
+# What 64 bits leave of an exact probability here: 2e-13 of each word's power of 2, the same again for the sum that it is divided by, and a step of
+# 2^-53 for each of some 10^4 additions.  A cumulated sum is off by no more than that altogether.
+P64 = 1e-12
+
+
+def drawn(r, u_next):
+    """The tokens that a sum of r past u_next times all of it may mean, where cumulated sums are off by P64."""
+    total = np.cumsum(r)
+    goal = float(u_next) * total[-1]
+    return [t for t in np.flatnonzero(r > -1) if total[t] >= goal - P64 and (total[t] - r[t]) <= goal + P64 and (r[t] > 0 or total[-1] < P64)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,noise", [(300, 3e-7), (1000, 1e-7), (8000, 3e-7), (8000, 1e-6), (40000, 1e-6)])
+def test_drafter_nearly_the_target(dtype, V, noise):
+    """The drafter's probabilities are the target's but for a few steps of fp32, as those of the same model in another batch: after a refusal the rest
+    is made of these differences alone."""
+    rng = np.random.default_rng(V)
+    n = 40
+    x = torch.tensor(rng.standard_normal((3 * n, V)) * 2).to(TYPES[dtype])
+    temperature = np.where(np.arange(n) % 2, np.float32(0.7), np.float32(1.0))
+    near, tokens = np.zeros((3 * n, V), np.float32), []
+    p = [ref.target(row, float(temperature[r // 3])) for r, row in enumerate(x.double().numpy())]
+    for r in range(3 * n):
+        near[r] = p[r] * (1 + rng.standard_normal(V) * noise)
+    for s in range(n):
+        over = near[3 * s] / p[3 * s]
+        tokens += [0, int(np.argmax(over)), int(rng.choice(V, p=p[3 * s] / p[3 * s].sum()))]       # the first draft is refused
+    u = np.where(np.arange(3 * n) % 3 == 1, np.float32(1 - 2.0 ** -24), rng.random(3 * n)).astype(np.float32)
+    c = dict(x=x.cuda(), tokens=tokens, cu=np.arange(n + 1) * 3, parent=[-1, 0, 0] * n, near=near, u=u, u_next=rng.random(n).astype(np.float32))
+    got, nxt, _, v = run(c, temperature)
+    assert v.device_status() == 0
+    for s in range(n):
+        q = near[3 * s].astype(np.float64)
+        r = np.maximum(p[3 * s] - q, 0)
+        second, R = tokens[3 * s + 2], r.sum()
+        border = abs(float(u[3 * s + 2]) * q[second] * R - r[second])
+        taken = float(u[3 * s + 2]) * q[second] * R < r[second]
+        assert got[s] == ([0, 2] if taken else [0]) or border < P64, (s, got[s], taken)
+        r = p[3 * s + 2] if got[s] == [0, 2] else np.maximum(r - q * R, 0)
+        assert nxt[s] in drawn(r, c["u_next"][s]), (s, nxt[s], got[s], drawn(r, c["u_next"][s]), R)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_last_word_of_the_rest(dtype):
+    """u_next at its end: the last word with a rest, behind which all words lie a step of fp32 below the drafter's."""
+    rng = np.random.default_rng(3)
+    n, V = 300, 4096
+    x = torch.tensor(rng.standard_normal((2 * n, V)) * 3).to(TYPES[dtype])
+    temperature = rng.uniform(0.5, 1.5, n).astype(np.float32)
+    near = np.zeros((2 * n, V), np.float32)
+    for r, row in enumerate(x.double().numpy()):
+        p = ref.target(row, float(temperature[r // 2]))
+        near[r] = np.nextafter(p.astype(np.float32), np.float32(1))
+        near[r, :V // 2] = p[:V // 2] * 0.999
+        near[r, 0] = 2 * p[0]
+    u_next = np.where(np.arange(n) % 2, np.float32(1), np.float32(1 - 2.0 ** -24)).astype(np.float32)
+    c = dict(x=x.cuda(), tokens=[0] * (2 * n), cu=np.arange(n + 1) * 2, parent=None, near=near, u=np.full(2 * n, 1 - 2.0 ** -24, np.float32), u_next=u_next)
+    got, nxt, _ = same(c, temperature)
+    assert all(g == [0] for g in got) and all(t == V // 2 - 1 for t in nxt[1::2])
