@@ -696,24 +696,23 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
           const double y = __shfl_up_sync(~0u, upto, o);
           if (lane >= o) upto += y;
         }
-        const uint32_t past = __ballot_sync(~0u, upto > goal);
+        const uint32_t past = __ballot_sync(~0u, last >= 0 && upto > goal);
         int g = __reduce_max_sync(~0u, last);
         double left = INFINITY;                            // what is to be passed inside of the group
         if (past) {
+          // the first lane whose sum passes the goal.  Added one by one its groups may just not pass it, since the scan adds in another order: the
+          // last word of the lane then.
           const int l = __ffs(past) - 1;
           double base = __shfl_sync(~0u, upto - sum, l);
-          int found = -1;
+          g = __shfl_sync(~0u, last, l);
           for (int i = l * each; i < min((l + 1) * each, mine); ++i) {
             const double x = s_group[i];
-            if (base + x > goal) {
-              found = i;
+            if (x > 0.0 && base + x > goal) {
+              g = i;
+              left = goal - base;
               break;
             }
             base += x;
-          }
-          if (found >= 0) {
-            g = found;
-            left = goal - base;
           }
         }
         float x[N];

@@ -387,3 +387,19 @@ def test_last_word_of_the_rest(dtype):
     c = dict(x=x.cuda(), tokens=[0] * (2 * n), cu=np.arange(n + 1) * 2, parent=None, near=near, u=np.full(2 * n, 1 - 2.0 ** -24, np.float32), u_next=u_next)
     got, nxt, _ = same(c, temperature)
     assert all(g == [0] for g in got) and all(t == V // 2 - 1 for t in nxt[1::2])
+
+
+@pytest.mark.parametrize("dtype,V", [("f32", 8192), ("f32", 16384), ("bf16", 16384), ("bf16", 65536)])
+def test_sums_that_end_between_groups(dtype, V):
+    """Rows of eight equal parts and u_next at eighths: the sum to be passed ends with a part, where only the order of additions tells on which side of it."""
+    rng = np.random.default_rng(V)
+    rows, parts = 30, 8
+    x = np.repeat(np.tile(rng.random((rows, V // parts)) * -3.0, (1, parts)), parts - 1, 0)
+    n = len(x)
+    u_next = np.tile(np.arange(1, parts) / parts, rows).astype(np.float32)
+    c = dict(x=torch.tensor(x).to(TYPES[dtype]).cuda(), tokens=[0] * n, cu=np.arange(n + 1), parent=None, near=None, u=np.zeros(n, np.float32), u_next=u_next)
+    _, nxt, _, _ = run(c)
+    # (the lightest word has 1e-7 of the whole, 64 bits are off by 1e-12)
+    for s, t in enumerate(nxt):
+        end = (1 + s % (parts - 1)) * (V // parts)
+        assert t in (end - 1, end), (s, t, end)
