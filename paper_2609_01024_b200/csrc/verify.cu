@@ -671,7 +671,7 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
       int owner = -1;
 #pragma unroll
       for (int r = 0; r < CL; ++r) {
-        if (owner < 0 && before + part[r] > target) owner = r;
+        if (owner < 0 && part[r] > 0.0 && before + part[r] > target) owner = r;
         if (owner < 0) before += part[r];
       }
       if (owner < 0) {                                     // rounding, or u_next at 1: the last word with any weight

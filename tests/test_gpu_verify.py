@@ -403,3 +403,13 @@ def test_sums_that_end_between_groups(dtype, V):
     for s, t in enumerate(nxt):
         end = (1 + s % (parts - 1)) * (V // parts)
         assert t in (end - 1, end), (s, t, end)
+
+
+@pytest.mark.parametrize("u_next", [-1.0, -1e-30, -0.0, 1.0, 2.0, float("nan"), float("inf"), float("-inf")])
+def test_numbers_outside_of_their_range(u_next):
+    """Where a word is eligible one comes out: -1 says that there is none."""
+    x = np.full((3, 3000), -np.inf)
+    x[:, 1000:2000] = np.random.default_rng(0).standard_normal((3, 1000))
+    c = dict(x=torch.tensor(x, dtype=torch.float32).cuda(), tokens=[0] * 3, cu=np.arange(4), parent=None, near=None, u=np.zeros(3, np.float32), u_next=np.full(3, u_next, np.float32))
+    _, nxt, _, v = run(c)
+    assert all(1000 <= t < 2000 for t in nxt) and v.device_status() == 0
