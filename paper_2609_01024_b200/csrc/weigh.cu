@@ -24,7 +24,8 @@ namespace {
 constexpr int kWarps = 12, kThreads = 32 * kWarps, kKeys = 16;
 constexpr int kItems = 48;              // pieces of 16 keys of a head in a block of keys, about
 constexpr int kMaxSubs = 16;            // pieces of 16 keys of one head in it
-// From this many columns (counted rows x heads of a group) of a sequence on, on average, the tensor-core kernel is taken.  Both, us, with 32
+// From this many columns (counted rows x heads of a group) of a sequence on, on average, the tensor-core kernel is taken.  Of a list the
+// host knows only how many rows it has room for: those are its counted rows here, or all packed rows if they are fewer.  Both, us, with 32
 // heads on 8 of 128 and so many counted rows a sequence (4 columns each), this one and the other:
 //   rows                       1          8           16          24          32          128
 //   64 sequences of 512    21.0, 56.7  30.1, 57.0  51.0, 57.6  74.2, 60.5  96.3, 58.1  392, 103
@@ -417,7 +418,8 @@ pcomoe_status pcomoe_cache_weigh(const pcomoe_attn_config *cfg, const pcomoe_cac
   // Many counted rows (columns, with the heads of a group) per sequence: the kernels that divide them into tiles.
   float *partial = (float *)((char *)d_workspace + 256);
   const int64_t room = (int64_t)cache->max_pages * cache->page_size;
-  if ((int64_t)T * a.g >= (int64_t)(cfg->dtype == PCOMOE_BF16 ? kManyColumns : kManyColumnsF32) * n)
+  const int64_t counted = d_keep ? std::min<int64_t>(T, (int64_t)n * keep_stride) : T;
+  if (counted * a.g >= (int64_t)(cfg->dtype == PCOMOE_BF16 ? kManyColumns : kManyColumnsF32) * n)
     return cfg->dtype == PCOMOE_BF16 ? launch_weigh_tc(a, cfg->head_dim, partial, room, sms, (cudaStream_t)stream)
                                      : launch_weigh_simt(a, cfg->head_dim, partial, room, sms, (cudaStream_t)stream);
   if (cfg->dtype == PCOMOE_BF16) return cfg->head_dim == 64 ? run<__nv_bfloat16, 64>(a, sms, (cudaStream_t)stream) : run<__nv_bfloat16, 128>(a, sms, (cudaStream_t)stream);

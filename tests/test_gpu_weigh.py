@@ -361,3 +361,16 @@ def test_units_without_columns(hq, hkv, d, ctx, add):
     c.check()
     kept = [list(range(0, a, 1 + i % 2)) for i, a in enumerate(add)]
     Case("bf16", hq, hkv, d, 32, ctx, add, kept, seed=hq).check()
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,drafts,kept", [("bf16", 8, 2, 48, 3), ("bf16", 32, 8, 24, 6), ("f32", 8, 2, 9, 2), ("f32", 16, 4, 40, 7), ("bf16", 8, 2, 48, 30), ("f32", 8, 2, 9, 9)])
+def test_kept_rows_of_many_drafts(dtype, hq, hkv, drafts, kept):
+    """The kernel is chosen by the rows that may count, not by the rows that were drafted: one launch where lists of a few rows name them, two (partial
+    sums and their join) from 96 columns a sequence on, in fp32 32."""
+    rng = np.random.default_rng(drafts)
+    lists = [sorted(rng.permutation(drafts)[:int(rng.integers(0, kept + 1))].tolist()) for _ in range(5)] + [list(range(kept))]
+    c = Case(dtype, hq, hkv, 128, 16, [200, 0, 33, 500, 64, 17], [drafts] * 6, lists, seed=kept)
+    c.check()
+    before = B.pcomoe_launch_count()
+    c.add_up()
+    assert B.pcomoe_launch_count() - before == (2 if kept * (hq // hkv) >= (96 if dtype == "bf16" else 32) else 1)
