@@ -21,7 +21,6 @@
 // MB; the first launch about 8), 8 trees of 17 to 48 rows 18.5, 5 sequences of 1 to 5 rows of 151936 words in fp32 20.6.
 #include <algorithm>
 #include <cfloat>
-#include <type_traits>
 
 #include "words.cuh"
 
@@ -60,7 +59,7 @@ constexpr int kMaxGroups = 1040;          // of a block: 2^20 fp32 words over 8 
 
 // 2^((x - m) c) in 64 bits for x <= m.  c16 = 16 c.  The nearest 16th apart, Taylor's series of the rest y / 16, |y| <= 1/2, up to the 5th
 // power (the first term left out is below 2e-13 of the result) and a table of 2^(k/16): 16 entries of 8 bytes lie in as many pairs
-// of banks, so that lanes that ask for different ones do not wait for one another.  0 below 2^-1000 and where x is -inf.
+// of banks, so that lanes that ask for different ones do not wait for one another.  0 below 2^-990 and where x is -inf.
 __device__ __forceinline__ double pow2(float x, float m, double c16, float least, const double *table) {
   const double magic = 6755399441055744.0;                 // 1.5 * 2^52: its last place is 1
   const double d = (double)fmaxf(x, least) - (double)m, t = fma(d, c16, magic);
@@ -325,14 +324,15 @@ __global__ void __launch_bounds__(32 * kSumWarps) row_sums_kernel(const __grid_c
   if (CL > 1) Cluster<CL>::barrier();                      // nobody leaves while others read its box
 }
 
-// The walk and the next token.  CL blocks per sequence.
+// The walk and the next token.  CL blocks per sequence.  kDrawn: there are probabilities that the drafts were drawn from.  (A kernel of its own without
+// them: with the code for what refusals leave in it, walks that never run it took 0.8 us longer.)
 constexpr int kWalkWarps = 16, kWalkThreads = 32 * kWalkWarps, kChunk = kWalkThreads;
 // Whether 32 bits may not decide want < r.  A row's sum is off by at most 2^-14 of itself (20 times 2^-23 from the products' rounding
 // where the words' own logarithms average 20 bits, and a step of 2^-24 for each addition of a lane); `size`: what want and r were formed from.
 __device__ __forceinline__ bool near_border(float want, float r, float size) {
   return !(fabsf(want - r) > (1.f / 8192) * size) || fmaxf(want, r) < 1e-30f;
 }
-template <typename T, int CL>
+template <typename T, int CL, bool kDrawn>
 __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_constant__ VerifyArgs a, int room) {
   // The launch before this one in the stream is row_sums_kernel's, which let this one begin only after all earlier work was
   // done: the arguments can be read before waiting for it, its sums and the caller's outputs not.
@@ -376,7 +376,11 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
   // Sums of row cur's groups, of this block in s_group, of every block in every thread: of e = 2^(c (x - m)), or (rest) of max(e - A s q, 0) with s
   // the sum of e over the row in 64 bits.
   double part[CL];
-  auto pass = [&](auto rest, bool marked) {
+  // (always inlined: a call would put these arrays into local memory)
+  using Words = uint4[kLoads];
+  using Near = float[kLoads][N];
+  using Weights = double[kLoads][N];
+  auto look = [&]() __attribute__((always_inline)) {
     if (!exact) sums = a.sums[rows.x + cur];
     row = row_of<T>(a, rows.x + cur);
     shift = shift_of(row);
@@ -384,80 +388,90 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
     per = (groups + CL - 1) / CL;
     g0 = min(rank * per, groups);
     g1 = min(g0 + per, groups);
-    const float m = sums.m, least = least_of(m, span);
-    const double cut = A * sums.s;
-    const float *near = rest.value ? a.near + (int64_t)(rows.x + cur) * a.near_stride : nullptr;
-    double we = 0.0;
-    for (int g = g0 + warp; g < g1; g += kWalkWarps * kLoads) {
-      uint4 raw[kLoads];
-      float y[kLoads][N];
-      if (g * 32 * N >= shift && (g + kWalkWarps * (kLoads - 1) + 1) * 32 * N - shift <= a.V && g + kWalkWarps * (kLoads - 1) < g1) {
-        const uint4 *p = (const uint4 *)(row - shift) + g * 32 + lane;                  // all inside the row
+  };
+  // the words of groups g, g + kWalkWarps, ..., and q there
+  auto bring = [&](int g, bool rest, Words &raw, Near &y) __attribute__((always_inline)) {
+    const float *near = rest ? a.near + (int64_t)(rows.x + cur) * a.near_stride : nullptr;
+    if (g * 32 * N >= shift && (g + kWalkWarps * (kLoads - 1) + 1) * 32 * N - shift <= a.V && g + kWalkWarps * (kLoads - 1) < g1) {
+      const uint4 *p = (const uint4 *)(row - shift) + g * 32 + lane;                    // all inside the row
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) raw[i] = p[32 * kWalkWarps * i];
-        if (rest.value) {
-          const float *q = near + (g * 32 + lane) * N - shift;
-          if (((uintptr_t)q & 15) == 0) {
+      for (int i = 0; i < kLoads; ++i) raw[i] = p[32 * kWalkWarps * i];
+      if (rest) {
+        const float *q = near + (g * 32 + lane) * N - shift;
+        if (((uintptr_t)q & 15) == 0) {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i)
+          for (int i = 0; i < kLoads; ++i)
 #pragma unroll
-              for (int k = 0; k < N; k += 4) *(float4 *)&y[i][k] = *(const float4 *)(q + 32 * kWalkWarps * N * i + k);
-          } else {
+            for (int k = 0; k < N; k += 4) *(float4 *)&y[i][k] = *(const float4 *)(q + 32 * kWalkWarps * N * i + k);
+        } else {
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i)
+          for (int i = 0; i < kLoads; ++i)
 #pragma unroll
-              for (int k = 0; k < N; ++k) y[i][k] = q[32 * kWalkWarps * N * i + k];
-          }
-        }
-      } else {
-        float none[N];
-#pragma unroll
-        for (int k = 0; k < N; ++k) none[k] = kNone;
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) {
-          const bool there = g + kWalkWarps * i < g1;
-          const int id = ((g + kWalkWarps * i) * 32 + lane) * N - shift;
-          raw[i] = there ? load_raw<T>(row, shift, a.V, g + kWalkWarps * i, lane) : Vec<T>::pack(none);
-          if (rest.value)
-#pragma unroll
-            for (int k = 0; k < N; ++k) y[i][k] = there && id + k >= 0 && id + k < a.V ? near[id + k] : 0.f;
+            for (int k = 0; k < N; ++k) y[i][k] = q[32 * kWalkWarps * N * i + k];
         }
       }
-      double e[kLoads][N];
+    } else {
+      float none[N];
+#pragma unroll
+      for (int k = 0; k < N; ++k) none[k] = kNone;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        float x[N];
-        Vec<T>::unpack(raw[i], x);
-        const uint32_t out = !rest.value && marked && g + kWalkWarps * i < g1 ? s_out[(g + kWalkWarps * i - g0) * 32 + lane] : 0u;
+        const bool there = g + kWalkWarps * i < g1;
+        const int id = ((g + kWalkWarps * i) * 32 + lane) * N - shift;
+        raw[i] = there ? load_raw<T>(row, shift, a.V, g + kWalkWarps * i, lane) : Vec<T>::pack(none);
+        if (rest)
 #pragma unroll
-        for (int k = 0; k < N; ++k) e[i][k] = pow2((out >> k) & 1 ? kNone : eligible(x[k]), m, c16, least, s_table);
-      }
-      if (rest.value) {
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-          for (int k = 0; k < N; ++k) e[i][k] = rest_of(e[i][k], cut, (double)real(y[i][k]));
-      }
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i)
-#pragma unroll
-        for (int o = 1; o < N; o <<= 1)
-#pragma unroll
-          for (int k = 0; k < N; k += 2 * o) e[i][k] += e[i][k + o];
-#pragma unroll
-      for (int o = 16; o; o >>= 1)
-#pragma unroll
-        for (int i = 0; i < kLoads; ++i) e[i][0] += __shfl_xor_sync(~0u, e[i][0], o);
-#pragma unroll
-      for (int i = 0; i < kLoads; ++i) {
-        if (g + kWalkWarps * i >= g1) break;
-        if (lane == 0) s_group[g + kWalkWarps * i - g0] = e[i][0];
-        we += e[i][0];
+          for (int k = 0; k < N; ++k) y[i][k] = there && id + k >= 0 && id + k < a.V ? near[id + k] : 0.f;
       }
     }
+  };
+  auto form = [&](int g, bool marked, const Words &raw, Weights &e) __attribute__((always_inline)) {
+    const float least = least_of(sums.m, span);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      float x[N];
+      Vec<T>::unpack(raw[i], x);
+      const uint32_t out = marked && g + kWalkWarps * i < g1 ? s_out[(g + kWalkWarps * i - g0) * 32 + lane] : 0u;
+#pragma unroll
+      for (int k = 0; k < N; ++k) e[i][k] = pow2((out >> k) & 1 ? kNone : eligible(x[k]), sums.m, c16, least, s_table);
+    }
+  };
+  auto leave = [&](const Near &y, Weights &e) __attribute__((always_inline)) {
+    const double cut = A * sums.s;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+      for (int k = 0; k < N; ++k) e[i][k] = rest_of(e[i][k], cut, (double)real(y[i][k]));
+  };
+  // the groups' sums, to s_group and added to we
+  auto add = [&](int g, const Weights &w, double &we) __attribute__((always_inline)) {
+    Weights e;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+      for (int k = 0; k < N; ++k) e[i][k] = w[i][k];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+      for (int o = 1; o < N; o <<= 1)
+#pragma unroll
+        for (int k = 0; k < N; k += 2 * o) e[i][k] += e[i][k + o];
+#pragma unroll
+    for (int o = 16; o; o >>= 1)
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) e[i][0] += __shfl_xor_sync(~0u, e[i][0], o);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      if (g + kWalkWarps * i >= g1) break;
+      if (lane == 0) s_group[g + kWalkWarps * i - g0] = e[i][0];
+      we += e[i][0];
+    }
+  };
+  // the warps' sums to all of the cluster; returns the row's
+  auto join = [&](double we) __attribute__((always_inline)) {
     slot ^= 1;
     if (lane == 0) s_warp[slot][warp] = we;
-    Cluster<CL>::barrier();                                // (the next pass writes to the other slot, the one after that behind its barrier)
+    Cluster<CL>::barrier();                                // (the next sums go to the other slot, the ones after that behind its barrier)
     constexpr int kRounds = (CL + 1) / 2;
     double v[kRounds];
 #pragma unroll
@@ -475,27 +489,73 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
     for (int o = 8; o; o >>= 1)
 #pragma unroll
       for (int i = 0; i < kRounds; ++i) v[i] += __shfl_xor_sync(~0u, v[i], o);
-#pragma unroll
-    for (int r = 0; r < CL; ++r) part[r] = __shfl_sync(~0u, v[r / 2], (r & 1) * 16);
-  };
-  auto sum_of_parts = [&]() {
     double s = 0.0;
 #pragma unroll
-    for (int r = 0; r < CL; ++r) s += part[r];
+    for (int r = 0; r < CL; ++r) {
+      part[r] = __shfl_sync(~0u, v[r / 2], (r & 1) * 16);
+      s += part[r];
+    }
     return s;
   };
+  // the sums of e; marked: without the words that s_out marks
+  auto pass = [&](bool marked) __attribute__((always_inline)) {
+    look();
+    double we = 0.0;
+    for (int g = g0 + warp; g < g1; g += kWalkWarps * kLoads) {
+      Words raw;
+      Near y;
+      Weights e;
+      bring(g, false, raw, y);
+      form(g, marked, raw, e);
+      add(g, e, we);
+    }
+    return join(we);
+  };
   // sums.s of row cur in 64 bits
-  auto refine = [&]() {
+  auto refine = [&]() __attribute__((always_inline)) {
     if (exact) return;
-    pass(std::false_type(), false);
-    sums.s = sum_of_parts();
+    sums.s = pass(false);
     exact = true;
   };
-  // what is left of the row after the refusals so far, in units of 2^(c m)
-  auto left_over = [&]() {
-    refine();
-    pass(std::true_type(), false);
-    return sum_of_parts();
+  // What is left of row cur after its refusals, in units of 2^(c m), and with it the row's sum in 64 bits.
+  auto left_over = [&]() __attribute__((always_inline)) {
+    look();
+    Words raw;
+    Near y;
+    Weights e;
+    double we = 0.0;
+    if (per <= kWalkWarps * kLoads) {                      // a warp's words stay in registers between the two sums
+      const int g = g0 + warp;
+      if (g < g1) {
+        bring(g, true, raw, y);
+        form(g, false, raw, e);
+      }
+      if (!exact) {
+        if (g < g1) add(g, e, we);
+        sums.s = join(we);
+        exact = true;
+        we = 0.0;
+      }
+      if (g < g1) {
+        leave(y, e);
+        add(g, e, we);
+      }
+      return join(we);
+    }
+    for (;;) {
+      const bool of_rest = exact;
+      we = 0.0;
+      for (int g = g0 + warp; g < g1; g += kWalkWarps * kLoads) {
+        bring(g, true, raw, y);
+        form(g, false, raw, e);
+        if (of_rest) leave(y, e);
+        add(g, e, we);
+      }
+      const double s = join(we);
+      if (of_rest) return s;
+      sums.s = s;
+      exact = true;
+    }
   };
   // p of a token at row cur, in 64 bits
   auto p_of = [&](int token) {
@@ -511,10 +571,10 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
   };
 
   if (rows.y == 1 || a.keep_stride == 1) pdl_grid_wait();
-  for (int c0 = 0; c0 < rows.y && rows.y > 1 && length < a.keep_stride; c0 += kChunk) {
-    // what the tests of the next drafts need: p and q of each one's token at its parent's row, in 32 bits
+  // what the tests of the drafts from `from` on need: p and q of each one's token at its parent's row, in 32 bits
+  auto gather = [&](int from) {
     __syncthreads();
-    const int j = c0 + tid, t = rows.x + j;
+    const int j = from + tid, t = rows.x + j;
     int up = -1, token = -1;
     float x = kNone, q = 1.f, p = 0.f;
     if (j < rows.y && j > 0) {
@@ -526,12 +586,12 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
         up = -1;
       } else {
         x = eligible(Vec<T>::one(row_of<T>(a, rows.x + up) + token));
-        if (a.near) q = real(a.near[(int64_t)(rows.x + up) * a.near_stride + token]);
+        if (kDrawn) q = real(a.near[(int64_t)(rows.x + up) * a.near_stride + token]);
       }
     }
     s_parent[tid] = up;
     s_q[tid] = q;
-    if (c0 == 0) pdl_grid_wait();
+    if (from == 0) pdl_grid_wait();
     if (up >= 0) {
       const RowSums at = a.sums[rows.x + up];
       if (greedy) p = token == at.best ? 1.f : 0.f;
@@ -543,84 +603,89 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
       s_first[tid] = near_border(want, p, want + p) ? 2 : want < p;
     }
     __syncthreads();
-    const int in_chunk = min(kChunk, rows.y - c0);
-    // every warp of every block takes the same way
-    int next = 0;
-    while (length < a.keep_stride) {
-      int hit = kChunk;
-      for (int b = next & ~31; b < in_chunk; b += 32) {
+  };
+  // Every warp of every block takes the same way.
+  int c0 = -kChunk, next = 0;                              // drafts c0 .. c0 + kChunk are at hand, those from c0 + next on still to be tested
+  double left = 0.0;                                       // of the row after the refusals so far, once asked for
+  for (;;) {
+    int hit = kChunk;                                      // the next draft on row cur; kChunk: there is none
+    while (rows.y > 1 && length < a.keep_stride) {
+      for (int b = next & ~31; c0 >= 0 && b < min(kChunk, rows.y - c0); b += 32) {
         const uint32_t m = __ballot_sync(~0u, b + lane >= next && s_parent[b + lane] == cur);
         if (m) {
           hit = b + __ffs(m) - 1;
           break;
         }
       }
-      if (hit == kChunk) break;
-      const bool again = !a.near && refused && named(cur + 1, c0 + hit, a.tokens[rows.x + c0 + hit]);      // a given token that is gone
-      if (due) {
-        double left;
-        if (greedy) {
-          // all of p lies on one word
-          sums = a.sums[rows.x + cur];
-          exact = true;
-          left = sums.best >= 0 ? fmax(1.0 - A * (double)real(a.near[(int64_t)(rows.x + cur) * a.near_stride + sums.best]), 0.0) : 0.0;
-        } else {
-          left = left_over();
-          left = sums.s > 0.0 ? left / sums.s : 0.0;
-        }
-        R = left;
-        due = false;
-        if (!(R > 0.0)) { A = 0.0; R = 1.0; }              // nothing is left: the target's own distribution again
-      }
-      bool taken, close;
-      const float q = s_q[hit], u = s_u[hit];
-      if (!refused) {
-        taken = s_first[hit] & 1;
-        close = s_first[hit] & 2;
-      } else {
-        const float p = s_p[hit], aq = (float)A * q, rr = a.near ? (float)R : 1.f - gone;
-        const float r = again ? 0.f : p - aq, want = u * q * rr;
-        taken = want < r;
-        close = near_border(want, r, u * q * (a.near ? rr : 1.f) + p + aq);
-      }
-      if (close) {                                         // 64 bits give the answer
-        const int token = a.tokens[rows.x + c0 + hit];
-        if (greedy) {
-          sums = a.sums[rows.x + cur];
-          exact = true;
-        }
-        refine();
-        const double p64 = p_of(token), r64 = again ? 0.0 : fmax(p64 - A * (double)q, 0.0);
-        double R64 = R;
-        if (!a.near) {
-          for (int k = cur + 1; k < c0 + hit; ++k) {       // without the refused tokens, each once
-            const int other = a.tokens[rows.x + k];
-            if (parent_of(k) == cur && other >= 0 && other < a.V && !named(cur + 1, k, other)) R64 -= p_of(other);
-          }
-          if (!(R64 > 0.0)) R64 = 1.0;
-        }
-        taken = (double)u * R64 * (double)q < r64;
-      }
-      if (taken) {
-        cur = c0 + hit;
-        if (first_block && tid == 0) a.keep[(int64_t)seq * a.keep_stride + length] = cur;
-        ++length;
-        A = 0.0;
-        R = 1.0;
-        gone = 0.f;
-        refused = 0;
-        due = exact = false;
-      } else {
-        ++refused;
-        if (a.near) {
-          A += R;
-          due = true;
-        } else if (!again) {
-          gone += s_p[hit];
-        }
-      }
-      next = hit + 1;
+      if (hit < kChunk || c0 + kChunk >= rows.y) break;
+      c0 += kChunk;
+      next = 0;
+      gather(c0);
     }
+    // what is left of the row is asked for by the next test, or by the next token
+    if (due) {
+      if (greedy) {
+        // all of p lies on one word
+        sums = a.sums[rows.x + cur];
+        exact = true;
+        left = R = sums.best >= 0 ? fmax(1.0 - A * (double)real(a.near[(int64_t)(rows.x + cur) * a.near_stride + sums.best]), 0.0) : 0.0;
+      } else {
+        left = left_over();
+        R = sums.s > 0.0 ? left / sums.s : 0.0;
+      }
+      due = false;
+      if (!(R > 0.0)) { A = 0.0; R = 1.0; }                // nothing is left: the target's own distribution again
+    }
+    if (hit == kChunk) break;
+    const bool again = !kDrawn && refused && named(cur + 1, c0 + hit, a.tokens[rows.x + c0 + hit]);      // a given token that is gone
+    bool taken, close;
+    const float q = s_q[hit], u = s_u[hit];
+    if (!refused) {
+      taken = s_first[hit] & 1;
+      close = s_first[hit] & 2;
+    } else {
+      const float p = s_p[hit], aq = (float)A * q, rr = kDrawn ? (float)R : 1.f - gone;
+      const float r = again ? 0.f : p - aq, want = u * q * rr;
+      taken = want < r;
+      close = near_border(want, r, u * q * (kDrawn ? rr : 1.f) + p + aq);
+    }
+    if (close) {                                         // 64 bits give the answer
+      const int token = a.tokens[rows.x + c0 + hit];
+      if (greedy) {
+        sums = a.sums[rows.x + cur];
+        exact = true;
+      }
+      refine();
+      const double p64 = p_of(token), r64 = again ? 0.0 : fmax(p64 - A * (double)q, 0.0);
+      double R64 = R;
+      if (!kDrawn) {
+        for (int k = cur + 1; k < c0 + hit; ++k) {       // without the refused tokens, each once
+          const int other = a.tokens[rows.x + k];
+          if (parent_of(k) == cur && other >= 0 && other < a.V && !named(cur + 1, k, other)) R64 -= p_of(other);
+        }
+        if (!(R64 > 0.0)) R64 = 1.0;
+      }
+      taken = (double)u * R64 * (double)q < r64;
+    }
+    if (taken) {
+      cur = c0 + hit;
+      if (first_block && tid == 0) a.keep[(int64_t)seq * a.keep_stride + length] = cur;
+      ++length;
+      A = 0.0;
+      R = 1.0;
+      gone = 0.f;
+      refused = 0;
+      due = exact = false;
+    } else {
+      ++refused;
+      if (kDrawn) {
+        A += R;
+        due = true;
+      } else if (!again) {
+        gone += s_p[hit];
+      }
+    }
+    next = hit + 1;
   }
   if (first_block) {
     if (tid == 0) { a.keep[(int64_t)seq * a.keep_stride] = 0; a.n_keep[seq] = length; }
@@ -631,7 +696,8 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
   if (greedy) {
     if (first_block && tid == 0) a.next[seq] = a.sums[rows.x + cur].best;
   } else {
-    bool rest = a.near && A > 0.0, marked = !a.near && refused > 0;
+    const bool rest = A > 0.0;                             // of drawn drafts; what is left is formed already
+    bool marked = !kDrawn && refused > 0;
     if (marked) {
       row = row_of<T>(a, rows.x + cur);
       shift = shift_of(row);
@@ -647,20 +713,12 @@ __global__ void __launch_bounds__(kWalkThreads, 1) walk_kernel(const __grid_cons
       }
       __syncthreads();
     }
-    double total = 0.0;                                    // what the token is drawn from, block by block in `part`
-    if (rest) {
-      total = left_over();
-      if (!(total > 0.0)) rest = false;                    // nothing is left: the target's own distribution
-    }
-    if (!rest) {
-      pass(std::false_type(), marked);
-      total = sum_of_parts();
-      if (marked && !(total > 0.0)) {
-        marked = false;
-        __syncthreads();                                   // the sums are read before they are formed again
-        pass(std::false_type(), false);
-        total = sum_of_parts();
-      }
+    double total = left;                                   // what the token is drawn from, block by block in `part`
+    while (!rest) {
+      total = pass(marked);
+      if (total > 0.0 || !marked) break;
+      marked = false;                                      // nothing is left: the target's own distribution
+      __syncthreads();                                     // the sums are read before they are formed again
     }
     if (!(total > 0.0)) {
       if (first_block && tid == 0) a.next[seq] = -1;
@@ -780,7 +838,7 @@ pcomoe_status launch_sums(const VerifyArgs &a, cudaStream_t st) {
   return PCOMOE_OK;
 }
 // Whether clusters of 16 blocks find room on the current device, which 8 always do: asked once for each device.
-template <typename T>
+template <typename T, bool kDrawn>
 bool room_for_16() {
   static std::atomic<uint64_t> asked{0}, there{0};
   int dev = -1;
@@ -798,28 +856,40 @@ bool room_for_16() {
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   int clusters = 0;
-  const bool ok = cudaFuncSetAttribute(walk_kernel<T, 16>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
-                  cudaFuncSetAttribute(walk_kernel<T, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxGroups * kGroupBytes) == cudaSuccess &&
-                  cudaOccupancyMaxActiveClusters(&clusters, walk_kernel<T, 16>, &cfg) == cudaSuccess && clusters > 0;
+  const bool ok = cudaFuncSetAttribute(walk_kernel<T, 16, kDrawn>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                  cudaFuncSetAttribute(walk_kernel<T, 16, kDrawn>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxGroups * kGroupBytes) == cudaSuccess &&
+                  cudaOccupancyMaxActiveClusters(&clusters, walk_kernel<T, 16, kDrawn>, &cfg) == cudaSuccess && clusters > 0;
   if (!ok) cudaGetLastError();                             // the answer is no, not an error of a later call
   if (ok) there.fetch_or(bit, std::memory_order_relaxed);
   asked.fetch_or(bit, std::memory_order_release);
   return ok;
 }
 
-template <typename T, int CL>
+template <typename T, int CL, bool kDrawn>
 pcomoe_status launch_walk(const VerifyArgs &a, int groups, cudaStream_t st) {
   const int room = ((groups + CL - 1) / CL + 1) & ~1;
   static PerDeviceOnce once;
   int dev = -1;
   PCOMOE_CUDA_TRY(cudaGetDevice(&dev));
   if (once.first_use(dev)) {
-    PCOMOE_CUDA_TRY(cudaFuncSetAttribute(walk_kernel<T, CL>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxGroups * kGroupBytes));
+    PCOMOE_CUDA_TRY(cudaFuncSetAttribute(walk_kernel<T, CL, kDrawn>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxGroups * kGroupBytes));
     once.done(dev);
   }
-  PCOMOE_CUDA_TRY(launch_clusters(walk_kernel<T, CL>, a.n, CL, kWalkThreads, (size_t)room * kGroupBytes, st, a, room));
+  PCOMOE_CUDA_TRY(launch_clusters(walk_kernel<T, CL, kDrawn>, a.n, CL, kWalkThreads, (size_t)room * kGroupBytes, st, a, room));
   count_launch();
   return PCOMOE_OK;
+}
+
+template <typename T, bool kDrawn>
+pcomoe_status launch_walk(const VerifyArgs &a, int groups, int cl, cudaStream_t st) {
+  if (cl == 16 && !room_for_16<T, kDrawn>()) cl = 8;
+  switch (cl) {
+    case 16: return launch_walk<T, 16, kDrawn>(a, groups, st);
+    case 1: return launch_walk<T, 1, kDrawn>(a, groups, st);
+    case 2: return launch_walk<T, 2, kDrawn>(a, groups, st);
+    case 4: return launch_walk<T, 4, kDrawn>(a, groups, st);
+    default: return launch_walk<T, 8, kDrawn>(a, groups, st);
+  }
 }
 
 template <typename T>
@@ -839,15 +909,8 @@ pcomoe_status run(const VerifyArgs &a, int sms, cudaStream_t st) {
     default: s = launch_sums<T, 8>(a, st); break;
   }
   if (s != PCOMOE_OK) return s;
-  int cl = blocks(a.n, kWalkWarps, 16);
-  if (cl == 16 && !room_for_16<T>()) cl = 8;
-  switch (cl) {
-    case 16: return launch_walk<T, 16>(a, groups, st);
-    case 1: return launch_walk<T, 1>(a, groups, st);
-    case 2: return launch_walk<T, 2>(a, groups, st);
-    case 4: return launch_walk<T, 4>(a, groups, st);
-    default: return launch_walk<T, 8>(a, groups, st);
-  }
+  const int cl = blocks(a.n, kWalkWarps, 16);
+  return a.near ? launch_walk<T, true>(a, groups, cl, st) : launch_walk<T, false>(a, groups, cl, st);
 }
 
 struct Range {                            // of memory; NULL: none
