@@ -525,7 +525,9 @@ pcomoe_status pcomoe_heads_rotate_cached(const pcomoe_rotate_config *cfg, const 
  * the k-th of them sees every position up to its own; with the log sums lse that the attention call left for it,
  *     d_weight[d_seqs[i]][p] += sum over counted rows and query heads of exp(scale q.k_p - lse)     for every p < seq_len.
  * Counted are all packed rows [d_cu_len[i], d_cu_len[i+1]), or, where d_keep is given, those numbered
- * d_keep[i][0 .. d_n_keep[i]) of them: the lists of pcomoe_cache_keep, after that call.
+ * d_keep[i][0 .. d_n_keep[i]) of them: the lists of pcomoe_cache_keep, after that call.  The host sees only keep_stride of how many rows these are,
+ * and chooses the kernel by it: lists no wider than they need be are the faster.  One kernel takes the whole call, by the average of its sequences: single
+ * rows and whole chunks of a prompt are faster in two calls.
  *   fresh        not 0: the counted rows' own positions hold nothing yet and are set, not added to (the first layer of a step)
  *   d_q [T,Hq,D] as in pcomoe_attn_cached, d_lse [T,Hq] fp32; d_keep [n, keep_stride] int32, d_n_keep [n], or both NULL
  *   d_weight     [max_seqs] rows of fp32, weight_stride >= max_pages * page_size elements apart.  Only positions below seq_len
@@ -573,11 +575,12 @@ pcomoe_status pcomoe_cache_evict(const pcomoe_cache *cache, int32_t n, const int
  *   d_draft_probs [T,V] fp32, rows draft_stride apart, or NULL.  Row j is the drafter's distribution behind row j, read only where
  *                a draft hangs on it; what is negative, infinite or NaN counts as 0.  NULL: every draft was given, q is all on it.
  *   d_temperature [n] fp32 or NULL (1); anything but a positive finite number: greedy, p is all on the lowest of the best ids
- *   d_u [T] fp32 in [0, 1), a number per draft (row 0's is not used), d_u_next [n]
+ *   d_u [T] fp32 in [0, 1), a number per draft (row 0's is not used), d_u_next [n]; a word whose probability is below 2^-990 of the best
+ *                one's has none
  *   d_keep [n, keep_stride] int32, d_n_keep [n]: the walk's rows, row 0 first, ready for pcomoe_cache_keep; the rest of d_keep is -1;
  *                a walk ends after keep_stride rows.
  *   d_next [n] int32: -1 where no word is eligible.  A sequence without rows gets n_keep = 0 and next = -1.
- * All that decides a token is formed in 64 bits.  Results are a function of the arguments.  Outputs are no inputs (INVALID_ARG), but
+ * All that decides a token is formed in 64 bits, but for tests that 32 bits decide by more than their error.  Results are a function of the arguments.  Outputs are no inputs (INVALID_ARG), but
  * where all sequences have one row d_tokens, d_parent and d_u may be outputs' (a longer one counts as empty then: INDEX).
  * Workspace: pcomoe_verify_workspace_bytes(T), 256-byte aligned, first 256 bytes zero before the first use, one call at a time.
  * Errors: INVALID_ARG, SHAPE (T < 0, V <= 0, n < 0 or > 65535, keep_stride < 0), UNSUPPORTED (V > 2^20), WORKSPACE, CUDA.

@@ -888,7 +888,8 @@ class CacheWeights:
 
     def add(self, q, lse, layer: int, seqs, cu_len, keep=None, n_keep=None, fresh: bool = False):
         """After Attention.cached or prompt: q [T, q_heads, head_dim] and lse [T, q_heads] of the packed rows, whose keys are the last cached positions
-        of their sequences.  After PagedCache.keep pass its lists, and only the kept rows count.  fresh: this is the first layer of the step."""
+        of their sequences.  After PagedCache.keep pass its lists, and only the kept rows count (no wider
+        than need be: the kernel is chosen by their width).  Decode rows and chunks of prompts are faster in two calls.  fresh: this is the first layer of the step."""
         T, n = q.shape[0], seqs.numel()
         shape, (row, head, one) = q.shape, q.stride()
         assert n <= self.max_listed and shape[1] == self.q_heads and shape[2] == self.cache.head_dim and q.dtype is _TORCH[self.cache.dtype] and one == 1 and \

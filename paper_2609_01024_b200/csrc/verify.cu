@@ -17,8 +17,8 @@
 // After a refusal of a drawn draft the row's sum is formed in 64 bits before the sums of max(p - A q, 0) are: where the drafter's probabilities are nearly
 // the target's, the rest is made of words so near p = A q that the sum in 32 bits says nothing about them.
 // What bounds them: the rows' one read (HBM) in the first; in the second a chain of dependent steps, since an operation in 64
-// bits takes some 45 clocks until the next one can use it.  Measured, both together: 32 sequences of 9 rows of 32000 words in bf16 21 us (18
-// MB; the first launch about 8), 8 trees of 17 to 48 rows 18.5, 5 sequences of 1 to 5 rows of 151936 words in fp32 20.6.
+// bits takes some 45 clocks until the next one can use it.  Measured, both together: 32 sequences of 9 rows of 32000 words in bf16 20.5 us (18
+// MB; the first launch about 8), 8 trees of 17 to 48 rows 18.4, 5 sequences of 1 to 5 rows of 151936 words in fp32 20.5.
 #include <algorithm>
 #include <cfloat>
 

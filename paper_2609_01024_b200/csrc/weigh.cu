@@ -10,7 +10,7 @@
 // warp MMAs (m16n8k16): the order of the inner dimension is free as long as both operands have the same one, and the queries
 // are laid out once per sequence in that order.  All heads of a block of keys are taken by one block of
 // threads and added in order, so nothing is added across blocks and no atomics are needed.  Measured, 32 heads on 8 of 128, bf16: one
-// row of each of 32 sequences of 1 to 4095 tokens (127 MB of keys) 30.8 us, 4.1 TB/s; 4 and 1 rows of two of 131 k and 100 k tokens
+// row of each of 32 sequences of 1 to 4095 tokens (121 MB of keys) 30.8 us, 3.9 TB/s; 4 and 1 rows of two of 131 k and 100 k tokens
 // (473 MB) 86 us, 5.5 TB/s, 0.85 of a plain copy's rate.
 #include <algorithm>
 #include <cmath>

@@ -16,9 +16,10 @@
 // ends of rounds of the grid's size in turn, so that in a prompt, whose later keys are seen by fewer rows, all get about the same
 // work.  (Drawn from a counter as they were finished the units took as long.)
 //
-// What bounds it: the special function unit, 16 exponentials per clock and SM (1024 clocks a step, in which the tensor cores work
+// What bounds it: for the most part the special function unit, 16 exponentials per clock and SM (1024 clocks a step, in which the tensor cores work
 // 512), and in long runs the power limit.  Measured: a prompt of 8192 tokens, 32 heads on 8 of 128, 0.36 ms in runs of a few
-// milliseconds and 0.39 ms in long ones (1.72 GHz at 980 W), 275 GFLOP and 1.07e9 exponentials.  Two groups instead of three took 6 %
+// milliseconds and 0.39 ms in long ones (1.72 GHz at 980 W), 275 GFLOP and 1.07e9 exponentials.  The fullest CTA has 476 steps there (450 on
+// average), so a step takes 1400 to 1500 clocks: some 400 are not the exponentials' and were not taken apart.  Two groups instead of three took 6 %
 // longer; a polynomial on the FMA pipe for a quarter of the exponentials 0.35 ms in short runs and no less in long ones.
 #include <algorithm>
 #include <type_traits>
